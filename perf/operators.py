@@ -367,12 +367,12 @@ def _plain_pages(s):
     rows = torch.arange(BLOCK, device=DEV) < (k["length"][win] % BLOCK)[:, None]
     k["open"][lose] = torch.where(rows[:, None, None, :, None], k["open"][win], k["open"][lose])
     k["held"][lose], k["length"][lose] = full, k["length"][win]
-    # reserve: the lowest free pages, in the order of the list, until one request cannot be met
+    # reserve: the lowest free pages, in the order of the list, until one request cannot be met (later ones get none, but may need none)
     refs[n_pages] = 1
     free = torch.sort((refs != 0).int(), stable=True)[1]
     need = (s["ahead"] // BLOCK - k["held"][every]).clamp(min=0) * (s["ahead"] // BLOCK <= width)
     upto = need.cumsum(0)
-    met = (upto <= (refs[:n_pages] == 0).sum()) & (s["ahead"] // BLOCK <= width)
+    met = ((need == 0) | (upto <= (refs[:n_pages] == 0).sum())) & (s["ahead"] // BLOCK <= width)
     at = col - k["held"][every][:, None]
     gets = (at >= 0) & (at < need[:, None]) & met[:, None]
     page = torch.where(gets, free[((upto - need)[:, None] + at).clamp(0, n_pages)].int(), n_pages)
