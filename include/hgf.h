@@ -39,7 +39,8 @@ typedef enum {
     HGF_ERR_WORKSPACE = 4,         /* workspace missing or smaller than hgf_workspace_bytes() */
     HGF_ERR_CUDA = 5,              /* a CUDA runtime/driver call failed (launch error, no device) */
     HGF_ERR_TIMEOUT = 6,           /* a bounded device-side wait gave up (reported by hgf_check_status) */
-    HGF_ERR_TOO_LARGE = 7          /* the problem needs more scratch than HGF_STATIC_SCRATCH_BYTES */
+    HGF_ERR_TOO_LARGE = 7,         /* the problem needs more scratch than HGF_STATIC_SCRATCH_BYTES */
+    HGF_ERR_CACHE = 8              /* a cache call met an index outside its arrays (reported by hgf_check_status) */
 } hgf_status;
 
 /* flags of hgf_linear_forward / hgf_workspace_bytes */
@@ -355,6 +356,102 @@ hgf_status hgf_diff_attention_forward(const void *q, const void *k, const void *
 double hgf_diff_lambda0(double head_dim);
 
 /*
+ * ---- K/V cache of the differential attention, in 8 bits ------------------------------------------------------
+ * (The paper stops at whole sequences; this is what a decode loop around its attention keeps: K1, K2 and V of the tokens so far.)
+ *
+ * Tokens are kept in blocks of HGF_CACHE_BLOCK.  A complete block is a page: int8 codes with one fp32 scale for each K/V head and each of K1, K2
+ * and V, after the paper's quantiser (Definition "Dynamic Activation Quantization") with the block in place of the token:
+ *     scale = max |x| / 127,   code = Round(127 x / max |x|)   (ties to even, all of it exact but the scale's one rounding to binary32)
+ * over the block's 64 tokens of that head.  A block without a finite maximum has codes 0 and scale NaN; an all-zero block codes 0 and scale 0.
+ * The tokens of a sequence's last, incomplete block stay bfloat16 ("open" rows) until the block is complete: the codes depend on the tokens alone,
+ * not on how many arrived at a time, and no value is quantised twice.
+ *
+ * The caller owns every array; a sequence lives in a slot:
+ *   codes     [n_pages][n_heads][3 * 64 * head_dim]  bytes.  For each head the codes of K1 and of K2, [64 tokens][head_dim], then those of V
+ *             transposed, [head_dim][64 tokens]; each as tiles of 16 rows by 32 columns, 512 bytes, column tiles of a row tile side by side; in a
+ *             tile row 8 a + g and column 16 h + 4 t + b (g < 8, t < 4, b < 4; a, h 0 or 1) are byte (4 g + t) * 16 + 8 h + 4 a + b
+ *   scales    [n_pages][n_heads][4]  fp32: of K1, K2, V, and one unused
+ *   open      [n_slots][n_heads][3][64][head_dim]  bfloat16: rows of K1, K2, V; the eight values 8 e .. 8 e + 7 of row r are stored at 8 (e ^ (r mod 8))
+ *   table     [n_slots][max_pages]  int32: the page of each block
+ *   held      [n_slots]  int32: entries of the table that are pages of this slot
+ *   length    [n_slots]  int32: tokens that it holds (floor(length / 64) of them in pages).  A caller may lower it within the open block (tokens that
+ *             are taken back); lower than that the tokens are no longer there as bfloat16, and the sequence has to be appended anew
+ *   refs      [n_pages]  int32: slots that hold the page; 0 = free
+ *   arrivals  [n_slots]  int32: zero when the cache is made, left at zero by every call
+ * A new cache is zero in held, length, refs and arrivals; the other arrays need no initialisation.
+ *
+ * Everything about the cache is on the device, so a decode loop (reserve ahead of time, then append and attend) can be captured into a graph.
+ * Calls on one cache that write it must be ordered on the device; calls that read it may overlap each other.  Lists name at most
+ * HGF_CACHE_MAX_SEQS slots.  An entry -1 of a list of slots is skipped and its rows are left as they were, as padding in a batch of fixed size.
+ * Slots, pages and row numbers are read on the device, so what is out of range there is skipped and reported by hgf_check_status (HGF_ERR_CACHE).
+ */
+#define HGF_CACHE_BLOCK 64
+#define HGF_CACHE_MAX_SEQS 1024
+typedef struct {
+    void *codes;
+    float *scales;
+    void *open;
+    int32_t *table, *held, *length, *refs, *arrivals;
+    int64_t n_pages, n_slots, max_pages; /* max_pages <= 2^24 */
+    int32_t n_heads, head_dim;           /* K/V heads; 64 or 128 */
+} hgf_cache;
+
+/*
+ * Gives slots the pages they need to grow to tokens[i] tokens: floor(tokens[i] / 64) in all, none are taken away.  The free pages with the lowest
+ * numbers are dealt in the order of the list; the first request that they do not suffice for gets none, nor do later ones that need some.
+ *   slots, tokens  device int32 [n]
+ *   granted        device int32 [n], nullable: 1 where the slot has its pages, else 0 (too few free pages, more than max_pages, a slot named before)
+ */
+hgf_status hgf_cache_reserve(const hgf_cache *cache, const int32_t *slots, const int32_t *tokens, int64_t n, int32_t *granted, void *stream);
+
+/*
+ * Appends tokens to sequences: rows starts[i] .. starts[i + 1] - 1 of k and v to the sequence in slots[i] (any number of rows each, also none).
+ *   k       [n_rows][2 * n_heads * head_dim]  bfloat16 as the K projection writes it: stream 1's heads, then stream 2's
+ *   v       [n_rows][n_heads * head_dim]      bfloat16
+ *   slots   device int32 [n_seqs];  starts  device int32 [n_seqs + 1], ascending, up to n_rows
+ *   done    device int32 [n_seqs], nullable: 1 where the rows were appended, 0 where they were not and the sequence is as it was - its pages do not
+ *           suffice (hgf_cache_reserve), one of them is shared, the slot is -1 or was named before in the list
+ */
+hgf_status hgf_cache_append(const hgf_cache *cache, const void *k, const void *v, int64_t n_rows, const int32_t *slots, const int32_t *starts,
+                            int64_t n_seqs, int32_t *done, void *stream);
+
+/*
+ * Reads tokens back as values, code * scale (the inverse of the append up to the rounding of the codes): tokens first[i], first[i] + 1, ... of the
+ * sequence in slots[i] become rows starts[i] .. starts[i + 1] - 1.  Rows of tokens that the sequence does not hold are left as they were.
+ *   k_out  [n_rows][2 * n_heads * head_dim], v_out [n_rows][n_heads * head_dim]: fp32, or bfloat16 with HGF_FLAG_OUT_BF16
+ */
+hgf_status hgf_cache_read(const hgf_cache *cache, const int32_t *slots, const int32_t *first, const int32_t *starts, int64_t n_seqs, int64_t n_rows,
+                          void *k_out, void *v_out, uint32_t flags, void *stream);
+
+/*
+ * Makes dst[i] a copy of the sequence in src[i]: the pages of its complete blocks are shared (refs), its open rows copied.  Pages that src holds
+ * ahead of its length stay its own.  dst[i] must be empty (length and held 0), named once, and not also a src of the list.
+ *   src, dst  device int32 [n];  done  device int32 [n], nullable: 1 where the copy was made, 0 where it was not and dst[i] is as it was
+ */
+hgf_status hgf_cache_fork(const hgf_cache *cache, const int32_t *src, const int32_t *dst, int64_t n, int32_t *done, void *stream);
+
+/* Empties slots: their pages are given back (free once no other slot holds them), held and length become 0.  A slot named twice is emptied once. */
+hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slots, int64_t n, void *stream);
+
+/*
+ * Causal differential attention of new tokens over cached ones:
+ *     O = ( Softmax(Q1 K1^T / sqrt(d_h)) - lambda * Softmax(Q2 K2^T / sqrt(d_h)) ) V * out_scale
+ * with K1, K2, V the values that the cache stands for.  Rows starts[i] .. starts[i + 1] - 1 of q are the LAST tokens that the sequence in slots[i]
+ * holds (append them first): with m rows and length L, row j attends to tokens 0 .. L - m + j.  A row that sees no token (L = 0, or more rows than
+ * tokens) is zero.  Decoding has one row a sequence; drafts that are verified and pieces of a prompt have more.
+ *   q    [n_rows][2 * n_heads * head_dim]  bfloat16: stream 1's heads, then stream 2's.  n_heads is a multiple of cache->n_heads: each
+ *        n_heads / cache->n_heads neighbouring heads share a K/V head
+ *   out  [n_rows][n_heads * head_dim]      fp32, or bfloat16 with HGF_FLAG_OUT_BF16
+ *   workspace  hgf_cached_workspace_bytes(...) bytes, 256-byte aligned; scratch, which calls that may overlap on the device do not share
+ * Scores come from q to 2^-22 of the row's largest magnitude, probabilities enter the second product to 2^-24, all sums are exact integers or fp32.
+ * A query row or a visible block with a value that is not finite gives outputs that are not finite.
+ */
+size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads);
+hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const void *q, int64_t n_rows, int32_t n_heads, const int32_t *slots,
+                                     const int32_t *starts, int64_t n_seqs, float lambda, float out_scale, void *out, void *workspace,
+                                     size_t workspace_bytes, uint32_t flags, void *stream);
+
+/*
  * Straight-through backward pass of the layer (paper, Section 2.2, Definition "Straight-Through
  * Estimator"): the forward pass of hgf_linear_forward is differentiated with both quantisers treated
  * as the identity (every activation lies inside its clipping range; the weight gradient is passed
@@ -391,6 +488,7 @@ hgf_status hgf_linear_backward(const void *x, int64_t M, const void *packed, flo
  * Device-side waits are bounded; when one gives up the kernel records it and returns.  This call
  * synchronises `stream`, reads and clears that record, and returns HGF_ERR_TIMEOUT if a wait gave up
  * since the last check (HGF_OK otherwise).  Outputs and workspaces of the calls since are undefined then.
+ * HGF_ERR_CACHE: no wait gave up, but a cache call met a slot, page, length or row number outside its arrays and skipped it.
  */
 hgf_status hgf_check_status(void *stream);
 

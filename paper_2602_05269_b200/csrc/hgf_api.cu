@@ -7,6 +7,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "hgf_cache.cuh"
 #include "hgf_common.cuh"
 
 namespace hgf {
@@ -840,7 +841,7 @@ extern "C" hgf_status hgf_check_status(void *stream) {
     if (v) {
         unsigned int zero = 0;
         cudaMemcpy(w, &zero, sizeof zero, cudaMemcpyHostToDevice);
-        return HGF_ERR_TIMEOUT;
+        return v == kStatusCache ? HGF_ERR_CACHE : HGF_ERR_TIMEOUT;
     }
     return HGF_OK;
 }
@@ -866,6 +867,7 @@ extern "C" const char *hgf_status_string(hgf_status s) {
         case HGF_ERR_CUDA: return "CUDA error";
         case HGF_ERR_TIMEOUT: return "a bounded device-side wait gave up";
         case HGF_ERR_TOO_LARGE: return "the problem needs more scratch than the library's built-in array holds";
+        case HGF_ERR_CACHE: return "a cache call met an index outside its arrays";
     }
     return "unknown status";
 }

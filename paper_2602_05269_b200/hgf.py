@@ -6,6 +6,7 @@ library's kernels.  If the library is missing, or a call fails, this raises: the
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.machinery
 import importlib.util
@@ -37,7 +38,9 @@ EXPORTS = ["hgf_packed_bytes", "hgf_pack_ternary", "hgf_unpack_ternary", "hgf_wo
            "hgf_linear_forward_phases", "hgf_linear_forward_ln",
            "hgf_packed_bytes_b3", "hgf_pack_ternary_b3", "hgf_unpack_ternary_b3",
            "hgf_selftest_wait_timeout", "hgf_group_create_ln",
-           "hgf_diff_attention_forward", "hgf_diff_lambda0", "hgf_backward_workspace_bytes", "hgf_linear_backward"]
+           "hgf_diff_attention_forward", "hgf_diff_lambda0", "hgf_backward_workspace_bytes", "hgf_linear_backward",
+           "hgf_cache_reserve", "hgf_cache_append", "hgf_cache_read", "hgf_cache_fork", "hgf_cache_free",
+           "hgf_cached_workspace_bytes", "hgf_diff_attention_cached"]
 
 
 class HgfError(RuntimeError):
@@ -61,6 +64,13 @@ class DebugOut(ctypes.Structure):
 class Grads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dW", ctypes.c_void_p), ("dAt", ctypes.c_void_p), ("dBt", ctypes.c_void_p),
                 ("dgate", ctypes.c_void_p)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("open", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("held", ctypes.c_void_p), ("length", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("arrivals", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("n_slots", ctypes.c_int64), ("max_pages", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class FrontEnd(ctypes.Structure):
@@ -119,6 +129,21 @@ def lib() -> ctypes.CDLL:
         L.hgf_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
         L.hgf_linear_backward.restype = c.c_int
         L.hgf_linear_backward.argtypes = [vp, i64, vp, c.c_float, i64, i64, vp, vp, i32, vp, vp, c.POINTER(Grads), vp, sz, u32, vp]
+        cache = c.POINTER(Cache)
+        L.hgf_cache_reserve.restype = c.c_int
+        L.hgf_cache_reserve.argtypes = [cache, vp, vp, i64, vp, vp]
+        L.hgf_cache_append.restype = c.c_int
+        L.hgf_cache_append.argtypes = [cache, vp, vp, i64, vp, vp, i64, vp, vp]
+        L.hgf_cache_read.restype = c.c_int
+        L.hgf_cache_read.argtypes = [cache, vp, vp, vp, i64, i64, vp, vp, u32, vp]
+        L.hgf_cache_fork.restype = c.c_int
+        L.hgf_cache_fork.argtypes = [cache, vp, vp, i64, vp, vp]
+        L.hgf_cache_free.restype = c.c_int
+        L.hgf_cache_free.argtypes = [cache, vp, i64, vp]
+        L.hgf_cached_workspace_bytes.restype = sz
+        L.hgf_cached_workspace_bytes.argtypes = [cache, i64, i64, i32]
+        L.hgf_diff_attention_cached.restype = c.c_int
+        L.hgf_diff_attention_cached.argtypes = [cache, vp, i64, i32, vp, vp, i64, c.c_float, c.c_float, vp, vp, sz, u32, vp]
         L.hgf_check_status.restype = c.c_int
         L.hgf_check_status.argtypes = [vp]
         L.hgf_tmax_tokens_per_s.restype = c.c_double
@@ -422,6 +447,144 @@ def diff_attention_forward(q, k, v, B: int, L: int, n_heads: int, head_dim: int,
     _check("hgf_diff_attention_forward",
            lib().hgf_diff_attention_forward(_ptr(q), _ptr(k), _ptr(v), B, L, n_heads, head_dim, ctypes.c_float(lam),
                                             ctypes.c_float(out_scale), _ptr(out), flags, _stream(stream)))
+    return out
+
+
+CACHE_BLOCK = 64
+CACHE_MAX_SEQS = 1024
+
+
+class KVCache:
+    """The arrays of an hgf_cache (8-bit paged K/V cache of the differential attention): `n_slots` sequences of up to
+    64 * max_pages + 63 tokens, in `n_pages` pages of 64 tokens, for `n_heads` K/V heads.  The arrays are attributes (codes, scales, open, table,
+    held, length, refs, arrivals) on one device; KVCache.of takes ones that exist already."""
+
+    _SHAPES = {"codes": (torch.int8, lambda c: (c.n_pages, c.n_heads, 3 * CACHE_BLOCK * c.head_dim)), "scales": (torch.float32, lambda c: (c.n_pages, c.n_heads, 4)),
+               "open": (torch.bfloat16, lambda c: (c.n_slots, c.n_heads, 3, CACHE_BLOCK, c.head_dim)), "table": (torch.int32, lambda c: (c.n_slots, c.max_pages)),
+               "held": (torch.int32, lambda c: (c.n_slots,)), "length": (torch.int32, lambda c: (c.n_slots,)), "refs": (torch.int32, lambda c: (c.n_pages,)),
+               "arrivals": (torch.int32, lambda c: (c.n_slots,))}
+
+    def __init__(self, n_heads: int, head_dim: int, n_pages: int, n_slots: int, max_pages: int, device="cuda"):
+        self.n_heads, self.head_dim, self.n_pages, self.n_slots, self.max_pages = n_heads, head_dim, n_pages, n_slots, max_pages
+        self._bind({name: torch.zeros(shape(self), dtype=dtype, device=device) for name, (dtype, shape) in self._SHAPES.items()})
+
+    @classmethod
+    def of(cls, n_heads: int, head_dim: int, **arrays):
+        """A cache on arrays that exist: every one of codes, scales, open, table, held, length, refs, arrivals."""
+        self = cls.__new__(cls)
+        self.n_heads, self.head_dim = n_heads, head_dim
+        self.n_pages = arrays["codes"].shape[0]
+        self.n_slots, self.max_pages = arrays["table"].shape
+        self._bind(arrays)
+        return self
+
+    def _bind(self, arrays):
+        assert set(arrays) == set(self._SHAPES), "the arrays of a cache are " + ", ".join(self._SHAPES)
+        for name, (dtype, shape) in self._SHAPES.items():
+            a = arrays[name]
+            assert a.dtype == dtype and tuple(a.shape) == shape(self) and a.is_contiguous() and a.device == arrays["codes"].device, f"cache array {name}"
+            setattr(self, name, a)
+        self.device = self.codes.device
+        self._struct = Cache(*(arrays[n].data_ptr() for n in self._SHAPES), self.n_pages, self.n_slots, self.max_pages, self.n_heads, self.head_dim)
+        self._ref = ctypes.byref(self._struct)
+
+
+def _on(stream):
+    """What a cache call makes for itself is made on the stream that the call runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _list(cache, *tensors):
+    """The lists of a cache call: int32 on the cache's device, dense."""
+    for a in tensors:
+        assert a is None or (a.dtype == torch.int32 and a.device == cache.device and a.is_contiguous() and a.dim() == 1), "lists of a cache call are dense int32 on its device"
+
+
+def cache_reserve(cache: KVCache, slots, tokens, *, granted=None, stream=None):
+    """hgf_cache_reserve: pages for slots[i] to grow to tokens[i] tokens.  Returns `granted` (int32 [n], made here if not given): 1 where it has them."""
+    _list(cache, slots, tokens, granted)
+    n = slots.numel()
+    if granted is None:
+        with _on(stream):
+            granted = torch.empty(n, dtype=torch.int32, device=cache.device)
+    assert tokens.numel() == n and granted.numel() == n
+    _check("hgf_cache_reserve", lib().hgf_cache_reserve(cache._ref, _ptr(slots), _ptr(tokens), n, _ptr(granted), _stream(stream)))
+    return granted
+
+
+def cache_append(cache: KVCache, k, v, slots, starts, *, done=None, stream=None):
+    """hgf_cache_append: rows starts[i] .. starts[i + 1] - 1 of k (bf16 [n_rows][2 * n_heads * head_dim]) and v (bf16 [n_rows][n_heads * head_dim])
+    to the sequence in slots[i].  Returns `done` (int32 [n_seqs], made here if not given): 1 where they were appended."""
+    _list(cache, slots, starts, done)
+    n, width = slots.numel(), cache.n_heads * cache.head_dim
+    assert k.device == v.device == cache.device and k.dtype == v.dtype == torch.bfloat16 and k.is_contiguous() and v.is_contiguous()
+    assert k.dim() == 2 and k.shape[1] == 2 * width and v.shape == (k.shape[0], width) and starts.numel() == n + 1
+    if done is None:
+        with _on(stream):
+            done = torch.empty(n, dtype=torch.int32, device=cache.device)
+    assert done.numel() == n
+    _check("hgf_cache_append", lib().hgf_cache_append(cache._ref, _ptr(k), _ptr(v), k.shape[0], _ptr(slots), _ptr(starts), n, _ptr(done), _stream(stream)))
+    return done
+
+
+def cache_read(cache: KVCache, slots, first, starts, n_rows: int | None = None, *, k=None, v=None, flags: int = 0, stream=None):
+    """hgf_cache_read: tokens first[i], first[i] + 1, ... of the sequence in slots[i] as rows starts[i] .. starts[i + 1] - 1 of (k, v): fp32, or bf16
+    with FLAG_OUT_BF16.  Without k and v, `n_rows` rows are made here, zero where nothing is read."""
+    _list(cache, slots, first, starts)
+    n, width = slots.numel(), cache.n_heads * cache.head_dim
+    if k is None:
+        dtype = torch.bfloat16 if flags & FLAG_OUT_BF16 else torch.float32
+        with _on(stream):
+            k, v = (torch.zeros((n_rows, w), dtype=dtype, device=cache.device) for w in (2 * width, width))
+    elif k.dtype == torch.bfloat16:
+        flags |= FLAG_OUT_BF16
+    assert k.device == v.device == cache.device and k.is_contiguous() and v.is_contiguous()
+    assert k.dtype == v.dtype == (torch.bfloat16 if flags & FLAG_OUT_BF16 else torch.float32)
+    assert k.dim() == 2 and k.shape[1] == 2 * width and v.shape == (k.shape[0], width) and starts.numel() == n + 1 and first.numel() == n
+    _check("hgf_cache_read",
+           lib().hgf_cache_read(cache._ref, _ptr(slots), _ptr(first), _ptr(starts), n, k.shape[0], _ptr(k), _ptr(v), flags, _stream(stream)))
+    return k, v
+
+
+def cache_fork(cache: KVCache, src, dst, *, done=None, stream=None):
+    """hgf_cache_fork: the empty slot dst[i] becomes a copy of the sequence in src[i].  Returns `done` (int32 [n]; made here if not given)."""
+    _list(cache, src, dst, done)
+    n = src.numel()
+    if done is None:
+        with _on(stream):
+            done = torch.empty(n, dtype=torch.int32, device=cache.device)
+    assert dst.numel() == n and done.numel() == n
+    _check("hgf_cache_fork", lib().hgf_cache_fork(cache._ref, _ptr(src), _ptr(dst), n, _ptr(done), _stream(stream)))
+    return done
+
+
+def cache_free(cache: KVCache, slots, *, stream=None) -> None:
+    """hgf_cache_free: empties the slots and gives their pages back."""
+    _list(cache, slots)
+    _check("hgf_cache_free", lib().hgf_cache_free(cache._ref, _ptr(slots), slots.numel(), _stream(stream)))
+
+
+def cached_workspace_bytes(cache: KVCache, n_seqs: int, n_rows: int, n_heads: int) -> int:
+    return int(lib().hgf_cached_workspace_bytes(cache._ref, n_seqs, n_rows, n_heads))
+
+
+def diff_attention_cached(cache: KVCache, q, slots, starts, lam: float, out_scale: float = 1.0, *, out=None, workspace=None, flags: int = 0,
+                          stream=None):
+    """hgf_diff_attention_cached: rows starts[i] .. starts[i + 1] - 1 of q (bf16 [n_rows][2 * n_heads * head_dim]), the last tokens of the sequence
+    in slots[i], attend to what the cache holds of it -> out [n_rows][n_heads * head_dim], fp32 (bf16 with FLAG_OUT_BF16)."""
+    _list(cache, slots, starts)
+    n, rows = slots.numel(), q.shape[0]
+    heads = q.shape[1] // (2 * cache.head_dim)
+    assert q.device == cache.device and q.dtype == torch.bfloat16 and q.is_contiguous() and q.shape[1] == 2 * heads * cache.head_dim and starts.numel() == n + 1
+    dtype = torch.bfloat16 if flags & FLAG_OUT_BF16 else torch.float32
+    if out is None or workspace is None:
+        with _on(stream):
+            out = torch.empty((rows, heads * cache.head_dim), dtype=dtype, device=q.device) if out is None else out
+            workspace = torch.empty(cached_workspace_bytes(cache, n, rows, heads), dtype=torch.uint8, device=q.device) if workspace is None else workspace
+    assert out.dtype == dtype and out.is_contiguous() and out.shape == (rows, heads * cache.head_dim)
+    _check("hgf_diff_attention_cached",
+           lib().hgf_diff_attention_cached(cache._ref, _ptr(q), rows, heads, _ptr(slots), _ptr(starts), n, lam, out_scale, _ptr(out), _ptr(workspace),
+                                           workspace.numel(), flags, _stream(stream)))
     return out
 
 
