@@ -1,4 +1,4 @@
-"""Thin binding of libhgf_b200.so: same names as the C ABI, argument marshalling only (ctypes; linear_forward, the call whose GPU time
+"""Thin binding of libhgf_b200.so: same names as the C ABI, argument marshalling only (ctypes; linear_forward and the cache calls, whose GPU time
 can be shorter than that, through the native module _hgf_python, csrc/hgf_python.cpp, where that loads and for the arguments that it takes).
 
 Tensors are torch CUDA tensors used purely as device memory; every step of the layer runs in the
@@ -80,11 +80,12 @@ class FrontEnd(ctypes.Structure):
 
 _lib = None
 _native_forward = None  # linear_forward's marshalling (set with _lib; None: ctypes)
+_native_cache = None    # the native module, for the cache calls' (likewise)
 
 
 def lib() -> ctypes.CDLL:
     """Load the CUDA library (built in-tree by paper_2602_05269_b200.build)."""
-    global _lib, _native_forward
+    global _lib, _native_forward, _native_cache
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_2602_05269_b200.build` "
@@ -168,6 +169,9 @@ def lib() -> ctypes.CDLL:
         if native is not None:
             native.bind(c.cast(L.hgf_linear_forward, vp).value, c.cast(L.hgf_linear_forward_ln, vp).value)
             _native_forward = native.linear_forward
+            native.bind_cache(*(c.cast(f, vp).value for f in (L.hgf_cache_reserve, L.hgf_cache_append, L.hgf_cache_read, L.hgf_cache_fork, L.hgf_cache_free,
+                                                              L.hgf_diff_attention_cached)))
+            _native_cache = native
         _lib = L
     return _lib
 
@@ -485,8 +489,11 @@ class KVCache:
             assert a.dtype == dtype and tuple(a.shape) == shape(self) and a.is_contiguous() and a.device == arrays["codes"].device, f"cache array {name}"
             setattr(self, name, a)
         self.device = self.codes.device
+        self._index = self.device.index if self.device.type == "cuda" else -1
         self._struct = Cache(*(arrays[n].data_ptr() for n in self._SHAPES), self.n_pages, self.n_slots, self.max_pages, self.n_heads, self.head_dim)
         self._ref = ctypes.byref(self._struct)
+        self._at = ctypes.addressof(self._struct)
+        lib()
 
 
 def _on(stream):
@@ -494,14 +501,24 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _done(call, status) -> bool:
+    """What a native cache call returned: done, refused, or (-1) not taken, so that the checks here say why."""
+    if status > 0:
+        raise HgfError(call, status)
+    return status == 0
+
+
 def _list(cache, *tensors):
-    """The lists of a cache call: int32 on the cache's device, dense."""
+    """The lists of a cache call: int32 on the cache's device, which has to be the current one, dense."""
+    assert cache.device.type == "cuda" and cache.device.index == torch.cuda.current_device(), f"the cache is on {cache.device}, which is not the current device"
     for a in tensors:
         assert a is None or (a.dtype == torch.int32 and a.device == cache.device and a.is_contiguous() and a.dim() == 1), "lists of a cache call are dense int32 on its device"
 
 
 def cache_reserve(cache: KVCache, slots, tokens, *, granted=None, stream=None):
     """hgf_cache_reserve: pages for slots[i] to grow to tokens[i] tokens.  Returns `granted` (int32 [n], made here if not given): 1 where it has them."""
+    if granted is not None and _native_cache and _done("hgf_cache_reserve", _native_cache.cache_reserve(cache._at, cache._index, slots, tokens, granted, stream)):
+        return granted
     _list(cache, slots, tokens, granted)
     n = slots.numel()
     if granted is None:
@@ -515,6 +532,8 @@ def cache_reserve(cache: KVCache, slots, tokens, *, granted=None, stream=None):
 def cache_append(cache: KVCache, k, v, slots, starts, *, done=None, stream=None):
     """hgf_cache_append: rows starts[i] .. starts[i + 1] - 1 of k (bf16 [n_rows][2 * n_heads * head_dim]) and v (bf16 [n_rows][n_heads * head_dim])
     to the sequence in slots[i].  Returns `done` (int32 [n_seqs], made here if not given): 1 where they were appended."""
+    if done is not None and _native_cache and _done("hgf_cache_append", _native_cache.cache_append(cache._at, cache._index, k, v, slots, starts, done, stream)):
+        return done
     _list(cache, slots, starts, done)
     n, width = slots.numel(), cache.n_heads * cache.head_dim
     assert k.device == v.device == cache.device and k.dtype == v.dtype == torch.bfloat16 and k.is_contiguous() and v.is_contiguous()
@@ -530,6 +549,8 @@ def cache_append(cache: KVCache, k, v, slots, starts, *, done=None, stream=None)
 def cache_read(cache: KVCache, slots, first, starts, n_rows: int | None = None, *, k=None, v=None, flags: int = 0, stream=None):
     """hgf_cache_read: tokens first[i], first[i] + 1, ... of the sequence in slots[i] as rows starts[i] .. starts[i + 1] - 1 of (k, v): fp32, or bf16
     with FLAG_OUT_BF16.  Without k and v, `n_rows` rows are made here, zero where nothing is read."""
+    if k is not None and not flags and _native_cache and _done("hgf_cache_read", _native_cache.cache_read(cache._at, cache._index, slots, first, starts, k, v, stream)):
+        return k, v
     _list(cache, slots, first, starts)
     n, width = slots.numel(), cache.n_heads * cache.head_dim
     if k is None:
@@ -548,11 +569,13 @@ def cache_read(cache: KVCache, slots, first, starts, n_rows: int | None = None, 
 
 def cache_fork(cache: KVCache, src, dst, *, done=None, stream=None):
     """hgf_cache_fork: the empty slot dst[i] becomes a copy of the sequence in src[i].  Returns `done` (int32 [n]; made here if not given)."""
-    _list(cache, src, dst, done)
-    n = src.numel()
     if done is None:
         with _on(stream):
-            done = torch.empty(n, dtype=torch.int32, device=cache.device)
+            done = torch.empty_like(src)
+    if _native_cache and _done("hgf_cache_fork", _native_cache.cache_fork(cache._at, cache._index, src, dst, done, stream)):
+        return done
+    _list(cache, src, dst, done)
+    n = src.numel()
     assert dst.numel() == n and done.numel() == n
     _check("hgf_cache_fork", lib().hgf_cache_fork(cache._ref, _ptr(src), _ptr(dst), n, _ptr(done), _stream(stream)))
     return done
@@ -560,6 +583,8 @@ def cache_fork(cache: KVCache, src, dst, *, done=None, stream=None):
 
 def cache_free(cache: KVCache, slots, *, stream=None) -> None:
     """hgf_cache_free: empties the slots and gives their pages back."""
+    if _native_cache and _done("hgf_cache_free", _native_cache.cache_free(cache._at, cache._index, slots, stream)):
+        return
     _list(cache, slots)
     _check("hgf_cache_free", lib().hgf_cache_free(cache._ref, _ptr(slots), slots.numel(), _stream(stream)))
 
@@ -572,6 +597,10 @@ def diff_attention_cached(cache: KVCache, q, slots, starts, lam: float, out_scal
                           stream=None):
     """hgf_diff_attention_cached: rows starts[i] .. starts[i + 1] - 1 of q (bf16 [n_rows][2 * n_heads * head_dim]), the last tokens of the sequence
     in slots[i], attend to what the cache holds of it -> out [n_rows][n_heads * head_dim], fp32 (bf16 with FLAG_OUT_BF16)."""
+    if out is not None and workspace is not None and _native_cache and _done(
+            "hgf_diff_attention_cached",
+            _native_cache.diff_attention_cached(cache._at, cache._index, q, slots, starts, lam, out_scale, out, workspace, flags, stream)):
+        return out
     _list(cache, slots, starts)
     n, rows = slots.numel(), q.shape[0]
     heads = q.shape[1] // (2 * cache.head_dim)

@@ -88,6 +88,23 @@ def test_workspace(hgf):
     assert bytes_(_struct(hgf), 4, 4, 4) == several        # shared heads
 
 
+def test_a_cache_in_host_memory_is_refused(hgf):
+    import torch
+    cache = hgf.KVCache(2, 64, 4, 2, 2, device="cpu")
+    assert cache.codes.shape == (4, 2, 3 * 64 * 64) and cache.open.shape == (2, 2, 3, 64, 64) and cache.table.shape == (2, 2) and cache.scales.shape == (4, 2, 4)
+    n, before = torch.zeros(2, dtype=torch.int32), hgf.launch_count()
+    k, v, f = (torch.zeros(1, w, dtype=torch.bfloat16) for w in (256, 128, 256))
+    out, ws = torch.zeros(1, 128), torch.zeros(1 << 22, dtype=torch.uint8)
+    for call in (lambda: hgf.cache_reserve(cache, n, n, granted=n), lambda: hgf.cache_append(cache, k, v, n[:1], n, done=n[:1]), lambda: hgf.cache_free(cache, n),
+                 lambda: hgf.cache_fork(cache, n, n, done=n), lambda: hgf.cache_read(cache, n[:1], n[:1], n, k=k, v=v),
+                 lambda: hgf.diff_attention_cached(cache, f, n[:1], n, 0.5, out=out, workspace=ws)):
+        with pytest.raises(AssertionError, match="not the current device"):
+            call()
+    assert hgf.launch_count() == before
+    with pytest.raises(AssertionError):
+        hgf.KVCache.of(2, 64, **{**{name: getattr(cache, name) for name in hgf.KVCache._SHAPES}, "refs": torch.zeros(5, dtype=torch.int32)})
+
+
 def test_status_string(hgf):
     assert hgf.status_string(8) not in {hgf.status_string(i) for i in (*range(8), 99)}
 

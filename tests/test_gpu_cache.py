@@ -468,6 +468,38 @@ def test_indices_out_of_range_are_skipped_and_reported(hgf):
     p.attend(range(4), [1] * 4)
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_arguments_that_do_not_fit_are_refused(hgf, monkeypatch, native):
+    """The same answers with the native marshalling and without it."""
+    if not native:
+        monkeypatch.setattr(hgf, "_native_cache", None)
+    p = Pair(hgf, 2, 64, n_slots=4)
+    p.fill([70, 70])
+    c, one, two = p.cache, ints([0]), ints([0, 1])
+    k, v = (torch.zeros((1, w), dtype=torch.bfloat16, device="cuda") for w in (256, 128))
+    out, ws, done = torch.zeros((1, 128), device="cuda"), torch.zeros(1 << 22, dtype=torch.uint8, device="cuda"), ints([0])
+    before = hgf.launch_count()
+    bad = [lambda: hgf.cache_reserve(c, one, two, granted=done), lambda: hgf.cache_reserve(c, one.long(), one, granted=done), lambda: hgf.cache_reserve(c, one.cpu(), one, granted=done),
+           lambda: hgf.cache_append(c, k.float(), v, one, two, done=done), lambda: hgf.cache_append(c, v, v, one, two, done=done), lambda: hgf.cache_append(c, k, v, one, one, done=done),
+           lambda: hgf.cache_append(c, k.expand(2, -1), v.expand(2, -1), one, two, done=done), lambda: hgf.cache_append(c, k, v.cpu(), one, two, done=done),
+           lambda: hgf.cache_fork(c, one, two, done=done), lambda: hgf.cache_free(c, one.long()), lambda: hgf.cache_free(c, ints(range(4))[::2]),
+           lambda: hgf.cache_read(c, one, one, two, k=k.float(), v=v), lambda: hgf.cache_read(c, one, one, two, k=v, v=v), lambda: hgf.cache_read(c, one, two, two, k=k, v=v),
+           lambda: hgf.diff_attention_cached(c, k[:, :200].contiguous(), one, two, 0.5, out=out, workspace=ws), lambda: hgf.diff_attention_cached(c, k, one, two, 0.5, out=out[:, :64], workspace=ws),
+           lambda: hgf.diff_attention_cached(c, k, one, two, 0.5, out=out, workspace=ws, flags=hgf.FLAG_OUT_BF16), lambda: hgf.diff_attention_cached(c, k, one, one, 0.5, out=out, workspace=ws)]
+    for call in bad:
+        with pytest.raises(AssertionError):
+            call()
+    for call, status in ((lambda: hgf.diff_attention_cached(c, k, one, two, 0.5, out=out, workspace=ws[:512]), 4), (lambda: hgf.diff_attention_cached(c, k, one, two, 0.5, out=out, workspace=ws[16:]), 3),
+                         (lambda: hgf.diff_attention_cached(c, torch.zeros((1, 3 * 128), dtype=torch.bfloat16, device="cuda"), one, two, 0.5), 2),
+                         (lambda: hgf.cache_free(c, ints(range(1025))), 2), (lambda: hgf.cache_append(c, k[:0], v[:0], one, two, done=done), 1)):
+        with pytest.raises(hgf.HgfError) as e:
+            call()
+        assert e.value.status == status
+    assert hgf.launch_count() == before
+    assert torch.equal(hgf.diff_attention_cached(c, k, one, two, 0.5, out=out, workspace=ws), hgf.diff_attention_cached(c, k, one, two, 0.5))
+    p.check()
+
+
 def test_tokens_taken_back(hgf):
     """Lowering a length within the open block, then going on: as if the tokens had never come."""
     p = Pair(hgf, 2, 64)
