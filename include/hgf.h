@@ -443,7 +443,8 @@ hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slots, int64_t 
  *        n_heads / cache->n_heads neighbouring heads share a K/V head
  *   out  [n_rows][n_heads * head_dim]      fp32, or bfloat16 with HGF_FLAG_OUT_BF16
  *   workspace  hgf_cached_workspace_bytes(...) bytes, 256-byte aligned; scratch, which calls that may overlap on the device do not share
- * Scores come from q to 2^-22 of the row's largest magnitude, probabilities enter the second product to 2^-24, all sums are exact integers or fp32.
+ * Scores come from q to 2^-22 of the row's largest magnitude; probabilities enter the second product to 2^-24 of the largest in their page (of several
+ * rows or shared heads with bf16 output: 2^-17); all sums are exact integers or fp32.
  * A query row or a visible block with a value that is not finite gives outputs that are not finite.
  */
 size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads);

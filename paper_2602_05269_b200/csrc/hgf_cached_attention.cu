@@ -1,47 +1,53 @@
 // Causal differential attention of new tokens over the 8-bit paged K/V cache (include/hgf.h, hgf_diff_attention_cached).
 //
-// What a page's head costs to read is 3 * 64 * DH bytes, and every byte is used for few products: the kernel is a stream from memory.  The work is
+// What a page's head costs to read is 3 * 64 * DH bytes, and for few query rows every byte is used for few products: a stream from memory.  The work is
 // cut into units of that size - a page of a sequence and K/V head, or 32 open tokens - and the units of all (sequence, group of query rows, head)
-// items are laid in one sequence, which is dealt in equal shares to the warps of one CTA an SM.  Each warp has a ring of units in shared memory that
-// one bulk copy each fills, and works alone: no barrier between warps.  An item that lies within one warp's share is finished there; of an item
-// that several share each leaves its softmax statistics and sums in the workspace, and a second kernel joins them, in the order of the tokens.
+// items are laid in one sequence, which is dealt in equal shares to one CTA an SM and within a CTA to its teams of warps.  A team has a ring of
+// units in shared memory that bulk copies fill, and works alone.  An item that lies within one team's share is finished there; of an item that
+// several share each leaves its softmax statistics and sums in the workspace.  What teams of one CTA share is joined at the end of that CTA, what
+// several CTAs share by a second kernel, both in the order of the tokens: the same call gives the same bits.
 //
 // Products are int8 tensor-core products on the codes as they lie in the page (m16n8k32, the codes as left operand), exact:
-//   scores   q as a 23-bit fixed-point number of the row's power of two, cut into three signed digits in base 256: three columns of the right operand
-//   values   probabilities as 24-bit fixed-point numbers of the running maximum (bits of 1 + p), three unsigned digits
-// so nothing is rounded to fewer than 22 bits on the way, at any output type.  The open tokens' bf16 go through bf16 products, with the probabilities
-// as sums of three bf16.
+//   scores   q as a 23-bit fixed-point number of the row's power of two, cut into three signed digits in base 256: columns of the right operand
+//   values   probabilities relative to the largest of the row's in this page, as fixed-point numbers of 24 bits (the bits of 1 + p), three unsigned
+//            digits; 16 bits, two digits, in the many-row form with bf16 output: at most 64 * 2^-17 of a page's weight, beside the output's 2^-9
+// The accumulators start at the bits of 1.5 * 2^23, so that a sum, below 2^22 in magnitude, is a float after one subtraction: I2F runs at an eighth
+// of the FMA rate and bounded the kernel.  The open tokens' bf16 go through bf16 products, with the probabilities as sums of three bf16.
 //
-// Two forms: ROWS = 1 for single tokens with heads of their own (both streams' digits fit the eight columns of one product), ROWS = 8 otherwise (a
-// product for each digit, eight query rows as its columns).
+// Two forms.  ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.
+// ROWS = 8 otherwise: a product for each digit, eight query rows as its columns; a warp takes one stream of one tile of eight rows, and a team is the
+// warps of up to four tiles, so that a page that is read once serves 32 rows.
 #include "hgf_cache.cuh"
 #include "hgf_warp.cuh"
 
 namespace hgf {
 
-constexpr int kCaMaxSms = 160;   // CTAs at most (the workspace has room for them)
-constexpr int kCaStages = 2;     // units in a warp's ring
+constexpr int kCaMaxSms = 160;      // CTAs at most (the workspace has room for them)
+constexpr int kCaMaxTeamTiles = 8;  // teams of a CTA times tiles of a team, at most
 
-template <int DH>
+template <int DH, int ROWS>
 struct CaCfg {
-    static constexpr int WARPS = DH == 64 ? 8 : 4, THREADS = WARPS * 32;
+    static constexpr int WARPS = ROWS == 8 ? 16 : (DH == 64 ? 8 : 4), THREADS = WARPS * 32;
     static constexpr int UNIT = 3 * kCacheBlock * DH;            // bytes of a unit
     static constexpr int STAGE = (UNIT + 16 + 127) / 128 * 128;  // with the page's scales
+    static constexpr int STAGES = DH == 64 ? 16 : 8;             // of all teams' rings
     static constexpr int KT = DH / 32, MT = DH / 16;
+    static constexpr int SCORES = ROWS == 1 ? 2 * kCacheBlock * 4 : 8 * 36 * 4;  // bytes a warp; rows 36 floats apart: eight rows' writes hit all banks
+    static constexpr int PART = 4 + 2 * DH;                      // floats: maximum and sum of stream 1, of stream 2, sums of values of both
+    static constexpr int SMEM = STAGES * STAGE + WARPS * SCORES + (kCacheMaxSeqs + 1) * 8;
 };
-constexpr int kCaScoreStride = 68;  // floats between rows of scores: eight rows' writes hit all banks
-template <int ROWS>
-constexpr int kCaScoreBytes = ROWS == 1 ? 2 * kCacheBlock * 4 : 8 * kCaScoreStride * 4;
 
 struct CaParams {
     CacheView c;
     const __nv_bfloat16 *q;
     const int32_t *slots, *starts;
     void *out;
-    int4 *items;          // [workers][2]: what the joining kernel does for a worker
-    float *parts;         // [workers][2][ROWS][4 + 2 DH]: maximum and sum of stream 1, of stream 2, sums of values
+    int4 *items;          // [CTAs][2]: what the joining kernel does for a CTA
+    float *cta_parts;     // [CTAs][2][tiles][ROWS][PART]
+    float *parts;         // [CTAs][teams][2][tiles][ROWS][PART]
     unsigned int *status;
     int n_seqs, n_rows, group, bf16;
+    int teams, tiles, stages;  // of a CTA; of a team; of a team's ring
     float lambda, out_scale, scale_log2;
 };
 
@@ -76,13 +82,12 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-// A sequence of the call and an item's place in it.
+
+// A sequence of the call.
 struct CaSeq {
-    int slot, row0, m, length, pages, units;
-    int tiles;
+    int slot, row0, m, length, pages, units, tiles;
 };
-template <int ROWS>
-__device__ __forceinline__ CaSeq ca_sequence(const CaParams &p, int i) {
+__device__ __forceinline__ CaSeq ca_sequence(const CaParams &p, int rows, int i) {
     CaSeq s = {};
     s.slot = p.slots[i];
     s.row0 = p.starts[i];
@@ -102,38 +107,99 @@ __device__ __forceinline__ CaSeq ca_sequence(const CaParams &p, int i) {
     s.pages = s.length >> 6;
     const int open = s.length & 63;
     s.units = s.pages + (open > 0) + (open > 32);
-    s.tiles = (s.m * p.group + ROWS - 1) / ROWS;
+    s.tiles = (s.m * p.group + rows - 1) / rows;
     return s;
 }
-
+// A unit's place: its sequence, the item's rows and head, its number in the item.
 struct CaCursor {
     CaSeq s;
     int seq, tile, head, unit;
 };
+// An item as it is left for joining: its first unit and the one behind its last, and where its rows go.
+struct CaItem {
+    long long from, to;
+    int row0, m, head, tile;
+};
 
-template <int DH, int ROWS>
-__global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel(CaParams p) {
-    using C = CaCfg<DH>;
+__device__ __forceinline__ void ca_write(const CaParams &p, const CaItem &it, int rr, int dh, int dim, float y) {
+    const size_t o = ((size_t)(it.row0 + rr / p.group) * p.c.H * p.group + it.head * p.group + rr % p.group) * dh + dim;
+    if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[o] = __float2bfloat16(y);
+    else reinterpret_cast<float *>(p.out)[o] = y;
+}
+
+// Joins n parts of an item, in order: at(j) is the j-th.  `to`: where the result stays a part, null if it is the output.  Threads deal (row, dim).
+template <int DH, int ROWS, class F>
+__device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int n, F at, float *to, int thread, int threads) {
     constexpr int PART = 4 + 2 * DH;
+    const int rows = min(ROWS * p.tiles, it.m * p.group - it.tile * ROWS * p.tiles);
+    for (int e = thread; e < rows * DH; e += threads) {
+        const int r = e / DH, dim = e % DH;
+        float m1 = -INFINITY, l1 = 0.0f, m2 = -INFINITY, l2 = 0.0f, o1 = 0.0f, o2 = 0.0f;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            const float *part = at(j) + r * PART;
+            const float4 s = *reinterpret_cast<const float4 *>(part);
+            const float v1 = part[4 + dim], v2 = part[4 + DH + dim];
+            const float n1 = fmaxf(m1, s.x), n2 = fmaxf(m2, s.z), b1 = n1 == -INFINITY ? 0.0f : n1, b2 = n2 == -INFINITY ? 0.0f : n2;
+            const float a1 = exp2_approx(m1 - b1), c1 = exp2_approx(s.x - b1), a2 = exp2_approx(m2 - b2), c2 = exp2_approx(s.z - b2);
+            l1 = l1 * a1 + s.y * c1;
+            o1 = o1 * a1 + v1 * c1;
+            l2 = l2 * a2 + s.w * c2;
+            o2 = o2 * a2 + v2 * c2;
+            m1 = n1;
+            m2 = n2;
+        }
+        if (to) {
+            float *part = to + r * PART;
+            if (dim == 0) *reinterpret_cast<float4 *>(part) = make_float4(m1, l1, m2, l2);
+            part[4 + dim] = o1;
+            part[4 + DH + dim] = o2;
+        } else {
+            const float y1 = l1 != 0.0f ? o1 / l1 : 0.0f, y2 = l2 != 0.0f ? o2 / l2 : 0.0f;
+            ca_write(p, it, it.tile * ROWS * p.tiles + r, DH, dim, (y1 - p.lambda * y2) * p.out_scale);
+        }
+    }
+}
+
+constexpr uint32_t kCaMagic = 0x4b400000u;      // 1.5 * 2^23: an accumulator that starts there is that float plus its sum
+constexpr float kCaMagicF = 12582912.0f;
+__device__ __forceinline__ float ca_float(int d) { return __int_as_float(d) - kCaMagicF; }
+__device__ __forceinline__ uint64_t ca_float2(int a, int b) {
+    return add_f32x2(pack_f32x2(__int_as_float(a), __int_as_float(b)), pack_f32x2(-kCaMagicF, -kCaMagicF));
+}
+
+// DP: digits of the probabilities.
+template <int DH, int ROWS, int DP>
+__global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_kernel(CaParams p) {
+    using C = CaCfg<DH, ROWS>;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, H = p.c.H;
-    uint8_t *ring = smem + warp * (kCaStages * C::STAGE);
-    float *scores = reinterpret_cast<float *>(smem + C::WARPS * kCaStages * C::STAGE + warp * kCaScoreBytes<ROWS>);
-    long long *prefix = reinterpret_cast<long long *>(smem + C::WARPS * (kCaStages * C::STAGE + kCaScoreBytes<ROWS>));
-    __shared__ long long wide[C::WARPS + 1];
-    __shared__ __align__(8) uint64_t bars[C::WARPS][kCaStages];
-    const uint32_t ring_a = dsmem_u32(ring);
-    if (lane < kCaStages) dmbar_init(dsmem_u32(&bars[warp][lane]), 1);
+    const int team_warps = ROWS == 1 ? 1 : 2 * p.tiles, team = ROWS == 1 ? warp : warp / team_warps;
+    const int member = ROWS == 1 ? 0 : warp - team * team_warps, my_tile = member >> 1, stream = member & 1;
+    const bool leads = member == 0;
+    const int stages = ROWS == 1 ? 2 : p.stages;
+    uint8_t *ring = smem + team * stages * C::STAGE;
+    float *scores = reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + warp * C::SCORES);
+    long long *prefix = reinterpret_cast<long long *>(smem + C::STAGES * C::STAGE + C::WARPS * C::SCORES);
+    __shared__ long long wide[C::WARPS];
+    __shared__ __align__(8) uint64_t bars[C::STAGES];
+    __shared__ int page_ok[C::STAGES];       // a stage's page number was one
+    __shared__ volatile int gave_up;         // a wait ran out: the others end, too
+    __shared__ CaItem first_item_of_cta, last_item_of[kCaMaxTeamTiles];
+    const uint32_t ring_a = dsmem_u32(ring), bars_a = dsmem_u32(bars) + team * stages * 8;
+    if (tid < C::STAGES) dmbar_init(dsmem_u32(&bars[tid]), 1);
+    if (tid == 0) gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     pdl_launch_dependents();
+    const int tile_rows = ROWS * (ROWS == 1 ? 1 : p.tiles);
 
     // ---- plan: the running sum of units over the sequences, by every CTA for itself
     long long total = 0;
-    for (int i0 = 0; i0 < p.n_seqs; i0 += C::THREADS) {
+    for (int i0 = 0; i0 < p.n_seqs; i0 += blockDim.x) {
         const int i = i0 + tid;
         long long mine = 0;
         if (i < p.n_seqs) {
-            const CaSeq s = ca_sequence<ROWS>(p, i);
+            const CaSeq s = ca_sequence(p, tile_rows, i);
             mine = (long long)s.tiles * H * s.units;
             if (blockIdx.x == 0 && s.slot == -2) atomicOr(p.status, kStatusCache);
         }
@@ -146,8 +212,8 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
         if (lane == 31) wide[warp] = sum;
         __syncthreads();
         long long before = total, all = 0;
-#pragma unroll
-        for (int w = 0; w < C::WARPS; ++w) {
+        const int warps = blockDim.x >> 5;
+        for (int w = 0; w < warps; ++w) {
             if (w < warp) before += wide[w];
             all += wide[w];
         }
@@ -155,28 +221,36 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
         total += all;
         __syncthreads();
     }
-    if (tid == 0) prefix[p.n_seqs] = total;
+    if (tid == 0) {
+        prefix[p.n_seqs] = total;
+        p.items[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+    }
     __syncthreads();
 
     // rows that see nothing because the sequence is empty
     const int width = H * p.group * DH;
     for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x)
         if (prefix[i + 1] == prefix[i]) {
-            const CaSeq s = ca_sequence<ROWS>(p, i);
+            const CaSeq s = ca_sequence(p, tile_rows, i);
             const size_t at = (size_t)s.row0 * width, n = (size_t)s.m * width;
-            for (size_t e = tid; e < n; e += C::THREADS) {
+            for (size_t e = tid; e < n; e += blockDim.x) {
                 if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[at + e] = __float2bfloat16(0.0f);
                 else reinterpret_cast<float *>(p.out)[at + e] = 0.0f;
             }
         }
 
-    // (no more workers than units, so that none is empty between two of an item; their numbers go round the CTAs)
-    const int workers = (int)min((long long)gridDim.x * C::WARPS, total), worker = warp * gridDim.x + blockIdx.x;
-    if (worker >= workers) {
-        if (lane == 0) p.items[2 * worker] = make_int4(0, 0, 0, 0);
-        return;
-    }
-    const long long u0 = total * worker / workers, u1 = total * (worker + 1) / workers;
+    // ---- shares.  As many CTAs as have a unit for each team, as many teams as have a unit: none is empty between two of an item, and a short item
+    // stays within a CTA.
+    const int teams_here = ROWS == 1 ? C::WARPS : p.teams;
+    const int ctas = (int)min((long long)gridDim.x, (total + teams_here - 1) / teams_here);
+    if ((int)blockIdx.x >= ctas) return;
+    const long long c0 = total * blockIdx.x / ctas, c1 = total * (blockIdx.x + 1) / ctas;
+    const int teams = (int)min((long long)teams_here, c1 - c0);
+    const bool works = team < teams;
+    const long long u0 = works ? c0 + (c1 - c0) * team / teams : c1, u1 = works ? c0 + (c1 - c0) * (team + 1) / teams : c1;
+    float *my_parts = p.parts + ((size_t)blockIdx.x * teams_here + team) * 2 * (ROWS == 1 ? 1 : p.tiles) * (ROWS * C::PART);
+    const int part_floats = (ROWS == 1 ? 1 : p.tiles) * (ROWS * C::PART);
+
     auto place = [&](long long u, CaCursor &k) {
         int lo = 0, hi = p.n_seqs - 1;
         while (lo < hi) {  // the last sequence that begins at or before u (of empty ones at the same place the last, which is not empty)
@@ -184,7 +258,7 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
             if (prefix[mid] <= u) lo = mid; else hi = mid - 1;
         }
         k.seq = lo;
-        k.s = ca_sequence<ROWS>(p, lo);
+        k.s = ca_sequence(p, tile_rows, lo);
         const long long in = u - prefix[lo], item = in / k.s.units;
         k.unit = (int)(in - item * k.s.units);
         k.tile = (int)(item / H);
@@ -198,25 +272,23 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
         if (++k.tile < k.s.tiles) return true;
         k.tile = 0;
         do ++k.seq; while (k.seq < p.n_seqs - 1 && prefix[k.seq + 1] == prefix[k.seq]);
-        if (k.seq < p.n_seqs) k.s = ca_sequence<ROWS>(p, k.seq);
+        if (k.seq < p.n_seqs) k.s = ca_sequence(p, tile_rows, k.seq);
         return true;
     };
-    // Tokens that query row r of a tile sees: those before row_sees().
-    auto row_sees = [&](const CaCursor &k, int r) {
-        const int at = k.tile * ROWS + r;
-        return at < k.s.m * p.group ? k.s.length - k.s.m + at / p.group + 1 : 0;
-    };
+    // Row `at` of an item's sequence (token, then head of the group) sees the tokens before this; rows that are not there see none.
+    auto row_sees = [&](const CaSeq &s, int at) { return at < s.m * p.group ? s.length - s.m + at / p.group + 1 : 0; };
+    auto last_sees = [&](const CaSeq &s, int tile) { return row_sees(s, min((tile + 1) * tile_rows, s.m * p.group) - 1); };
     auto unit_token = [&](const CaCursor &k) { return k.unit < k.s.pages ? k.unit << 6 : (k.s.pages << 6) + ((k.unit - k.s.pages) << 5); };
-    auto tile_sees = [&](const CaCursor &k) {  // of the tile's last row
-        return k.s.length - k.s.m + min(k.tile * ROWS + ROWS - 1, k.s.m * p.group - 1) / p.group + 1;
+    auto team_sync = [&] {
+        if (ROWS == 1) __syncwarp();
+        else bar_sync(1 + team, team_warps * 32);
     };
 
-    // ---- the ring: page numbers 32 at a time, one bulk copy a unit
-    uint32_t loaded = 0;  // per stage: its unit was fetched
+    // ---- the ring: the leading warp fetches, page numbers 32 at a time, one bulk copy a unit
     int pages32 = 0, pages_at = -32, pages_seq = -1;
     auto fetch = [&](const CaCursor &k, int stage) {
-        const uint32_t bar = dsmem_u32(&bars[warp][stage]), dst = ring_a + stage * C::STAGE;
-        bool ok = unit_token(k) < tile_sees(k);
+        const uint32_t bar = bars_a + stage * 8, dst = ring_a + stage * C::STAGE;
+        if (unit_token(k) >= last_sees(k.s, k.tile)) return;  // (nobody waits for it either)
         if (k.unit < k.s.pages) {
             if (pages_seq != k.seq || (k.unit & ~31) != pages_at) {
                 pages_seq = k.seq;
@@ -224,86 +296,102 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
                 pages32 = pages_at + lane < k.s.pages ? p.c.table[(size_t)k.s.slot * p.c.max_pages + pages_at + lane] : 0;
             }
             const int page = __shfl_sync(0xffffffffu, pages32, k.unit & 31);
-            if (ok && (page < 0 || page >= p.c.n_pages)) {
-                ok = false;
-                if (lane == 0) atomicOr(p.status, kStatusCache);
+            const bool ok = page >= 0 && page < p.c.n_pages;
+            if (lane == 0) {
+                page_ok[team * stages + stage] = ok;
+                if (ok) {
+                    const size_t at = (size_t)page * H + k.head;
+                    announce(bar, C::UNIT + 16);
+                    bulk_load_announced(dst, p.c.codes + at * C::UNIT, C::UNIT, bar);
+                    bulk_load_announced(dst + C::UNIT, p.c.scales + at, 16, bar);
+                } else {
+                    atomicOr(p.status, kStatusCache);
+                    announce(bar, 0);
+                }
             }
-            if (ok && lane == 0) {
-                const size_t at = (size_t)page * H + k.head;
-                announce(bar, C::UNIT + 16);
-                bulk_load_announced(dst, p.c.codes + at * C::UNIT, C::UNIT, bar);
-                bulk_load_announced(dst + C::UNIT, p.c.scales + at, 16, bar);
-            }
-        } else if (ok && lane == 0) {
+        } else if (lane == 0) {
             const int half = k.unit - k.s.pages, rows = min(32, (k.s.length & 63) - 32 * half);
             const __nv_bfloat16 *src = p.c.open + (((size_t)k.s.slot * H + k.head) * 3 * kCacheBlock + 32 * half) * DH;
+            page_ok[team * stages + stage] = 1;
             announce(bar, 3 * rows * DH * 2);
 #pragma unroll
             for (int n = 0; n < 3; ++n) bulk_load_announced(dst + n * 32 * DH * 2, src + (size_t)n * kCacheBlock * DH, rows * DH * 2, bar);
         }
-        loaded = ok ? loaded | 1u << stage : loaded & ~(1u << stage);
     };
     uint32_t phases = 0;
-    auto arrived = [&](int stage) {  // waits, bounded, for the stage's copies
-        const uint32_t bar = dsmem_u32(&bars[warp][stage]), parity = phases >> stage & 1u;
+    auto arrived = [&](int stage, bool last) {  // waits, bounded, for the stage's copies
+        const uint32_t bar = bars_a + stage * 8, parity = phases >> stage & 1u;
         bool got = dmbar_try_wait(bar, parity);
         if (__all_sync(0xffffffffu, got)) return true;
         const unsigned long long since = dec_timer_ns();
         for (uint32_t polls = 1; !got && !(got = dmbar_try_wait(bar, parity)); ++polls)
-            if ((polls & 255u) == 0 && dec_timer_ns() - since > kDecWaitLimitNs) break;
-        if (!got) atomicExch(p.status, 0xb00u);
+            if ((polls & 255u) == 0 && ((!last && gave_up) || dec_timer_ns() - since > kDecWaitLimitNs)) break;
+        if (!got) {
+            gave_up = 1;
+            atomicExch(p.status, 0xb00u);
+        }
         return (bool)__all_sync(0xffffffffu, got);
     };
 
     CaCursor ahead, k;
-    place(u0, ahead);
-    k = ahead;
+    if (works) place(u0, k);
+    ahead = k;
     long long ahead_u = u0;
-    __syncwarp();
-#pragma unroll
-    for (int s = 0; s < kCaStages; ++s)
-        if (ahead_u < u1) {
+    if (leads)
+        for (int s = 0; s < stages && ahead_u < u1; ++s) {
             fetch(ahead, s);
             advance(ahead);
             ++ahead_u;
         }
+    if (works && team == 0 && lane == 0 && leads) first_item_of_cta = {u0 - k.unit, u0 - k.unit + k.s.units, k.s.row0, k.s.m, k.head, k.tile};
 
     // ---- state of the item
     // ROWS = 1: m, l of the lane's stream (lanes 0-15 stream 1, 16-31 stream 2); acc[mt][e]: dims 16 mt + g + 8 e, in lanes t of stream t / 2.
-    // ROWS = 8: m[st], l[st] of row g; acc[st][mt][e]: dim 16 mt + g + 8 (e / 2), row 2 t + e % 2.
-    constexpr int NS = ROWS == 1 ? 1 : 2, NE = ROWS == 1 ? 2 : 4;
-    float m[NS], l[NS], acc[NS][C::MT][NE];
-    uint32_t qd[2][ROWS == 1 ? 1 : 3][C::KT][2];  // right operand of the scores: digits of q
-    float qs[NS];                                 // what a digit sum is worth, with 1 / sqrt(d) and log2 e
-    const int my_stream = lane >> 4, limb = g & 3;
+    // ROWS = 8: m, l of row g, of the warp's stream; acc[mt][e]: dim 16 mt + g + 8 (e / 2), row 2 t + e % 2.
+    constexpr int NE = ROWS == 1 ? 2 : 4, ND = ROWS == 1 ? 1 : 3;
+    float m = -INFINITY, l = 0.0f, acc[C::MT][NE];
+    uint32_t qd[ROWS == 1 ? 2 : 1][ND][C::KT][2];  // right operand of the scores: digits of q (ROWS = 1: for K1 and for K2)
+    float qs = 0.0f;                               // what a digit sum is worth, with 1 / sqrt(d) and log2 e
+    int sees_g = 0, sees_e[2] = {0, 0}, sees_tile = 0, sees_all = 0;  // tokens that row g, rows 2 t and 2 t + 1, any row, every row of the tile sees
+    const int my_stream = ROWS == 1 ? lane >> 4 : stream, limb = g & 3;
     const uint32_t limb_sel = 0x0040u + (uint32_t)((2 - limb) & 3) * 0x0011u;  // byte 2 - limb of two words
     const uint32_t limb_xor = limb == 0 ? 0x80808080u : 0u, limb_keep = limb == 3 ? 0u : 0xffffffffu;
+    const int heads = H * p.group;
 
+    auto q_row = [&](int n, int at) {  // stream n of the item's row
+        return p.q + ((size_t)(k.s.row0 + at / p.group) * 2 + n) * heads * DH + (size_t)(k.head * p.group + at % p.group) * DH;
+    };
     auto begin_item = [&] {
+        m = -INFINITY;
+        l = 0.0f;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            m[s] = -INFINITY;
-            l[s] = 0.0f;
+        for (int a = 0; a < C::MT; ++a)
 #pragma unroll
-            for (int a = 0; a < C::MT; ++a)
-#pragma unroll
-                for (int e = 0; e < NE; ++e) acc[s][a][e] = 0.0f;
+            for (int e = 0; e < NE; ++e) acc[a][e] = 0.0f;
+        const int base = k.tile * tile_rows + my_tile * ROWS, there = k.s.m * p.group;
+        if (ROWS == 1) {
+            sees_g = sees_tile = sees_all = row_sees(k.s, base);
+        } else {
+            sees_g = row_sees(k.s, base + g);
+            sees_e[0] = row_sees(k.s, base + 2 * t);
+            sees_e[1] = row_sees(k.s, base + 2 * t + 1);
+            sees_tile = base < there ? row_sees(k.s, min(base + 7, there - 1)) : 0;
+            sees_all = min(row_sees(k.s, base), row_sees(k.s, base + 7));
         }
         // q's digits: q = f * 2^(E - 21) with E the exponent of the row's largest magnitude, so |f| < 2^22; f + 0x808080 has in each byte the
         // balanced digit plus 128.
-        const int heads = H * p.group;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int r = ROWS == 1 ? 0 : g, at = k.tile * ROWS + r;
-            const bool there = at < k.s.m * p.group && (ROWS == 8 || (g >> 2) == n);
-            const __nv_bfloat16 *src = p.q + ((size_t)(k.s.row0 + (there ? at / p.group : 0)) * 2 + n) * heads * DH + (size_t)(k.head * p.group + (there ? at % p.group : 0)) * DH;
+        for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n) {
+            const int at = base + (ROWS == 1 ? 0 : g);
+            const bool mine = at < there && (ROWS == 8 || (g >> 2) == n);
+            const __nv_bfloat16 *src = q_row(ROWS == 1 ? n : stream, mine ? at : 0);
             uint2 w[C::KT][2];
             uint32_t top = 0;
 #pragma unroll
             for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    w[kt][h] = there ? *reinterpret_cast<const uint2 *>(src + kt * 32 + h * 16 + 4 * t) : make_uint2(0, 0);
+                    w[kt][h] = mine ? *reinterpret_cast<const uint2 *>(src + kt * 32 + h * 16 + 4 * t) : make_uint2(0, 0);
                     top = __vmaxu2(top, __vmaxu2(w[kt][h].x & 0x7fff7fffu, w[kt][h].y & 0x7fff7fffu));
                 }
             top = max(top >> 16, top & 0xffffu);
@@ -312,7 +400,7 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
             const int E = max((int)(top >> 7) - 127, -100);  // (below 2^-100 the scores are zero for any purpose, above that 2^(21 - E) is a float)
             const float f = __uint_as_float((uint32_t)(127 + 21 - E) << 23);
             const float back = top >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 - 21 + E) << 23);
-            if (ROWS == 8 || n == my_stream) qs[ROWS == 1 ? 0 : n] = back * p.scale_log2;
+            if (ROWS == 8 || n == my_stream) qs = back * p.scale_log2;
 #pragma unroll
             for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
@@ -324,62 +412,90 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
                     d[3] = (uint32_t)__float2int_rn(bf16hi_to_float(w[kt][h].y) * f) + 0x808080u;
                     if (ROWS == 1) {
                         const uint32_t v = __byte_perm(__byte_perm(d[0], d[1], limb_sel), __byte_perm(d[2], d[3], limb_sel), 0x5410) ^ 0x80808080u;
-                        qd[n][0][kt][h] = there ? v & limb_keep : 0u;
+                        qd[n][0][kt][h] = mine ? v & limb_keep : 0u;
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 3; ++j) {
+                        for (int j = 0; j < ND; ++j) {
                             const uint32_t sel = 0x0040u + (uint32_t)(2 - j) * 0x0011u;
-                            qd[n][ROWS == 1 ? 0 : j][kt][h] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
+                            qd[n][j][kt][h] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
                         }
                     }
                 }
         }
     };
 
-    // Softmax step of a row on `x` (16 or 8 tokens of this lane, the row's others in the lanes with the same g): new maximum, the probabilities in
-    // place of the scores, and what the sums so far are to be multiplied with.
-    auto softmax_step = [&](auto &x, float &mx, float &sum) {
+    // Softmax step of a row on `x`, scores before their factor f (16 or 8 tokens of this lane, the row's others in the lanes with the same g; the first
+    // `sees` of the unit's tokens count, `token(j)` is the j-th of the lane's): the probabilities relative to the unit's largest in place of the scores,
+    // and what the sums so far (alpha) and the unit's (worth) are to be multiplied with.
+    auto softmax_step = [&](auto &x, float f, bool partly, int sees, auto token, float &alpha, float &worth) {
         constexpr int N = sizeof(x) / sizeof(float);
+        if (partly) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (token(j) >= sees) x[j] = -INFINITY;
+        }
         float top = x[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) top = fmaxf(top, x[j]);
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const float now = fmaxf(mx, top), base = now == -INFINITY ? 0.0f : now, alpha = exp2_approx(mx - base);
+        // (f is zero for a page of zeros: then nothing is -inf but what is masked)
+        const float here = top == -INFINITY ? -INFINITY : top * f, now = fmaxf(m, here), base = now == -INFINITY ? 0.0f : now;
+        const float minus = here == -INFINITY ? 0.0f : -here;
+        alpha = exp2_approx(m - base);
+        worth = exp2_approx(here - base);
         float s = 0.0f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            x[j] = exp2_approx(x[j] - base);
+            const float y = fmaf(x[j], f, minus);
+            x[j] = partly && token(j) >= sees ? 0.0f : exp2_approx(y);
             s += x[j];
         }
-        mx = now;
-        sum = fmaf(sum, alpha, s);
-        return alpha;
+        m = now;
+        l = fmaf(l, alpha, s * worth);
     };
 
-    bool fresh = true;                       // the unit begins an item, or the share
-    const bool begins_inside = k.unit != 0;  // the share's first item began in another share
-    bool first_item = true;
-    int4 join = make_int4(0, 0, 0, 0), join_at = join;
-
+    const bool begins_inside = works && k.unit != 0;  // the share's first item began in another share
+    bool fresh = true, first_item = true;
+    // A warp whose wait ran out computes and fetches no more, but takes its steps to the end: the others of its team meet it at their barrier.
+    bool dead = false;
+    int stage = 0;
     for (long long u = u0; u < u1; ++u) {
-        const int stage = (int)(u - u0) & (kCaStages - 1);
         if (fresh) begin_item();
         const uint8_t *unit = ring + stage * C::STAGE;
-        if (loaded >> stage & 1u) {
-            if (!arrived(stage)) {
-                if (loaded >> (stage ^ 1) & 1u) arrived(stage ^ 1);  // (no copy outlives the CTA)
-                break;
+        const int token0 = unit_token(k);
+        if (token0 < last_sees(k.s, k.tile)) {
+            if (!dead) {
+                if (arrived(stage, false)) {
+                    phases ^= 1u << stage;
+                } else {
+                    dead = true;
+                    if (leads)  // (no copy outlives the CTA)
+                        for (int s = 0; u + s < ahead_u; ++s) arrived((stage + s) % stages, true);
+                }
             }
-            phases ^= 1u << stage;
-            const int token0 = unit_token(k);
-            if (k.unit < k.s.pages) {
+            const bool ok = !dead && page_ok[team * stages + stage];
+            const bool open_unit = k.unit >= k.s.pages;
+            if (open_unit) {
+                // what lies behind the last row is no value: V's rows there become zero (K's only give scores that are not looked at)
+                const int rows = min(32, (k.s.length & 63) - 32 * (k.unit - k.s.pages));
+                uint8_t *mine = ring + stage * C::STAGE;
+                if (leads)
+                    for (int e = lane; e < (32 - rows) * (DH / 8); e += 32) *reinterpret_cast<uint4 *>(mine + 2 * 32 * DH * 2 + rows * DH * 2 + e * 16) = make_uint4(0, 0, 0, 0);
+                team_sync();
+            }
+            if (ok && !open_unit && token0 < sees_tile) {
                 const float4 sc = *reinterpret_cast<const float4 *>(unit + C::UNIT);
+                float alpha, worth;
+                auto token = [&](int j) { return (j >> 2) * 16 + 4 * t + (j & 3); };
+                const bool partly = sees_all - token0 < kCacheBlock;
+                const float f = qs * (my_stream ? sc.y : sc.x);
+                float x[16];
                 if constexpr (ROWS == 1) {
                     const float wa = t & 1 ? 1.0f : 65536.0f, wb = t & 1 ? 0.0f : 256.0f;
 #pragma unroll
                     for (int mt = 0; mt < 4; ++mt) {
-                        int d[4] = {0, 0, 0, 0};
+                        int d[4] = {(int)kCaMagic, (int)kCaMagic, (int)kCaMagic, (int)kCaMagic};
 #pragma unroll
                         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -387,29 +503,21 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
                                 const uint4 a = *reinterpret_cast<const uint4 *>(unit + n * kCacheBlock * DH + ((mt * C::KT + kt) * 32 + lane) * 16);
                                 mma_s8s8(d, a, qd[n][0][kt][0], qd[n][0][kt][1]);
                             }
-                        float lo = fmaf((float)d[0], wa, (float)d[1] * wb), hi = fmaf((float)d[2], wa, (float)d[3] * wb);
+                        float lo = fmaf(ca_float(d[0]), wa, ca_float(d[1]) * wb), hi = fmaf(ca_float(d[2]), wa, ca_float(d[3]) * wb);
                         lo += __shfl_xor_sync(0xffffffffu, lo, 1);
                         hi += __shfl_xor_sync(0xffffffffu, hi, 1);
                         scores[(t >> 1) * kCacheBlock + mt * 16 + g + (t & 1) * 8] = t & 1 ? hi : lo;
                     }
                     __syncwarp();
-                    const float f = qs[0] * (my_stream ? sc.y : sc.x);
-                    float x[16];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float4 v = *reinterpret_cast<const float4 *>(scores + my_stream * kCacheBlock + j * 16 + 4 * t);
-                        x[4 * j] = v.x * f;
-                        x[4 * j + 1] = v.y * f;
-                        x[4 * j + 2] = v.z * f;
-                        x[4 * j + 3] = v.w * f;
+                        x[4 * j] = v.x;
+                        x[4 * j + 1] = v.y;
+                        x[4 * j + 2] = v.z;
+                        x[4 * j + 3] = v.w;
                     }
-                    const int sees = row_sees(k, 0) - token0;
-                    if (sees < kCacheBlock) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if ((j >> 2) * 16 + 4 * t + (j & 3) >= sees) x[j] = -INFINITY;
-                    }
-                    const float alpha = softmax_step(x, m[0], l[0]);
+                    softmax_step(x, f, partly, sees_g - token0, token, alpha, worth);
                     uint32_t b[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -418,397 +526,340 @@ __global__ void __launch_bounds__(CaCfg<DH>::THREADS, 1) cached_attention_kernel
                         for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[4 * j + e]);
                         b[j] = (__byte_perm(__byte_perm(w[0], w[1], limb_sel), __byte_perm(w[2], w[3], limb_sel), 0x5410) ^ limb_xor) & limb_keep;
                     }
-                    const float scale = __shfl_sync(0xffffffffu, alpha, (t >> 1) * 16);
+                    const float scale = __shfl_sync(0xffffffffu, alpha, (t >> 1) * 16), sv = sc.z * __shfl_sync(0xffffffffu, worth, (t >> 1) * 16);
                     // digits of 2^23 p: weights 2^-7, 2^-15, 2^-23
-                    const float va = sc.z * (t & 1 ? 1.1920928955078125e-7f : 0.0078125f), vb = t & 1 ? 0.0f : sc.z * 3.0517578125e-5f;
+                    const float va = sv * (t & 1 ? 1.1920928955078125e-7f : 0.0078125f), vb = t & 1 ? 0.0f : sv * 3.0517578125e-5f;
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        int d[4] = {0, 0, 0, 0};
+                        int d[4] = {(int)kCaMagic, (int)kCaMagic, (int)kCaMagic, (int)kCaMagic};
 #pragma unroll
                         for (int kt = 0; kt < 2; ++kt) {
                             const uint4 a = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
                             mma_s8u8(d, a, b[2 * kt], b[2 * kt + 1]);
                         }
-                        acc[0][mt][0] = fmaf((float)d[0], va, fmaf((float)d[1], vb, acc[0][mt][0] * scale));
-                        acc[0][mt][1] = fmaf((float)d[2], va, fmaf((float)d[3], vb, acc[0][mt][1] * scale));
+                        acc[mt][0] = fmaf(ca_float(d[0]), va, fmaf(ca_float(d[1]), vb, acc[mt][0] * scale));
+                        acc[mt][1] = fmaf(ca_float(d[2]), va, fmaf(ca_float(d[3]), vb, acc[mt][1] * scale));
                     }
                 } else {
-                    const int sees = row_sees(k, g) - token0;
-                    const bool partly = row_sees(k, 0) - token0 < kCacheBlock || row_sees(k, 7) - token0 < kCacheBlock;
-                    uint32_t b[2][3][4];
-                    float alpha[2];
+                    const uint64_t base256 = pack_f32x2(256.0f, 256.0f);
+                    const uint8_t *codes = unit + stream * kCacheBlock * DH;
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
+                    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                        for (int mt = 0; mt < 4; ++mt) {
-                            int d[3][4] = {};
+                        for (int mh = 0; mh < 2; ++mh) {
+                            const int mt = 2 * half + mh;
+                            int d[3][4];
+#pragma unroll
+                            for (int j = 0; j < 3; ++j)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) d[j][e] = (int)kCaMagic;
 #pragma unroll
                             for (int kt = 0; kt < C::KT; ++kt) {
-                                const uint4 a = *reinterpret_cast<const uint4 *>(unit + n * kCacheBlock * DH + ((mt * C::KT + kt) * 32 + lane) * 16);
+                                const uint4 a = *reinterpret_cast<const uint4 *>(codes + ((mt * C::KT + kt) * 32 + lane) * 16);
 #pragma unroll
-                                for (int j = 0; j < 3; ++j) mma_s8s8(d[j], a, qd[n][j][kt][0], qd[n][j][kt][1]);
+                                for (int j = 0; j < 3; ++j) mma_s8s8(d[j], a, qd[0][ND - 1 ? j : 0][kt][0], qd[0][ND - 1 ? j : 0][kt][1]);
                             }
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                scores[(2 * t + (e & 1)) * kCaScoreStride + mt * 16 + g + (e >> 1) * 8] = fmaf((float)(d[0][e] * 256 + d[1][e]), 256.0f, (float)d[2][e]);
+                            for (int e = 0; e < 4; e += 2) {
+                                float v0, v1;
+                                unpack_f32x2(fma_f32x2(fma_f32x2(ca_float2(d[0][e], d[0][e + 1]), base256, ca_float2(d[1][e], d[1][e + 1])), base256, ca_float2(d[2][e], d[2][e + 1])), v0, v1);
+                                scores[(2 * t) * 36 + mh * 16 + g + 4 * e] = v0;
+                                scores[(2 * t + 1) * 36 + mh * 16 + g + 4 * e] = v1;
+                            }
                         }
                         __syncwarp();
-                        const float f = qs[n] * (n ? sc.y : sc.x);
-                        float x[16];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float4 v = *reinterpret_cast<const float4 *>(scores + g * kCaScoreStride + j * 16 + 4 * t);
-                            x[4 * j] = v.x * f;
-                            x[4 * j + 1] = v.y * f;
-                            x[4 * j + 2] = v.z * f;
-                            x[4 * j + 3] = v.w * f;
+                        for (int j = 0; j < 2; ++j) {
+                            const float4 v = *reinterpret_cast<const float4 *>(scores + g * 36 + j * 16 + 4 * t);
+                            x[8 * half + 4 * j] = v.x;
+                            x[8 * half + 4 * j + 1] = v.y;
+                            x[8 * half + 4 * j + 2] = v.z;
+                            x[8 * half + 4 * j + 3] = v.w;
                         }
-                        __syncwarp();  // (the other stream's scores follow in the same place)
-                        if (partly) {
+                        __syncwarp();
+                    }
+                    softmax_step(x, f, partly, sees_g - token0, token, alpha, worth);
+                    uint32_t b[DP][4];
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if ((j >> 2) * 16 + 4 * t + (j & 3) >= sees) x[j] = -INFINITY;
-                        }
-                        alpha[n] = softmax_step(x, m[n], l[n]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t w[4];
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t w[4];
+                        if (DP == 3) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[4 * j + e]);
+                            b[0][j] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
+                        } else {  // (65535 p beside 128: p = 1 stays within 16 bits)
 #pragma unroll
-                            for (int z = 0; z < 3; ++z) {
-                                const uint32_t sel = 0x0040u + (uint32_t)(2 - z) * 0x0011u;
-                                b[n][z][j] = __byte_perm(__byte_perm(w[0], w[1], sel), __byte_perm(w[2], w[3], sel), 0x5410) ^ (z ? 0u : 0x80808080u);
-                            }
+                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(fmaf(x[4 * j + e], 0.9999847412109375f, 128.0f));
                         }
+                        const uint32_t w01 = __byte_perm(w[0], w[1], 0x5140), w23 = __byte_perm(w[2], w[3], 0x5140);
+                        b[DP - 2][j] = __byte_perm(w01, w23, 0x7632);
+                        b[DP - 1][j] = __byte_perm(w01, w23, 0x5410);
                     }
-                    float scale[2][2], worth[2];
+                    // (a row that sees none of the page takes nothing of it, not even a scale that is NaN)
+                    constexpr float kUnit = DP == 3 ? 1.1920928955078125e-7f : 1.0f / 65535.0f;
+                    float scale[2], sv[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        scale[0][e] = __shfl_sync(0xffffffffu, alpha[0], (2 * t + e) * 4);
-                        scale[1][e] = __shfl_sync(0xffffffffu, alpha[1], (2 * t + e) * 4);
-                        // (a row that sees none of the page takes nothing of it, not even a scale that is NaN)
-                        worth[e] = row_sees(k, 2 * t + e) > token0 ? sc.z * 1.1920928955078125e-7f : 0.0f;
+                        scale[e] = __shfl_sync(0xffffffffu, alpha, (2 * t + e) * 4);
+                        sv[e] = __shfl_sync(0xffffffffu, worth, (2 * t + e) * 4);
+                        sv[e] = sees_e[e] > token0 ? sv[e] * sc.z * kUnit : 0.0f;
                     }
+                    const uint64_t scale2 = pack_f32x2(scale[0], scale[1]), sv2 = pack_f32x2(sv[0], sv[1]);
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        uint4 a[2];
+                        int d[DP][4];
 #pragma unroll
-                        for (int kt = 0; kt < 2; ++kt) a[kt] = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
+                        for (int z = 0; z < DP; ++z)
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            int d[3][4] = {};
+                            for (int e = 0; e < 4; ++e) d[z][e] = (int)kCaMagic;
 #pragma unroll
-                            for (int kt = 0; kt < 2; ++kt)
+                        for (int kt = 0; kt < 2; ++kt) {
+                            const uint4 a = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
 #pragma unroll
-                                for (int z = 0; z < 3; ++z) mma_s8u8(d[z], a[kt], b[n][z][2 * kt], b[n][z][2 * kt + 1]);
+                            for (int z = 0; z < DP; ++z) mma_s8u8(d[z], a, b[z][2 * kt], b[z][2 * kt + 1]);
+                        }
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float v = fmaf((float)(d[0][e] * 256 + d[1][e]), 256.0f, (float)d[2][e]);
-                                acc[n][mt][e] = fmaf(v, worth[e & 1], acc[n][mt][e] * scale[n][e & 1]);
-                            }
+                        for (int e = 0; e < NE; e += 2) {
+                            uint64_t v = fma_f32x2(ca_float2(d[0][e], d[0][e + 1]), base256, ca_float2(d[1][e], d[1][e + 1]));
+                            if (DP == 3) v = fma_f32x2(v, base256, ca_float2(d[DP - 1][e], d[DP - 1][e + 1]));
+                            unpack_f32x2(fma_f32x2(v, sv2, mul_f32x2(pack_f32x2(acc[mt][e], acc[mt][e + 1]), scale2)), acc[mt][e], acc[mt][e + 1]);
                         }
                     }
                 }
-            } else {
+            } else if (ok && open_unit && token0 < sees_tile) {
                 // ---- 32 open tokens
-                const int half = k.unit - k.s.pages, rows = min(32, (k.s.length & 63) - 32 * half);
-                uint8_t *mine = ring + stage * C::STAGE;
+                const int rows = min(32, (k.s.length & 63) - 32 * (k.unit - k.s.pages));
                 const uint32_t at = ring_a + stage * C::STAGE;
-                // what lies behind the last row is no value: V's rows there become zero (K's only give scores that are not looked at)
-                for (int e = lane; e < (32 - rows) * (DH / 8); e += 32) *reinterpret_cast<uint4 *>(mine + 2 * 32 * DH * 2 + rows * DH * 2 + e * 16) = make_uint4(0, 0, 0, 0);
-                __syncwarp();
-                const int heads = H * p.group;
-                float alpha[NS], f[NS];
-                uint32_t b[NS][ROWS == 1 ? 1 : 3][2][2];
-                // (a query that is not finite: digits mean nothing, but the products of its bf16 values do; qs is NaN then)
-#pragma unroll
-                for (int n = 0; n < NS; ++n) f[n] = qs[n] == qs[n] ? p.scale_log2 : qs[n];
+                const int q_at = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g);
+                const bool q_there = q_at < k.s.m * p.group;
                 auto q_pair = [&](int n, int col) -> uint32_t {  // q's values col, col + 1 of this lane's column
-                    const int r = ROWS == 1 ? 0 : g, rr = k.tile * ROWS + r;
-                    const bool there = rr < k.s.m * p.group && (ROWS == 8 || g == 4 * n);
-                    if (!there) return 0;
-                    return *reinterpret_cast<const uint32_t *>(p.q + ((size_t)(k.s.row0 + rr / p.group) * 2 + n) * heads * DH + (size_t)(k.head * p.group + rr % p.group) * DH + col);
+                    if (!q_there || (ROWS == 1 && g != 4 * n)) return 0;
+                    return *reinterpret_cast<const uint32_t *>(q_row(n, q_at) + col);
                 };
                 auto k_eight = [&](int n, int mt, int kt) {
                     const int r = mt * 16 + (lane & 15);
                     return ldmatrix4(at + n * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, kt * 2 + (lane >> 4)) * 16);
                 };
-                if constexpr (ROWS == 1) {
-                    float d[2][4] = {};
+                float d[2][4] = {};
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n)
 #pragma unroll
-                        for (int kt = 0; kt < DH / 16; ++kt) {
-                            const uint32_t b0 = q_pair(n, kt * 16 + 2 * t), b1 = q_pair(n, kt * 16 + 8 + 2 * t);
+                    for (int kt = 0; kt < DH / 16; ++kt) {
+                        const int st = ROWS == 1 ? n : stream;
+                        const uint32_t b0 = q_pair(st, kt * 16 + 2 * t), b1 = q_pair(st, kt * 16 + 8 + 2 * t);
 #pragma unroll
-                            for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(n, mt, kt), b0, b1);
-                        }
-                    if (!(t & 1)) {
+                        for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(st, mt, kt), b0, b1);
+                    }
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) {
+                for (int mt = 0; mt < 2; ++mt) {
+                    if (ROWS == 1) {
+                        if (!(t & 1)) {
                             scores[(t >> 1) * kCacheBlock + mt * 16 + g] = d[mt][0];
                             scores[(t >> 1) * kCacheBlock + mt * 16 + g + 8] = d[mt][2];
                         }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) scores[(2 * t + (e & 1)) * 36 + mt * 16 + g + (e >> 1) * 8] = d[mt][e];
                     }
                 }
+                __syncwarp();
+                const float *row = scores + (ROWS == 1 ? my_stream * kCacheBlock : g * 36);
+                float x[8], alpha, worth;
 #pragma unroll
-                for (int n = 0; n < NS; ++n) {
-                    if constexpr (ROWS == 8) {
-                        float d[2][4] = {};
+                for (int j = 0; j < 4; ++j) {  // tokens 8 j + 2 t, 8 j + 2 t + 1
+                    const float2 v = *reinterpret_cast<const float2 *>(row + 8 * j + 2 * t);
+                    x[2 * j] = v.x;
+                    x[2 * j + 1] = v.y;
+                }
+                __syncwarp();
+                // (a query that is not finite: its digits mean nothing, but the products of its bf16 values do; qs is NaN then)
+                softmax_step(x, qs == qs ? p.scale_log2 : qs, true, min(rows, sees_g - token0), [&](int j) { return (j >> 1) * 8 + 2 * t + (j & 1); }, alpha, worth);
+                // p as a sum of three bf16, each the rounding of what the ones before leave
+                uint32_t b[ROWS == 1 ? 1 : 3][2][2];
 #pragma unroll
-                        for (int kt = 0; kt < DH / 16; ++kt) {
-                            const uint32_t b0 = q_pair(n, kt * 16 + 2 * t), b1 = q_pair(n, kt * 16 + 8 + 2 * t);
+                for (int j = 0; j < 4; ++j) {
+                    float a0 = x[2 * j], a1 = x[2 * j + 1];
 #pragma unroll
-                            for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(n, mt, kt), b0, b1);
-                        }
-#pragma unroll
-                        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) scores[(2 * t + (e & 1)) * kCaScoreStride + mt * 16 + g + (e >> 1) * 8] = d[mt][e];
+                    for (int z = 0; z < 3; ++z) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(a0, a1);
+                        const uint32_t w = *reinterpret_cast<const uint32_t *>(&v);
+                        if (ROWS == 8) b[ROWS == 8 ? z : 0][j >> 1][j & 1] = w;
+                        else if (limb == z) b[0][j >> 1][j & 1] = w;
+                        a0 -= bf16lo_to_float(w);
+                        a1 -= bf16hi_to_float(w);
                     }
-                    __syncwarp();
-                    const float *row = scores + (ROWS == 1 ? my_stream * kCacheBlock : g * kCaScoreStride);
-                    const int sees = min(rows, row_sees(k, ROWS == 1 ? 0 : g) - token0);
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {  // tokens 8 j + 2 t, 8 j + 2 t + 1
-                        const float2 v = *reinterpret_cast<const float2 *>(row + 8 * j + 2 * t);
-                        x[2 * j] = 8 * j + 2 * t < sees ? v.x * f[n] : -INFINITY;
-                        x[2 * j + 1] = 8 * j + 2 * t + 1 < sees ? v.y * f[n] : -INFINITY;
-                    }
-                    __syncwarp();
-                    alpha[n] = softmax_step(x, m[n], l[n]);
-                    // p as a sum of three bf16, each the rounding of what the ones before leave
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float a0 = x[2 * j], a1 = x[2 * j + 1];
-#pragma unroll
-                        for (int z = 0; z < 3; ++z) {
-                            const __nv_bfloat162 v = __floats2bfloat162_rn(a0, a1);
-                            const uint32_t w = *reinterpret_cast<const uint32_t *>(&v);
-                            if (ROWS == 8) b[n][ROWS == 8 ? z : 0][j >> 1][j & 1] = w;
-                            else if (limb == z) b[n][0][j >> 1][j & 1] = w;
-                            a0 -= bf16lo_to_float(w);
-                            a1 -= bf16hi_to_float(w);
-                        }
-                        if (ROWS == 1 && limb == 3) b[n][0][j >> 1][j & 1] = 0;
-                    }
+                    if (ROWS == 1 && limb == 3) b[0][j >> 1][j & 1] = 0;
                 }
                 auto v_eight = [&](int mt, int kt) {
                     const int r = kt * 16 + (lane & 7) + (lane >> 4) * 8;
                     return ldmatrix4_trans(at + 2 * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, mt * 2 + (lane >> 3 & 1)) * 16);
                 };
                 if constexpr (ROWS == 1) {
-                    const float scale = __shfl_sync(0xffffffffu, alpha[0], (t >> 1) * 16), wb = t & 1 ? 0.0f : 1.0f;
+                    const float scale = __shfl_sync(0xffffffffu, alpha, (t >> 1) * 16), sv = __shfl_sync(0xffffffffu, worth, (t >> 1) * 16);
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int kt = 0; kt < 2; ++kt) mma_bf16(d, v_eight(mt, kt), b[0][0][kt][0], b[0][0][kt][1]);
-                        acc[0][mt][0] = fmaf(d[1], wb, fmaf(acc[0][mt][0], scale, d[0]));
-                        acc[0][mt][1] = fmaf(d[3], wb, fmaf(acc[0][mt][1], scale, d[2]));
+                        for (int kt = 0; kt < 2; ++kt) mma_bf16(o, v_eight(mt, kt), b[0][kt][0], b[0][kt][1]);
+                        acc[mt][0] = fmaf(t & 1 ? o[0] : o[0] + o[1], sv, acc[mt][0] * scale);
+                        acc[mt][1] = fmaf(t & 1 ? o[2] : o[2] + o[3], sv, acc[mt][1] * scale);
                     }
                 } else {
-                    float scale[2][2];
+                    float scale[2], sv[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        scale[0][e] = __shfl_sync(0xffffffffu, alpha[0], (2 * t + e) * 4);
-                        scale[1][e] = __shfl_sync(0xffffffffu, alpha[NS - 1], (2 * t + e) * 4);
+                        scale[e] = __shfl_sync(0xffffffffu, alpha, (2 * t + e) * 4);
+                        sv[e] = __shfl_sync(0xffffffffu, worth, (2 * t + e) * 4);
                     }
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        const uint4 a[2] = {v_eight(mt, 0), v_eight(mt, 1)};
+                        float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int n = 0; n < NS; ++n) {
-                            float d[4];
+                        for (int kt = 0; kt < 2; ++kt) {
+                            const uint4 a = v_eight(mt, kt);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) d[e] = acc[n][mt][e % NE] * scale[n][e & 1];
-#pragma unroll
-                            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                                for (int z = 0; z < 3; ++z) mma_bf16(d, a[kt], b[n][ROWS == 8 ? z : 0][kt][0], b[n][ROWS == 8 ? z : 0][kt][1]);
-                            // (a row that sees none of these tokens takes nothing of them, not even a value that is NaN)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (row_sees(k, 2 * t + (e & 1)) > token0) acc[n][mt][e % NE] = d[e];
+                            for (int z = 0; z < 3; ++z) mma_bf16(o, a, b[ROWS == 8 ? z : 0][kt][0], b[ROWS == 8 ? z : 0][kt][1]);
                         }
+                        // (a row that sees none of these tokens takes nothing of them, not even a value that is NaN)
+#pragma unroll
+                        for (int e = 0; e < NE; ++e) acc[mt][e] = sees_e[e & 1] > token0 ? fmaf(o[e], sv[e & 1], acc[mt][e] * scale[e & 1]) : acc[mt][e];
                     }
                 }
-                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");  // (the next copy into the stage comes after the zeros)
             }
+            if (open_unit) asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");  // (the next copy into the stage comes after the zeros)
         }
-        __syncwarp();
-        if (ahead_u < u1) {
+        team_sync();
+        if (leads && !dead && ahead_u < u1) {
             fetch(ahead, stage);
             advance(ahead);
             ++ahead_u;
-        } else {
-            loaded &= ~(1u << stage);
         }
+        if (++stage == stages) stage = 0;
 
         // ---- the item's end, or the share's
         const bool item_ends = k.unit == k.s.units - 1;
         if (item_ends || u + 1 == u1) {
             const bool whole = item_ends && !(first_item && begins_inside);
-            float *part = p.parts + ((size_t)worker * 2 + (first_item ? 0 : 1)) * (ROWS * PART);
-            if (!item_ends && !(first_item && begins_inside)) {
-                // the item begins here and goes on elsewhere: this worker's entry names what is to be joined, to the last worker of the item
-                const long long end = u - k.unit + k.s.units;  // (its end in the sequence of units)
-                const int last = (int)((end * workers - 1) / total);
-                join = make_int4(first_item ? 1 : 2, last, k.head, k.tile);
-                join_at = make_int4(k.s.row0, k.s.m, 0, 0);
-            }
+            float *part = my_parts + (first_item && !whole ? 0 : part_floats) + my_tile * (ROWS * C::PART);
+            const CaItem it = {u - k.unit, u - k.unit + k.s.units, k.s.row0, k.s.m, k.head, k.tile};
+            if (u + 1 == u1 && leads && lane == 0) last_item_of[team] = it;
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
             if constexpr (ROWS == 1) {
-                l[0] += __shfl_xor_sync(0xffffffffu, l[0], 1);
-                l[0] += __shfl_xor_sync(0xffffffffu, l[0], 2);
-                const float l1 = __shfl_sync(0xffffffffu, l[0], 0), l2 = __shfl_sync(0xffffffffu, l[0], 16);
-                const float m1 = __shfl_sync(0xffffffffu, m[0], 0), m2 = __shfl_sync(0xffffffffu, m[0], 16);
+                const float l1 = __shfl_sync(0xffffffffu, l, 0), l2 = __shfl_sync(0xffffffffu, l, 16);
+                const float m1 = __shfl_sync(0xffffffffu, m, 0), m2 = __shfl_sync(0xffffffffu, m, 16);
                 const float i1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f, i2 = l2 != 0.0f ? p.lambda * p.out_scale / l2 : 0.0f;
-                const size_t at = ((size_t)(k.s.row0 + k.tile / p.group) * H * p.group + k.head * p.group + k.tile % p.group) * DH;
 #pragma unroll
                 for (int mt = 0; mt < C::MT; ++mt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float v = acc[0][mt][e];
+                        float v = acc[mt][e];
                         v += __shfl_xor_sync(0xffffffffu, v, 1);
                         const float other = __shfl_xor_sync(0xffffffffu, v, 2);  // in lanes t = 0: stream 2's
                         const int dim = mt * 16 + g + 8 * e;
                         if (whole) {
-                            const float y = v * i1 - other * i2;
-                            if (t == 0) {
-                                if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[at + dim] = __float2bfloat16(y);
-                                else reinterpret_cast<float *>(p.out)[at + dim] = y;
-                            }
+                            if (t == 0) ca_write(p, it, k.tile, DH, dim, v * i1 - other * i2);
                         } else if (!(t & 1)) {
                             part[4 + (t >> 1) * DH + dim] = v;
                         }
                     }
                 if (!whole && lane == 0) *reinterpret_cast<float4 *>(part) = make_float4(m1, l1, m2, l2);
             } else {
-#pragma unroll
-                for (int n = 0; n < NS; ++n) {
-                    l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
-                    l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
-                }
-                if (!whole && t == 0) *reinterpret_cast<float4 *>(part + g * PART) = make_float4(m[0], l[0], m[NS - 1], l[NS - 1]);
+                // the second stream's warps leave their sums, of a whole item as they enter the output; the first's finish those
+                if (!whole && t == 0) *reinterpret_cast<float2 *>(part + g * C::PART + 2 * stream) = make_float2(m, l);
+                float inv[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = 2 * t + e, rr = k.tile * ROWS + r;
-                    const float l1 = __shfl_sync(0xffffffffu, l[0], r * 4), l2 = __shfl_sync(0xffffffffu, l[NS - 1], r * 4);
-                    const float i1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f, i2 = l2 != 0.0f ? p.lambda * p.out_scale / l2 : 0.0f;
-                    const bool there = rr < k.s.m * p.group;
-                    const size_t at = ((size_t)(k.s.row0 + rr / p.group) * H * p.group + k.head * p.group + rr % p.group) * DH;
+                    const float le = __shfl_sync(0xffffffffu, l, (2 * t + e) * 4);
+                    inv[e] = !whole ? 1.0f : le != 0.0f ? (stream ? p.lambda : 1.0f) * p.out_scale / le : 0.0f;
+                }
+                if (!whole || stream)
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float v1 = acc[0][mt][(2 * h + e) % NE], v2 = acc[NS - 1][mt][(2 * h + e) % NE];
-                            const int dim = mt * 16 + g + 8 * h;
-                            if (!whole) {
-                                part[r * PART + 4 + dim] = v1;
-                                part[r * PART + 4 + DH + dim] = v2;
-                            } else if (there) {
-                                const float y = v1 * i1 - v2 * i2;
-                                if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[at + dim] = __float2bfloat16(y);
-                                else reinterpret_cast<float *>(p.out)[at + dim] = y;
+                        for (int e = 0; e < NE; ++e) part[(2 * t + (e & 1)) * C::PART + 4 + stream * DH + mt * 16 + g + 8 * (e >> 1)] = acc[mt][e] * inv[e & 1];
+                if (whole) {
+                    team_sync();
+                    if (!stream) {
+#pragma unroll
+                        for (int mt = 0; mt < C::MT; ++mt)
+#pragma unroll
+                            for (int e = 0; e < NE; ++e) {
+                                const int r = 2 * t + (e & 1), dim = mt * 16 + g + 8 * (e >> 1), rr = k.tile * tile_rows + my_tile * 8 + r;
+                                if (rr < k.s.m * p.group) ca_write(p, it, rr, DH, dim, acc[mt][e] * inv[e & 1] - part[r * C::PART + 4 + DH + dim]);
                             }
-                        }
+                    }
                 }
             }
             first_item = false;
         }
         fresh = advance(k);
     }
-    if (lane == 0) {
-        p.items[2 * worker] = join;
-        p.items[2 * worker + 1] = join_at;
+
+    // ---- items that teams of this CTA share
+    __syncthreads();
+    if (!works) return;
+    auto team_of = [&](long long unit) { return (int)(((unit - c0 + 1) * teams - 1) / (c1 - c0)); };
+    auto join_here = [&](const CaItem &it, int from, bool slot1, float *to) {
+        const float *base = p.parts + ((size_t)blockIdx.x * teams_here + from) * 2 * part_floats;
+        ca_join<DH, ROWS>(p, it, team_of(min(it.to, c1) - 1) - from + 1, [&](int j) { return base + (size_t)j * 2 * part_floats + (j == 0 && slot1 ? part_floats : 0); }, to,
+                          member * 32 + lane, team_warps * 32);
+    };
+    float *cta_part = p.cta_parts + (size_t)blockIdx.x * 2 * part_floats;
+    if (team == 0 && first_item_of_cta.from < c0) join_here(first_item_of_cta, 0, false, cta_part);
+    const CaItem it = last_item_of[team];
+    if (it.from >= u0 && it.to > u1) {  // begins in this team's share and goes on
+        const bool goes_on = it.to > c1, slot1 = it.from > c0;
+        join_here(it, team, it.from > u0, goes_on ? cta_part + (slot1 ? part_floats : 0) : nullptr);
+        if (goes_on && leads && lane == 0) {
+            p.items[2 * blockIdx.x] = make_int4(slot1 ? 2 : 1, (int)((it.to * ctas - 1) / total), it.head, it.tile);
+            p.items[2 * blockIdx.x + 1] = make_int4(it.row0, it.m, 0, 0);
+        }
     }
 }
 
-// Joins the parts of the items that several workers shared: block w the one that begins in worker w's share and does not end there, if there is one.
+// Joins the parts of the items that several CTAs shared: block w the one that begins in CTA w's share and does not end there, if there is one.
 template <int DH, int ROWS>
-__global__ void __launch_bounds__(512) cached_attention_join_kernel(CaParams p) {
-    constexpr int PART = 4 + 2 * DH, WAYS = 512 / DH;  // threads: a dim each, the parts dealt to WAYS of them
-    __shared__ float sums[WAYS][2][DH], stat[WAYS][4];
-    const int dim = threadIdx.x % DH, way = threadIdx.x / DH, w0 = blockIdx.x;
+__global__ void __launch_bounds__(256) cached_attention_join_kernel(CaParams p) {
+    const int w0 = blockIdx.x, part_floats = p.tiles * ROWS * (4 + 2 * DH);
     pdl_wait();
-    const int4 item = p.items[2 * w0];
+    const int4 item = p.items[2 * w0], at = p.items[2 * w0 + 1];
     if (!item.x) return;
-    const int4 at = p.items[2 * w0 + 1];
-    const int H = p.c.H, n = item.y - w0 + 1;
-    for (int r = 0; r < ROWS; ++r) {
-        const int rr = item.w * ROWS + r;
-        if (rr >= at.y * p.group) break;
-        float m1 = -INFINITY, l1 = 0.0f, m2 = -INFINITY, l2 = 0.0f, o1 = 0.0f, o2 = 0.0f;
-#pragma unroll 4
-        for (int j = way; j < n; j += WAYS) {
-            const float *part = p.parts + ((size_t)(w0 + j) * 2 + (j == 0 && item.x == 2 ? 1 : 0)) * (ROWS * PART) + r * PART;
-            const float4 s = *reinterpret_cast<const float4 *>(part);
-            const float v1 = part[4 + dim], v2 = part[4 + DH + dim];
-            const float n1 = fmaxf(m1, s.x), n2 = fmaxf(m2, s.z), b1 = n1 == -INFINITY ? 0.0f : n1, b2 = n2 == -INFINITY ? 0.0f : n2;
-            const float a1 = exp2_approx(m1 - b1), c1 = exp2_approx(s.x - b1), a2 = exp2_approx(m2 - b2), c2 = exp2_approx(s.z - b2);
-            l1 = l1 * a1 + s.y * c1;
-            o1 = o1 * a1 + v1 * c1;
-            l2 = l2 * a2 + s.w * c2;
-            o2 = o2 * a2 + v2 * c2;
-            m1 = n1;
-            m2 = n2;
-        }
-        sums[way][0][dim] = o1;
-        sums[way][1][dim] = o2;
-        if (dim == 0) {
-            stat[way][0] = m1;
-            stat[way][1] = l1;
-            stat[way][2] = m2;
-            stat[way][3] = l2;
-        }
-        __syncthreads();
-        if (way == 0) {
-            float y[2];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float top = -INFINITY, l = 0.0f, o = 0.0f;
-#pragma unroll
-                for (int j = 0; j < WAYS; ++j) top = fmaxf(top, stat[j][2 * s]);
-                const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-                for (int j = 0; j < WAYS; ++j) {
-                    const float a = exp2_approx(stat[j][2 * s] - base);
-                    l += stat[j][2 * s + 1] * a;
-                    o += sums[j][s][dim] * a;
-                }
-                y[s] = l != 0.0f ? o / l : 0.0f;
-            }
-            const float v = (y[0] - p.lambda * y[1]) * p.out_scale;
-            const size_t o = ((size_t)(at.x + rr / p.group) * H * p.group + item.z * p.group + rr % p.group) * DH + dim;
-            if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[o] = __float2bfloat16(v);
-            else reinterpret_cast<float *>(p.out)[o] = v;
-        }
-        __syncthreads();
-    }
+    const CaItem it = {0, 0, at.x, at.y, item.z, item.w};
+    const float *base = p.cta_parts + (size_t)w0 * 2 * part_floats;
+    ca_join<DH, ROWS>(p, it, item.y - w0 + 1, [&](int j) { return base + (size_t)j * 2 * part_floats + (j == 0 && item.x == 2 ? part_floats : 0); }, nullptr, threadIdx.x, blockDim.x);
 }
 
-// One row an item where the call's rows are single tokens with heads of their own (on average: any call is right in either form).
-static int ca_rows(int64_t n_seqs, int64_t n_rows, int group) { return n_rows * group <= n_seqs ? 1 : 8; }
+// How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows, as many to a team as
+// the sequences have on average, up to four (any call is right in any of these forms).
+struct CaForm {
+    int rows, tiles, teams, stages, threads;
+};
+static CaForm ca_form(int head_dim, int64_t n_seqs, int64_t n_rows, int group) {
+    if (n_rows * group <= n_seqs) return head_dim == 64 ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
+    const int64_t rows = (n_rows * group + n_seqs - 1) / n_seqs;
+    const int tiles = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+    // (two units of a ring at least)
+    const int all = head_dim == 64 ? 16 : 8, most = all / 2, teams = 8 / tiles < most ? 8 / tiles : most;
+    return CaForm{8, tiles, teams, all / teams, teams * tiles * 64};
+}
 
-template <int DH, int ROWS>
-static cudaError_t launch_cached_attention(const CaParams &p, cudaStream_t stream) {
-    using C = CaCfg<DH>;
-    constexpr int SMEM = C::WARPS * (kCaStages * C::STAGE + kCaScoreBytes<ROWS>) + (kCacheMaxSeqs + 1) * 8;
-    static_assert(SMEM <= 226 * 1024, "shared memory of a CTA");
+template <int DH, int ROWS, int DP>
+static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaStream_t stream) {
+    using C = CaCfg<DH, ROWS>;
+    static_assert(C::SMEM <= 226 * 1024, "shared memory of a CTA");
     static std::atomic<unsigned long long> attr_done{0};
-    cudaError_t e = ensure_dynamic_smem(cached_attention_kernel<DH, ROWS>, SMEM, attr_done);
+    cudaError_t e = ensure_dynamic_smem(cached_attention_kernel<DH, ROWS, DP>, C::SMEM, attr_done);
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;
     const int grid = sms < kCaMaxSms ? sms : kCaMaxSms;
-    cached_attention_kernel<DH, ROWS><<<grid, C::THREADS, SMEM, stream>>>(p);
+    cached_attention_kernel<DH, ROWS, DP><<<grid, threads, C::SMEM, stream>>>(p);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(grid * C::WARPS));
-    cfg.blockDim = dim3(512);
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -821,9 +872,10 @@ static cudaError_t launch_cached_attention(const CaParams &p, cudaStream_t strea
     return cudaSuccess;
 }
 
-static size_t ca_items_bytes(int head_dim) { return align_up((size_t)kCaMaxSms * (head_dim == 64 ? CaCfg<64>::WARPS : CaCfg<128>::WARPS) * 2 * sizeof(int4), 256); }
-static size_t ca_workspace(int head_dim, int rows) {
-    return ca_items_bytes(head_dim) + align_up((size_t)kCaMaxSms * (head_dim == 64 ? CaCfg<64>::WARPS : CaCfg<128>::WARPS) * 2 * rows * (4 + 2 * head_dim) * 4, 256);
+static size_t ca_items_bytes() { return align_up((size_t)kCaMaxSms * 2 * sizeof(int4), 256); }
+static size_t ca_cta_parts_bytes(int head_dim, const CaForm &f) { return align_up((size_t)kCaMaxSms * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256); }
+static size_t ca_workspace(int head_dim, const CaForm &f) {
+    return ca_items_bytes() + ca_cta_parts_bytes(head_dim, f) + align_up((size_t)kCaMaxSms * f.teams * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256);
 }
 
 }  // namespace hgf
@@ -832,37 +884,44 @@ using namespace hgf;
 
 extern "C" size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads) {
     if (!cache || (cache->head_dim != 64 && cache->head_dim != 128) || cache->n_heads <= 0 || n_heads <= 0 || n_rows <= 0 || n_seqs <= 0) return 256;
-    return ca_workspace(cache->head_dim, ca_rows(n_seqs, n_rows, n_heads / cache->n_heads));
+    return ca_workspace(cache->head_dim, ca_form(cache->head_dim, n_seqs, n_rows, n_heads / cache->n_heads));
 }
 
 extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const void *q, int64_t n_rows, int32_t n_heads, const int32_t *slots,
                                                 const int32_t *starts, int64_t n_seqs, float lambda, float out_scale, void *out, void *workspace,
-                                                size_t workspace_bytes, uint32_t flags, void *stream) {
+                                                size_t workspace_bytes, uint32_t flags, void *stream_) {
     if (!q || !slots || !starts || !out || n_rows <= 0 || n_heads <= 0 || (flags & ~HGF_FLAG_OUT_BF16)) return HGF_ERR_INVALID_ARG;
     CaParams p = {};
     if (const hgf_status st = parse_cache(cache, n_seqs, &p.c)) return st;
     if (n_heads % cache->n_heads || n_heads > 65535 || n_rows > (1 << 24) || n_rows * (n_heads / cache->n_heads) > 0x3fffffffll) return HGF_ERR_UNSUPPORTED_SHAPE;
     if (((uintptr_t)q | (uintptr_t)out) & 15u) return HGF_ERR_MISALIGNED;
-    const int group = n_heads / cache->n_heads, rows = ca_rows(n_seqs, n_rows, group), dh = cache->head_dim;
-    if (!workspace || workspace_bytes < ca_workspace(dh, rows)) return HGF_ERR_WORKSPACE;
+    const int group = n_heads / cache->n_heads, dh = cache->head_dim;
+    const CaForm f = ca_form(dh, n_seqs, n_rows, group);
+    if (!workspace || workspace_bytes < ca_workspace(dh, f)) return HGF_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255u) return HGF_ERR_MISALIGNED;
     p.q = (const __nv_bfloat16 *)q;
     p.slots = slots;
     p.starts = starts;
     p.out = out;
     p.items = (int4 *)workspace;
-    p.parts = (float *)((char *)workspace + ca_items_bytes(dh));
+    p.cta_parts = (float *)((char *)workspace + ca_items_bytes());
+    p.parts = (float *)((char *)p.cta_parts + ca_cta_parts_bytes(dh, f));
     p.status = device_status_word();
     if (!p.status) return HGF_ERR_CUDA;
     p.n_seqs = (int)n_seqs;
     p.n_rows = (int)n_rows;
     p.group = group;
     p.bf16 = (flags & HGF_FLAG_OUT_BF16) != 0;
+    p.teams = f.teams;
+    p.tiles = f.tiles;
+    p.stages = f.stages;
     p.lambda = lambda;
     p.out_scale = out_scale;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)dh));
+    const cudaStream_t stream = (cudaStream_t)stream_;
     cudaError_t e;
-    if (dh == 64) e = rows == 1 ? launch_cached_attention<64, 1>(p, (cudaStream_t)stream) : launch_cached_attention<64, 8>(p, (cudaStream_t)stream);
-    else e = rows == 1 ? launch_cached_attention<128, 1>(p, (cudaStream_t)stream) : launch_cached_attention<128, 8>(p, (cudaStream_t)stream);
+    if (f.rows == 1) e = dh == 64 ? launch_cached_attention<64, 1, 3>(p, f.threads, stream) : launch_cached_attention<128, 1, 3>(p, f.threads, stream);
+    else if (p.bf16) e = dh == 64 ? launch_cached_attention<64, 8, 2>(p, f.threads, stream) : launch_cached_attention<128, 8, 2>(p, f.threads, stream);
+    else e = dh == 64 ? launch_cached_attention<64, 8, 3>(p, f.threads, stream) : launch_cached_attention<128, 8, 3>(p, f.threads, stream);
     return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
 }

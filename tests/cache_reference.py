@@ -114,13 +114,14 @@ class Reference:
         return out
 
 
-def attention(values, q, m, heads, lam, out_scale):
+def attention(values, q, m, heads, lam, out_scale, coarse=False):
     """values [3][H][n][dh]; q float64 [m][2][heads][dh], the last m of n tokens -> (out [m][heads][dh], tolerance of each row and head).
 
     The tolerance follows the kernel's number formats: q to 2^-22 of its row's largest magnitude (a score is off by that times the sum of |k|), scores and
     exponentials in binary32 (four roundings of the score's size, 2^-22 of the exponential; a score's absolute error is a probability's relative
     one, twice with the normalisation), probabilities to 2^-24 of the largest (twice that, with what the sum has left of it), sums of one term a page in
-    binary32; all of it times the largest |v| and both streams' weights."""
+    binary32; all of it times the largest |v| and both streams' weights.  `coarse`: probabilities to 2^-17 of the largest in their page of 64, so a page's
+    are off by 64 * 2^-17 of its largest at most, which is no more than its weight: all of them by 2^-11 of the sum."""
     _, H, n, dh = values.shape
     out, tol = np.zeros((m, heads, dh)), np.zeros((m, heads))
     for j in range(m):
@@ -135,7 +136,7 @@ def attention(values, q, m, heads, lam, out_scale):
                 p = np.exp(s - s.max())
                 out[j, h] += w * (1 if st == 0 else -1) * (p @ kv[2]) / p.sum()
                 ds = 2.0 ** -22 * np.abs(q[j, st, h]).max() * np.abs(kv[st]).sum(1).max() / np.sqrt(dh) + 4 * 2.0 ** -24 * np.abs(kv[st] * q[j, st, h]).sum(1).max() / np.sqrt(dh)
-                tol[j, h] += abs(w) * big * (2 * (ds + 2.0 ** -21) + 2 * sees * 2.0 ** -24 / p.sum() + (sees / BLOCK + 20) * 2.0 ** -23)
+                tol[j, h] += abs(w) * big * (2 * (ds + 2.0 ** -21) + 2 * sees * 2.0 ** -24 / p.sum() + (sees / BLOCK + 20) * 2.0 ** -23 + (2.0 ** -11 if coarse else 0))
     return out * out_scale, tol * abs(out_scale)
 
 
