@@ -51,15 +51,16 @@ struct CaParams {
     float lambda, out_scale, scale_log2;
 };
 
-__device__ __forceinline__ void mma_s8s8(int (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
-                 : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+// d = c + a b; c may be d.
+__device__ __forceinline__ void mma_s8s8(int (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1, const int (&c)[4]) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};\n"
+                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+                 : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
-__device__ __forceinline__ void mma_s8u8(int (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
-                 : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+__device__ __forceinline__ void mma_s8u8(int (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1, const int (&c)[4]) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};\n"
+                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+                 : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
@@ -127,36 +128,43 @@ __device__ __forceinline__ void ca_write(const CaParams &p, const CaItem &it, in
     else reinterpret_cast<float *>(p.out)[o] = y;
 }
 
-// Joins n parts of an item, in order: at(j) is the j-th.  `to`: where the result stays a part, null if it is the output.  Threads deal (row, dim).
+// Joins n parts of an item, in order: at(j) is the j-th.  `to`: where the result stays a part, null if it is the output.  Threads deal (row, four dims) of
+// `rows` rows from row0 on.
 template <int DH, int ROWS, class F>
-__device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int n, F at, float *to, int thread, int threads) {
-    constexpr int PART = 4 + 2 * DH;
-    const int rows = min(ROWS * p.tiles, it.m * p.group - it.tile * ROWS * p.tiles);
-    for (int e = thread; e < rows * DH; e += threads) {
-        const int r = e / DH, dim = e % DH;
-        float m1 = -INFINITY, l1 = 0.0f, m2 = -INFINITY, l2 = 0.0f, o1 = 0.0f, o2 = 0.0f;
+__device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int n, F at, float *to, int row0, int rows, int thread, int threads) {
+    constexpr int PART = 4 + 2 * DH, FOURS = DH / 4;
+    const int all = ROWS * p.tiles, end = min(min(row0 + rows, all), it.m * p.group - it.tile * all);
+    for (int e = row0 * FOURS + thread; e < end * FOURS; e += threads) {
+        const int r = e / FOURS, dim = e % FOURS * 4;
+        float m1 = -INFINITY, l1 = 0.0f, m2 = -INFINITY, l2 = 0.0f, o1[4] = {}, o2[4] = {};
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const float *part = at(j) + r * PART;
-            const float4 s = *reinterpret_cast<const float4 *>(part);
-            const float v1 = part[4 + dim], v2 = part[4 + DH + dim];
+            const float4 s = *reinterpret_cast<const float4 *>(part), v1 = *reinterpret_cast<const float4 *>(part + 4 + dim), v2 = *reinterpret_cast<const float4 *>(part + 4 + DH + dim);
             const float n1 = fmaxf(m1, s.x), n2 = fmaxf(m2, s.z), b1 = n1 == -INFINITY ? 0.0f : n1, b2 = n2 == -INFINITY ? 0.0f : n2;
             const float a1 = exp2_approx(m1 - b1), c1 = exp2_approx(s.x - b1), a2 = exp2_approx(m2 - b2), c2 = exp2_approx(s.z - b2);
+            const float w1[4] = {v1.x, v1.y, v1.z, v1.w}, w2[4] = {v2.x, v2.y, v2.z, v2.w};
             l1 = l1 * a1 + s.y * c1;
-            o1 = o1 * a1 + v1 * c1;
             l2 = l2 * a2 + s.w * c2;
-            o2 = o2 * a2 + v2 * c2;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                o1[d] = o1[d] * a1 + w1[d] * c1;
+                o2[d] = o2[d] * a2 + w2[d] * c2;
+            }
             m1 = n1;
             m2 = n2;
         }
         if (to) {
             float *part = to + r * PART;
             if (dim == 0) *reinterpret_cast<float4 *>(part) = make_float4(m1, l1, m2, l2);
-            part[4 + dim] = o1;
-            part[4 + DH + dim] = o2;
+            *reinterpret_cast<float4 *>(part + 4 + dim) = make_float4(o1[0], o1[1], o1[2], o1[3]);
+            *reinterpret_cast<float4 *>(part + 4 + DH + dim) = make_float4(o2[0], o2[1], o2[2], o2[3]);
         } else {
-            const float y1 = l1 != 0.0f ? o1 / l1 : 0.0f, y2 = l2 != 0.0f ? o2 / l2 : 0.0f;
-            ca_write(p, it, it.tile * ROWS * p.tiles + r, DH, dim, (y1 - p.lambda * y2) * p.out_scale);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const float y1 = l1 != 0.0f ? o1[d] / l1 : 0.0f, y2 = l2 != 0.0f ? o2[d] / l2 : 0.0f;
+                ca_write(p, it, it.tile * all + r, DH, dim + d, (y1 - p.lambda * y2) * p.out_scale);
+            }
         }
     }
 }
@@ -286,9 +294,9 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 
     // ---- the ring: the leading warp fetches, page numbers 32 at a time, one bulk copy a unit
     int pages32 = 0, pages_at = -32, pages_seq = -1;
-    auto fetch = [&](const CaCursor &k, int stage) {
+    auto fetch = [&](const CaCursor &k, int sees, int stage) {
         const uint32_t bar = bars_a + stage * 8, dst = ring_a + stage * C::STAGE;
-        if (unit_token(k) >= last_sees(k.s, k.tile)) return;  // (nobody waits for it either)
+        if (unit_token(k) >= sees) return;  // (nobody waits for it either)
         if (k.unit < k.s.pages) {
             if (pages_seq != k.seq || (k.unit & ~31) != pages_at) {
                 pages_seq = k.seq;
@@ -337,12 +345,13 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     if (works) place(u0, k);
     ahead = k;
     long long ahead_u = u0;
+    int ahead_sees = works ? last_sees(k.s, k.tile) : 0;  // tokens that the last row of the item sees
+    auto fetch_next = [&](int stage) {
+        fetch(ahead, ahead_sees, stage);
+        if (++ahead_u < u1 && advance(ahead)) ahead_sees = last_sees(ahead.s, ahead.tile);
+    };
     if (leads)
-        for (int s = 0; s < stages && ahead_u < u1; ++s) {
-            fetch(ahead, s);
-            advance(ahead);
-            ++ahead_u;
-        }
+        for (int s = 0; s < stages && ahead_u < u1; ++s) fetch_next(s);
     if (works && team == 0 && lane == 0 && leads) first_item_of_cta = {u0 - k.unit, u0 - k.unit + k.s.units, k.s.row0, k.s.m, k.head, k.tile};
 
     // ---- state of the item
@@ -352,7 +361,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     float m = -INFINITY, l = 0.0f, acc[C::MT][NE];
     uint32_t qd[ROWS == 1 ? 2 : 1][ND][C::KT][2];  // right operand of the scores: digits of q (ROWS = 1: for K1 and for K2)
     float qs = 0.0f;                               // what a digit sum is worth, with 1 / sqrt(d) and log2 e
-    int sees_g = 0, sees_e[2] = {0, 0}, sees_tile = 0, sees_all = 0;  // tokens that row g, rows 2 t and 2 t + 1, any row, every row of the tile sees
+    int sees_g = 0, sees_e[2] = {0, 0}, sees_tile = 0, sees_all = 0, sees_item = 0;  // tokens that row g, rows 2 t and 2 t + 1, any row, every row of the tile, any of the item sees
     const int my_stream = ROWS == 1 ? lane >> 4 : stream, limb = g & 3;
     const uint32_t limb_sel = 0x0040u + (uint32_t)((2 - limb) & 3) * 0x0011u;  // byte 2 - limb of two words
     const uint32_t limb_xor = limb == 0 ? 0x80808080u : 0u, limb_keep = limb == 3 ? 0u : 0xffffffffu;
@@ -369,6 +378,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 #pragma unroll
             for (int e = 0; e < NE; ++e) acc[a][e] = 0.0f;
         const int base = k.tile * tile_rows + my_tile * ROWS, there = k.s.m * p.group;
+        sees_item = last_sees(k.s, k.tile);
         if (ROWS == 1) {
             sees_g = sees_tile = sees_all = row_sees(k.s, base);
         } else {
@@ -455,6 +465,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         l = fmaf(l, alpha, s * worth);
     };
 
+    int magic[4] = {(int)kCaMagic, (int)kCaMagic, (int)kCaMagic, (int)kCaMagic};
     const bool begins_inside = works && k.unit != 0;  // the share's first item began in another share
     bool fresh = true, first_item = true;
     // A warp whose wait ran out computes and fetches no more, but takes its steps to the end: the others of its team meet it at their barrier.
@@ -464,7 +475,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         if (fresh) begin_item();
         const uint8_t *unit = ring + stage * C::STAGE;
         const int token0 = unit_token(k);
-        if (token0 < last_sees(k.s, k.tile)) {
+        if (token0 < sees_item) {
             if (!dead) {
                 if (arrived(stage, false)) {
                     phases ^= 1u << stage;
@@ -495,13 +506,13 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     const float wa = t & 1 ? 1.0f : 65536.0f, wb = t & 1 ? 0.0f : 256.0f;
 #pragma unroll
                     for (int mt = 0; mt < 4; ++mt) {
-                        int d[4] = {(int)kCaMagic, (int)kCaMagic, (int)kCaMagic, (int)kCaMagic};
+                        int d[4];
 #pragma unroll
                         for (int n = 0; n < 2; ++n)
 #pragma unroll
                             for (int kt = 0; kt < C::KT; ++kt) {
                                 const uint4 a = *reinterpret_cast<const uint4 *>(unit + n * kCacheBlock * DH + ((mt * C::KT + kt) * 32 + lane) * 16);
-                                mma_s8s8(d, a, qd[n][0][kt][0], qd[n][0][kt][1]);
+                                mma_s8s8(d, a, qd[n][0][kt][0], qd[n][0][kt][1], n + kt ? d : magic);
                             }
                         float lo = fmaf(ca_float(d[0]), wa, ca_float(d[1]) * wb), hi = fmaf(ca_float(d[2]), wa, ca_float(d[3]) * wb);
                         lo += __shfl_xor_sync(0xffffffffu, lo, 1);
@@ -531,11 +542,11 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     const float va = sv * (t & 1 ? 1.1920928955078125e-7f : 0.0078125f), vb = t & 1 ? 0.0f : sv * 3.0517578125e-5f;
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        int d[4] = {(int)kCaMagic, (int)kCaMagic, (int)kCaMagic, (int)kCaMagic};
+                        int d[4];
 #pragma unroll
                         for (int kt = 0; kt < 2; ++kt) {
                             const uint4 a = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
-                            mma_s8u8(d, a, b[2 * kt], b[2 * kt + 1]);
+                            mma_s8u8(d, a, b[2 * kt], b[2 * kt + 1], kt ? d : magic);
                         }
                         acc[mt][0] = fmaf(ca_float(d[0]), va, fmaf(ca_float(d[1]), vb, acc[mt][0] * scale));
                         acc[mt][1] = fmaf(ca_float(d[2]), va, fmaf(ca_float(d[3]), vb, acc[mt][1] * scale));
@@ -550,14 +561,10 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                             const int mt = 2 * half + mh;
                             int d[3][4];
 #pragma unroll
-                            for (int j = 0; j < 3; ++j)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) d[j][e] = (int)kCaMagic;
-#pragma unroll
                             for (int kt = 0; kt < C::KT; ++kt) {
                                 const uint4 a = *reinterpret_cast<const uint4 *>(codes + ((mt * C::KT + kt) * 32 + lane) * 16);
 #pragma unroll
-                                for (int j = 0; j < 3; ++j) mma_s8s8(d[j], a, qd[0][ND - 1 ? j : 0][kt][0], qd[0][ND - 1 ? j : 0][kt][1]);
+                                for (int j = 0; j < 3; ++j) mma_s8s8(d[j], a, qd[0][ND - 1 ? j : 0][kt][0], qd[0][ND - 1 ? j : 0][kt][1], kt ? d[j] : magic);
                             }
 #pragma unroll
                             for (int e = 0; e < 4; e += 2) {
@@ -609,14 +616,10 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     for (int mt = 0; mt < C::MT; ++mt) {
                         int d[DP][4];
 #pragma unroll
-                        for (int z = 0; z < DP; ++z)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) d[z][e] = (int)kCaMagic;
-#pragma unroll
                         for (int kt = 0; kt < 2; ++kt) {
                             const uint4 a = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
 #pragma unroll
-                            for (int z = 0; z < DP; ++z) mma_s8u8(d[z], a, b[z][2 * kt], b[z][2 * kt + 1]);
+                            for (int z = 0; z < DP; ++z) mma_s8u8(d[z], a, b[z][2 * kt], b[z][2 * kt + 1], kt ? d[z] : magic);
                         }
 #pragma unroll
                         for (int e = 0; e < NE; e += 2) {
@@ -729,11 +732,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
             if (open_unit) asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");  // (the next copy into the stage comes after the zeros)
         }
         team_sync();
-        if (leads && !dead && ahead_u < u1) {
-            fetch(ahead, stage);
-            advance(ahead);
-            ++ahead_u;
-        }
+        if (leads && !dead && ahead_u < u1) fetch_next(stage);
         if (++stage == stages) stage = 0;
 
         // ---- the item's end, or the share's
@@ -803,7 +802,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     auto join_here = [&](const CaItem &it, int from, bool slot1, float *to) {
         const float *base = p.parts + ((size_t)blockIdx.x * teams_here + from) * 2 * part_floats;
         ca_join<DH, ROWS>(p, it, team_of(min(it.to, c1) - 1) - from + 1, [&](int j) { return base + (size_t)j * 2 * part_floats + (j == 0 && slot1 ? part_floats : 0); }, to,
-                          member * 32 + lane, team_warps * 32);
+                          0, tile_rows, member * 32 + lane, team_warps * 32);
     };
     float *cta_part = p.cta_parts + (size_t)blockIdx.x * 2 * part_floats;
     if (team == 0 && first_item_of_cta.from < c0) join_here(first_item_of_cta, 0, false, cta_part);
@@ -818,7 +817,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     }
 }
 
-// Joins the parts of the items that several CTAs shared: block w the one that begins in CTA w's share and does not end there, if there is one.
+// Joins the parts of the items that several CTAs shared: block w the one that begins in CTA w's share and does not end there, if there is one; eight rows each.
 template <int DH, int ROWS>
 __global__ void __launch_bounds__(256) cached_attention_join_kernel(CaParams p) {
     const int w0 = blockIdx.x, part_floats = p.tiles * ROWS * (4 + 2 * DH);
@@ -827,7 +826,8 @@ __global__ void __launch_bounds__(256) cached_attention_join_kernel(CaParams p) 
     if (!item.x) return;
     const CaItem it = {0, 0, at.x, at.y, item.z, item.w};
     const float *base = p.cta_parts + (size_t)w0 * 2 * part_floats;
-    ca_join<DH, ROWS>(p, it, item.y - w0 + 1, [&](int j) { return base + (size_t)j * 2 * part_floats + (j == 0 && item.x == 2 ? part_floats : 0); }, nullptr, threadIdx.x, blockDim.x);
+    ca_join<DH, ROWS>(p, it, item.y - w0 + 1, [&](int j) { return base + (size_t)j * 2 * part_floats + (j == 0 && item.x == 2 ? part_floats : 0); }, nullptr, 8 * blockIdx.y, 8,
+                      threadIdx.x, blockDim.x);
 }
 
 // How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows, as many to a team as
@@ -858,8 +858,8 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(256);
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)p.tiles);
+    cfg.blockDim = dim3(ROWS * DH / 4);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
