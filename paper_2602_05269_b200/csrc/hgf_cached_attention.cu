@@ -34,7 +34,9 @@ struct CaCfg {
     static constexpr int KT = DH / 32, MT = DH / 16;
     static constexpr int SCORES = ROWS == 1 ? 2 * kCacheBlock * 4 : 8 * 36 * 4;  // bytes a warp; rows 36 floats apart: eight rows' writes hit all banks
     static constexpr int PART = 4 + 2 * DH;                      // floats: maximum and sum of stream 1, of stream 2, sums of values of both
-    static constexpr int SMEM = STAGES * STAGE + WARPS * SCORES + (kCacheMaxSeqs + 1) * 8;
+    // (prefix sums, rounded up to 16 bytes; the parts of single tokens, two a warp, in shared memory)
+    static constexpr int PREFIX = (kCacheMaxSeqs + 2) * 8, PARTS = ROWS == 1 ? WARPS * 2 * PART * 4 : 0;
+    static constexpr int SMEM = STAGES * STAGE + WARPS * SCORES + PREFIX + PARTS;
 };
 
 struct CaParams {
@@ -44,7 +46,7 @@ struct CaParams {
     void *out;
     int4 *items;          // [CTAs][2]: what the joining kernel does for a CTA
     float *cta_parts;     // [CTAs][2][tiles][ROWS][PART]
-    float *parts;         // [CTAs][teams][2][tiles][ROWS][PART]
+    float *parts;         // [CTAs][teams][2][tiles][ROWS][PART], ROWS = 8
     unsigned int *status;
     int n_seqs, n_rows, group, bf16;
     int teams, tiles, stages;  // of a CTA; of a team; of a team's ring
@@ -84,6 +86,13 @@ __device__ __forceinline__ float exp2_approx(float x) {
 }
 
 
+constexpr uint32_t kCaMagic = 0x4b400000u;      // 1.5 * 2^23: an accumulator that starts there is that float plus its sum
+constexpr float kCaMagicF = 12582912.0f;
+__device__ __forceinline__ float ca_float(int d) { return __int_as_float(d) - kCaMagicF; }
+__device__ __forceinline__ uint64_t ca_float2(int a, int b) {
+    return add_f32x2(pack_f32x2(__int_as_float(a), __int_as_float(b)), pack_f32x2(-kCaMagicF, -kCaMagicF));
+}
+
 // A sequence of the call.
 struct CaSeq {
     int slot, row0, m, length, pages, units, tiles;
@@ -107,9 +116,17 @@ __device__ __forceinline__ CaSeq ca_sequence(const CaParams &p, int rows, int i)
     }
     s.pages = s.length >> 6;
     const int open = s.length & 63;
-    s.units = s.pages + (open > 0) + (open > 32);
+    // (one more for what an item costs apart from its units, to begin and to end: no token is in it, so nothing is read)
+    s.units = s.length ? s.pages + (open > 0) + (open > 32) + 1 : 0;
     s.tiles = (s.m * p.group + rows - 1) / rows;
     return s;
+}
+// total * i / n and its inverse, the share of n that `unit` is in; i and n at most 1024 (a 64-bit division takes some 150 clocks, a 32-bit one 30).
+__device__ __forceinline__ long long ca_share(long long total, int i, int n) {
+    return total < (1 << 21) ? (long long)((uint32_t)total * (uint32_t)i / (uint32_t)n) : total * i / n;
+}
+__device__ __forceinline__ int ca_share_of(long long total, long long unit, int n) {
+    return total < (1 << 21) ? (int)((((uint32_t)unit + 1) * (uint32_t)n - 1) / (uint32_t)total) : (int)(((unit + 1) * n - 1) / total);
 }
 // A unit's place: its sequence, the item's rows and head, its number in the item.
 struct CaCursor {
@@ -128,52 +145,48 @@ __device__ __forceinline__ void ca_write(const CaParams &p, const CaItem &it, in
     else reinterpret_cast<float *>(p.out)[o] = y;
 }
 
-// Joins n parts of an item, in order: at(j) is the j-th.  `to`: where the result stays a part, null if it is the output.  Threads deal (row, four dims) of
-// `rows` rows from row0 on.
-template <int DH, int ROWS, class F>
-__device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int n, F at, float *to, int row0, int rows, int thread, int threads) {
-    constexpr int PART = 4 + 2 * DH, FOURS = DH / 4;
-    const int all = ROWS * p.tiles, end = min(min(row0 + rows, all), it.m * p.group - it.tile * all);
-    for (int e = row0 * FOURS + thread; e < end * FOURS; e += threads) {
-        const int r = e / FOURS, dim = e % FOURS * 4;
-        float m1 = -INFINITY, l1 = 0.0f, m2 = -INFINITY, l2 = 0.0f, o1[4] = {}, o2[4] = {};
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) {
-            const float *part = at(j) + r * PART;
-            const float4 s = *reinterpret_cast<const float4 *>(part), v1 = *reinterpret_cast<const float4 *>(part + 4 + dim), v2 = *reinterpret_cast<const float4 *>(part + 4 + DH + dim);
-            const float n1 = fmaxf(m1, s.x), n2 = fmaxf(m2, s.z), b1 = n1 == -INFINITY ? 0.0f : n1, b2 = n2 == -INFINITY ? 0.0f : n2;
-            const float a1 = exp2_approx(m1 - b1), c1 = exp2_approx(s.x - b1), a2 = exp2_approx(m2 - b2), c2 = exp2_approx(s.z - b2);
-            const float w1[4] = {v1.x, v1.y, v1.z, v1.w}, w2[4] = {v2.x, v2.y, v2.z, v2.w};
-            l1 = l1 * a1 + s.y * c1;
-            l2 = l2 * a2 + s.w * c2;
+// What parts of an item add up to, for four dims of a row.
+struct CaSum {
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {}, o[2][4] = {};
+
+    __device__ __forceinline__ void add(const float4 &ml, const float4 &v1, const float4 &v2) {
+        const float pm[2] = {ml.x, ml.z}, pl[2] = {ml.y, ml.w}, v[2][4] = {{v1.x, v1.y, v1.z, v1.w}, {v2.x, v2.y, v2.z, v2.w}};
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                o1[d] = o1[d] * a1 + w1[d] * c1;
-                o2[d] = o2[d] * a2 + w2[d] * c2;
-            }
-            m1 = n1;
-            m2 = n2;
-        }
-        if (to) {
-            float *part = to + r * PART;
-            if (dim == 0) *reinterpret_cast<float4 *>(part) = make_float4(m1, l1, m2, l2);
-            *reinterpret_cast<float4 *>(part + 4 + dim) = make_float4(o1[0], o1[1], o1[2], o1[3]);
-            *reinterpret_cast<float4 *>(part + 4 + DH + dim) = make_float4(o2[0], o2[1], o2[2], o2[3]);
-        } else {
+        for (int s = 0; s < 2; ++s) {
+            const float now = fmaxf(m[s], pm[s]), base = now == -INFINITY ? 0.0f : now, a = exp2_approx(m[s] - base), c = exp2_approx(pm[s] - base);
+            l[s] = l[s] * a + pl[s] * c;
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const float y1 = l1 != 0.0f ? o1[d] / l1 : 0.0f, y2 = l2 != 0.0f ? o2[d] / l2 : 0.0f;
-                ca_write(p, it, it.tile * all + r, DH, dim + d, (y1 - p.lambda * y2) * p.out_scale);
-            }
+            for (int d = 0; d < 4; ++d) o[s][d] = o[s][d] * a + v[s][d] * c;
+            m[s] = now;
         }
     }
-}
-
-constexpr uint32_t kCaMagic = 0x4b400000u;      // 1.5 * 2^23: an accumulator that starts there is that float plus its sum
-constexpr float kCaMagicF = 12582912.0f;
-__device__ __forceinline__ float ca_float(int d) { return __int_as_float(d) - kCaMagicF; }
-__device__ __forceinline__ uint64_t ca_float2(int a, int b) {
-    return add_f32x2(pack_f32x2(__int_as_float(a), __int_as_float(b)), pack_f32x2(-kCaMagicF, -kCaMagicF));
+    __device__ __forceinline__ void add_part(const float *part, int dh, int dim) {
+        add(*reinterpret_cast<const float4 *>(part), *reinterpret_cast<const float4 *>(part + 4 + dim), *reinterpret_cast<const float4 *>(part + 4 + dh + dim));
+    }
+    __device__ __forceinline__ void store_part(float *part, int dh, int dim, bool first) const {
+        if (first) *reinterpret_cast<float4 *>(part) = make_float4(m[0], l[0], m[1], l[1]);
+        *reinterpret_cast<float4 *>(part + 4 + dim) = make_float4(o[0][0], o[0][1], o[0][2], o[0][3]);
+        *reinterpret_cast<float4 *>(part + 4 + dh + dim) = make_float4(o[1][0], o[1][1], o[1][2], o[1][3]);
+    }
+    __device__ __forceinline__ void write(const CaParams &p, const CaItem &it, int rr, int dh, int dim) const {
+        const float i1 = l[0] != 0.0f ? p.out_scale / l[0] : 0.0f, i2 = l[1] != 0.0f ? p.lambda * p.out_scale / l[1] : 0.0f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) ca_write(p, it, rr, dh, dim + d, o[0][d] * i1 - o[1][d] * i2);
+    }
+};
+// Joins n parts of an item, in order: at(j) is the j-th.  `to`: where the result stays a part, null if it is the output.  Threads deal (row, four dims).
+template <int DH, int ROWS, class F>
+__device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int n, F at, float *to, int thread, int threads) {
+    constexpr int PART = 4 + 2 * DH, FOURS = DH / 4;
+    const int all = ROWS * p.tiles, end = min(all, it.m * p.group - it.tile * all);
+    for (int e = thread; e < end * FOURS; e += threads) {
+        const int r = e / FOURS, dim = e % FOURS * 4;
+        CaSum sum;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) sum.add_part(at(j) + r * PART, DH, dim);
+        if (to) sum.store_part(to + r * PART, DH, dim, dim == 0);
+        else sum.write(p, it, it.tile * all + r, DH, dim);
+    }
 }
 
 // DP: digits of the probabilities.
@@ -198,42 +211,52 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     if (tid < C::STAGES) dmbar_init(dsmem_u32(&bars[tid]), 1);
     if (tid == 0) gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    __syncthreads();
     pdl_launch_dependents();
     const int tile_rows = ROWS * (ROWS == 1 ? 1 : p.tiles);
 
     // ---- plan: the running sum of units over the sequences, by every CTA for itself
+    // (up to 32 of them: by every warp for itself, without a barrier)
     long long total = 0;
-    for (int i0 = 0; i0 < p.n_seqs; i0 += blockDim.x) {
-        const int i = i0 + tid;
-        long long mine = 0;
-        if (i < p.n_seqs) {
-            const CaSeq s = ca_sequence(p, tile_rows, i);
-            mine = (long long)s.tiles * H * s.units;
-            if (blockIdx.x == 0 && s.slot == -2) atomicOr(p.status, kStatusCache);
-        }
-        long long sum = mine;
+    if (tid == 0) p.items[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+    auto units_of = [&](int i) {
+        const CaSeq s = ca_sequence(p, tile_rows, i);
+        if (blockIdx.x == 0 && s.slot == -2) atomicOr(p.status, kStatusCache);
+        return (long long)s.tiles * H * s.units;
+    };
+    auto warp_sum = [&](long long sum) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long v = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += v;
         }
-        if (lane == 31) wide[warp] = sum;
-        __syncthreads();
-        long long before = total, all = 0;
-        const int warps = blockDim.x >> 5;
-        for (int w = 0; w < warps; ++w) {
-            if (w < warp) before += wide[w];
-            all += wide[w];
+        return sum;
+    };
+    if (p.n_seqs <= 32) {
+        const long long mine = lane < p.n_seqs ? units_of(lane) : 0, sum = warp_sum(mine);
+        total = __shfl_sync(0xffffffffu, sum, 31);
+        if (lane < p.n_seqs) prefix[lane] = sum - mine;  // (every warp writes the same values)
+        if (lane == 0) prefix[p.n_seqs] = total;
+    } else {
+        for (int i0 = 0; i0 < p.n_seqs; i0 += blockDim.x) {
+            const int i = i0 + tid;
+            const long long mine = i < p.n_seqs ? units_of(i) : 0, sum = warp_sum(mine);
+            if (lane == 31) wide[warp] = sum;
+            __syncthreads();
+            long long before = total, all = 0;
+            const int warps = blockDim.x >> 5;
+            for (int w = 0; w < warps; ++w) {
+                if (w < warp) before += wide[w];
+                all += wide[w];
+            }
+            if (i < p.n_seqs) prefix[i] = before + sum - mine;
+            total += all;
+            __syncthreads();
         }
-        if (i < p.n_seqs) prefix[i] = before + sum - mine;
-        total += all;
+        if (tid == 0) prefix[p.n_seqs] = total;
         __syncthreads();
     }
-    if (tid == 0) {
-        prefix[p.n_seqs] = total;
-        p.items[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
-    }
-    __syncthreads();
+    __syncwarp();
 
     // rows that see nothing because the sequence is empty
     const int width = H * p.group * DH;
@@ -250,14 +273,15 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     // ---- shares.  As many CTAs as have a unit for each team, as many teams as have a unit: none is empty between two of an item, and a short item
     // stays within a CTA.
     const int teams_here = ROWS == 1 ? C::WARPS : p.teams;
-    const int ctas = (int)min((long long)gridDim.x, (total + teams_here - 1) / teams_here);
+    const int ctas = total < (long long)gridDim.x * teams_here ? ((int)total + teams_here - 1) / teams_here : (int)gridDim.x;
     if ((int)blockIdx.x >= ctas) return;
-    const long long c0 = total * blockIdx.x / ctas, c1 = total * (blockIdx.x + 1) / ctas;
+    const long long c0 = ca_share(total, blockIdx.x, ctas), c1 = ca_share(total, blockIdx.x + 1, ctas);
     const int teams = (int)min((long long)teams_here, c1 - c0);
     const bool works = team < teams;
-    const long long u0 = works ? c0 + (c1 - c0) * team / teams : c1, u1 = works ? c0 + (c1 - c0) * (team + 1) / teams : c1;
-    float *my_parts = p.parts + ((size_t)blockIdx.x * teams_here + team) * 2 * (ROWS == 1 ? 1 : p.tiles) * (ROWS * C::PART);
+    const long long u0 = works ? c0 + ca_share(c1 - c0, team, teams) : c1, u1 = works ? c0 + ca_share(c1 - c0, team + 1, teams) : c1;
     const int part_floats = (ROWS == 1 ? 1 : p.tiles) * (ROWS * C::PART);
+    float *parts = ROWS == 1 ? reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + C::WARPS * C::SCORES + C::PREFIX) : p.parts + (size_t)blockIdx.x * teams_here * 2 * part_floats;
+    float *my_parts = parts + team * 2 * part_floats;
 
     auto place = [&](long long u, CaCursor &k) {
         int lo = 0, hi = p.n_seqs - 1;
@@ -267,9 +291,10 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         }
         k.seq = lo;
         k.s = ca_sequence(p, tile_rows, lo);
-        const long long in = u - prefix[lo], item = in / k.s.units;
+        const long long in = u - prefix[lo];
+        const long long item = in <= 0xffffffffll ? (long long)((uint32_t)in / (uint32_t)k.s.units) : in / k.s.units;
         k.unit = (int)(in - item * k.s.units);
-        k.tile = (int)(item / H);
+        k.tile = item <= 0xffffffffll ? (int)((uint32_t)item / (uint32_t)H) : (int)(item / H);
         k.head = (int)(item - (long long)k.tile * H);
     };
     auto advance = [&](CaCursor &k) {  // to the next unit; true: of another item
@@ -343,15 +368,6 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 
     CaCursor ahead, k;
     if (works) place(u0, k);
-    ahead = k;
-    long long ahead_u = u0;
-    int ahead_sees = works ? last_sees(k.s, k.tile) : 0;  // tokens that the last row of the item sees
-    auto fetch_next = [&](int stage) {
-        fetch(ahead, ahead_sees, stage);
-        if (++ahead_u < u1 && advance(ahead)) ahead_sees = last_sees(ahead.s, ahead.tile);
-    };
-    if (leads)
-        for (int s = 0; s < stages && ahead_u < u1; ++s) fetch_next(s);
     if (works && team == 0 && lane == 0 && leads) first_item_of_cta = {u0 - k.unit, u0 - k.unit + k.s.units, k.s.row0, k.s.m, k.head, k.tile};
 
     // ---- state of the item
@@ -367,9 +383,30 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     const uint32_t limb_xor = limb == 0 ? 0x80808080u : 0u, limb_keep = limb == 3 ? 0u : 0xffffffffu;
     const int heads = H * p.group;
 
-    auto q_row = [&](int n, int at) {  // stream n of the item's row
-        return p.q + ((size_t)(k.s.row0 + at / p.group) * 2 + n) * heads * DH + (size_t)(k.head * p.group + at % p.group) * DH;
+    auto q_row = [&](const CaCursor &k, int n, int at) {  // stream n of the item's row
+        const int token = p.group == 1 ? at : at / p.group;
+        return p.q + ((size_t)(k.s.row0 + token) * 2 + n) * heads * DH + (size_t)(k.head * p.group + at - token * p.group) * DH;
     };
+    uint2 qw[C::KT][2];                            // q's values in the places of its digits: of row g (ROWS = 1: the one row) and the lane's stream
+    auto load_q = [&](const CaCursor &k) {
+        const int at = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g);
+        const bool there = at < k.s.m * p.group;
+        const __nv_bfloat16 *src = q_row(k, my_stream, there ? at : 0) + 4 * t;
+#pragma unroll
+        for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) qw[kt][h] = there ? *reinterpret_cast<const uint2 *>(src + kt * 32 + h * 16) : make_uint2(0, 0);
+    };
+    if (ROWS == 1 && works) load_q(k);
+    ahead = k;
+    long long ahead_u = u0;
+    int ahead_sees = works ? last_sees(k.s, k.tile) : 0;  // tokens that the last row of the item sees
+    auto fetch_next = [&](int stage) {
+        fetch(ahead, ahead_sees, stage);
+        if (++ahead_u < u1 && advance(ahead)) ahead_sees = last_sees(ahead.s, ahead.tile);
+    };
+    if (leads)
+        for (int s = 0; s < stages && ahead_u < u1; ++s) fetch_next(s);
     auto begin_item = [&] {
         m = -INFINITY;
         l = 0.0f;
@@ -388,50 +425,41 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
             sees_tile = base < there ? row_sees(k.s, min(base + 7, there - 1)) : 0;
             sees_all = min(row_sees(k.s, base), row_sees(k.s, base + 7));
         }
+        if (ROWS == 8) load_q(k);
         // q's digits: q = f * 2^(E - 21) with E the exponent of the row's largest magnitude, so |f| < 2^22; f + 0x808080 has in each byte the
-        // balanced digit plus 128.
+        // balanced digit plus 128.  (f is rounded by adding 1.5 * 2^23.)
+        uint32_t top = 0;
 #pragma unroll
-        for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n) {
-            const int at = base + (ROWS == 1 ? 0 : g);
-            const bool mine = at < there && (ROWS == 8 || (g >> 2) == n);
-            const __nv_bfloat16 *src = q_row(ROWS == 1 ? n : stream, mine ? at : 0);
-            uint2 w[C::KT][2];
-            uint32_t top = 0;
+        for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
-            for (int kt = 0; kt < C::KT; ++kt)
+            for (int h = 0; h < 2; ++h) top = __vmaxu2(top, __vmaxu2(qw[kt][h].x & 0x7fff7fffu, qw[kt][h].y & 0x7fff7fffu));
+        top = max(top >> 16, top & 0xffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int E = max((int)(top >> 7) - 127, -100);  // (below 2^-100 the scores are zero for any purpose, above that 2^(21 - E) is a float)
+        const float f = __uint_as_float((uint32_t)(127 + 21 - E) << 23);
+        const float back = top >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 - 21 + E) << 23);
+        qs = back * p.scale_log2;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    w[kt][h] = mine ? *reinterpret_cast<const uint2 *>(src + kt * 32 + h * 16 + 4 * t) : make_uint2(0, 0);
-                    top = __vmaxu2(top, __vmaxu2(w[kt][h].x & 0x7fff7fffu, w[kt][h].y & 0x7fff7fffu));
-                }
-            top = max(top >> 16, top & 0xffffu);
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int E = max((int)(top >> 7) - 127, -100);  // (below 2^-100 the scores are zero for any purpose, above that 2^(21 - E) is a float)
-            const float f = __uint_as_float((uint32_t)(127 + 21 - E) << 23);
-            const float back = top >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 - 21 + E) << 23);
-            if (ROWS == 8 || n == my_stream) qs = back * p.scale_log2;
+        for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
-            for (int kt = 0; kt < C::KT; ++kt)
+            for (int h = 0; h < 2; ++h) {
+                const float v[4] = {bf16lo_to_float(qw[kt][h].x), bf16hi_to_float(qw[kt][h].x), bf16lo_to_float(qw[kt][h].y), bf16hi_to_float(qw[kt][h].y)};
+                uint32_t d[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t d[4];
-                    d[0] = (uint32_t)__float2int_rn(bf16lo_to_float(w[kt][h].x) * f) + 0x808080u;
-                    d[1] = (uint32_t)__float2int_rn(bf16hi_to_float(w[kt][h].x) * f) + 0x808080u;
-                    d[2] = (uint32_t)__float2int_rn(bf16lo_to_float(w[kt][h].y) * f) + 0x808080u;
-                    d[3] = (uint32_t)__float2int_rn(bf16hi_to_float(w[kt][h].y) * f) + 0x808080u;
-                    if (ROWS == 1) {
-                        const uint32_t v = __byte_perm(__byte_perm(d[0], d[1], limb_sel), __byte_perm(d[2], d[3], limb_sel), 0x5410) ^ 0x80808080u;
-                        qd[n][0][kt][h] = mine ? v & limb_keep : 0u;
-                    } else {
+                for (int e = 0; e < 4; ++e) d[e] = __float_as_uint(fmaf(v[e], f, kCaMagicF)) + (0x808080u - 0x400000u);
+                if (ROWS == 1) {
+                    const uint32_t w = (__byte_perm(__byte_perm(d[0], d[1], limb_sel), __byte_perm(d[2], d[3], limb_sel), 0x5410) ^ 0x80808080u) & limb_keep;
+                    qd[0][0][kt][h] = my_stream ? 0u : w;
+                    qd[ROWS == 1 ? 1 : 0][0][kt][h] = my_stream ? w : 0u;
+                } else {
 #pragma unroll
-                        for (int j = 0; j < ND; ++j) {
-                            const uint32_t sel = 0x0040u + (uint32_t)(2 - j) * 0x0011u;
-                            qd[n][j][kt][h] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
-                        }
+                    for (int j = 0; j < ND; ++j) {
+                        const uint32_t sel = 0x0040u + (uint32_t)(2 - j) * 0x0011u;
+                        qd[0][j][kt][h] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
                     }
                 }
-        }
+            }
     };
 
     // Softmax step of a row on `x`, scores before their factor f (16 or 8 tokens of this lane, the row's others in the lanes with the same g; the first
@@ -473,6 +501,14 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     int stage = 0;
     for (long long u = u0; u < u1; ++u) {
         if (fresh) begin_item();
+        // (the next item's q is on its way while this one's last unit is worked on)
+        CaCursor next;
+        const bool item_ends = k.unit == k.s.units - 1;
+        if (ROWS == 1 && item_ends && u + 1 < u1) {
+            next = k;
+            advance(next);
+            load_q(next);
+        }
         const uint8_t *unit = ring + stage * C::STAGE;
         const int token0 = unit_token(k);
         if (token0 < sees_item) {
@@ -636,22 +672,26 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                 const int q_at = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g);
                 const bool q_there = q_at < k.s.m * p.group;
                 auto q_pair = [&](int n, int col) -> uint32_t {  // q's values col, col + 1 of this lane's column
-                    if (!q_there || (ROWS == 1 && g != 4 * n)) return 0;
-                    return *reinterpret_cast<const uint32_t *>(q_row(n, q_at) + col);
+                    if (!q_there || (ROWS == 1 && limb)) return 0;
+                    return *reinterpret_cast<const uint32_t *>(q_row(k, n, q_at) + col);
                 };
                 auto k_eight = [&](int n, int mt, int kt) {
                     const int r = mt * 16 + (lane & 15);
                     return ldmatrix4(at + n * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, kt * 2 + (lane >> 4)) * 16);
                 };
                 float d[2][4] = {};
+                uint32_t qb[DH / 16][2];
+#pragma unroll
+                for (int kt = 0; kt < DH / 16; ++kt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) qb[kt][h] = q_pair(my_stream, kt * 16 + 8 * h + 2 * t);
 #pragma unroll
                 for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n)
 #pragma unroll
                     for (int kt = 0; kt < DH / 16; ++kt) {
-                        const int st = ROWS == 1 ? n : stream;
-                        const uint32_t b0 = q_pair(st, kt * 16 + 2 * t), b1 = q_pair(st, kt * 16 + 8 + 2 * t);
+                        const bool mine = ROWS == 8 || my_stream == n;
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(st, mt, kt), b0, b1);
+                        for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(ROWS == 1 ? n : stream, mt, kt), mine ? qb[kt][0] : 0u, mine ? qb[kt][1] : 0u);
                     }
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
@@ -736,7 +776,6 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         if (++stage == stages) stage = 0;
 
         // ---- the item's end, or the share's
-        const bool item_ends = k.unit == k.s.units - 1;
         if (item_ends || u + 1 == u1) {
             const bool whole = item_ends && !(first_item && begins_inside);
             float *part = my_parts + (first_item && !whole ? 0 : part_floats) + my_tile * (ROWS * C::PART);
@@ -747,7 +786,11 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
             if constexpr (ROWS == 1) {
                 const float l1 = __shfl_sync(0xffffffffu, l, 0), l2 = __shfl_sync(0xffffffffu, l, 16);
                 const float m1 = __shfl_sync(0xffffffffu, m, 0), m2 = __shfl_sync(0xffffffffu, m, 16);
-                const float i1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f, i2 = l2 != 0.0f ? p.lambda * p.out_scale / l2 : 0.0f;
+                float i1 = 0.0f, i2 = 0.0f;
+                if (whole) {
+                    i1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f;
+                    i2 = l2 != 0.0f ? p.lambda * p.out_scale / l2 : 0.0f;
+                }
 #pragma unroll
                 for (int mt = 0; mt < C::MT; ++mt)
 #pragma unroll
@@ -792,17 +835,23 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
             }
             first_item = false;
         }
-        fresh = advance(k);
+        fresh = item_ends;
+        if (ROWS == 1) {
+            if (item_ends && u + 1 < u1) k = next;
+            else ++k.unit;
+        } else if (u + 1 < u1) {
+            advance(k);
+        }
     }
 
     // ---- items that teams of this CTA share
     __syncthreads();
     if (!works) return;
-    auto team_of = [&](long long unit) { return (int)(((unit - c0 + 1) * teams - 1) / (c1 - c0)); };
+    auto team_of = [&](long long unit) { return ca_share_of(c1 - c0, unit - c0, teams); };
     auto join_here = [&](const CaItem &it, int from, bool slot1, float *to) {
-        const float *base = p.parts + ((size_t)blockIdx.x * teams_here + from) * 2 * part_floats;
+        const float *base = parts + from * 2 * part_floats;
         ca_join<DH, ROWS>(p, it, team_of(min(it.to, c1) - 1) - from + 1, [&](int j) { return base + (size_t)j * 2 * part_floats + (j == 0 && slot1 ? part_floats : 0); }, to,
-                          0, tile_rows, member * 32 + lane, team_warps * 32);
+                          member * 32 + lane, team_warps * 32);
     };
     float *cta_part = p.cta_parts + (size_t)blockIdx.x * 2 * part_floats;
     if (team == 0 && first_item_of_cta.from < c0) join_here(first_item_of_cta, 0, false, cta_part);
@@ -811,23 +860,37 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         const bool goes_on = it.to > c1, slot1 = it.from > c0;
         join_here(it, team, it.from > u0, goes_on ? cta_part + (slot1 ? part_floats : 0) : nullptr);
         if (goes_on && leads && lane == 0) {
-            p.items[2 * blockIdx.x] = make_int4(slot1 ? 2 : 1, (int)((it.to * ctas - 1) / total), it.head, it.tile);
+            p.items[2 * blockIdx.x] = make_int4(slot1 ? 2 : 1, ca_share_of(total, it.to - 1, ctas), it.head, it.tile);
             p.items[2 * blockIdx.x + 1] = make_int4(it.row0, it.m, 0, 0);
         }
     }
 }
 
-// Joins the parts of the items that several CTAs shared: block w the one that begins in CTA w's share and does not end there, if there is one; eight rows each.
+// Joins the parts of the items that several CTAs shared: block w the one that begins in CTA w's share and does not end there, if there is one; eight rows
+// each.  A single row's parts, which can be as many as there are CTAs, are dealt to eight groups of threads.
 template <int DH, int ROWS>
-__global__ void __launch_bounds__(256) cached_attention_join_kernel(CaParams p) {
-    const int w0 = blockIdx.x, part_floats = p.tiles * ROWS * (4 + 2 * DH);
+__global__ void __launch_bounds__(8 * DH / 4) cached_attention_join_kernel(CaParams p) {
+    constexpr int PART = 4 + 2 * DH, FOURS = DH / 4;
+    __shared__ __align__(16) float smem[ROWS == 1 ? 8 * PART : 4];
+    const int w0 = blockIdx.x, group = threadIdx.x / FOURS, dim = threadIdx.x % FOURS * 4, all = ROWS * p.tiles, part_floats = all * PART;
     pdl_wait();
     const int4 item = p.items[2 * w0], at = p.items[2 * w0 + 1];
     if (!item.x) return;
     const CaItem it = {0, 0, at.x, at.y, item.z, item.w};
-    const float *base = p.cta_parts + (size_t)w0 * 2 * part_floats;
-    ca_join<DH, ROWS>(p, it, item.y - w0 + 1, [&](int j) { return base + (size_t)j * 2 * part_floats + (j == 0 && item.x == 2 ? part_floats : 0); }, nullptr, 8 * blockIdx.y, 8,
-                      threadIdx.x, blockDim.x);
+    const int r = ROWS == 1 ? 0 : 8 * blockIdx.y + group, n = item.y - w0 + 1;
+    if (r >= it.m * p.group - it.tile * all) return;
+    const float *base = p.cta_parts + (size_t)w0 * 2 * part_floats + r * PART;
+    CaSum sum;
+#pragma unroll 4
+    for (int j = ROWS == 1 ? group : 0; j < n; j += ROWS == 1 ? 8 : 1) sum.add_part(base + (size_t)j * 2 * part_floats + (j == 0 && item.x == 2 ? part_floats : 0), DH, dim);
+    if (ROWS == 1) {
+        sum.store_part(smem + group * PART, DH, dim, dim == 0);
+        __syncthreads();
+        if (group) return;
+        sum = CaSum();
+        for (int j = 0; j < min(n, 8); ++j) sum.add_part(smem + j * PART, DH, dim);
+    }
+    sum.write(p, it, it.tile * all + r, DH, dim);
 }
 
 // How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows, as many to a team as
@@ -859,7 +922,7 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid, (unsigned)p.tiles);
-    cfg.blockDim = dim3(ROWS * DH / 4);
+    cfg.blockDim = dim3(8 * DH / 4);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -875,7 +938,7 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
 static size_t ca_items_bytes() { return align_up((size_t)kCaMaxSms * 2 * sizeof(int4), 256); }
 static size_t ca_cta_parts_bytes(int head_dim, const CaForm &f) { return align_up((size_t)kCaMaxSms * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256); }
 static size_t ca_workspace(int head_dim, const CaForm &f) {
-    return ca_items_bytes() + ca_cta_parts_bytes(head_dim, f) + align_up((size_t)kCaMaxSms * f.teams * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256);
+    return ca_items_bytes() + ca_cta_parts_bytes(head_dim, f) + (f.rows == 1 ? 0 : align_up((size_t)kCaMaxSms * f.teams * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256));
 }
 
 }  // namespace hgf
