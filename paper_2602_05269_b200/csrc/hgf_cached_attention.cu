@@ -15,24 +15,26 @@
 // of the FMA rate and bounded the kernel.  The open tokens' bf16 go through bf16 products, with the probabilities as sums of three bf16.
 //
 // Two forms.  ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.
-// ROWS = 8 otherwise: a product for each digit, eight query rows as its columns; a warp takes one stream of one tile of eight rows, and a team is the
-// warps of up to four tiles, so that a page that is read once serves 32 rows.
+// There the codes are the left operand, tokens (or dims) as its rows.  ROWS = 16 otherwise: sixteen query rows are the left operand, a product for each
+// digit, the codes the right one (a lane's sixteen bytes are the same either way round); a warp takes one stream of one tile of sixteen rows, and a
+// team is the warps of one or two tiles, so that a page that is read once serves up to 32 rows.  The columns of the scores' products are the page's
+// tokens in such an order that a lane gets four neighbouring tokens of its rows: the probabilities' digits are then in place for the second product.
 #include "hgf_cache.cuh"
 #include "hgf_warp.cuh"
 
 namespace hgf {
 
 constexpr int kCaMaxSms = 160;      // CTAs at most (the workspace has room for them)
-constexpr int kCaMaxTeamTiles = 8;  // teams of a CTA times tiles of a team, at most
+constexpr int kCaMaxTeams = 8;      // teams of a CTA at most
 
 template <int DH, int ROWS>
 struct CaCfg {
-    static constexpr int WARPS = ROWS == 8 ? 16 : (DH == 64 ? 8 : 4), THREADS = WARPS * 32;
+    static constexpr int WARPS = ROWS == 1 && DH == 128 ? 4 : 8, THREADS = WARPS * 32;
     static constexpr int UNIT = 3 * kCacheBlock * DH;            // bytes of a unit
     static constexpr int STAGE = (UNIT + 16 + 127) / 128 * 128;  // with the page's scales
     static constexpr int STAGES = DH == 64 ? 16 : 8;             // of all teams' rings
     static constexpr int KT = DH / 32, MT = DH / 16;
-    static constexpr int SCORES = ROWS == 1 ? 2 * kCacheBlock * 4 : 8 * 36 * 4;  // bytes a warp; rows 36 floats apart: eight rows' writes hit all banks
+    static constexpr int SCORES = ROWS == 1 ? 2 * kCacheBlock * 4 : 0;  // bytes a warp
     static constexpr int PART = 4 + 2 * DH;                      // floats: maximum and sum of stream 1, of stream 2, sums of values of both
     // (prefix sums, rounded up to 16 bytes; the parts of single tokens, two a warp, in shared memory)
     static constexpr int PREFIX = (kCacheMaxSeqs + 2) * 8, PARTS = ROWS == 1 ? WARPS * 2 * PART * 4 : 0;
@@ -46,7 +48,7 @@ struct CaParams {
     void *out;
     int4 *items;          // [CTAs][2]: what the joining kernel does for a CTA
     float *cta_parts;     // [CTAs][2][tiles][ROWS][PART]
-    float *parts;         // [CTAs][teams][2][tiles][ROWS][PART], ROWS = 8
+    float *parts;         // [CTAs][teams][2][tiles][ROWS][PART], ROWS = 16
     unsigned int *status;
     int n_seqs, n_rows, group, bf16;
     int teams, tiles, stages;  // of a CTA; of a team; of a team's ring
@@ -63,6 +65,11 @@ __device__ __forceinline__ void mma_s8u8(int (&d)[4], const uint4 &a, uint32_t b
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};\n"
                  : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
                  : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
+}
+__device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const int (&c)[4]) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};\n"
+                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4 &a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
@@ -145,6 +152,12 @@ __device__ __forceinline__ void ca_write(const CaParams &p, const CaItem &it, in
     else reinterpret_cast<float *>(p.out)[o] = y;
 }
 
+__device__ __forceinline__ void ca_write2(const CaParams &p, const CaItem &it, int rr, int dh, int dim, float y0, float y1) {
+    const size_t o = ((size_t)(it.row0 + rr / p.group) * p.c.H * p.group + it.head * p.group + rr % p.group) * dh + dim;
+    if (p.bf16) *reinterpret_cast<__nv_bfloat162 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + o) = __floats2bfloat162_rn(y0, y1);
+    else *reinterpret_cast<float2 *>(reinterpret_cast<float *>(p.out) + o) = make_float2(y0, y1);
+}
+
 // What parts of an item add up to, for four dims of a row.
 struct CaSum {
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {}, o[2][4] = {};
@@ -171,7 +184,7 @@ struct CaSum {
     __device__ __forceinline__ void write(const CaParams &p, const CaItem &it, int rr, int dh, int dim) const {
         const float i1 = l[0] != 0.0f ? p.out_scale / l[0] : 0.0f, i2 = l[1] != 0.0f ? p.lambda * p.out_scale / l[1] : 0.0f;
 #pragma unroll
-        for (int d = 0; d < 4; ++d) ca_write(p, it, rr, dh, dim + d, o[0][d] * i1 - o[1][d] * i2);
+        for (int d = 0; d < 4; d += 2) ca_write2(p, it, rr, dh, dim + d, o[0][d] * i1 - o[1][d] * i2, o[0][d + 1] * i1 - o[1][d + 1] * i2);
     }
 };
 // Joins n parts of an item, in order: at(j) is the j-th.  `to`: where the result stays a part, null if it is the output.  Threads deal (row, four dims).
@@ -206,7 +219,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     __shared__ __align__(8) uint64_t bars[C::STAGES];
     __shared__ int page_ok[C::STAGES];       // a stage's page number was one
     __shared__ volatile int gave_up;         // a wait ran out: the others end, too
-    __shared__ CaItem first_item_of_cta, last_item_of[kCaMaxTeamTiles];
+    __shared__ CaItem first_item_of_cta, last_item_of[kCaMaxTeams];
     const uint32_t ring_a = dsmem_u32(ring), bars_a = dsmem_u32(bars) + team * stages * 8;
     if (tid < C::STAGES) dmbar_init(dsmem_u32(&bars[tid]), 1);
     if (tid == 0) gave_up = 0;
@@ -372,12 +385,12 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 
     // ---- state of the item
     // ROWS = 1: m, l of the lane's stream (lanes 0-15 stream 1, 16-31 stream 2); acc[mt][e]: dims 16 mt + g + 8 e, in lanes t of stream t / 2.
-    // ROWS = 8: m, l of row g, of the warp's stream; acc[mt][e]: dim 16 mt + g + 8 (e / 2), row 2 t + e % 2.
-    constexpr int NE = ROWS == 1 ? 2 : 4, ND = ROWS == 1 ? 1 : 3;
-    float m = -INFINITY, l = 0.0f, acc[C::MT][NE];
-    uint32_t qd[ROWS == 1 ? 2 : 1][ND][C::KT][2];  // right operand of the scores: digits of q (ROWS = 1: for K1 and for K2)
-    float qs = 0.0f;                               // what a digit sum is worth, with 1 / sqrt(d) and log2 e
-    int sees_g = 0, sees_e[2] = {0, 0}, sees_tile = 0, sees_all = 0, sees_item = 0;  // tokens that row g, rows 2 t and 2 t + 1, any row, every row of the tile, any of the item sees
+    // ROWS = 16: m, l of rows g and g + 8, of the warp's stream; acc[nt][e]: dim 8 nt + 2 t + e % 2, row g + 8 (e / 2).
+    constexpr int NR = ROWS == 1 ? 1 : 2, NA = ROWS == 1 ? C::MT : DH / 8, NE = ROWS == 1 ? 2 : 4, ND = ROWS == 1 ? 1 : 3;
+    float m[NR], l[NR], acc[NA][NE];
+    uint32_t qd[ROWS == 1 ? 2 : ND][C::KT][ROWS == 1 ? 2 : 4];  // digits of q: ROWS = 1 for K1 and for K2, as right operand; ROWS = 16 each digit, as left operand
+    float qs[NR];                                  // what a digit sum is worth, with 1 / sqrt(d) and log2 e
+    int sees[NR] = {}, sees_tile = 0, sees_all = 0, sees_item = 0;  // tokens that the lane's rows, any row, every row of the tile, any of the item sees
     const int my_stream = ROWS == 1 ? lane >> 4 : stream, limb = g & 3;
     const uint32_t limb_sel = 0x0040u + (uint32_t)((2 - limb) & 3) * 0x0011u;  // byte 2 - limb of two words
     const uint32_t limb_xor = limb == 0 ? 0x80808080u : 0u, limb_keep = limb == 3 ? 0u : 0xffffffffu;
@@ -387,15 +400,18 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         const int token = p.group == 1 ? at : at / p.group;
         return p.q + ((size_t)(k.s.row0 + token) * 2 + n) * heads * DH + (size_t)(k.head * p.group + at - token * p.group) * DH;
     };
-    uint2 qw[C::KT][2];                            // q's values in the places of its digits: of row g (ROWS = 1: the one row) and the lane's stream
+    uint2 qw[NR][C::KT][2];                        // q's values in the places of its digits: of the lane's rows (ROWS = 1: the one row) and stream
     auto load_q = [&](const CaCursor &k) {
-        const int at = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g);
-        const bool there = at < k.s.m * p.group;
-        const __nv_bfloat16 *src = q_row(k, my_stream, there ? at : 0) + 4 * t;
 #pragma unroll
-        for (int kt = 0; kt < C::KT; ++kt)
+        for (int r = 0; r < NR; ++r) {
+            const int at = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g + 8 * r);
+            const bool there = at < k.s.m * p.group;
+            const __nv_bfloat16 *src = q_row(k, my_stream, there ? at : 0) + 4 * t;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) qw[kt][h] = there ? *reinterpret_cast<const uint2 *>(src + kt * 32 + h * 16) : make_uint2(0, 0);
+            for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) qw[r][kt][h] = there ? *reinterpret_cast<const uint2 *>(src + kt * 32 + h * 16) : make_uint2(0, 0);
+        }
     };
     if (ROWS == 1 && works) load_q(k);
     ahead = k;
@@ -408,69 +424,72 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     if (leads)
         for (int s = 0; s < stages && ahead_u < u1; ++s) fetch_next(s);
     auto begin_item = [&] {
-        m = -INFINITY;
-        l = 0.0f;
 #pragma unroll
-        for (int a = 0; a < C::MT; ++a)
+        for (int a = 0; a < NA; ++a)
 #pragma unroll
             for (int e = 0; e < NE; ++e) acc[a][e] = 0.0f;
         const int base = k.tile * tile_rows + my_tile * ROWS, there = k.s.m * p.group;
         sees_item = last_sees(k.s, k.tile);
         if (ROWS == 1) {
-            sees_g = sees_tile = sees_all = row_sees(k.s, base);
+            sees[0] = sees_tile = sees_all = row_sees(k.s, base);
         } else {
-            sees_g = row_sees(k.s, base + g);
-            sees_e[0] = row_sees(k.s, base + 2 * t);
-            sees_e[1] = row_sees(k.s, base + 2 * t + 1);
-            sees_tile = base < there ? row_sees(k.s, min(base + 7, there - 1)) : 0;
-            sees_all = min(row_sees(k.s, base), row_sees(k.s, base + 7));
+            sees[0] = row_sees(k.s, base + g);
+            sees[NR - 1] = row_sees(k.s, base + g + 8);
+            sees_tile = base < there ? row_sees(k.s, min(base + 15, there - 1)) : 0;
+            sees_all = min(row_sees(k.s, base), row_sees(k.s, base + 15));
         }
-        if (ROWS == 8) load_q(k);
+        if (ROWS == 16) load_q(k);
         // q's digits: q = f * 2^(E - 21) with E the exponent of the row's largest magnitude, so |f| < 2^22; f + 0x808080 has in each byte the
         // balanced digit plus 128.  (f is rounded by adding 1.5 * 2^23.)
-        uint32_t top = 0;
 #pragma unroll
-        for (int kt = 0; kt < C::KT; ++kt)
+        for (int r = 0; r < NR; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+            uint32_t top = 0;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) top = __vmaxu2(top, __vmaxu2(qw[kt][h].x & 0x7fff7fffu, qw[kt][h].y & 0x7fff7fffu));
-        top = max(top >> 16, top & 0xffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int E = max((int)(top >> 7) - 127, -100);  // (below 2^-100 the scores are zero for any purpose, above that 2^(21 - E) is a float)
-        const float f = __uint_as_float((uint32_t)(127 + 21 - E) << 23);
-        const float back = top >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 - 21 + E) << 23);
-        qs = back * p.scale_log2;
+            for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
-        for (int kt = 0; kt < C::KT; ++kt)
+                for (int h = 0; h < 2; ++h) top = __vmaxu2(top, __vmaxu2(qw[r][kt][h].x & 0x7fff7fffu, qw[r][kt][h].y & 0x7fff7fffu));
+            top = max(top >> 16, top & 0xffffu);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int E = max((int)(top >> 7) - 127, -100);  // (below 2^-100 the scores are zero for any purpose, above that 2^(21 - E) is a float)
+            const float f = __uint_as_float((uint32_t)(127 + 21 - E) << 23);
+            const float back = top >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 - 21 + E) << 23);
+            qs[r] = back * p.scale_log2;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float v[4] = {bf16lo_to_float(qw[kt][h].x), bf16hi_to_float(qw[kt][h].x), bf16lo_to_float(qw[kt][h].y), bf16hi_to_float(qw[kt][h].y)};
-                uint32_t d[4];
+            for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[e] = __float_as_uint(fmaf(v[e], f, kCaMagicF)) + (0x808080u - 0x400000u);
-                if (ROWS == 1) {
-                    const uint32_t w = (__byte_perm(__byte_perm(d[0], d[1], limb_sel), __byte_perm(d[2], d[3], limb_sel), 0x5410) ^ 0x80808080u) & limb_keep;
-                    qd[0][0][kt][h] = my_stream ? 0u : w;
-                    qd[ROWS == 1 ? 1 : 0][0][kt][h] = my_stream ? w : 0u;
-                } else {
+                for (int h = 0; h < 2; ++h) {
+                    const uint2 w = qw[r][kt][h];
+                    const float v[4] = {bf16lo_to_float(w.x), bf16hi_to_float(w.x), bf16lo_to_float(w.y), bf16hi_to_float(w.y)};
+                    uint32_t d[4];
 #pragma unroll
-                    for (int j = 0; j < ND; ++j) {
-                        const uint32_t sel = 0x0040u + (uint32_t)(2 - j) * 0x0011u;
-                        qd[0][j][kt][h] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
+                    for (int e = 0; e < 4; ++e) d[e] = __float_as_uint(fmaf(v[e], f, kCaMagicF)) + (0x808080u - 0x400000u);
+                    if (ROWS == 1) {
+                        const uint32_t x = (__byte_perm(__byte_perm(d[0], d[1], limb_sel), __byte_perm(d[2], d[3], limb_sel), 0x5410) ^ 0x80808080u) & limb_keep;
+                        qd[0][kt][h] = my_stream ? 0u : x;
+                        qd[1][kt][h] = my_stream ? x : 0u;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < ND; ++j) {
+                            const uint32_t sel = 0x0040u + (uint32_t)(2 - j) * 0x0011u;
+                            qd[j][kt][ROWS == 1 ? h : 2 * h + r] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
+                        }
                     }
                 }
-            }
+        }
     };
 
-    // Softmax step of a row on `x`, scores before their factor f (16 or 8 tokens of this lane, the row's others in the lanes with the same g; the first
-    // `sees` of the unit's tokens count, `token(j)` is the j-th of the lane's): the probabilities relative to the unit's largest in place of the scores,
+    // Softmax step of row r on `x`, scores before their factor f (16 or 8 tokens of this lane, the row's others in the lanes with the same g; the first
+    // `count` of the unit's tokens count, `token(j)` is the j-th of the lane's): the probabilities relative to the unit's largest in place of the scores,
     // and what the sums so far (alpha) and the unit's (worth) are to be multiplied with.
-    auto softmax_step = [&](auto &x, float f, bool partly, int sees, auto token, float &alpha, float &worth) {
+    auto softmax_step = [&](auto &x, int r, float f, bool partly, int count, auto token, float &alpha, float &worth) {
         constexpr int N = sizeof(x) / sizeof(float);
         if (partly) {
 #pragma unroll
             for (int j = 0; j < N; ++j)
-                if (token(j) >= sees) x[j] = -INFINITY;
+                if (token(j) >= count) x[j] = -INFINITY;
         }
         float top = x[0];
 #pragma unroll
@@ -478,19 +497,19 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // (f is zero for a page of zeros: then nothing is -inf but what is masked)
-        const float here = top == -INFINITY ? -INFINITY : top * f, now = fmaxf(m, here), base = now == -INFINITY ? 0.0f : now;
+        const float here = top == -INFINITY ? -INFINITY : top * f, now = fmaxf(m[r], here), base = now == -INFINITY ? 0.0f : now;
         const float minus = here == -INFINITY ? 0.0f : -here;
-        alpha = exp2_approx(m - base);
+        alpha = exp2_approx(m[r] - base);
         worth = exp2_approx(here - base);
-        float s = 0.0f;
+        float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const float y = fmaf(x[j], f, minus);
-            x[j] = partly && token(j) >= sees ? 0.0f : exp2_approx(y);
-            s += x[j];
+            x[j] = partly && token(j) >= count ? 0.0f : exp2_approx(y);
+            sum += x[j];
         }
-        m = now;
-        l = fmaf(l, alpha, s * worth);
+        m[r] = now;
+        l[r] = fmaf(l[r], alpha, sum * worth);
     };
 
     int magic[4] = {(int)kCaMagic, (int)kCaMagic, (int)kCaMagic, (int)kCaMagic};
@@ -533,11 +552,9 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
             }
             if (ok && !open_unit && token0 < sees_tile) {
                 const float4 sc = *reinterpret_cast<const float4 *>(unit + C::UNIT);
-                float alpha, worth;
                 auto token = [&](int j) { return (j >> 2) * 16 + 4 * t + (j & 3); };
                 const bool partly = sees_all - token0 < kCacheBlock;
-                const float f = qs * (my_stream ? sc.y : sc.x);
-                float x[16];
+                float x[NR][16], alpha[NR], worth[NR];
                 if constexpr (ROWS == 1) {
                     const float wa = t & 1 ? 1.0f : 65536.0f, wb = t & 1 ? 0.0f : 256.0f;
 #pragma unroll
@@ -548,7 +565,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 #pragma unroll
                             for (int kt = 0; kt < C::KT; ++kt) {
                                 const uint4 a = *reinterpret_cast<const uint4 *>(unit + n * kCacheBlock * DH + ((mt * C::KT + kt) * 32 + lane) * 16);
-                                mma_s8s8(d, a, qd[n][0][kt][0], qd[n][0][kt][1], n + kt ? d : magic);
+                                mma_s8s8(d, a, qd[n][kt][0], qd[n][kt][1], n + kt ? d : magic);
                             }
                         float lo = fmaf(ca_float(d[0]), wa, ca_float(d[1]) * wb), hi = fmaf(ca_float(d[2]), wa, ca_float(d[3]) * wb);
                         lo += __shfl_xor_sync(0xffffffffu, lo, 1);
@@ -559,21 +576,21 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float4 v = *reinterpret_cast<const float4 *>(scores + my_stream * kCacheBlock + j * 16 + 4 * t);
-                        x[4 * j] = v.x;
-                        x[4 * j + 1] = v.y;
-                        x[4 * j + 2] = v.z;
-                        x[4 * j + 3] = v.w;
+                        x[0][4 * j] = v.x;
+                        x[0][4 * j + 1] = v.y;
+                        x[0][4 * j + 2] = v.z;
+                        x[0][4 * j + 3] = v.w;
                     }
-                    softmax_step(x, f, partly, sees_g - token0, token, alpha, worth);
+                    softmax_step(x[0], 0, qs[0] * (my_stream ? sc.y : sc.x), partly, sees[0] - token0, token, alpha[0], worth[0]);
                     uint32_t b[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t w[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[4 * j + e]);
+                        for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[0][4 * j + e]);
                         b[j] = (__byte_perm(__byte_perm(w[0], w[1], limb_sel), __byte_perm(w[2], w[3], limb_sel), 0x5410) ^ limb_xor) & limb_keep;
                     }
-                    const float scale = __shfl_sync(0xffffffffu, alpha, (t >> 1) * 16), sv = sc.z * __shfl_sync(0xffffffffu, worth, (t >> 1) * 16);
+                    const float scale = __shfl_sync(0xffffffffu, alpha[0], (t >> 1) * 16), sv = sc.z * __shfl_sync(0xffffffffu, worth[0], (t >> 1) * 16);
                     // digits of 2^23 p: weights 2^-7, 2^-15, 2^-23
                     const float va = sv * (t & 1 ? 1.1920928955078125e-7f : 0.0078125f), vb = t & 1 ? 0.0f : sv * 3.0517578125e-5f;
 #pragma unroll
@@ -589,79 +606,74 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     }
                 } else {
                     const uint64_t base256 = pack_f32x2(256.0f, 256.0f);
-                    const uint8_t *codes = unit + stream * kCacheBlock * DH;
+                    // Column n of a product is token 4 (n / 2) + n % 2 of sixteen, or the one two further: a lane's two columns are then its first or
+                    // last two of four neighbouring tokens.  In the tile such a token's row is 8 a + g' with a = n / 4.
+                    const uint8_t *codes = unit + stream * kCacheBlock * DH + (((g & 1) + 4 * (g >> 1 & 1)) * 4 + t) * 16 + (g >> 2) * 4;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
+                    for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int mh = 0; mh < 2; ++mh) {
-                            const int mt = 2 * half + mh;
+                        for (int two = 0; two < 2; ++two) {
                             int d[3][4];
 #pragma unroll
                             for (int kt = 0; kt < C::KT; ++kt) {
-                                const uint4 a = *reinterpret_cast<const uint4 *>(codes + ((mt * C::KT + kt) * 32 + lane) * 16);
+                                const uint8_t *at = codes + (j * C::KT + kt) * 512 + two * 128;
+                                const uint32_t b0 = *reinterpret_cast<const uint32_t *>(at), b1 = *reinterpret_cast<const uint32_t *>(at + 8);
 #pragma unroll
-                                for (int j = 0; j < 3; ++j) mma_s8s8(d[j], a, qd[0][ND - 1 ? j : 0][kt][0], qd[0][ND - 1 ? j : 0][kt][1], kt ? d[j] : magic);
+                                for (int z = 0; z < 3; ++z) mma_s8s8(d[z], make_uint4(qd[z][kt][0], qd[z][kt][1], qd[z][kt][ROWS == 1 ? 0 : 2], qd[z][kt][ROWS == 1 ? 0 : 3]), b0, b1, kt ? d[z] : magic);
                             }
 #pragma unroll
-                            for (int e = 0; e < 4; e += 2) {
-                                float v0, v1;
-                                unpack_f32x2(fma_f32x2(fma_f32x2(ca_float2(d[0][e], d[0][e + 1]), base256, ca_float2(d[1][e], d[1][e + 1])), base256, ca_float2(d[2][e], d[2][e + 1])), v0, v1);
-                                scores[(2 * t) * 36 + mh * 16 + g + 4 * e] = v0;
-                                scores[(2 * t + 1) * 36 + mh * 16 + g + 4 * e] = v1;
-                            }
+                            for (int r = 0; r < NR; ++r)
+                                unpack_f32x2(fma_f32x2(fma_f32x2(ca_float2(d[0][2 * r], d[0][2 * r + 1]), base256, ca_float2(d[1][2 * r], d[1][2 * r + 1])), base256,
+                                                       ca_float2(d[2][2 * r], d[2][2 * r + 1])),
+                                             x[r][4 * j + 2 * two], x[r][4 * j + 2 * two + 1]);
                         }
-                        __syncwarp();
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float4 v = *reinterpret_cast<const float4 *>(scores + g * 36 + j * 16 + 4 * t);
-                            x[8 * half + 4 * j] = v.x;
-                            x[8 * half + 4 * j + 1] = v.y;
-                            x[8 * half + 4 * j + 2] = v.z;
-                            x[8 * half + 4 * j + 3] = v.w;
-                        }
-                        __syncwarp();
-                    }
-                    softmax_step(x, f, partly, sees_g - token0, token, alpha, worth);
-                    uint32_t b[DP][4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t w[4];
-                        if (DP == 3) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[4 * j + e]);
-                            b[0][j] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
-                        } else {  // (65535 p beside 128: p = 1 stays within 16 bits)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(fmaf(x[4 * j + e], 0.9999847412109375f, 128.0f));
-                        }
-                        const uint32_t w01 = __byte_perm(w[0], w[1], 0x5140), w23 = __byte_perm(w[2], w[3], 0x5140);
-                        b[DP - 2][j] = __byte_perm(w01, w23, 0x7632);
-                        b[DP - 1][j] = __byte_perm(w01, w23, 0x5410);
-                    }
-                    // (a row that sees none of the page takes nothing of it, not even a scale that is NaN)
+                    const float sk = stream ? sc.y : sc.x;
+                    uint32_t pd[DP][2][4];  // digits of the probabilities, as left operand of the two products over 32 tokens
+                    uint64_t scale2[NR], sv2[NR];
                     constexpr float kUnit = DP == 3 ? 1.1920928955078125e-7f : 1.0f / 65535.0f;
-                    float scale[2], sv[2];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        scale[e] = __shfl_sync(0xffffffffu, alpha, (2 * t + e) * 4);
-                        sv[e] = __shfl_sync(0xffffffffu, worth, (2 * t + e) * 4);
-                        sv[e] = sees_e[e] > token0 ? sv[e] * sc.z * kUnit : 0.0f;
+                    for (int r = 0; r < NR; ++r) {
+                        softmax_step(x[r], r, qs[r] * sk, partly, sees[r] - token0, token, alpha[r], worth[r]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t w[4];
+                            const int kt = j >> 1, at = 2 * (j & 1) + r;
+                            if (DP == 3) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[r][4 * j + e]);
+                                pd[0][kt][at] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
+                            } else {  // (65535 p beside 128: p = 1 stays within 16 bits)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(fmaf(x[r][4 * j + e], 0.9999847412109375f, 128.0f));
+                            }
+                            const uint32_t w01 = __byte_perm(w[0], w[1], 0x5140), w23 = __byte_perm(w[2], w[3], 0x5140);
+                            pd[DP - 2][kt][at] = __byte_perm(w01, w23, 0x7632);
+                            pd[DP - 1][kt][at] = __byte_perm(w01, w23, 0x5410);
+                        }
+                        // (a row that sees none of the page takes nothing of it, not even a scale that is NaN)
+                        const float sv = sees[r] > token0 ? worth[r] * sc.z * kUnit : 0.0f;
+                        scale2[r] = pack_f32x2(alpha[r], alpha[r]);
+                        sv2[r] = pack_f32x2(sv, sv);
                     }
-                    const uint64_t scale2 = pack_f32x2(scale[0], scale[1]), sv2 = pack_f32x2(sv[0], sv[1]);
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        int d[DP][4];
+                        uint4 v[2];
 #pragma unroll
-                        for (int kt = 0; kt < 2; ++kt) {
-                            const uint4 a = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
+                        for (int kt = 0; kt < 2; ++kt) v[kt] = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
 #pragma unroll
-                            for (int z = 0; z < DP; ++z) mma_s8u8(d[z], a, b[z][2 * kt], b[z][2 * kt + 1], kt ? d[z] : magic);
-                        }
+                        for (int a = 0; a < 2; ++a) {
+                            int d[DP][4];
+                            float (&o)[NE] = acc[ROWS == 1 ? 0 : 2 * mt + a];
 #pragma unroll
-                        for (int e = 0; e < NE; e += 2) {
-                            uint64_t v = fma_f32x2(ca_float2(d[0][e], d[0][e + 1]), base256, ca_float2(d[1][e], d[1][e + 1]));
-                            if (DP == 3) v = fma_f32x2(v, base256, ca_float2(d[DP - 1][e], d[DP - 1][e + 1]));
-                            unpack_f32x2(fma_f32x2(v, sv2, mul_f32x2(pack_f32x2(acc[mt][e], acc[mt][e + 1]), scale2)), acc[mt][e], acc[mt][e + 1]);
+                            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                                for (int z = 0; z < DP; ++z) mma_u8s8(d[z], pd[z][kt], a ? v[kt].y : v[kt].x, a ? v[kt].w : v[kt].z, kt ? d[z] : magic);
+#pragma unroll
+                            for (int r = 0; r < NR; ++r) {
+                                uint64_t y = fma_f32x2(ca_float2(d[0][2 * r], d[0][2 * r + 1]), base256, ca_float2(d[1][2 * r], d[1][2 * r + 1]));
+                                if (DP == 3) y = fma_f32x2(y, base256, ca_float2(d[DP - 1][2 * r], d[DP - 1][2 * r + 1]));
+                                unpack_f32x2(fma_f32x2(y, sv2[r], mul_f32x2(pack_f32x2(o[(2 * r) % NE], o[(2 * r + 1) % NE]), scale2[r])), o[(2 * r) % NE], o[(2 * r + 1) % NE]);
+                            }
                         }
                     }
                 }
@@ -669,103 +681,128 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                 // ---- 32 open tokens
                 const int rows = min(32, (k.s.length & 63) - 32 * (k.unit - k.s.pages));
                 const uint32_t at = ring_a + stage * C::STAGE;
-                const int q_at = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g);
-                const bool q_there = q_at < k.s.m * p.group;
-                auto q_pair = [&](int n, int col) -> uint32_t {  // q's values col, col + 1 of this lane's column
-                    if (!q_there || (ROWS == 1 && limb)) return 0;
-                    return *reinterpret_cast<const uint32_t *>(q_row(k, n, q_at) + col);
-                };
-                auto k_eight = [&](int n, int mt, int kt) {
-                    const int r = mt * 16 + (lane & 15);
-                    return ldmatrix4(at + n * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, kt * 2 + (lane >> 4)) * 16);
-                };
-                float d[2][4] = {};
-                uint32_t qb[DH / 16][2];
+                auto token = [&](int j) { return (j >> 1) * 8 + 2 * t + (j & 1); };
+                float x[NR][8], alpha[NR], worth[NR];
+                uint32_t qb[NR][DH / 16][2];  // q's values as pairs
 #pragma unroll
-                for (int kt = 0; kt < DH / 16; ++kt)
+                for (int r = 0; r < NR; ++r) {
+                    const int row = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g + 8 * r);
+                    const bool there = row < k.s.m * p.group && (ROWS == 16 || !limb);
+                    const __nv_bfloat16 *src = q_row(k, my_stream, there ? row : 0) + 2 * t;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) qb[kt][h] = q_pair(my_stream, kt * 16 + 8 * h + 2 * t);
+                    for (int kt = 0; kt < DH / 16; ++kt)
 #pragma unroll
-                for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n)
-#pragma unroll
-                    for (int kt = 0; kt < DH / 16; ++kt) {
-                        const bool mine = ROWS == 8 || my_stream == n;
-#pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(ROWS == 1 ? n : stream, mt, kt), mine ? qb[kt][0] : 0u, mine ? qb[kt][1] : 0u);
-                    }
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
-                    if (ROWS == 1) {
-                        if (!(t & 1)) {
-                            scores[(t >> 1) * kCacheBlock + mt * 16 + g] = d[mt][0];
-                            scores[(t >> 1) * kCacheBlock + mt * 16 + g + 8] = d[mt][2];
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) scores[(2 * t + (e & 1)) * 36 + mt * 16 + g + (e >> 1) * 8] = d[mt][e];
-                    }
+                        for (int h = 0; h < 2; ++h) qb[r][kt][h] = there ? *reinterpret_cast<const uint32_t *>(src + kt * 16 + 8 * h) : 0u;
                 }
-                __syncwarp();
-                const float *row = scores + (ROWS == 1 ? my_stream * kCacheBlock : g * 36);
-                float x[8], alpha, worth;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {  // tokens 8 j + 2 t, 8 j + 2 t + 1
-                    const float2 v = *reinterpret_cast<const float2 *>(row + 8 * j + 2 * t);
-                    x[2 * j] = v.x;
-                    x[2 * j + 1] = v.y;
-                }
-                __syncwarp();
-                // (a query that is not finite: its digits mean nothing, but the products of its bf16 values do; qs is NaN then)
-                softmax_step(x, qs == qs ? p.scale_log2 : qs, true, min(rows, sees_g - token0), [&](int j) { return (j >> 1) * 8 + 2 * t + (j & 1); }, alpha, worth);
                 // p as a sum of three bf16, each the rounding of what the ones before leave
-                uint32_t b[ROWS == 1 ? 1 : 3][2][2];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float a0 = x[2 * j], a1 = x[2 * j + 1];
+                auto three = [&](float a0, float a1, uint32_t (&w)[3]) {
 #pragma unroll
                     for (int z = 0; z < 3; ++z) {
                         const __nv_bfloat162 v = __floats2bfloat162_rn(a0, a1);
-                        const uint32_t w = *reinterpret_cast<const uint32_t *>(&v);
-                        if (ROWS == 8) b[ROWS == 8 ? z : 0][j >> 1][j & 1] = w;
-                        else if (limb == z) b[0][j >> 1][j & 1] = w;
-                        a0 -= bf16lo_to_float(w);
-                        a1 -= bf16hi_to_float(w);
+                        w[z] = *reinterpret_cast<const uint32_t *>(&v);
+                        a0 -= bf16lo_to_float(w[z]);
+                        a1 -= bf16hi_to_float(w[z]);
                     }
-                    if (ROWS == 1 && limb == 3) b[0][j >> 1][j & 1] = 0;
-                }
-                auto v_eight = [&](int mt, int kt) {
-                    const int r = kt * 16 + (lane & 7) + (lane >> 4) * 8;
-                    return ldmatrix4_trans(at + 2 * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, mt * 2 + (lane >> 3 & 1)) * 16);
                 };
+                auto v_four = [&](int i, int kt) {  // dims 16 i .. 16 i + 15 of sixteen tokens, as four 8 x 8: (dims 0-7, tokens 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15)
+                    const int r = kt * 16 + (lane & 7) + (lane >> 4) * 8;
+                    return ldmatrix4_trans(at + 2 * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, i * 2 + (lane >> 3 & 1)) * 16);
+                };
+                // (a query that is not finite: its digits mean nothing, but the products of its bf16 values do; qs is NaN then)
                 if constexpr (ROWS == 1) {
-                    const float scale = __shfl_sync(0xffffffffu, alpha, (t >> 1) * 16), sv = __shfl_sync(0xffffffffu, worth, (t >> 1) * 16);
+                    auto k_eight = [&](int n, int mt, int kt) {
+                        const int r = mt * 16 + (lane & 15);
+                        return ldmatrix4(at + n * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, kt * 2 + (lane >> 4)) * 16);
+                    };
+                    float d[2][4] = {};
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int kt = 0; kt < DH / 16; ++kt)
+#pragma unroll
+                            for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(n, mt, kt), my_stream == n ? qb[0][kt][0] : 0u, my_stream == n ? qb[0][kt][1] : 0u);
+                    if (!(t & 1)) {
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt) {
+                            scores[(t >> 1) * kCacheBlock + mt * 16 + g] = d[mt][0];
+                            scores[(t >> 1) * kCacheBlock + mt * 16 + g + 8] = d[mt][2];
+                        }
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 v = *reinterpret_cast<const float2 *>(scores + my_stream * kCacheBlock + 8 * j + 2 * t);
+                        x[0][2 * j] = v.x;
+                        x[0][2 * j + 1] = v.y;
+                    }
+                    __syncwarp();
+                    softmax_step(x[0], 0, qs[0] == qs[0] ? p.scale_log2 : qs[0], true, min(rows, sees[0] - token0), token, alpha[0], worth[0]);
+                    uint32_t b[2][2];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t w[3];
+                        three(x[0][2 * j], x[0][2 * j + 1], w);
+                        b[j >> 1][j & 1] = limb == 0 ? w[0] : limb == 1 ? w[1] : limb == 2 ? w[2] : 0u;
+                    }
+                    const float scale = __shfl_sync(0xffffffffu, alpha[0], (t >> 1) * 16), sv = __shfl_sync(0xffffffffu, worth[0], (t >> 1) * 16);
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
                         float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int kt = 0; kt < 2; ++kt) mma_bf16(o, v_eight(mt, kt), b[0][kt][0], b[0][kt][1]);
+                        for (int kt = 0; kt < 2; ++kt) mma_bf16(o, v_four(mt, kt), b[kt][0], b[kt][1]);
                         acc[mt][0] = fmaf(t & 1 ? o[0] : o[0] + o[1], sv, acc[mt][0] * scale);
                         acc[mt][1] = fmaf(t & 1 ? o[2] : o[2] + o[3], sv, acc[mt][1] * scale);
                     }
                 } else {
-                    float scale[2], sv[2];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        scale[e] = __shfl_sync(0xffffffffu, alpha, (2 * t + e) * 4);
-                        sv[e] = __shfl_sync(0xffffffffu, worth, (2 * t + e) * 4);
+                    for (int two = 0; two < 2; ++two) {  // sixteen tokens
+                        float d[2][4] = {};
+#pragma unroll
+                        for (int kt = 0; kt < DH / 16; ++kt) {
+                            const int r = two * 16 + (lane & 7) + (lane >> 4) * 8;  // (tokens 0-7, dims 0-7), (0-7, 8-15), (8-15, 0-7), (8-15, 8-15)
+                            const uint4 kk = ldmatrix4(at + stream * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, kt * 2 + (lane >> 3 & 1)) * 16);
+                            const uint4 a = make_uint4(qb[0][kt][0], qb[NR - 1][kt][0], qb[0][kt][1], qb[NR - 1][kt][1]);
+                            mma_bf16(d[0], a, kk.x, kk.y);
+                            mma_bf16(d[1], a, kk.z, kk.w);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[ROWS == 1 ? 0 : e >> 1][4 * two + 2 * i + (e & 1)] = d[i][e];
+                    }
+                    uint32_t b[2][3][4];  // the probabilities' three, as left operand of the products over sixteen tokens
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) {
+                        softmax_step(x[r], r, qs[r] == qs[r] ? p.scale_log2 : qs[r], true, min(rows, sees[r] - token0), token, alpha[r], worth[r]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t w[3];
+                            three(x[r][2 * j], x[r][2 * j + 1], w);
+#pragma unroll
+                            for (int z = 0; z < 3; ++z) b[j >> 1][z][2 * (j & 1) + r] = w[z];
+                        }
                     }
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        float o[2][4] = {};
 #pragma unroll
                         for (int kt = 0; kt < 2; ++kt) {
-                            const uint4 a = v_eight(mt, kt);
+                            const uint4 v = v_four(mt, kt);
 #pragma unroll
-                            for (int z = 0; z < 3; ++z) mma_bf16(o, a, b[ROWS == 8 ? z : 0][kt][0], b[ROWS == 8 ? z : 0][kt][1]);
+                            for (int z = 0; z < 3; ++z) {
+                                const uint4 a = make_uint4(b[kt][z][0], b[kt][z][1], b[kt][z][2], b[kt][z][3]);
+                                mma_bf16(o[0], a, v.x, v.z);
+                                mma_bf16(o[1], a, v.y, v.w);
+                            }
                         }
                         // (a row that sees none of these tokens takes nothing of them, not even a value that is NaN)
 #pragma unroll
-                        for (int e = 0; e < NE; ++e) acc[mt][e] = sees_e[e & 1] > token0 ? fmaf(o[e], sv[e & 1], acc[mt][e] * scale[e & 1]) : acc[mt][e];
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < NE; ++e) {
+                                float &y = acc[ROWS == 1 ? 0 : 2 * mt + i][e];
+                                if (sees[(e >> 1) % NR] > token0) y = fmaf(o[i][e], worth[(e >> 1) % NR], y * alpha[(e >> 1) % NR]);
+                            }
                     }
                 }
             }
@@ -781,11 +818,14 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
             float *part = my_parts + (first_item && !whole ? 0 : part_floats) + my_tile * (ROWS * C::PART);
             const CaItem it = {u - k.unit, u - k.unit + k.s.units, k.s.row0, k.s.m, k.head, k.tile};
             if (u + 1 == u1 && leads && lane == 0) last_item_of[team] = it;
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+            }
             if constexpr (ROWS == 1) {
-                const float l1 = __shfl_sync(0xffffffffu, l, 0), l2 = __shfl_sync(0xffffffffu, l, 16);
-                const float m1 = __shfl_sync(0xffffffffu, m, 0), m2 = __shfl_sync(0xffffffffu, m, 16);
+                const float l1 = __shfl_sync(0xffffffffu, l[0], 0), l2 = __shfl_sync(0xffffffffu, l[0], 16);
+                const float m1 = __shfl_sync(0xffffffffu, m[0], 0), m2 = __shfl_sync(0xffffffffu, m[0], 16);
                 float i1 = 0.0f, i2 = 0.0f;
                 if (whole) {
                     i1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f;
@@ -808,28 +848,30 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                 if (!whole && lane == 0) *reinterpret_cast<float4 *>(part) = make_float4(m1, l1, m2, l2);
             } else {
                 // the second stream's warps leave their sums, of a whole item as they enter the output; the first's finish those
-                if (!whole && t == 0) *reinterpret_cast<float2 *>(part + g * C::PART + 2 * stream) = make_float2(m, l);
-                float inv[2];
+                float inv[NR];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float le = __shfl_sync(0xffffffffu, l, (2 * t + e) * 4);
-                    inv[e] = !whole ? 1.0f : le != 0.0f ? (stream ? p.lambda : 1.0f) * p.out_scale / le : 0.0f;
+                for (int r = 0; r < NR; ++r) {
+                    float *mine = part + (g + 8 * r) * C::PART;
+                    if (!whole && t == 0) *reinterpret_cast<float2 *>(mine + 2 * stream) = make_float2(m[r], l[r]);
+                    inv[r] = !whole ? 1.0f : l[r] != 0.0f ? (stream ? p.lambda : 1.0f) * p.out_scale / l[r] : 0.0f;
+                    if (!whole || stream)
+#pragma unroll
+                        for (int a = 0; a < NA; ++a)
+                            *reinterpret_cast<float2 *>(mine + 4 + stream * DH + 8 * a + 2 * t) = make_float2(acc[a][(2 * r) % NE] * inv[r], acc[a][(2 * r + 1) % NE] * inv[r]);
                 }
-                if (!whole || stream)
-#pragma unroll
-                    for (int mt = 0; mt < C::MT; ++mt)
-#pragma unroll
-                        for (int e = 0; e < NE; ++e) part[(2 * t + (e & 1)) * C::PART + 4 + stream * DH + mt * 16 + g + 8 * (e >> 1)] = acc[mt][e] * inv[e & 1];
                 if (whole) {
                     team_sync();
-                    if (!stream) {
 #pragma unroll
-                        for (int mt = 0; mt < C::MT; ++mt)
+                    for (int r = 0; r < NR; ++r) {
+                        const int row = my_tile * ROWS + g + 8 * r, rr = k.tile * tile_rows + row;
+                        if (!stream && rr < k.s.m * p.group) {
+                            const float *other = part + (g + 8 * r) * C::PART + 4 + DH + 2 * t;
 #pragma unroll
-                            for (int e = 0; e < NE; ++e) {
-                                const int r = 2 * t + (e & 1), dim = mt * 16 + g + 8 * (e >> 1), rr = k.tile * tile_rows + my_tile * 8 + r;
-                                if (rr < k.s.m * p.group) ca_write(p, it, rr, DH, dim, acc[mt][e] * inv[e & 1] - part[r * C::PART + 4 + DH + dim]);
+                            for (int a = 0; a < NA; ++a) {
+                                const float2 o = *reinterpret_cast<const float2 *>(other + 8 * a);
+                                ca_write2(p, it, rr, DH, 8 * a + 2 * t, acc[a][(2 * r) % NE] * inv[r] - o.x, acc[a][(2 * r + 1) % NE] * inv[r] - o.y);
                             }
+                        }
                     }
                 }
             }
@@ -893,18 +935,15 @@ __global__ void __launch_bounds__(8 * DH / 4) cached_attention_join_kernel(CaPar
     sum.write(p, it, it.tile * all + r, DH, dim);
 }
 
-// How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows, as many to a team as
-// the sequences have on average, up to four (any call is right in any of these forms).
+// How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of sixteen rows, two to a team where the
+// sequences have more than that on average (any call is right in any of these forms).
 struct CaForm {
     int rows, tiles, teams, stages, threads;
 };
 static CaForm ca_form(int head_dim, int64_t n_seqs, int64_t n_rows, int group) {
     if (n_rows * group <= n_seqs) return head_dim == 64 ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
-    const int64_t rows = (n_rows * group + n_seqs - 1) / n_seqs;
-    const int tiles = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-    // (two units of a ring at least)
-    const int all = head_dim == 64 ? 16 : 8, most = all / 2, teams = 8 / tiles < most ? 8 / tiles : most;
-    return CaForm{8, tiles, teams, all / teams, teams * tiles * 64};
+    const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;
+    return CaForm{16, tiles, teams, (head_dim == 64 ? 16 : 8) / teams, 256};
 }
 
 template <int DH, int ROWS, int DP>
@@ -921,7 +960,7 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid, (unsigned)p.tiles);
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)(ROWS == 1 ? 1 : p.tiles * ROWS / 8));
     cfg.blockDim = dim3(8 * DH / 4);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -984,7 +1023,7 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     const cudaStream_t stream = (cudaStream_t)stream_;
     cudaError_t e;
     if (f.rows == 1) e = dh == 64 ? launch_cached_attention<64, 1, 3>(p, f.threads, stream) : launch_cached_attention<128, 1, 3>(p, f.threads, stream);
-    else if (p.bf16) e = dh == 64 ? launch_cached_attention<64, 8, 2>(p, f.threads, stream) : launch_cached_attention<128, 8, 2>(p, f.threads, stream);
-    else e = dh == 64 ? launch_cached_attention<64, 8, 3>(p, f.threads, stream) : launch_cached_attention<128, 8, 3>(p, f.threads, stream);
+    else if (p.bf16) e = dh == 64 ? launch_cached_attention<64, 16, 2>(p, f.threads, stream) : launch_cached_attention<128, 16, 2>(p, f.threads, stream);
+    else e = dh == 64 ? launch_cached_attention<64, 16, 3>(p, f.threads, stream) : launch_cached_attention<128, 16, 3>(p, f.threads, stream);
     return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
 }
