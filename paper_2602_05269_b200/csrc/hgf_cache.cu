@@ -40,226 +40,333 @@ __device__ static bool last_arrival(int32_t *arrivals, int blocks) {
     return true;
 }
 
+// The sequence and piece of a block of threads: piece x of the launch belongs to sequence i, where sequence i has its pieces from
+// starts[i] / 64 + i * per on (`per` pieces and one for each 64 rows are room for all that it can have).  All threads call it; `slots` (shared memory)
+// holds the list of slots afterwards.
+struct CachePiece {
+    int i;        // -1: the starts are no ascending row numbers up to n_rows
+    int row0, m;  // the sequence's rows
+    int piece;
+    int slot;
+    bool first;   // no earlier entry of the list names the slot
+};
+__device__ __forceinline__ CachePiece find_piece(const int32_t *__restrict__ list, const int32_t *__restrict__ starts, int n, int n_rows, int per, int x, int *slots) {
+    CachePiece p = {-1, 0, 0, 0, -1, false};
+    int below = 0;
+    bool bad = false;
+    for (int j0 = 0; j0 < n; j0 += blockDim.x) {
+        const int j = j0 + threadIdx.x;
+        bool mine = false;
+        if (j < n) {
+            const int a = starts[j], b = starts[j + 1];
+            slots[j] = list[j];
+            bad = bad || a < 0 || b < a || b > n_rows;
+            mine = (a >> 6) + j * per <= x;
+        }
+        below += __syncthreads_count(mine);
+    }
+    if (__syncthreads_or(bad)) return p;
+    p.i = below - 1;
+    p.row0 = starts[p.i];
+    p.m = starts[p.i + 1] - p.row0;
+    p.piece = x - ((p.row0 >> 6) + p.i * per);
+    p.slot = slots[p.i];
+    bool again = false;
+    for (int j = threadIdx.x; j < p.i; j += blockDim.x) again = again || slots[j] == p.slot;
+    p.first = !__syncthreads_or(again);
+    return p;
+}
+// Blocks of threads a piece's heads are dealt to, so that there are about `blocks` in all: a block's look-ups serve several heads where there are many pieces.
+static unsigned head_shares(int64_t pieces, int H, int blocks) {
+    const int64_t want = (blocks + pieces - 1) / pieces;
+    const int64_t each = (H + (want < H ? want : H) - 1) / (want < H ? want : H);  // heads of a block
+    return (unsigned)((H + each - 1) / each);
+}
+
 // ---- append ---------------------------------------------------------------------------------------------------------------------
-// A block of threads takes one K/V head of one piece: a block of 64 tokens that becomes complete, whose values it reads from the open rows and the
-// new ones, quantises, and writes as a page; the sequence's first piece also writes the rows that stay open, after its reads of the rows that
-// these replace.  Bound by memory: each new value is read once, each code written once.
+// A block of threads takes one piece and every gridDim.y-th K/V head of it: a block of 64 tokens that becomes complete, whose values it reads from the open
+// rows and the new ones, quantises, and writes as a page; the sequence's first piece also writes the rows that stay open, after its reads of the rows
+// that these replace.  Each new value is read once, each code written once; what bounds it is the chain of dependent look-ups in front (starts, slot, length,
+// table, counts: about 4 us), which is why a block has several heads.
 constexpr int kAppendThreads = 256;
 
+// Four lanes (l, l + 8, l + 16, l + 24) hold a word of four bytes each, a 4 x 4 matrix: its transpose.
+__device__ __forceinline__ uint32_t transpose_bytes(uint32_t w, int lane) {
+    uint32_t o = __shfl_xor_sync(0xffffffffu, w, 16);
+    w = lane & 16 ? __byte_perm(o, w, 0x7632) : __byte_perm(w, o, 0x5410);
+    o = __shfl_xor_sync(0xffffffffu, w, 8);
+    return lane & 8 ? __byte_perm(o, w, 0x7351) : __byte_perm(w, o, 0x6240);
+}
+
 template <int DH>
-__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(CacheView c, const __nv_bfloat16 *__restrict__ k, const __nv_bfloat16 *__restrict__ v, int n_rows,
+__global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append_kernel(CacheView c, const __nv_bfloat16 *__restrict__ k, const __nv_bfloat16 *__restrict__ v, int n_rows,
                                                                        const int32_t *__restrict__ slots, const int32_t *__restrict__ starts, int n_seqs, int32_t *done,
                                                                        unsigned int *status) {
-    constexpr int EIGHTS = DH / 8, PER = kCacheBlock * EIGHTS / kAppendThreads;  // eights of a row; eights of one tensor's block a thread holds
+    constexpr int EIGHTS = DH / 8, PER = kCacheBlock * EIGHTS / kAppendThreads, WARPS = kAppendThreads / 32;  // eights of a row; eights of one tensor's block a thread holds
     __shared__ __align__(16) uint8_t page_smem[3 * kCacheBlock * DH];
-    __shared__ uint32_t top_smem[3][kAppendThreads / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, head = blockIdx.y, H = c.H;
-
-    const int i = cache_find_sequence(starts, n_seqs, n_rows, 1, blockIdx.x);
-    if (i < 0) {
+    __shared__ uint32_t top_smem[3][WARPS];
+    __shared__ int slot_smem[kCacheMaxSeqs];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, head0 = blockIdx.y, H = c.H;
+    pdl_launch_dependents();
+    pdl_wait();
+    const CachePiece p = find_piece(slots, starts, n_seqs, n_rows, 1, blockIdx.x, slot_smem);
+    if (p.i < 0) {
         if (tid == 0) {
             atomicOr(status, kStatusCache);
-            if (done && head == 0)
+            if (done && head0 == 0)
                 for (int j = blockIdx.x; j < n_seqs; j += gridDim.x) done[j] = 0;
         }
         return;
     }
-    const int row0 = starts[i], m = starts[i + 1] - row0, piece = (int)blockIdx.x - ((row0 >> 6) + i), slot = slots[i];
-    const bool first = cache_first_of(slots, i, slot), leads = piece == 0 && head == 0 && tid == 0;
-    if (slot < 0 || slot >= c.n_slots || !first) {
+    const int i = p.i, row0 = p.row0, m = p.m, piece = p.piece, slot = p.slot;
+    const bool leads = piece == 0 && head0 == 0 && tid == 0;
+    if (slot < 0 || slot >= c.n_slots || !p.first) {
         if (leads) {
             if (done) done[i] = 0;
-            if (slot != -1 && first) atomicOr(status, kStatusCache);
+            if (slot != -1 && p.first) atomicOr(status, kStatusCache);
         }
         return;
     }
     const int held = c.held[slot], length = c.length[slot], block0 = length >> 6, open0 = length & 63;
     const long long after = (long long)length + m;
     const bool sane = cache_slot_ok(c, held, length);
-    bool fits = sane && (after >> 6) <= held, in_range = true;
-    const int blocks = fits ? (int)(after >> 6) - block0 : 0;
+    bool fits = sane && (after >> 6) <= held;
+    const int blocks = fits ? (int)(after >> 6) - block0 : 0, pieces = blocks > 1 ? blocks : 1;
     const int32_t *table = c.table + (size_t)slot * c.max_pages + (sane ? block0 : 0);
-    {
-        bool shared = false, off = false;
-        for (int b = tid; b < blocks; b += kAppendThreads) {
-            const int page = table[b];
-            const bool ok = page >= 0 && page < c.n_pages;
-            off = off || !ok;
-            shared = shared || (ok && c.refs[page] != 1);
-        }
-        in_range = !__syncthreads_or(off);
-        fits = !__syncthreads_or(shared) && fits && in_range;
+    const size_t kw = (size_t)2 * H * DH, vw = (size_t)H * DH;
+    auto open_rows = [&](int head) { return c.open + ((size_t)slot * H + head) * (3 * kCacheBlock * DH); };
+    auto new_eight = [&](int n, int head, int row, int eight) {  // eight `eight` of a head of tensor n of the call's row `row`
+        const __nv_bfloat16 *src = n < 2 ? k + (size_t)row * kw + ((size_t)n * H + head) * DH : v + (size_t)row * vw + (size_t)head * DH;
+        return *reinterpret_cast<const uint4 *>(src + 8 * eight);
+    };
+    // A warp's lanes take eight eights of four rows.
+    auto row_of = [&](int u) { return (warp + u * WARPS) / (EIGHTS / 8) * 4 + (lane >> 3); };
+    auto eight_of = [&](int u) { return (warp + u * WARPS) % (EIGHTS / 8) * 8 + (lane & 7); };
+    const int t0 = (block0 + piece) * kCacheBlock;  // first token of the block
+    uint4 x[3][PER];
+    auto load = [&](int head) {
+        const __nv_bfloat16 *open = open_rows(head);
+#pragma unroll
+        for (int n = 0; n < 3; ++n)
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const int r = row_of(u), e = eight_of(u);
+                x[n][u] = t0 + r < length ? *reinterpret_cast<const uint4 *>(open + ((size_t)n * kCacheBlock + r) * DH + 8 * cache_open_eight(r, e))
+                                          : new_eight(n, head, row0 + t0 + r - length, e);
+            }
+    };
+    if (piece < blocks) load(head0);  // (on their way during the look-ups below)
+    bool shared = false, off = false;
+    for (int b = tid; b < blocks; b += kAppendThreads) {
+        const int page = table[b];
+        const bool ok = page >= 0 && page < c.n_pages;
+        off = off || !ok;
+        shared = shared || (ok && c.refs[page] != 1);
+    }
+    if (blocks) {
+        off = __syncthreads_or(off);
+        fits = !__syncthreads_or(shared) && !off;
     }
     if (!fits) {
         if (leads) {
             if (done) done[i] = 0;
-            if (!sane || !in_range) atomicOr(status, kStatusCache);
+            if (!sane || off) atomicOr(status, kStatusCache);
         }
         return;
     }
-    const int pieces = blocks > 1 ? blocks : 1;
     if (piece >= pieces) return;
 
-    const size_t kw = (size_t)2 * H * DH, vw = (size_t)H * DH;
-    __nv_bfloat16 *open = c.open + ((size_t)slot * H + head) * (3 * kCacheBlock * DH);
-    auto new_eight = [&](int n, int row, int eight) {  // eight `eight` of tensor n of the call's row `row`
-        const __nv_bfloat16 *src = n < 2 ? k + (size_t)row * kw + ((size_t)n * H + head) * DH : v + (size_t)row * vw + (size_t)head * DH;
-        return *reinterpret_cast<const uint4 *>(src + 8 * eight);
-    };
     if (piece < blocks) {
-        const int t0 = (block0 + piece) * kCacheBlock;  // first token of the block
-        uint4 x[3][PER];
-        uint32_t top[3];
-#pragma unroll
-        for (int n = 0; n < 3; ++n) {
-#pragma unroll
-            for (int u = 0; u < PER; ++u) {
-                const int at = tid + u * kAppendThreads, r = at / EIGHTS, e = at % EIGHTS;
-                x[n][u] = t0 + r < length ? *reinterpret_cast<const uint4 *>(open + ((size_t)n * kCacheBlock + r) * DH + 8 * cache_open_eight(r, e))
-                                          : new_eight(n, row0 + t0 + r - length, e);
+        const int page = table[piece];
+        for (int head = head0; head < H; head += gridDim.y) {
+            if (head != head0) {
+                load(head);
+                __syncthreads();  // (the page before has left shared memory)
             }
-        }
 #pragma unroll
-        for (int n = 0; n < 3; ++n) {
-            uint32_t acc = 0;
+            for (int n = 0; n < 3; ++n) {
+                uint32_t acc = 0;
 #pragma unroll
-            for (int u = 0; u < PER; ++u) acc = absmax8_bits(acc, x[n][u]);
-            acc = __reduce_max_sync(0xffffffffu, max(acc >> 16, acc & 0xffffu));
-            if (lane == 0) top_smem[n][warp] = acc;
-        }
-        __syncthreads();
+                for (int u = 0; u < PER; ++u) acc = absmax8_bits(acc, x[n][u]);
+                acc = __reduce_max_sync(0xffffffffu, max(acc >> 16, acc & 0xffffu));
+                if (lane == 0) top_smem[n][warp] = acc;
+            }
+            __syncthreads();
+            uint32_t top[3];
 #pragma unroll
-        for (int n = 0; n < 3; ++n) {
-            top[n] = 0;
+            for (int n = 0; n < 3; ++n) {
+                top[n] = 0;
 #pragma unroll
-            for (int w = 0; w < kAppendThreads / 32; ++w) top[n] = max(top[n], top_smem[n][w]);
-            const float gamma = __uint_as_float(top[n] << 16);
-            // (bf16 patterns from 0x7f80 on are infinities and NaN; below 2^-100 the quotient 127 / max could leave binary32's range)
-            const bool zero = top[n] == 0 || top[n] >= 0x7f80u;
-            QuantScale s = make_quant_scale(gamma);
-            if (gamma < 7.9e-31f) s.fast = false;
+                for (int w = 0; w < WARPS; ++w) top[n] = max(top[n], top_smem[n][w]);
+                const float gamma = __uint_as_float(top[n] << 16);
+                // (bf16 patterns from 0x7f80 on are infinities and NaN; below 2^-100 the quotient 127 / max could leave binary32's range)
+                const bool zero = top[n] == 0 || top[n] >= 0x7f80u;
+                QuantScale s = make_quant_scale(gamma);
+                if (gamma < 7.9e-31f) s.fast = false;
+                uint8_t *dst = page_smem + n * kCacheBlock * DH;
 #pragma unroll
-            for (int u = 0; u < PER; ++u) {
-                const int at = tid + u * kAppendThreads, r = at / EIGHTS, e = at % EIGHTS;
-                int sum = 0;
-                const uint2 q = zero ? make_uint2(0, 0) : quant8(x[n][u], s, sum);
-                if (n < 2) {
-                    uint8_t *dst = page_smem + n * kCacheBlock * DH;
-                    *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(r, 8 * e, DH)) = q.x;
-                    *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(r, 8 * e + 4, DH)) = q.y;
-                } else {
-                    uint8_t *dst = page_smem + 2 * kCacheBlock * DH;
-#pragma unroll
-                    for (int b = 0; b < 8; ++b) dst[cache_tile_byte(8 * e + b, r, kCacheBlock)] = (uint8_t)((b < 4 ? q.x : q.y) >> (8 * (b & 3)));
+                for (int u = 0; u < PER; ++u) {
+                    const int r = row_of(u), e = eight_of(u);
+                    int sum = 0;
+                    const uint2 q = zero ? make_uint2(0, 0) : quant8(x[n][u], s, sum);
+                    if (n < 2) {
+                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(r, 8 * e, DH)) = q.x;
+                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(r, 8 * e + 4, DH)) = q.y;
+                    } else {  // four lanes' rows become four bytes of a dim each
+                        const int d = 8 * e + (lane >> 3), r4 = r & ~3;
+                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(d, r4, kCacheBlock)) = transpose_bytes(q.x, lane);
+                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(d + 4, r4, kCacheBlock)) = transpose_bytes(q.y, lane);
+                    }
                 }
             }
-        }
-        __syncthreads();
-        const size_t at = (size_t)table[piece] * H + head;
-        uint4 *dst = reinterpret_cast<uint4 *>(c.codes + at * (3 * kCacheBlock * DH));
-        for (int j = tid; j < 3 * kCacheBlock * DH / 16; j += kAppendThreads) dst[j] = reinterpret_cast<const uint4 *>(page_smem)[j];
-        if (tid == 0) {
-            auto scale = [](uint32_t t) { return t >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __fdiv_rn(__uint_as_float(t << 16), 127.0f); };
-            c.scales[at] = make_float4(scale(top[0]), scale(top[1]), scale(top[2]), 0.0f);
+            __syncthreads();
+            const size_t at = (size_t)page * H + head;
+            uint4 *dst = reinterpret_cast<uint4 *>(c.codes + at * (3 * kCacheBlock * DH));
+#pragma unroll
+            for (int j = 0; j < 3 * kCacheBlock * DH / 16 / kAppendThreads; ++j) dst[tid + j * kAppendThreads] = reinterpret_cast<const uint4 *>(page_smem)[tid + j * kAppendThreads];
+            if (tid == 0) {
+                auto scale = [](uint32_t t) { return t >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __fdiv_rn(__uint_as_float(t << 16), 127.0f); };
+                c.scales[at] = make_float4(scale(top[0]), scale(top[1]), scale(top[2]), 0.0f);
+            }
         }
     }
     if (piece == 0) {
         // rows that stay open: those of the last block, or all new ones if none became complete
         const int from = blocks ? 0 : open0, rows = blocks ? (int)(after & 63) : m, src0 = row0 + m - rows;
-        for (int at = tid; at < 3 * rows * EIGHTS; at += kAppendThreads) {
-            const int n = at / (rows * EIGHTS), r = at / EIGHTS % rows, e = at % EIGHTS;
-            *reinterpret_cast<uint4 *>(open + ((size_t)n * kCacheBlock + from + r) * DH + 8 * cache_open_eight(from + r, e)) = new_eight(n, src0 + r, e);
+        const int heads = (H - head0 + gridDim.y - 1) / gridDim.y, all = heads * 3 * rows * EIGHTS;
+        for (int at = tid; at < all; at += kAppendThreads) {
+            const int e = at % EIGHTS, n = at / EIGHTS % 3, head = head0 + at / (3 * EIGHTS) % heads * gridDim.y, r = at / (3 * EIGHTS * heads);
+            *reinterpret_cast<uint4 *>(open_rows(head) + ((size_t)n * kCacheBlock + from + r) * DH + 8 * cache_open_eight(from + r, e)) = new_eight(n, head, src0 + r, e);
         }
     }
     __syncthreads();
-    if (tid == 0 && last_arrival(c.arrivals + slot, pieces * H)) {
+    if (tid == 0 && last_arrival(c.arrivals + slot, pieces * gridDim.y)) {
         c.length[slot] = (int)after;
         if (done) done[i] = 1;
     }
 }
 
 // ---- read -------------------------------------------------------------------------------------------------------------------------
-// A block of threads takes one K/V head of one block of tokens that a range touches: the page through shared memory, whole, since a token's codes are
-// spread over it; open rows straight from where they are.
+// A block of threads takes one block of tokens that a range touches and every gridDim.y-th K/V head of it: the page through shared memory, whole, since a
+// token's codes are spread over it, the next head's on its way meanwhile; open rows straight from where they are.  Bound by the writes.
 constexpr int kReadThreads = 256;
 
+template <int DH>
+constexpr int kReadSmem = 2 * 3 * kCacheBlock * DH;
+
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory"); }
+
+// Byte k of w, a signed code, as a float.
+__device__ __forceinline__ float code_float(uint32_t flipped, int k) { return __uint_as_float(__byte_perm(flipped, 0x4b000000u, 0x7540 + k)) - 8388736.0f; }
+
 template <int DH, bool BF16>
-__global__ void __launch_bounds__(kReadThreads) cache_read_kernel(CacheView c, const int32_t *__restrict__ slots, const int32_t *__restrict__ firsts, const int32_t *__restrict__ starts,
+__global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c, const int32_t *__restrict__ slots, const int32_t *__restrict__ firsts, const int32_t *__restrict__ starts,
                                                                    int n_seqs, int n_rows, void *__restrict__ k_out, void *__restrict__ v_out, unsigned int *status) {
-    constexpr int EIGHTS = DH / 8;
-    __shared__ __align__(16) uint8_t page_smem[3 * kCacheBlock * DH];
-    const int tid = threadIdx.x, head = blockIdx.y, H = c.H;
-    const int i = cache_find_sequence(starts, n_seqs, n_rows, 2, blockIdx.x);
-    if (i < 0) {
+    constexpr int EIGHTS = DH / 8, PAGE = 3 * kCacheBlock * DH;
+    extern __shared__ __align__(16) uint8_t pages_smem[];
+    __shared__ int slot_smem[kCacheMaxSeqs];
+    const int tid = threadIdx.x, head0 = blockIdx.y, H = c.H;
+    pdl_launch_dependents();
+    pdl_wait();
+    const CachePiece p = find_piece(slots, starts, n_seqs, n_rows, 2, blockIdx.x, slot_smem);
+    if (p.i < 0) {
         if (tid == 0) atomicOr(status, kStatusCache);
         return;
     }
-    const int row0 = starts[i], m = starts[i + 1] - row0, piece = (int)blockIdx.x - ((row0 >> 6) + 2 * i), slot = slots[i];
+    const int row0 = p.row0, m = p.m, slot = p.slot;
     if (slot == -1 || m == 0) return;
-    const int first = firsts[i];
+    const int first = firsts[p.i];
     if (slot < 0 || slot >= c.n_slots || first < 0 || !cache_slot_ok(c, c.held[slot], c.length[slot])) {
         if (tid == 0) atomicOr(status, kStatusCache);
         return;
     }
     const int length = c.length[slot];
-    const long long end = min((long long)first + m, (long long)length), b0 = (long long)((first >> 6) + piece) << 6;
+    const long long end = min((long long)first + m, (long long)length), b0 = (long long)((first >> 6) + p.piece) << 6;
     const int from = (int)max(b0, (long long)first), to = (int)min(b0 + kCacheBlock, end);
     if (from >= to) return;
-    const bool closed = b0 + kCacheBlock <= length;
-    const __nv_bfloat16 *open = c.open + ((size_t)slot * H + head) * (3 * kCacheBlock * DH);
-    float sc[3] = {0.0f, 0.0f, 0.0f};
-    if (closed) {
-        const int page = c.table[(size_t)slot * c.max_pages + (int)(b0 >> 6)];
-        if (page < 0 || page >= c.n_pages) {
-            if (tid == 0) atomicOr(status, kStatusCache);
-            return;
-        }
-        const size_t at = (size_t)page * H + head;
-        const uint4 *src = reinterpret_cast<const uint4 *>(c.codes + at * (3 * kCacheBlock * DH));
-#pragma unroll 4
-        for (int j = tid; j < 3 * kCacheBlock * DH / 16; j += kReadThreads) reinterpret_cast<uint4 *>(page_smem)[j] = src[j];
-        const float4 s4 = c.scales[at];
-        sc[0] = s4.x;
-        sc[1] = s4.y;
-        sc[2] = s4.z;
-        __syncthreads();
-    }
     const int rows = to - from, r0 = (int)(from - b0);
     const size_t kw = (size_t)2 * H * DH, vw = (size_t)H * DH, out0 = (size_t)row0 + (from - first);
+    // values at a row of the range, from dim `dim` of a head of tensor n on
+    auto put = [&](int n, int head, int row, int dim, const auto &f) {
+        constexpr int N = sizeof(f) / sizeof(float);
+        const size_t o = n < 2 ? (out0 + row) * kw + ((size_t)n * H + head) * DH + dim : (out0 + row) * vw + (size_t)head * DH + dim;
+        void *base = n < 2 ? k_out : v_out;
+        if (BF16) {
+            uint32_t w[N / 2];
 #pragma unroll
-    for (int n = 0; n < 3; ++n)
-        for (int at = tid; at < rows * EIGHTS; at += kReadThreads) {
-            const int r = r0 + at / EIGHTS, e = at % EIGHTS;
-            float f[8];
-            if (closed) {
-                const uint8_t *src = page_smem + n * kCacheBlock * DH;
-                if (n < 2) {
-                    const uint32_t w[2] = {*reinterpret_cast<const uint32_t *>(src + cache_tile_byte(r, 8 * e, DH)), *reinterpret_cast<const uint32_t *>(src + cache_tile_byte(r, 8 * e + 4, DH))};
-#pragma unroll
-                    for (int b = 0; b < 8; ++b) f[b] = (float)(int8_t)(w[b >> 2] >> (8 * (b & 3))) * sc[n];
-                } else {
-#pragma unroll
-                    for (int b = 0; b < 8; ++b) f[b] = (float)(int8_t)src[cache_tile_byte(8 * e + b, r, kCacheBlock)] * sc[n];
-                }
-            } else {
-                unpack8(*reinterpret_cast<const uint4 *>(open + ((size_t)n * kCacheBlock + r) * DH + 8 * cache_open_eight(r, e)), f);
+            for (int b = 0; b < N / 2; ++b) {
+                const __nv_bfloat162 x = __floats2bfloat162_rn(f[2 * b], f[2 * b + 1]);
+                w[b] = *reinterpret_cast<const uint32_t *>(&x);
             }
-            const size_t o = n < 2 ? (out0 + at / EIGHTS) * kw + ((size_t)n * H + head) * DH + 8 * e : (out0 + at / EIGHTS) * vw + (size_t)head * DH + 8 * e;
-            void *base = n < 2 ? k_out : v_out;
-            if (BF16) {
-                uint32_t w[4];
+            if constexpr (N == 8) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(base) + o) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(base) + o) = make_uint2(w[0], w[1]);
+        } else {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * b], f[2 * b + 1]);
-                    w[b] = *reinterpret_cast<const uint32_t *>(&p);
-                }
-                *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(base) + o) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-                float4 *dst = reinterpret_cast<float4 *>(reinterpret_cast<float *>(base) + o);
-                dst[0] = make_float4(f[0], f[1], f[2], f[3]);
-                dst[1] = make_float4(f[4], f[5], f[6], f[7]);
+            for (int b = 0; b < N; b += 4) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(base) + o + b) = make_float4(f[b], f[b + 1], f[b + 2], f[b + 3]);
+        }
+    };
+    if (b0 + kCacheBlock > length) {
+        const int heads = (H - head0 + gridDim.y - 1) / gridDim.y, all = heads * 3 * rows * EIGHTS;
+#pragma unroll 4
+        for (int at = tid; at < all; at += kReadThreads) {
+            const int e = at % EIGHTS, n = at / EIGHTS % 3, head = head0 + at / (3 * EIGHTS) % heads * gridDim.y, row = at / (3 * EIGHTS * heads), r = r0 + row;
+            float f[8];
+            unpack8(*reinterpret_cast<const uint4 *>(c.open + (((size_t)slot * H + head) * 3 + n) * (kCacheBlock * DH) + (size_t)r * DH + 8 * cache_open_eight(r, e)), f);
+            put(n, head, row, 8 * e, f);
+        }
+        return;
+    }
+    const int page = c.table[(size_t)slot * c.max_pages + (int)(b0 >> 6)];
+    if (page < 0 || page >= c.n_pages) {
+        if (tid == 0) atomicOr(status, kStatusCache);
+        return;
+    }
+    const uint32_t smem = dsmem_u32(pages_smem);
+    auto fetch = [&](int head, int buf) {
+        if (head < H) {
+            const int8_t *src = c.codes + ((size_t)page * H + head) * PAGE;
+#pragma unroll
+            for (int j = 0; j < PAGE / 16 / kReadThreads; ++j) copy_async16(smem + buf * PAGE + (tid + j * kReadThreads) * 16, src + (tid + j * kReadThreads) * 16);
+        }
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+    };
+    fetch(head0, 0);
+    int buf = 0;
+    for (int head = head0; head < H; head += gridDim.y, buf ^= 1) {
+        const float4 sc = c.scales[(size_t)page * H + head];
+        fetch(head + gridDim.y, buf ^ 1);
+        asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+        __syncthreads();
+        const uint8_t *src = pages_smem + buf * PAGE;
+#pragma unroll 2
+        for (int at = tid; at < 2 * rows * EIGHTS; at += kReadThreads) {
+            const int e = at % EIGHTS, n = at / EIGHTS & 1, row = at / (2 * EIGHTS), r = r0 + row;
+            const float s = n ? sc.y : sc.x;
+            float f[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(src + n * kCacheBlock * DH + cache_tile_byte(r, 8 * e + 4 * h, DH)) ^ 0x80808080u;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) f[4 * h + b] = code_float(w, b) * s;
+            }
+            put(n, head, row, 8 * e, f);
+        }
+        // four rows of four dims of V at a time: a word is four tokens of a dim
+#pragma unroll
+        for (int u = 0; u < kCacheBlock / 4 * (DH / 4) / kReadThreads; ++u) {
+            const int at = tid + u * kReadThreads, d = at % (DH / 4) * 4, r4 = at / (DH / 4) * 4;
+            if (r4 + 3 < r0 || r4 >= r0 + rows) continue;
+            uint32_t w[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) w[b] = *reinterpret_cast<const uint32_t *>(src + 2 * kCacheBlock * DH + cache_tile_byte(d + b, r4, kCacheBlock)) ^ 0x80808080u;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float f[4] = {code_float(w[0], r) * sc.z, code_float(w[1], r) * sc.z, code_float(w[2], r) * sc.z, code_float(w[3], r) * sc.z};
+                if (r4 + r >= r0 && r4 + r < r0 + rows) put(2, head, r4 + r - r0, d, f);
             }
         }
+        __syncthreads();
+    }
 }
 
 // ---- pages ------------------------------------------------------------------------------------------------------------------------
@@ -293,10 +400,13 @@ constexpr int kReserveThreads = 1024, kReserveStep = 16;  // reference counts a 
 
 __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheView c, const int32_t *__restrict__ slots, const int32_t *__restrict__ tokens, int n, int32_t *granted,
                                                                         unsigned int *status) {
-    __shared__ int slot_of[kCacheMaxSeqs], upto[kCacheMaxSeqs], held_of[kCacheMaxSeqs], sums[32];
+    __shared__ __align__(16) int slot_of[kCacheMaxSeqs];
+    __shared__ int upto[kCacheMaxSeqs], held_of[kCacheMaxSeqs], sums[32];
     __shared__ long long wide[32];
     __shared__ int dealt_smem;
     const int tid = threadIdx.x;
+    pdl_launch_dependents();
+    pdl_wait();
     const int slot = tid < n ? slots[tid] : -1;
     slot_of[tid] = slot;
     if (tid == 0) dealt_smem = 0;
@@ -306,11 +416,14 @@ __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheVie
         atomicOr(status, kStatusCache);
         able = false;
     }
-    for (int j = 0; j < tid && able; ++j) able = slot_of[j] != slot;
-    int need = 0, held = 0;
+    int need = 0, held = able ? c.held[slot] : 0;
+    const int want = able ? tokens[tid] : 0;
+    for (int j = 0; j + 4 <= tid; j += 4) {
+        const int4 v = *reinterpret_cast<const int4 *>(slot_of + j);
+        able = able && v.x != slot && v.y != slot && v.z != slot && v.w != slot;
+    }
+    for (int j = tid & ~3; j < tid; ++j) able = able && slot_of[j] != slot;
     if (able) {
-        held = c.held[slot];
-        const int want = tokens[tid];
         if (held < 0 || held > c.max_pages || want < 0) {
             atomicOr(status, kStatusCache);
             able = false;
@@ -343,19 +456,40 @@ __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheVie
     }
     __syncthreads();
     constexpr int STEP = kReserveThreads * kReserveStep;
-    int found = 0;
-    if (total > 0)
-        for (long long p0 = 0; p0 < c.n_pages && found < total; p0 += STEP) {
-            int mine = 0;
+    auto free_pages = [&](long long p0) {  // of this thread's sixteen from p0 on: a bit each
+        uint32_t mask = 0;
+        const long long at = p0 + tid * kReserveStep;
+        if (at + kReserveStep <= c.n_pages) {
+            int4 v[kReserveStep / 4];
 #pragma unroll
-            for (int u = 0; u < kReserveStep; ++u) {
-                const long long p = p0 + tid * kReserveStep + u;
-                mine += p < c.n_pages && c.refs[p] == 0;
-            }
+            for (int u = 0; u < kReserveStep / 4; ++u) v[u] = *reinterpret_cast<const int4 *>(c.refs + at + 4 * u);
+#pragma unroll
+            for (int u = 0; u < kReserveStep / 4; ++u)
+                mask |= ((v[u].x == 0 ? 1u : 0u) | (v[u].y == 0 ? 2u : 0u) | (v[u].z == 0 ? 4u : 0u) | (v[u].w == 0 ? 8u : 0u)) << (4 * u);
+        } else {
+            int v[kReserveStep];
+#pragma unroll
+            for (int u = 0; u < kReserveStep; ++u) v[u] = at + u < c.n_pages ? c.refs[at + u] : 1;
+#pragma unroll
+            for (int u = 0; u < kReserveStep; ++u) mask |= (v[u] == 0 ? 1u : 0u) << u;
+        }
+        return mask;
+    };
+    constexpr int KEPT = 4;  // steps whose pages the second walk has at hand
+    uint32_t kept[KEPT] = {};
+    int found = 0;
+    if (total > 0) {
+        int step = 0;
+        for (long long p0 = 0; p0 < c.n_pages && found < total; p0 += STEP, ++step) {
+            const uint32_t mask = free_pages(p0);
+#pragma unroll
+            for (int u = 0; u < KEPT; ++u)
+                if (u == step) kept[u] = mask;
             int sum;
-            block_exclusive_sum(mine, sums, &sum);
+            block_exclusive_sum(__popc(mask), sums, &sum);
             found += sum;
         }
+    }
     const bool met = able && (need == 0 || upto[tid] <= found);
     if (granted && tid < n) granted[tid] = met;
     // pages dealt: as far as the requests that are met reach
@@ -363,13 +497,13 @@ __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheVie
     __syncthreads();
     const int dealt = dealt_smem;
     int base = 0;
-    for (long long p0 = 0; p0 < c.n_pages && base < dealt; p0 += STEP) {
-        uint32_t free_mask = 0;
+    int step = 0;
+    for (long long p0 = 0; p0 < c.n_pages && base < dealt; p0 += STEP, ++step) {
+        uint32_t free_mask = kept[0];
 #pragma unroll
-        for (int u = 0; u < kReserveStep; ++u) {
-            const long long p = p0 + tid * kReserveStep + u;
-            if (p < c.n_pages && c.refs[p] == 0) free_mask |= 1u << u;
-        }
+        for (int u = 1; u < KEPT; ++u)
+            if (u == step) free_mask = kept[u];
+        if (step >= KEPT) free_mask = free_pages(p0);
         int sum, rank = base + block_exclusive_sum(__popc(free_mask), sums, &sum);
         base += sum;
         for (; free_mask && rank < dealt; free_mask &= free_mask - 1, ++rank) {
@@ -388,6 +522,8 @@ __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheVie
 }
 
 __global__ void __launch_bounds__(256) cache_free_kernel(CacheView c, const int32_t *__restrict__ slots, unsigned int *status) {
+    pdl_launch_dependents();
+    pdl_wait();
     const int i = blockIdx.x, slot = slots[i];
     const bool first = cache_first_of(slots, i, slot);
     if (slot == -1 || !first) return;
@@ -414,61 +550,87 @@ __global__ void __launch_bounds__(256) cache_free_kernel(CacheView c, const int3
     if (off) atomicOr(status, kStatusCache);
 }
 
-// A block of threads copies the open rows of one K/V head; the first of a pair also shares the pages, and the last to have read the state changes it.
+// A block of threads copies the open rows of every gridDim.y-th K/V head; the first of a pair also shares the pages, and the last to have read the state
+// changes it.  Bound by the copy: the rows are asked for before it is known whether the copy is made.
 template <int DH>
 __global__ void __launch_bounds__(256) cache_fork_kernel(CacheView c, const int32_t *__restrict__ srcs, const int32_t *__restrict__ dsts, int n, int32_t *done, unsigned int *status) {
-    const int i = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, H = c.H, src = srcs[i], dst = dsts[i];
+    const int i = blockIdx.x, head0 = blockIdx.y, tid = threadIdx.x, H = c.H;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int src = srcs[i], dst = dsts[i];
+    const bool skip = src == -1 || dst == -1, off = !skip && (src < 0 || src >= c.n_slots || dst < 0 || dst >= c.n_slots), look = !skip && !off;
+    const int held = look ? c.held[src] : 0, length = look ? c.length[src] : 0;
+    bool empty = look && c.held[dst] == 0 && c.length[dst] == 0;
+    const bool sane = look && cache_slot_ok(c, held, length);
     bool clash = false;
     for (int j = tid; j < n; j += blockDim.x) clash = clash || (j < i && dsts[j] == dst) || dsts[j] == src;
-    clash = __syncthreads_or(clash);
-    const bool skip = src == -1 || dst == -1, off = !skip && (src < 0 || src >= c.n_slots || dst < 0 || dst >= c.n_slots);
-    int held = 0, length = 0;
-    bool empty = false, sane = false;
-    if (!skip && !off && !clash) {
-        held = c.held[src];
-        length = c.length[src];
-        empty = c.held[dst] == 0 && c.length[dst] == 0;
-        sane = cache_slot_ok(c, held, length);
-    }
-    const int full = length >> 6, rows = length & 63;
+    const int full = sane ? length >> 6 : 0, rows = sane ? length & 63 : 0;
     bool bad_page = false;
-    if (empty && sane) {
+    if (look)
         for (int b = tid; b < full; b += blockDim.x) {
             const int page = c.table[(size_t)src * c.max_pages + b];
             bad_page = bad_page || page < 0 || page >= c.n_pages;
         }
-    }
+    // `per` units of sixteen bytes of each of the three of each head: six of these parts at a time, a unit of each in flight per thread
+    const int per = rows * (DH / 8), parts = (H - head0 + gridDim.y - 1) / gridDim.y * 3;
+    constexpr int AT_ONCE = 6, TENSOR = kCacheBlock * DH / 8;
+    const uint4 *from = reinterpret_cast<const uint4 *>(c.open) + ((size_t)(look ? src : 0) * H + head0) * (3 * TENSOR);
+    uint4 *to = reinterpret_cast<uint4 *>(c.open) + ((size_t)(look ? dst : 0) * H + head0) * (3 * TENSOR);
+    uint4 v[AT_ONCE];
+    auto load = [&](int part0, int at) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (part0 + u < parts && at < per) v[u] = from[((size_t)((part0 + u) / 3) * gridDim.y * 3 + (part0 + u) % 3) * TENSOR + at];
+    };
+    load(0, tid);
+    clash = __syncthreads_or(clash);
     bad_page = __syncthreads_or(bad_page);
+    empty = empty && !clash;
     if (!empty || !sane || bad_page) {
-        if (head == 0 && tid == 0) {
+        if (head0 == 0 && tid == 0) {
             if (done) done[i] = 0;
             if (off || (empty && !sane) || bad_page) atomicOr(status, kStatusCache);
         }
         return;
     }
-    const uint4 *from = reinterpret_cast<const uint4 *>(c.open + ((size_t)src * H + head) * (3 * kCacheBlock * DH));
-    uint4 *to = reinterpret_cast<uint4 *>(c.open + ((size_t)dst * H + head) * (3 * kCacheBlock * DH));
-    const int per = rows * (DH / 8);
-#pragma unroll 4
-    for (int at = tid; at < 3 * per; at += blockDim.x) {
-        const int t = at / per, j = t * kCacheBlock * (DH / 8) + at - t * per;
-        to[j] = from[j];
-    }
-    if (head == 0)
+    for (int part0 = 0; part0 < parts; part0 += AT_ONCE)
+        for (int at = tid; at < per; at += 256) {
+            if (part0 || at != tid) load(part0, at);
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (part0 + u < parts) to[((size_t)((part0 + u) / 3) * gridDim.y * 3 + (part0 + u) % 3) * TENSOR + at] = v[u];
+        }
+    if (head0 == 0)
         for (int b = tid; b < full; b += blockDim.x) {
             const int page = c.table[(size_t)src * c.max_pages + b];
             c.table[(size_t)dst * c.max_pages + b] = page;
             atomicAdd(c.refs + page, 1);
         }
     __syncthreads();
-    if (tid == 0 && last_arrival(c.arrivals + dst, H)) {
+    if (tid == 0 && last_arrival(c.arrivals + dst, gridDim.y)) {
         c.held[dst] = full;
         c.length[dst] = length;
         if (done) done[i] = 1;
     }
 }
 
-static hgf_status launched() { return cudaGetLastError() == cudaSuccess ? HGF_OK : HGF_ERR_CUDA; }
+// Launches with the attribute that lets a kernel's blocks start, up to their wait for the kernel before, while that one still runs.
+template <class... A, class... B>
+static hgf_status launch(void (*kernel)(A...), dim3 grid, int threads, size_t smem, void *stream, B... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, A(args)...) != cudaSuccess) return HGF_ERR_CUDA;
+    count_launch();
+    return HGF_OK;
+}
 
 }  // namespace hgf
 
@@ -480,9 +642,7 @@ extern "C" hgf_status hgf_cache_reserve(const hgf_cache *cache, const int32_t *s
     if (const hgf_status st = parse_cache(cache, n, &c)) return st;
     unsigned int *status = device_status_word();
     if (!status) return HGF_ERR_CUDA;
-    cache_reserve_kernel<<<1, kReserveThreads, 0, (cudaStream_t)stream>>>(c, slots, tokens, (int)n, granted, status);
-    count_launch();
-    return launched();
+    return launch(cache_reserve_kernel, dim3(1), kReserveThreads, 0, stream, c, slots, tokens, (int)n, granted, status);
 }
 
 extern "C" hgf_status hgf_cache_append(const hgf_cache *cache, const void *k, const void *v, int64_t n_rows, const int32_t *slots, const int32_t *starts,
@@ -494,11 +654,9 @@ extern "C" hgf_status hgf_cache_append(const hgf_cache *cache, const void *k, co
     if (((uintptr_t)k | (uintptr_t)v) & 15u) return HGF_ERR_MISALIGNED;
     unsigned int *status = device_status_word();
     if (!status) return HGF_ERR_CUDA;
-    const dim3 grid((unsigned)(n_rows / kCacheBlock + n_seqs), (unsigned)c.H);
-    auto kernel = cache->head_dim == 64 ? cache_append_kernel<64> : cache_append_kernel<128>;
-    kernel<<<grid, kAppendThreads, 0, (cudaStream_t)stream>>>(c, (const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v, (int)n_rows, slots, starts, (int)n_seqs, done, status);
-    count_launch();
-    return launched();
+    const int64_t pieces = n_rows / kCacheBlock + n_seqs;
+    return launch(cache->head_dim == 64 ? cache_append_kernel<64> : cache_append_kernel<128>, dim3((unsigned)pieces, head_shares(pieces, c.H, 600)), kAppendThreads, 0, stream, c,
+                  (const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v, (int)n_rows, slots, starts, (int)n_seqs, done, status);
 }
 
 extern "C" hgf_status hgf_cache_read(const hgf_cache *cache, const int32_t *slots, const int32_t *first, const int32_t *starts, int64_t n_seqs, int64_t n_rows,
@@ -510,12 +668,13 @@ extern "C" hgf_status hgf_cache_read(const hgf_cache *cache, const int32_t *slot
     if (((uintptr_t)k_out | (uintptr_t)v_out) & 15u) return HGF_ERR_MISALIGNED;
     unsigned int *status = device_status_word();
     if (!status) return HGF_ERR_CUDA;
-    const dim3 grid((unsigned)(n_rows / kCacheBlock + 2 * n_seqs), (unsigned)c.H);
-    const bool bf16 = (flags & HGF_FLAG_OUT_BF16) != 0;
-    auto kernel = cache->head_dim == 64 ? (bf16 ? cache_read_kernel<64, true> : cache_read_kernel<64, false>) : (bf16 ? cache_read_kernel<128, true> : cache_read_kernel<128, false>);
-    kernel<<<grid, kReadThreads, 0, (cudaStream_t)stream>>>(c, slots, first, starts, (int)n_seqs, (int)n_rows, k_out, v_out, status);
-    count_launch();
-    return launched();
+    const int64_t pieces = n_rows / kCacheBlock + 2 * n_seqs;
+    const bool bf16 = (flags & HGF_FLAG_OUT_BF16) != 0, narrow = cache->head_dim == 64;
+    auto kernel = narrow ? (bf16 ? cache_read_kernel<64, true> : cache_read_kernel<64, false>) : (bf16 ? cache_read_kernel<128, true> : cache_read_kernel<128, false>);
+    static std::atomic<unsigned long long> done_wide{0}, done_wide_bf16{0};
+    if (!narrow && ensure_dynamic_smem(kernel, kReadSmem<128>, bf16 ? done_wide_bf16 : done_wide) != cudaSuccess) return HGF_ERR_CUDA;
+    return launch(kernel, dim3((unsigned)pieces, head_shares(pieces, c.H, 1600)), kReadThreads, narrow ? kReadSmem<64> : kReadSmem<128>, stream, c, slots, first, starts, (int)n_seqs,
+                  (int)n_rows, k_out, v_out, status);
 }
 
 extern "C" hgf_status hgf_cache_fork(const hgf_cache *cache, const int32_t *src, const int32_t *dst, int64_t n, int32_t *done, void *stream) {
@@ -524,10 +683,7 @@ extern "C" hgf_status hgf_cache_fork(const hgf_cache *cache, const int32_t *src,
     if (const hgf_status st = parse_cache(cache, n, &c)) return st;
     unsigned int *status = device_status_word();
     if (!status) return HGF_ERR_CUDA;
-    auto kernel = cache->head_dim == 64 ? cache_fork_kernel<64> : cache_fork_kernel<128>;
-    kernel<<<dim3((unsigned)n, (unsigned)c.H), 256, 0, (cudaStream_t)stream>>>(c, src, dst, (int)n, done, status);
-    count_launch();
-    return launched();
+    return launch(cache->head_dim == 64 ? cache_fork_kernel<64> : cache_fork_kernel<128>, dim3((unsigned)n, head_shares(n, c.H, 600)), 256, 0, stream, c, src, dst, (int)n, done, status);
 }
 
 extern "C" hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slots, int64_t n, void *stream) {
@@ -536,7 +692,5 @@ extern "C" hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slot
     if (const hgf_status st = parse_cache(cache, n, &c)) return st;
     unsigned int *status = device_status_word();
     if (!status) return HGF_ERR_CUDA;
-    cache_free_kernel<<<(unsigned)n, 256, 0, (cudaStream_t)stream>>>(c, slots, status);
-    count_launch();
-    return launched();
+    return launch(cache_free_kernel, dim3((unsigned)n), 256, 0, stream, c, slots, status);
 }

@@ -39,24 +39,6 @@ __device__ __forceinline__ bool cache_slot_ok(const CacheView &c, int held, int 
     return held >= 0 && held <= c.max_pages && length >= 0 && (length >> 6) <= held;
 }
 
-// The sequence that piece x of a launch belongs to, where sequence i has its pieces from starts[i] / 64 + i * per on (`per` pieces and one for each
-// 64 rows are room for all that it can have): i, or -1 if the starts are no ascending row numbers up to n_rows.  All threads of a block call it.
-__device__ __forceinline__ int cache_find_sequence(const int32_t *__restrict__ starts, int n, int n_rows, int per, int x) {
-    int below = 0;
-    bool bad = false;
-    for (int j0 = 0; j0 < n; j0 += blockDim.x) {
-        const int j = j0 + threadIdx.x;
-        bool mine = false;
-        if (j < n) {
-            const int a = starts[j], b = starts[j + 1];
-            bad = bad || a < 0 || b < a || b > n_rows;
-            mine = (a >> 6) + j * per <= x;
-        }
-        below += __syncthreads_count(mine);
-    }
-    return __syncthreads_or(bad) ? -1 : below - 1;
-}
-
 // Whether entry i of a list of slots is the first that names its slot.
 __device__ __forceinline__ bool cache_first_of(const int32_t *__restrict__ slots, int i, int slot) {
     bool again = false;

@@ -225,6 +225,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     if (tid == 0) gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     __syncthreads();
+    pdl_wait();
     pdl_launch_dependents();
     const int tile_rows = ROWS * (ROWS == 1 ? 1 : p.tiles);
 
@@ -956,18 +957,21 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;
     const int grid = sms < kCaMaxSms ? sms : kCaMaxSms;
-    cached_attention_kernel<DH, ROWS, DP><<<grid, threads, C::SMEM, stream>>>(p);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid, (unsigned)(ROWS == 1 ? 1 : p.tiles * ROWS / 8));
-    cfg.blockDim = dim3(8 * DH / 4);
-    cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    cfg.stream = stream;
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = C::SMEM;
+    e = cudaLaunchKernelEx(&cfg, cached_attention_kernel<DH, ROWS, DP>, p);
+    if (e != cudaSuccess) return e;
+    cfg.dynamicSmemBytes = 0;
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)(ROWS == 1 ? 1 : p.tiles * ROWS / 8));
+    cfg.blockDim = dim3(8 * DH / 4);
     e = cudaLaunchKernelEx(&cfg, cached_attention_join_kernel<DH, ROWS>, p);
     if (e != cudaSuccess) return e;
     count_launch(2);
