@@ -139,22 +139,33 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
         const __nv_bfloat16 *src = n < 2 ? k + (size_t)row * kw + ((size_t)n * H + head) * DH : v + (size_t)row * vw + (size_t)head * DH;
         return *reinterpret_cast<const uint4 *>(src + 8 * eight);
     };
-    // A warp's lanes take eight eights of four rows.
-    auto row_of = [&](int u) { return (warp + u * WARPS) / (EIGHTS / 8) * 4 + (lane >> 3); };
-    auto eight_of = [&](int u) { return (warp + u * WARPS) % (EIGHTS / 8) * 8 + (lane & 7); };
+    // A warp's lanes take eight eights of four rows; a thread's u-th unit lies ROWS_ON rows further down, at the same dims.
+    constexpr int ROWS_ON = DH == 64 ? 32 : 16;
+    const int r_first = DH == 64 ? 4 * warp + (lane >> 3) : 4 * (warp >> 1) + (lane >> 3), eight = DH == 64 ? lane & 7 : (warp & 1) * 8 + (lane & 7);
     const int t0 = (block0 + piece) * kCacheBlock;  // first token of the block
     uint4 x[3][PER];
     auto load = [&](int head) {
         const __nv_bfloat16 *open = open_rows(head);
+        const __nv_bfloat16 *kp = k + (ptrdiff_t)(row0 + t0 + r_first - length) * (ptrdiff_t)kw + (size_t)head * DH + 8 * eight;  // (looked at from the first new row on)
+        const __nv_bfloat16 *vp = v + (ptrdiff_t)(row0 + t0 + r_first - length) * (ptrdiff_t)vw + (size_t)head * DH + 8 * eight;
 #pragma unroll
-        for (int n = 0; n < 3; ++n)
+        for (int u = 0; u < PER; ++u) {
+            const int r = r_first + u * ROWS_ON;
+            if (t0 + r < length) {
 #pragma unroll
-            for (int u = 0; u < PER; ++u) {
-                const int r = row_of(u), e = eight_of(u);
-                x[n][u] = t0 + r < length ? *reinterpret_cast<const uint4 *>(open + ((size_t)n * kCacheBlock + r) * DH + 8 * cache_open_eight(r, e))
-                                          : new_eight(n, head, row0 + t0 + r - length, e);
+                for (int n = 0; n < 3; ++n) x[n][u] = *reinterpret_cast<const uint4 *>(open + ((size_t)n * kCacheBlock + r) * DH + 8 * cache_open_eight(r, eight));
+            } else {
+                x[0][u] = *reinterpret_cast<const uint4 *>(kp + (size_t)u * ROWS_ON * kw);
+                x[1][u] = *reinterpret_cast<const uint4 *>(kp + (size_t)u * ROWS_ON * kw + vw);
+                x[2][u] = *reinterpret_cast<const uint4 *>(vp + (size_t)u * ROWS_ON * vw);
             }
+        }
     };
+    // Where its bytes go in the page: of K the words of dims 0-3 and, sixteen bytes on, 4-7; of V, after four lanes' rows have become four bytes of a dim
+    // each, the words of one of dims 0-3 and, 256 bytes on, one of dims 4-7.
+    const int k_byte = cache_tile_byte(r_first, 8 * eight, DH), v_byte = cache_tile_byte(8 * eight + (lane >> 3), r_first & ~3, kCacheBlock);
+    constexpr int K_ON = 2048;
+    auto v_on = [](int u) { return DH == 64 ? 512 * u : 512 * (u >> 1) + 8 * (u & 1); };
     if (piece < blocks) load(head0);  // (on their way during the look-ups below)
     bool shared = false, off = false;
     for (int b = tid; b < blocks; b += kAppendThreads) {
@@ -203,19 +214,17 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
                 const bool zero = top[n] == 0 || top[n] >= 0x7f80u;
                 QuantScale s = make_quant_scale(gamma);
                 if (gamma < 7.9e-31f) s.fast = false;
-                uint8_t *dst = page_smem + n * kCacheBlock * DH;
+                uint8_t *dst = page_smem + n * kCacheBlock * DH + (n < 2 ? k_byte : v_byte);
 #pragma unroll
                 for (int u = 0; u < PER; ++u) {
-                    const int r = row_of(u), e = eight_of(u);
                     int sum = 0;
-                    const uint2 q = zero ? make_uint2(0, 0) : quant8(x[n][u], s, sum);
+                    const uint2 q = zero ? make_uint2(0, 0) : quant8<true>(x[n][u], s, sum);
                     if (n < 2) {
-                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(r, 8 * e, DH)) = q.x;
-                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(r, 8 * e + 4, DH)) = q.y;
-                    } else {  // four lanes' rows become four bytes of a dim each
-                        const int d = 8 * e + (lane >> 3), r4 = r & ~3;
-                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(d, r4, kCacheBlock)) = transpose_bytes(q.x, lane);
-                        *reinterpret_cast<uint32_t *>(dst + cache_tile_byte(d + 4, r4, kCacheBlock)) = transpose_bytes(q.y, lane);
+                        *reinterpret_cast<uint32_t *>(dst + u * K_ON) = q.x;
+                        *reinterpret_cast<uint32_t *>(dst + u * K_ON + 16) = q.y;
+                    } else {
+                        *reinterpret_cast<uint32_t *>(dst + v_on(u)) = transpose_bytes(q.x, lane);
+                        *reinterpret_cast<uint32_t *>(dst + v_on(u) + 256) = transpose_bytes(q.y, lane);
                     }
                 }
             }
@@ -233,11 +242,20 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
     if (piece == 0) {
         // rows that stay open: those of the last block, or all new ones if none became complete
         const int from = blocks ? 0 : open0, rows = blocks ? (int)(after & 63) : m, src0 = row0 + m - rows;
-        const int heads = (H - head0 + gridDim.y - 1) / gridDim.y, all = heads * 3 * rows * EIGHTS;
-        for (int at = tid; at < all; at += kAppendThreads) {
-            const int e = at % EIGHTS, n = at / EIGHTS % 3, head = head0 + at / (3 * EIGHTS) % heads * gridDim.y, r = at / (3 * EIGHTS * heads);
-            *reinterpret_cast<uint4 *>(open_rows(head) + ((size_t)n * kCacheBlock + from + r) * DH + 8 * cache_open_eight(from + r, e)) = new_eight(n, head, src0 + r, e);
-        }
+        constexpr int ROWS_AT_ONCE = kAppendThreads / EIGHTS;
+        const int e = tid % EIGHTS, r_mine = tid / EIGHTS;
+        for (int head = head0; head < H; head += gridDim.y)
+#pragma unroll
+            for (int q = 0; q < kCacheBlock / ROWS_AT_ONCE; ++q) {
+                const int r = r_mine + q * ROWS_AT_ONCE;
+                if (r < rows) {
+                    uint4 y[3];
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) y[n] = new_eight(n, head, src0 + r, e);
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) *reinterpret_cast<uint4 *>(open_rows(head) + ((size_t)n * kCacheBlock + from + r) * DH + 8 * cache_open_eight(from + r, e)) = y[n];
+                }
+            }
     }
     __syncthreads();
     if (tid == 0 && last_arrival(c.arrivals + slot, pieces * gridDim.y)) {
@@ -286,11 +304,8 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
     if (from >= to) return;
     const int rows = to - from, r0 = (int)(from - b0);
     const size_t kw = (size_t)2 * H * DH, vw = (size_t)H * DH, out0 = (size_t)row0 + (from - first);
-    // values at a row of the range, from dim `dim` of a head of tensor n on
-    auto put = [&](int n, int head, int row, int dim, const auto &f) {
+    auto put = [](void *base, size_t at, const auto &f) {
         constexpr int N = sizeof(f) / sizeof(float);
-        const size_t o = n < 2 ? (out0 + row) * kw + ((size_t)n * H + head) * DH + dim : (out0 + row) * vw + (size_t)head * DH + dim;
-        void *base = n < 2 ? k_out : v_out;
         if (BF16) {
             uint32_t w[N / 2];
 #pragma unroll
@@ -298,22 +313,39 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
                 const __nv_bfloat162 x = __floats2bfloat162_rn(f[2 * b], f[2 * b + 1]);
                 w[b] = *reinterpret_cast<const uint32_t *>(&x);
             }
-            if constexpr (N == 8) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(base) + o) = make_uint4(w[0], w[1], w[2], w[3]);
-            else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(base) + o) = make_uint2(w[0], w[1]);
+            if constexpr (N == 8) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(base) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(base) + at) = make_uint2(w[0], w[1]);
         } else {
 #pragma unroll
-            for (int b = 0; b < N; b += 4) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(base) + o + b) = make_float4(f[b], f[b + 1], f[b + 2], f[b + 3]);
+            for (int b = 0; b < N; b += 4) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(base) + at + b) = make_float4(f[b], f[b + 1], f[b + 2], f[b + 3]);
         }
     };
+    // A thread has the same eight dims of every ROWS_ON-th row: of K1 or K2 in a page, of each of the three of open rows.
+    constexpr int ROWS_ON = kReadThreads / (2 * EIGHTS), OPEN_ON = kReadThreads / EIGHTS;
     if (b0 + kCacheBlock > length) {
-        const int heads = (H - head0 + gridDim.y - 1) / gridDim.y, all = heads * 3 * rows * EIGHTS;
-#pragma unroll 4
-        for (int at = tid; at < all; at += kReadThreads) {
-            const int e = at % EIGHTS, n = at / EIGHTS % 3, head = head0 + at / (3 * EIGHTS) % heads * gridDim.y, row = at / (3 * EIGHTS * heads), r = r0 + row;
-            float f[8];
-            unpack8(*reinterpret_cast<const uint4 *>(c.open + (((size_t)slot * H + head) * 3 + n) * (kCacheBlock * DH) + (size_t)r * DH + 8 * cache_open_eight(r, e)), f);
-            put(n, head, row, 8 * e, f);
-        }
+        const int e = tid % EIGHTS;
+        for (int head = head0; head < H; head += gridDim.y)
+#pragma unroll
+            for (int q = 0; q < kCacheBlock / OPEN_ON; ++q) {
+                const int r = tid / EIGHTS + q * OPEN_ON;
+                if (r < r0 || r >= r0 + rows) continue;
+                const __nv_bfloat16 *src = c.open + ((size_t)slot * H + head) * (3 * kCacheBlock * DH) + (size_t)r * DH + 8 * cache_open_eight(r, e);
+                uint4 y[3];
+#pragma unroll
+                for (int n = 0; n < 3; ++n) y[n] = *reinterpret_cast<const uint4 *>(src + n * kCacheBlock * DH);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) {
+                    const size_t row = out0 + r - r0;
+                    const size_t at = n < 2 ? row * kw + ((size_t)n * H + head) * DH + 8 * e : row * vw + (size_t)head * DH + 8 * e;
+                    if (BF16) {
+                        *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(n < 2 ? k_out : v_out) + at) = y[n];
+                    } else {
+                        float f[8];
+                        unpack8(y[n], f);
+                        put(n < 2 ? k_out : v_out, at, f);
+                    }
+                }
+            }
         return;
     }
     const int page = c.table[(size_t)slot * c.max_pages + (int)(b0 >> 6)];
@@ -331,6 +363,8 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
         asm volatile("cp.async.commit_group;\n" ::: "memory");
     };
     fetch(head0, 0);
+    const int e = tid % EIGHTS, n = tid / EIGHTS & 1, r_first = tid / (2 * EIGHTS), d4 = tid % (DH / 4) * 4, r4 = tid / (DH / 4) * 4;
+    const int k_byte = n * kCacheBlock * DH + cache_tile_byte(r_first, 8 * e, DH), v_byte = 2 * kCacheBlock * DH + cache_tile_byte(d4, r4, kCacheBlock);
     int buf = 0;
     for (int head = head0; head < H; head += gridDim.y, buf ^= 1) {
         const float4 sc = c.scales[(size_t)page * H + head];
@@ -338,31 +372,32 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
         asm volatile("cp.async.wait_group 1;\n" ::: "memory");
         __syncthreads();
         const uint8_t *src = pages_smem + buf * PAGE;
-#pragma unroll 2
-        for (int at = tid; at < 2 * rows * EIGHTS; at += kReadThreads) {
-            const int e = at % EIGHTS, n = at / EIGHTS & 1, row = at / (2 * EIGHTS), r = r0 + row;
-            const float s = n ? sc.y : sc.x;
+        const float s = n ? sc.y : sc.x;
+        const size_t k_at = ((ptrdiff_t)out0 - r0 + r_first) * (ptrdiff_t)kw + ((size_t)n * H + head) * DH + 8 * e;
+#pragma unroll
+        for (int q = 0; q < kCacheBlock / ROWS_ON; ++q) {
+            const int r = r_first + q * ROWS_ON;
+            if (r < r0 || r >= r0 + rows) continue;
+            // (sixteen rows on is a tile row on; eight, the other half of a lane's bytes)
+            const uint8_t *at = src + k_byte + (DH == 64 ? q * (DH / 32) * 512 : (q >> 1) * (DH / 32) * 512 + 4 * (q & 1));
+            const uint32_t w[2] = {*reinterpret_cast<const uint32_t *>(at) ^ 0x80808080u, *reinterpret_cast<const uint32_t *>(at + 16) ^ 0x80808080u};
             float f[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(src + n * kCacheBlock * DH + cache_tile_byte(r, 8 * e + 4 * h, DH)) ^ 0x80808080u;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) f[4 * h + b] = code_float(w, b) * s;
-            }
-            put(n, head, row, 8 * e, f);
+            for (int b = 0; b < 8; ++b) f[b] = code_float(w[b >> 2], b & 3) * s;
+            put(k_out, k_at + (size_t)q * ROWS_ON * kw, f);
         }
-        // four rows of four dims of V at a time: a word is four tokens of a dim
+        // four rows of four dims of V at a time: a word is four tokens of a dim, and the next dim's is 64 bytes on
 #pragma unroll
-        for (int u = 0; u < kCacheBlock / 4 * (DH / 4) / kReadThreads; ++u) {
-            const int at = tid + u * kReadThreads, d = at % (DH / 4) * 4, r4 = at / (DH / 4) * 4;
-            if (r4 + 3 < r0 || r4 >= r0 + rows) continue;
+        for (int u = 0; u < DH / 64; ++u) {
+            const int row = r4 + 32 * u;
+            if (row + 3 < r0 || row >= r0 + rows) continue;
             uint32_t w[4];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) w[b] = *reinterpret_cast<const uint32_t *>(src + 2 * kCacheBlock * DH + cache_tile_byte(d + b, r4, kCacheBlock)) ^ 0x80808080u;
+            for (int b = 0; b < 4; ++b) w[b] = *reinterpret_cast<const uint32_t *>(src + v_byte + u * 512 + b * 64) ^ 0x80808080u;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float f[4] = {code_float(w[0], r) * sc.z, code_float(w[1], r) * sc.z, code_float(w[2], r) * sc.z, code_float(w[3], r) * sc.z};
-                if (r4 + r >= r0 && r4 + r < r0 + rows) put(2, head, r4 + r - r0, d, f);
+                if (row + r >= r0 && row + r < r0 + rows) put(v_out, (out0 + row + r - r0) * vw + (size_t)head * DH + d4, f);
             }
         }
         __syncthreads();
