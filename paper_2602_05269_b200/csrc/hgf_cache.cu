@@ -320,8 +320,8 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
             for (int b = 0; b < N; b += 4) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(base) + at + b) = make_float4(f[b], f[b + 1], f[b + 2], f[b + 3]);
         }
     };
-    // A thread has the same eight dims of every ROWS_ON-th row: of K1 or K2 in a page, of each of the three of open rows.
-    constexpr int ROWS_ON = kReadThreads / (2 * EIGHTS), OPEN_ON = kReadThreads / EIGHTS;
+    // A thread has the same sixteen bytes of output of every ROWS_ON-th row of K1 or K2 in a page, and the same eight dims of every OPEN_ON-th open row.
+    constexpr int DIMS = BF16 ? 8 : 4, UNITS = DH / DIMS, ROWS_ON = kReadThreads / (2 * UNITS), OPEN_ON = kReadThreads / EIGHTS;
     if (b0 + kCacheBlock > length) {
         const int e = tid % EIGHTS;
         for (int head = head0; head < H; head += gridDim.y)
@@ -363,8 +363,8 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
         asm volatile("cp.async.commit_group;\n" ::: "memory");
     };
     fetch(head0, 0);
-    const int e = tid % EIGHTS, n = tid / EIGHTS & 1, r_first = tid / (2 * EIGHTS), d4 = tid % (DH / 4) * 4, r4 = tid / (DH / 4) * 4;
-    const int k_byte = n * kCacheBlock * DH + cache_tile_byte(r_first, 8 * e, DH), v_byte = 2 * kCacheBlock * DH + cache_tile_byte(d4, r4, kCacheBlock);
+    const int dim = tid % UNITS * DIMS, n = tid / UNITS & 1, r_first = tid / (2 * UNITS), d4 = tid % (DH / 4) * 4, r4 = tid / (DH / 4) * 4;
+    const int k_byte = n * kCacheBlock * DH + cache_tile_byte(r_first, dim, DH), v_byte = 2 * kCacheBlock * DH + cache_tile_byte(d4, r4, kCacheBlock);
     int buf = 0;
     for (int head = head0; head < H; head += gridDim.y, buf ^= 1) {
         const float4 sc = c.scales[(size_t)page * H + head];
@@ -373,17 +373,19 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
         __syncthreads();
         const uint8_t *src = pages_smem + buf * PAGE;
         const float s = n ? sc.y : sc.x;
-        const size_t k_at = ((ptrdiff_t)out0 - r0 + r_first) * (ptrdiff_t)kw + ((size_t)n * H + head) * DH + 8 * e;
+        const size_t k_at = ((ptrdiff_t)out0 - r0 + r_first) * (ptrdiff_t)kw + ((size_t)n * H + head) * DH + dim;
 #pragma unroll
         for (int q = 0; q < kCacheBlock / ROWS_ON; ++q) {
             const int r = r_first + q * ROWS_ON;
             if (r < r0 || r >= r0 + rows) continue;
-            // (sixteen rows on is a tile row on; eight, the other half of a lane's bytes)
-            const uint8_t *at = src + k_byte + (DH == 64 ? q * (DH / 32) * 512 : (q >> 1) * (DH / 32) * 512 + 4 * (q & 1));
-            const uint32_t w[2] = {*reinterpret_cast<const uint32_t *>(at) ^ 0x80808080u, *reinterpret_cast<const uint32_t *>(at + 16) ^ 0x80808080u};
-            float f[8];
+            const uint8_t *at = src + k_byte + cache_tile_byte(q * ROWS_ON, 0, DH);  // (r_first and the step have no bit in common)
+            float f[DIMS];
 #pragma unroll
-            for (int b = 0; b < 8; ++b) f[b] = code_float(w[b >> 2], b & 3) * s;
+            for (int h = 0; h < DIMS / 4; ++h) {
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(at + 16 * h) ^ 0x80808080u;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) f[4 * h + b] = code_float(w, b) * s;
+            }
             put(k_out, k_at + (size_t)q * ROWS_ON * kw, f);
         }
         // four rows of four dims of V at a time: a word is four tokens of a dim, and the next dim's is 64 bytes on
