@@ -455,11 +455,12 @@ __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheVie
     }
     int need = 0, held = able ? c.held[slot] : 0;
     const int want = able ? tokens[tid] : 0;
-    for (int j = 0; j + 4 <= tid; j += 4) {
+#pragma unroll 4
+    for (int j = 0; able && j + 4 <= tid; j += 4) {
         const int4 v = *reinterpret_cast<const int4 *>(slot_of + j);
         able = able && v.x != slot && v.y != slot && v.z != slot && v.w != slot;
     }
-    for (int j = tid & ~3; j < tid; ++j) able = able && slot_of[j] != slot;
+    for (int j = tid & ~3; able && j < tid; ++j) able = slot_of[j] != slot;
     if (able) {
         if (held < 0 || held > c.max_pages || want < 0) {
             atomicOr(status, kStatusCache);
@@ -482,11 +483,13 @@ __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheVie
         }
         if (lane == 31) wide[warp] = s;
         __syncthreads();
-        long long before = 0, all = 0;
-        for (int w = 0; w < 32; ++w) {
-            if (w < warp) before += wide[w];
-            all += wide[w];
+        long long w = wide[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long t = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += t;
         }
+        const long long all = __shfl_sync(0xffffffffu, w, 31), upto_here = __shfl_sync(0xffffffffu, w, (warp + 31) & 31), before = warp ? upto_here : 0;
         upto[tid] = (int)min(s + before, 0x7fffffffll);
         held_of[tid] = held;
         total = (int)min(all, 0x7fffffffll);
@@ -543,16 +546,23 @@ __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheVie
         if (step >= KEPT) free_mask = free_pages(p0);
         int sum, rank = base + block_exclusive_sum(__popc(free_mask), sums, &sum);
         base += sum;
-        for (; free_mask && rank < dealt; free_mask &= free_mask - 1, ++rank) {
-            const int p = (int)(p0 + tid * kReserveStep + __ffs(free_mask) - 1);
+        if (free_mask && rank < dealt) {
             int lo = 0, hi = n - 1;  // the first request whose running sum is above the rank
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
                 if (upto[mid] > rank) hi = mid; else lo = mid + 1;
             }
-            const int before = lo ? upto[lo - 1] : 0;
-            c.table[(size_t)slot_of[lo] * c.max_pages + held_of[lo] + rank - before] = p;
-            c.refs[p] = 1;
+            int32_t *entry = nullptr;  // where the rank's page goes
+            for (int end = 0; free_mask && rank < dealt; free_mask &= free_mask - 1, ++rank, ++entry) {
+                if (rank >= end) {
+                    while (upto[lo] <= rank) ++lo;
+                    end = upto[lo];
+                    entry = c.table + (size_t)slot_of[lo] * c.max_pages + held_of[lo] + rank - (lo ? upto[lo - 1] : 0);
+                }
+                const int p = (int)(p0 + tid * kReserveStep + __ffs(free_mask) - 1);
+                *entry = p;
+                c.refs[p] = 1;
+            }
         }
     }
     if (met && need) c.held[slot] = held + need;
