@@ -192,13 +192,25 @@ template <int DH, int ROWS, class F>
 __device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int n, F at, float *to, int thread, int threads) {
     constexpr int PART = 4 + 2 * DH, FOURS = DH / 4;
     const int all = ROWS * p.tiles, end = min(all, it.m * p.group - it.tile * all);
-    for (int e = thread; e < end * FOURS; e += threads) {
-        const int r = e / FOURS, dim = e % FOURS * 4;
-        CaSum sum;
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) sum.add_part(at(j) + r * PART, DH, dim);
-        if (to) sum.store_part(to + r * PART, DH, dim, dim == 0);
-        else sum.write(p, it, it.tile * all + r, DH, dim);
+    constexpr int AT_ONCE = ROWS == 1 ? 1 : 4;  // places of a thread whose loads are in flight together
+    for (int e0 = thread; e0 < end * FOURS; e0 += AT_ONCE * threads) {
+        CaSum sum[AT_ONCE];
+#pragma unroll 2
+        for (int j = 0; j < n; ++j) {
+            const float *part = at(j);
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int e = min(e0 + u * threads, end * FOURS - 1);
+                sum[u].add_part(part + e / FOURS * PART, DH, e % FOURS * 4);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int e = e0 + u * threads, r = e / FOURS, dim = e % FOURS * 4;
+            if (e >= end * FOURS) break;
+            if (to) sum[u].store_part(to + r * PART, DH, dim, dim == 0);
+            else sum[u].write(p, it, it.tile * all + r, DH, dim);
+        }
     }
 }
 
@@ -498,15 +510,14 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // (f is zero for a page of zeros: then nothing is -inf but what is masked)
-        const float here = top == -INFINITY ? -INFINITY : top * f, now = fmaxf(m[r], here), base = now == -INFINITY ? 0.0f : now;
+        f += 1.17549435e-38f;  // (a page of zeros has f = 0, and what is masked has to stay at -inf)
+        const float here = top * f, now = fmaxf(m[r], here), base = now == -INFINITY ? 0.0f : now;
         const float minus = here == -INFINITY ? 0.0f : -here;
         alpha = exp2_approx(m[r] - base);
         worth = exp2_approx(here - base);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const float y = fmaf(x[j], f, minus);
-            x[j] = partly && token(j) >= count ? 0.0f : exp2_approx(y);
+            x[j] = exp2_approx(fmaf(x[j], f, minus));
             sums[j & 3] += x[j];
         }
         m[r] = now;
