@@ -44,14 +44,14 @@ __device__ static bool last_arrival(int32_t *arrivals, int blocks) {
 // starts[i] / 64 + i * per on (`per` pieces and one for each 64 rows are room for all that it can have).  All threads call it; `slots` (shared memory)
 // holds the list of slots afterwards.
 struct CachePiece {
-    int i;        // -1: the starts are no ascending row numbers up to n_rows
+    int i;        // -1: the starts are no ascending row numbers up to n_rows; -2: nobody's (before the first sequence's rows)
     int row0, m;  // the sequence's rows
-    int piece;
+    int piece, pieces;  // this one, and how many the sequence has in the launch, needed or not
     int slot;
     bool first;   // no earlier entry of the list names the slot
 };
 __device__ __forceinline__ CachePiece find_piece(const int32_t *__restrict__ list, const int32_t *__restrict__ starts, int n, int n_rows, int per, int x, int *slots) {
-    CachePiece p = {-1, 0, 0, 0, -1, false};
+    CachePiece p = {-1, 0, 0, 0, 0, -1, false};
     int below = 0;
     bool bad = false;
     for (int j0 = 0; j0 < n; j0 += blockDim.x) {
@@ -66,10 +66,12 @@ __device__ __forceinline__ CachePiece find_piece(const int32_t *__restrict__ lis
         below += __syncthreads_count(mine);
     }
     if (__syncthreads_or(bad)) return p;
-    p.i = below - 1;
+    p.i = below ? below - 1 : -2;
+    if (p.i < 0) return p;
     p.row0 = starts[p.i];
     p.m = starts[p.i + 1] - p.row0;
     p.piece = x - ((p.row0 >> 6) + p.i * per);
+    p.pieces = (p.i + 1 < n ? ((p.row0 + p.m) >> 6) + (p.i + 1) * per : (int)gridDim.x) - (x - p.piece);
     p.slot = slots[p.i];
     bool again = false;
     for (int j = threadIdx.x; j < p.i; j += blockDim.x) again = again || slots[j] == p.slot;
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
     pdl_wait();
     const CachePiece p = find_piece(slots, starts, n_seqs, n_rows, 1, blockIdx.x, slot_smem);
     if (p.i < 0) {
-        if (tid == 0) {
+        if (tid == 0 && p.i == -1) {
             atomicOr(status, kStatusCache);
             if (done && head0 == 0)
                 for (int j = blockIdx.x; j < n_seqs; j += gridDim.x) done[j] = 0;
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
     const long long after = (long long)length + m;
     const bool sane = cache_slot_ok(c, held, length);
     bool fits = sane && (after >> 6) <= held;
-    const int blocks = fits ? (int)(after >> 6) - block0 : 0, pieces = blocks > 1 ? blocks : 1;
+    const int blocks = fits ? (int)(after >> 6) - block0 : 0;
     const int32_t *table = c.table + (size_t)slot * c.max_pages + (sane ? block0 : 0);
     const size_t kw = (size_t)2 * H * DH, vw = (size_t)H * DH;
     auto open_rows = [&](int head) { return c.open + ((size_t)slot * H + head) * (3 * kCacheBlock * DH); };
@@ -185,7 +187,6 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
         }
         return;
     }
-    if (piece >= pieces) return;
 
     if (piece < blocks) {
         const int page = table[piece];
@@ -257,8 +258,9 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
                 }
             }
     }
+    // (pieces that the sequence turned out not to need arrive as well: they have read its length, too)
     __syncthreads();
-    if (tid == 0 && last_arrival(c.arrivals + slot, pieces * gridDim.y)) {
+    if (tid == 0 && last_arrival(c.arrivals + slot, p.pieces * gridDim.y)) {
         c.length[slot] = (int)after;
         if (done) done[i] = 1;
     }
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(kReadThreads, 4) cache_read_kernel(CacheView c
     pdl_wait();
     const CachePiece p = find_piece(slots, starts, n_seqs, n_rows, 2, blockIdx.x, slot_smem);
     if (p.i < 0) {
-        if (tid == 0) atomicOr(status, kStatusCache);
+        if (tid == 0 && p.i == -1) atomicOr(status, kStatusCache);
         return;
     }
     const int row0 = p.row0, m = p.m, slot = p.slot;

@@ -156,6 +156,46 @@ def test_codes_at_the_edges_of_the_quantiser(hgf):
     p.check()
 
 
+def test_rows_that_begin_later(hgf):
+    """The first sequence's rows need not be the call's first."""
+    p = Pair(hgf, 2, 64)
+    p.reserve([0, 1], [200, 200])
+    k, v = rows(p.rng, 400, 256), rows(p.rng, 400, 128)
+    for starts in ([130, 200, 390], [64, 64, 70], [399, 400, 400]):
+        got = hgf.cache_append(p.cache, bf16(k), bf16(v), ints([0, 1]), ints(starts)).tolist()
+        assert got == p.ref.append([0, 1], starts, k, v) == [1, 1]
+        p.check()
+    kk, vv = torch.full((400, 256), 7.0, device="cuda"), torch.full((400, 128), 7.0, device="cuda")
+    hgf.cache_read(p.cache, ints([1]), ints([0]), ints([300, 400]), k=kk, v=vv)
+    want = torch.from_numpy(p.ref.values(1)).float()[:, :, :100]
+    assert torch.equal(vv[300:].cpu().view(100, 2, 64), want[2].permute(1, 0, 2)) and (vv[:300] == 7.0).all() and (kk[:300] == 7.0).all()
+    hgf.check_status()
+
+
+def test_append_to_more_sequences_than_run_at_once(hgf):
+    """Blocks of threads that a sequence turns out not to need may run long after those that it needs: they must not take its new length for the old one."""
+    n, m = 1024, 70
+    cache = hgf.KVCache(1, 64, 3 * n, n, 4)
+    hgf.cache_reserve(cache, ints(range(n)), ints([200] * n))
+    k, v = torch.randn(n * m, 128, device="cuda").bfloat16(), torch.randn(n * m, 64, device="cuda").bfloat16()
+    starts = ints(range(0, n * m + 1, m))
+    for step in range(2):                    # 70, 140 tokens: of each step's two possible blocks one is complete
+        assert hgf.cache_append(cache, k, v, ints(range(n)), starts).all()
+        assert (cache.length == m * (step + 1)).all() and not cache.arrivals.any()
+    got_k, got_v = hgf.cache_read(cache, ints(range(n)), ints([128] * n), ints(range(0, 12 * n + 1, 12)), 12 * n)
+    assert torch.equal(got_v.view(n, 12, 64), v.view(n, m, 64)[:, 58:].float()) and torch.equal(got_k.view(n, 12, 128), k.view(n, m, 128)[:, 58:].float())
+    got_k, _ = hgf.cache_read(cache, ints(range(n)), ints([0] * n), ints(range(0, 128 * n + 1, 128)), 128 * n)
+    want = torch.cat([k.view(n, m, 128), k.view(n, m, 128)[:, :58]], 1).float()
+    # half a step, 1 / 127 of each block's and stream's largest; the value's two roundings beside it
+    top = want.view(n, 2, 64, 2, 64).abs().amax((2, 4), keepdim=True)
+    assert ((got_k.view(n, 128, 128) - want).view(n, 2, 64, 2, 64).abs() <= top * (0.5 / 127 + 2.0 ** -22)).all()
+    out = hgf.diff_attention_cached(cache, torch.zeros(n, 128, device="cuda").bfloat16(), ints(range(n)), ints(range(n + 1)), 0.25)
+    got_k, got_v = hgf.cache_read(cache, ints(range(n)), ints([0] * n), ints(range(0, 140 * n + 1, 140)), 140 * n)
+    mean = 0.75 * got_v.view(n, 140, 64).double().mean(1)
+    assert (out - mean).abs().max() <= 1.25 * got_v.abs().max() * (2 * 140 * 2.0 ** -24 / 140 + 30 * 2.0 ** -23)   # (all probabilities are equal)
+    hgf.check_status()
+
+
 def test_append_without_room_leaves_the_sequence(hgf):
     p = Pair(hgf, 2, 64, n_pages=4, n_slots=6, max_pages=3)
     p.reserve([0, 1], [64, 64])
@@ -337,6 +377,23 @@ def test_scores_of_all_sizes(hgf, m):
     p.attend(slots, counts, spread=8.0)
     p.attend(slots, counts, spread=1e-30)
     p.attend(slots, counts, q=np.zeros((3 * m + 2, 256), np.uint16))
+
+
+@pytest.mark.parametrize("m", [1, 40])
+def test_blocks_of_zeros(hgf, m):
+    """Keys that are all zero (a scale of zero), behind and in front of others, in rows that see part of them."""
+    p = Pair(hgf, 2, 64, n_pages=20, n_slots=2)
+
+    def change(k, v):
+        k.reshape(-1, 2, 2, 64)[:64, 0] = 0
+        k.reshape(-1, 2, 2, 64)[128:200] = 0
+        v[64:128] = 0
+
+    p.reserve([0, 1], [200, 256])
+    p.append([0], [200], change=change)
+    p.append([1], [256], change=change)
+    p.attend([0, 1], [m, m])
+    p.attend([0, 1], [m, m], spread=5.0)
 
 
 @pytest.mark.parametrize("m", [1, 3])
