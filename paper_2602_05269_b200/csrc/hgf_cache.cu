@@ -188,13 +188,25 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
         return;
     }
 
+    // rows that stay open: those of the last block, or all new ones if none became complete
+    auto keep_open = [&](int head) {
+        constexpr int ROWS_AT_ONCE = kAppendThreads / EIGHTS;
+        const int from = blocks ? 0 : open0, rows = blocks ? (int)(after & 63) : m, src0 = row0 + m - rows, e = tid % EIGHTS, r_mine = tid / EIGHTS;
+#pragma unroll
+        for (int q = 0; q < kCacheBlock / ROWS_AT_ONCE; ++q) {
+            const int r = r_mine + q * ROWS_AT_ONCE;
+            if (r < rows) {
+                uint4 y[3];
+#pragma unroll
+                for (int n = 0; n < 3; ++n) y[n] = new_eight(n, head, src0 + r, e);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) *reinterpret_cast<uint4 *>(open_rows(head) + ((size_t)n * kCacheBlock + from + r) * DH + 8 * cache_open_eight(from + r, e)) = y[n];
+            }
+        }
+    };
     if (piece < blocks) {
         const int page = table[piece];
         for (int head = head0; head < H; head += gridDim.y) {
-            if (head != head0) {
-                load(head);
-                __syncthreads();  // (the page before has left shared memory)
-            }
 #pragma unroll
             for (int n = 0; n < 3; ++n) {
                 uint32_t acc = 0;
@@ -203,7 +215,8 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
                 acc = __reduce_max_sync(0xffffffffu, max(acc >> 16, acc & 0xffffu));
                 if (lane == 0) top_smem[n][warp] = acc;
             }
-            __syncthreads();
+            __syncthreads();                  // (and the page before has left shared memory, and all of the block's open rows have been read)
+            if (piece == 0) keep_open(head);
             uint32_t top[3];
 #pragma unroll
             for (int n = 0; n < 3; ++n) {
@@ -229,6 +242,7 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
                     }
                 }
             }
+            if (head + gridDim.y < H) load(head + gridDim.y);
             __syncthreads();
             const size_t at = (size_t)page * H + head;
             uint4 *dst = reinterpret_cast<uint4 *>(c.codes + at * (3 * kCacheBlock * DH));
@@ -239,24 +253,8 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
                 c.scales[at] = make_float4(scale(top[0]), scale(top[1]), scale(top[2]), 0.0f);
             }
         }
-    }
-    if (piece == 0) {
-        // rows that stay open: those of the last block, or all new ones if none became complete
-        const int from = blocks ? 0 : open0, rows = blocks ? (int)(after & 63) : m, src0 = row0 + m - rows;
-        constexpr int ROWS_AT_ONCE = kAppendThreads / EIGHTS;
-        const int e = tid % EIGHTS, r_mine = tid / EIGHTS;
-        for (int head = head0; head < H; head += gridDim.y)
-#pragma unroll
-            for (int q = 0; q < kCacheBlock / ROWS_AT_ONCE; ++q) {
-                const int r = r_mine + q * ROWS_AT_ONCE;
-                if (r < rows) {
-                    uint4 y[3];
-#pragma unroll
-                    for (int n = 0; n < 3; ++n) y[n] = new_eight(n, head, src0 + r, e);
-#pragma unroll
-                    for (int n = 0; n < 3; ++n) *reinterpret_cast<uint4 *>(open_rows(head) + ((size_t)n * kCacheBlock + from + r) * DH + 8 * cache_open_eight(from + r, e)) = y[n];
-                }
-            }
+    } else if (piece == 0) {
+        for (int head = head0; head < H; head += gridDim.y) keep_open(head);
     }
     // (pieces that the sequence turned out not to need arrive as well: they have read its length, too)
     __syncthreads();
