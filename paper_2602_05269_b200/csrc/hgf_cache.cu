@@ -100,6 +100,35 @@ __device__ __forceinline__ uint32_t transpose_bytes(uint32_t w, int lane) {
     return lane & 8 ? __byte_perm(o, w, 0x7351) : __byte_perm(w, o, 0x6240);
 }
 
+// Factor f with which rint(x f) is the rounding of the exact quotient 127 x / gamma, ties to even, for bf16 |x| <= gamma, in one multiplication.  With
+// eight-bit mantissas X and G the quotient is 127 X 2^e / G; unless it is half-way between two integers it is 1 / (2 G) or more away from that, far more
+// than two steps of f move it.  127 is a prime, so it is half-way only where 127 divides G, G = 254, or where it divides the odd number 2 n + 1 <= 254 of
+// the point n + 1/2, so n = 63 and |x| = gamma / 2.  For G = 254 the factor is a power of two, the product exact and the tie left to the rounding; else the
+// factor is the quotient 127 / gamma rounded and one step more, which takes |x| = gamma / 2 above 63.5, to the even 64.
+__device__ __forceinline__ float code_factor(float gamma) {
+    const float f = __fdiv_rn(127.0f, gamma);
+    return (__float_as_uint(gamma) >> 16 & 0x7fu) == 0x7eu ? f : __uint_as_float(__float_as_uint(f) + 1u);
+}
+// Codes of eight values (two words), x * up * f: rounded by adding 1.5 * 2^23, whose low byte is then the code.
+__device__ __forceinline__ uint2 codes8(const uint4 &v, float up, float f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const uint64_t f2 = pack_f32x2(f, f), up2 = pack_f32x2(up, up), magic = pack_f32x2(12582912.0f, 12582912.0f);
+    uint32_t b[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint64_t x = pack_f32x2(bf16lo_to_float(w[e]), bf16hi_to_float(w[e]));
+        if (up != 1.0f) x = mul_f32x2(x, up2);
+        float t0, t1;
+        unpack_f32x2(fma_f32x2(x, f2, magic), t0, t1);
+        b[2 * e] = __float_as_uint(t0);
+        b[2 * e + 1] = __float_as_uint(t1);
+    }
+    uint32_t o[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) o[h] = __byte_perm(__byte_perm(b[4 * h], b[4 * h + 1], 0x0040), __byte_perm(b[4 * h + 2], b[4 * h + 3], 0x0040), 0x5410);
+    return make_uint2(o[0], o[1]);
+}
+
 template <int DH>
 __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append_kernel(CacheView c, const __nv_bfloat16 *__restrict__ k, const __nv_bfloat16 *__restrict__ v, int n_rows,
                                                                        const int32_t *__restrict__ slots, const int32_t *__restrict__ starts, int n_seqs, int32_t *done,
@@ -224,15 +253,13 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
 #pragma unroll
                 for (int w = 0; w < WARPS; ++w) top[n] = max(top[n], top_smem[n][w]);
                 const float gamma = __uint_as_float(top[n] << 16);
-                // (bf16 patterns from 0x7f80 on are infinities and NaN; below 2^-100 the quotient 127 / max could leave binary32's range)
+                // (bf16 patterns from 0x7f80 on are infinities and NaN; below 2^-100 the factor could leave binary32's range)
                 const bool zero = top[n] == 0 || top[n] >= 0x7f80u;
-                QuantScale s = make_quant_scale(gamma);
-                if (gamma < 7.9e-31f) s.fast = false;
+                const float up = gamma < 7.888609052210118e-31f ? 1.2676506002282294e30f : 1.0f, f = zero ? 0.0f : code_factor(gamma * up);
                 uint8_t *dst = page_smem + n * kCacheBlock * DH + (n < 2 ? k_byte : v_byte);
 #pragma unroll
                 for (int u = 0; u < PER; ++u) {
-                    int sum = 0;
-                    const uint2 q = zero ? make_uint2(0, 0) : quant8<true>(x[n][u], s, sum);
+                    const uint2 q = zero ? make_uint2(0, 0) : codes8(x[n][u], up, f);
                     if (n < 2) {
                         *reinterpret_cast<uint32_t *>(dst + u * K_ON) = q.x;
                         *reinterpret_cast<uint32_t *>(dst + u * K_ON + 16) = q.y;

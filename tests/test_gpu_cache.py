@@ -156,6 +156,26 @@ def test_codes_at_the_edges_of_the_quantiser(hgf):
     p.check()
 
 
+@pytest.mark.parametrize("exponent", [-133, -100, -60, 0, 119])
+def test_codes_for_every_pair_of_mantissas(hgf, exponent):
+    """128 heads whose largest value has each of the mantissas of bf16, and values with each mantissa, sign and eight exponents under it."""
+    H, dh = 128, 64
+    values = np.stack([np.ldexp(128.0 + (np.arange(64 * 64) // 16) % 128, -(np.arange(64 * 64) % 8)) * np.where(np.arange(64 * 64) // 8 % 2, 1, -1)] * H).reshape(H, 64, 64)
+    top = 128.0 + np.arange(H)
+    values[np.abs(values) > top[:, None, None]] *= 0.5
+    values[:, 5, 7] = top
+    bits_ = f32_to_bf16_bits(np.ldexp(values, exponent).astype(np.float32)).transpose(1, 0, 2)      # token, head, dim (below 2^-126 some round: they are bf16 all the same)
+    p = Pair(hgf, H, dh, n_pages=1, n_slots=1, max_pages=1)
+    p.reserve([0], [64])
+
+    def change(k, v):
+        k.reshape(64, 2, H, dh)[:] = bits_[:, None]
+        v.reshape(64, H, dh)[:] = bits_
+
+    p.append([0], [64], change=change)
+    p.check()
+
+
 def test_rows_that_begin_later(hgf):
     """The first sequence's rows need not be the call's first."""
     p = Pair(hgf, 2, 64)
