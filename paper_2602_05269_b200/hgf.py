@@ -554,6 +554,7 @@ def cache_read(cache: KVCache, slots, first, starts, n_rows: int | None = None, 
     _list(cache, slots, first, starts)
     n, width = slots.numel(), cache.n_heads * cache.head_dim
     if k is None:
+        assert n_rows is not None, "cache_read takes either n_rows or k and v"
         dtype = torch.bfloat16 if flags & FLAG_OUT_BF16 else torch.float32
         with _on(stream):
             k, v = (torch.zeros((n_rows, w), dtype=dtype, device=cache.device) for w in (2 * width, width))
