@@ -36,8 +36,9 @@ struct CaCfg {
     static constexpr int KT = DH / 32, MT = DH / 16;
     static constexpr int SCORES = ROWS == 1 ? 2 * kCacheBlock * 4 : 0;  // bytes a warp
     static constexpr int PART = 4 + 2 * DH;                      // floats: maximum and sum of stream 1, of stream 2, sums of values of both
-    // (prefix sums, rounded up to 16 bytes; the parts of single tokens, two a warp, in shared memory)
-    static constexpr int PREFIX = (kCacheMaxSeqs + 2) * 8, PARTS = ROWS == 1 ? WARPS * 2 * PART * 4 : 0;
+    // (prefix sums, rounded up to 16 bytes; of single tokens the parts, two a warp; else room for 64 dims of the second stream's sums, for each pair of
+    // warps, in rows 68 floats apart)
+    static constexpr int PREFIX = (kCacheMaxSeqs + 2) * 8, GIVEN = 16 * 68, PARTS = ROWS == 1 ? WARPS * 2 * PART * 4 : WARPS / 2 * GIVEN * 4;
     static constexpr int SMEM = STAGES * STAGE + WARPS * SCORES + PREFIX + PARTS;
 };
 
@@ -52,7 +53,7 @@ struct CaParams {
     unsigned int *status;
     int n_seqs, n_rows, group, bf16;
     int teams, tiles, stages;  // of a CTA; of a team; of a team's ring
-    float lambda, out_scale, scale_log2;
+    float lambda, out_scale, scale_log2, per_group;  // (per_group: 1 / group)
 };
 
 // d = c + a b; c may be d.
@@ -100,9 +101,9 @@ __device__ __forceinline__ uint64_t ca_float2(int a, int b) {
     return add_f32x2(pack_f32x2(__int_as_float(a), __int_as_float(b)), pack_f32x2(-kCaMagicF, -kCaMagicF));
 }
 
-// A sequence of the call.
+// A sequence of the call; its items are tiles tile0 .. tiles - 1, since no row of those before sees a token.
 struct CaSeq {
-    int slot, row0, m, length, pages, units, tiles;
+    int slot, row0, m, length, pages, units, tile0, tiles;
 };
 __device__ __forceinline__ CaSeq ca_sequence(const CaParams &p, int rows, int i) {
     CaSeq s = {};
@@ -126,6 +127,7 @@ __device__ __forceinline__ CaSeq ca_sequence(const CaParams &p, int rows, int i)
     // (one more for what an item costs apart from its units, to begin and to end: no token is in it, so nothing is read)
     s.units = s.length ? s.pages + (open > 0) + (open > 32) + 1 : 0;
     s.tiles = (s.m * p.group + rows - 1) / rows;
+    s.tile0 = s.m > s.length ? (s.m - s.length) * p.group / rows : 0;
     return s;
 }
 // total * i / n and its inverse, the share of n that `unit` is in; i and n at most 1024 (a 64-bit division takes some 150 clocks, a 32-bit one 30).
@@ -152,10 +154,12 @@ __device__ __forceinline__ void ca_write(const CaParams &p, const CaItem &it, in
     else reinterpret_cast<float *>(p.out)[o] = y;
 }
 
+__device__ __forceinline__ void ca_put2(const CaParams &p, size_t at, float y0, float y1) {
+    if (p.bf16) *reinterpret_cast<__nv_bfloat162 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + at) = __floats2bfloat162_rn(y0, y1);
+    else *reinterpret_cast<float2 *>(reinterpret_cast<float *>(p.out) + at) = make_float2(y0, y1);
+}
 __device__ __forceinline__ void ca_write2(const CaParams &p, const CaItem &it, int rr, int dh, int dim, float y0, float y1) {
-    const size_t o = ((size_t)(it.row0 + rr / p.group) * p.c.H * p.group + it.head * p.group + rr % p.group) * dh + dim;
-    if (p.bf16) *reinterpret_cast<__nv_bfloat162 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + o) = __floats2bfloat162_rn(y0, y1);
-    else *reinterpret_cast<float2 *>(reinterpret_cast<float *>(p.out) + o) = make_float2(y0, y1);
+    ca_put2(p, ((size_t)(it.row0 + rr / p.group) * p.c.H * p.group + it.head * p.group + rr % p.group) * dh + dim, y0, y1);
 }
 
 // What parts of an item add up to, for four dims of a row.
@@ -231,10 +235,11 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     __shared__ __align__(8) uint64_t bars[C::STAGES];
     __shared__ int page_ok[C::STAGES];       // a stage's page number was one
     __shared__ volatile int gave_up;         // a wait ran out: the others end, too
+    __shared__ int unseen;                   // there are rows that see no token
     __shared__ CaItem first_item_of_cta, last_item_of[kCaMaxTeams];
     const uint32_t ring_a = dsmem_u32(ring), bars_a = dsmem_u32(bars) + team * stages * 8;
     if (tid < C::STAGES) dmbar_init(dsmem_u32(&bars[tid]), 1);
-    if (tid == 0) gave_up = 0;
+    if (tid == 0) gave_up = unseen = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     __syncthreads();
     pdl_wait();
@@ -248,7 +253,8 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     auto units_of = [&](int i) {
         const CaSeq s = ca_sequence(p, tile_rows, i);
         if (blockIdx.x == 0 && s.slot == -2) atomicOr(p.status, kStatusCache);
-        return (long long)s.tiles * H * s.units;
+        if (s.m > s.length) unseen = 1;
+        return (long long)(s.tiles - s.tile0) * H * s.units;
     };
     auto warp_sum = [&](long long sum) {
 #pragma unroll
@@ -284,17 +290,18 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     }
     __syncwarp();
 
-    // rows that see nothing because the sequence is empty
-    const int width = H * p.group * DH;
-    for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x)
-        if (prefix[i + 1] == prefix[i]) {
+    // rows that see no token: the first of more rows than the sequence has tokens.  (A warp that has not come across one does its part all the same once
+    // another has: the flag is read behind a barrier.)
+    __syncthreads();
+    if (unseen) {
+        const int width = H * p.group * DH;
+        for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x) {
             const CaSeq s = ca_sequence(p, tile_rows, i);
-            const size_t at = (size_t)s.row0 * width, n = (size_t)s.m * width;
-            for (size_t e = tid; e < n; e += blockDim.x) {
-                if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[at + e] = __float2bfloat16(0.0f);
-                else reinterpret_cast<float *>(p.out)[at + e] = 0.0f;
-            }
+            const size_t at = (size_t)s.row0 * width, n = (size_t)max(s.m - s.length, 0) * width;  // (16 bytes at a time: width is a multiple of 64)
+            if (p.bf16) for (size_t e = 8 * tid; e < n; e += 8 * blockDim.x) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
+            else for (size_t e = 4 * tid; e < n; e += 4 * blockDim.x) *reinterpret_cast<uint4 *>(reinterpret_cast<float *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
         }
+    }
 
     // ---- shares.  As many CTAs as have a unit for each team, as many teams as have a unit: none is empty between two of an item, and a short item
     // stays within a CTA.
@@ -308,6 +315,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     const int part_floats = (ROWS == 1 ? 1 : p.tiles) * (ROWS * C::PART);
     float *parts = ROWS == 1 ? reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + C::WARPS * C::SCORES + C::PREFIX) : p.parts + (size_t)blockIdx.x * teams_here * 2 * part_floats;
     float *my_parts = parts + team * 2 * part_floats;
+    float *given = reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + C::WARPS * C::SCORES + C::PREFIX) + (ROWS == 1 ? 0 : (warp >> 1) * C::GIVEN);
 
     auto place = [&](long long u, CaCursor &k) {
         int lo = 0, hi = p.n_seqs - 1;
@@ -322,6 +330,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         k.unit = (int)(in - item * k.s.units);
         k.tile = item <= 0xffffffffll ? (int)((uint32_t)item / (uint32_t)H) : (int)(item / H);
         k.head = (int)(item - (long long)k.tile * H);
+        k.tile += k.s.tile0;
     };
     auto advance = [&](CaCursor &k) {  // to the next unit; true: of another item
         if (++k.unit < k.s.units) return false;
@@ -329,14 +338,16 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         if (++k.head < H) return true;
         k.head = 0;
         if (++k.tile < k.s.tiles) return true;
-        k.tile = 0;
         do ++k.seq; while (k.seq < p.n_seqs - 1 && prefix[k.seq + 1] == prefix[k.seq]);
         if (k.seq < p.n_seqs) k.s = ca_sequence(p, tile_rows, k.seq);
+        k.tile = k.s.tile0;
         return true;
     };
-    // Row `at` of an item's sequence (token, then head of the group) sees the tokens before this; rows that are not there see none.
-    auto row_sees = [&](const CaSeq &s, int at) { return at < s.m * p.group ? s.length - s.m + at / p.group + 1 : 0; };
-    auto last_sees = [&](const CaSeq &s, int tile) { return row_sees(s, min((tile + 1) * tile_rows, s.m * p.group) - 1); };
+    // The last row of an item sees the tokens before this.
+    auto last_sees = [&](const CaSeq &s, int tile) {
+        const int at = (tile + 1) * tile_rows - 1;
+        return s.length - s.m + 1 + min(s.m - 1, p.group == 1 ? at : at / p.group);
+    };
     auto unit_token = [&](const CaCursor &k) { return k.unit < k.s.pages ? k.unit << 6 : (k.s.pages << 6) + ((k.unit - k.s.pages) << 5); };
     auto team_sync = [&] {
         if (ROWS == 1) __syncwarp();
@@ -409,24 +420,35 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     const uint32_t limb_xor = limb == 0 ? 0x80808080u : 0u, limb_keep = limb == 3 ? 0u : 0xffffffffu;
     const int heads = H * p.group;
 
-    auto q_row = [&](const CaCursor &k, int n, int at) {  // stream n of the item's row
-        const int token = p.group == 1 ? at : at / p.group;
-        return p.q + ((size_t)(k.s.row0 + token) * 2 + n) * heads * DH + (size_t)(k.head * p.group + at - token * p.group) * DH;
+    // Of the tile's row r: its token and its head of the group.  (One division an item: what is left is below 2^17, where a product with the rounded 1 / group
+    // is off by far less than the half that it stands from the next integer.)
+    struct Tile {
+        int token, left;  // of its first row
     };
+    auto tile_of = [&](const CaCursor &k) {
+        const int at = k.tile * tile_rows + my_tile * ROWS, token = p.group == 1 ? at : at / p.group;
+        return Tile{token, at - token * p.group};
+    };
+    auto token_of = [&](const Tile &b, int r) { return p.group == 1 ? b.token + r : b.token + (int)(((float)(b.left + r) + 0.5f) * p.per_group); };
+    auto q_row = [&](const CaCursor &k, const Tile &b, int n, int r) {  // stream n of the tile's row r
+        const int token = token_of(b, r);
+        return p.q + ((size_t)(k.s.row0 + token) * 2 + n) * heads * DH + (size_t)(k.head * p.group + b.left + r - (token - b.token) * p.group) * DH;
+    };
+    Tile tile = {0, 0};  // the item's
     uint2 qw[NR][C::KT][2];                        // q's values in the places of its digits: of the lane's rows (ROWS = 1: the one row) and stream
-    auto load_q = [&](const CaCursor &k) {
+    auto load_q = [&](const CaCursor &k, const Tile &b) {
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            const int at = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g + 8 * r);
-            const bool there = at < k.s.m * p.group;
-            const __nv_bfloat16 *src = q_row(k, my_stream, there ? at : 0) + 4 * t;
+            const int row = ROWS == 1 ? 0 : g + 8 * r;
+            const bool there = token_of(b, row) < k.s.m;
+            const __nv_bfloat16 *src = q_row(k, b, my_stream, there ? row : 0) + 4 * t;
 #pragma unroll
             for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) qw[r][kt][h] = there ? *reinterpret_cast<const uint2 *>(src + kt * 32 + h * 16) : make_uint2(0, 0);
         }
     };
-    if (ROWS == 1 && works) load_q(k);
+    if (ROWS == 1 && works) load_q(k, tile_of(k));
     ahead = k;
     long long ahead_u = u0;
     int ahead_sees = works ? last_sees(k.s, k.tile) : 0;  // tokens that the last row of the item sees
@@ -441,17 +463,23 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         for (int a = 0; a < NA; ++a)
 #pragma unroll
             for (int e = 0; e < NE; ++e) acc[a][e] = 0.0f;
-        const int base = k.tile * tile_rows + my_tile * ROWS, there = k.s.m * p.group;
+        tile = tile_of(k);
+        if (ROWS == 16) load_q(k, tile);
+        // row r sees the tokens before first + its token, if it is there
+        const int first = k.s.length - k.s.m + 1;
+        auto sees_of = [&](int r) {
+            const int token = token_of(tile, r);
+            return token < k.s.m ? first + token : 0;
+        };
         sees_item = last_sees(k.s, k.tile);
         if (ROWS == 1) {
-            sees[0] = sees_tile = sees_all = row_sees(k.s, base);
+            sees[0] = sees_tile = sees_all = sees_of(0);
         } else {
-            sees[0] = row_sees(k.s, base + g);
-            sees[NR - 1] = row_sees(k.s, base + g + 8);
-            sees_tile = base < there ? row_sees(k.s, min(base + 15, there - 1)) : 0;
-            sees_all = min(row_sees(k.s, base), row_sees(k.s, base + 15));
+            sees[0] = sees_of(g);
+            sees[NR - 1] = sees_of(g + 8);
+            sees_tile = tile.token < k.s.m ? first + min(k.s.m - 1, token_of(tile, 15)) : 0;
+            sees_all = min(sees_of(0), sees_of(15));
         }
-        if (ROWS == 16) load_q(k);
         // q's digits: q = f * 2^(E - 21) with E the exponent of the row's largest magnitude, so |f| < 2^22; f + 0x808080 has in each byte the
         // balanced digit plus 128.  (f is rounded by adding 1.5 * 2^23.)
 #pragma unroll
@@ -526,19 +554,21 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 
     int magic[4] = {(int)kCaMagic, (int)kCaMagic, (int)kCaMagic, (int)kCaMagic};
     const bool begins_inside = works && k.unit != 0;  // the share's first item began in another share
-    bool fresh = true, first_item = true;
+    bool fresh = true, first_item = true, has_next = false;
+    CaCursor next;
     // A warp whose wait ran out computes and fetches no more, but takes its steps to the end: the others of its team meet it at their barrier.
     bool dead = false;
     int stage = 0;
     for (long long u = u0; u < u1; ++u) {
         if (fresh) begin_item();
-        // (the next item's q is on its way while this one's last unit is worked on)
-        CaCursor next;
+        // (the next item's q is on its way while this one's last units are worked on)
         const bool item_ends = k.unit == k.s.units - 1;
-        if (ROWS == 1 && item_ends && u + 1 < u1) {
+        if (ROWS == 1 && !has_next && k.unit >= k.s.units - 2 && u + (k.s.units - k.unit) < u1) {
             next = k;
+            next.unit = k.s.units - 1;
             advance(next);
-            load_q(next);
+            load_q(next, tile_of(next));
+            has_next = true;
         }
         const uint8_t *unit = ring + stage * C::STAGE;
         const int token0 = unit_token(k);
@@ -698,9 +728,9 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                 uint32_t qb[NR][DH / 16][2];  // q's values as pairs
 #pragma unroll
                 for (int r = 0; r < NR; ++r) {
-                    const int row = k.tile * tile_rows + my_tile * ROWS + (ROWS == 1 ? 0 : g + 8 * r);
-                    const bool there = row < k.s.m * p.group && (ROWS == 16 || !limb);
-                    const __nv_bfloat16 *src = q_row(k, my_stream, there ? row : 0) + 2 * t;
+                    const int row = ROWS == 1 ? 0 : g + 8 * r;
+                    const bool there = ROWS == 1 ? !limb : token_of(tile, row) < k.s.m;
+                    const __nv_bfloat16 *src = q_row(k, tile, my_stream, there ? row : 0) + 2 * t;
 #pragma unroll
                     for (int kt = 0; kt < DH / 16; ++kt)
 #pragma unroll
@@ -827,7 +857,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         // ---- the item's end, or the share's
         if (item_ends || u + 1 == u1) {
             const bool whole = item_ends && !(first_item && begins_inside);
-            float *part = my_parts + (first_item && !whole ? 0 : part_floats) + my_tile * (ROWS * C::PART);
+            float *part = my_parts + (first_item ? 0 : part_floats) + my_tile * (ROWS * C::PART);
             const CaItem it = {u - k.unit, u - k.unit + k.s.units, k.s.row0, k.s.m, k.head, k.tile};
             if (u + 1 == u1 && leads && lane == 0) last_item_of[team] = it;
 #pragma unroll
@@ -859,31 +889,43 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     }
                 if (!whole && lane == 0) *reinterpret_cast<float4 *>(part) = make_float4(m1, l1, m2, l2);
             } else {
-                // the second stream's warps leave their sums, of a whole item as they enter the output; the first's finish those
                 float inv[NR];
 #pragma unroll
                 for (int r = 0; r < NR; ++r) {
-                    float *mine = part + (g + 8 * r) * C::PART;
-                    if (!whole && t == 0) *reinterpret_cast<float2 *>(mine + 2 * stream) = make_float2(m[r], l[r]);
-                    inv[r] = !whole ? 1.0f : l[r] != 0.0f ? (stream ? p.lambda : 1.0f) * p.out_scale / l[r] : 0.0f;
-                    if (!whole || stream)
+                    inv[r] = l[r] != 0.0f ? (stream ? p.lambda : 1.0f) * p.out_scale / l[r] : 0.0f;
+                    if (!whole) {
+                        float *mine = part + (g + 8 * r) * C::PART;
+                        if (t == 0) *reinterpret_cast<float2 *>(mine + 2 * stream) = make_float2(m[r], l[r]);
 #pragma unroll
-                        for (int a = 0; a < NA; ++a)
-                            *reinterpret_cast<float2 *>(mine + 4 + stream * DH + 8 * a + 2 * t) = make_float2(acc[a][(2 * r) % NE] * inv[r], acc[a][(2 * r + 1) % NE] * inv[r]);
+                        for (int a = 0; a < NA; ++a) *reinterpret_cast<float2 *>(mine + 4 + stream * DH + 8 * a + 2 * t) = make_float2(acc[a][(2 * r) % NE], acc[a][(2 * r + 1) % NE]);
+                    }
                 }
-                if (whole) {
-                    team_sync();
+                if (whole) {  // the second stream's warps give theirs, as they enter the output, to the first's
 #pragma unroll
-                    for (int r = 0; r < NR; ++r) {
-                        const int row = my_tile * ROWS + g + 8 * r, rr = k.tile * tile_rows + row;
-                        if (!stream && rr < k.s.m * p.group) {
-                            const float *other = part + (g + 8 * r) * C::PART + 4 + DH + 2 * t;
+                    for (int part64 = 0; part64 < DH / 64; ++part64) {
+                        if (part64) team_sync();
+                        if (stream)
 #pragma unroll
-                            for (int a = 0; a < NA; ++a) {
-                                const float2 o = *reinterpret_cast<const float2 *>(other + 8 * a);
-                                ca_write2(p, it, rr, DH, 8 * a + 2 * t, acc[a][(2 * r) % NE] * inv[r] - o.x, acc[a][(2 * r + 1) % NE] * inv[r] - o.y);
+                            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                                for (int a = 0; a < 8; ++a) {
+                                    const float *o = acc[ROWS == 1 ? 0 : 8 * part64 + a];
+                                    *reinterpret_cast<float2 *>(given + (g + 8 * r) * 68 + 8 * a + 2 * t) = make_float2(o[(2 * r) % NE] * inv[r], o[(2 * r + 1) % NE] * inv[r]);
+                                }
+                        team_sync();
+                        if (!stream)
+#pragma unroll
+                            for (int r = 0; r < NR; ++r) {
+                                const int token = token_of(tile, g + 8 * r);
+                                if (token >= k.s.m) continue;
+                                const size_t row = (size_t)(k.s.row0 + token) * heads + k.head * p.group + tile.left + g + 8 * r - (token - tile.token) * p.group;
+#pragma unroll
+                                for (int a = 0; a < 8; ++a) {
+                                    const float *o = acc[ROWS == 1 ? 0 : 8 * part64 + a];
+                                    const float2 other = *reinterpret_cast<const float2 *>(given + (g + 8 * r) * 68 + 8 * a + 2 * t);
+                                    ca_put2(p, row * DH + 64 * part64 + 8 * a + 2 * t, o[(2 * r) % NE] * inv[r] - other.x, o[(2 * r + 1) % NE] * inv[r] - other.y);
+                                }
                             }
-                        }
                     }
                 }
             }
@@ -891,8 +933,12 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         }
         fresh = item_ends;
         if (ROWS == 1) {
-            if (item_ends && u + 1 < u1) k = next;
-            else ++k.unit;
+            if (item_ends && u + 1 < u1) {
+                k = next;
+                has_next = false;
+            } else {
+                ++k.unit;
+            }
         } else if (u + 1 < u1) {
             advance(k);
         }
@@ -1035,6 +1081,7 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     p.lambda = lambda;
     p.out_scale = out_scale;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)dh));
+    p.per_group = (float)(1.0 / group);
     const cudaStream_t stream = (cudaStream_t)stream_;
     cudaError_t e;
     if (f.rows == 1) e = dh == 64 ? launch_cached_attention<64, 1, 3>(p, f.threads, stream) : launch_cached_attention<128, 1, 3>(p, f.threads, stream);
