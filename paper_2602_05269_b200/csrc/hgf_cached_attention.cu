@@ -14,11 +14,13 @@
 // The accumulators start at the bits of 1.5 * 2^23, so that a sum, below 2^22 in magnitude, is a float after one subtraction: I2F runs at an eighth
 // of the FMA rate and bounded the kernel.  The open tokens' bf16 go through bf16 products, with the probabilities as sums of three bf16.
 //
-// Two forms.  ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.
-// There the codes are the left operand, tokens (or dims) as its rows.  ROWS = 16 otherwise: sixteen query rows are the left operand, a product for each
-// digit, the codes the right one (a lane's sixteen bytes are the same either way round); a warp takes one stream of one tile of sixteen rows, and a
-// team is the warps of one or two tiles, so that a page that is read once serves up to 32 rows.  The columns of the scores' products are the page's
-// tokens in such an order that a lane gets four neighbouring tokens of its rows: the probabilities' digits are then in place for the second product.
+// Three forms.  ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.  There
+// and with ROWS = 8, a few tokens or heads that share K and V, the codes are the left operand, tokens (or dims) as its rows; eight query rows are the
+// columns of a product for each digit, and a team is a warp for each stream.  ROWS = 16, for more: sixteen query rows are the left operand and the
+// codes the right one (a lane's sixteen bytes are the same either way round); a warp takes one stream of one tile of sixteen rows, and a team is the
+// warps of one or two tiles, so that a page that is read once serves up to 32 rows.  There the columns of the scores' products are the page's tokens in
+// such an order that a lane gets four neighbouring tokens of its rows: the probabilities' digits are then in place for the second product, where
+// ROWS = 8 turns the scores through shared memory.
 #include "hgf_cache.cuh"
 #include "hgf_warp.cuh"
 
@@ -29,16 +31,16 @@ constexpr int kCaMaxTeams = 8;      // teams of a CTA at most
 
 template <int DH, int ROWS>
 struct CaCfg {
-    static constexpr int WARPS = ROWS == 1 && DH == 128 ? 4 : 8, THREADS = WARPS * 32;
+    static constexpr int WARPS = ROWS == 8 && DH == 64 ? 16 : ROWS == 1 && DH == 128 ? 4 : 8, THREADS = WARPS * 32;
     static constexpr int UNIT = 3 * kCacheBlock * DH;            // bytes of a unit
     static constexpr int STAGE = (UNIT + 16 + 127) / 128 * 128;  // with the page's scales
     static constexpr int STAGES = DH == 64 ? 16 : 8;             // of all teams' rings
     static constexpr int KT = DH / 32, MT = DH / 16;
-    static constexpr int SCORES = ROWS == 1 ? 2 * kCacheBlock * 4 : 0;  // bytes a warp
+    static constexpr int SCORES = ROWS == 1 ? 2 * kCacheBlock * 4 : ROWS == 8 ? 8 * 36 * 4 : 0;  // bytes a warp; rows 36 floats apart: eight rows' writes hit all banks
     static constexpr int PART = 4 + 2 * DH;                      // floats: maximum and sum of stream 1, of stream 2, sums of values of both
-    // (prefix sums, rounded up to 16 bytes; of single tokens the parts, two a warp; else room for 64 dims of the second stream's sums, for each pair of
-    // warps, in rows 68 floats apart)
-    static constexpr int PREFIX = (kCacheMaxSeqs + 2) * 8, GIVEN = 16 * 68, PARTS = ROWS == 1 ? WARPS * 2 * PART * 4 : WARPS / 2 * GIVEN * 4;
+    // (prefix sums, rounded up to 16 bytes; of single tokens the parts, two a warp; of sixteen rows room for 64 dims of the second stream's sums, for each
+    // pair of warps, in rows 68 floats apart, which with eight rows is the pair's room for scores)
+    static constexpr int PREFIX = (kCacheMaxSeqs + 2) * 8, GIVEN = 16 * 68, PARTS = ROWS == 1 ? WARPS * 2 * PART * 4 : ROWS == 16 ? WARPS / 2 * GIVEN * 4 : 0;
     static constexpr int SMEM = STAGES * STAGE + WARPS * SCORES + PREFIX + PARTS;
 };
 
@@ -49,7 +51,7 @@ struct CaParams {
     void *out;
     int4 *items;          // [CTAs][2]: what the joining kernel does for a CTA
     float *cta_parts;     // [CTAs][2][tiles][ROWS][PART]
-    float *parts;         // [CTAs][teams][2][tiles][ROWS][PART], ROWS = 16
+    float *parts;         // [CTAs][teams][2][tiles][ROWS][PART], ROWS > 1
     unsigned int *status;
     int n_seqs, n_rows, group, bf16;
     int teams, tiles, stages;  // of a CTA; of a team; of a team's ring
@@ -315,7 +317,8 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     const int part_floats = (ROWS == 1 ? 1 : p.tiles) * (ROWS * C::PART);
     float *parts = ROWS == 1 ? reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + C::WARPS * C::SCORES + C::PREFIX) : p.parts + (size_t)blockIdx.x * teams_here * 2 * part_floats;
     float *my_parts = parts + team * 2 * part_floats;
-    float *given = reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + C::WARPS * C::SCORES + C::PREFIX) + (ROWS == 1 ? 0 : (warp >> 1) * C::GIVEN);
+    float *given = ROWS == 8 ? reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + (warp & ~1) * C::SCORES)
+                             : reinterpret_cast<float *>(smem + C::STAGES * C::STAGE + C::WARPS * C::SCORES + C::PREFIX) + (ROWS == 1 ? 0 : (warp >> 1) * C::GIVEN);
 
     auto place = [&](long long u, CaCursor &k) {
         int lo = 0, hi = p.n_seqs - 1;
@@ -409,10 +412,12 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 
     // ---- state of the item
     // ROWS = 1: m, l of the lane's stream (lanes 0-15 stream 1, 16-31 stream 2); acc[mt][e]: dims 16 mt + g + 8 e, in lanes t of stream t / 2.
+    // ROWS = 8: m, l of row g, of the warp's stream; acc[mt][e]: dim 16 mt + g + 8 (e / 2), row 2 t + e % 2.
     // ROWS = 16: m, l of rows g and g + 8, of the warp's stream; acc[nt][e]: dim 8 nt + 2 t + e % 2, row g + 8 (e / 2).
-    constexpr int NR = ROWS == 1 ? 1 : 2, NA = ROWS == 1 ? C::MT : DH / 8, NE = ROWS == 1 ? 2 : 4, ND = ROWS == 1 ? 1 : 3;
+    constexpr int NR = ROWS == 16 ? 2 : 1, NA = ROWS == 16 ? DH / 8 : C::MT, NE = ROWS == 1 ? 2 : 4, ND = ROWS == 1 ? 1 : 3;
     float m[NR], l[NR], acc[NA][NE];
-    uint32_t qd[ROWS == 1 ? 2 : ND][C::KT][ROWS == 1 ? 2 : 4];  // digits of q: ROWS = 1 for K1 and for K2, as right operand; ROWS = 16 each digit, as left operand
+    uint32_t qd[ROWS == 1 ? 2 : ND][C::KT][ROWS == 16 ? 4 : 2];  // digits of q: ROWS = 1 for K1 and for K2, as right operand; else each digit, as right or left operand
+    int sees_e[2] = {0, 0};                        // (ROWS = 8) tokens that rows 2 t and 2 t + 1 see
     float qs[NR];                                  // what a digit sum is worth, with 1 / sqrt(d) and log2 e
     int sees[NR] = {}, sees_tile = 0, sees_all = 0, sees_item = 0;  // tokens that the lane's rows, any row, every row of the tile, any of the item sees
     const int my_stream = ROWS == 1 ? lane >> 4 : stream, limb = g & 3;
@@ -464,7 +469,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 #pragma unroll
             for (int e = 0; e < NE; ++e) acc[a][e] = 0.0f;
         tile = tile_of(k);
-        if (ROWS == 16) load_q(k, tile);
+        if (ROWS > 1) load_q(k, tile);
         // row r sees the tokens before first + its token, if it is there
         const int first = k.s.length - k.s.m + 1;
         auto sees_of = [&](int r) {
@@ -474,6 +479,12 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         sees_item = last_sees(k.s, k.tile);
         if (ROWS == 1) {
             sees[0] = sees_tile = sees_all = sees_of(0);
+        } else if (ROWS == 8) {
+            sees[0] = sees_of(g);
+            sees_e[0] = sees_of(2 * t);
+            sees_e[1] = sees_of(2 * t + 1);
+            sees_tile = sees_item;
+            sees_all = min(sees_of(0), sees_of(7));
         } else {
             sees[0] = sees_of(g);
             sees[NR - 1] = sees_of(g + 8);
@@ -515,7 +526,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 #pragma unroll
                         for (int j = 0; j < ND; ++j) {
                             const uint32_t sel = 0x0040u + (uint32_t)(2 - j) * 0x0011u;
-                            qd[j][kt][ROWS == 1 ? h : 2 * h + r] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
+                            qd[j][kt][ROWS == 16 ? 2 * h + r : h] = __byte_perm(__byte_perm(d[0], d[1], sel), __byte_perm(d[2], d[3], sel), 0x5410) ^ 0x80808080u;
                         }
                     }
                 }
@@ -646,6 +657,83 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                         acc[mt][0] = fmaf(ca_float(d[0]), va, fmaf(ca_float(d[1]), vb, acc[mt][0] * scale));
                         acc[mt][1] = fmaf(ca_float(d[2]), va, fmaf(ca_float(d[3]), vb, acc[mt][1] * scale));
                     }
+                } else if constexpr (ROWS == 8) {
+                    const uint64_t base256 = pack_f32x2(256.0f, 256.0f);
+                    const uint8_t *codes = unit + stream * kCacheBlock * DH;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                        for (int mh = 0; mh < 2; ++mh) {
+                            const int mt = 2 * half + mh;
+                            int d[3][4];
+#pragma unroll
+                            for (int kt = 0; kt < C::KT; ++kt) {
+                                const uint4 a = *reinterpret_cast<const uint4 *>(codes + ((mt * C::KT + kt) * 32 + lane) * 16);
+#pragma unroll
+                                for (int z = 0; z < 3; ++z) mma_s8s8(d[z], a, qd[z][kt][0], qd[z][kt][1], kt ? d[z] : magic);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; e += 2) {
+                                float v0, v1;
+                                unpack_f32x2(fma_f32x2(fma_f32x2(ca_float2(d[0][e], d[0][e + 1]), base256, ca_float2(d[1][e], d[1][e + 1])), base256, ca_float2(d[2][e], d[2][e + 1])), v0, v1);
+                                scores[2 * t * 36 + mh * 16 + g + 4 * e] = v0;
+                                scores[2 * t * 36 + 36 + mh * 16 + g + 4 * e] = v1;
+                            }
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const float4 v = *reinterpret_cast<const float4 *>(scores + g * 36 + j * 16 + 4 * t);
+                            x[0][8 * half + 4 * j] = v.x;
+                            x[0][8 * half + 4 * j + 1] = v.y;
+                            x[0][8 * half + 4 * j + 2] = v.z;
+                            x[0][8 * half + 4 * j + 3] = v.w;
+                        }
+                        __syncwarp();
+                    }
+                    softmax_step(x[0], 0, qs[0] * (stream ? sc.y : sc.x), partly, sees[0] - token0, token, alpha[0], worth[0]);
+                    uint32_t pd[DP][4];  // digits of the probabilities, as right operand
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t w[4];
+                        if (DP == 3) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[0][4 * j + e]);
+                            pd[0][j] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
+                        } else {  // (65535 p beside 128: p = 1 stays within 16 bits)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(fmaf(x[0][4 * j + e], 0.9999847412109375f, 128.0f));
+                        }
+                        const uint32_t w01 = __byte_perm(w[0], w[1], 0x5140), w23 = __byte_perm(w[2], w[3], 0x5140);
+                        pd[DP - 2][j] = __byte_perm(w01, w23, 0x7632);
+                        pd[DP - 1][j] = __byte_perm(w01, w23, 0x5410);
+                    }
+                    // (a row that sees none of the page takes nothing of it, not even a scale that is NaN)
+                    constexpr float kUnit = DP == 3 ? 1.1920928955078125e-7f : 1.0f / 65535.0f;
+                    float scale[2], sv[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        scale[e] = __shfl_sync(0xffffffffu, alpha[0], (2 * t + e) * 4);
+                        sv[e] = __shfl_sync(0xffffffffu, worth[0], (2 * t + e) * 4);
+                        sv[e] = sees_e[e] > token0 ? sv[e] * sc.z * kUnit : 0.0f;
+                    }
+                    const uint64_t scale2 = pack_f32x2(scale[0], scale[1]), sv2 = pack_f32x2(sv[0], sv[1]);
+#pragma unroll
+                    for (int mt = 0; mt < C::MT; ++mt) {
+                        int d[DP][4];
+#pragma unroll
+                        for (int kt = 0; kt < 2; ++kt) {
+                            const uint4 a = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
+#pragma unroll
+                            for (int z = 0; z < DP; ++z) mma_s8u8(d[z], a, pd[z][2 * kt], pd[z][2 * kt + 1], kt ? d[z] : magic);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            uint64_t y = fma_f32x2(ca_float2(d[0][e], d[0][e + 1]), base256, ca_float2(d[1][e], d[1][e + 1]));
+                            if (DP == 3) y = fma_f32x2(y, base256, ca_float2(d[DP - 1][e], d[DP - 1][e + 1]));
+                            unpack_f32x2(fma_f32x2(y, sv2, mul_f32x2(pack_f32x2(acc[mt][e % NE], acc[mt][(e + 1) % NE]), scale2)), acc[mt][e % NE], acc[mt][(e + 1) % NE]);
+                        }
+                    }
                 } else {
                     const uint64_t base256 = pack_f32x2(256.0f, 256.0f);
                     // Column n of a product is token 4 (n / 2) + n % 2 of sixteen, or the one two further: a lane's two columns are then its first or
@@ -661,7 +749,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                                 const uint8_t *at = codes + (j * C::KT + kt) * 512 + two * 128;
                                 const uint32_t b0 = *reinterpret_cast<const uint32_t *>(at), b1 = *reinterpret_cast<const uint32_t *>(at + 8);
 #pragma unroll
-                                for (int z = 0; z < 3; ++z) mma_s8s8(d[z], make_uint4(qd[z][kt][0], qd[z][kt][1], qd[z][kt][ROWS == 1 ? 0 : 2], qd[z][kt][ROWS == 1 ? 0 : 3]), b0, b1, kt ? d[z] : magic);
+                                for (int z = 0; z < 3; ++z) mma_s8s8(d[z], make_uint4(qd[z][kt][0], qd[z][kt][1], qd[z][kt][ROWS == 16 ? 2 : 0], qd[z][kt][ROWS == 16 ? 3 : 0]), b0, b1, kt ? d[z] : magic);
                             }
 #pragma unroll
                             for (int r = 0; r < NR; ++r)
@@ -705,7 +793,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 #pragma unroll
                         for (int a = 0; a < 2; ++a) {
                             int d[DP][4];
-                            float (&o)[NE] = acc[ROWS == 1 ? 0 : 2 * mt + a];
+                            float (&o)[NE] = acc[ROWS == 16 ? 2 * mt + a : 0];
 #pragma unroll
                             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -751,49 +839,83 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     return ldmatrix4_trans(at + 2 * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, i * 2 + (lane >> 3 & 1)) * 16);
                 };
                 // (a query that is not finite: its digits mean nothing, but the products of its bf16 values do; qs is NaN then)
-                if constexpr (ROWS == 1) {
+                if constexpr (ROWS != 16) {
                     auto k_eight = [&](int n, int mt, int kt) {
                         const int r = mt * 16 + (lane & 15);
                         return ldmatrix4(at + n * 32 * DH * 2 + r * DH * 2 + cache_open_eight(r, kt * 2 + (lane >> 4)) * 16);
                     };
                     float d[2][4] = {};
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
+                    for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n)
 #pragma unroll
-                        for (int kt = 0; kt < DH / 16; ++kt)
+                        for (int kt = 0; kt < DH / 16; ++kt) {
+                            const bool mine = ROWS == 8 || my_stream == n;
 #pragma unroll
-                            for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(n, mt, kt), my_stream == n ? qb[0][kt][0] : 0u, my_stream == n ? qb[0][kt][1] : 0u);
-                    if (!(t & 1)) {
+                            for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(ROWS == 1 ? n : stream, mt, kt), mine ? qb[0][kt][0] : 0u, mine ? qb[0][kt][1] : 0u);
+                        }
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) {
+                    for (int mt = 0; mt < 2; ++mt) {
+                        if (ROWS == 8) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) scores[(2 * t + (e & 1)) * 36 + mt * 16 + g + (e >> 1) * 8] = d[mt][e];
+                        } else if (!(t & 1)) {
                             scores[(t >> 1) * kCacheBlock + mt * 16 + g] = d[mt][0];
                             scores[(t >> 1) * kCacheBlock + mt * 16 + g + 8] = d[mt][2];
                         }
                     }
                     __syncwarp();
+                    const float *row = scores + (ROWS == 8 ? g * 36 : my_stream * kCacheBlock);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float2 v = *reinterpret_cast<const float2 *>(scores + my_stream * kCacheBlock + 8 * j + 2 * t);
+                        const float2 v = *reinterpret_cast<const float2 *>(row + 8 * j + 2 * t);
                         x[0][2 * j] = v.x;
                         x[0][2 * j + 1] = v.y;
                     }
                     __syncwarp();
                     softmax_step(x[0], 0, qs[0] == qs[0] ? p.scale_log2 : qs[0], true, min(rows, sees[0] - token0), token, alpha[0], worth[0]);
-                    uint32_t b[2][2];
+                    uint32_t b[3][2][2];  // (ROWS = 1: the lane's digit, in the first)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t w[3];
                         three(x[0][2 * j], x[0][2 * j + 1], w);
-                        b[j >> 1][j & 1] = limb == 0 ? w[0] : limb == 1 ? w[1] : limb == 2 ? w[2] : 0u;
+                        if (ROWS == 8) {
+#pragma unroll
+                            for (int z = 0; z < 3; ++z) b[z][j >> 1][j & 1] = w[z];
+                        } else {
+                            b[0][j >> 1][j & 1] = limb == 0 ? w[0] : limb == 1 ? w[1] : limb == 2 ? w[2] : 0u;
+                        }
                     }
-                    const float scale = __shfl_sync(0xffffffffu, alpha[0], (t >> 1) * 16), sv = __shfl_sync(0xffffffffu, worth[0], (t >> 1) * 16);
+                    if constexpr (ROWS == 1) {
+                        const float scale = __shfl_sync(0xffffffffu, alpha[0], (t >> 1) * 16), sv = __shfl_sync(0xffffffffu, worth[0], (t >> 1) * 16);
 #pragma unroll
-                    for (int mt = 0; mt < C::MT; ++mt) {
-                        float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        for (int mt = 0; mt < C::MT; ++mt) {
+                            float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int kt = 0; kt < 2; ++kt) mma_bf16(o, v_four(mt, kt), b[kt][0], b[kt][1]);
-                        acc[mt][0] = fmaf(t & 1 ? o[0] : o[0] + o[1], sv, acc[mt][0] * scale);
-                        acc[mt][1] = fmaf(t & 1 ? o[2] : o[2] + o[3], sv, acc[mt][1] * scale);
+                            for (int kt = 0; kt < 2; ++kt) mma_bf16(o, v_four(mt, kt), b[0][kt][0], b[0][kt][1]);
+                            acc[mt][0] = fmaf(t & 1 ? o[0] : o[0] + o[1], sv, acc[mt][0] * scale);
+                            acc[mt][1] = fmaf(t & 1 ? o[2] : o[2] + o[3], sv, acc[mt][1] * scale);
+                        }
+                    } else {
+                        float scale[2], sv[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            scale[e] = __shfl_sync(0xffffffffu, alpha[0], (2 * t + e) * 4);
+                            sv[e] = __shfl_sync(0xffffffffu, worth[0], (2 * t + e) * 4);
+                        }
+#pragma unroll
+                        for (int mt = 0; mt < C::MT; ++mt) {
+                            float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                            for (int kt = 0; kt < 2; ++kt) {
+                                const uint4 v = v_four(mt, kt);
+#pragma unroll
+                                for (int z = 0; z < 3; ++z) mma_bf16(o, v, b[z][kt][0], b[z][kt][1]);
+                            }
+                            // (a row that sees none of these tokens takes nothing of them, not even a value that is NaN)
+#pragma unroll
+                            for (int e = 0; e < NE; ++e)
+                                if (sees_e[e & 1] > token0) acc[mt][e] = fmaf(o[e], sv[e & 1], acc[mt][e] * scale[e & 1]);
+                        }
                     }
                 } else {
 #pragma unroll
@@ -810,7 +932,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[ROWS == 1 ? 0 : e >> 1][4 * two + 2 * i + (e & 1)] = d[i][e];
+                            for (int e = 0; e < 4; ++e) x[ROWS == 16 ? e >> 1 : 0][4 * two + 2 * i + (e & 1)] = d[i][e];
                     }
                     uint32_t b[2][3][4];  // the probabilities' three, as left operand of the products over sixteen tokens
 #pragma unroll
@@ -842,7 +964,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
                             for (int e = 0; e < NE; ++e) {
-                                float &y = acc[ROWS == 1 ? 0 : 2 * mt + i][e];
+                                float &y = acc[ROWS == 16 ? 2 * mt + i : 0][e];
                                 if (sees[(e >> 1) % NR] > token0) y = fmaf(o[i][e], worth[(e >> 1) % NR], y * alpha[(e >> 1) % NR]);
                             }
                     }
@@ -888,6 +1010,49 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                         }
                     }
                 if (!whole && lane == 0) *reinterpret_cast<float4 *>(part) = make_float4(m1, l1, m2, l2);
+            } else if constexpr (ROWS == 8) {
+                if (!whole) {
+                    if (t == 0) *reinterpret_cast<float2 *>(part + g * C::PART + 2 * stream) = make_float2(m[0], l[0]);
+#pragma unroll
+                    for (int mt = 0; mt < C::MT; ++mt)
+#pragma unroll
+                        for (int e = 0; e < NE; ++e) part[(2 * t + (e & 1)) * C::PART + 4 + stream * DH + mt * 16 + g + 8 * (e >> 1)] = acc[mt][e];
+                } else {  // the second stream's warp gives its sums, as they enter the output, to the first's
+                    const float mine = l[0] != 0.0f ? (stream ? p.lambda : 1.0f) * p.out_scale / l[0] : 0.0f;
+                    float inv[2];
+                    size_t row[2];
+                    bool there[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        inv[e] = __shfl_sync(0xffffffffu, mine, (2 * t + e) * 4);
+                        const int token = token_of(tile, 2 * t + e);
+                        there[e] = token < k.s.m;
+                        row[e] = ((size_t)(k.s.row0 + token) * heads + k.head * p.group + tile.left + 2 * t + e - (token - tile.token) * p.group) * DH;
+                    }
+#pragma unroll
+                    for (int part64 = 0; part64 < DH / 64; ++part64) {
+                        if (part64) team_sync();
+                        if (stream)
+#pragma unroll
+                            for (int a = 0; a < 4; ++a)
+#pragma unroll
+                                for (int e = 0; e < NE; ++e) given[(2 * t + (e & 1)) * 68 + a * 16 + g + 8 * (e >> 1)] = acc[4 * part64 + a][e] * inv[e & 1];
+                        team_sync();
+                        if (!stream)
+#pragma unroll
+                            for (int a = 0; a < 4; ++a)
+#pragma unroll
+                                for (int e = 0; e < NE; ++e) {
+                                    const int dim = a * 16 + g + 8 * (e >> 1);
+                                    const float y = acc[4 * part64 + a][e] * inv[e & 1] - given[(2 * t + (e & 1)) * 68 + dim];
+                                    if (!there[e & 1]) continue;
+                                    const size_t o = row[e & 1] + 64 * part64 + dim;
+                                    if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[o] = __float2bfloat16(y);
+                                    else reinterpret_cast<float *>(p.out)[o] = y;
+                                }
+                    }
+                    team_sync();  // (the room is that of the scores)
+                }
             } else {
                 float inv[NR];
 #pragma unroll
@@ -909,7 +1074,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                             for (int r = 0; r < NR; ++r)
 #pragma unroll
                                 for (int a = 0; a < 8; ++a) {
-                                    const float *o = acc[ROWS == 1 ? 0 : 8 * part64 + a];
+                                    const float *o = acc[ROWS == 16 ? 8 * part64 + a : 0];
                                     *reinterpret_cast<float2 *>(given + (g + 8 * r) * 68 + 8 * a + 2 * t) = make_float2(o[(2 * r) % NE] * inv[r], o[(2 * r + 1) % NE] * inv[r]);
                                 }
                         team_sync();
@@ -921,7 +1086,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                                 const size_t row = (size_t)(k.s.row0 + token) * heads + k.head * p.group + tile.left + g + 8 * r - (token - tile.token) * p.group;
 #pragma unroll
                                 for (int a = 0; a < 8; ++a) {
-                                    const float *o = acc[ROWS == 1 ? 0 : 8 * part64 + a];
+                                    const float *o = acc[ROWS == 16 ? 8 * part64 + a : 0];
                                     const float2 other = *reinterpret_cast<const float2 *>(given + (g + 8 * r) * 68 + 8 * a + 2 * t);
                                     ca_put2(p, row * DH + 64 * part64 + 8 * a + 2 * t, o[(2 * r) % NE] * inv[r] - other.x, o[(2 * r + 1) % NE] * inv[r] - other.y);
                                 }
@@ -993,15 +1158,17 @@ __global__ void __launch_bounds__(8 * DH / 4) cached_attention_join_kernel(CaPar
     sum.write(p, it, it.tile * all + r, DH, dim);
 }
 
-// How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of sixteen rows, two to a team where the
-// sequences have more than that on average (any call is right in any of these forms).
+// How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows where the sequences have up
+// to that many on average, else of sixteen, two to a team where they have more than that (any call is right in any of these forms).
 struct CaForm {
     int rows, tiles, teams, stages, threads;
 };
 static CaForm ca_form(int head_dim, int64_t n_seqs, int64_t n_rows, int group) {
-    if (n_rows * group <= n_seqs) return head_dim == 64 ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
+    const bool narrow = head_dim == 64;
+    if (n_rows * group <= n_seqs) return narrow ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
+    if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 8, 2, 512} : CaForm{8, 1, 4, 2, 256};
     const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;
-    return CaForm{16, tiles, teams, (head_dim == 64 ? 16 : 8) / teams, 256};
+    return CaForm{16, tiles, teams, (narrow ? 16 : 8) / teams, 256};
 }
 
 template <int DH, int ROWS, int DP>
@@ -1027,7 +1194,7 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     e = cudaLaunchKernelEx(&cfg, cached_attention_kernel<DH, ROWS, DP>, p);
     if (e != cudaSuccess) return e;
     cfg.dynamicSmemBytes = 0;
-    cfg.gridDim = dim3((unsigned)grid, (unsigned)(ROWS == 1 ? 1 : p.tiles * ROWS / 8));
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)(ROWS == 16 ? 2 * p.tiles : 1));
     cfg.blockDim = dim3(8 * DH / 4);
     e = cudaLaunchKernelEx(&cfg, cached_attention_join_kernel<DH, ROWS>, p);
     if (e != cudaSuccess) return e;
@@ -1084,8 +1251,9 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     p.per_group = (float)(1.0 / group);
     const cudaStream_t stream = (cudaStream_t)stream_;
     cudaError_t e;
-    if (f.rows == 1) e = dh == 64 ? launch_cached_attention<64, 1, 3>(p, f.threads, stream) : launch_cached_attention<128, 1, 3>(p, f.threads, stream);
-    else if (p.bf16) e = dh == 64 ? launch_cached_attention<64, 16, 2>(p, f.threads, stream) : launch_cached_attention<128, 16, 2>(p, f.threads, stream);
-    else e = dh == 64 ? launch_cached_attention<64, 16, 3>(p, f.threads, stream) : launch_cached_attention<128, 16, 3>(p, f.threads, stream);
+    auto launch = [&](auto narrow, auto wide) { return (dh == 64 ? narrow : wide)(p, f.threads, stream); };
+    if (f.rows == 1) e = launch(launch_cached_attention<64, 1, 3>, launch_cached_attention<128, 1, 3>);
+    else if (f.rows == 8) e = p.bf16 ? launch(launch_cached_attention<64, 8, 2>, launch_cached_attention<128, 8, 2>) : launch(launch_cached_attention<64, 8, 3>, launch_cached_attention<128, 8, 3>);
+    else e = p.bf16 ? launch(launch_cached_attention<64, 16, 2>, launch_cached_attention<128, 16, 2>) : launch(launch_cached_attention<64, 16, 3>, launch_cached_attention<128, 16, 3>);
     return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
 }
