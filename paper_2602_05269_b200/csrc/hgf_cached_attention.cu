@@ -31,7 +31,7 @@ constexpr int kCaMaxTeams = 8;      // teams of a CTA at most
 
 template <int DH, int ROWS>
 struct CaCfg {
-    static constexpr int WARPS = ROWS == 8 && DH == 64 ? 16 : ROWS == 1 && DH == 128 ? 4 : 8, THREADS = WARPS * 32;
+    static constexpr int WARPS = ROWS == 1 && DH == 128 ? 4 : 8, THREADS = WARPS * 32;
     static constexpr int UNIT = 3 * kCacheBlock * DH;            // bytes of a unit
     static constexpr int STAGE = (UNIT + 16 + 127) / 128 * 128;  // with the page's scales
     static constexpr int STAGES = DH == 64 ? 16 : 8;             // of all teams' rings
@@ -1166,7 +1166,7 @@ struct CaForm {
 static CaForm ca_form(int head_dim, int64_t n_seqs, int64_t n_rows, int group) {
     const bool narrow = head_dim == 64;
     if (n_rows * group <= n_seqs) return narrow ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
-    if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 8, 2, 512} : CaForm{8, 1, 4, 2, 256};
+    if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 4, 4, 256} : CaForm{8, 1, 4, 2, 256};
     const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;
     return CaForm{16, tiles, teams, (narrow ? 16 : 8) / teams, 256};
 }
