@@ -238,6 +238,10 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     __shared__ int page_ok[C::STAGES];       // a stage's page number was one
     __shared__ volatile int gave_up;         // a wait ran out: the others end, too
     __shared__ int unseen;                   // there are rows that see no token
+    __shared__ uint32_t odd_of[ROWS == 1 ? C::WARPS : C::WARPS / 2][2][DH];  // of a team's 64 open tokens, for each dim, those with a value that is not finite
+    __shared__ volatile int odd_at[kCaMaxTeams];  // the unit of a team's share in which there last were some
+    uint32_t (*odd)[DH] = odd_of[team];
+    if (tid < kCaMaxTeams) odd_at[tid] = -1;
     __shared__ CaItem first_item_of_cta, last_item_of[kCaMaxTeams];
     const uint32_t ring_a = dsmem_u32(ring), bars_a = dsmem_u32(bars) + team * stages * 8;
     if (tid < C::STAGES) dmbar_init(dsmem_u32(&bars[tid]), 1);
@@ -419,7 +423,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     uint32_t qd[ROWS == 1 ? 2 : ND][C::KT][ROWS == 16 ? 4 : 2];  // digits of q: ROWS = 1 for K1 and for K2, as right operand; else each digit, as right or left operand
     int sees_e[2] = {0, 0};                        // (ROWS = 8) tokens that rows 2 t and 2 t + 1 see
     float qs[NR];                                  // what a digit sum is worth, with 1 / sqrt(d) and log2 e
-    int sees[NR] = {}, sees_tile = 0, sees_all = 0, sees_item = 0;  // tokens that the lane's rows, any row, every row of the tile, any of the item sees
+    int sees[NR] = {}, sees_tile = 0, sees_all = 0, sees_item = 0, sees_first = 0;  // tokens that the lane's rows, any row, every row of the tile, any of the item, its first row sees
     const int my_stream = ROWS == 1 ? lane >> 4 : stream, limb = g & 3;
     const uint32_t limb_sel = 0x0040u + (uint32_t)((2 - limb) & 3) * 0x0011u;  // byte 2 - limb of two words
     const uint32_t limb_xor = limb == 0 ? 0x80808080u : 0u, limb_keep = limb == 3 ? 0u : 0xffffffffu;
@@ -477,6 +481,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
             return token < k.s.m ? first + token : 0;
         };
         sees_item = last_sees(k.s, k.tile);
+        sees_first = k.s.length - k.s.m + 1 + (p.group == 1 ? k.tile * tile_rows : k.tile * tile_rows / p.group);
         if (ROWS == 1) {
             sees[0] = sees_tile = sees_all = sees_of(0);
         } else if (ROWS == 8) {
@@ -549,7 +554,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        f += 1.17549435e-38f;  // (a page of zeros has f = 0, and what is masked has to stay at -inf)
+        f = count > 0 ? f + 1.17549435e-38f : 1.0f;  // (a page of zeros has f = 0, one that the row sees nothing of may have NaN, and what is masked has to stay at -inf)
         const float here = top * f, now = fmaxf(m[r], here), base = now == -INFINITY ? 0.0f : now;
         const float minus = here == -INFINITY ? 0.0f : -here;
         alpha = exp2_approx(m[r] - base);
@@ -569,6 +574,7 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
     CaCursor next;
     // A warp whose wait ran out computes and fetches no more, but takes its steps to the end: the others of its team meet it at their barrier.
     bool dead = false;
+    int odd_halves = 0;  // the item's open units that had values which are not finite taken out
     int stage = 0;
     for (long long u = u0; u < u1; ++u) {
         if (fresh) begin_item();
@@ -601,7 +607,34 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                 uint8_t *mine = ring + stage * C::STAGE;
                 if (leads)
                     for (int e = lane; e < (32 - rows) * (DH / 8); e += 32) *reinterpret_cast<uint4 *>(mine + 2 * 32 * DH * 2 + rows * DH * 2 + e * 16) = make_uint4(0, 0, 0, 0);
+                // Where a row sees some of these tokens and not all, zero times a value that is not finite would reach it: such values become zero here, and
+                // odd[.][dim] says of which tokens there were some.  (Looked for in a wide pass first: there are none.)
+                const bool some = sees_first < token0 + rows;
+                __nv_bfloat16 *values = reinterpret_cast<__nv_bfloat16 *>(mine + 2 * 32 * DH * 2);
+                if (some) {
+                    uint32_t top = 0;
+                    for (int e = member * 32 + lane; e < rows * (DH / 8); e += team_warps * 32) {
+                        const uint4 w = reinterpret_cast<const uint4 *>(values)[e];
+                        top = __vmaxu2(top, __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
+                    }
+                    if (max(top >> 16, top & 0xffffu) >= 0x7f80u) odd_at[team] = (int)(u - u0);
+                }
                 team_sync();
+                if (some && odd_at[team] == (int)(u - u0)) {
+                    const int half = k.unit - k.s.pages;
+                    odd_halves |= 1 << half;
+                    for (int dim = member * 32 + lane; dim < DH; dim += team_warps * 32) {
+                        uint32_t which = 0;
+                        for (int r = 0; r < rows; ++r) {
+                            __nv_bfloat16 &x = values[r * DH + cache_open_eight(r, dim >> 3) * 8 + (dim & 7)];
+                            if ((__bfloat16_as_ushort(x) & 0x7f80) != 0x7f80) continue;
+                            which |= 1u << r;
+                            x = __ushort_as_bfloat16(0);
+                        }
+                        odd[half][dim] = which;
+                    }
+                    team_sync();
+                }
             }
             if (ok && !open_unit && token0 < sees_tile) {
                 const float4 sc = *reinterpret_cast<const float4 *>(unit + C::UNIT);
@@ -846,13 +879,19 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     };
                     float d[2][4] = {};
 #pragma unroll
-                    for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n)
+                    for (int n = 0; n < (ROWS == 1 ? 2 : 1); ++n) {
+                        float one[2][4] = {};
 #pragma unroll
-                        for (int kt = 0; kt < DH / 16; ++kt) {
-                            const bool mine = ROWS == 8 || my_stream == n;
+                        for (int kt = 0; kt < DH / 16; ++kt)
 #pragma unroll
-                            for (int mt = 0; mt < 2; ++mt) mma_bf16(d[mt], k_eight(ROWS == 1 ? n : stream, mt, kt), mine ? qb[0][kt][0] : 0u, mine ? qb[0][kt][1] : 0u);
-                        }
+                            for (int mt = 0; mt < 2; ++mt) mma_bf16(one[mt], k_eight(ROWS == 1 ? n : stream, mt, kt), qb[0][kt][0], qb[0][kt][1]);
+                        // (ROWS = 1: of each stream's keys, its columns)
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (ROWS == 8 || t >> 1 == n) d[mt][e] = one[mt][e];
+                    }
 #pragma unroll
                     for (int mt = 0; mt < 2; ++mt) {
                         if (ROWS == 8) {
@@ -1093,6 +1132,22 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                             }
                     }
                 }
+            }
+            if (odd_halves) {  // what was left out of the sums, in their place
+                team_sync();
+                const float nan = __uint_as_float(0x7fc00000u);
+                for (int e = member * 32 + lane; e < tile_rows * DH; e += team_warps * 32) {
+                    const int r = e / DH, dim = e % DH, token = (k.tile * tile_rows + r) / p.group, seen = k.s.length - k.s.m + 1 + token - 64 * k.s.pages;
+                    bool bad = false;
+                    for (int half = 0; half < 2; ++half)
+                        if (odd_halves >> half & 1 && seen > 32 * half) bad |= (odd[half][dim] & 0xffffffffu >> (32 - min(seen - 32 * half, 32))) != 0;
+                    if (token >= k.s.m || !bad) continue;
+                    float *row = my_parts + (first_item ? 0 : part_floats) + r * C::PART + 4;
+                    if (whole) ca_write(p, it, k.tile * tile_rows + r, DH, dim, nan);
+                    else row[dim] = row[DH + dim] = nan;
+                }
+                team_sync();
+                odd_halves = 0;
             }
             first_item = false;
         }

@@ -459,6 +459,48 @@ def test_rows_before_a_block_that_is_not_finite(hgf):
     assert np.isfinite(out[100:102]).all() and not np.isfinite(out[110:120, 9]).any() and np.isfinite(np.delete(out[110:120], 9, 1)).all()   # tokens 30 .. 49
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("group", [1, 3])
+@pytest.mark.parametrize("a_sequence", [1, 8, 16, 32])
+def test_what_is_not_finite_stays_with_the_rows_that_see_it(hgf, dh, group, a_sequence):
+    """Rows on both sides of a page whose K scale is NaN, of an open value and of an open key that are not finite; queries that are not, of rows without tokens.
+
+    `a_sequence`: rows times heads of a group that a sequence has on average, with sequences that have none."""
+    L, m = 148, 100
+    p = Pair(hgf, 2, dh, n_pages=20, n_slots=2)
+
+    def change(k, v):
+        k.reshape(-1, 2, 2, dh)[70, 0, 0, 5] = 0x7fc0     # block 1 of head 0, K1
+        v.reshape(-1, 2, dh)[135, 1, 7] = 0xff80          # head 1, open: V, and K2 below
+        k.reshape(-1, 2, 2, dh)[140, 1, 1, 9] = 0x7f80
+
+    p.reserve([0, 1], [L, 70])
+    p.append([0], [L], change=change)
+    p.append([1], [70])
+    idle = -(-m * group // a_sequence) - 1
+    for n, slot in ((m, 0), (72, 1)):
+        q = rows(p.rng, m, 2 * 2 * group * dh)
+        if slot == 1:
+            q[:2] = 0x7fc0
+        for flat in (False, True):
+            out = torch.full((m, 2 * group * dh), 5.0, dtype=torch.bfloat16 if flat else torch.float32, device="cuda")
+            hgf.diff_attention_cached(p.cache, bf16(q), ints([slot] + [-1] * idle), ints([0] + [n] * (idle + 1)), 0.5, out=out,
+                                      flags=hgf.FLAG_OUT_BF16 if flat else 0)
+            out = out.float().cpu().numpy().reshape(m, 2, group, dh)
+            assert (out[n:] == 5.0).all()
+            if slot == 1:
+                assert (out[:2] == 0.0).all() and np.isfinite(out[:n]).all()
+                continue
+            sees, bad = L - m + 1 + np.arange(m), ~np.isfinite(out)
+            assert (bad[:, 0].all((1, 2)) == (sees > 64)).all() and not bad[sees <= 64, 0].any()
+            assert not bad[sees <= 135, 1].any()
+            some = (sees > 135) & (sees <= 140)
+            assert bad[some, 1, :, 7].all() and not np.delete(bad[some, 1], 7, 2).any()
+            # the open key's score is infinity with the sign of the query there: no weight, or a NaN
+            nan = (bf16_bits_to_f32(q).reshape(m, 2, 2, group, dh)[:, 1, 1, :, 9] >= 0)[sees > 140]
+            assert bad[sees > 140, 1, :, 7].all() and (np.delete(bad[sees > 140, 1], 7, 2) == nan[:, :, None]).all()
+
+
 def test_agrees_with_the_definition_while_nothing_is_quantised(hgf):
     """Up to 63 tokens the cache holds bf16, so the attention is that of whole sequences."""
     H, dh, n = 3, 64, 63
