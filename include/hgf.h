@@ -444,10 +444,11 @@ hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slots, int64_t 
  *   out  [n_rows][n_heads * head_dim]      fp32, or bfloat16 with HGF_FLAG_OUT_BF16
  *   workspace  hgf_cached_workspace_bytes(...) bytes, 256-byte aligned; scratch, which calls that may overlap on the device do not share
  * Scores come from q to 2^-22 of the row's largest magnitude; probabilities enter the second product to 2^-24 of the largest in their page (of several
- * rows or shared heads with bf16 output: 2^-17); all sums are exact integers or fp32.
+ * rows or shared heads with bf16 output: 2^-17, or 2^-16 of themselves); all sums are exact integers or fp32.
  * A query row, a block or an open value of V that is not finite gives outputs that are not finite in the rows that see tokens, it or one of its tokens (an
  * open value in its dim only), and in no others.  An infinite score of an open key is no weight if it is negative, else NaN.
- * (Scores are expected within binary32's range, and the largest |v| of a block at 0 or above 2^-90: below, the lower digits of its probabilities are lost.)
+ * (Scores are expected within binary32's range, and the largest |v| of a block at 0 or between 2^-90 and 2^100: outside, the lower digits
+ * of its probabilities are lost, or sums pass that range.)
  */
 size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads);
 hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const void *q, int64_t n_rows, int32_t n_heads, const int32_t *slots,

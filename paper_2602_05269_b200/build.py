@@ -30,7 +30,7 @@ def module_path() -> str:
 
 
 def _deps(src: str):
-    return [src, os.path.join(CSRC, "hgf_common.cuh"), os.path.join(CSRC, "hgf_tc.cuh"), os.path.join(CSRC, "hgf_warp.cuh"), os.path.join(CSRC, "hgf_cache.cuh"), os.path.join(HERE, "..", "include", "hgf.h")]
+    return [src, os.path.join(CSRC, "hgf_common.cuh"), os.path.join(CSRC, "hgf_tc.cuh"), os.path.join(CSRC, "hgf_warp.cuh"), os.path.join(CSRC, "hgf_cache.cuh"), os.path.join(CSRC, "hgf_cached_attention_tc.cuh"), os.path.join(HERE, "..", "include", "hgf.h")]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -14,13 +14,15 @@
 // The accumulators start at the bits of 1.5 * 2^23, so that a sum, below 2^22 in magnitude, is a float after one subtraction: I2F runs at an eighth
 // of the FMA rate and bounded the kernel.  The open tokens' bf16 go through bf16 products, with the probabilities as sums of three bf16.
 //
-// Three forms.  ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.  There
+// Four forms.  Many rows with bf16 output are tcgen05 products (hgf_cached_attention_tc.cuh).  Here ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.  There
 // and with ROWS = 8, a few tokens or heads that share K and V, the codes are the left operand, tokens (or dims) as its rows; eight query rows are the
 // columns of a product for each digit, and a team is a warp for each stream.  ROWS = 16, for more: sixteen query rows are the left operand and the
 // codes the right one (a lane's sixteen bytes are the same either way round); a warp takes one stream of one tile of sixteen rows, and a team is the
 // warps of one or two tiles, so that a page that is read once serves up to 32 rows.  There the columns of the scores' products are the page's tokens in
 // such an order that a lane gets four neighbouring tokens of its rows: the probabilities' digits are then in place for the second product, where
 // ROWS = 8 turns the scores through shared memory.
+#include <algorithm>
+
 #include "hgf_cache.cuh"
 #include "hgf_warp.cuh"
 
@@ -219,6 +221,10 @@ __device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int
         }
     }
 }
+
+}  // namespace hgf
+#include "hgf_cached_attention_tc.cuh"
+namespace hgf {
 
 // DP: digits of the probabilities.
 template <int DH, int ROWS, int DP>
@@ -1214,24 +1220,26 @@ __global__ void __launch_bounds__(8 * DH / 4) cached_attention_join_kernel(CaPar
 }
 
 // How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows where the sequences have up
-// to that many on average, else of sixteen, two to a team where they have more than that (any call is right in any of these forms).
+// to that many on average, else of sixteen, two to a team where they have more than that; with bf16 output of 128 where they have more than 80 (any call is right
+// in any of these forms).
 struct CaForm {
     int rows, tiles, teams, stages, threads;
 };
-static CaForm ca_form(int head_dim, int64_t n_seqs, int64_t n_rows, int group) {
+static CaForm ca_form(int head_dim, int64_t n_seqs, int64_t n_rows, int group, bool bf16) {
     const bool narrow = head_dim == 64;
+    // (100 rows of 1000 tokens, 8 sequences, 16 heads of 64: 49.8 us here, 49.8 in tiles of sixteen; 256 rows of 6000 tokens 74 and 145; but 64 rows of 4096 tokens,
+    // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty)
+    if (bf16 && n_rows * group > 80 * n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
     if (n_rows * group <= n_seqs) return narrow ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
     if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 4, 4, 256} : CaForm{8, 1, 4, 2, 256};
     const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;
     return CaForm{16, tiles, teams, (narrow ? 16 : 8) / teams, 256};
 }
 
-template <int DH, int ROWS, int DP>
-static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaStream_t stream) {
-    using C = CaCfg<DH, ROWS>;
-    static_assert(C::SMEM <= 226 * 1024, "shared memory of a CTA");
-    static std::atomic<unsigned long long> attr_done{0};
-    cudaError_t e = ensure_dynamic_smem(cached_attention_kernel<DH, ROWS, DP>, C::SMEM, attr_done);
+// `kernel` and the joining of its parts, which are of tiles of p.tiles * ROWS rows.
+template <int DH, int ROWS>
+static cudaError_t launch_with_join(void (*kernel)(CaParams), size_t smem, std::atomic<unsigned long long> &attr_done, const CaParams &p, int threads, cudaStream_t stream) {
+    cudaError_t e = ensure_dynamic_smem(kernel, smem, attr_done);
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;
@@ -1245,8 +1253,8 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     cfg.stream = stream;
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = C::SMEM;
-    e = cudaLaunchKernelEx(&cfg, cached_attention_kernel<DH, ROWS, DP>, p);
+    cfg.dynamicSmemBytes = smem;
+    e = cudaLaunchKernelEx(&cfg, kernel, p);
     if (e != cudaSuccess) return e;
     cfg.dynamicSmemBytes = 0;
     cfg.gridDim = dim3((unsigned)grid, (unsigned)(ROWS == 16 ? 2 * p.tiles : 1));
@@ -1255,6 +1263,18 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     if (e != cudaSuccess) return e;
     count_launch(2);
     return cudaSuccess;
+}
+template <int DH, int ROWS, int DP>
+static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaStream_t stream) {
+    using C = CaCfg<DH, ROWS>;
+    static_assert(C::SMEM <= 226 * 1024, "shared memory of a CTA");
+    static std::atomic<unsigned long long> attr_done{0};
+    return launch_with_join<DH, ROWS>(cached_attention_kernel<DH, ROWS, DP>, C::SMEM, attr_done, p, threads, stream);
+}
+template <int DH>
+static cudaError_t launch_cached_attention_tc(const CaParams &p, int threads, cudaStream_t stream) {
+    static std::atomic<unsigned long long> attr_done{0};
+    return launch_with_join<DH, 16>(cached_attention_tc_kernel<DH>, CtCfg<DH>::SMEM, attr_done, p, threads, stream);
 }
 
 static size_t ca_items_bytes() { return align_up((size_t)kCaMaxSms * 2 * sizeof(int4), 256); }
@@ -1269,7 +1289,9 @@ using namespace hgf;
 
 extern "C" size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads) {
     if (!cache || (cache->head_dim != 64 && cache->head_dim != 128) || cache->n_heads <= 0 || n_heads <= 0 || n_rows <= 0 || n_seqs <= 0) return 256;
-    return ca_workspace(cache->head_dim, ca_form(cache->head_dim, n_seqs, n_rows, n_heads / cache->n_heads));
+    size_t bytes = 0;  // (of either type of output)
+    for (const bool bf16 : {false, true}) bytes = std::max(bytes, ca_workspace(cache->head_dim, ca_form(cache->head_dim, n_seqs, n_rows, n_heads / cache->n_heads, bf16)));
+    return bytes;
 }
 
 extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const void *q, int64_t n_rows, int32_t n_heads, const int32_t *slots,
@@ -1281,7 +1303,7 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     if (n_heads % cache->n_heads || n_heads > 65535 || n_rows > (1 << 24) || n_rows * (n_heads / cache->n_heads) > 0x3fffffffll) return HGF_ERR_UNSUPPORTED_SHAPE;
     if (((uintptr_t)q | (uintptr_t)out) & 15u) return HGF_ERR_MISALIGNED;
     const int group = n_heads / cache->n_heads, dh = cache->head_dim;
-    const CaForm f = ca_form(dh, n_seqs, n_rows, group);
+    const CaForm f = ca_form(dh, n_seqs, n_rows, group, (flags & HGF_FLAG_OUT_BF16) != 0);
     if (!workspace || workspace_bytes < ca_workspace(dh, f)) return HGF_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255u) return HGF_ERR_MISALIGNED;
     p.q = (const __nv_bfloat16 *)q;
@@ -1307,7 +1329,8 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     const cudaStream_t stream = (cudaStream_t)stream_;
     cudaError_t e;
     auto launch = [&](auto narrow, auto wide) { return (dh == 64 ? narrow : wide)(p, f.threads, stream); };
-    if (f.rows == 1) e = launch(launch_cached_attention<64, 1, 3>, launch_cached_attention<128, 1, 3>);
+    if (!f.stages) e = launch(launch_cached_attention_tc<64>, launch_cached_attention_tc<128>);
+    else if (f.rows == 1) e = launch(launch_cached_attention<64, 1, 3>, launch_cached_attention<128, 1, 3>);
     else if (f.rows == 8) e = p.bf16 ? launch(launch_cached_attention<64, 8, 2>, launch_cached_attention<128, 8, 2>) : launch(launch_cached_attention<64, 8, 3>, launch_cached_attention<128, 8, 3>);
     else e = p.bf16 ? launch(launch_cached_attention<64, 16, 2>, launch_cached_attention<128, 16, 2>) : launch(launch_cached_attention<64, 16, 3>, launch_cached_attention<128, 16, 3>);
     return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;

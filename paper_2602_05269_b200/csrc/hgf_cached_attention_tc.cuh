@@ -1,0 +1,651 @@
+// Cached differential attention of many rows a sequence with bf16 output, on tcgen05 (included by hgf_cached_attention.cu).
+//
+// An item is 128 rows (row: token times heads of the group) of a sequence and K/V head, a step one page of 64 tokens (the open tokens are one step more).
+// All items' steps are one sequence, dealt in equal shares to one CTA an SM: a CTA walks segments, each the steps of one item that lie in its share; a
+// segment that is not its whole item leaves maximum, sum and sums of values in the workspace, and the joining kernel adds such parts in the order of the
+// tokens.  Within a CTA:
+//   warp 14      brings pages into a ring of shared memory, a bulk copy each
+//   warps 0-3    write query tiles, and the pages' codes as bf16 (exact: a code has seven bits and a sign) into rings of K and of V, as the operands' layouts
+//                have them; V lies transposed in a page, so both operands have their contraction index contiguous
+//   warps 12, 13 issue the products of a stream each: S = Q K^T of the codes, and O += P V of the codes
+//   warps 4-7    softmax of stream 1, warps 8-11 of stream 2: a thread owns a row; scores times the page's scale of K, the page's scale of V in the exponent
+// A probability enters the second product as a sum of two bf16, off by 2^-16 of itself at most, beside the output's 2^-8; all sums are fp32.
+//
+// What bounds it is the issue of instructions: 1500 a step and scheduler (54 % of the slots, with the instruction cache behind another fifth of the
+// waits), of them 340 in each softmax warp's 64 x 32 probabilities and 350 in a converting warp; tensor pipe 26 %, exponentials 34 %.
+// Measured, 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 145 us with the int8 form, 74 us here; 8 K/V heads with four query heads each, 30000 tokens,
+// 128 rows: 438 and 172 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 107 us.  Steps: codes from global memory into registers 81 us (of the
+// first), with the bulk copies and segments kept in registers 85 (spills went to the L2 cache), segments in shared memory 76, V's scale in the exponent 74; two
+// converting warps of a larger share of registers 99.
+#pragma once
+#include "hgf_tc.cuh"
+
+namespace hgf {
+
+constexpr int kCtRows = 128, kCtThreads = 480;
+constexpr float kCtSlack = 8.0f, kCtNone = -1e30f;  // (a maximum of nothing)
+
+template <int DH>
+struct CtCfg {
+    static constexpr int NBLK = DH / 64, KST = DH == 64 ? 3 : 2, GST = DH == 64 ? 4 : 2, NQ = DH == 64 ? 2 : 1, NO = DH == 64 ? 2 : 1;  // stages of the operands, of the pages; buffers of query tiles, of O_1 and O_2
+    static constexpr int Q_BYTES = NBLK * kCtRows * 128, K_BYTES = NBLK * kCacheBlock * 128, V_BYTES = DH * 128;
+    static constexpr int OFF_K = NQ * 2 * Q_BYTES, OFF_V = OFF_K + KST * 2 * K_BYTES, OFF_G = OFF_V + KST * V_BYTES,
+                         UNIT = 3 * kCacheBlock * DH, G_BYTES = (UNIT + 16 + 127) / 128 * 128, OFF_BAR = OFF_G + GST * G_BYTES;
+    static constexpr int BAR_QFULL = 0, BAR_QEMPTY = 2, BAR_OEMPTY = 4, BAR_L = 6, BAR_END = 8, BAR_KFULL = 10, BAR_KEMPTY = BAR_KFULL + KST, BAR_VFULL = BAR_KEMPTY + KST,
+                         BAR_VEMPTY = BAR_VFULL + KST, BAR_SFULL = BAR_VEMPTY + KST /* [stream][buffer] */, BAR_PFULL = BAR_SFULL + 4, BAR_GFULL = BAR_PFULL + 4, BAR_GEMPTY = BAR_GFULL + GST,
+                         BAR_COUNT = BAR_GEMPTY + GST;
+    static constexpr int OFF_SCALES = OFF_BAR + 384;             // [8] float4: K1, K2, V of step g % 8
+    static constexpr int OFF_ODD = OFF_SCALES + 128;             // [8][4] ints: of segment % 8, a warp found open values that are not finite
+    static constexpr int OFF_L = OFF_ODD + 128;                  // [2][2][128] floats
+    static constexpr int OFF_PREFIX = OFF_L + 2 * 2 * kCtRows * 4;
+    static constexpr int SMEM = OFF_PREFIX + (kCacheMaxSeqs + 2) * 8 + 1024;
+    static constexpr int COL_S = 0, COL_O = 4 * kCacheBlock;     // scores: + (2 stream + buffer) 64; O: + (2 buffer + stream) DH
+    static constexpr int PART = 4 + 2 * DH;
+    static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCacheBlock >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
+    static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
+    static_assert(BAR_COUNT * 8 + 16 <= 384 && COL_O + NO * 2 * DH <= 512 && SMEM <= 226 * 1024, "barriers, tensor and shared memory");
+};
+
+__device__ __forceinline__ CaSeq ct_sequence(const CaParams &p, int i) {
+    CaSeq s = ca_sequence(p, kCtRows, i);
+    s.units = s.pages + ((s.length & 63) != 0);
+    return s;
+}
+// The steps unit .. end - 1 of an item: those of the share's next segment.
+struct CtSegment {
+    CaSeq s;
+    int seq, tile, head, unit, end, visible;  // visible: steps that a row of the tile sees something of
+    long long u;                              // of `unit`
+    __device__ __forceinline__ int stop() const { return min(end, visible); }
+    __device__ __forceinline__ bool whole() const { return unit == 0 && end == s.units; }
+    __device__ __forceinline__ void bound(const CaParams &p, long long u1) {
+        end = (int)min((long long)s.units, unit + (u1 - u));
+        const int at = (tile + 1) * kCtRows - 1, last = s.length - s.m + 1 + min(s.m - 1, p.group == 1 ? at : at / p.group);
+        visible = (last + 63) >> 6;
+    }
+    __device__ __forceinline__ void first(const CaParams &p, const long long *prefix, long long u0, long long u1) {
+        int lo = 0, hi = p.n_seqs - 1;
+        while (lo < hi) {  // the last sequence that begins at or before u0 (of empty ones at the same place the last, which is not empty)
+            const int mid = (lo + hi + 1) >> 1;
+            if (prefix[mid] <= u0) lo = mid; else hi = mid - 1;
+        }
+        u = u0;
+        seq = lo;
+        s = ct_sequence(p, lo);
+        const long long in = u0 - prefix[lo], item = in / s.units;
+        unit = (int)(in - item * s.units);
+        tile = (int)(item / p.c.H);
+        head = (int)(item - (long long)tile * p.c.H);
+        tile += s.tile0;
+        bound(p, u1);
+    }
+    __device__ __forceinline__ bool next(const CaParams &p, const long long *prefix, long long u1) {
+        u += end - unit;
+        if (u >= u1) return false;
+        unit = 0;
+        if (++head == p.c.H) {
+            head = 0;
+            if (++tile == s.tiles) {
+                do ++seq; while (seq < p.n_seqs - 1 && prefix[seq + 1] == prefix[seq]);
+                s = ct_sequence(p, seq);
+                tile = s.tile0;
+            }
+        }
+        bound(p, u1);
+        return true;
+    }
+};
+
+// Four codes as bf16: of a byte c, 128 + its low seven bits less 128 or, for a negative one, 256.
+__device__ __forceinline__ uint2 ct_bf16(uint32_t codes) {
+    const uint32_t w[2] = {__byte_perm(codes, 0x43434343u, 0x4140), __byte_perm(codes, 0x43434343u, 0x4342)};
+    uint32_t r[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t x = w[i] & 0xff7fff7fu, y = w[i] & 0xff80ff80u;
+        const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+        r[i] = *reinterpret_cast<const uint32_t *>(&d);
+    }
+    return make_uint2(r[0], r[1]);
+}
+
+__device__ __forceinline__ float lg2_approx(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaParams p) {
+    using C = CtCfg<DH>;
+    constexpr int KV = kCacheBlock;
+    extern __shared__ uint8_t ct_smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)ct_smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t sbase = smem_u32(smem), bar0 = sbase + C::OFF_BAR;
+    auto bar = [&](int i) { return bar0 + 8u * i; };
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::OFF_BAR + C::BAR_COUNT * 8);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::OFF_BAR + C::BAR_COUNT * 8 + 4);
+    __shared__ volatile int page_ok[C::GST];
+    // A warp's segment lies in shared memory, where its first lane moves it on: in registers it costs every role sixteen of them, and what they spilled went
+    // through the L2 cache, since the L1 has no room beside so much shared memory.
+    __shared__ CtSegment segments[kCtThreads / 32 + 2];
+    int *unseen = reinterpret_cast<int *>(smem + C::OFF_BAR + C::BAR_COUNT * 8 + 8);
+    float4 *scales = reinterpret_cast<float4 *>(smem + C::OFF_SCALES);
+    volatile int *odd = reinterpret_cast<volatile int *>(smem + C::OFF_ODD);
+    float *s_l = reinterpret_cast<float *>(smem + C::OFF_L);
+    long long *prefix = reinterpret_cast<long long *>(smem + C::OFF_PREFIX);
+    __shared__ long long wide[kCtThreads / 32];
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, H = p.c.H;
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(C::BAR_QFULL + i), 4);
+            mbar_init(bar(C::BAR_QEMPTY + i), 2);  // a commit from each issuer
+            mbar_init(bar(C::BAR_OEMPTY + i), 8);
+            mbar_init(bar(C::BAR_L + i), 8);
+            mbar_init(bar(C::BAR_END + i), 1);
+        }
+        for (int s = 0; s < C::KST; ++s) {
+            mbar_init(bar(C::BAR_KFULL + s), 4);
+            mbar_init(bar(C::BAR_KEMPTY + s), 2);
+            mbar_init(bar(C::BAR_VFULL + s), 4);
+            mbar_init(bar(C::BAR_VEMPTY + s), 2);
+        }
+        for (int s = 0; s < C::GST; ++s) {
+            mbar_init(bar(C::BAR_GFULL + s), 1);
+            mbar_init(bar(C::BAR_GEMPTY + s), 4);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(bar(C::BAR_SFULL + i), 1);
+            mbar_init(bar(C::BAR_PFULL + i), 4);
+        }
+        *abort_flag = 0;
+        *unseen = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        fence_proxy_async();
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    pdl_wait();
+    pdl_launch_dependents();
+
+    // ---- plan, by every CTA for itself
+    if (tid == 0) p.items[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+    long long total = 0;
+    for (int i0 = 0; i0 < p.n_seqs; i0 += kCtThreads) {
+        const int i = i0 + tid;
+        long long mine = 0;
+        if (i < p.n_seqs) {
+            const CaSeq s = ct_sequence(p, i);
+            if (blockIdx.x == 0 && s.slot == -2) atomicOr(p.status, kStatusCache);
+            if (s.m > s.length) *unseen = 1;
+            mine = (long long)(s.tiles - s.tile0) * H * s.units;
+        }
+        long long sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 31) wide[warp] = sum;
+        __syncthreads();
+        long long before = total;
+        for (int w = 0; w < kCtThreads / 32; ++w) {
+            if (w < warp) before += wide[w];
+            total += wide[w];
+        }
+        if (i < p.n_seqs) prefix[i] = before + sum - mine;
+        __syncthreads();
+    }
+    if (tid == 0) prefix[p.n_seqs] = total;
+    __syncthreads();
+    if (*unseen) {  // rows that see no token
+        const int width = H * p.group * DH;
+        for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x) {
+            const CaSeq s = ct_sequence(p, i);
+            const size_t at = (size_t)s.row0 * width, n = (size_t)max(s.m - s.length, 0) * width;
+            for (size_t e = 8 * tid; e < n; e += 8 * kCtThreads) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
+        }
+    }
+    const int ctas = (int)min((long long)gridDim.x, total);
+    const bool works = (int)blockIdx.x < ctas;
+    const long long c0 = works ? ca_share(total, blockIdx.x, ctas) : 0, c1 = works ? ca_share(total, blockIdx.x + 1, ctas) : 0;
+
+    auto first_segment = [&](CtSegment &s) {
+        if (lane == 0) s.first(p, prefix, c0, c1);
+        __syncwarp();
+    };
+    auto next_segment = [&](CtSegment &s) {
+        int more = 0;
+        __syncwarp();
+        if (lane == 0) more = s.next(p, prefix, c1);
+        more = __shfl_sync(0xffffffffu, more, 0);
+        __syncwarp();
+        return more != 0;
+    };
+    if (works && warp < 4) {
+        // ------------------------------------------------------------------ queries, keys and values into shared memory
+        const int g4 = lane >> 2, t = lane & 3;
+        auto wait = [&](int i, uint32_t par, unsigned int code) { return __all_sync(0xffffffffu, mbar_wait(bar(i), par, abort_flag, p.status, code)) != 0; };
+        auto there = [&](int i) {  // what this warp wrote is there for the products
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(i));
+        };
+        constexpr int KN = DH / 16, VN = DH / 32;  // tiles of 16 x 32 codes of a warp: of K (both streams 4 KT), of V
+        bool ok = true;
+        int ks = 0, vs = 0, gs = 0, qb = 0, g = 0, segment = 0;
+        uint32_t kph = 1, vph = 1, gph = 0, qph = 1;
+        CtSegment &seg = segments[warp];
+        first_segment(seg);
+        bool more = true;
+        for (; ok && more; more = next_segment(seg)) {
+            const int stop = seg.stop(), first = seg.unit, pages = seg.s.pages;
+            if (first >= stop) continue;
+            // sixteen codes of a tile: four neighbouring ones of two rows and two places
+            auto store = [&](uint8_t *rows, int row0, int chunk0, const uint4 &x) {
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row0 + g4 + 8 * (i & 1), chunk = chunk0 + 2 * (i >> 1) + (t >> 1);
+                    *reinterpret_cast<uint2 *>(rows + row * 128 + ((chunk ^ g4) << 4) + (t & 1) * 8) = ct_bf16(w[i]);
+                }
+            };
+            if (!(ok = wait(C::BAR_QEMPTY + qb, qph, 0xb10u + qb))) break;
+            {
+                const int at = seg.tile * kCtRows + tid, token = p.group == 1 ? at : at / p.group;
+                const bool in = token < seg.s.m;
+                const size_t row = (size_t)(seg.s.row0 + (in ? token : 0)) * 2 * H * p.group + seg.head * p.group + (in ? at - token * p.group : 0);
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (row + (size_t)st * H * p.group) * DH);
+                    uint8_t *dst = smem + (2 * qb + st) * C::Q_BYTES + tid * 128;
+                    uint4 v[DH / 8];
+#pragma unroll
+                    for (int c = 0; c < DH / 8; ++c) v[c] = in ? src[c] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int c = 0; c < DH / 8; ++c) *reinterpret_cast<uint4 *>(dst + (c >> 3) * kCtRows * 128 + (((c & 7) ^ (tid & 7)) << 4)) = v[c];
+                }
+                there(C::BAR_QFULL + qb);
+                if (++qb == C::NQ) { qb = 0; qph ^= 1u; }
+            }
+            for (int j = first; j < stop; ++j, ++g) {
+                const bool page = j < pages;
+                const int rows = page ? KV : seg.s.length & 63;
+                const uint4 *open = reinterpret_cast<const uint4 *>(p.c.open + ((size_t)seg.s.slot * H + seg.head) * 3 * KV * DH);
+                if (page && !(ok = wait(C::BAR_GFULL + gs, gph, 0xb18u + gs))) break;
+                const uint4 *codes = reinterpret_cast<const uint4 *>(smem + C::OFF_G + gs * C::G_BYTES) + lane;
+                const bool good = page && page_ok[gs];
+                if (!(ok = wait(C::BAR_KEMPTY + ks, kph, 0xb20u + ks))) break;
+                uint8_t *k = smem + C::OFF_K + ks * 2 * C::K_BYTES;
+                if (page) {
+#pragma unroll
+                    for (int i = 0; i < KN; ++i) {  // tile n of stream n / (4 KT): sixteen tokens, 32 dims
+                        const int n = 4 * i + warp, stream = n / (DH / 8), mt = n % (DH / 8) / (DH / 32), kt = n % (DH / 32);
+                        store(k + stream * C::K_BYTES + (kt >> 1) * KV * 128, mt * 16, (kt & 1) * 4, good ? codes[n * 32] : make_uint4(0, 0, 0, 0));
+                    }
+                } else {  // (the rows' eights lie in the places that the operand's layout gives them)
+#pragma unroll 4
+                    for (int e = tid; e < 2 * KV * DH / 8; e += 128) {
+                        const int stream = e / (KV * DH / 8), r = e / (DH / 8) % KV, c = e % (DH / 8);
+                        *reinterpret_cast<uint4 *>(k + stream * C::K_BYTES + (c >> 3) * KV * 128 + r * 128 + ((c & 7) << 4)) = r < rows ? open[e] : make_uint4(0, 0, 0, 0);
+                    }
+                }
+                if (tid == 0) scales[g & 7] = !page ? make_float4(1.0f, 1.0f, 1.0f, 0.0f) : good ? *reinterpret_cast<const float4 *>(smem + C::OFF_G + gs * C::G_BYTES + C::UNIT) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                there(C::BAR_KFULL + ks);
+                if (++ks == C::KST) { ks = 0; kph ^= 1u; }
+                if (!(ok = wait(C::BAR_VEMPTY + vs, vph, 0xb30u + vs))) break;
+                uint8_t *v = smem + C::OFF_V + vs * C::V_BYTES;
+                if (page) {
+#pragma unroll
+                    for (int i = 0; i < VN; ++i) {  // sixteen dims, 32 tokens
+                        const int n = 4 * i + warp;
+                        store(v, (n >> 1) * 16, (n & 1) * 4, good ? codes[(4 * KN + n) * 32] : make_uint4(0, 0, 0, 0));
+                    }
+                } else {  // values that are not finite become zero here, and the rows that see them are told at the end: zero times such a value is no zero
+                    bool some = false;
+                    const int r = tid & 63;
+#pragma unroll 4
+                    for (int c = tid >> 6; c < DH / 8; c += 2) {
+                        const uint4 x = r < rows ? open[2 * KV * DH / 8 + r * (DH / 8) + cache_open_eight(r, c)] : make_uint4(0, 0, 0, 0);
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            uint32_t bits = w[q >> 1] >> (16 * (q & 1)) & 0xffffu;
+                            if ((bits & 0x7f80u) == 0x7f80u) {
+                                bits = 0;
+                                some = true;
+                            }
+                            *reinterpret_cast<uint16_t *>(v + (8 * c + q) * 128 + (((r >> 3) ^ q) << 4) + (r & 7) * 2) = (uint16_t)bits;
+                        }
+                    }
+                    some = __any_sync(0xffffffffu, some);
+                    if (lane == 0) odd[4 * (segment & 7) + warp] = some;
+                }
+                if (page) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(C::BAR_GEMPTY + gs));
+                    if (++gs == C::GST) { gs = 0; gph ^= 1u; }
+                }
+                there(C::BAR_VFULL + vs);
+                if (++vs == C::KST) { vs = 0; vph ^= 1u; }
+            }
+            ++segment;
+        }
+    } else if (works && warp == 14) {
+        // ------------------------------------------------------------------ pages into shared memory
+        uint32_t issued[C::GST] = {};
+        bool ok = true, more = true;
+        int gs = 0, pages32 = 0;
+        uint32_t gph = 1;
+        CtSegment &seg = segments[warp];
+        first_segment(seg);
+        for (; ok && more; more = next_segment(seg)) {
+            const int first = seg.unit, pages = seg.s.pages, head = seg.head, stop = min(seg.stop(), pages);
+            const int32_t *table = p.c.table + (size_t)seg.s.slot * p.c.max_pages;
+            for (int j = first; j < stop; ++j) {
+                if (j == first || (j & 31) == 0) pages32 = (j & ~31) + lane < pages ? table[(j & ~31) + lane] : 0;
+                const int page = __shfl_sync(0xffffffffu, pages32, j & 31);
+                const bool good = page >= 0 && page < p.c.n_pages;
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_GEMPTY + gs), gph, abort_flag, p.status, 0xb90u + gs)) != 0;
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t full = bar(C::BAR_GFULL + gs), dst = sbase + C::OFF_G + gs * C::G_BYTES;
+                    const size_t at = (size_t)(good ? page : 0) * H + head;
+                    page_ok[gs] = good;
+                    if (good) {
+                        mbar_arrive_expect_tx(full, C::UNIT + 16);
+                        bulk_load_1d(dst, p.c.codes + at * C::UNIT, C::UNIT, full);
+                        bulk_load_1d(dst + C::UNIT, p.c.scales + at, 16, full);
+                    } else {
+                        atomicOr(p.status, kStatusCache);
+                        mbar_arrive(full);
+                    }
+                }
+                ++issued[gs];
+                if (++gs == C::GST) { gs = 0; gph ^= 1u; }
+            }
+        }
+        // never leave with a copy in flight
+        for (int q = 0; q < C::GST; ++q)
+            if (issued[q])
+                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(bar(C::BAR_GFULL + q), (issued[q] - 1u) & 1u); ++i) {}
+    } else if (works && (warp == 12 || warp == 13)) {
+        // ------------------------------------------------------------------ the products of a stream
+        const int st = warp - 12;
+        auto wait = [&](int i, uint32_t par, unsigned int code) { return __all_sync(0xffffffffu, mbar_wait_poll(bar(i), par, abort_flag, p.status, code)) != 0; };
+        const uint64_t q_desc = make_sw128_desc(sbase + st * C::Q_BYTES), k_desc = make_sw128_desc(sbase + C::OFF_K + st * C::K_BYTES), v_desc = make_sw128_desc(sbase + C::OFF_V);
+        const uint32_t s_col = tmem_base + C::COL_S + 2 * st * KV;
+        // The scores run two steps ahead of P V: the products execute in order, so P of a step has been read when the scores of two steps on replace it.
+        bool ok = true, s_more = true, p_more = true;
+        int ks = 0, vs = 0, sqb = 0, pob = 0, g = 0, sj = 0;
+        uint32_t kph = 0, vph = 0, sqph = 0, poph = 1;
+        CtSegment &sseg = segments[warp], &pseg = segments[warp - 12 + kCtThreads / 32];
+        int s_first = 0, s_stop = 0, p_first = 0, p_stop = 0;
+        auto full = [&](CtSegment &s, bool &more, int &first, int &stop) {  // on to a segment with steps
+            while (more && s.unit >= s.stop()) more = next_segment(s);
+            first = s.unit;
+            stop = s.stop();
+        };
+        first_segment(sseg);
+        first_segment(pseg);
+        full(sseg, s_more, s_first, s_stop);
+        full(pseg, p_more, p_first, p_stop);
+        sj = s_first;
+        auto next_scores = [&](int buf) {
+            if (sj == s_first && !wait(C::BAR_QFULL + sqb, sqph, 0xb40u + sqb)) return false;
+            if (!wait(C::BAR_KFULL + ks, kph, 0xb48u + ks)) return false;
+            tc_fence_after();
+            const uint64_t qd = q_desc + (uint64_t)(sqb * (2 * C::Q_BYTES >> 4)), kd = k_desc + (uint64_t)(ks * (2 * C::K_BYTES >> 4));
+#pragma unroll
+            for (int blk = 0; blk < C::NBLK; ++blk)
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    warp_mma_f16(s_col + buf * KV, qd + (uint64_t)(blk * (kCtRows * 128 >> 4) + 2 * kk), kd + (uint64_t)(blk * (KV * 128 >> 4) + 2 * kk), C::IDESC_S, (blk | kk) ? 1u : 0u);
+            warp_commit(bar(C::BAR_SFULL + 2 * st + buf));  // also: P V of two steps before is complete
+            warp_commit(bar(C::BAR_KEMPTY + ks));
+            if (++ks == C::KST) { ks = 0; kph ^= 1u; }
+            if (++sj == s_stop) {
+                warp_commit(bar(C::BAR_QEMPTY + sqb));
+                if (++sqb == C::NQ) { sqb = 0; sqph ^= 1u; }
+                s_more = next_segment(sseg);
+                full(sseg, s_more, s_first, s_stop);
+                sj = s_first;
+            }
+            return true;
+        };
+        for (int i = 0; ok && i < 2 && s_more; ++i) ok = next_scores(i);
+        while (ok && p_more) {
+            if (!(ok = wait(C::BAR_OEMPTY + pob, poph, 0xb50u + pob))) break;
+            const uint32_t o_col = tmem_base + C::COL_O + (2 * pob + st) * DH;
+            for (int j = p_first; j < p_stop; ++j, ++g) {
+                const int buf = g & 1;
+                if (!(ok = wait(C::BAR_VFULL + vs, vph, 0xb58u + vs))) break;
+                if (!(ok = wait(C::BAR_PFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xb60u + st))) break;
+                tc_fence_after();
+                const uint64_t vd = v_desc + (uint64_t)(vs * (C::V_BYTES >> 4));
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int kk = 0; kk < KV / 16; ++kk)
+                        warp_mma_f16_ts(o_col, s_col + buf * KV + 32 * part + 8 * kk, vd + (uint64_t)(2 * kk), C::IDESC_PV, (j != p_first || part || kk) ? 1u : 0u);
+                warp_commit(bar(C::BAR_VEMPTY + vs));
+                if (j + 1 == p_stop) warp_commit(bar(C::BAR_END + st));
+                if (++vs == C::KST) { vs = 0; vph ^= 1u; }
+                if (s_more) { if (!(ok = next_scores(buf))) break; }
+                else warp_commit(bar(C::BAR_SFULL + 2 * st + buf));
+            }
+            if (++pob == C::NO) { pob = 0; poph ^= 1u; }
+            p_more = next_segment(pseg);
+            full(pseg, p_more, p_first, p_stop);
+        }
+    } else if (works && warp < 12) {
+        // ------------------------------------------------------------------ softmax of one stream, one row per thread
+        const int st = warp >= 8 ? 1 : 0, quarter = warp & 3, row = 32 * quarter + lane;
+        const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16);
+        auto wait = [&](int i, uint32_t par, unsigned int code) { return __all_sync(0xffffffffu, mbar_wait_poll(bar(i), par, abort_flag, p.status, code)) != 0; };
+        bool ok = true, more = true;
+        int g = 0, ob = 0, segment = 0;
+        CtSegment &seg = segments[warp];
+        first_segment(seg);
+        for (; ok && more; more = next_segment(seg)) {
+            const int first = seg.unit, stop = seg.stop(), at = seg.tile * kCtRows + row, token = p.group == 1 ? at : at / p.group;
+            const int sees = token < seg.s.m ? seg.s.length - seg.s.m + 1 + token : 0;
+            const bool whole = seg.whole();
+            auto part_at = [&] { return p.cta_parts + (((size_t)blockIdx.x * 2 + (seg.u - seg.unit > c0)) * kCtRows + row) * C::PART; };
+            if (const long long from = seg.u - seg.unit, to = from + seg.s.units; !whole && to > c1 && from >= c0 && warp == 4 && lane == 0) {
+                p.items[2 * blockIdx.x] = make_int4(from > c0 ? 2 : 1, ca_share_of(total, to - 1, ctas), seg.head, seg.tile);
+                p.items[2 * blockIdx.x + 1] = make_int4(seg.s.row0, seg.s.m, 0, 0);
+            }
+            if (first >= stop) {  // (never a whole item: its first step is visible)
+                float *part = part_at();
+                part[2 * st] = kCtNone;
+                part[2 * st + 1] = 0.0f;
+                for (int d = 0; d < DH; d += 4) *reinterpret_cast<float4 *>(part + 4 + st * DH + d) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                continue;
+            }
+            const uint32_t o_addr = lane_base + C::COL_O + (2 * ob + st) * DH;
+            float m = kCtNone;
+            uint64_t l2 = 0;  // the row's sum, two partial sums
+            for (int j = first; j < stop; ++j, ++g) {
+                const int buf = g & 1, n = sees - KV * j;  // n: of the step's tokens, those that the row sees
+                const uint32_t s_addr = lane_base + C::COL_S + (2 * st + buf) * KV;
+                if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xb70u + st))) break;
+                tc_fence_after();
+                if (__all_sync(0xffffffffu, n <= 0)) {
+                    uint32_t zero[32];
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) zero[u] = 0u;
+                    tmem_st32(s_addr, zero);
+                    tmem_st32(s_addr + 32, zero);
+                } else {
+                    const float4 sc = scales[g & 7];
+                    // (a page of zeros has the factor 0, and what is masked has to stay at -inf; of a page that the row sees nothing of not even a NaN counts)
+                    const float f = n > 0 ? p.scale_log2 * (st ? sc.y : sc.x) + 1.17549435e-38f : 1.0f;
+                    // The scale of V enters the exponent; the row's sum is multiplied by its inverse once a step.  (A page of zeros has the scale 0 and codes 0.)
+                    const float sv = n > 0 && sc.z != 0.0f ? sc.z : 1.0f, log_sv = lg2_approx(sv);
+                    uint32_t v0[32], v1[32];
+                    tmem_ld32(s_addr, v0);
+                    tmem_ld32(s_addr + 32, v1);
+                    tmem_ld_wait();
+                    if (__any_sync(0xffffffffu, n < KV)) {
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) {
+                            if (u >= n) v0[u] = 0xff800000u;
+                            if (32 + u >= n) v1[u] = 0xff800000u;
+                        }
+                    }
+                    float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < 32; u += 4) {
+                        m0 = fmaxf(m0, fmaxf(__uint_as_float(v0[u]), __uint_as_float(v0[u + 1])));
+                        m1 = fmaxf(m1, fmaxf(__uint_as_float(v0[u + 2]), __uint_as_float(v0[u + 3])));
+                        m2 = fmaxf(m2, fmaxf(__uint_as_float(v1[u]), __uint_as_float(v1[u + 1])));
+                        m3 = fmaxf(m3, fmaxf(__uint_as_float(v1[u + 2]), __uint_as_float(v1[u + 3])));
+                    }
+                    const float here = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * f;
+                    // The reference of the exponentials follows the maximum only where that has moved by more than kCtSlack, so O and l are rescaled rarely.
+                    const float now = here - m > kCtSlack ? here : m;
+                    if (j > first && __any_sync(0xffffffffu, now != m)) {
+                        // O is at rest once P V of the step before is complete: the barrier of the next step's scores follows it
+                        if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xb78u + st))) break;
+                        tc_fence_after();
+                        const float alpha = exp2_approx(m - now);
+                        const uint64_t a2 = pack_f32x2(alpha, alpha);
+                        l2 = mul_f32x2(l2, a2);
+#pragma unroll
+                        for (int cc = 0; cc < DH; cc += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o_addr + cc, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * alpha);
+                            tmem_st16(o_addr + cc, o);
+                        }
+                    }
+                    m = now;
+                    const uint64_t f2 = pack_f32x2(f, f), minus = pack_f32x2(log_sv - m, log_sv - m), minus1 = pack_f32x2(-1.0f, -1.0f);
+                    uint64_t sum_a = 0, sum_b = 0;
+                    // 32 scores -> their probabilities' first parts and second parts, sixteen columns each
+                    auto part_of = [&](const uint32_t (&v)[32], uint64_t &sum, int at) {
+                        uint32_t hi[16], lo[16];
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) {
+                            float x0, x1;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * u]), __uint_as_float(v[2 * u + 1])), f2, minus), x0, x1);
+                            const uint64_t e = pack_f32x2(exp2_approx(x0), exp2_approx(x1));
+                            sum = add_f32x2(sum, e);
+                            unpack_f32x2(e, x0, x1);
+                            const __nv_bfloat162 first = __floats2bfloat162_rn(x0, x1);
+                            hi[u] = *reinterpret_cast<const uint32_t *>(&first);
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(hi[u] << 16), __uint_as_float(hi[u] & 0xffff0000u)), minus1, e), x0, x1);
+                            const __nv_bfloat162 second = __floats2bfloat162_rn(x0, x1);
+                            lo[u] = *reinterpret_cast<const uint32_t *>(&second);
+                        }
+                        tmem_st16(s_addr + at, hi);
+                        tmem_st16(s_addr + 32 + at, lo);
+                    };
+                    part_of(v0, sum_a, 0);
+                    part_of(v1, sum_b, 16);
+                    const float back = __frcp_rn(sv);
+                    l2 = fma_f32x2(add_f32x2(sum_a, sum_b), pack_f32x2(back, back), l2);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::BAR_PFULL + 2 * st + buf));
+            }
+            if (!ok) break;
+            // ---- the segment's end
+            if (!(ok = wait(C::BAR_END + st, (uint32_t)segment & 1u, 0xb80u + st))) break;
+            float la, lb;
+            unpack_f32x2(l2, la, lb);
+            const float l = la + lb;
+            // open values that are not finite were left out: NaN where a row sees them
+            const int open0 = 64 * seg.s.pages, open_seen = stop > seg.s.pages ? min(sees - open0, seg.s.length - open0) : 0;
+            const volatile int *o4 = odd + 4 * (segment & 7);
+            const bool checked = stop > seg.s.pages && (o4[0] | o4[1] | o4[2] | o4[3]);
+            const __nv_bfloat16 *values = p.c.open + (((size_t)seg.s.slot * H + seg.head) * 3 + 2) * KV * DH;
+            auto not_finite = [&](int dim) {
+                for (int r = 0; r < open_seen; ++r)
+                    if ((__bfloat16_as_ushort(values[(size_t)r * DH + cache_open_eight(r, dim >> 3) * 8 + (dim & 7)]) & 0x7f80) == 0x7f80) return true;
+                return false;
+            };
+            if (whole) {
+                float *sl = s_l + (segment & 1) * 2 * kCtRows;
+                sl[st * kCtRows + row] = l;
+            }
+            // (both streams have got so far: their O are complete, their sums there)
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::BAR_L + (segment & 1)));
+            if (!(ok = wait(C::BAR_L + (segment & 1), (uint32_t)(segment >> 1) & 1u, 0xb88u))) break;
+            tc_fence_after();
+            if (whole) {
+                const float *sl = s_l + (segment & 1) * 2 * kCtRows;
+                const float l1 = sl[row], l2 = sl[kCtRows + row];
+                const float w1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f, w2 = l2 != 0.0f ? p.out_scale * p.lambda / l2 : 0.0f;
+                const uint32_t o_base = lane_base + C::COL_O + 2 * ob * DH;
+                __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(p.out) + ((size_t)(seg.s.row0 + token) * H * p.group + seg.head * p.group + at - token * p.group) * DH;
+#pragma unroll
+                for (int cc = st * (DH / 2); cc < (st + 1) * (DH / 2); cc += 32) {
+                    uint32_t v1[32], v2[32];
+                    tmem_ld32(o_base + cc, v1);
+                    tmem_ld32(o_base + DH + cc, v2);
+                    tmem_ld_wait();
+                    if (token < seg.s.m) {
+#pragma unroll
+                        for (int u = 0; u < 32; u += 8) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v1[u + 2 * e]) * w1 - __uint_as_float(v2[u + 2 * e]) * w2,
+                                                                               __uint_as_float(v1[u + 2 * e + 1]) * w1 - __uint_as_float(v2[u + 2 * e + 1]) * w2);
+                                o[e] = *reinterpret_cast<const uint32_t *>(&y);
+                            }
+                            *reinterpret_cast<uint4 *>(out + cc + u) = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                    }
+                }
+                if (checked && token < seg.s.m)
+                    for (int dim = st * (DH / 2); dim < (st + 1) * (DH / 2); ++dim)
+                        if (not_finite(dim)) out[dim] = __ushort_as_bfloat16(0x7fc0);
+            } else {
+                float *part = part_at();
+                part[2 * st] = m;
+                part[2 * st + 1] = l;
+                float *sums = part + 4 + st * DH;
+#pragma unroll
+                for (int cc = 0; cc < DH; cc += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(o_addr + cc, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4 *>(sums + cc + u) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
+                }
+                if (checked)
+                    for (int dim = 0; dim < DH; ++dim)
+                        if (not_finite(dim)) sums[dim] = __uint_as_float(0x7fc00000u);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::BAR_OEMPTY + ob));
+            if (++ob == C::NO) ob = 0;
+            ++segment;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 12) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base), "r"(512) : "memory");
+    }
+}
+
+}  // namespace hgf

@@ -332,6 +332,58 @@ def test_rows_that_see_nothing_and_padding(hgf, dh):
     p.attend([-1, 4], [0, 1])
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("group", [1, 3])
+def test_many_rows(hgf, dh, group):
+    """Tiles of 128 rows: rows that see nothing, tiles that end inside, open tokens alone, skipped sequences; items that many workers share and workers with many."""
+    p = Pair(hgf, 2, dh, n_pages=200, n_slots=8)
+    p.fill([0, 3, 64, 130, 1000, 63, 5000, 321])
+    for out_bf16 in (True, False):
+        p.attend([4], [300 // group], group=group, out_bf16=out_bf16, pad=0)
+        p.attend([6], [128], group=group, out_bf16=out_bf16, pad=0)
+        p.attend([5, 0, -1, 3, 1, 4, 2], [90, 100, 70, 250, 5, 129, 64], group=group, out_bf16=out_bf16, pad=0)
+        p.attend([7, 6], [321, 1], group=group, out_bf16=out_bf16, pad=0, spread=4.0)
+        p.attend([2], [200], group=group, out_bf16=out_bf16, pad=0)
+    p.attend([0], [150], group=group, out_bf16=True, pad=0)
+
+
+def test_many_rows_of_many_sequences(hgf):
+    p = Pair(hgf, 5, 64, n_pages=300, n_slots=90)
+    p.fill([65 + 2 * i for i in range(90)])
+    p.attend(list(range(90)), [85] * 90, out_bf16=True, pad=0)
+
+
+def test_many_rows_with_blocks_of_zeros(hgf):
+    p = Pair(hgf, 2, 64, n_pages=20, n_slots=1)
+
+    def change(k, v):
+        k.reshape(-1, 2, 2, 64)[:64, 0] = 0
+        k.reshape(-1, 2, 2, 64)[128:200] = 0
+        v[64:128] = 0
+
+    p.reserve([0], [200])
+    p.append([0], [200], change=change)
+    p.attend([0], [150], out_bf16=True, pad=0)
+    p.attend([0], [150], out_bf16=True, pad=0, spread=5.0)
+
+
+def test_many_rows_skip_a_page_that_is_none(hgf):
+    p = Pair(hgf, 2, 64, n_pages=20, n_slots=2)
+    p.fill([200, 200])
+    q, slots, starts = rows(p.rng, 240, 256), ints([0, 1]), ints([0, 120, 240])
+    want = hgf.diff_attention_cached(p.cache, bf16(q), slots, starts, 0.5, flags=hgf.FLAG_OUT_BF16)
+    good = p.cache.table[1, 1].item()
+    for page in (-1, 20):
+        p.cache.table[1, 1] = page
+        out = hgf.diff_attention_cached(p.cache, bf16(q), slots, starts, 0.5, flags=hgf.FLAG_OUT_BF16)
+        with pytest.raises(hgf.HgfError) as e:
+            hgf.check_status()
+        assert e.value.status == 8 and torch.equal(out[:120], want[:120])
+    p.cache.table[1, 1] = good
+    assert torch.equal(hgf.diff_attention_cached(p.cache, bf16(q), slots, starts, 0.5, flags=hgf.FLAG_OUT_BF16), want)
+    hgf.check_status()
+
+
 def test_one_row_form_takes_any_counts(hgf):
     """No more rows than sequences on the whole picks the form for single tokens; a sequence may have several all the same."""
     p = Pair(hgf, 3, 64, n_pages=90, n_slots=16)
@@ -461,7 +513,7 @@ def test_rows_before_a_block_that_is_not_finite(hgf):
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("group", [1, 3])
-@pytest.mark.parametrize("a_sequence", [1, 8, 16, 32])
+@pytest.mark.parametrize("a_sequence", [1, 8, 16, 32, 300])
 def test_what_is_not_finite_stays_with_the_rows_that_see_it(hgf, dh, group, a_sequence):
     """Rows on both sides of a page whose K scale is NaN, of an open value and of an open key that are not finite; queries that are not, of rows without tokens.
 
