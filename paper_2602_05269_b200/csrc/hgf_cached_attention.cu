@@ -14,7 +14,7 @@
 // The accumulators start at the bits of 1.5 * 2^23, so that a sum, below 2^22 in magnitude, is a float after one subtraction: I2F runs at an eighth
 // of the FMA rate and bounded the kernel.  The open tokens' bf16 go through bf16 products, with the probabilities as sums of three bf16.
 //
-// Four forms.  Many rows with bf16 output are tcgen05 products (hgf_cached_attention_tc.cuh).  Here ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.  There
+// Four forms.  Many rows with bf16 output, or 64 wide, are tcgen05 products (hgf_cached_attention_tc.cuh).  Here ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.  There
 // and with ROWS = 8, a few tokens or heads that share K and V, the codes are the left operand, tokens (or dims) as its rows; eight query rows are the
 // columns of a product for each digit, and a team is a warp for each stream.  ROWS = 16, for more: sixteen query rows are the left operand and the
 // codes the right one (a lane's sixteen bytes are the same either way round); a warp takes one stream of one tile of sixteen rows, and a team is the
@@ -1220,16 +1220,18 @@ __global__ void __launch_bounds__(8 * DH / 4) cached_attention_join_kernel(CaPar
 }
 
 // How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows where the sequences have up
-// to that many on average, else of sixteen, two to a team where they have more than that; with bf16 output of 128 where they have more than 80 (any call is right
-// in any of these forms).
+// to that many on average, else of sixteen, two to a team where they have more than that; with bf16 output or 64 wide of 128 where they have more than 80 (any call is right
+// in any of these forms; the sequences' lengths are on the device).
 struct CaForm {
     int rows, tiles, teams, stages, threads;
 };
-static CaForm ca_form(int head_dim, int64_t n_seqs, int64_t n_rows, int group, bool bf16) {
-    const bool narrow = head_dim == 64;
+static CaForm ca_form(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int n_heads, bool bf16) {
+    const bool narrow = cache->head_dim == 64;
+    const int group = n_heads / cache->n_heads;
     // (100 rows of 1000 tokens, 8 sequences, 16 heads of 64: 49.8 us here, 49.8 in tiles of sixteen; 256 rows of 6000 tokens 74 and 145; but 64 rows of 4096 tokens,
-    // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty)
-    if (bf16 && n_rows * group > 80 * n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
+    // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty.  A pool of fewer than four pages a sequence holds short ones, where an item's beginning and
+    // end count: 121 sequences of 2 tokens with 235 rows 182 and 119.)
+    if ((bf16 || narrow) && n_rows * group > 80 * n_seqs && cache->n_pages >= 4 * n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
     if (n_rows * group <= n_seqs) return narrow ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
     if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 4, 4, 256} : CaForm{8, 1, 4, 2, 256};
     const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;
@@ -1271,10 +1273,10 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     static std::atomic<unsigned long long> attr_done{0};
     return launch_with_join<DH, ROWS>(cached_attention_kernel<DH, ROWS, DP>, C::SMEM, attr_done, p, threads, stream);
 }
-template <int DH>
+template <int DH, int PARTS>
 static cudaError_t launch_cached_attention_tc(const CaParams &p, int threads, cudaStream_t stream) {
     static std::atomic<unsigned long long> attr_done{0};
-    return launch_with_join<DH, 16>(cached_attention_tc_kernel<DH>, CtCfg<DH>::SMEM, attr_done, p, threads, stream);
+    return launch_with_join<DH, 16>(cached_attention_tc_kernel<DH, PARTS>, CtCfg<DH, PARTS>::SMEM, attr_done, p, threads, stream);
 }
 
 static size_t ca_items_bytes() { return align_up((size_t)kCaMaxSms * 2 * sizeof(int4), 256); }
@@ -1290,7 +1292,7 @@ using namespace hgf;
 extern "C" size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads) {
     if (!cache || (cache->head_dim != 64 && cache->head_dim != 128) || cache->n_heads <= 0 || n_heads <= 0 || n_rows <= 0 || n_seqs <= 0) return 256;
     size_t bytes = 0;  // (of either type of output)
-    for (const bool bf16 : {false, true}) bytes = std::max(bytes, ca_workspace(cache->head_dim, ca_form(cache->head_dim, n_seqs, n_rows, n_heads / cache->n_heads, bf16)));
+    for (const bool bf16 : {false, true}) bytes = std::max(bytes, ca_workspace(cache->head_dim, ca_form(cache, n_seqs, n_rows, n_heads, bf16)));
     return bytes;
 }
 
@@ -1303,7 +1305,7 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     if (n_heads % cache->n_heads || n_heads > 65535 || n_rows > (1 << 24) || n_rows * (n_heads / cache->n_heads) > 0x3fffffffll) return HGF_ERR_UNSUPPORTED_SHAPE;
     if (((uintptr_t)q | (uintptr_t)out) & 15u) return HGF_ERR_MISALIGNED;
     const int group = n_heads / cache->n_heads, dh = cache->head_dim;
-    const CaForm f = ca_form(dh, n_seqs, n_rows, group, (flags & HGF_FLAG_OUT_BF16) != 0);
+    const CaForm f = ca_form(cache, n_seqs, n_rows, n_heads, (flags & HGF_FLAG_OUT_BF16) != 0);
     if (!workspace || workspace_bytes < ca_workspace(dh, f)) return HGF_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255u) return HGF_ERR_MISALIGNED;
     p.q = (const __nv_bfloat16 *)q;
@@ -1329,7 +1331,7 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     const cudaStream_t stream = (cudaStream_t)stream_;
     cudaError_t e;
     auto launch = [&](auto narrow, auto wide) { return (dh == 64 ? narrow : wide)(p, f.threads, stream); };
-    if (!f.stages) e = launch(launch_cached_attention_tc<64>, launch_cached_attention_tc<128>);
+    if (!f.stages) e = p.bf16 ? launch(launch_cached_attention_tc<64, 2>, launch_cached_attention_tc<128, 2>) : launch_cached_attention_tc<64, 3>(p, f.threads, stream);
     else if (f.rows == 1) e = launch(launch_cached_attention<64, 1, 3>, launch_cached_attention<128, 1, 3>);
     else if (f.rows == 8) e = p.bf16 ? launch(launch_cached_attention<64, 8, 2>, launch_cached_attention<128, 8, 2>) : launch(launch_cached_attention<64, 8, 3>, launch_cached_attention<128, 8, 3>);
     else e = p.bf16 ? launch(launch_cached_attention<64, 16, 2>, launch_cached_attention<128, 16, 2>) : launch(launch_cached_attention<64, 16, 3>, launch_cached_attention<128, 16, 3>);

@@ -1,4 +1,4 @@
-// Cached differential attention of many rows a sequence with bf16 output, on tcgen05 (included by hgf_cached_attention.cu).
+// Cached differential attention of many rows a sequence, with bf16 output or 64 wide, on tcgen05 (included by hgf_cached_attention.cu).
 //
 // An item is 128 rows (row: token times heads of the group) of a sequence and K/V head, a step one page of 64 tokens (the open tokens are one step more).
 // All items' steps are one sequence, dealt in equal shares to one CTA an SM: a CTA walks segments, each the steps of one item that lie in its share; a
@@ -9,12 +9,13 @@
 //                have them; V lies transposed in a page, so both operands have their contraction index contiguous
 //   warps 12, 13 issue the products of a stream each: S = Q K^T of the codes, and O += P V of the codes
 //   warps 4-7    softmax of stream 1, warps 8-11 of stream 2: a thread owns a row; scores times the page's scale of K, the page's scale of V in the exponent
-// A probability enters the second product as a sum of two bf16, off by 2^-16 of itself at most, beside the output's 2^-8; all sums are fp32.
+// With bf16 output a probability enters the second product as a sum of two bf16, off by 2^-16 of itself at most, beside the output's 2^-8; with fp32 output as
+// three, 2^-24.  For a third part tensor memory has room 64 wide only.  All sums are fp32.
 //
 // What bounds it is the issue of instructions: 1500 a step and scheduler (54 % of the slots, with the instruction cache behind another fifth of the
 // waits), of them 340 in each softmax warp's 64 x 32 probabilities and 350 in a converting warp; tensor pipe 26 %, exponentials 34 %.
 // Measured, 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 145 us with the int8 form, 74 us here; 8 K/V heads with four query heads each, 30000 tokens,
-// 128 rows: 438 and 172 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 107 us.  Steps: codes from global memory into registers 81 us (of the
+// 128 rows: 438 and 172 us; the first with fp32 output 157 and 99 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 107 us.  Steps: codes from global memory into registers 81 us (of the
 // first), with the bulk copies and segments kept in registers 85 (spills went to the L2 cache), segments in shared memory 76, V's scale in the exponent 74; two
 // converting warps of a larger share of registers 99.
 #pragma once
@@ -23,11 +24,12 @@
 namespace hgf {
 
 constexpr int kCtRows = 128, kCtThreads = 480;
+constexpr int kCtFlush = 8;  // a power of two
 constexpr float kCtSlack = 8.0f, kCtNone = -1e30f;  // (a maximum of nothing)
 
-template <int DH>
+template <int DH, int PARTS>
 struct CtCfg {
-    static constexpr int NBLK = DH / 64, KST = DH == 64 ? 3 : 2, GST = DH == 64 ? 4 : 2, NQ = DH == 64 ? 2 : 1, NO = DH == 64 ? 2 : 1;  // stages of the operands, of the pages; buffers of query tiles, of O_1 and O_2
+    static constexpr int NBLK = DH / 64, KST = DH == 64 ? 3 : 2, GST = DH == 128 ? 2 : PARTS == 2 ? 4 : 3, NQ = DH == 64 && PARTS == 2 ? 2 : 1, NO = NQ;  // stages of the operands, of the pages; buffers of query tiles, of O_1 and O_2
     static constexpr int Q_BYTES = NBLK * kCtRows * 128, K_BYTES = NBLK * kCacheBlock * 128, V_BYTES = DH * 128;
     static constexpr int OFF_K = NQ * 2 * Q_BYTES, OFF_V = OFF_K + KST * 2 * K_BYTES, OFF_G = OFF_V + KST * V_BYTES,
                          UNIT = 3 * kCacheBlock * DH, G_BYTES = (UNIT + 16 + 127) / 128 * 128, OFF_BAR = OFF_G + GST * G_BYTES;
@@ -37,13 +39,16 @@ struct CtCfg {
     static constexpr int OFF_SCALES = OFF_BAR + 384;             // [8] float4: K1, K2, V of step g % 8
     static constexpr int OFF_ODD = OFF_SCALES + 128;             // [8][4] ints: of segment % 8, a warp found open values that are not finite
     static constexpr int OFF_L = OFF_ODD + 128;                  // [2][2][128] floats
-    static constexpr int OFF_PREFIX = OFF_L + 2 * 2 * kCtRows * 4;
+    static constexpr int OFF_F = OFF_L + 2 * 2 * kCtRows * 4;    // [2][2][128] floats
+    static constexpr int OFF_ACC = OFF_F + 2 * 2 * kCtRows * 4;  // (three parts) [2][128][DH] floats, sixteen bytes c of row r at place c ^ (r & 7)
+    static constexpr int OFF_PREFIX = OFF_ACC + (PARTS == 3 ? 2 * kCtRows * DH * 4 : 0);
     static constexpr int SMEM = OFF_PREFIX + (kCacheMaxSeqs + 2) * 8 + 1024;
-    static constexpr int COL_S = 0, COL_O = 4 * kCacheBlock;     // scores: + (2 stream + buffer) 64; O: + (2 buffer + stream) DH
+    static constexpr int COL_S = 0, COL_O = 4 * kCacheBlock, COL_P3 = COL_O + NO * 2 * DH;  // third parts: + (2 stream + buffer) 32
+    //    // scores: + (2 stream + buffer) 64; O: + (2 buffer + stream) DH
     static constexpr int PART = 4 + 2 * DH;
     static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCacheBlock >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
-    static_assert(BAR_COUNT * 8 + 16 <= 384 && COL_O + NO * 2 * DH <= 512 && SMEM <= 226 * 1024, "barriers, tensor and shared memory");
+    static_assert(BAR_COUNT * 8 + 16 <= 384 && COL_P3 + (PARTS == 3 ? 128 : 0) <= 512 && SMEM <= 226 * 1024, "barriers, tensor and shared memory");
 };
 
 __device__ __forceinline__ CaSeq ct_sequence(const CaParams &p, int i) {
@@ -115,9 +120,9 @@ __device__ __forceinline__ float lg2_approx(float x) {
     return y;
 }
 
-template <int DH>
+template <int DH, int PARTS>
 __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaParams p) {
-    using C = CtCfg<DH>;
+    using C = CtCfg<DH, PARTS>;
     constexpr int KV = kCacheBlock;
     extern __shared__ uint8_t ct_smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)ct_smem_raw + 1023) & ~(uintptr_t)1023);
@@ -132,7 +137,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
     int *unseen = reinterpret_cast<int *>(smem + C::OFF_BAR + C::BAR_COUNT * 8 + 8);
     float4 *scales = reinterpret_cast<float4 *>(smem + C::OFF_SCALES);
     volatile int *odd = reinterpret_cast<volatile int *>(smem + C::OFF_ODD);
-    float *s_l = reinterpret_cast<float *>(smem + C::OFF_L);
+    float *s_l = reinterpret_cast<float *>(smem + C::OFF_L), *s_f = reinterpret_cast<float *>(smem + C::OFF_F);
     long long *prefix = reinterpret_cast<long long *>(smem + C::OFF_PREFIX);
     __shared__ long long wide[kCtThreads / 32];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, H = p.c.H;
@@ -210,7 +215,8 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x) {
             const CaSeq s = ct_sequence(p, i);
             const size_t at = (size_t)s.row0 * width, n = (size_t)max(s.m - s.length, 0) * width;
-            for (size_t e = 8 * tid; e < n; e += 8 * kCtThreads) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
+            if (PARTS == 2) for (size_t e = 8 * tid; e < n; e += 8 * kCtThreads) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
+            else for (size_t e = 4 * tid; e < n; e += 4 * kCtThreads) *reinterpret_cast<uint4 *>(reinterpret_cast<float *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
         }
     }
     const int ctas = (int)min((long long)gridDim.x, total);
@@ -431,10 +437,10 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 tc_fence_after();
                 const uint64_t vd = v_desc + (uint64_t)(vs * (C::V_BYTES >> 4));
 #pragma unroll
-                for (int part = 0; part < 2; ++part)
+                for (int part = 0; part < PARTS; ++part)
 #pragma unroll
                     for (int kk = 0; kk < KV / 16; ++kk)
-                        warp_mma_f16_ts(o_col, s_col + buf * KV + 32 * part + 8 * kk, vd + (uint64_t)(2 * kk), C::IDESC_PV, (j != p_first || part || kk) ? 1u : 0u);
+                        warp_mma_f16_ts(o_col, (part < 2 ? s_col + buf * KV + 32 * part : tmem_base + C::COL_P3 + (2 * st + buf) * 32) + 8 * kk, vd + (uint64_t)(2 * kk), C::IDESC_PV, ((PARTS == 2 ? j != p_first : ((j - p_first) & (kCtFlush - 1)) != 0) || part || kk) ? 1u : 0u);
                 warp_commit(bar(C::BAR_VEMPTY + vs));
                 if (j + 1 == p_stop) warp_commit(bar(C::BAR_END + st));
                 if (++vs == C::KST) { vs = 0; vph ^= 1u; }
@@ -452,6 +458,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         auto wait = [&](int i, uint32_t par, unsigned int code) { return __all_sync(0xffffffffu, mbar_wait_poll(bar(i), par, abort_flag, p.status, code)) != 0; };
         bool ok = true, more = true;
         int g = 0, ob = 0, segment = 0;
+        auto acc_at = [&](int stream, int c) { return reinterpret_cast<float4 *>(smem + C::OFF_ACC + ((size_t)stream * kCtRows + row) * DH * 4 + ((c ^ (row & 7)) << 4)); };
         CtSegment &seg = segments[warp];
         first_segment(seg);
         for (; ok && more; more = next_segment(seg)) {
@@ -473,23 +480,50 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             const uint32_t o_addr = lane_base + C::COL_O + (2 * ob + st) * DH;
             float m = kCtNone;
             uint64_t l2 = 0;  // the row's sum, two partial sums
+            float m_acc = kCtNone;
+            bool flushed = false;
             for (int j = first; j < stop; ++j, ++g) {
                 const int buf = g & 1, n = sees - KV * j;  // n: of the step's tokens, those that the row sees
                 const uint32_t s_addr = lane_base + C::COL_S + (2 * st + buf) * KV;
                 if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xb70u + st))) break;
                 tc_fence_after();
+                if (PARTS == 3 && j > first && ((j - first) & (kCtFlush - 1)) == 0) {
+                    // The products' sums are cut off, not rounded, and lose 2^-25 of themselves with each addition: every kCtFlush steps they are added up here
+                    // instead and begin anew.  (Error against 64 bits after 41 steps without it
+                    // 4.4e-6 and 92 us, with it 1.3e-6 and 99 us, as 2 x 256 rows of 6000 tokens.)
+                    if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xb7cu + st))) break;
+                    tc_fence_after();
+                    const float beta = flushed ? exp2_approx(m_acc - m) : 0.0f;
+#pragma unroll
+                    for (int cc = 0; cc < DH; cc += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(o_addr + cc, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int u = 0; u < 16; u += 4) {
+                            float4 *a = acc_at(st, (cc + u) >> 2);
+                            float4 y = flushed ? *a : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            y = make_float4(fmaf(y.x, beta, __uint_as_float(o[u])), fmaf(y.y, beta, __uint_as_float(o[u + 1])), fmaf(y.z, beta, __uint_as_float(o[u + 2])),
+                                            fmaf(y.w, beta, __uint_as_float(o[u + 3])));
+                            *a = y;
+                        }
+                    }
+                    m_acc = m;
+                    flushed = true;
+                }
                 if (__all_sync(0xffffffffu, n <= 0)) {
                     uint32_t zero[32];
 #pragma unroll
                     for (int u = 0; u < 32; ++u) zero[u] = 0u;
                     tmem_st32(s_addr, zero);
                     tmem_st32(s_addr + 32, zero);
+                    if (PARTS == 3) tmem_st32(lane_base + C::COL_P3 + (2 * st + buf) * 32, zero);
                 } else {
                     const float4 sc = scales[g & 7];
                     // (a page of zeros has the factor 0, and what is masked has to stay at -inf; of a page that the row sees nothing of not even a NaN counts)
                     const float f = n > 0 ? p.scale_log2 * (st ? sc.y : sc.x) + 1.17549435e-38f : 1.0f;
                     // The scale of V enters the exponent; the row's sum is multiplied by its inverse once a step.  (A page of zeros has the scale 0 and codes 0.)
-                    const float sv = n > 0 && sc.z != 0.0f ? sc.z : 1.0f, log_sv = lg2_approx(sv);
+                    const float sv = n > 0 && sc.z != 0.0f ? sc.z : 1.0f, log_sv = PARTS == 2 ? lg2_approx(sv) : 0.0f;
                     uint32_t v0[32], v1[32];
                     tmem_ld32(s_addr, v0);
                     tmem_ld32(s_addr + 32, v1);
@@ -530,30 +564,36 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                         }
                     }
                     m = now;
-                    const uint64_t f2 = pack_f32x2(f, f), minus = pack_f32x2(log_sv - m, log_sv - m), minus1 = pack_f32x2(-1.0f, -1.0f);
+                    const uint64_t f2 = pack_f32x2(f, f), minus = pack_f32x2(log_sv - m, log_sv - m), minus1 = pack_f32x2(-1.0f, -1.0f), sv2 = pack_f32x2(sv, sv);
                     uint64_t sum_a = 0, sum_b = 0;
                     // 32 scores -> their probabilities' first parts and second parts, sixteen columns each
                     auto part_of = [&](const uint32_t (&v)[32], uint64_t &sum, int at) {
-                        uint32_t hi[16], lo[16];
+                        uint32_t hi[16], lo[16], third[16];
 #pragma unroll
                         for (int u = 0; u < 16; ++u) {
                             float x0, x1;
                             unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * u]), __uint_as_float(v[2 * u + 1])), f2, minus), x0, x1);
-                            const uint64_t e = pack_f32x2(exp2_approx(x0), exp2_approx(x1));
+                            uint64_t e = pack_f32x2(exp2_approx(x0), exp2_approx(x1));
                             sum = add_f32x2(sum, e);
+                            if (PARTS == 3) e = mul_f32x2(e, sv2);
                             unpack_f32x2(e, x0, x1);
                             const __nv_bfloat162 first = __floats2bfloat162_rn(x0, x1);
                             hi[u] = *reinterpret_cast<const uint32_t *>(&first);
                             unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(hi[u] << 16), __uint_as_float(hi[u] & 0xffff0000u)), minus1, e), x0, x1);
                             const __nv_bfloat162 second = __floats2bfloat162_rn(x0, x1);
                             lo[u] = *reinterpret_cast<const uint32_t *>(&second);
+                            if (PARTS == 3) {
+                                const __nv_bfloat162 rest = __floats2bfloat162_rn(x0 - __uint_as_float(lo[u] << 16), x1 - __uint_as_float(lo[u] & 0xffff0000u));
+                                third[u] = *reinterpret_cast<const uint32_t *>(&rest);
+                            }
                         }
                         tmem_st16(s_addr + at, hi);
                         tmem_st16(s_addr + 32 + at, lo);
+                        if (PARTS == 3) tmem_st16(lane_base + C::COL_P3 + (2 * st + buf) * 32 + at, third);
                     };
                     part_of(v0, sum_a, 0);
                     part_of(v1, sum_b, 16);
-                    const float back = __frcp_rn(sv);
+                    const float back = PARTS == 2 ? __frcp_rn(sv) : 1.0f;
                     l2 = fma_f32x2(add_f32x2(sum_a, sum_b), pack_f32x2(back, back), l2);
                 }
                 tmem_st_wait();
@@ -577,10 +617,22 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     if ((__bfloat16_as_ushort(values[(size_t)r * DH + cache_open_eight(r, dim >> 3) * 8 + (dim & 7)]) & 0x7f80) == 0x7f80) return true;
                 return false;
             };
+            const float flush_scale = flushed ? exp2_approx(m_acc - m) : 0.0f;
             if (whole) {
-                float *sl = s_l + (segment & 1) * 2 * kCtRows;
-                sl[st * kCtRows + row] = l;
+                s_l[((segment & 1) * 2 + st) * kCtRows + row] = l;
+                if (PARTS == 3) s_f[((segment & 1) * 2 + st) * kCtRows + row] = flush_scale;
             }
+            auto add_flushed = [&](uint32_t (&v)[32], int stream, int cc, float scale) {
+                if (PARTS == 2 || scale == 0.0f) return;
+#pragma unroll
+                for (int u = 0; u < 32; u += 4) {
+                    const float4 a = *acc_at(stream, (cc + u) >> 2);
+                    v[u] = __float_as_uint(fmaf(a.x, scale, __uint_as_float(v[u])));
+                    v[u + 1] = __float_as_uint(fmaf(a.y, scale, __uint_as_float(v[u + 1])));
+                    v[u + 2] = __float_as_uint(fmaf(a.z, scale, __uint_as_float(v[u + 2])));
+                    v[u + 3] = __float_as_uint(fmaf(a.w, scale, __uint_as_float(v[u + 3])));
+                }
+            };
             // (both streams have got so far: their O are complete, their sums there)
             tc_fence_before();
             __syncwarp();
@@ -592,30 +644,40 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 const float l1 = sl[row], l2 = sl[kCtRows + row];
                 const float w1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f, w2 = l2 != 0.0f ? p.out_scale * p.lambda / l2 : 0.0f;
                 const uint32_t o_base = lane_base + C::COL_O + 2 * ob * DH;
-                __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(p.out) + ((size_t)(seg.s.row0 + token) * H * p.group + seg.head * p.group + at - token * p.group) * DH;
+                const size_t out = ((size_t)(seg.s.row0 + token) * H * p.group + seg.head * p.group + at - token * p.group) * DH;
 #pragma unroll
                 for (int cc = st * (DH / 2); cc < (st + 1) * (DH / 2); cc += 32) {
                     uint32_t v1[32], v2[32];
                     tmem_ld32(o_base + cc, v1);
                     tmem_ld32(o_base + DH + cc, v2);
                     tmem_ld_wait();
-                    if (token < seg.s.m) {
+                    add_flushed(v1, 0, cc, s_f[(segment & 1) * 2 * kCtRows + row]);
+                    add_flushed(v2, 1, cc, s_f[((segment & 1) * 2 + 1) * kCtRows + row]);
+                    if (token >= seg.s.m) continue;
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) v1[u] = __float_as_uint(__uint_as_float(v1[u]) * w1 - __uint_as_float(v2[u]) * w2);
+                    if (PARTS == 2) {
 #pragma unroll
                         for (int u = 0; u < 32; u += 8) {
                             uint32_t o[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v1[u + 2 * e]) * w1 - __uint_as_float(v2[u + 2 * e]) * w2,
-                                                                               __uint_as_float(v1[u + 2 * e + 1]) * w1 - __uint_as_float(v2[u + 2 * e + 1]) * w2);
+                                const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v1[u + 2 * e]), __uint_as_float(v1[u + 2 * e + 1]));
                                 o[e] = *reinterpret_cast<const uint32_t *>(&y);
                             }
-                            *reinterpret_cast<uint4 *>(out + cc + u) = make_uint4(o[0], o[1], o[2], o[3]);
+                            *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + out + cc + u) = make_uint4(o[0], o[1], o[2], o[3]);
                         }
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4 *>(reinterpret_cast<float *>(p.out) + out + cc + u) = make_uint4(v1[u], v1[u + 1], v1[u + 2], v1[u + 3]);
                     }
                 }
                 if (checked && token < seg.s.m)
                     for (int dim = st * (DH / 2); dim < (st + 1) * (DH / 2); ++dim)
-                        if (not_finite(dim)) out[dim] = __ushort_as_bfloat16(0x7fc0);
+                        if (not_finite(dim)) {
+                            if (PARTS == 2) reinterpret_cast<__nv_bfloat16 *>(p.out)[out + dim] = __ushort_as_bfloat16(0x7fc0);
+                            else reinterpret_cast<float *>(p.out)[out + dim] = __uint_as_float(0x7fc00000u);
+                        }
             } else {
                 float *part = part_at();
                 part[2 * st] = m;
@@ -626,6 +688,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     uint32_t v[32];
                     tmem_ld32(o_addr + cc, v);
                     tmem_ld_wait();
+                    add_flushed(v, st, cc, flush_scale);
 #pragma unroll
                     for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4 *>(sums + cc + u) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
                 }

@@ -348,9 +348,17 @@ def test_many_rows(hgf, dh, group):
 
 
 def test_many_rows_of_many_sequences(hgf):
-    p = Pair(hgf, 5, 64, n_pages=300, n_slots=90)
+    p = Pair(hgf, 5, 64, n_pages=400, n_slots=90)
     p.fill([65 + 2 * i for i in range(90)])
     p.attend(list(range(90)), [85] * 90, out_bf16=True, pad=0)
+    p.attend(list(range(90)), [84] * 90, pad=0)
+
+
+def test_many_rows_in_a_small_pool(hgf):
+    p = Pair(hgf, 2, 64, n_pages=9, n_slots=3)
+    p.fill([100, 2, 190])
+    for out_bf16 in (True, False):
+        p.attend([0, 1, 2], [90, 120, 81], out_bf16=out_bf16, pad=0)
 
 
 def test_many_rows_with_blocks_of_zeros(hgf):
