@@ -12,10 +12,11 @@
 // With bf16 output a probability enters the second product as a sum of two bf16, off by 2^-16 of itself at most, beside the output's 2^-8; with fp32 output as
 // three, 2^-24.  For a third part tensor memory has room 64 wide only.  All sums are fp32.
 //
-// What bounds it is the issue of instructions: 1500 a step and scheduler (54 % of the slots, with the instruction cache behind another fifth of the
-// waits), of them 340 in each softmax warp's 64 x 32 probabilities and 350 in a converting warp; tensor pipe 26 %, exponentials 34 %.
+// What bounds it is the instructions: 1500 a step and scheduler, of them 340 in each softmax warp's 64 x 32 probabilities and 350 in a converting warp, and
+// their fetching, as the roles' loops together are longer than what a scheduler keeps (41 to 54 % of the issue slots used; tensor pipe 20 to 26 %,
+// exponentials 20 to 34 %, memory 3 to 5 %).
 // Measured, 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 145 us with the int8 form, 74 us here; 8 K/V heads with four query heads each, 30000 tokens,
-// 128 rows: 438 and 172 us; the first with fp32 output 157 and 99 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 107 us.  Steps: codes from global memory into registers 81 us (of the
+// 128 rows: 438 and 172 us; the first with fp32 output 157 and 89 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 99 us.  Steps: codes from global memory into registers 81 us (of the
 // first), with the bulk copies and segments kept in registers 85 (spills went to the L2 cache), segments in shared memory 76, V's scale in the exponent 74; two
 // converting warps of a larger share of registers 99.
 #pragma once
@@ -244,7 +245,10 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(i));
         };
-        constexpr int KN = DH / 16, VN = DH / 32;  // tiles of 16 x 32 codes of a warp: of K (both streams 4 KT), of V
+        constexpr int KN = DH / 16, VN = DH / 32;  // tiles of 16 x 32 codes of a warp: of K, of V
+        // (Instructions are fetched from afar - a third of all waits - and the less code the loops have the better, but for the form with the shortest steps: 2 x 256
+        // rows of 6000 tokens with fp32 output 96 us unrolled, 89 not; 4 x 128 rows of 8192 tokens 128 wide 107 and 99; 128 rows of 30000 tokens, bf16, 173 and 186.)
+        constexpr int KU = DH == 64 && PARTS == 2 ? KN : 1, VU = DH == 64 && PARTS == 2 ? VN : 1;
         bool ok = true;
         int ks = 0, vs = 0, gs = 0, qb = 0, g = 0, segment = 0;
         uint32_t kph = 1, vph = 1, gph = 0, qph = 1;
@@ -291,7 +295,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (!(ok = wait(C::BAR_KEMPTY + ks, kph, 0xb20u + ks))) break;
                 uint8_t *k = smem + C::OFF_K + ks * 2 * C::K_BYTES;
                 if (page) {
-#pragma unroll
+#pragma unroll KU
                     for (int i = 0; i < KN; ++i) {  // tile n of stream n / (4 KT): sixteen tokens, 32 dims
                         const int n = 4 * i + warp, stream = n / (DH / 8), mt = n % (DH / 8) / (DH / 32), kt = n % (DH / 32);
                         store(k + stream * C::K_BYTES + (kt >> 1) * KV * 128, mt * 16, (kt & 1) * 4, good ? codes[n * 32] : make_uint4(0, 0, 0, 0));
@@ -309,7 +313,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (!(ok = wait(C::BAR_VEMPTY + vs, vph, 0xb30u + vs))) break;
                 uint8_t *v = smem + C::OFF_V + vs * C::V_BYTES;
                 if (page) {
-#pragma unroll
+#pragma unroll VU
                     for (int i = 0; i < VN; ++i) {  // sixteen dims, 32 tokens
                         const int n = 4 * i + warp;
                         store(v, (n >> 1) * 16, (n & 1) * 4, good ? codes[(4 * KN + n) * 32] : make_uint4(0, 0, 0, 0));
@@ -490,7 +494,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (PARTS == 3 && j > first && ((j - first) & (kCtFlush - 1)) == 0) {
                     // The products' sums are cut off, not rounded, and lose 2^-25 of themselves with each addition: every kCtFlush steps they are added up here
                     // instead and begin anew.  (Error against 64 bits after 41 steps without it
-                    // 4.4e-6 and 92 us, with it 1.3e-6 and 99 us, as 2 x 256 rows of 6000 tokens.)
+                    // 4.4e-6 and 92 us, with it 1.3e-6 and 99 us, of 2 x 256 rows of 6000 tokens.)
                     if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xb7cu + st))) break;
                     tc_fence_after();
                     const float beta = flushed ? exp2_approx(m_acc - m) : 0.0f;
@@ -623,14 +627,15 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (PARTS == 3) s_f[((segment & 1) * 2 + st) * kCtRows + row] = flush_scale;
             }
             auto add_flushed = [&](uint32_t (&v)[32], int stream, int cc, float scale) {
-                if (PARTS == 2 || scale == 0.0f) return;
+                if (PARTS == 3 && scale != 0.0f) {
 #pragma unroll
-                for (int u = 0; u < 32; u += 4) {
-                    const float4 a = *acc_at(stream, (cc + u) >> 2);
-                    v[u] = __float_as_uint(fmaf(a.x, scale, __uint_as_float(v[u])));
-                    v[u + 1] = __float_as_uint(fmaf(a.y, scale, __uint_as_float(v[u + 1])));
-                    v[u + 2] = __float_as_uint(fmaf(a.z, scale, __uint_as_float(v[u + 2])));
-                    v[u + 3] = __float_as_uint(fmaf(a.w, scale, __uint_as_float(v[u + 3])));
+                    for (int u = 0; u < 32; u += 4) {
+                        const float4 a = *acc_at(stream, (cc + u) >> 2);
+                        v[u] = __float_as_uint(fmaf(a.x, scale, __uint_as_float(v[u])));
+                        v[u + 1] = __float_as_uint(fmaf(a.y, scale, __uint_as_float(v[u + 1])));
+                        v[u + 2] = __float_as_uint(fmaf(a.z, scale, __uint_as_float(v[u + 2])));
+                        v[u + 3] = __float_as_uint(fmaf(a.w, scale, __uint_as_float(v[u + 3])));
+                    }
                 }
             };
             // (both streams have got so far: their O are complete, their sums there)
