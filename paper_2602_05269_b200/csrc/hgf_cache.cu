@@ -89,7 +89,8 @@ static unsigned head_shares(int64_t pieces, int H, int blocks) {
 // A block of threads takes one piece and every gridDim.y-th K/V head of it: a block of 64 tokens that becomes complete, whose values it reads from the open
 // rows and the new ones, quantises, and writes as a page; the sequence's first piece also writes the rows that stay open, after its reads of the rows
 // that these replace.  Each new value is read once, each code written once; what bounds it is the chain of dependent look-ups in front (starts, slot, length,
-// table, counts: about 4 us), which is why a block has several heads.
+// table, counts: about 4 us), which is why a block has several heads.  Measured, kernel alone, memory cold: 64 sequences with one token each, 16 heads of 64, 10.6 us; six with up to 1400
+// tokens 20.3 us (addresses found anew for every page 31).
 constexpr int kAppendThreads = 256;
 
 // Four lanes (l, l + 8, l + 16, l + 24) hold a word of four bytes each, a 4 x 4 matrix: its transpose.
@@ -293,7 +294,8 @@ __global__ void __launch_bounds__(kAppendThreads, DH == 64 ? 4 : 2) cache_append
 
 // ---- read -------------------------------------------------------------------------------------------------------------------------
 // A block of threads takes one block of tokens that a range touches and every gridDim.y-th K/V head of it: the page through shared memory, whole, since a
-// token's codes are spread over it, the next head's on its way meanwhile; open rows straight from where they are.  Bound by the writes.
+// token's codes are spread over it, the next head's on its way meanwhile; open rows straight from where they are.  Bound by the writes: four sequences of up to
+// 8192 tokens, 128 wide, fp32 out, 420 MB in all in 77 us, 83 % of the floor at 6567 GB/s of copy bandwidth (four bytes of output a thread and store: 97).
 constexpr int kReadThreads = 256;
 
 template <int DH>
@@ -459,7 +461,7 @@ __device__ static int block_exclusive_sum(int v, int *smem /* [32] */, int *tota
 
 // One block of threads deals the lowest free pages: the requests' running sum of pages in shared memory, then the reference counts in order, each free
 // page to the request that its rank falls into.  A first walk counts the free pages, as far as they are asked for, so that a request that cannot be
-// met in full takes none.
+// met in full takes none.  Bound by its dependent look-ups: 6.9 us for one request, 10.5 for 48 sequences of up to 4000 tokens.
 constexpr int kReserveThreads = 1024, kReserveStep = 16;  // reference counts a thread looks at in one step
 
 __global__ void __launch_bounds__(kReserveThreads) cache_reserve_kernel(CacheView c, const int32_t *__restrict__ slots, const int32_t *__restrict__ tokens, int n, int32_t *granted,
@@ -625,7 +627,7 @@ __global__ void __launch_bounds__(256) cache_free_kernel(CacheView c, const int3
 }
 
 // A block of threads copies the open rows of every gridDim.y-th K/V head; the first of a pair also shares the pages, and the last to have read the state
-// changes it.  Bound by the copy: the rows are asked for before it is known whether the copy is made.
+// changes it.  Bound by the copy, 11.2 us for 144 forks (7 for three): the rows are asked for before it is known whether the copy is made.
 template <int DH>
 __global__ void __launch_bounds__(256) cache_fork_kernel(CacheView c, const int32_t *__restrict__ srcs, const int32_t *__restrict__ dsts, int n, int32_t *done, unsigned int *status) {
     const int i = blockIdx.x, head0 = blockIdx.y, tid = threadIdx.x, H = c.H;

@@ -21,6 +21,14 @@
 // warps of one or two tiles, so that a page that is read once serves up to 32 rows.  There the columns of the scores' products are the page's tokens in
 // such an order that a lane gets four neighbouring tokens of its rows: the probabilities' digits are then in place for the second product, where
 // ROWS = 8 turns the scores through shared memory.
+//
+// Measured (one B200; floor: the cache's bytes once at 6567 GB/s of copy bandwidth):
+//   single tokens   64 sequences of up to 4096 tokens, 16 heads of 128: 248 us, 99 % of the floor's rate; one of 131071 tokens, 16 heads of 64: 73 us, 84 %;
+//                   32 of up to 2048: 32 us, 63 % - 4 us to begin, unequal ends of the CTAs, the join; one of 200 tokens: 9 us, launches and look-ups
+//   shared heads    16 sequences of up to 2900 tokens, 5 drafts of 4 query heads a K/V head, 128 wide: 52 us, floor 14.  Bound by dependent issue at two warps
+//                   a scheduler (0.29 instructions issued a clock; 890 a page, stream and sixteen rows, 96 of them products; integer tensor pipe 25 % busy).
+//                   Tiles of eight rows against sixteen: one sequence of 59361 tokens, two heads a K/V head, 128 wide 71 and 110 us; with sixteen warps instead of
+//                   eight for those, 64 wide, 51 and 49 (13 sequences of 5 tokens 13.6 and 9.9)
 #include <algorithm>
 
 #include "hgf_cache.cuh"
