@@ -570,13 +570,18 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         f = count > 0 ? f + 1.17549435e-38f : 1.0f;  // (a page of zeros has f = 0, one that the row sees nothing of may have NaN, and what is masked has to stay at -inf)
         const float here = top * f, now = fmaxf(m[r], here), base = now == -INFINITY ? 0.0f : now;
-        const float minus = here == -INFINITY ? 0.0f : -here;
+        const float minus = top == -INFINITY ? 0.0f : -top;
+        const uint64_t minus2 = pack_f32x2(minus, minus), f2 = pack_f32x2(f, f);
         alpha = exp2_approx(m[r] - base);
         worth = exp2_approx(here - base);
+        // (the difference first: the largest gives exactly 1, however large the scores)
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            x[j] = exp2_approx(fmaf(x[j], f, minus));
+        for (int j = 0; j < N; j += 2) {
+            unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(x[j], x[j + 1]), minus2), f2), x[j], x[j + 1]);
+            x[j] = exp2_approx(x[j]);
+            x[j + 1] = exp2_approx(x[j + 1]);
             sums[j & 3] += x[j];
+            sums[(j + 1) & 3] += x[j + 1];
         }
         m[r] = now;
         l[r] = fmaf(l[r], alpha, ((sums[0] + sums[1]) + (sums[2] + sums[3])) * worth);
@@ -1290,7 +1295,7 @@ static cudaError_t launch_cached_attention_tc(const CaParams &p, int threads, cu
 static size_t ca_items_bytes() { return align_up((size_t)kCaMaxSms * 2 * sizeof(int4), 256); }
 static size_t ca_cta_parts_bytes(int head_dim, const CaForm &f) { return align_up((size_t)kCaMaxSms * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256); }
 static size_t ca_workspace(int head_dim, const CaForm &f) {
-    return ca_items_bytes() + ca_cta_parts_bytes(head_dim, f) + (f.rows == 1 ? 0 : align_up((size_t)kCaMaxSms * f.teams * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256));
+    return ca_items_bytes() + ca_cta_parts_bytes(head_dim, f) + (f.rows == 1 || !f.stages ? 0 : align_up((size_t)kCaMaxSms * f.teams * 2 * f.tiles * f.rows * (4 + 2 * head_dim) * 4, 256));
 }
 
 }  // namespace hgf

@@ -15,9 +15,9 @@
 // What bounds it is the instructions: 1500 a step and scheduler, of them 340 in each softmax warp's 64 x 32 probabilities and 350 in a converting warp, and
 // their fetching, as the roles' loops together are longer than what a scheduler keeps (41 to 54 % of the issue slots used; tensor pipe 20 to 26 %,
 // exponentials 20 to 34 %, memory 3 to 5 %).
-// Measured, 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 145 us with the int8 form, 74 us here; 8 K/V heads with four query heads each, 30000 tokens,
-// 128 rows: 438 and 172 us; the first with fp32 output 157 and 89 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 99 us.  Steps: codes from global memory into registers 81 us (of the
-// first), with the bulk copies and segments kept in registers 85 (spills went to the L2 cache), segments in shared memory 76, V's scale in the exponent 74; two
+// Measured, 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 145 us with the int8 form, 77 us here; 8 K/V heads with four query heads each, 30000 tokens,
+// 128 rows: 438 and 180 us; the first with fp32 output 157 and 91 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 101 us.  Steps: codes from global memory into registers 81 us (of the
+// first), with the bulk copies and segments kept in registers 85 (spills went to the L2 cache), segments in shared memory 76, V's scale in the exponent 74, scores relative to the step's largest first 77; two
 // converting warps of a larger share of registers 99.
 #pragma once
 #include "hgf_tc.cuh"
@@ -26,7 +26,7 @@ namespace hgf {
 
 constexpr int kCtRows = 128, kCtThreads = 480;
 constexpr int kCtFlush = 8;  // a power of two
-constexpr float kCtSlack = 8.0f, kCtNone = -1e30f;  // (a maximum of nothing)
+constexpr float kCtSlack = 8.0f, kCtNone = -3e38f;  // (a maximum of nothing: finite, so that differences of two are zero)
 
 template <int DH, int PARTS>
 struct CtCfg {
@@ -44,8 +44,8 @@ struct CtCfg {
     static constexpr int OFF_ACC = OFF_F + 2 * 2 * kCtRows * 4;  // (three parts) [2][128][DH] floats, sixteen bytes c of row r at place c ^ (r & 7)
     static constexpr int OFF_PREFIX = OFF_ACC + (PARTS == 3 ? 2 * kCtRows * DH * 4 : 0);
     static constexpr int SMEM = OFF_PREFIX + (kCacheMaxSeqs + 2) * 8 + 1024;
-    static constexpr int COL_S = 0, COL_O = 4 * kCacheBlock, COL_P3 = COL_O + NO * 2 * DH;  // third parts: + (2 stream + buffer) 32
-    //    // scores: + (2 stream + buffer) 64; O: + (2 buffer + stream) DH
+    static constexpr int COL_S = 0, COL_O = 4 * kCacheBlock, COL_P3 = COL_O + NO * 2 * DH;
+    // (scores: + (2 stream + buffer) 64; O: + (2 buffer + stream) DH; third parts of the probabilities: + (2 stream + buffer) 32)
     static constexpr int PART = 4 + 2 * DH;
     static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCacheBlock >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     *reinterpret_cast<uint2 *>(rows + row * 128 + ((chunk ^ g4) << 4) + (t & 1) * 8) = ct_bf16(w[i]);
                 }
             };
-            if (!(ok = wait(C::BAR_QEMPTY + qb, qph, 0xb10u + qb))) break;
+            if (!(ok = wait(C::BAR_QEMPTY + qb, qph, 0xc10u + qb))) break;
             {
                 const int at = seg.tile * kCtRows + tid, token = p.group == 1 ? at : at / p.group;
                 const bool in = token < seg.s.m;
@@ -289,10 +289,10 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 const bool page = j < pages;
                 const int rows = page ? KV : seg.s.length & 63;
                 const uint4 *open = reinterpret_cast<const uint4 *>(p.c.open + ((size_t)seg.s.slot * H + seg.head) * 3 * KV * DH);
-                if (page && !(ok = wait(C::BAR_GFULL + gs, gph, 0xb18u + gs))) break;
+                if (page && !(ok = wait(C::BAR_GFULL + gs, gph, 0xc18u + gs))) break;
                 const uint4 *codes = reinterpret_cast<const uint4 *>(smem + C::OFF_G + gs * C::G_BYTES) + lane;
                 const bool good = page && page_ok[gs];
-                if (!(ok = wait(C::BAR_KEMPTY + ks, kph, 0xb20u + ks))) break;
+                if (!(ok = wait(C::BAR_KEMPTY + ks, kph, 0xc20u + ks))) break;
                 uint8_t *k = smem + C::OFF_K + ks * 2 * C::K_BYTES;
                 if (page) {
 #pragma unroll KU
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (tid == 0) scales[g & 7] = !page ? make_float4(1.0f, 1.0f, 1.0f, 0.0f) : good ? *reinterpret_cast<const float4 *>(smem + C::OFF_G + gs * C::G_BYTES + C::UNIT) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 there(C::BAR_KFULL + ks);
                 if (++ks == C::KST) { ks = 0; kph ^= 1u; }
-                if (!(ok = wait(C::BAR_VEMPTY + vs, vph, 0xb30u + vs))) break;
+                if (!(ok = wait(C::BAR_VEMPTY + vs, vph, 0xc30u + vs))) break;
                 uint8_t *v = smem + C::OFF_V + vs * C::V_BYTES;
                 if (page) {
 #pragma unroll VU
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (j == first || (j & 31) == 0) pages32 = (j & ~31) + lane < pages ? table[(j & ~31) + lane] : 0;
                 const int page = __shfl_sync(0xffffffffu, pages32, j & 31);
                 const bool good = page >= 0 && page < p.c.n_pages;
-                ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_GEMPTY + gs), gph, abort_flag, p.status, 0xb90u + gs)) != 0;
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_GEMPTY + gs), gph, abort_flag, p.status, 0xc90u + gs)) != 0;
                 if (!ok) break;
                 if (lane == 0) {
                     const uint32_t full = bar(C::BAR_GFULL + gs), dst = sbase + C::OFF_G + gs * C::G_BYTES;
@@ -409,8 +409,8 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         full(pseg, p_more, p_first, p_stop);
         sj = s_first;
         auto next_scores = [&](int buf) {
-            if (sj == s_first && !wait(C::BAR_QFULL + sqb, sqph, 0xb40u + sqb)) return false;
-            if (!wait(C::BAR_KFULL + ks, kph, 0xb48u + ks)) return false;
+            if (sj == s_first && !wait(C::BAR_QFULL + sqb, sqph, 0xc40u + sqb)) return false;
+            if (!wait(C::BAR_KFULL + ks, kph, 0xc48u + ks)) return false;
             tc_fence_after();
             const uint64_t qd = q_desc + (uint64_t)(sqb * (2 * C::Q_BYTES >> 4)), kd = k_desc + (uint64_t)(ks * (2 * C::K_BYTES >> 4));
 #pragma unroll
@@ -432,12 +432,12 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         };
         for (int i = 0; ok && i < 2 && s_more; ++i) ok = next_scores(i);
         while (ok && p_more) {
-            if (!(ok = wait(C::BAR_OEMPTY + pob, poph, 0xb50u + pob))) break;
+            if (!(ok = wait(C::BAR_OEMPTY + pob, poph, 0xc50u + pob))) break;
             const uint32_t o_col = tmem_base + C::COL_O + (2 * pob + st) * DH;
             for (int j = p_first; j < p_stop; ++j, ++g) {
                 const int buf = g & 1;
-                if (!(ok = wait(C::BAR_VFULL + vs, vph, 0xb58u + vs))) break;
-                if (!(ok = wait(C::BAR_PFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xb60u + st))) break;
+                if (!(ok = wait(C::BAR_VFULL + vs, vph, 0xc58u + vs))) break;
+                if (!(ok = wait(C::BAR_PFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xc60u + st))) break;
                 tc_fence_after();
                 const uint64_t vd = v_desc + (uint64_t)(vs * (C::V_BYTES >> 4));
 #pragma unroll
@@ -489,13 +489,13 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             for (int j = first; j < stop; ++j, ++g) {
                 const int buf = g & 1, n = sees - KV * j;  // n: of the step's tokens, those that the row sees
                 const uint32_t s_addr = lane_base + C::COL_S + (2 * st + buf) * KV;
-                if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xb70u + st))) break;
+                if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xc70u + st))) break;
                 tc_fence_after();
                 if (PARTS == 3 && j > first && ((j - first) & (kCtFlush - 1)) == 0) {
                     // The products' sums are cut off, not rounded, and lose 2^-25 of themselves with each addition: every kCtFlush steps they are added up here
                     // instead and begin anew.  (Error against 64 bits after 41 steps without it
                     // 4.4e-6 and 92 us, with it 1.3e-6 and 99 us, of 2 x 256 rows of 6000 tokens.)
-                    if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xb7cu + st))) break;
+                    if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xc7cu + st))) break;
                     tc_fence_after();
                     const float beta = flushed ? exp2_approx(m_acc - m) : 0.0f;
 #pragma unroll
@@ -547,12 +547,12 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                         m2 = fmaxf(m2, fmaxf(__uint_as_float(v1[u]), __uint_as_float(v1[u + 1])));
                         m3 = fmaxf(m3, fmaxf(__uint_as_float(v1[u + 2]), __uint_as_float(v1[u + 3])));
                     }
-                    const float here = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * f;
+                    const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)), here = top * f;
                     // The reference of the exponentials follows the maximum only where that has moved by more than kCtSlack, so O and l are rescaled rarely.
                     const float now = here - m > kCtSlack ? here : m;
                     if (j > first && __any_sync(0xffffffffu, now != m)) {
                         // O is at rest once P V of the step before is complete: the barrier of the next step's scores follows it
-                        if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xb78u + st))) break;
+                        if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xc78u + st))) break;
                         tc_fence_after();
                         const float alpha = exp2_approx(m - now);
                         const uint64_t a2 = pack_f32x2(alpha, alpha);
@@ -568,15 +568,16 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                         }
                     }
                     m = now;
-                    const uint64_t f2 = pack_f32x2(f, f), minus = pack_f32x2(log_sv - m, log_sv - m), minus1 = pack_f32x2(-1.0f, -1.0f), sv2 = pack_f32x2(sv, sv);
+                    const uint64_t f2 = pack_f32x2(f, f), minus = top == -INFINITY ? 0 : pack_f32x2(-top, -top), rest2 = pack_f32x2(here - m + log_sv, here - m + log_sv), minus1 = pack_f32x2(-1.0f, -1.0f), sv2 = pack_f32x2(sv, sv);
                     uint64_t sum_a = 0, sum_b = 0;
+                    // (relative to the step's largest first, which is then exact however large the scores)
                     // 32 scores -> their probabilities' first parts and second parts, sixteen columns each
                     auto part_of = [&](const uint32_t (&v)[32], uint64_t &sum, int at) {
                         uint32_t hi[16], lo[16], third[16];
 #pragma unroll
                         for (int u = 0; u < 16; ++u) {
                             float x0, x1;
-                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * u]), __uint_as_float(v[2 * u + 1])), f2, minus), x0, x1);
+                            unpack_f32x2(fma_f32x2(add_f32x2(pack_f32x2(__uint_as_float(v[2 * u]), __uint_as_float(v[2 * u + 1])), minus), f2, rest2), x0, x1);
                             uint64_t e = pack_f32x2(exp2_approx(x0), exp2_approx(x1));
                             sum = add_f32x2(sum, e);
                             if (PARTS == 3) e = mul_f32x2(e, sv2);
@@ -607,7 +608,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             }
             if (!ok) break;
             // ---- the segment's end
-            if (!(ok = wait(C::BAR_END + st, (uint32_t)segment & 1u, 0xb80u + st))) break;
+            if (!(ok = wait(C::BAR_END + st, (uint32_t)segment & 1u, 0xc80u + st))) break;
             float la, lb;
             unpack_f32x2(l2, la, lb);
             const float l = la + lb;
@@ -642,7 +643,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::BAR_L + (segment & 1)));
-            if (!(ok = wait(C::BAR_L + (segment & 1), (uint32_t)(segment >> 1) & 1u, 0xb88u))) break;
+            if (!(ok = wait(C::BAR_L + (segment & 1), (uint32_t)(segment >> 1) & 1u, 0xc88u))) break;
             tc_fence_after();
             if (whole) {
                 const float *sl = s_l + (segment & 1) * 2 * kCtRows;

@@ -375,6 +375,27 @@ def test_many_rows_with_blocks_of_zeros(hgf):
     p.attend([0], [150], out_bf16=True, pad=0, spread=5.0)
 
 
+@pytest.mark.parametrize("m", [1, 3, 40, 100])
+@pytest.mark.parametrize("out_bf16", [False, True])
+def test_scores_far_below_zero(hgf, m, out_bf16):
+    """Equal scores of about -2^102 * 64 / 8: every token that a row sees has the same weight."""
+    p = Pair(hgf, 2, 64, n_pages=20, n_slots=1)
+
+    def change(k, v):
+        k[:] = f32_to_bf16_bits(np.full(1, -2.0 ** 50, np.float32))[0]
+
+    p.reserve([0], [192])
+    p.append([0], [192], change=change)
+    q = np.full((m, 256), f32_to_bf16_bits(np.full(1, 2.0 ** 52, np.float32))[0], np.uint16)
+    out = hgf.diff_attention_cached(p.cache, bf16(q), ints([0]), ints([0, m]), 0.25, flags=hgf.FLAG_OUT_BF16 if out_bf16 else 0).float().cpu().numpy().reshape(m, 2, 64)
+    v = p.ref.values(0)[2]
+    for j in range(m):
+        want = 0.75 * v[:, :192 - m + j + 1].mean(1)
+        # (sums of up to 192 terms in binary32, a probability to 2^-16 at least, half a step of bf16)
+        tol = np.abs(v).max() * (2 * 192 * 2.0 ** -24 + (2 * 2.0 ** -16 if out_bf16 else 2.0 ** -22)) + (2.0 ** -8 * np.abs(want) if out_bf16 else 0)
+        assert (np.abs(out[j] - want) <= tol).all()
+
+
 def test_many_rows_skip_a_page_that_is_none(hgf):
     p = Pair(hgf, 2, 64, n_pages=20, n_slots=2)
     p.fill([200, 200])
@@ -721,6 +742,42 @@ def test_captured_decode_loop(hgf, group):
             p.attend([0, 1, 2], [1, 2, 1], group=group)
     p.check()
     hgf.check_status()
+
+
+@pytest.mark.parametrize("dh, group, out_bf16", [(64, 1, False), (64, 3, True), (128, 1, True)])
+def test_captured_pieces_of_a_prompt(hgf, dh, group, out_bf16):
+    """Pieces of two prompts, appended and attended to in one captured graph, replayed without a stop between them: the tiles of 128 rows."""
+    H, piece, pieces = 2, 97, 6
+    p = Pair(hgf, H, dh, n_pages=40, n_slots=2)
+    p.fill([0, 77])
+    p.reserve([0, 1], [piece * pieces, 77 + piece * pieces])
+    slots, starts, n = ints([1, 0]), ints([0, piece, 2 * piece]), 2 * piece
+    k, v, q = (torch.zeros((n, w * dh), dtype=torch.bfloat16, device="cuda") for w in (2 * H, H, 2 * H * group))
+    out = torch.zeros((n, H * group * dh), dtype=torch.bfloat16 if out_bf16 else torch.float32, device="cuda")
+    ws = torch.empty(hgf.cached_workspace_bytes(p.cache, 2, n, H * group), dtype=torch.uint8, device="cuda")
+    done, flags = torch.zeros(2, dtype=torch.int32, device="cuda"), hgf.FLAG_OUT_BF16 if out_bf16 else 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hgf.cache_append(p.cache, k, v, slots, starts, done=done)
+        hgf.diff_attention_cached(p.cache, q, slots, starts, 0.6, out=out, workspace=ws, flags=flags)
+    bits_ = [[rows(p.rng, n, w * dh) for w in (2 * H, H, 2 * H * group)] for _ in range(pieces)]
+    new, outs = [[bf16(x) for x in piece_] for piece_ in bits_], []
+    for nk, nv, nq in new:
+        k.copy_(nk), v.copy_(nv), q.copy_(nq)
+        graph.replay()
+        outs.append(out.clone())
+    again = hgf.diff_attention_cached(p.cache, q, slots, starts, 0.6, flags=flags)
+    assert torch.equal(again, outs[-1])
+    hgf.check_status()
+    for (kb, vb, qb), got in zip(bits_, outs):
+        p.ref.append([1, 0], [0, piece, n], kb, vb)
+        got = got.float().cpu().numpy().astype(np.float64).reshape(n, H * group, dh)
+        qf = bf16_bits_to_f32(qb).astype(np.float64).reshape(n, 2, H * group, dh)
+        for i, s in enumerate([1, 0]):
+            want, tol = attention(p.ref.values(s), qf[i * piece:(i + 1) * piece], piece, H * group, 0.6, 1.0, coarse=out_bf16)
+            tol = tol[:, :, None] + (2.0 ** -8 * np.abs(want) if out_bf16 else 0)
+            assert (np.abs(got[i * piece:(i + 1) * piece] - want) <= tol).all()
+    p.check()
 
 
 def test_on_another_stream(hgf):
