@@ -1241,10 +1241,10 @@ struct CaForm {
 static CaForm ca_form(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int n_heads, bool bf16) {
     const bool narrow = cache->head_dim == 64;
     const int group = n_heads / cache->n_heads;
-    // (100 rows of 1000 tokens, 8 sequences, 16 heads of 64: 49.8 us here, 49.8 in tiles of sixteen; 256 rows of 6000 tokens 74 and 145; but 64 rows of 4096 tokens,
-    // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty.  A pool of fewer than four pages a sequence holds short ones, where an item's beginning and
-    // end count: 121 sequences of 2 tokens with 235 rows 182 and 119.)
-    if ((bf16 || narrow) && n_rows * group > 80 * n_seqs && cache->n_pages >= 4 * n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
+    // (100 rows of 1000 tokens, 8 sequences, 16 heads of 64: 49.8 us here, 49.8 in tiles of sixteen; 256 rows of 6000 tokens 77 and 145; but 64 rows of 4096 tokens,
+    // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty.  A pool of fewer pages than sequences holds some tens of tokens each, where an item's
+    // beginning and end count: 121 sequences of up to 80 tokens, 60 rows of four heads a K/V head, 334 and 281; but 40 of up to 190, 190 rows, 108 and 137.)
+    if ((bf16 || narrow) && n_rows * group > 80 * n_seqs && cache->n_pages >= n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
     if (n_rows * group <= n_seqs) return narrow ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
     if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 4, 4, 256} : CaForm{8, 1, 4, 2, 256};
     const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;

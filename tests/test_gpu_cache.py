@@ -355,8 +355,8 @@ def test_many_rows_of_many_sequences(hgf):
 
 
 def test_many_rows_in_a_small_pool(hgf):
-    p = Pair(hgf, 2, 64, n_pages=9, n_slots=3)
-    p.fill([100, 2, 190])
+    p = Pair(hgf, 2, 64, n_pages=2, n_slots=3)
+    p.fill([63, 2, 100])
     for out_bf16 in (True, False):
         p.attend([0, 1, 2], [90, 120, 81], out_bf16=out_bf16, pad=0)
 
