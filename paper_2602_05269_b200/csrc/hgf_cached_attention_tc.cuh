@@ -16,7 +16,7 @@
 // their fetching, as the roles' loops together are longer than what a scheduler keeps (41 to 54 % of the issue slots used; tensor pipe 20 to 26 %,
 // exponentials 20 to 34 %, memory 3 to 5 %).
 // Measured, 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 145 us with the int8 form, 77 us here; 8 K/V heads with four query heads each, 30000 tokens,
-// 128 rows: 438 and 180 us; the first with fp32 output 157 and 91 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 101 us.  Steps: codes from global memory into registers 81 us (of the
+// 128 rows: 438 and 174 us; the first with fp32 output 157 and 91 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 101 us.  Steps: codes from global memory into registers 81 us (of the
 // first), with the bulk copies and segments kept in registers 85 (spills went to the L2 cache), segments in shared memory 76, V's scale in the exponent 74, scores relative to the step's largest first 77; two
 // converting warps of a larger share of registers 99.
 #pragma once
@@ -30,7 +30,7 @@ constexpr float kCtSlack = 8.0f, kCtNone = -3e38f;  // (a maximum of nothing: fi
 
 template <int DH, int PARTS>
 struct CtCfg {
-    static constexpr int NBLK = DH / 64, KST = DH == 64 ? 3 : 2, GST = DH == 128 ? 2 : PARTS == 2 ? 4 : 3, NQ = DH == 64 && PARTS == 2 ? 2 : 1, NO = NQ;  // stages of the operands, of the pages; buffers of query tiles, of O_1 and O_2
+    static constexpr int NBLK = DH / 64, KST = DH == 128 ? 2 : PARTS == 2 ? 4 : 3, GST = DH == 128 ? 2 : PARTS == 2 ? 4 : 3, NQ = DH == 64 && PARTS == 2 ? 2 : 1, NO = NQ;  // stages of the operands, of the pages; buffers of query tiles, of O_1 and O_2
     static constexpr int Q_BYTES = NBLK * kCtRows * 128, K_BYTES = NBLK * kCacheBlock * 128, V_BYTES = DH * 128;
     static constexpr int OFF_K = NQ * 2 * Q_BYTES, OFF_V = OFF_K + KST * 2 * K_BYTES, OFF_G = OFF_V + KST * V_BYTES,
                          UNIT = 3 * kCacheBlock * DH, G_BYTES = (UNIT + 16 + 127) / 128 * 128, OFF_BAR = OFF_G + GST * G_BYTES;
@@ -45,6 +45,7 @@ struct CtCfg {
     static constexpr int OFF_PREFIX = OFF_ACC + (PARTS == 3 ? 2 * kCtRows * DH * 4 : 0);
     static constexpr int SMEM = OFF_PREFIX + (kCacheMaxSeqs + 2) * 8 + 1024;
     static constexpr int COL_S = 0, COL_O = 4 * kCacheBlock, COL_P3 = COL_O + NO * 2 * DH;
+    // (as many stages as shared memory takes; four of the operands instead of three 180 -> 174 us of the second case above)
     // (scores: + (2 stream + buffer) 64; O: + (2 buffer + stream) DH; third parts of the probabilities: + (2 stream + buffer) 32)
     static constexpr int PART = 4 + 2 * DH;
     static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCacheBlock >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
