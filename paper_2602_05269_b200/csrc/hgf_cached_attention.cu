@@ -10,7 +10,7 @@
 // Products are int8 tensor-core products on the codes as they lie in the page (m16n8k32, the codes as left operand), exact:
 //   scores   q as a 23-bit fixed-point number of the row's power of two, cut into three signed digits in base 256: columns of the right operand
 //   values   probabilities relative to the largest of the row's in this page, as fixed-point numbers of 24 bits (the bits of 1 + p), three unsigned
-//            digits; 16 bits, two digits, in the many-row form with bf16 output: at most 64 * 2^-17 of a page's weight, beside the output's 2^-9
+//            digits, whatever the output's type (two digits, 16 bits, moved one bf16 output in a hundred to its neighbour for 3 us of the 55 below)
 // The accumulators start at the bits of 1.5 * 2^23, so that a sum, below 2^22 in magnitude, is a float after one subtraction: I2F runs at an eighth
 // of the FMA rate and bounded the kernel.  The open tokens' bf16 go through bf16 products, with the probabilities as sums of three bf16.
 //
@@ -25,7 +25,7 @@
 // Measured (one B200; floor: the cache's bytes once at 6567 GB/s of copy bandwidth):
 //   single tokens   64 sequences of up to 4096 tokens, 16 heads of 128: 248 us, 99 % of the floor's rate; one of 131071 tokens, 16 heads of 64: 73 us, 84 %;
 //                   32 of up to 2048: 32 us, 63 % - 4 us to begin, unequal ends of the CTAs, the join; one of 200 tokens: 9 us, launches and look-ups
-//   shared heads    16 sequences of up to 2900 tokens, 5 drafts of 4 query heads a K/V head, 128 wide: 52 us, floor 14.  Bound by dependent issue at two warps
+//   shared heads    16 sequences of up to 2900 tokens, 5 drafts of 4 query heads a K/V head, 128 wide: 55 us, floor 14.  Bound by dependent issue at two warps
 //                   a scheduler (0.29 instructions issued a clock; 890 a page, stream and sixteen rows, 96 of them products; integer tensor pipe 25 % busy).
 //                   Tiles of eight rows against sixteen: one sequence of 59361 tokens, two heads a K/V head, 128 wide 71 and 110 us; with sixteen warps instead of
 //                   eight for those, 64 wide, 51 and 49 (13 sequences of 5 tokens 13.6 and 9.9)
@@ -234,8 +234,7 @@ __device__ __forceinline__ void ca_join(const CaParams &p, const CaItem &it, int
 #include "hgf_cached_attention_tc.cuh"
 namespace hgf {
 
-// DP: digits of the probabilities.
-template <int DH, int ROWS, int DP>
+template <int DH, int ROWS>
 __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_kernel(CaParams p) {
     using C = CaCfg<DH, ROWS>;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -744,24 +743,19 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                         __syncwarp();
                     }
                     softmax_step(x[0], 0, qs[0] * (stream ? sc.y : sc.x), partly, sees[0] - token0, token, alpha[0], worth[0]);
-                    uint32_t pd[DP][4];  // digits of the probabilities, as right operand
+                    uint32_t pd[3][4];  // digits of the probabilities, as right operand
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t w[4];
-                        if (DP == 3) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[0][4 * j + e]);
-                            pd[0][j] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
-                        } else {  // (65535 p beside 128: p = 1 stays within 16 bits)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(fmaf(x[0][4 * j + e], 0.9999847412109375f, 128.0f));
-                        }
+                        for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[0][4 * j + e]);
+                        pd[0][j] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
                         const uint32_t w01 = __byte_perm(w[0], w[1], 0x5140), w23 = __byte_perm(w[2], w[3], 0x5140);
-                        pd[DP - 2][j] = __byte_perm(w01, w23, 0x7632);
-                        pd[DP - 1][j] = __byte_perm(w01, w23, 0x5410);
+                        pd[1][j] = __byte_perm(w01, w23, 0x7632);
+                        pd[2][j] = __byte_perm(w01, w23, 0x5410);
                     }
                     // (a row that sees none of the page takes nothing of it, not even a scale that is NaN)
-                    constexpr float kUnit = DP == 3 ? 1.1920928955078125e-7f : 1.0f / 65535.0f;
+                    constexpr float kUnit = 1.1920928955078125e-7f;
                     float scale[2], sv[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
@@ -772,17 +766,17 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                     const uint64_t scale2 = pack_f32x2(scale[0], scale[1]), sv2 = pack_f32x2(sv[0], sv[1]);
 #pragma unroll
                     for (int mt = 0; mt < C::MT; ++mt) {
-                        int d[DP][4];
+                        int d[3][4];
 #pragma unroll
                         for (int kt = 0; kt < 2; ++kt) {
                             const uint4 a = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
 #pragma unroll
-                            for (int z = 0; z < DP; ++z) mma_s8u8(d[z], a, pd[z][2 * kt], pd[z][2 * kt + 1], kt ? d[z] : magic);
+                            for (int z = 0; z < 3; ++z) mma_s8u8(d[z], a, pd[z][2 * kt], pd[z][2 * kt + 1], kt ? d[z] : magic);
                         }
 #pragma unroll
                         for (int e = 0; e < 4; e += 2) {
                             uint64_t y = fma_f32x2(ca_float2(d[0][e], d[0][e + 1]), base256, ca_float2(d[1][e], d[1][e + 1]));
-                            if (DP == 3) y = fma_f32x2(y, base256, ca_float2(d[DP - 1][e], d[DP - 1][e + 1]));
+                            y = fma_f32x2(y, base256, ca_float2(d[2][e], d[2][e + 1]));
                             unpack_f32x2(fma_f32x2(y, sv2, mul_f32x2(pack_f32x2(acc[mt][e % NE], acc[mt][(e + 1) % NE]), scale2)), acc[mt][e % NE], acc[mt][(e + 1) % NE]);
                         }
                     }
@@ -810,9 +804,9 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                                              x[r][4 * j + 2 * two], x[r][4 * j + 2 * two + 1]);
                         }
                     const float sk = stream ? sc.y : sc.x;
-                    uint32_t pd[DP][2][4];  // digits of the probabilities, as left operand of the two products over 32 tokens
+                    uint32_t pd[3][2][4];  // digits of the probabilities, as left operand of the two products over 32 tokens
                     uint64_t scale2[NR], sv2[NR];
-                    constexpr float kUnit = DP == 3 ? 1.1920928955078125e-7f : 1.0f / 65535.0f;
+                    constexpr float kUnit = 1.1920928955078125e-7f;
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
                         softmax_step(x[r], r, qs[r] * sk, partly, sees[r] - token0, token, alpha[r], worth[r]);
@@ -820,17 +814,12 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                         for (int j = 0; j < 4; ++j) {
                             uint32_t w[4];
                             const int kt = j >> 1, at = 2 * (j & 1) + r;
-                            if (DP == 3) {
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[r][4 * j + e]);
-                                pd[0][kt][at] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
-                            } else {  // (65535 p beside 128: p = 1 stays within 16 bits)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(fmaf(x[r][4 * j + e], 0.9999847412109375f, 128.0f));
-                            }
+                            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(1.0f + x[r][4 * j + e]);
+                            pd[0][kt][at] = __byte_perm(__byte_perm(w[0], w[1], 0x0062), __byte_perm(w[2], w[3], 0x0062), 0x5410) ^ 0x80808080u;
                             const uint32_t w01 = __byte_perm(w[0], w[1], 0x5140), w23 = __byte_perm(w[2], w[3], 0x5140);
-                            pd[DP - 2][kt][at] = __byte_perm(w01, w23, 0x7632);
-                            pd[DP - 1][kt][at] = __byte_perm(w01, w23, 0x5410);
+                            pd[1][kt][at] = __byte_perm(w01, w23, 0x7632);
+                            pd[2][kt][at] = __byte_perm(w01, w23, 0x5410);
                         }
                         // (a row that sees none of the page takes nothing of it, not even a scale that is NaN)
                         const float sv = sees[r] > token0 ? worth[r] * sc.z * kUnit : 0.0f;
@@ -844,16 +833,16 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
                         for (int kt = 0; kt < 2; ++kt) v[kt] = *reinterpret_cast<const uint4 *>(unit + 2 * kCacheBlock * DH + ((mt * 2 + kt) * 32 + lane) * 16);
 #pragma unroll
                         for (int a = 0; a < 2; ++a) {
-                            int d[DP][4];
+                            int d[3][4];
                             float (&o)[NE] = acc[ROWS == 16 ? 2 * mt + a : 0];
 #pragma unroll
                             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                                for (int z = 0; z < DP; ++z) mma_u8s8(d[z], pd[z][kt], a ? v[kt].y : v[kt].x, a ? v[kt].w : v[kt].z, kt ? d[z] : magic);
+                                for (int z = 0; z < 3; ++z) mma_u8s8(d[z], pd[z][kt], a ? v[kt].y : v[kt].x, a ? v[kt].w : v[kt].z, kt ? d[z] : magic);
 #pragma unroll
                             for (int r = 0; r < NR; ++r) {
                                 uint64_t y = fma_f32x2(ca_float2(d[0][2 * r], d[0][2 * r + 1]), base256, ca_float2(d[1][2 * r], d[1][2 * r + 1]));
-                                if (DP == 3) y = fma_f32x2(y, base256, ca_float2(d[DP - 1][2 * r], d[DP - 1][2 * r + 1]));
+                                y = fma_f32x2(y, base256, ca_float2(d[2][2 * r], d[2][2 * r + 1]));
                                 unpack_f32x2(fma_f32x2(y, sv2[r], mul_f32x2(pack_f32x2(o[(2 * r) % NE], o[(2 * r + 1) % NE]), scale2[r])), o[(2 * r) % NE], o[(2 * r + 1) % NE]);
                             }
                         }
@@ -1279,12 +1268,12 @@ static cudaError_t launch_with_join(void (*kernel)(CaParams), size_t smem, std::
     count_launch(2);
     return cudaSuccess;
 }
-template <int DH, int ROWS, int DP>
+template <int DH, int ROWS>
 static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaStream_t stream) {
     using C = CaCfg<DH, ROWS>;
     static_assert(C::SMEM <= 226 * 1024, "shared memory of a CTA");
     static std::atomic<unsigned long long> attr_done{0};
-    return launch_with_join<DH, ROWS>(cached_attention_kernel<DH, ROWS, DP>, C::SMEM, attr_done, p, threads, stream);
+    return launch_with_join<DH, ROWS>(cached_attention_kernel<DH, ROWS>, C::SMEM, attr_done, p, threads, stream);
 }
 template <int DH, int PARTS>
 static cudaError_t launch_cached_attention_tc(const CaParams &p, int threads, cudaStream_t stream) {
@@ -1345,8 +1334,8 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     cudaError_t e;
     auto launch = [&](auto narrow, auto wide) { return (dh == 64 ? narrow : wide)(p, f.threads, stream); };
     if (!f.stages) e = p.bf16 ? launch(launch_cached_attention_tc<64, 2>, launch_cached_attention_tc<128, 2>) : launch_cached_attention_tc<64, 3>(p, f.threads, stream);
-    else if (f.rows == 1) e = launch(launch_cached_attention<64, 1, 3>, launch_cached_attention<128, 1, 3>);
-    else if (f.rows == 8) e = p.bf16 ? launch(launch_cached_attention<64, 8, 2>, launch_cached_attention<128, 8, 2>) : launch(launch_cached_attention<64, 8, 3>, launch_cached_attention<128, 8, 3>);
-    else e = p.bf16 ? launch(launch_cached_attention<64, 16, 2>, launch_cached_attention<128, 16, 2>) : launch(launch_cached_attention<64, 16, 3>, launch_cached_attention<128, 16, 3>);
+    else if (f.rows == 1) e = launch(launch_cached_attention<64, 1>, launch_cached_attention<128, 1>);
+    else if (f.rows == 8) e = launch(launch_cached_attention<64, 8>, launch_cached_attention<128, 8>);
+    else e = launch(launch_cached_attention<64, 16>, launch_cached_attention<128, 16>);
     return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
 }

@@ -1,0 +1,35 @@
+"""Cached attention (hgf_diff_attention_cached) gives the same answer in each of its forms: single tokens, tiles of eight and of sixteen rows.
+
+Which form a call takes goes by its rows times the heads that share a K/V head, per entry of its list; entries -1 without rows set that average here."""
+import pytest
+import torch
+
+from cache_reference import rows
+from test_gpu_cache import Pair, bf16, hgf, ints  # noqa: F401  (hgf is the fixture)
+
+pytestmark = pytest.mark.gpu
+
+AVERAGES = [1, 8, 16, 32]
+
+
+def call(p, q, slot, n, average, out_bf16, group=1, lam=0.5):
+    """The last n tokens of `slot`, in the form for `average` rows times heads an entry: [rows of q][heads][dh] in binary32, and the output as it came."""
+    idle = -(-n * group // average) - 1
+    flags = p.hgf.FLAG_OUT_BF16 if out_bf16 else 0
+    out = p.hgf.diff_attention_cached(p.cache, bf16(q), ints([slot] + [-1] * idle), ints([0] + [n] * (idle + 1)), lam, flags=flags)
+    return out.float().cpu().numpy().reshape(len(q), -1, p.dh), out
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("group", [1, 4])
+@pytest.mark.parametrize("average", AVERAGES)
+def test_bf16_output_is_the_rounding_of_binary32(hgf, dh, group, average):  # noqa: F811
+    """The type of the output says how the output is rounded, and nothing of how it is computed."""
+    p = Pair(hgf, 2, dh, n_pages=120, n_slots=3, max_pages=60)
+    p.fill([700, 60, 3333])
+    n = {1: 60, 8: 5, 16: 9, 32: 40}[average]
+    for slot, spread in ((0, 1.0), (1, 3.0), (2, 1.0), (2, 0.1)):
+        q = rows(p.rng, n, 4 * group * dh, spread)
+        one, two = (call(p, q, slot, n, average, b, group=group, lam=0.7)[1] for b in (False, True))
+        assert torch.equal(one.bfloat16(), two)
+    hgf.check_status()
