@@ -443,8 +443,9 @@ hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slots, int64_t 
  *        n_heads / cache->n_heads neighbouring heads share a K/V head
  *   out  [n_rows][n_heads * head_dim]      fp32, or bfloat16 with HGF_FLAG_OUT_BF16
  *   workspace  hgf_cached_workspace_bytes(...) bytes (0.2 to 0.4 MB for single tokens, up to 43 for many rows), 256-byte aligned; scratch, which calls that may overlap on the device do not share
- * Scores come from q to 2^-22 of the row's largest magnitude; probabilities enter the second product to 2^-24 of the largest in their page (of
- * more than 80 rows times heads of a group a sequence, with bf16 output: 2^-16 of themselves); all sums are exact integers or fp32.
+ * Scores come from q to 2^-22 of the row's largest magnitude; probabilities enter the second product to 2^-24 of the largest in their page; sums
+ * are exact integers or fp32, of more than 80 rows times heads of a group a sequence cut off instead of rounded within eight pages (2^-26 of themselves a
+ * term of sixteen tokens on average).  The output's type says how the output is rounded, and nothing of how it is computed.
  * A query row, a block or an open value of V that is not finite gives outputs that are not finite in the rows that see tokens, it or one of its tokens (an
  * open value in its dim only), and in no others.  An infinite score of an open key is no weight if it is negative, else NaN.
  * (Scores are expected within binary32's range, and the largest |v| of a block at 0 or between 2^-90 and 2^100: outside, the lower digits

@@ -14,7 +14,7 @@
 // The accumulators start at the bits of 1.5 * 2^23, so that a sum, below 2^22 in magnitude, is a float after one subtraction: I2F runs at an eighth
 // of the FMA rate and bounded the kernel.  The open tokens' bf16 go through bf16 products, with the probabilities as sums of three bf16.
 //
-// Four forms.  Many rows with bf16 output, or 64 wide, are tcgen05 products (hgf_cached_attention_tc.cuh).  Here ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.  There
+// Four forms.  Many rows are tcgen05 products (hgf_cached_attention_tc.cuh).  Here ROWS = 1, for single tokens with heads of their own: a warp is a team, both streams' digits fit the eight columns of one product.  There
 // and with ROWS = 8, a few tokens or heads that share K and V, the codes are the left operand, tokens (or dims) as its rows; eight query rows are the
 // columns of a product for each digit, and a team is a warp for each stream.  ROWS = 16, for more: sixteen query rows are the left operand and the
 // codes the right one (a lane's sixteen bytes are the same either way round); a warp takes one stream of one tile of sixteen rows, and a team is the
@@ -29,8 +29,6 @@
 //                   a scheduler (0.29 instructions issued a clock; 890 a page, stream and sixteen rows, 96 of them products; integer tensor pipe 25 % busy).
 //                   Tiles of eight rows against sixteen: one sequence of 59361 tokens, two heads a K/V head, 128 wide 71 and 110 us; with sixteen warps instead of
 //                   eight for those, 64 wide, 51 and 49 (13 sequences of 5 tokens 13.6 and 9.9)
-#include <algorithm>
-
 #include "hgf_cache.cuh"
 #include "hgf_warp.cuh"
 
@@ -189,8 +187,9 @@ struct CaSum {
             m[s] = now;
         }
     }
-    __device__ __forceinline__ void add_part(const float *part, int dh, int dim) {
-        add(*reinterpret_cast<const float4 *>(part), *reinterpret_cast<const float4 *>(part + 4 + dim), *reinterpret_cast<const float4 *>(part + 4 + dh + dim));
+    __device__ __forceinline__ void add_part(const float *part, int dh, int dim, int fours = 1) {  // (each four floats of a part `fours` of such from the last)
+        const float4 *at = reinterpret_cast<const float4 *>(part);
+        add(*at, at[(1 + (dim >> 2)) * fours], at[(1 + ((dh + dim) >> 2)) * fours]);
     }
     __device__ __forceinline__ void store_part(float *part, int dh, int dim, bool first) const {
         if (first) *reinterpret_cast<float4 *>(part) = make_float4(m[0], l[0], m[1], l[1]);
@@ -1195,22 +1194,23 @@ __global__ void __launch_bounds__(CaCfg<DH, ROWS>::THREADS, 1) cached_attention_
 }
 
 // Joins the parts of the items that several CTAs shared: block w the one that begins in CTA w's share and does not end there, if there is one; eight rows
-// each.  A single row's parts, which can be as many as there are CTAs, are dealt to eight groups of threads.
-template <int DH, int ROWS>
+// each.  A single row's parts, which can be as many as there are CTAs, are dealt to eight groups of threads.  ROWS_BESIDE: of a part sixteen bytes of each row, then
+// the next sixteen of each (the tcgen05 form), else row after row.
+template <int DH, int ROWS, bool ROWS_BESIDE>
 __global__ void __launch_bounds__(8 * DH / 4) cached_attention_join_kernel(CaParams p) {
     constexpr int PART = 4 + 2 * DH, FOURS = DH / 4;
     __shared__ __align__(16) float smem[ROWS == 1 ? 8 * PART : 4];
-    const int w0 = blockIdx.x, group = threadIdx.x / FOURS, dim = threadIdx.x % FOURS * 4, all = ROWS * p.tiles, part_floats = all * PART;
+    const int w0 = blockIdx.x, group = ROWS_BESIDE ? threadIdx.x % 8 : threadIdx.x / FOURS, dim = (ROWS_BESIDE ? threadIdx.x / 8 : threadIdx.x % FOURS) * 4, all = ROWS * p.tiles, part_floats = all * PART;
     pdl_wait();
     const int4 item = p.items[2 * w0], at = p.items[2 * w0 + 1];
     if (!item.x) return;
     const CaItem it = {0, 0, at.x, at.y, item.z, item.w};
     const int r = ROWS == 1 ? 0 : 8 * blockIdx.y + group, n = item.y - w0 + 1;
     if (r >= it.m * p.group - it.tile * all) return;
-    const float *base = p.cta_parts + (size_t)w0 * 2 * part_floats + r * PART;
+    const float *base = p.cta_parts + (size_t)w0 * 2 * part_floats + r * (ROWS_BESIDE ? 4 : PART);
     CaSum sum;
 #pragma unroll 4
-    for (int j = ROWS == 1 ? group : 0; j < n; j += ROWS == 1 ? 8 : 1) sum.add_part(base + (size_t)j * 2 * part_floats + (j == 0 && item.x == 2 ? part_floats : 0), DH, dim);
+    for (int j = ROWS == 1 ? group : 0; j < n; j += ROWS == 1 ? 8 : 1) sum.add_part(base + (size_t)j * 2 * part_floats + (j == 0 && item.x == 2 ? part_floats : 0), DH, dim, ROWS_BESIDE ? all : 1);
     if (ROWS == 1) {
         sum.store_part(smem + group * PART, DH, dim, dim == 0);
         __syncthreads();
@@ -1222,18 +1222,18 @@ __global__ void __launch_bounds__(8 * DH / 4) cached_attention_join_kernel(CaPar
 }
 
 // How a call's rows are dealt.  One row an item where they are single tokens with heads of their own, else tiles of eight rows where the sequences have up
-// to that many on average, else of sixteen, two to a team where they have more than that; with bf16 output or 64 wide of 128 where they have more than 80 (any call is right
-// in any of these forms; the sequences' lengths are on the device).
+// to that many on average, else of sixteen, two to a team where they have more than that, of 128 where they have more than 80 (any call is right
+// in any of these forms; the sequences' lengths are on the device).  The output's type has no say, so that it says nothing but how the output is rounded.
 struct CaForm {
     int rows, tiles, teams, stages, threads;
 };
-static CaForm ca_form(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int n_heads, bool bf16) {
+static CaForm ca_form(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int n_heads) {
     const bool narrow = cache->head_dim == 64;
     const int group = n_heads / cache->n_heads;
-    // (100 rows of 1000 tokens, 8 sequences, 16 heads of 64: 49.8 us here, 49.8 in tiles of sixteen; 256 rows of 6000 tokens 77 and 145; but 64 rows of 4096 tokens,
+    // (256 rows of 6000 tokens, 2 sequences, 16 heads of 64: 91 us here, 157 in tiles of sixteen; but 64 rows of 4096 tokens,
     // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty.  A pool of fewer pages than sequences holds some tens of tokens each, where an item's
     // beginning and end count: 121 sequences of up to 80 tokens, 60 rows of four heads a K/V head, 334 and 281; but 40 of up to 190, 190 rows, 108 and 137.)
-    if ((bf16 || narrow) && n_rows * group > 80 * n_seqs && cache->n_pages >= n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
+    if (n_rows * group > 80 * n_seqs && cache->n_pages >= n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
     if (n_rows * group <= n_seqs) return narrow ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
     if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 4, 4, 256} : CaForm{8, 1, 4, 2, 256};
     const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;
@@ -1241,7 +1241,7 @@ static CaForm ca_form(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, in
 }
 
 // `kernel` and the joining of its parts, which are of tiles of p.tiles * ROWS rows.
-template <int DH, int ROWS>
+template <int DH, int ROWS, bool ROWS_BESIDE>
 static cudaError_t launch_with_join(void (*kernel)(CaParams), size_t smem, std::atomic<unsigned long long> &attr_done, const CaParams &p, int threads, cudaStream_t stream) {
     cudaError_t e = ensure_dynamic_smem(kernel, smem, attr_done);
     if (e != cudaSuccess) return e;
@@ -1263,7 +1263,7 @@ static cudaError_t launch_with_join(void (*kernel)(CaParams), size_t smem, std::
     cfg.dynamicSmemBytes = 0;
     cfg.gridDim = dim3((unsigned)grid, (unsigned)(ROWS == 16 ? 2 * p.tiles : 1));
     cfg.blockDim = dim3(8 * DH / 4);
-    e = cudaLaunchKernelEx(&cfg, cached_attention_join_kernel<DH, ROWS>, p);
+    e = cudaLaunchKernelEx(&cfg, cached_attention_join_kernel<DH, ROWS, ROWS_BESIDE>, p);
     if (e != cudaSuccess) return e;
     count_launch(2);
     return cudaSuccess;
@@ -1273,12 +1273,12 @@ static cudaError_t launch_cached_attention(const CaParams &p, int threads, cudaS
     using C = CaCfg<DH, ROWS>;
     static_assert(C::SMEM <= 226 * 1024, "shared memory of a CTA");
     static std::atomic<unsigned long long> attr_done{0};
-    return launch_with_join<DH, ROWS>(cached_attention_kernel<DH, ROWS>, C::SMEM, attr_done, p, threads, stream);
+    return launch_with_join<DH, ROWS, false>(cached_attention_kernel<DH, ROWS>, C::SMEM, attr_done, p, threads, stream);
 }
-template <int DH, int PARTS>
+template <int DH>
 static cudaError_t launch_cached_attention_tc(const CaParams &p, int threads, cudaStream_t stream) {
     static std::atomic<unsigned long long> attr_done{0};
-    return launch_with_join<DH, 16>(cached_attention_tc_kernel<DH, PARTS>, CtCfg<DH, PARTS>::SMEM, attr_done, p, threads, stream);
+    return launch_with_join<DH, 16, true>(cached_attention_tc_kernel<DH>, CtCfg<DH>::SMEM, attr_done, p, threads, stream);
 }
 
 static size_t ca_items_bytes() { return align_up((size_t)kCaMaxSms * 2 * sizeof(int4), 256); }
@@ -1293,9 +1293,7 @@ using namespace hgf;
 
 extern "C" size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads) {
     if (!cache || (cache->head_dim != 64 && cache->head_dim != 128) || cache->n_heads <= 0 || n_heads <= 0 || n_rows <= 0 || n_seqs <= 0) return 256;
-    size_t bytes = 0;  // (of either type of output)
-    for (const bool bf16 : {false, true}) bytes = std::max(bytes, ca_workspace(cache->head_dim, ca_form(cache, n_seqs, n_rows, n_heads, bf16)));
-    return bytes;
+    return ca_workspace(cache->head_dim, ca_form(cache, n_seqs, n_rows, n_heads));
 }
 
 extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const void *q, int64_t n_rows, int32_t n_heads, const int32_t *slots,
@@ -1307,7 +1305,7 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     if (n_heads % cache->n_heads || n_heads > 65535 || n_rows > (1 << 24) || n_rows * (n_heads / cache->n_heads) > 0x3fffffffll) return HGF_ERR_UNSUPPORTED_SHAPE;
     if (((uintptr_t)q | (uintptr_t)out) & 15u) return HGF_ERR_MISALIGNED;
     const int group = n_heads / cache->n_heads, dh = cache->head_dim;
-    const CaForm f = ca_form(cache, n_seqs, n_rows, n_heads, (flags & HGF_FLAG_OUT_BF16) != 0);
+    const CaForm f = ca_form(cache, n_seqs, n_rows, n_heads);
     if (!workspace || workspace_bytes < ca_workspace(dh, f)) return HGF_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255u) return HGF_ERR_MISALIGNED;
     p.q = (const __nv_bfloat16 *)q;
@@ -1333,7 +1331,7 @@ extern "C" hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const vo
     const cudaStream_t stream = (cudaStream_t)stream_;
     cudaError_t e;
     auto launch = [&](auto narrow, auto wide) { return (dh == 64 ? narrow : wide)(p, f.threads, stream); };
-    if (!f.stages) e = p.bf16 ? launch(launch_cached_attention_tc<64, 2>, launch_cached_attention_tc<128, 2>) : launch_cached_attention_tc<64, 3>(p, f.threads, stream);
+    if (!f.stages) e = launch(launch_cached_attention_tc<64>, launch_cached_attention_tc<128>);
     else if (f.rows == 1) e = launch(launch_cached_attention<64, 1>, launch_cached_attention<128, 1>);
     else if (f.rows == 8) e = launch(launch_cached_attention<64, 8>, launch_cached_attention<128, 8>);
     else e = launch(launch_cached_attention<64, 16>, launch_cached_attention<128, 16>);

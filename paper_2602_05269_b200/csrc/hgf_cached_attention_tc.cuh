@@ -1,4 +1,4 @@
-// Cached differential attention of many rows a sequence, with bf16 output or 64 wide, on tcgen05 (included by hgf_cached_attention.cu).
+// Cached differential attention of many rows a sequence, on tcgen05 (included by hgf_cached_attention.cu).
 //
 // An item is 128 rows (row: token times heads of the group) of a sequence and K/V head, a step one page of 64 tokens (the open tokens are one step more).
 // All items' steps are one sequence, dealt in equal shares to one CTA an SM: a CTA walks segments, each the steps of one item that lie in its share; a
@@ -9,16 +9,21 @@
 //                have them; V lies transposed in a page, so both operands have their contraction index contiguous
 //   warps 12, 13 issue the products of a stream each: S = Q K^T of the codes, and O += P V of the codes
 //   warps 4-7    softmax of stream 1, warps 8-11 of stream 2: a thread owns a row; scores times the page's scale of K, the page's scale of V in the exponent
-// With bf16 output a probability enters the second product as a sum of two bf16, off by 2^-16 of itself at most, beside the output's 2^-8; with fp32 output as
-// three, 2^-24.  For a third part tensor memory has room 64 wide only.  All sums are fp32.
+// A probability enters the second product as a sum of three bf16, off by 2^-24 of itself at most, whatever the output's type.  All sums are fp32.  The products' are cut
+// off, not rounded, and lose 2^-26 of themselves with each addition (4.4e-6 after 41 steps), so every eight steps they are added up elsewhere and begin anew: in
+// shared memory 64 wide, else in the room that the CTA has in the workspace for parts, whose place is free until the part is.
+// Tensor memory (512 columns) holds scores and probabilities of two steps a stream beside O 64 wide.  128 wide O takes 256 of them, and a step's
+// scores and probabilities 96 (the third parts behind the 64 that scores and the others share): one step a stream, whose scores follow P V of the step before.
 //
 // What bounds it is the instructions: 1500 a step and scheduler, of them 340 in each softmax warp's 64 x 32 probabilities and 350 in a converting warp, and
 // their fetching, as the roles' loops together are longer than what a scheduler keeps (41 to 54 % of the issue slots used; tensor pipe 20 to 26 %,
 // exponentials 20 to 34 %, memory 3 to 5 %).
-// Measured, 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 145 us with the int8 form, 77 us here; 8 K/V heads with four query heads each, 30000 tokens,
-// 128 rows: 438 and 174 us; the first with fp32 output 157 and 91 us; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 157 and 101 us.  Steps: codes from global memory into registers 81 us (of the
-// first), with the bulk copies and segments kept in registers 85 (spills went to the L2 cache), segments in shared memory 76, V's scale in the exponent 74, scores relative to the step's largest first 77; two
-// converting warps of a larger share of registers 99.
+// Measured, calls back to back, either type of output: 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 100 us; 8 K/V heads with four query heads each, 30000
+// tokens, 128 rows: 217; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 117; one of 30000, 512 rows: 349 (the last two with the int8 form 208 and 705).
+// With probabilities in two parts, 16 bits, and sums that run on 64 steps (off by 7.5e-6 after 30000 tokens, growing with the length; plain fp32 3.9e-6, here 1.4e-6) 85, 171, 98 and
+// 275.  Steps (the first case in fp32): codes from global memory into registers, segments kept in registers (spills went to the L2 cache) 99;
+// segments in shared memory 91; the parts' sixteen bytes of neighbouring rows side by side 104 -> 100 (sequences of one length; the third case 155 -> 117);
+// two converting warps of a larger share of registers 99 for 82.
 #pragma once
 #include "hgf_tc.cuh"
 
@@ -28,29 +33,29 @@ constexpr int kCtRows = 128, kCtThreads = 480;
 constexpr int kCtFlush = 8;  // a power of two
 constexpr float kCtSlack = 8.0f, kCtNone = -3e38f;  // (a maximum of nothing: finite, so that differences of two are zero)
 
-template <int DH, int PARTS>
+template <int DH>
 struct CtCfg {
-    static constexpr int NBLK = DH / 64, KST = DH == 128 ? 2 : PARTS == 2 ? 4 : 3, GST = DH == 128 ? 2 : PARTS == 2 ? 4 : 3, NQ = DH == 64 && PARTS == 2 ? 2 : 1, NO = NQ;  // stages of the operands, of the pages; buffers of query tiles, of O_1 and O_2
+    static constexpr int NBLK = DH / 64, KST = DH == 128 ? 2 : 3, GST = KST, NS = DH == 128 ? 1 : 2;  // stages of the operands, of the pages (as many as shared memory takes); scores a stream
     static constexpr int Q_BYTES = NBLK * kCtRows * 128, K_BYTES = NBLK * kCacheBlock * 128, V_BYTES = DH * 128;
-    static constexpr int OFF_K = NQ * 2 * Q_BYTES, OFF_V = OFF_K + KST * 2 * K_BYTES, OFF_G = OFF_V + KST * V_BYTES,
+    static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + KST * 2 * K_BYTES, OFF_G = OFF_V + KST * V_BYTES,
                          UNIT = 3 * kCacheBlock * DH, G_BYTES = (UNIT + 16 + 127) / 128 * 128, OFF_BAR = OFF_G + GST * G_BYTES;
-    static constexpr int BAR_QFULL = 0, BAR_QEMPTY = 2, BAR_OEMPTY = 4, BAR_L = 6, BAR_END = 8, BAR_KFULL = 10, BAR_KEMPTY = BAR_KFULL + KST, BAR_VFULL = BAR_KEMPTY + KST,
+    static constexpr int BAR_QFULL = 0, BAR_QEMPTY = 1, BAR_OEMPTY = 2, BAR_L = 3, BAR_END = 5, BAR_KFULL = 7, BAR_KEMPTY = BAR_KFULL + KST, BAR_VFULL = BAR_KEMPTY + KST,
                          BAR_VEMPTY = BAR_VFULL + KST, BAR_SFULL = BAR_VEMPTY + KST /* [stream][buffer] */, BAR_PFULL = BAR_SFULL + 4, BAR_GFULL = BAR_PFULL + 4, BAR_GEMPTY = BAR_GFULL + GST,
                          BAR_COUNT = BAR_GEMPTY + GST;
     static constexpr int OFF_SCALES = OFF_BAR + 384;             // [8] float4: K1, K2, V of step g % 8
     static constexpr int OFF_ODD = OFF_SCALES + 128;             // [8][4] ints: of segment % 8, a warp found open values that are not finite
     static constexpr int OFF_L = OFF_ODD + 128;                  // [2][2][128] floats
     static constexpr int OFF_F = OFF_L + 2 * 2 * kCtRows * 4;    // [2][2][128] floats
-    static constexpr int OFF_ACC = OFF_F + 2 * 2 * kCtRows * 4;  // (three parts) [2][128][DH] floats, sixteen bytes c of row r at place c ^ (r & 7)
-    static constexpr int OFF_PREFIX = OFF_ACC + (PARTS == 3 ? 2 * kCtRows * DH * 4 : 0);
+    static constexpr int OFF_ACC = OFF_F + 2 * 2 * kCtRows * 4;  // (64 wide) [2][128][64] floats, sixteen bytes c of row r at place c ^ (r & 7)
+    static constexpr int OFF_PREFIX = OFF_ACC + (DH == 64 ? 2 * kCtRows * DH * 4 : 0);
     static constexpr int SMEM = OFF_PREFIX + (kCacheMaxSeqs + 2) * 8 + 1024;
-    static constexpr int COL_S = 0, COL_O = 4 * kCacheBlock, COL_P3 = COL_O + NO * 2 * DH;
-    // (as many stages as shared memory takes; four of the operands instead of three 180 -> 174 us of the second case above)
-    // (scores: + (2 stream + buffer) 64; O: + (2 buffer + stream) DH; third parts of the probabilities: + (2 stream + buffer) 32)
+    static constexpr int COL_O = 256;  // O: + stream DH
+    static __host__ __device__ constexpr int col_s(int stream, int buf) { return NS == 2 ? (2 * stream + buf) * 64 : stream * 96; }                      // scores, and the probabilities' first and second parts
+    static __host__ __device__ constexpr int col_p3(int stream, int buf) { return NS == 2 ? COL_O + 2 * DH + (2 * stream + buf) * 32 : stream * 96 + 64; }  // their third parts
     static constexpr int PART = 4 + 2 * DH;
     static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCacheBlock >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kCtRows >> 4) << 24);
-    static_assert(BAR_COUNT * 8 + 16 <= 384 && COL_P3 + (PARTS == 3 ? 128 : 0) <= 512 && SMEM <= 226 * 1024, "barriers, tensor and shared memory");
+    static_assert(BAR_COUNT * 8 + 16 <= 384 && COL_O + 2 * DH + (NS == 2 ? 128 : 0) <= 512 && SMEM <= 226 * 1024, "barriers, tensor and shared memory");
 };
 
 __device__ __forceinline__ CaSeq ct_sequence(const CaParams &p, int i) {
@@ -116,16 +121,10 @@ __device__ __forceinline__ uint2 ct_bf16(uint32_t codes) {
     return make_uint2(r[0], r[1]);
 }
 
-__device__ __forceinline__ float lg2_approx(float x) {
-    float y;
-    asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
-    return y;
-}
-
-template <int DH, int PARTS>
+template <int DH>
 __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaParams p) {
-    using C = CtCfg<DH, PARTS>;
-    constexpr int KV = kCacheBlock;
+    using C = CtCfg<DH>;
+    constexpr int KV = kCacheBlock, NS = C::NS;
     extern __shared__ uint8_t ct_smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)ct_smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t sbase = smem_u32(smem), bar0 = sbase + C::OFF_BAR;
@@ -145,10 +144,10 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, H = p.c.H;
 
     if (tid == 0) {
+        mbar_init(bar(C::BAR_QFULL), 4);
+        mbar_init(bar(C::BAR_QEMPTY), 2);  // a commit from each issuer
+        mbar_init(bar(C::BAR_OEMPTY), 8);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(C::BAR_QFULL + i), 4);
-            mbar_init(bar(C::BAR_QEMPTY + i), 2);  // a commit from each issuer
-            mbar_init(bar(C::BAR_OEMPTY + i), 8);
             mbar_init(bar(C::BAR_L + i), 8);
             mbar_init(bar(C::BAR_END + i), 1);
         }
@@ -217,7 +216,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         for (int i = blockIdx.x; i < p.n_seqs; i += gridDim.x) {
             const CaSeq s = ct_sequence(p, i);
             const size_t at = (size_t)s.row0 * width, n = (size_t)max(s.m - s.length, 0) * width;
-            if (PARTS == 2) for (size_t e = 8 * tid; e < n; e += 8 * kCtThreads) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
+            if (p.bf16) for (size_t e = 8 * tid; e < n; e += 8 * kCtThreads) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
             else for (size_t e = 4 * tid; e < n; e += 4 * kCtThreads) *reinterpret_cast<uint4 *>(reinterpret_cast<float *>(p.out) + at + e) = make_uint4(0, 0, 0, 0);
         }
     }
@@ -247,11 +246,8 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             if (lane == 0) mbar_arrive(bar(i));
         };
         constexpr int KN = DH / 16, VN = DH / 32;  // tiles of 16 x 32 codes of a warp: of K, of V
-        // (Instructions are fetched from afar - a third of all waits - and the less code the loops have the better, but for the form with the shortest steps: 2 x 256
-        // rows of 6000 tokens with fp32 output 96 us unrolled, 89 not; 4 x 128 rows of 8192 tokens 128 wide 107 and 99; 128 rows of 30000 tokens, bf16, 173 and 186.)
-        constexpr int KU = DH == 64 && PARTS == 2 ? KN : 1, VU = DH == 64 && PARTS == 2 ? VN : 1;
         bool ok = true;
-        int ks = 0, vs = 0, gs = 0, qb = 0, g = 0, segment = 0;
+        int ks = 0, vs = 0, gs = 0, g = 0, segment = 0;
         uint32_t kph = 1, vph = 1, gph = 0, qph = 1;
         CtSegment &seg = segments[warp];
         first_segment(seg);
@@ -268,7 +264,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     *reinterpret_cast<uint2 *>(rows + row * 128 + ((chunk ^ g4) << 4) + (t & 1) * 8) = ct_bf16(w[i]);
                 }
             };
-            if (!(ok = wait(C::BAR_QEMPTY + qb, qph, 0xc10u + qb))) break;
+            if (!(ok = wait(C::BAR_QEMPTY, qph, 0xc10u))) break;
             {
                 const int at = seg.tile * kCtRows + tid, token = p.group == 1 ? at : at / p.group;
                 const bool in = token < seg.s.m;
@@ -276,15 +272,15 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
                     const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (row + (size_t)st * H * p.group) * DH);
-                    uint8_t *dst = smem + (2 * qb + st) * C::Q_BYTES + tid * 128;
+                    uint8_t *dst = smem + st * C::Q_BYTES + tid * 128;
                     uint4 v[DH / 8];
 #pragma unroll
                     for (int c = 0; c < DH / 8; ++c) v[c] = in ? src[c] : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int c = 0; c < DH / 8; ++c) *reinterpret_cast<uint4 *>(dst + (c >> 3) * kCtRows * 128 + (((c & 7) ^ (tid & 7)) << 4)) = v[c];
                 }
-                there(C::BAR_QFULL + qb);
-                if (++qb == C::NQ) { qb = 0; qph ^= 1u; }
+                there(C::BAR_QFULL);
+                qph ^= 1u;
             }
             for (int j = first; j < stop; ++j, ++g) {
                 const bool page = j < pages;
@@ -296,7 +292,9 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (!(ok = wait(C::BAR_KEMPTY + ks, kph, 0xc20u + ks))) break;
                 uint8_t *k = smem + C::OFF_K + ks * 2 * C::K_BYTES;
                 if (page) {
-#pragma unroll KU
+                    // (Not unrolled: instructions are fetched from afar - a third of all waits - and the less code the loops have the better.  2 x 256 rows of 6000
+                    // tokens 96 us unrolled, 89 not; 4 x 128 rows of 8192 tokens 128 wide 107 and 99.)
+#pragma unroll 1
                     for (int i = 0; i < KN; ++i) {  // tile n of stream n / (4 KT): sixteen tokens, 32 dims
                         const int n = 4 * i + warp, stream = n / (DH / 8), mt = n % (DH / 8) / (DH / 32), kt = n % (DH / 32);
                         store(k + stream * C::K_BYTES + (kt >> 1) * KV * 128, mt * 16, (kt & 1) * 4, good ? codes[n * 32] : make_uint4(0, 0, 0, 0));
@@ -314,7 +312,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (!(ok = wait(C::BAR_VEMPTY + vs, vph, 0xc30u + vs))) break;
                 uint8_t *v = smem + C::OFF_V + vs * C::V_BYTES;
                 if (page) {
-#pragma unroll VU
+#pragma unroll 1
                     for (int i = 0; i < VN; ++i) {  // sixteen dims, 32 tokens
                         const int n = 4 * i + warp;
                         store(v, (n >> 1) * 16, (n & 1) * 4, good ? codes[(4 * KN + n) * 32] : make_uint4(0, 0, 0, 0));
@@ -392,10 +390,9 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         const int st = warp - 12;
         auto wait = [&](int i, uint32_t par, unsigned int code) { return __all_sync(0xffffffffu, mbar_wait_poll(bar(i), par, abort_flag, p.status, code)) != 0; };
         const uint64_t q_desc = make_sw128_desc(sbase + st * C::Q_BYTES), k_desc = make_sw128_desc(sbase + C::OFF_K + st * C::K_BYTES), v_desc = make_sw128_desc(sbase + C::OFF_V);
-        const uint32_t s_col = tmem_base + C::COL_S + 2 * st * KV;
-        // The scores run two steps ahead of P V: the products execute in order, so P of a step has been read when the scores of two steps on replace it.
+        // The scores run NS steps ahead of P V: the products execute in order, so P of a step has been read when the scores of NS steps on replace it.
         bool ok = true, s_more = true, p_more = true;
-        int ks = 0, vs = 0, sqb = 0, pob = 0, g = 0, sj = 0;
+        int ks = 0, vs = 0, g = 0, sj = 0;
         uint32_t kph = 0, vph = 0, sqph = 0, poph = 1;
         CtSegment &sseg = segments[warp], &pseg = segments[warp - 12 + kCtThreads / 32];
         int s_first = 0, s_stop = 0, p_first = 0, p_stop = 0;
@@ -410,49 +407,50 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         full(pseg, p_more, p_first, p_stop);
         sj = s_first;
         auto next_scores = [&](int buf) {
-            if (sj == s_first && !wait(C::BAR_QFULL + sqb, sqph, 0xc40u + sqb)) return false;
+            if (sj == s_first && !wait(C::BAR_QFULL, sqph, 0xc40u)) return false;
             if (!wait(C::BAR_KFULL + ks, kph, 0xc48u + ks)) return false;
             tc_fence_after();
-            const uint64_t qd = q_desc + (uint64_t)(sqb * (2 * C::Q_BYTES >> 4)), kd = k_desc + (uint64_t)(ks * (2 * C::K_BYTES >> 4));
+            const uint64_t kd = k_desc + (uint64_t)(ks * (2 * C::K_BYTES >> 4));
 #pragma unroll
             for (int blk = 0; blk < C::NBLK; ++blk)
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)
-                    warp_mma_f16(s_col + buf * KV, qd + (uint64_t)(blk * (kCtRows * 128 >> 4) + 2 * kk), kd + (uint64_t)(blk * (KV * 128 >> 4) + 2 * kk), C::IDESC_S, (blk | kk) ? 1u : 0u);
-            warp_commit(bar(C::BAR_SFULL + 2 * st + buf));  // also: P V of two steps before is complete
+                    warp_mma_f16(tmem_base + C::col_s(st, buf), q_desc + (uint64_t)(blk * (kCtRows * 128 >> 4) + 2 * kk), kd + (uint64_t)(blk * (KV * 128 >> 4) + 2 * kk), C::IDESC_S, (blk | kk) ? 1u : 0u);
+            warp_commit(bar(C::BAR_SFULL + 2 * st + buf));  // also: P V of NS steps before is complete
             warp_commit(bar(C::BAR_KEMPTY + ks));
             if (++ks == C::KST) { ks = 0; kph ^= 1u; }
             if (++sj == s_stop) {
-                warp_commit(bar(C::BAR_QEMPTY + sqb));
-                if (++sqb == C::NQ) { sqb = 0; sqph ^= 1u; }
+                warp_commit(bar(C::BAR_QEMPTY));
+                sqph ^= 1u;
                 s_more = next_segment(sseg);
                 full(sseg, s_more, s_first, s_stop);
                 sj = s_first;
             }
             return true;
         };
-        for (int i = 0; ok && i < 2 && s_more; ++i) ok = next_scores(i);
+        for (int i = 0; ok && i < NS && s_more; ++i) ok = next_scores(i);
         while (ok && p_more) {
-            if (!(ok = wait(C::BAR_OEMPTY + pob, poph, 0xc50u + pob))) break;
-            const uint32_t o_col = tmem_base + C::COL_O + (2 * pob + st) * DH;
+            if (!(ok = wait(C::BAR_OEMPTY, poph, 0xc50u))) break;
+            poph ^= 1u;
+            const uint32_t o_col = tmem_base + C::COL_O + st * DH;
             for (int j = p_first; j < p_stop; ++j, ++g) {
-                const int buf = g & 1;
+                const int buf = NS == 2 ? g & 1 : 0;
                 if (!(ok = wait(C::BAR_VFULL + vs, vph, 0xc58u + vs))) break;
-                if (!(ok = wait(C::BAR_PFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xc60u + st))) break;
+                if (!(ok = wait(C::BAR_PFULL + 2 * st + buf, (uint32_t)(g >> (NS - 1)) & 1u, 0xc60u + st))) break;
                 tc_fence_after();
                 const uint64_t vd = v_desc + (uint64_t)(vs * (C::V_BYTES >> 4));
 #pragma unroll
-                for (int part = 0; part < PARTS; ++part)
+                for (int part = 0; part < 3; ++part)
 #pragma unroll
                     for (int kk = 0; kk < KV / 16; ++kk)
-                        warp_mma_f16_ts(o_col, (part < 2 ? s_col + buf * KV + 32 * part : tmem_base + C::COL_P3 + (2 * st + buf) * 32) + 8 * kk, vd + (uint64_t)(2 * kk), C::IDESC_PV, ((PARTS == 2 ? j != p_first : ((j - p_first) & (kCtFlush - 1)) != 0) || part || kk) ? 1u : 0u);
+                        warp_mma_f16_ts(o_col, tmem_base + (part < 2 ? C::col_s(st, buf) + 32 * part : C::col_p3(st, buf)) + 8 * kk, vd + (uint64_t)(2 * kk), C::IDESC_PV,
+                                        (((j - p_first) & (kCtFlush - 1)) != 0 || part || kk) ? 1u : 0u);
                 warp_commit(bar(C::BAR_VEMPTY + vs));
                 if (j + 1 == p_stop) warp_commit(bar(C::BAR_END + st));
                 if (++vs == C::KST) { vs = 0; vph ^= 1u; }
                 if (s_more) { if (!(ok = next_scores(buf))) break; }
                 else warp_commit(bar(C::BAR_SFULL + 2 * st + buf));
             }
-            if (++pob == C::NO) { pob = 0; poph ^= 1u; }
             p_more = next_segment(pseg);
             full(pseg, p_more, p_first, p_stop);
         }
@@ -462,56 +460,65 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
         const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16);
         auto wait = [&](int i, uint32_t par, unsigned int code) { return __all_sync(0xffffffffu, mbar_wait_poll(bar(i), par, abort_flag, p.status, code)) != 0; };
         bool ok = true, more = true;
-        int g = 0, ob = 0, segment = 0;
-        auto acc_at = [&](int stream, int c) { return reinterpret_cast<float4 *>(smem + C::OFF_ACC + ((size_t)stream * kCtRows + row) * DH * 4 + ((c ^ (row & 7)) << 4)); };
+        int g = 0, segment = 0;
         CtSegment &seg = segments[warp];
         first_segment(seg);
         for (; ok && more; more = next_segment(seg)) {
             const int first = seg.unit, stop = seg.stop(), at = seg.tile * kCtRows + row, token = p.group == 1 ? at : at / p.group;
             const int sees = token < seg.s.m ? seg.s.length - seg.s.m + 1 + token : 0;
             const bool whole = seg.whole();
-            auto part_at = [&] { return p.cta_parts + (((size_t)blockIdx.x * 2 + (seg.u - seg.unit > c0)) * kCtRows + row) * C::PART; };
+            // The row's place for the segment as a part: the CTA's first if the item begins in front of the share or with it (then it is the first segment), else the
+            // second, which the last segment alone can need as a part.
+            // Sixteen bytes of a row lie kCtRows * 16 bytes apart, those of neighbouring rows side by side, as neighbouring threads have them.
+            float4 *const part = reinterpret_cast<float4 *>(p.cta_parts + ((size_t)blockIdx.x * 2 + (seg.u - seg.unit > c0)) * kCtRows * C::PART) + row;
+            auto sums_at = [&](int stream, int c) { return part + (1 + stream * (DH / 4) + c) * kCtRows; };
+            auto put_ml = [&](float m, float l) { reinterpret_cast<float2 *>(part)[st] = make_float2(m, l); };
+            auto acc_at = [&](int stream, int c) {  // sixteen bytes of the row's sums from before the products' last new beginning
+                return DH == 64 ? reinterpret_cast<float4 *>(smem + C::OFF_ACC + ((size_t)stream * kCtRows + row) * DH * 4 + ((c ^ (row & 7)) << 4)) : sums_at(stream, c);
+            };
             if (const long long from = seg.u - seg.unit, to = from + seg.s.units; !whole && to > c1 && from >= c0 && warp == 4 && lane == 0) {
                 p.items[2 * blockIdx.x] = make_int4(from > c0 ? 2 : 1, ca_share_of(total, to - 1, ctas), seg.head, seg.tile);
                 p.items[2 * blockIdx.x + 1] = make_int4(seg.s.row0, seg.s.m, 0, 0);
             }
             if (first >= stop) {  // (never a whole item: its first step is visible)
-                float *part = part_at();
-                part[2 * st] = kCtNone;
-                part[2 * st + 1] = 0.0f;
-                for (int d = 0; d < DH; d += 4) *reinterpret_cast<float4 *>(part + 4 + st * DH + d) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                put_ml(kCtNone, 0.0f);
+                for (int c = 0; c < DH / 4; ++c) *sums_at(st, c) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 continue;
             }
-            const uint32_t o_addr = lane_base + C::COL_O + (2 * ob + st) * DH;
+            const uint32_t o_addr = lane_base + C::COL_O + st * DH;
             float m = kCtNone;
             uint64_t l2 = 0;  // the row's sum, two partial sums
             float m_acc = kCtNone;
             bool flushed = false;
             for (int j = first; j < stop; ++j, ++g) {
-                const int buf = g & 1, n = sees - KV * j;  // n: of the step's tokens, those that the row sees
-                const uint32_t s_addr = lane_base + C::COL_S + (2 * st + buf) * KV;
-                if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> 1) & 1u, 0xc70u + st))) break;
+                const int buf = NS == 2 ? g & 1 : 0, n = sees - KV * j;  // n: of the step's tokens, those that the row sees
+                const uint32_t s_addr = lane_base + C::col_s(st, buf), p3_addr = lane_base + C::col_p3(st, buf);
+                if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> (NS - 1)) & 1u, 0xc70u + st))) break;
                 tc_fence_after();
-                if (PARTS == 3 && j > first && ((j - first) & (kCtFlush - 1)) == 0) {
-                    // The products' sums are cut off, not rounded, and lose 2^-25 of themselves with each addition: every kCtFlush steps they are added up here
-                    // instead and begin anew.  (Error against 64 bits after 41 steps without it
-                    // 4.4e-6 and 92 us, with it 1.3e-6 and 99 us, of 2 x 256 rows of 6000 tokens.)
-                    if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xc7cu + st))) break;
+                // O is at rest once P V of the step before is complete: the barrier of scores that were issued behind it says so, the step's own where a stream has
+                // one step of scores, else the next step's.
+                auto at_rest = [&](unsigned int code) {
+                    if (NS == 1) return true;
+                    if (!wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, code)) return false;
                     tc_fence_after();
+                    return true;
+                };
+                if (j > first && ((j - first) & (kCtFlush - 1)) == 0) {
+                    // (2 x 256 rows of 6000 tokens, error against 64 bits: 1.3e-6, without it 4.4e-6, and 92 us for 99)
+                    if (!(ok = at_rest(0xc7cu + st))) break;
                     const float beta = flushed ? exp2_approx(m_acc - m) : 0.0f;
 #pragma unroll
                     for (int cc = 0; cc < DH; cc += 16) {
                         uint32_t o[16];
+                        float4 a[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) a[u] = flushed ? *acc_at(st, (cc >> 2) + u) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                         tmem_ld16(o_addr + cc, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int u = 0; u < 16; u += 4) {
-                            float4 *a = acc_at(st, (cc + u) >> 2);
-                            float4 y = flushed ? *a : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                            y = make_float4(fmaf(y.x, beta, __uint_as_float(o[u])), fmaf(y.y, beta, __uint_as_float(o[u + 1])), fmaf(y.z, beta, __uint_as_float(o[u + 2])),
-                                            fmaf(y.w, beta, __uint_as_float(o[u + 3])));
-                            *a = y;
-                        }
+                        for (int u = 0; u < 4; ++u)
+                            *acc_at(st, (cc >> 2) + u) = make_float4(fmaf(a[u].x, beta, __uint_as_float(o[4 * u])), fmaf(a[u].y, beta, __uint_as_float(o[4 * u + 1])),
+                                                                     fmaf(a[u].z, beta, __uint_as_float(o[4 * u + 2])), fmaf(a[u].w, beta, __uint_as_float(o[4 * u + 3])));
                     }
                     m_acc = m;
                     flushed = true;
@@ -522,13 +529,13 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     for (int u = 0; u < 32; ++u) zero[u] = 0u;
                     tmem_st32(s_addr, zero);
                     tmem_st32(s_addr + 32, zero);
-                    if (PARTS == 3) tmem_st32(lane_base + C::COL_P3 + (2 * st + buf) * 32, zero);
+                    tmem_st32(p3_addr, zero);
                 } else {
                     const float4 sc = scales[g & 7];
                     // (a page of zeros has the factor 0, and what is masked has to stay at -inf; of a page that the row sees nothing of not even a NaN counts)
                     const float f = n > 0 ? p.scale_log2 * (st ? sc.y : sc.x) + 1.17549435e-38f : 1.0f;
-                    // The scale of V enters the exponent; the row's sum is multiplied by its inverse once a step.  (A page of zeros has the scale 0 and codes 0.)
-                    const float sv = n > 0 && sc.z != 0.0f ? sc.z : 1.0f, log_sv = PARTS == 2 ? lg2_approx(sv) : 0.0f;
+                    // (a page of zeros has the scale 0 and codes 0)
+                    const float sv = n > 0 && sc.z != 0.0f ? sc.z : 1.0f;
                     uint32_t v0[32], v1[32];
                     tmem_ld32(s_addr, v0);
                     tmem_ld32(s_addr + 32, v1);
@@ -552,9 +559,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     // The reference of the exponentials follows the maximum only where that has moved by more than kCtSlack, so O and l are rescaled rarely.
                     const float now = here - m > kCtSlack ? here : m;
                     if (j > first && __any_sync(0xffffffffu, now != m)) {
-                        // O is at rest once P V of the step before is complete: the barrier of the next step's scores follows it
-                        if (!(ok = wait(C::BAR_SFULL + 2 * st + (buf ^ 1), (uint32_t)((g + 1) >> 1) & 1u, 0xc78u + st))) break;
-                        tc_fence_after();
+                        if (!(ok = at_rest(0xc78u + st))) break;
                         const float alpha = exp2_approx(m - now);
                         const uint64_t a2 = pack_f32x2(alpha, alpha);
                         l2 = mul_f32x2(l2, a2);
@@ -569,10 +574,10 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                         }
                     }
                     m = now;
-                    const uint64_t f2 = pack_f32x2(f, f), minus = top == -INFINITY ? 0 : pack_f32x2(-top, -top), rest2 = pack_f32x2(here - m + log_sv, here - m + log_sv), minus1 = pack_f32x2(-1.0f, -1.0f), sv2 = pack_f32x2(sv, sv);
+                    const uint64_t f2 = pack_f32x2(f, f), minus = top == -INFINITY ? 0 : pack_f32x2(-top, -top), rest2 = pack_f32x2(here - m, here - m), minus1 = pack_f32x2(-1.0f, -1.0f), sv2 = pack_f32x2(sv, sv);
                     uint64_t sum_a = 0, sum_b = 0;
                     // (relative to the step's largest first, which is then exact however large the scores)
-                    // 32 scores -> their probabilities' first parts and second parts, sixteen columns each
+                    // 32 scores -> their probabilities, times the scale of V, in three parts, sixteen columns each
                     auto part_of = [&](const uint32_t (&v)[32], uint64_t &sum, int at) {
                         uint32_t hi[16], lo[16], third[16];
 #pragma unroll
@@ -581,26 +586,23 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                             unpack_f32x2(fma_f32x2(add_f32x2(pack_f32x2(__uint_as_float(v[2 * u]), __uint_as_float(v[2 * u + 1])), minus), f2, rest2), x0, x1);
                             uint64_t e = pack_f32x2(exp2_approx(x0), exp2_approx(x1));
                             sum = add_f32x2(sum, e);
-                            if (PARTS == 3) e = mul_f32x2(e, sv2);
+                            e = mul_f32x2(e, sv2);
                             unpack_f32x2(e, x0, x1);
                             const __nv_bfloat162 first = __floats2bfloat162_rn(x0, x1);
                             hi[u] = *reinterpret_cast<const uint32_t *>(&first);
                             unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(hi[u] << 16), __uint_as_float(hi[u] & 0xffff0000u)), minus1, e), x0, x1);
                             const __nv_bfloat162 second = __floats2bfloat162_rn(x0, x1);
                             lo[u] = *reinterpret_cast<const uint32_t *>(&second);
-                            if (PARTS == 3) {
-                                const __nv_bfloat162 rest = __floats2bfloat162_rn(x0 - __uint_as_float(lo[u] << 16), x1 - __uint_as_float(lo[u] & 0xffff0000u));
-                                third[u] = *reinterpret_cast<const uint32_t *>(&rest);
-                            }
+                            const __nv_bfloat162 rest = __floats2bfloat162_rn(x0 - __uint_as_float(lo[u] << 16), x1 - __uint_as_float(lo[u] & 0xffff0000u));
+                            third[u] = *reinterpret_cast<const uint32_t *>(&rest);
                         }
                         tmem_st16(s_addr + at, hi);
                         tmem_st16(s_addr + 32 + at, lo);
-                        if (PARTS == 3) tmem_st16(lane_base + C::COL_P3 + (2 * st + buf) * 32 + at, third);
+                        tmem_st16(p3_addr + at, third);
                     };
                     part_of(v0, sum_a, 0);
                     part_of(v1, sum_b, 16);
-                    const float back = PARTS == 2 ? __frcp_rn(sv) : 1.0f;
-                    l2 = fma_f32x2(add_f32x2(sum_a, sum_b), pack_f32x2(back, back), l2);
+                    l2 = add_f32x2(l2, add_f32x2(sum_a, sum_b));
                 }
                 tmem_st_wait();
                 tc_fence_before();
@@ -626,10 +628,10 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             const float flush_scale = flushed ? exp2_approx(m_acc - m) : 0.0f;
             if (whole) {
                 s_l[((segment & 1) * 2 + st) * kCtRows + row] = l;
-                if (PARTS == 3) s_f[((segment & 1) * 2 + st) * kCtRows + row] = flush_scale;
+                s_f[((segment & 1) * 2 + st) * kCtRows + row] = flush_scale;
             }
             auto add_flushed = [&](uint32_t (&v)[32], int stream, int cc, float scale) {
-                if (PARTS == 3 && scale != 0.0f) {
+                if (scale != 0.0f) {
 #pragma unroll
                     for (int u = 0; u < 32; u += 4) {
                         const float4 a = *acc_at(stream, (cc + u) >> 2);
@@ -650,7 +652,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 const float *sl = s_l + (segment & 1) * 2 * kCtRows;
                 const float l1 = sl[row], l2 = sl[kCtRows + row];
                 const float w1 = l1 != 0.0f ? p.out_scale / l1 : 0.0f, w2 = l2 != 0.0f ? p.out_scale * p.lambda / l2 : 0.0f;
-                const uint32_t o_base = lane_base + C::COL_O + 2 * ob * DH;
+                const uint32_t o_base = lane_base + C::COL_O;
                 const size_t out = ((size_t)(seg.s.row0 + token) * H * p.group + seg.head * p.group + at - token * p.group) * DH;
 #pragma unroll
                 for (int cc = st * (DH / 2); cc < (st + 1) * (DH / 2); cc += 32) {
@@ -663,7 +665,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     if (token >= seg.s.m) continue;
 #pragma unroll
                     for (int u = 0; u < 32; ++u) v1[u] = __float_as_uint(__uint_as_float(v1[u]) * w1 - __uint_as_float(v2[u]) * w2);
-                    if (PARTS == 2) {
+                    if (p.bf16) {
 #pragma unroll
                         for (int u = 0; u < 32; u += 8) {
                             uint32_t o[4];
@@ -682,14 +684,11 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 if (checked && token < seg.s.m)
                     for (int dim = st * (DH / 2); dim < (st + 1) * (DH / 2); ++dim)
                         if (not_finite(dim)) {
-                            if (PARTS == 2) reinterpret_cast<__nv_bfloat16 *>(p.out)[out + dim] = __ushort_as_bfloat16(0x7fc0);
+                            if (p.bf16) reinterpret_cast<__nv_bfloat16 *>(p.out)[out + dim] = __ushort_as_bfloat16(0x7fc0);
                             else reinterpret_cast<float *>(p.out)[out + dim] = __uint_as_float(0x7fc00000u);
                         }
             } else {
-                float *part = part_at();
-                part[2 * st] = m;
-                part[2 * st + 1] = l;
-                float *sums = part + 4 + st * DH;
+                put_ml(m, l);
 #pragma unroll
                 for (int cc = 0; cc < DH; cc += 32) {
                     uint32_t v[32];
@@ -697,16 +696,15 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     tmem_ld_wait();
                     add_flushed(v, st, cc, flush_scale);
 #pragma unroll
-                    for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4 *>(sums + cc + u) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
+                    for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4 *>(sums_at(st, (cc + u) >> 2)) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
                 }
                 if (checked)
                     for (int dim = 0; dim < DH; ++dim)
-                        if (not_finite(dim)) sums[dim] = __uint_as_float(0x7fc00000u);
+                        if (not_finite(dim)) reinterpret_cast<float *>(sums_at(st, dim >> 2))[dim & 3] = __uint_as_float(0x7fc00000u);
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(C::BAR_OEMPTY + ob));
-            if (++ob == C::NO) ob = 0;
+            if (lane == 0) mbar_arrive(bar(C::BAR_OEMPTY));
             ++segment;
         }
     }

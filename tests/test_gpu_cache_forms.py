@@ -1,4 +1,4 @@
-"""Cached attention (hgf_diff_attention_cached) gives the same answer in each of its forms: single tokens, tiles of eight and of sixteen rows.
+"""Cached attention (hgf_diff_attention_cached) gives the same answer in each of its forms: single tokens, tiles of eight, of sixteen and of 128 rows.
 
 Which form a call takes goes by its rows times the heads that share a K/V head, per entry of its list; entries -1 without rows set that average here."""
 import pytest
@@ -9,7 +9,7 @@ from test_gpu_cache import Pair, bf16, hgf, ints  # noqa: F401  (hgf is the fixt
 
 pytestmark = pytest.mark.gpu
 
-AVERAGES = [1, 8, 16, 32]
+AVERAGES = [1, 8, 16, 32, 300]
 
 
 def call(p, q, slot, n, average, out_bf16, group=1, lam=0.5):
@@ -27,7 +27,7 @@ def test_bf16_output_is_the_rounding_of_binary32(hgf, dh, group, average):  # no
     """The type of the output says how the output is rounded, and nothing of how it is computed."""
     p = Pair(hgf, 2, dh, n_pages=120, n_slots=3, max_pages=60)
     p.fill([700, 60, 3333])
-    n = {1: 60, 8: 5, 16: 9, 32: 40}[average]
+    n = {1: 60, 8: 5, 16: 9, 32: 40, 300: 130}[average]
     for slot, spread in ((0, 1.0), (1, 3.0), (2, 1.0), (2, 0.1)):
         q = rows(p.rng, n, 4 * group * dh, spread)
         one, two = (call(p, q, slot, n, average, b, group=group, lam=0.7)[1] for b in (False, True))
