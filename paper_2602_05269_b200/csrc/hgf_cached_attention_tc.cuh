@@ -42,7 +42,7 @@ struct CtCfg {
     static constexpr int BAR_QFULL = 0, BAR_QEMPTY = 1, BAR_OEMPTY = 2, BAR_L = 3, BAR_END = 5, BAR_KFULL = 7, BAR_KEMPTY = BAR_KFULL + KST, BAR_VFULL = BAR_KEMPTY + KST,
                          BAR_VEMPTY = BAR_VFULL + KST, BAR_SFULL = BAR_VEMPTY + KST /* [stream][buffer] */, BAR_PFULL = BAR_SFULL + 4, BAR_GFULL = BAR_PFULL + 4, BAR_GEMPTY = BAR_GFULL + GST,
                          BAR_COUNT = BAR_GEMPTY + GST;
-    static constexpr int OFF_SCALES = OFF_BAR + 384;             // [8] float4: K1, K2, V of step g % 8
+    static constexpr int OFF_SCALES = OFF_BAR + 384;             // [8] float4: K1, K2, V of step g % 8, and 0 where its page is none
     static constexpr int OFF_ODD = OFF_SCALES + 128;             // [8][4] ints: of segment % 8, a warp found open values that are not finite
     static constexpr int OFF_L = OFF_ODD + 128;                  // [2][2][128] floats
     static constexpr int OFF_F = OFF_L + 2 * 2 * kCtRows * 4;    // [2][2][128] floats
@@ -306,7 +306,11 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                         *reinterpret_cast<uint4 *>(k + stream * C::K_BYTES + (c >> 3) * KV * 128 + r * 128 + ((c & 7) << 4)) = r < rows ? open[e] : make_uint4(0, 0, 0, 0);
                     }
                 }
-                if (tid == 0) scales[g & 7] = !page ? make_float4(1.0f, 1.0f, 1.0f, 0.0f) : good ? *reinterpret_cast<const float4 *>(smem + C::OFF_G + gs * C::G_BYTES + C::UNIT) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (tid == 0) {
+                    float4 sc = page && good ? *reinterpret_cast<const float4 *>(smem + C::OFF_G + gs * C::G_BYTES + C::UNIT) : make_float4(1.0f, 1.0f, 1.0f, 0.0f);
+                    sc.w = page && !good ? 0.0f : 1.0f;
+                    scales[g & 7] = sc;
+                }
                 there(C::BAR_KFULL + ks);
                 if (++ks == C::KST) { ks = 0; kph ^= 1u; }
                 if (!(ok = wait(C::BAR_VEMPTY + vs, vph, 0xc30u + vs))) break;
@@ -491,10 +495,12 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             float m_acc = kCtNone;
             bool flushed = false;
             for (int j = first; j < stop; ++j, ++g) {
-                const int buf = NS == 2 ? g & 1 : 0, n = sees - KV * j;  // n: of the step's tokens, those that the row sees
+                const int buf = NS == 2 ? g & 1 : 0;
                 const uint32_t s_addr = lane_base + C::col_s(st, buf), p3_addr = lane_base + C::col_p3(st, buf);
                 if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> (NS - 1)) & 1u, 0xc70u + st))) break;
                 tc_fence_after();
+                const float4 sc = scales[g & 7];
+                const int n = sc.w != 0.0f ? sees - KV * j : 0;  // of the step's tokens, those that the row sees: none of a page whose number is out of range
                 // O is at rest once P V of the step before is complete: the barrier of scores that were issued behind it says so, the step's own where a stream has
                 // one step of scores, else the next step's.
                 auto at_rest = [&](unsigned int code) {
@@ -531,7 +537,6 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     tmem_st32(s_addr + 32, zero);
                     tmem_st32(p3_addr, zero);
                 } else {
-                    const float4 sc = scales[g & 7];
                     // (a page of zeros has the factor 0, and what is masked has to stay at -inf; of a page that the row sees nothing of not even a NaN counts)
                     const float f = n > 0 ? p.scale_log2 * (st ? sc.y : sc.x) + 1.17549435e-38f : 1.0f;
                     // (a page of zeros has the scale 0 and codes 0)

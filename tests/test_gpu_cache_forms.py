@@ -1,10 +1,12 @@
 """Cached attention (hgf_diff_attention_cached) gives the same answer in each of its forms: single tokens, tiles of eight, of sixteen and of 128 rows.
 
 Which form a call takes goes by its rows times the heads that share a K/V head, per entry of its list; entries -1 without rows set that average here."""
+import numpy as np
 import pytest
 import torch
 
-from cache_reference import rows
+from cache_reference import BLOCK, attention, rows
+from paper_2602_05269_b200.inputs import bf16_bits_to_f32
 from test_gpu_cache import Pair, bf16, hgf, ints  # noqa: F401  (hgf is the fixture)
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +35,33 @@ def test_bf16_output_is_the_rounding_of_binary32(hgf, dh, group, average):  # no
         one, two = (call(p, q, slot, n, average, b, group=group, lam=0.7)[1] for b in (False, True))
         assert torch.equal(one.bfloat16(), two)
     hgf.check_status()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("average", AVERAGES)
+@pytest.mark.parametrize("out_bf16", [False, True])
+def test_a_page_that_is_none_is_left_out(hgf, dh, average, out_bf16):  # noqa: F811
+    """Rows attend to the tokens of the pages that are there; with none of these and no open token a row is zero."""
+    H, n = 2, 100 if average == 300 else 5
+    p = Pair(hgf, H, dh, n_pages=20, n_slots=4)
+    p.fill([200, 64, 300, 70])
+    for slot, block in ((0, 1), (1, 0), (2, 3), (2, 0), (3, 0)):
+        length, good = len(p.ref.tokens[slot]), p.cache.table[slot, block].item()
+        q = rows(p.rng, n, 2 * H * dh)
+        qf = bf16_bits_to_f32(q).astype(np.float64).reshape(n, 2, H, dh)
+        kept = np.delete(np.arange(length), np.s_[block * BLOCK:(block + 1) * BLOCK])
+        for page in (-1, 20):
+            p.cache.table[slot, block] = page
+            got, _ = call(p, q, slot, n, average, out_bf16, lam=0.7)
+            with pytest.raises(hgf.HgfError) as e:
+                hgf.check_status()
+            assert e.value.status == 8
+            for j in range(n):
+                seen = kept[kept < length - n + j + 1]
+                if not len(seen):
+                    assert (got[j] == 0.0).all()
+                    continue
+                want, tol = attention(p.ref.values(slot)[:, :, seen], qf[j:j + 1], 1, H, 0.7, 1.0)
+                tol = tol[0][:, None] + (2.0 ** -8 * np.abs(want[0]) if out_bf16 else 0)   # (half a step of bf16)
+                assert (np.abs(got[j] - want[0]) <= tol).all()
+        p.cache.table[slot, block] = good
