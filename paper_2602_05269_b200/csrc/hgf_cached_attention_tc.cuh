@@ -132,6 +132,9 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::OFF_BAR + C::BAR_COUNT * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::OFF_BAR + C::BAR_COUNT * 8 + 4);
     __shared__ volatile int page_ok[C::GST];
+    // [segment % 4][stream][32 rows] of a segment's queries, those with a value that is not finite, a bit a row.  (Queries are written when the scores of the segment before
+    // are complete, so its softmax may be behind by the NS steps that scores run ahead, which can be NS segments.)
+    __shared__ volatile uint32_t odd_q[4][2][4];
     // A warp's segment lies in shared memory, where its first lane moves it on: in registers it costs every role sixteen of them, and what they spilled went
     // through the L2 cache, since the L1 has no room beside so much shared memory.
     __shared__ CtSegment segments[kCtThreads / 32 + 2];
@@ -278,6 +281,11 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     for (int c = 0; c < DH / 8; ++c) v[c] = in ? src[c] : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int c = 0; c < DH / 8; ++c) *reinterpret_cast<uint4 *>(dst + (c >> 3) * kCtRows * 128 + (((c & 7) ^ (tid & 7)) << 4)) = v[c];
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int c = 0; c < DH / 8; ++c) top = absmax8_bits(top, v[c]);
+                    const uint32_t which = __ballot_sync(0xffffffffu, max(top >> 16, top & 0xffffu) >= 0x7f80u);
+                    if (lane == 0) odd_q[segment & 3][st][warp] = which;
                 }
                 there(C::BAR_QFULL);
                 qph ^= 1u;
@@ -499,6 +507,8 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                 const uint32_t s_addr = lane_base + C::col_s(st, buf), p3_addr = lane_base + C::col_p3(st, buf);
                 if (!(ok = wait(C::BAR_SFULL + 2 * st + buf, (uint32_t)(g >> (NS - 1)) & 1u, 0xc70u + st))) break;
                 tc_fence_after();
+                // (A query that is infinite may have no score but -inf, which would be no weight: its maximum is NaN from the beginning, and with it all that follows.)
+                if (j == first && sees > 0 && (odd_q[segment & 3][st][quarter] >> lane & 1u)) m = __uint_as_float(0x7fc00000u);
                 const float4 sc = scales[g & 7];
                 const int n = sc.w != 0.0f ? sees - KV * j : 0;  // of the step's tokens, those that the row sees: none of a page whose number is out of range
                 // O is at rest once P V of the step before is complete: the barrier of scores that were issued behind it says so, the step's own where a stream has
@@ -537,7 +547,7 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     tmem_st32(s_addr + 32, zero);
                     tmem_st32(p3_addr, zero);
                 } else {
-                    // (a page of zeros has the factor 0, and what is masked has to stay at -inf; of a page that the row sees nothing of not even a NaN counts)
+                    // (a page of zeros has the factor 0, and what is masked has to stay at -inf; of a page that the row sees nothing of not even a NaN counts.)
                     const float f = n > 0 ? p.scale_log2 * (st ? sc.y : sc.x) + 1.17549435e-38f : 1.0f;
                     // (a page of zeros has the scale 0 and codes 0)
                     const float sv = n > 0 && sc.z != 0.0f ? sc.z : 1.0f;

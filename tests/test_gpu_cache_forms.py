@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from cache_reference import BLOCK, attention, rows
-from paper_2602_05269_b200.inputs import bf16_bits_to_f32
+from paper_2602_05269_b200.inputs import bf16_bits_to_f32, f32_to_bf16_bits
 from test_gpu_cache import Pair, bf16, hgf, ints  # noqa: F401  (hgf is the fixture)
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +65,35 @@ def test_a_page_that_is_none_is_left_out(hgf, dh, average, out_bf16):  # noqa: F
                 tol = tol[0][:, None] + (2.0 ** -8 * np.abs(want[0]) if out_bf16 else 0)   # (half a step of bf16)
                 assert (np.abs(got[j] - want[0]) <= tol).all()
         p.cache.table[slot, block] = good
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("group", [1, 3])
+@pytest.mark.parametrize("average", AVERAGES)
+@pytest.mark.parametrize("value", [0x7f80, 0xff80, 0x7fc0])
+def test_a_query_that_is_not_finite_is_seen_in_its_row_and_head(hgf, dh, group, average, value):  # noqa: F811
+    """One such element, where every key that the row sees has the sign that makes the score minus infinity (or NaN): no row may pass for one without weight."""
+    H, dim = 2, 11
+    p = Pair(hgf, H, dh, n_pages=20, n_slots=3)
+
+    def change(k, v):  # K of stream 1 in head 0, of stream 2 in head 1: never 0 in that dim, nor rounded to it
+        sign = np.float32(-1.0 if value == 0x7f80 else 1.0)
+        for stream, head in ((0, 0), (1, 1)):
+            k.reshape(-1, 2, H, dh)[:, stream, head, dim] = f32_to_bf16_bits(sign * (1.0 + np.arange(len(k)) % 3).astype(np.float32))[:]
+
+    p.reserve([0, 1, 2], [200] * 3)
+    p.append([0, 1, 2], [30, 134, 200], change=change)
+    for slot, n in ((0, 100), (1, 100), (2, 100), (2, 1), (0, 30)):
+        length, heads = len(p.ref.tokens[slot]), H * group
+        for at in {0, max(0, n - length), n // 2, n - 1}:   # (the second: the first row that sees a token)
+            q = rows(p.rng, n, 2 * heads * dh)
+            qq = q.reshape(n, 2, heads, dh)
+            qq[at, 0, group - 1, dim] = value        # a head of the group on K/V head 0
+            qq[at, 1, group, dim] = value            # and one on K/V head 1
+            for out_bf16 in (False, True):
+                got, _ = call(p, q, slot, n, average, out_bf16, group=group)
+                odd = ~np.isfinite(got)
+                want = np.zeros((n, heads), bool)
+                want[at, [group - 1, group]] = length - n + at + 1 > 0
+                assert (odd.all(2) == want).all() and (odd.any(2) == want).all()
+    hgf.check_status()
