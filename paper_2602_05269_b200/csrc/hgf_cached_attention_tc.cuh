@@ -643,10 +643,10 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
             const float flush_scale = flushed ? exp2_approx(m_acc - m) : 0.0f;
             if (whole) {
                 s_l[((segment & 1) * 2 + st) * kCtRows + row] = l;
-                s_f[((segment & 1) * 2 + st) * kCtRows + row] = flush_scale;
+                s_f[((segment & 1) * 2 + st) * kCtRows + row] = flush_scale;  // (`flushed` is alike for all rows and both streams)
             }
             auto add_flushed = [&](uint32_t (&v)[32], int stream, int cc, float scale) {
-                if (scale != 0.0f) {
+                if (flushed) {  // (with a scale of zero as well: what is not finite stays so)
 #pragma unroll
                     for (int u = 0; u < 32; u += 4) {
                         const float4 a = *acc_at(stream, (cc + u) >> 2);

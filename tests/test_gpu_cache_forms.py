@@ -97,3 +97,35 @@ def test_a_query_that_is_not_finite_is_seen_in_its_row_and_head(hgf, dh, group, 
                 want[at, [group - 1, group]] = length - n + at + 1 > 0
                 assert (odd.all(2) == want).all() and (odd.any(2) == want).all()
     hgf.check_status()
+
+
+# ---- long walks of one worker -----------------------------------------------------------------------------------------
+# Tiles of 128 rows keep a running maximum and begin their sums anew every eight pages.  80 entries that name one sequence of 21 blocks, two heads each, are
+# more than 21 blocks for each of 148 to 160 workers: most walk through a whole item.
+ENTRIES, M, LENGTH, HEADS = 80, 100, 1300, 2
+
+
+def walk(p, q, out_bf16, lam=0.7):
+    starts = ints(range(0, ENTRIES * M + 1, M))
+    out = p.hgf.diff_attention_cached(p.cache, bf16(q), ints([0] * ENTRIES), starts, lam, flags=p.hgf.FLAG_OUT_BF16 if out_bf16 else 0)
+    p.hgf.check_status()
+    return out.view(ENTRIES, M, HEADS, p.dh)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("out_bf16", [False, True])
+@pytest.mark.parametrize("block", [0, 7, 8, 12, 19])
+@pytest.mark.parametrize("large", [13, 17, 18])
+def test_a_value_that_is_not_finite_is_not_forgotten(hgf, dh, out_bf16, block, large):  # noqa: F811
+    """A block with a NaN in front of scores that leave it no weight: 0 times NaN, in every row that sees it."""
+    p = Pair(hgf, HEADS, dh, n_pages=90, n_slots=1, max_pages=21)
+
+    def change(k, v):
+        k[large * BLOCK:] = f32_to_bf16_bits(bf16_bits_to_f32(k[large * BLOCK:]) * np.float32(1000.0))
+        v.reshape(-1, HEADS, dh)[block * BLOCK + 5, 0, 3] = 0x7fc0
+
+    p.reserve([0], [LENGTH])
+    p.append([0], [LENGTH], change=change)
+    out = walk(p, rows(p.rng, ENTRIES * M, 2 * HEADS * dh), out_bf16)
+    sees = LENGTH - M + 1 + torch.arange(M, device="cuda") > block * BLOCK
+    assert torch.isnan(out[:, sees, 0]).all() and torch.isfinite(out[:, ~sees, 0]).all() and torch.isfinite(out[:, :, 1]).all()
