@@ -113,6 +113,37 @@ def walk(p, q, out_bf16, lam=0.7):
 
 
 @pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("way", ["up", "down", "jump"])
+def test_the_largest_score_moves_along_a_walk(hgf, dh, way):  # noqa: F811
+    """Keys that grow or shrink along the sequence, or are large from block 12 on, against 64 bits."""
+    p = Pair(hgf, HEADS, dh, n_pages=90, n_slots=1, max_pages=21)
+    size = {"up": np.geomspace(0.2, 20.0, LENGTH), "down": np.geomspace(20.0, 0.2, LENGTH), "jump": np.where(np.arange(LENGTH) < 12 * BLOCK, 0.5, 30.0)}[way]
+
+    def change(k, v):
+        k[:] = f32_to_bf16_bits(bf16_bits_to_f32(k) * size.astype(np.float32)[:, None])
+
+    p.reserve([0], [LENGTH])
+    p.append([0], [LENGTH], change=change)
+    bits = rows(p.rng, ENTRIES * M, 2 * HEADS * dh)
+    q = torch.from_numpy(bf16_bits_to_f32(bits)).cuda().double().view(ENTRIES, M, 2, HEADS, dh)
+    kv, lam, root = torch.from_numpy(p.ref.values(0)).cuda(), 0.7, dh ** -0.5
+    sees = torch.arange(LENGTH, device="cuda")[None] <= LENGTH - M + torch.arange(M, device="cuda")[:, None]
+    big, want, tol = kv[2].abs().amax((1, 2)), 0.0, 0.0
+    for st, w in ((0, 1.0), (1, -lam)):
+        s = torch.einsum("emhd,hnd->emhn", q[:, :, st], kv[st]) * root
+        s = s.masked_fill(~sees[:, None], -torch.inf)
+        e = torch.exp(s - s.amax(-1, keepdim=True))
+        want = want + w * torch.einsum("emhn,hnd->emhd", e / e.sum(-1, keepdim=True), kv[2])
+        # cache_reference.attention's tolerance, its largest over all tokens, and 96 terms of a sum that are cut off, 2^-23 each, where it counts one rounding a page
+        ds = 2.0 ** -22 * q[:, :, st].abs().amax(-1) * kv[st].abs().sum(-1).amax(-1) * root
+        ds = ds + 4 * 2.0 ** -24 * torch.einsum("emhd,hnd->emhn", q[:, :, st].abs(), kv[st].abs()).amax(-1) * root
+        tol = tol + abs(w) * big * (2 * (ds + 2.0 ** -21) + 2 * LENGTH * 2.0 ** -24 / e.sum(-1) + (LENGTH / BLOCK + 20 + 96) * 2.0 ** -23)
+    for out_bf16 in (False, True):
+        off = (walk(p, bits, out_bf16).double() - want).abs()
+        assert (off <= tol[..., None] + (2.0 ** -8 * want.abs() if out_bf16 else 0)).all()   # (half a step of bf16)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("out_bf16", [False, True])
 @pytest.mark.parametrize("block", [0, 7, 8, 12, 19])
 @pytest.mark.parametrize("large", [13, 17, 18])
