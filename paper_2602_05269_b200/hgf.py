@@ -603,6 +603,7 @@ def diff_attention_cached(cache: KVCache, q, slots, starts, lam: float, out_scal
             _native_cache.diff_attention_cached(cache._at, cache._index, q, slots, starts, lam, out_scale, out, workspace, flags, stream)):
         return out
     _list(cache, slots, starts)
+    assert q.dim() == 2, "q is a matrix"
     n, rows = slots.numel(), q.shape[0]
     heads = q.shape[1] // (2 * cache.head_dim)
     assert q.device == cache.device and q.dtype == torch.bfloat16 and q.is_contiguous() and q.shape[1] == 2 * heads * cache.head_dim and starts.numel() == n + 1
@@ -611,7 +612,8 @@ def diff_attention_cached(cache: KVCache, q, slots, starts, lam: float, out_scal
         with _on(stream):
             out = torch.empty((rows, heads * cache.head_dim), dtype=dtype, device=q.device) if out is None else out
             workspace = torch.empty(cached_workspace_bytes(cache, n, rows, heads), dtype=torch.uint8, device=q.device) if workspace is None else workspace
-    assert out.dtype == dtype and out.is_contiguous() and out.shape == (rows, heads * cache.head_dim)
+    assert out.device == cache.device and out.dtype == dtype and out.is_contiguous() and out.shape == (rows, heads * cache.head_dim)
+    assert workspace.device == cache.device and workspace.dtype == torch.uint8 and workspace.is_contiguous(), "the workspace is dense bytes on the cache's device"
     _check("hgf_diff_attention_cached",
            lib().hgf_diff_attention_cached(cache._ref, _ptr(q), rows, heads, _ptr(slots), _ptr(starts), n, lam, out_scale, _ptr(out), _ptr(workspace),
                                            workspace.numel(), flags, _stream(stream)))

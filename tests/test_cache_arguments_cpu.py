@@ -1,0 +1,52 @@
+"""What the Python calls of the K/V cache check by themselves, on a machine without a GPU: the library is a stand-in that must not be reached."""
+import pytest
+import torch
+
+from paper_2602_05269_b200 import build as hgf_build
+
+
+@pytest.fixture
+def hgf(monkeypatch):
+    hgf_build.build()
+    from paper_2602_05269_b200 import hgf as binding
+    binding.lib()
+
+    class Library:
+        def hgf_cached_workspace_bytes(self, *args):
+            return 1 << 16
+
+        def hgf_diff_attention_cached(self, *args):
+            self.called = True
+            return 0
+
+    library = Library()
+    library.called = False
+    monkeypatch.setattr(binding, "_native_cache", None)
+    monkeypatch.setattr(binding, "_list", lambda cache, *tensors: None)   # (it refuses a cache in host memory, which stands for the GPU's here)
+    monkeypatch.setattr(binding, "_stream", lambda stream: None)
+    cache = binding.KVCache(2, 64, 4, 2, 2, device="cpu")
+    monkeypatch.setattr(binding, "lib", lambda: library)
+    return binding, cache, library
+
+
+def test_attention_refuses_memory_that_is_not_the_caches(hgf):
+    """`out`, the workspace and q on another device (meta stands for it), of another type or shape, or with gaps."""
+    binding, cache, library = hgf
+    slots, starts = torch.zeros(1, dtype=torch.int32), torch.tensor([0, 3], dtype=torch.int32)
+    q, out, ws = torch.zeros(3, 256, dtype=torch.bfloat16), torch.zeros(3, 128), torch.zeros(1 << 16, dtype=torch.uint8)
+
+    def call(**change):
+        a = {"q": q, "out": out, "workspace": ws, **change}
+        return binding.diff_attention_cached(cache, a["q"], slots, starts, 0.5, out=a["out"], workspace=a["workspace"])
+
+    assert call() is out and library.called
+    assert call(out=None).shape == (3, 128) and call(workspace=None) is out
+    library.called = False
+    bad = [{"out": out.to("meta")}, {"out": out.to("meta"), "workspace": None}, {"out": out.bfloat16()}, {"out": torch.zeros(128, 3).t()}, {"out": out[:2]},
+           {"workspace": ws.to("meta")}, {"workspace": ws.to("meta"), "out": None}, {"workspace": torch.zeros(1 << 16)}, {"workspace": ws.view(torch.int8)}, {"workspace": ws[::2]},
+           {"q": q.to("meta")}, {"q": q.float()}, {"q": torch.zeros(3, 256, 2, dtype=torch.bfloat16)}, {"q": torch.zeros(256, dtype=torch.bfloat16)},
+           {"q": torch.zeros(3, 255, dtype=torch.bfloat16)}]
+    for change in bad:
+        with pytest.raises(AssertionError):
+            call(**change)
+    assert not library.called

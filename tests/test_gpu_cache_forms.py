@@ -160,3 +160,22 @@ def test_a_value_that_is_not_finite_is_not_forgotten(hgf, dh, out_bf16, block, l
     out = walk(p, rows(p.rng, ENTRIES * M, 2 * HEADS * dh), out_bf16)
     sees = LENGTH - M + 1 + torch.arange(M, device="cuda") > block * BLOCK
     assert torch.isnan(out[:, sees, 0]).all() and torch.isfinite(out[:, ~sees, 0]).all() and torch.isfinite(out[:, :, 1]).all()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_an_output_or_workspace_elsewhere_is_refused(hgf, monkeypatch, native):  # noqa: F811
+    if not native:
+        monkeypatch.setattr(hgf, "_native_cache", None)
+    p = Pair(hgf, 2, 64, n_slots=1)
+    p.fill([70])
+    q, slots, starts = torch.zeros((1, 256), dtype=torch.bfloat16, device="cuda"), ints([0]), ints([0, 1])
+    out, ws = torch.zeros((1, 128), device="cuda"), torch.zeros(1 << 22, dtype=torch.uint8, device="cuda")
+    before = hgf.launch_count()
+    for args in ({"out": out.cpu(), "workspace": ws}, {"out": out.cpu()}, {"out": out, "workspace": ws.cpu()}, {"workspace": ws.cpu()}, {"out": out, "workspace": ws.float()},
+                 {"out": out, "workspace": ws[::2]}):
+        with pytest.raises(AssertionError):
+            hgf.diff_attention_cached(p.cache, q, slots, starts, 0.5, **args)
+    with pytest.raises(AssertionError):
+        hgf.diff_attention_cached(p.cache, q.view(1, 256, 1).expand(1, 256, 2).contiguous(), slots, starts, 0.5, out=out, workspace=ws)
+    assert hgf.launch_count() == before
+    assert torch.equal(hgf.diff_attention_cached(p.cache, q, slots, starts, 0.5, out=out, workspace=ws), hgf.diff_attention_cached(p.cache, q, slots, starts, 0.5))
