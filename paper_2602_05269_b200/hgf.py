@@ -461,7 +461,7 @@ CACHE_MAX_SEQS = 1024
 class KVCache:
     """The arrays of an hgf_cache (8-bit paged K/V cache of the differential attention): `n_slots` sequences of up to
     64 * max_pages + 63 tokens, in `n_pages` pages of 64 tokens, for `n_heads` K/V heads.  The arrays are attributes (codes, scales, open, table,
-    held, length, refs, arrivals) on one device; KVCache.of takes ones that exist already."""
+    held, length, refs, arrivals) on one device, to be changed in place only, since the library goes by their addresses; KVCache.of takes ones that exist already."""
 
     _SHAPES = {"codes": (torch.int8, lambda c: (c.n_pages, c.n_heads, 3 * CACHE_BLOCK * c.head_dim)), "scales": (torch.float32, lambda c: (c.n_pages, c.n_heads, 4)),
                "open": (torch.bfloat16, lambda c: (c.n_slots, c.n_heads, 3, CACHE_BLOCK, c.head_dim)), "table": (torch.int32, lambda c: (c.n_slots, c.max_pages)),
@@ -493,7 +493,18 @@ class KVCache:
         self._struct = Cache(*(arrays[n].data_ptr() for n in self._SHAPES), self.n_pages, self.n_slots, self.max_pages, self.n_heads, self.head_dim)
         self._ref = ctypes.byref(self._struct)
         self._at = ctypes.addressof(self._struct)
+        self._bound = frozenset((*self._SHAPES, "n_heads", "head_dim", "n_pages", "n_slots", "max_pages", "device", "_index", "_struct", "_ref", "_at", "_bound"))
         lib()
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__.get("_bound", ()) and value is not getattr(self, name):  # (`cache.length -= n` assigns the tensor that it changed)
+            raise AttributeError(f"{name} of a cache is what the library was given: change the array in place, or make another cache")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        if name in self.__dict__.get("_bound", ()):
+            raise AttributeError(f"{name} of a cache is what the library was given")
+        super().__delattr__(name)
 
 
 def _on(stream):

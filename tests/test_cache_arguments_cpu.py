@@ -50,3 +50,28 @@ def test_attention_refuses_memory_that_is_not_the_caches(hgf):
         with pytest.raises(AssertionError):
             call(**change)
     assert not library.called
+
+
+def test_a_caches_arrays_are_changed_in_place_only(hgf):
+    """The library goes by the addresses taken when the cache was made: another tensor in an array's place would leave it with memory that is given back."""
+    binding, cache, _ = hgf
+    cache = binding.KVCache.of(2, 64, **{name: getattr(cache, name) for name in binding.KVCache._SHAPES})
+    at = {name: getattr(cache, name).data_ptr() for name in binding.KVCache._SHAPES}
+    cache.length.fill_(7)
+    for name in binding.KVCache._SHAPES:
+        array = getattr(cache, name)
+        with pytest.raises(AttributeError, match=name):
+            setattr(cache, name, array.clone())
+        with pytest.raises(AttributeError, match=name):
+            delattr(cache, name)
+        assert getattr(cache, name) is array
+    with pytest.raises(AttributeError, match="length"):
+        cache.length = cache.length - 2
+    for name in ("n_heads", "head_dim", "n_pages", "n_slots", "max_pages", "device"):
+        with pytest.raises(AttributeError, match=name):
+            setattr(cache, name, 1000)
+    assert cache.length.tolist() == [7, 7]
+    cache.length -= 2                          # (in place: the same tensor)
+    cache.length[1] = 3
+    cache.note = "a caller's own attributes are theirs"
+    assert cache.length.tolist() == [5, 3] and all(getattr(cache, name).data_ptr() == a for name, a in at.items())
