@@ -677,24 +677,26 @@ __global__ void __launch_bounds__(kCtThreads, 1) cached_attention_tc_kernel(CaPa
                     tmem_ld_wait();
                     add_flushed(v1, 0, cc, s_f[(segment & 1) * 2 * kCtRows + row]);
                     add_flushed(v2, 1, cc, s_f[((segment & 1) * 2 + 1) * kCtRows + row]);
-                    if (token >= seg.s.m) continue;
+                    if (token < seg.s.m) {
 #pragma unroll
-                    for (int u = 0; u < 32; ++u) v1[u] = __float_as_uint(__uint_as_float(v1[u]) * w1 - __uint_as_float(v2[u]) * w2);
-                    if (p.bf16) {
+                        for (int u = 0; u < 32; ++u) v1[u] = __float_as_uint(__uint_as_float(v1[u]) * w1 - __uint_as_float(v2[u]) * w2);
+                        if (p.bf16) {
 #pragma unroll
-                        for (int u = 0; u < 32; u += 8) {
-                            uint32_t o[4];
+                            for (int u = 0; u < 32; u += 8) {
+                                uint32_t o[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v1[u + 2 * e]), __uint_as_float(v1[u + 2 * e + 1]));
-                                o[e] = *reinterpret_cast<const uint32_t *>(&y);
+                                for (int e = 0; e < 4; ++e) {
+                                    const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v1[u + 2 * e]), __uint_as_float(v1[u + 2 * e + 1]));
+                                    o[e] = *reinterpret_cast<const uint32_t *>(&y);
+                                }
+                                *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + out + cc + u) = make_uint4(o[0], o[1], o[2], o[3]);
                             }
-                            *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + out + cc + u) = make_uint4(o[0], o[1], o[2], o[3]);
-                        }
-                    } else {
+                        } else {
 #pragma unroll
-                        for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4 *>(reinterpret_cast<float *>(p.out) + out + cc + u) = make_uint4(v1[u], v1[u + 1], v1[u + 2], v1[u + 3]);
+                            for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4 *>(reinterpret_cast<float *>(p.out) + out + cc + u) = make_uint4(v1[u], v1[u + 1], v1[u + 2], v1[u + 3]);
+                        }
                     }
+                    __syncwarp();  // (tcgen05.ld takes the whole warp, in the next round again)
                 }
                 if (checked && token < seg.s.m)
                     for (int dim = st * (DH / 2); dim < (st + 1) * (DH / 2); ++dim)
