@@ -1231,9 +1231,9 @@ static CaForm ca_form(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, in
     const bool narrow = cache->head_dim == 64;
     const int group = n_heads / cache->n_heads;
     // (256 rows of 6000 tokens, 2 sequences, 16 heads of 64: 91 us here, 157 in tiles of sixteen; but 64 rows of 4096 tokens,
-    // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty.  A pool of fewer pages than sequences holds some tens of tokens each, where an item's
-    // beginning and end count: 121 sequences of up to 80 tokens, 60 rows of four heads a K/V head, 334 and 281; but 40 of up to 190, 190 rows, 108 and 137.)
-    if (n_rows * group > 80 * n_seqs && cache->n_pages >= n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
+    // 16 heads of 128, 71 and 58, since half of a tile of 128 is empty.  Sequences of a page or less each go either way: 121 of up to 80 tokens, 60 rows of four heads a
+    // K/V head, 389 here and 302 in tiles of sixteen; 100 of up to 63 tokens, 30 rows of eight heads, 80 and 119.  What would tell them apart is on the device.)
+    if (n_rows * group > 80 * n_seqs) return CaForm{16, kCtRows / 16, 1, 0, kCtThreads};
     if (n_rows * group <= n_seqs) return narrow ? CaForm{1, 1, 8, 2, 256} : CaForm{1, 1, 4, 2, 128};
     if (n_rows * group <= 8 * n_seqs) return narrow ? CaForm{8, 1, 4, 4, 256} : CaForm{8, 1, 4, 2, 256};
     const int tiles = n_rows * group <= 16 * n_seqs ? 1 : 2, teams = 4 / tiles;

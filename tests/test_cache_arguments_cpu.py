@@ -1,4 +1,6 @@
 """What the Python calls of the K/V cache check by themselves, on a machine without a GPU: the library is a stand-in that must not be reached."""
+import ctypes
+
 import pytest
 import torch
 
@@ -75,3 +77,16 @@ def test_a_caches_arrays_are_changed_in_place_only(hgf):
     cache.length[1] = 3
     cache.note = "a caller's own attributes are theirs"
     assert cache.length.tolist() == [5, 3] and all(getattr(cache, name).data_ptr() == a for name, a in at.items())
+
+
+def _cache(hgf, **change):
+    v = {**{name: 4096 for name in hgf.KVCache._SHAPES}, "n_pages": 8, "n_slots": 4, "max_pages": 3, "n_heads": 2, "head_dim": 64, **change}
+    return ctypes.byref(hgf.Cache(*(v[n] for n, _ in hgf.Cache._fields_)))
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_the_attentions_form_does_not_go_by_the_pool(dh):
+    """A pool has the size of its longest load, which says nothing of a call: its workspace, and so its form, is the same."""
+    from paper_2602_05269_b200 import hgf
+    for n_seqs, n_rows in ((40, 40), (40, 90), (40, 500), (40, 4000), (1, 100)):
+        assert len({hgf.lib().hgf_cached_workspace_bytes(_cache(hgf, head_dim=dh, n_pages=n), n_seqs, n_rows, 2) for n in (1, 39, 40, 5000)}) == 1
