@@ -442,7 +442,12 @@ hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slots, int64_t 
  *   q    [n_rows][2 * n_heads * head_dim]  bfloat16: stream 1's heads, then stream 2's.  n_heads is a multiple of cache->n_heads: each
  *        n_heads / cache->n_heads neighbouring heads share a K/V head
  *   out  [n_rows][n_heads * head_dim]      fp32, or bfloat16 with HGF_FLAG_OUT_BF16
- *   workspace  hgf_cached_workspace_bytes(...) bytes (0.2 to 0.4 MB for single tokens, up to 43 for many rows), 256-byte aligned; scratch, which calls that may overlap on the device do not share
+ *   workspace  hgf_cached_workspace_bytes(...) bytes (0.2 to 0.4 MB for single tokens, up to 43 for many rows), 256-byte aligned; scratch, which calls that may overlap on the device do not share.
+ *        They go by the rows that a sequence has on average, so the same rows in fewer sequences can need more: for a workspace that serves calls of any list ask for
+ *        n_seqs = 1 and the most rows
+ * How the work is dealt goes by that average too, n_rows * (heads that share a K/V head) / n_seqs, entries -1 and sequences without rows among them; every call is right in
+ * every way, but rows that differ much are faster in calls of their own (16 heads of 64: a piece of 2500 rows over 6000 tokens beside 30 single tokens over 2000 each
+ * 835 us, in two calls 552; 256 rows over 6000 tokens 75 us, in a list padded to 256 entries 507)
  * Scores come from q to 2^-22 of the row's largest magnitude; probabilities enter the second product to 2^-24 of the largest in their page; sums
  * are exact integers or fp32, of more than 80 rows times heads of a group a sequence cut off instead of rounded within eight pages (2^-26 of themselves a
  * term of sixteen tokens on average).  The output's type says how the output is rounded, and nothing of how it is computed.

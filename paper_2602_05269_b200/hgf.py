@@ -602,6 +602,7 @@ def cache_free(cache: KVCache, slots, *, stream=None) -> None:
 
 
 def cached_workspace_bytes(cache: KVCache, n_seqs: int, n_rows: int, n_heads: int) -> int:
+    """hgf_cached_workspace_bytes: for a call of these sizes.  With n_seqs = 1 and the most rows: for every call with up to as many rows."""
     return int(lib().hgf_cached_workspace_bytes(cache._ref, n_seqs, n_rows, n_heads))
 
 

@@ -90,3 +90,14 @@ def test_the_attentions_form_does_not_go_by_the_pool(dh):
     from paper_2602_05269_b200 import hgf
     for n_seqs, n_rows in ((40, 40), (40, 90), (40, 500), (40, 4000), (1, 100)):
         assert len({hgf.lib().hgf_cached_workspace_bytes(_cache(hgf, head_dim=dh, n_pages=n), n_seqs, n_rows, 2) for n in (1, 39, 40, 5000)}) == 1
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("group", [1, 3, 8])
+def test_one_workspace_for_all_calls_of_a_program(dh, group):
+    """The bytes for all of the most rows in one sequence suffice for fewer rows and any number of sequences."""
+    from paper_2602_05269_b200 import hgf
+    need = lambda n_seqs, n_rows: hgf.lib().hgf_cached_workspace_bytes(_cache(hgf, head_dim=dh), n_seqs, n_rows, 2 * group)  # noqa: E731
+    for most in (1, 2, 9, 20, 81, 600):
+        enough = need(1, most)
+        assert all(need(n_seqs, n_rows) <= enough for n_rows in range(1, most + 1) for n_seqs in (*range(1, 12), 30, 31, 64, 200, 1024))
