@@ -179,3 +179,58 @@ def test_an_output_or_workspace_elsewhere_is_refused(hgf, monkeypatch, native): 
         hgf.diff_attention_cached(p.cache, q.view(1, 256, 1).expand(1, 256, 2).contiguous(), slots, starts, 0.5, out=out, workspace=ws)
     assert hgf.launch_count() == before
     assert torch.equal(hgf.diff_attention_cached(p.cache, q, slots, starts, 0.5, out=out, workspace=ws), hgf.diff_attention_cached(p.cache, q, slots, starts, 0.5))
+
+
+@pytest.mark.parametrize("tokens", [1, 5, 100])
+def test_a_block_between_its_layers(hgf, tokens):  # noqa: F811
+    """LayerNorm and projections, append, attention, output layer, read-back: back to back, where each launch may begin under the one before, and in a graph,
+    with the bits that the same calls give when the device is waited for after each."""
+    H, dh, S, steps = 2, 64, 3, 30
+    d, n = H * dh, tokens * S
+    g = torch.Generator().manual_seed(17)
+    weights = {name: (*hgf.pack_ternary(torch.randn(rows_, d, generator=g).cuda()), d, rows_) for name, rows_ in (("q", 2 * d), ("k", 2 * d), ("v", d), ("o", d))}
+    slots, starts, first = ints([2, 0, 1]), ints(range(0, n + 1, tokens)), ints([0] * S)
+    norm = {"ln_weight": torch.ones(d, device="cuda"), "ln_bias": torch.zeros(d, device="cuda")}
+    x0 = torch.randn(n, d, generator=g).cuda().bfloat16()
+
+    def run(wait, graph=False):
+        cache = hgf.KVCache(H, dh, S * (steps * tokens // 64 + 2), S, steps * tokens // 64 + 2)
+        hgf.cache_reserve(cache, slots, ints([steps * tokens] * S))
+        x, q, k, v = x0.clone(), *(torch.empty(n, w * d, dtype=torch.bfloat16, device="cuda") for w in (2, 2, 1))
+        out, done = torch.empty(n, d, dtype=torch.bfloat16, device="cuda"), torch.empty(S, dtype=torch.int32, device="cuda")
+        kr, vr = torch.zeros(n, 2 * d, device="cuda"), torch.zeros(n, d, device="cuda")
+        ws = torch.empty(hgf.cached_workspace_bytes(cache, S, n, H), dtype=torch.uint8, device="cuda")
+        lws = [torch.empty(hgf.workspace_bytes(n, d, w * d, 0), dtype=torch.uint8, device="cuda") for w in (2, 2, 1, 1)]
+
+        def layer(name, src, dst, i):
+            packed, gamma, d_in, d_out = weights[name]
+            hgf.linear_forward(src, packed, gamma, d_in, d_out, y=dst, workspace=lws[i], flags=hgf.FLAG_OUT_BF16, **({} if name == "o" else norm))
+            wait()
+
+        def step():
+            for i, (name, dst) in enumerate((("q", q), ("k", k), ("v", v))):
+                layer(name, x, dst, i)
+            hgf.cache_append(cache, k, v, slots, starts, done=done)
+            wait()
+            hgf.diff_attention_cached(cache, q, slots, starts, 0.3, out=out, workspace=ws, flags=hgf.FLAG_OUT_BF16)
+            wait()
+            layer("o", out, x, 3)
+            hgf.cache_read(cache, slots, first, starts, k=kr, v=vr)
+            wait()
+
+        outs = []
+        if graph:
+            captured = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(captured):
+                step()
+        for _ in range(steps):
+            captured.replay() if graph else step()
+            outs += [x.clone(), out.clone(), kr.clone(), done.clone()]
+        hgf.check_status()
+        return outs + [cache.length.clone(), cache.codes[cache.table[:, :steps * tokens // 64].flatten().long()], cache.open[:, :, :, :steps * tokens % 64].clone()]
+
+    want = run(torch.cuda.synchronize)
+    assert all(torch.isfinite(t.float()).all() for t in want) and want[-3].tolist() == [steps * tokens] * S
+    for kind in (False, True, False):
+        for a, b in zip(run(lambda: None, kind), want):
+            assert torch.equal(a, b)
