@@ -449,12 +449,12 @@ hgf_status hgf_cache_free(const hgf_cache *cache, const int32_t *slots, int64_t 
  * every way, but rows that differ much are faster in calls of their own (16 heads of 64: a piece of 2500 rows over 6000 tokens beside 30 single tokens over 2000 each
  * 835 us, in two calls 552; 256 rows over 6000 tokens 75 us, in a list padded to 256 entries 507)
  * Scores come from q to 2^-22 of the row's largest magnitude; probabilities enter the second product to 2^-24 of the largest in their page; sums
- * are exact integers or fp32, of more than 80 rows times heads of a group a sequence cut off instead of rounded within eight pages (2^-26 of themselves a
- * term of sixteen tokens on average).  The output's type says how the output is rounded, and nothing of how it is computed.
+ * are exact integers or fp32, those of more than 80 rows times heads of a group a sequence cut off instead of rounded within eight pages (96 additions, 2^-23 of the
+ * sum each at most; 1.4e-6 in all against 64 bits at 6000 tokens as at 30000).  The output's type says how the output is rounded, and nothing of how it is computed.
  * A query row, a block or an open value of V that is not finite gives outputs that are not finite in the rows that see tokens, it or one of its tokens (an
  * open value in its dim only), and in no others.  An infinite score of an open key is no weight if it is negative, else NaN.
- * (Scores are expected within binary32's range, and the largest |v| of a block at 0 or between 2^-90 and 2^100: outside, the lower digits
- * of its probabilities are lost, or sums pass that range.)
+ * (Scores are expected within binary32's range, the largest |q| of a row and head at 0 or above 2^-100, and the largest |v| of a block at 0 or between 2^-90 and 2^100:
+ * outside, the lower digits of q or of the block's probabilities are lost, or sums pass that range.)
  */
 size_t hgf_cached_workspace_bytes(const hgf_cache *cache, int64_t n_seqs, int64_t n_rows, int32_t n_heads);
 hgf_status hgf_diff_attention_cached(const hgf_cache *cache, const void *q, int64_t n_rows, int32_t n_heads, const int32_t *slots,

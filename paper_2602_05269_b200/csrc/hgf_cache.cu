@@ -88,9 +88,10 @@ static unsigned head_shares(int64_t pieces, int H, int blocks) {
 // ---- append ---------------------------------------------------------------------------------------------------------------------
 // A block of threads takes one piece and every gridDim.y-th K/V head of it: a block of 64 tokens that becomes complete, whose values it reads from the open
 // rows and the new ones, quantises, and writes as a page; the sequence's first piece also writes the rows that stay open, after its reads of the rows
-// that these replace.  Each new value is read once, each code written once; what bounds it is the chain of dependent look-ups in front (starts, slot, length,
-// table, counts: about 4 us), which is why a block has several heads.  Measured, kernel alone, memory cold: 64 sequences with one token each, 16 heads of 64, 10.6 us; six with up to 1400
-// tokens 20.3 us (addresses found anew for every page 31).
+// that these replace.  Each new value is read once, each code written once.  What bounds it is the chain of dependent look-ups in front (starts, slot, length,
+// table, counts: about 4 us), which is why a block has several heads, and then that a block goes through its two or three heads in turn - reduce, barrier, quantise, barrier,
+// store, the next head's loads under the stores - with all blocks in step.  Measured, kernel alone, memory cold: 64 sequences with one token each, 16 heads of 64, 10.6 us (the few whose
+// block becomes complete end last); six with up to 1400 tokens 20.3 us for 53 MB (addresses found anew for every page 31).
 constexpr int kAppendThreads = 256;
 
 // Four lanes (l, l + 8, l + 16, l + 24) hold a word of four bytes each, a 4 x 4 matrix: its transpose.

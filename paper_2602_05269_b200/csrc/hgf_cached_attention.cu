@@ -26,7 +26,8 @@
 //   single tokens   64 sequences of up to 4096 tokens, 16 heads of 128: 248 us, 99 % of the floor's rate; one of 131071 tokens, 16 heads of 64: 73 us, 84 %;
 //                   32 of up to 2048: 32 us, 63 % - 4 us to begin, unequal ends of the CTAs, the join; one of 200 tokens: 9 us, launches and look-ups
 //   shared heads    16 sequences of up to 2900 tokens, 5 drafts of 4 query heads a K/V head, 128 wide: 55 us, floor 14.  Bound by dependent issue at two warps
-//                   a scheduler (0.29 instructions issued a clock; 890 a page, stream and sixteen rows, 96 of them products; integer tensor pipe 25 % busy).
+//                   a scheduler (0.30 instructions issued a clock; 1600 a page, stream and sixteen rows with waits and items' ends, 192 of them products; integer tensor
+//                   pipe 28 % busy).  Most sequences have one tile of sixteen, three of the sixteen two: 63 % of the tiles' rows are there.
 //                   Tiles of eight rows against sixteen: one sequence of 59361 tokens, two heads a K/V head, 128 wide 71 and 110 us; with sixteen warps instead of
 //                   eight for those, 64 wide, 51 and 49 (13 sequences of 5 tokens 13.6 and 9.9)
 #include "hgf_cache.cuh"

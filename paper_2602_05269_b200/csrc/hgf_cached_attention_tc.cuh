@@ -15,11 +15,11 @@
 // Tensor memory (512 columns) holds scores and probabilities of two steps a stream beside O 64 wide.  128 wide O takes 256 of them, and a step's
 // scores and probabilities 96 (the third parts behind the 64 that scores and the others share): one step a stream, whose scores follow P V of the step before.
 //
-// What bounds it is the instructions: 1500 a step and scheduler, of them 340 in each softmax warp's 64 x 32 probabilities and 350 in a converting warp, and
-// their fetching, as the roles' loops together are longer than what a scheduler keeps (41 to 54 % of the issue slots used; tensor pipe 20 to 26 %,
-// exponentials 20 to 34 %, memory 3 to 5 %).
-// Measured, calls back to back, either type of output: 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 100 us; 8 K/V heads with four query heads each, 30000
-// tokens, 128 rows: 217; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 117; one of 30000, 512 rows: 349 (the last two with the int8 form 208 and 705).
+// What bounds it 64 wide is the instructions: 2300 a step and scheduler with waits and segments' ends, and their fetching, as the roles' loops together are longer than
+// what a scheduler keeps (49 % of the issue slots used; tensor pipe 22 %, exponentials 22 %, memory 5 %).  128 wide (2340, 37 % of the slots, tensor pipe 27 %) it is the
+// chain scores, softmax, P V of a stream, of which one step is under way at a time.
+// Measured, calls back to back, either type of output: 16 heads of 64, 2 sequences of 6000 tokens, 256 rows each: 102 us; 8 K/V heads with four query heads each, 30000
+// tokens, 128 rows: 219; 8 heads of 128, 4 sequences of 8192 tokens, 128 rows: 121; one of 30000, 512 rows: 359 (the last two with the int8 form 208 and 705).
 // With probabilities in two parts, 16 bits, and sums that run on 64 steps (off by 7.5e-6 after 30000 tokens, growing with the length; plain fp32 3.9e-6, here 1.4e-6) 85, 171, 98 and
 // 275.  Steps (the first case in fp32): codes from global memory into registers, segments kept in registers (spills went to the L2 cache) 99;
 // segments in shared memory 91; the parts' sixteen bytes of neighbouring rows side by side 104 -> 100 (sequences of one length; the third case 155 -> 117);
