@@ -234,3 +234,33 @@ def test_a_block_between_its_layers(hgf, tokens):  # noqa: F811
     for kind in (False, True, False):
         for a, b in zip(run(lambda: None, kind), want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("average", AVERAGES)
+def test_a_workspace_may_hold_anything_and_calls_overlap(hgf, dh, average):  # noqa: F811
+    """The same bits with a workspace of ones and of NaN, of exactly the bytes that are asked for, and from calls on two streams with a workspace each."""
+    p = Pair(hgf, 2, dh, n_pages=120, n_slots=2, max_pages=60)
+    p.fill([3333, 1300])
+    S, m = (60, 1) if average == 1 else (60, {8: 5, 16: 13, 32: 40, 300: 110}[average])
+    slots, starts = ints([i % 2 for i in range(S)]), ints(range(0, S * m + 1, m))
+    q = [bf16(rows(p.rng, S * m, 4 * dh)) for _ in range(2)]
+    n = hgf.cached_workspace_bytes(p.cache, S, S * m, 2)
+    ws = [torch.full((n,), fill, dtype=torch.uint8, device="cuda") for fill in (0xff, 1)]
+    call = lambda i, w, **kw: hgf.diff_attention_cached(p.cache, q[i], slots, starts, 0.7, workspace=w, **kw)  # noqa: E731
+    want = [call(i, torch.zeros(n, dtype=torch.uint8, device="cuda")) for i in range(2)]
+    for i in range(2):
+        for w in ws:
+            w.fill_(0xff if w is ws[0] else 1)
+            assert torch.equal(call(i, w), want[i])
+    with pytest.raises(hgf.HgfError):
+        call(0, ws[0][:-256])
+    outs = [[torch.empty_like(want[i]) for _ in range(8)] for i in range(2)]
+    side = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for j in range(8):
+        for i in range(2):
+            call(i, ws[i], out=outs[i][j], stream=side[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i in range(2) for o in outs[i])
+    hgf.check_status()
