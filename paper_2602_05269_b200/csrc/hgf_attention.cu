@@ -12,6 +12,8 @@ namespace hgf {
 struct AttnParams {
     const __nv_bfloat16 *q, *k, *v;  // q, k [B*L][2*h*dh]; v [B*L][h*dh]
     void *out;                       // [B*L][h*dh] fp32 or bf16
+    __nv_bfloat16 *streams;          // [B*L][2*h*dh] (for the backward pass, else null)
+    float *lse;                      // [B][h][2][L]
     int B, L, h;
     float lambda, out_scale, scale_log2;  // scale_log2 = log2(e) / sqrt(dh)
     uint32_t flags;
@@ -93,7 +95,8 @@ __device__ __forceinline__ void exchange_blocks(uint32_t (&v)[16], int lane) {
     }
 }
 
-template <int DH>
+// SAVE: for the backward pass each stream's own output O_s / l_s (bf16) and log2 of its sum of 2^(scale s) go to memory, too.
+template <int DH, bool SAVE>
 __global__ void __launch_bounds__(kTaThreads, 1)
 ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                          const __grid_constant__ CUtensorMap tmap_v, const AttnParams p, unsigned int *status) {
@@ -111,7 +114,7 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     const int L = p.L, h = p.h, nqt = (L + kTaBM - 1) / kTaBM, bhs = p.B * h, items = nqt * bhs, G = (int)gridDim.x;
     // The CTA's k-th tile: the tiles in order of falling length (late queries first) are dealt in rounds, every other
     // round backwards, so that the CTAs' sums stay close.
-    struct Tile { int q0, tok0, hd, J; };
+    struct Tile { int q0, tok0, hd, J, bh; };
     auto tile_of = [&](int k, Tile &t) {
         const int i = k * G + ((k & 1) ? G - 1 - (int)blockIdx.x : (int)blockIdx.x);
         if (i >= items) return false;
@@ -119,6 +122,7 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
         t.q0 = qt * kTaBM;
         t.tok0 = (bh / h) * L;
         t.hd = bh % h;
+        t.bh = bh;
         t.J = (keys + KV - 1) / KV;
         return true;
     };
@@ -412,7 +416,10 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
             unpack_f32x2(l2a, la, lb);
             unpack_f32x2(l2b, lc, ld);
             float *sl = s_l + (k & 1) * 2 * kTaBM;
-            sl[st * kTaBM + row] = (la + lb) + (lc + ld);
+            const float l = (la + lb) + (lc + ld);
+            sl[st * kTaBM + row] = l;
+            if constexpr (SAVE)
+                if (qi < L) p.lse[((size_t)t.bh * 2 + st) * L + qi] = m * c + log2f(l);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::BAR_L + (k & 1)));
@@ -431,6 +438,23 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(C::BAR_OEMPTY + ob));
+                }
+                if constexpr (SAVE) {
+                    const float r1 = 1.0f / sl[row], r2 = 1.0f / sl[kTaBM + row];
+                    __nv_bfloat16 *dst = p.streams + (size_t)(t.tok0 + qi) * (2 * (size_t)h * DH) + (size_t)t.hd * DH + cc;
+                    if (qi < L) {
+#pragma unroll
+                        for (int u = 0; u < 32; u += 8) {
+                            uint32_t o1[4], o2[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                o1[e] = pack_bf16(__uint_as_float(v1[u + 2 * e]) * r1, __uint_as_float(v1[u + 2 * e + 1]) * r1);
+                                o2[e] = pack_bf16(__uint_as_float(v2[u + 2 * e]) * r2, __uint_as_float(v2[u + 2 * e + 1]) * r2);
+                            }
+                            *reinterpret_cast<uint4 *>(dst + u) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
+                            *reinterpret_cast<uint4 *>(dst + (size_t)h * DH + u) = make_uint4(o2[0], o2[1], o2[2], o2[3]);
+                        }
+                    }
                 }
                 if constexpr (DH == 128) {
                     // Four neighbouring rows exchange 16-byte blocks, so that four lanes store 64 consecutive bytes of one row:
@@ -502,11 +526,11 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     }
 }
 
-template <int DH>
+template <int DH, bool SAVE>
 static cudaError_t launch_attention_tc(const AttnParams &p, cudaStream_t stream) {
     using C = TaCfg<DH>;
     static std::atomic<unsigned long long> attr_done{0};
-    cudaError_t e = ensure_dynamic_smem(ta_diff_attention_kernel<DH>, C::SMEM_BYTES, attr_done);
+    cudaError_t e = ensure_dynamic_smem(ta_diff_attention_kernel<DH, SAVE>, C::SMEM_BYTES, attr_done);
     if (e != cudaSuccess) return e;
     unsigned int *status = device_status_word();
     if (!status) return cudaErrorMemoryAllocation;
@@ -519,7 +543,7 @@ static cudaError_t launch_attention_tc(const AttnParams &p, cudaStream_t stream)
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;
     const unsigned items = (unsigned)(((p.L + kTaBM - 1) / kTaBM) * p.B * p.h), grid = items < (unsigned)sms ? items : (unsigned)sms;
-    ta_diff_attention_kernel<DH><<<grid, kTaThreads, C::SMEM_BYTES, stream>>>(mq, mk, mv, p, status);
+    ta_diff_attention_kernel<DH, SAVE><<<grid, kTaThreads, C::SMEM_BYTES, stream>>>(mq, mk, mv, p, status);
     count_launch();
     return cudaGetLastError();
 }
@@ -528,20 +552,23 @@ static cudaError_t launch_attention_tc(const AttnParams &p, cudaStream_t stream)
 
 using namespace hgf;
 
-extern "C" hgf_status hgf_diff_attention_forward(const void *q, const void *k, const void *v, int64_t B, int64_t L,
-                                                 int32_t n_heads, int32_t head_dim, float lambda, float out_scale, void *out,
-                                                 uint32_t flags, void *stream) {
+static hgf_status attention_forward(const void *q, const void *k, const void *v, int64_t B, int64_t L, int32_t n_heads, int32_t head_dim,
+                                    float lambda, float out_scale, void *out, bool save, void *streams, float *lse, uint32_t flags,
+                                    void *stream) {
     if (!q || !k || !v || !out || B <= 0 || L <= 0 || n_heads <= 0) return HGF_ERR_INVALID_ARG;
+    if (save && (!streams || !lse)) return HGF_ERR_INVALID_ARG;
     if (flags & ~HGF_FLAG_OUT_BF16) return HGF_ERR_INVALID_ARG;
     if ((head_dim != 64 && head_dim != 128) || B > 65535 || n_heads > 65535 || L > (1 << 24)) return HGF_ERR_UNSUPPORTED_SHAPE;
     // token rows and CTAs are counted in 32 bits
     if (B * L > 0x7fffffffll || (uint64_t)B * (uint64_t)n_heads * (uint64_t)((L + kTaBM - 1) / kTaBM) > 0x7fffffffull) return HGF_ERR_UNSUPPORTED_SHAPE;
-    if ((((uintptr_t)q) | ((uintptr_t)k) | ((uintptr_t)v) | ((uintptr_t)out)) & 15u) return HGF_ERR_MISALIGNED;
+    if ((((uintptr_t)q) | ((uintptr_t)k) | ((uintptr_t)v) | ((uintptr_t)out) | ((uintptr_t)streams) | ((uintptr_t)lse)) & 15u) return HGF_ERR_MISALIGNED;
     AttnParams p = {};
     p.q = (const __nv_bfloat16 *)q;
     p.k = (const __nv_bfloat16 *)k;
     p.v = (const __nv_bfloat16 *)v;
     p.out = out;
+    p.streams = (__nv_bfloat16 *)streams;
+    p.lse = lse;
     p.B = (int)B;
     p.L = (int)L;
     p.h = n_heads;
@@ -549,8 +576,22 @@ extern "C" hgf_status hgf_diff_attention_forward(const void *q, const void *k, c
     p.out_scale = out_scale;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)head_dim));
     p.flags = flags;
-    const cudaError_t e = head_dim == 64 ? launch_attention_tc<64>(p, (cudaStream_t)stream) : launch_attention_tc<128>(p, (cudaStream_t)stream);
+    cudaStream_t s = (cudaStream_t)stream;
+    const cudaError_t e = head_dim == 64 ? (save ? launch_attention_tc<64, true>(p, s) : launch_attention_tc<64, false>(p, s))
+                                         : (save ? launch_attention_tc<128, true>(p, s) : launch_attention_tc<128, false>(p, s));
     return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
+}
+
+extern "C" hgf_status hgf_diff_attention_forward(const void *q, const void *k, const void *v, int64_t B, int64_t L,
+                                                 int32_t n_heads, int32_t head_dim, float lambda, float out_scale, void *out,
+                                                 uint32_t flags, void *stream) {
+    return attention_forward(q, k, v, B, L, n_heads, head_dim, lambda, out_scale, out, false, nullptr, nullptr, flags, stream);
+}
+
+extern "C" hgf_status hgf_diff_attention_forward_train(const void *q, const void *k, const void *v, int64_t B, int64_t L, int32_t n_heads,
+                                                       int32_t head_dim, float lambda, float out_scale, void *out, void *streams, float *lse,
+                                                       uint32_t flags, void *stream) {
+    return attention_forward(q, k, v, B, L, n_heads, head_dim, lambda, out_scale, out, true, streams, lse, flags, stream);
 }
 
 extern "C" double hgf_diff_lambda0(double head_dim) { return 0.8 - 0.6 * exp(-0.3 * head_dim); }

@@ -1,0 +1,574 @@
+// Gradients of the causal differential attention (hgf_attention.cu).  With c = 1 / sqrt(d_h), P_s the probabilities of stream s,
+// G the output's gradient, A_ij = G_i . V_j, D_s,i = G_i . O_s,i = sum_j P_s,ij A_ij, w_1 = out_scale and w_2 = -lambda out_scale:
+//     dV_j = out_scale sum_i (P_1 - lambda P_2)_ij G_i          T_s,ij = P_s,ij (A_ij - D_s,i)
+//     dQ_s,i = c w_s sum_j T_s,ij K_s,j      dK_s,j = c w_s sum_i T_s,ij Q_s,i      dlambda = -out_scale sum_ij P_2,ij A_ij
+// The probabilities are not kept: they are formed again, P = 2^(scale_log2 q.k - lse), from the forward pass's lse (base 2).
+#include <cmath>
+
+#include "hgf_tc.cuh"
+
+namespace hgf {
+
+struct AttnBackParams {
+    __nv_bfloat16 *d2, *d1;          // gradients of the two-stream tensor (dK or dQ) and, for keys, of V; d1 null for queries
+    const float *stats;              // [B*h][ceil(L / 64)][-lse_1, -lse_2, -D_1, -D_2][64]
+    double *dl_part;                 // (queries) [grid][8] partial sums of P_2 (.) A
+    const double *dl_in;             // (keys) the same, of the launch before; null: none
+    float *dlambda;
+    int dl_n;
+    int B, L, h;
+    float lambda, out_scale, scale, scale_log2;  // scale = 1 / sqrt(dh), scale_log2 = log2(e) / sqrt(dh)
+};
+
+__device__ __forceinline__ float tb_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t tb_pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t tb_pack_bf16(uint64_t v) {
+    float lo, hi;
+    unpack_f32x2(v, lo, hi);
+    return tb_pack_bf16(lo, hi);
+}
+
+// ---- D and lse in the order in which the main kernels read them ------------------------------------------------------
+// A block takes 64 tokens of a (batch element, head): a row of G, O_1 and O_2 is read by head_dim / 8 lanes, 16 bytes each, the 256
+// results of the block are one contiguous KiB.  Rows behind the sequence get probability 0 (-lse = -infinity).
+template <int DH>
+__global__ void __launch_bounds__(256)
+attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, const float *lse, float *stats, int B, int L, int h) {
+    constexpr int LPR = DH / 8, RPW = 32 / LPR;
+    __shared__ float s_d[2][64];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = (L + 63) / 64;
+    const long long tiles = (long long)B * h * blocks;
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const long long bh = tile / blocks;
+        const int i0 = (int)(tile % blocks) * 64, hd = (int)(bh % h);
+        const size_t tok0 = (size_t)(bh / h) * L, width = (size_t)h * DH;
+#pragma unroll
+        for (int it = 0; it < 8 / RPW; ++it) {
+            const int r = warp * 8 + it * RPW + lane / LPR, i = i0 + r;
+            float d1 = 0.0f, d2 = 0.0f;
+            if (i < L) {
+                const size_t col = (size_t)hd * DH + (lane % LPR) * 8;
+                const uint4 g = __ldg(reinterpret_cast<const uint4 *>(dout + (tok0 + i) * width + col));
+                const uint4 a = __ldg(reinterpret_cast<const uint4 *>(streams + (tok0 + i) * 2 * width + col));
+                const uint4 b = __ldg(reinterpret_cast<const uint4 *>(streams + (tok0 + i) * 2 * width + width + col));
+                const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float g0 = bf16lo_to_float(gw[e]), g1 = bf16hi_to_float(gw[e]);
+                    d1 = fmaf(g0, bf16lo_to_float(aw[e]), fmaf(g1, bf16hi_to_float(aw[e]), d1));
+                    d2 = fmaf(g0, bf16lo_to_float(bw[e]), fmaf(g1, bf16hi_to_float(bw[e]), d2));
+                }
+            }
+#pragma unroll
+            for (int o = LPR / 2; o; o >>= 1) {
+                d1 += __shfl_xor_sync(0xffffffffu, d1, o);
+                d2 += __shfl_xor_sync(0xffffffffu, d2, o);
+            }
+            if (lane % LPR == 0) {
+                s_d[0][r] = d1;
+                s_d[1][r] = d2;
+            }
+        }
+        __syncthreads();
+        const int kind = threadIdx.x >> 6, r = threadIdx.x & 63, i = i0 + r;
+        float v;
+        if (kind < 2) v = i < L ? -__ldg(lse + (bh * 2 + kind) * L + i) : -INFINITY;
+        else v = i < L ? -s_d[kind - 2][r] : 0.0f;
+        stats[tile * 256 + threadIdx.x] = v;
+        __syncthreads();
+    }
+}
+
+// ---- the gradients ----------------------------------------------------------------------------------------------------
+// One skeleton for both sides.  KEYS: a tile is 128 keys, lane = key, in steps of 64 queries from the tile's first on (dK, dV).
+// Otherwise a tile is 128 queries, lane = query, in steps of 64 keys up to the tile's last (dQ).  Two passes form the scores twice,
+// 11 products instead of 8, but every sum has one owner and one order: no atomics, no fp32 copy of dQ.
+//   warp 0      TMA producer: the tile's resident operands (K_s and V, or Q_s and G), then a step's streamed ones
+//   warp 1      front products: the scores of a step and A, [128 x 64] fp32 in tensor memory
+//   warp 2      back products: the accumulators += T_s (or P) times the step's rows; the first operand is bf16 in tensor
+//               memory, written over the scores that it came from; the second the streamed tile in its stored form
+//   warps 4-11  a thread owns a lane and half of the step's columns
+// NS streams are in flight at a time: two for head_dim 64; for head_dim 128 the accumulators take too many columns, so the
+// streams are items of their own, one after the other (with dV kept over both).
+constexpr int kTbThreads = 384, kTbTile = 128, kTbStep = 64;
+
+template <int DH, bool KEYS>
+struct TbCfg {
+    static constexpr int NS = DH == 64 ? 2 : 1;
+    static constexpr int NBLK = DH / 64;
+    static constexpr int NRES = DH == 64 ? 2 : 1;   // buffers of the resident operands
+    static constexpr int ST = DH == 64 ? 5 : 4;     // ring stages
+    static constexpr int RES_TILE = NBLK * kTbTile * 128, RES_BYTES = (NS + 1) * RES_TILE;
+    static constexpr int ROW_BLOCK = kTbStep * 128, ROW_TILE = NBLK * ROW_BLOCK, ROW_BYTES = (NS + 1) * ROW_TILE;
+    static constexpr int OFF_RING = NRES * RES_BYTES, OFF_STATS = OFF_RING + ST * ROW_BYTES, OFF_BAR = OFF_STATS + (KEYS ? ST * 1024 : 0);
+    static constexpr int BAR_RESFULL = 0, BAR_RESEMPTY = BAR_RESFULL + NRES, BAR_FULL = BAR_RESEMPTY + NRES, BAR_EMPTY = BAR_FULL + ST,
+                         BAR_S = BAR_EMPTY + ST,       // [parity of the step] scores are there
+                         BAR_A = BAR_S + 2,            // A is there
+                         BAR_AREAD = BAR_A + 2,        // A has been read
+                         BAR_P = BAR_AREAD + 2,        // first operands of the back products are there
+                         BAR_BACK = BAR_P + 2,         // back products are complete
+                         BAR_ACC = BAR_BACK + 2,       // all products of an item
+                         BAR_ACCREAD = BAR_ACC + 1, BAR_COUNT = BAR_ACCREAD + 1;
+    static constexpr int SMEM_BYTES = OFF_BAR + 512 + 1024;
+    // tensor-memory columns: accumulators (dV, then dK_s or dQ_s), score buffers [parity][stream], A buffers
+    static constexpr int NA = DH == 64 && KEYS ? 1 : 2;
+    static constexpr int COL_V = 0, COL_T = KEYS ? DH : 0, COL_S = COL_T + NS * DH, COL_A = COL_S + 2 * NS * kTbStep;
+    static constexpr uint32_t IDESC_F = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTbStep >> 3) << 17) | ((uint32_t)(kTbTile >> 4) << 24);
+    static constexpr uint32_t IDESC_B = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kTbTile >> 4) << 24);
+    static_assert(BAR_COUNT * 8 + 16 <= 512, "barrier block");
+    static_assert(COL_A + NA * kTbStep <= 512 && SMEM_BYTES <= 227 * 1024, "tensor and shared memory");
+};
+
+template <int DH, bool KEYS>
+__global__ void __launch_bounds__(kTbThreads, 1)
+attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __grid_constant__ CUtensorMap map_res1,
+                          const __grid_constant__ CUtensorMap map_row2, const __grid_constant__ CUtensorMap map_row1, const AttnBackParams p,
+                          unsigned int *status) {
+    using C = TbCfg<DH, KEYS>;
+    constexpr int NS = C::NS;
+    extern __shared__ uint8_t tb_smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)tb_smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t sbase = smem_u32(smem), bar0 = sbase + C::OFF_BAR;
+    auto bar = [&](int i) { return bar0 + 8u * i; };
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::OFF_BAR + C::BAR_COUNT * 8);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::OFF_BAR + C::BAR_COUNT * 8 + 4);
+
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int L = p.L, h = p.h, nt = (L + kTbTile - 1) / kTbTile, n64 = (L + kTbStep - 1) / kTbStep, G = (int)gridDim.x;
+    const long long bhs = (long long)p.B * h, tiles = nt * bhs;
+    // The CTA's k-th item; tiles in order of falling length are dealt in rounds, every other round backwards.
+    struct Item { int r0, s0, J, b, hd, st; long long bh; };
+    auto item_of = [&](int k, Item &t) {
+        const int kt = NS == 2 ? k : k >> 1;
+        const long long i = (long long)kt * G + ((kt & 1) ? G - 1 - (int)blockIdx.x : (int)blockIdx.x);
+        if (i >= tiles) return false;
+        const int rank = (int)(i / bhs), tile = KEYS ? rank : nt - 1 - rank;
+        t.bh = i % bhs;
+        t.r0 = tile * kTbTile;
+        t.s0 = KEYS ? t.r0 : 0;
+        t.J = KEYS ? n64 - t.r0 / kTbStep : min(n64, t.r0 / kTbStep + 2);
+        t.b = (int)(t.bh / h);
+        t.hd = (int)(t.bh % h);
+        t.st = NS == 2 ? 0 : 1 - (k & 1);  // (one stream at a time: the second first)
+        return true;
+    };
+
+    if (tid == 0) {
+        for (int i = 0; i < C::NRES; ++i) {
+            mbar_init(bar(C::BAR_RESFULL + i), 1);
+            mbar_init(bar(C::BAR_RESEMPTY + i), 1);
+        }
+        for (int s = 0; s < C::ST; ++s) {
+            mbar_init(bar(C::BAR_FULL + s), 1);
+            mbar_init(bar(C::BAR_EMPTY + s), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(C::BAR_S + i), 1);
+            mbar_init(bar(C::BAR_A + i), 1);
+            mbar_init(bar(C::BAR_AREAD + i), 8);
+            mbar_init(bar(C::BAR_P + i), 8);
+            mbar_init(bar(C::BAR_BACK + i), 1);
+        }
+        mbar_init(bar(C::BAR_ACC), 1);
+        mbar_init(bar(C::BAR_ACCREAD), 8);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        fence_proxy_async();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    auto wait = [&](int i, uint32_t par, unsigned int code) {
+        return __all_sync(0xffffffffu, mbar_wait_poll(bar(i), par, abort_flag, status, code)) != 0;
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        uint32_t issued[C::ST] = {}, res_issued[C::NRES] = {};
+        int s = 0, rb = 0;
+        uint32_t ph = 1, rph = 1;
+        bool ok = true;
+        Item t;
+        for (int k = 0; ok && item_of(k, t); ++k) {
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_RESEMPTY + rb), rph, abort_flag, status, 0xb00u + rb)) != 0;
+            if (!ok) break;
+            if (lane == 0) {
+                const uint32_t full = bar(C::BAR_RESFULL + rb), dst = sbase + rb * C::RES_BYTES;
+                mbar_arrive_expect_tx(full, C::RES_BYTES);
+                for (int blk = 0; blk < C::NBLK; ++blk) {
+                    for (int a = 0; a < NS; ++a)
+                        tma_load_3d(dst + a * C::RES_TILE + blk * kTbTile * 128, &map_res2, ((t.st + a) * h + t.hd) * DH + 64 * blk, t.r0, t.b, full);
+                    tma_load_3d(dst + NS * C::RES_TILE + blk * kTbTile * 128, &map_res1, t.hd * DH + 64 * blk, t.r0, t.b, full);
+                }
+            }
+            ++res_issued[rb];
+            if (++rb == C::NRES) { rb = 0; rph ^= 1u; }
+            for (int j = 0; j < t.J; ++j) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_EMPTY + s), ph, abort_flag, status, 0xb08u + s)) != 0;
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t full = bar(C::BAR_FULL + s), dst = sbase + C::OFF_RING + s * C::ROW_BYTES;
+                    const int row = t.s0 + j * kTbStep;
+                    mbar_arrive_expect_tx(full, C::ROW_BYTES + (KEYS ? 1024 : 0));
+                    for (int blk = 0; blk < C::NBLK; ++blk) {
+                        for (int a = 0; a < NS; ++a)
+                            tma_load_3d(dst + a * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row2, ((t.st + a) * h + t.hd) * DH + 64 * blk, row, t.b, full);
+                        tma_load_3d(dst + NS * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row1, t.hd * DH + 64 * blk, row, t.b, full);
+                    }
+                    if constexpr (KEYS) bulk_load_1d(sbase + C::OFF_STATS + s * 1024, p.stats + (t.bh * n64 + row / kTbStep) * 256, 1024, full);
+                }
+                ++issued[s];
+                if (++s == C::ST) { s = 0; ph ^= 1u; }
+            }
+        }
+        // never leave with a copy in flight
+        for (int q = 0; q < C::ST; ++q)
+            if (issued[q])
+                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(bar(C::BAR_FULL + q), (issued[q] - 1u) & 1u); ++i) {}
+        for (int q = 0; q < C::NRES; ++q)
+            if (res_issued[q])
+                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(bar(C::BAR_RESFULL + q), (res_issued[q] - 1u) & 1u); ++i) {}
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ front products
+        const uint64_t res_desc = make_sw128_desc(sbase), row_desc = make_sw128_desc(sbase + C::OFF_RING);
+        auto product = [&](uint32_t d, uint64_t a, uint64_t b) {
+#pragma unroll
+            for (int blk = 0; blk < C::NBLK; ++blk)
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    warp_mma_f16(d, a + (uint64_t)(blk * (kTbTile * 128 >> 4) + 2 * kk), b + (uint64_t)(blk * (C::ROW_BLOCK >> 4) + 2 * kk), C::IDESC_F,
+                                 (blk | kk) ? 1u : 0u);
+        };
+        bool ok = true;
+        int s = 0, rb = 0, g = 0;
+        uint32_t ph = 0, rph = 0;
+        Item t;
+        for (int k = 0; ok && item_of(k, t); ++k) {
+            if (!(ok = wait(C::BAR_RESFULL + rb, rph, 0xb10u))) break;
+            const uint64_t res = res_desc + (uint64_t)(rb * (C::RES_BYTES >> 4));
+            for (int j = 0; j < t.J; ++j, ++g) {
+                const int par = g & 1, ab = C::NA == 2 ? par : 0;
+                const uint64_t rows = row_desc + (uint64_t)(s * (C::ROW_BYTES >> 4));
+                if (!(ok = wait(C::BAR_FULL + s, ph, 0xb12u))) break;
+                // the buffers are free when the back products of two steps before are complete
+                if (!(ok = wait(C::BAR_BACK + par, ((uint32_t)(g >> 1) & 1u) ^ 1u, 0xb14u))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int a = 0; a < NS; ++a)
+                    product(tmem + C::COL_S + (par * NS + a) * kTbStep, res + (uint64_t)(a * (C::RES_TILE >> 4)), rows + (uint64_t)(a * (C::ROW_TILE >> 4)));
+                warp_commit(bar(C::BAR_S + par));
+                if constexpr (C::NA == 1) {
+                    if (!(ok = wait(C::BAR_AREAD, ((uint32_t)g & 1u) ^ 1u, 0xb16u))) break;
+                    tc_fence_after();
+                }
+                product(tmem + C::COL_A + ab * kTbStep, res + (uint64_t)(NS * (C::RES_TILE >> 4)), rows + (uint64_t)(NS * (C::ROW_TILE >> 4)));
+                warp_commit(bar(C::BAR_A + ab));
+                if (++s == C::ST) { s = 0; ph ^= 1u; }
+            }
+            if (!ok) break;
+            warp_commit(bar(C::BAR_RESEMPTY + rb));
+            if (++rb == C::NRES) { rb = 0; rph ^= 1u; }
+        }
+    } else if (warp == 2) {
+        // ------------------------------------------------------------------ back products
+        const uint64_t row_desc = make_sw128_mn_desc(sbase + C::OFF_RING, C::ROW_BLOCK);
+        auto product = [&](uint32_t d, uint32_t a, uint64_t b, bool first) {  // (a: sixteen columns of each half of the step)
+#pragma unroll
+            for (int kk = 0; kk < kTbStep / 16; ++kk)
+                warp_mma_f16_ts(d, a + (kk >> 1) * 32 + (kk & 1) * 8, b + (uint64_t)(128 * kk), C::IDESC_B, (!first || kk) ? 1u : 0u);
+        };
+        bool ok = true;
+        int s = 0, g = 0;
+        Item t;
+        for (int k = 0; ok && item_of(k, t); ++k) {
+            if (!(ok = wait(C::BAR_ACCREAD, ((uint32_t)k & 1u) ^ 1u, 0xb20u))) break;
+            for (int j = 0; j < t.J; ++j, ++g) {
+                const int par = g & 1;
+                const uint64_t rows = row_desc + (uint64_t)(s * (C::ROW_BYTES >> 4));
+                if (!(ok = wait(C::BAR_P + par, (uint32_t)(g >> 1) & 1u, 0xb22u))) break;
+                tc_fence_after();
+                const uint32_t col = tmem + C::COL_S + par * NS * kTbStep;
+                if constexpr (KEYS) product(tmem + C::COL_V, col + 16, rows + (uint64_t)(NS * (C::ROW_TILE >> 4)), j == 0 && (NS == 2 || t.st == 1));
+#pragma unroll
+                for (int a = 0; a < NS; ++a)
+                    product(tmem + C::COL_T + a * DH, col + a * kTbStep, rows + (uint64_t)(a * (C::ROW_TILE >> 4)), j == 0);
+                warp_commit(bar(C::BAR_BACK + par));
+                warp_commit(bar(C::BAR_EMPTY + s));
+                if (++s == C::ST) s = 0;
+            }
+            if (!ok) break;
+            warp_commit(bar(C::BAR_ACC));
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ probabilities and their gradients
+        const int half = warp >= 8 ? 1 : 0, quarter = warp & 3, row = 32 * quarter + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
+        const float c = p.scale_log2;
+        const uint64_t c2 = pack_f32x2(c, c);
+        double dl = 0.0;
+        bool ok = true;
+        int s = 0, g = 0;
+        Item t;
+        for (int k = 0; ok && item_of(k, t); ++k) {
+            const int mine = t.r0 + row, w0 = t.r0 + 32 * quarter;  // the thread's key or query; the warp's first
+            uint64_t nl[2] = {}, nd[2] = {}, sum = 0;               // (queries) -lse and -D of the row, twice each
+            if constexpr (!KEYS) {
+#pragma unroll
+                for (int a = 0; a < NS; ++a) {
+                    const float *st = p.stats + (t.bh * n64 + mine / 64) * 256 + mine % 64 + 64 * (t.st + a);
+                    const float l = mine < L ? __ldg(st) : -INFINITY, d = mine < L ? __ldg(st + 128) : 0.0f;
+                    nl[a] = pack_f32x2(l, l);
+                    nd[a] = pack_f32x2(d, d);
+                }
+            }
+            // what P is weighed by on its way into dV: 1 and -lambda
+            const float wp = NS == 2 || t.st == 1 ? -p.lambda : 1.0f;
+            const uint64_t wp2 = pack_f32x2(wp, wp);
+            for (int j = 0; j < t.J; ++j, ++g) {
+                const int par = g & 1, ab = C::NA == 2 ? par : 0, c0 = t.s0 + j * kTbStep + 32 * half;  // the thread's first column
+                const uint32_t s_addr = lane_base + C::COL_S + par * NS * kTbStep + 32 * half;
+                const float *stats = reinterpret_cast<const float *>(smem + C::OFF_STATS + s * 1024) + 32 * half + 64 * t.st;
+                if (!(ok = wait(C::BAR_S + par, (uint32_t)(g >> 1) & 1u, 0xb30u))) break;
+                tc_fence_after();
+                uint32_t x[NS][32];
+#pragma unroll
+                for (int a = 0; a < NS; ++a) tmem_ld32(s_addr + a * kTbStep, x[a]);
+                tmem_ld_wait();
+                // some pair of the warp has its key behind its query
+                if (KEYS ? c0 < w0 + 31 : c0 + 31 > w0) {
+#pragma unroll
+                    for (int a = 0; a < NS; ++a)
+#pragma unroll
+                        for (int u = 0; u < 32; ++u)
+                            if (KEYS ? c0 + u < mine : c0 + u > mine) x[a][u] = 0xff800000u;  // -inf: probability 0
+                }
+#pragma unroll
+                for (int a = 0; a < NS; ++a)
+#pragma unroll
+                    for (int u = 0; u < 32; u += 4) {
+                        ulonglong2 n = make_ulonglong2(nl[a], nl[a]);
+                        if constexpr (KEYS) n = *reinterpret_cast<const ulonglong2 *>(stats + 64 * a + u);
+                        float y[4];
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[a][u]), __uint_as_float(x[a][u + 1])), c2, n.x), y[0], y[1]);
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[a][u + 2]), __uint_as_float(x[a][u + 3])), c2, n.y), y[2], y[3]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[a][u + e] = __float_as_uint(tb_ex2(y[e]));
+                    }
+                if (!(ok = wait(C::BAR_A + ab, C::NA == 2 ? (uint32_t)(g >> 1) & 1u : (uint32_t)g & 1u, 0xb32u))) break;
+                tc_fence_after();
+                uint32_t dp[32];
+                tmem_ld32(lane_base + C::COL_A + ab * kTbStep + 32 * half, dp);
+                tmem_ld_wait();
+                if constexpr (C::NA == 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(C::BAR_AREAD));
+                }
+                auto two = [](const uint32_t *v) { return pack_f32x2(__uint_as_float(v[0]), __uint_as_float(v[1])); };
+                // P and T are rounded to bf16 for the products (2^-9 each, fp32 sums), as the forward pass rounds P
+                if constexpr (KEYS) {
+                    uint32_t o[16];
+#pragma unroll
+                    for (int u = 0; u < 32; u += 2)
+                        o[u >> 1] = tb_pack_bf16(NS == 2 ? fma_f32x2(two(&x[NS - 1][u]), wp2, two(&x[0][u])) : mul_f32x2(two(&x[0][u]), wp2));
+                    tmem_st16(s_addr + 16, o);
+                }
+#pragma unroll
+                for (int a = 0; a < NS; ++a) {
+                    uint32_t o[16];
+#pragma unroll
+                    for (int u = 0; u < 32; u += 4) {
+                        ulonglong2 n = make_ulonglong2(nd[a], nd[a]);
+                        if constexpr (KEYS) n = *reinterpret_cast<const ulonglong2 *>(stats + 128 + 64 * a + u);
+                        const uint64_t t0 = mul_f32x2(two(&x[a][u]), add_f32x2(two(&dp[u]), n.x)), t1 = mul_f32x2(two(&x[a][u + 2]), add_f32x2(two(&dp[u + 2]), n.y));
+                        o[u >> 1] = tb_pack_bf16(t0);
+                        o[(u >> 1) + 1] = tb_pack_bf16(t1);
+                        if (!KEYS && a == NS - 1) sum = add_f32x2(add_f32x2(t0, t1), sum);  // (of the second stream, or of the one at hand)
+                    }
+                    tmem_st16(s_addr + a * kTbStep, o);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::BAR_P + par));
+                if (++s == C::ST) s = 0;
+            }
+            if (!ok) break;
+            if constexpr (!KEYS) {
+                // sum_j P_2 A = D_2 + sum_j T_2: what P_2's sum is off from 1 then weighs the small T only
+                if (NS == 2 || t.st == 1) {
+                    float a, b, d, unused;
+                    unpack_f32x2(sum, a, b);
+                    unpack_f32x2(nd[NS - 1], d, unused);
+                    dl += (double)a + (double)b - (half ? 0.0 : (double)d);
+                }
+            }
+            // ---- outputs: this warp's rows, half of each accumulator's columns
+            if (!(ok = wait(C::BAR_ACC, (uint32_t)k & 1u, 0xb40u))) break;
+            tc_fence_after();
+            const size_t tok = (size_t)t.b * L + mine, width = (size_t)h * DH;
+            auto put = [&](uint32_t col, float f, __nv_bfloat16 *dst) {
+#pragma unroll
+                for (int cc = 0; cc < DH / 2; cc += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(lane_base + col + half * (DH / 2) + cc, v);
+                    tmem_ld_wait();
+                    if (mine < L) {
+#pragma unroll
+                        for (int u = 0; u < 32; u += 8) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[e] = tb_pack_bf16(__uint_as_float(v[u + 2 * e]) * f, __uint_as_float(v[u + 2 * e + 1]) * f);
+                            *reinterpret_cast<uint4 *>(dst + half * (DH / 2) + cc + u) = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                    }
+                }
+            };
+            if constexpr (KEYS)
+                if (NS == 2 || t.st == 0) put(C::COL_V, p.out_scale, p.d1 + tok * width + (size_t)t.hd * DH);
+#pragma unroll
+            for (int a = 0; a < NS; ++a)
+                put(C::COL_T + a * DH, p.out_scale * p.scale * (t.st + a == 1 ? -p.lambda : 1.0f),
+                    p.d2 + tok * 2 * width + ((size_t)(t.st + a) * h + t.hd) * DH);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::BAR_ACCREAD));
+        }
+        if constexpr (!KEYS) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) dl += __shfl_xor_sync(0xffffffffu, dl, o);
+            if (lane == 0) p.dl_part[(size_t)blockIdx.x * 8 + warp - 4] = dl;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// dlambda = -out_scale times the sum of the partial sums, in one order.
+__global__ void __launch_bounds__(32) attention_dlambda_kernel(const double *part, int n, float out_scale, float *dlambda) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n; i += 32) s += part[i];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (threadIdx.x == 0) *dlambda = (float)(-(double)out_scale * s);
+}
+
+static bool make_map_tokens(CUtensorMap *map, const void *base, uint64_t width, uint64_t L, uint64_t B, uint32_t rows) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    // (a dimension of its own for the batch: what lies behind a sequence reads as zeros, not as the next one)
+    cuuint64_t dims[3] = {width, L, B}, strides[2] = {width * 2, width * 2 * L};
+    cuuint32_t box[3] = {64, rows, 1}, one[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DH, bool KEYS>
+static cudaError_t launch_backward_pass(const AttnBackParams &p, const void *res2, const void *res1, const void *row2, const void *row1, int grid,
+                                        cudaStream_t stream) {
+    using C = TbCfg<DH, KEYS>;
+    static std::atomic<unsigned long long> attr_done{0};
+    cudaError_t e = ensure_dynamic_smem(attention_backward_kernel<DH, KEYS>, C::SMEM_BYTES, attr_done);
+    if (e != cudaSuccess) return e;
+    unsigned int *status = device_status_word();
+    if (!status) return cudaErrorMemoryAllocation;
+    const uint64_t w = (uint64_t)p.h * DH;
+    CUtensorMap m[4];
+    if (!make_map_tokens(&m[0], res2, 2 * w, p.L, p.B, kTbTile) || !make_map_tokens(&m[1], res1, w, p.L, p.B, kTbTile) ||
+        !make_map_tokens(&m[2], row2, 2 * w, p.L, p.B, kTbStep) || !make_map_tokens(&m[3], row1, w, p.L, p.B, kTbStep))
+        return cudaErrorInvalidValue;
+    attention_backward_kernel<DH, KEYS><<<grid, kTbThreads, C::SMEM_BYTES, stream>>>(m[0], m[1], m[2], m[3], p, status);
+    count_launch();
+    return cudaGetLastError();
+}
+
+constexpr int kTbMaxGrid = 1024;
+static size_t stats_bytes(int64_t B, int64_t L, int64_t h) { return (size_t)(B * h) * (size_t)((L + 63) / 64) * 1024; }
+
+template <int DH>
+static cudaError_t launch_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
+                                   const hgf_attention_grads &grads, AttnBackParams p, void *workspace, cudaStream_t stream) {
+    const int sms = device_sm_count();
+    if (!sms) return cudaErrorInvalidDevice;
+    const long long bhs = (long long)p.B * p.h, blocks = bhs * ((p.L + 63) / 64), tiles = bhs * ((p.L + kTbTile - 1) / kTbTile);
+    const int most = sms < kTbMaxGrid ? sms : kTbMaxGrid, grid = tiles < most ? (int)tiles : most;
+    float *stats = (float *)workspace;
+    p.stats = stats;
+    p.dl_part = (double *)((char *)workspace + stats_bytes(p.B, p.L, p.h));
+    attention_stats_kernel<DH><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream>>>(
+        (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)streams, lse, stats, p.B, p.L, p.h);
+    count_launch();
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess && (grads.dk || grads.dv)) {
+        p.d2 = (__nv_bfloat16 *)grads.dk;
+        p.d1 = (__nv_bfloat16 *)grads.dv;
+        e = launch_backward_pass<DH, true>(p, k, v, q, dout, grid, stream);
+    }
+    if (e == cudaSuccess && (grads.dq || grads.dlambda)) {
+        p.d2 = (__nv_bfloat16 *)grads.dq;
+        p.d1 = nullptr;
+        e = launch_backward_pass<DH, false>(p, q, dout, k, v, grid, stream);
+    }
+    if (e == cudaSuccess && grads.dlambda) {
+        attention_dlambda_kernel<<<1, 32, 0, stream>>>(p.dl_part, grid * 8, p.out_scale, grads.dlambda);
+        count_launch();
+        e = cudaGetLastError();
+    }
+    return e;
+}
+
+}  // namespace hgf
+
+using namespace hgf;
+
+static bool backward_sizes_ok(int64_t B, int64_t L, int32_t n_heads, int32_t head_dim) {
+    if ((head_dim != 64 && head_dim != 128) || B > 65535 || n_heads > 65535 || L > (1 << 24)) return false;
+    return B * L <= 0x7fffffffll && (uint64_t)B * (uint64_t)n_heads * (uint64_t)((L + kTbTile - 1) / kTbTile) <= 0x7fffffffull;
+}
+
+extern "C" size_t hgf_diff_attention_backward_workspace_bytes(int64_t B, int64_t L, int32_t n_heads, int32_t head_dim) {
+    if (B <= 0 || L <= 0 || n_heads <= 0 || !backward_sizes_ok(B, L, n_heads, head_dim)) return 0;
+    return stats_bytes(B, L, n_heads) + (size_t)kTbMaxGrid * 8 * sizeof(double);
+}
+
+extern "C" hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
+                                                  int64_t B, int64_t L, int32_t n_heads, int32_t head_dim, float lambda, float out_scale,
+                                                  const hgf_attention_grads *grads, void *workspace, size_t workspace_bytes, uint32_t flags,
+                                                  void *stream) {
+    if (!q || !k || !v || !dout || !streams || !lse || !grads || B <= 0 || L <= 0 || n_heads <= 0 || flags) return HGF_ERR_INVALID_ARG;
+    if (!backward_sizes_ok(B, L, n_heads, head_dim)) return HGF_ERR_UNSUPPORTED_SHAPE;
+    if ((grads->dk == nullptr) != (grads->dv == nullptr) || (!grads->dq && grads->dlambda)) return HGF_ERR_INVALID_ARG;
+    if ((((uintptr_t)q) | ((uintptr_t)k) | ((uintptr_t)v) | ((uintptr_t)dout) | ((uintptr_t)streams) | ((uintptr_t)lse) | ((uintptr_t)grads->dq) |
+         ((uintptr_t)grads->dk) | ((uintptr_t)grads->dv)) & 15u || ((uintptr_t)grads->dlambda & 3u))
+        return HGF_ERR_MISALIGNED;
+    if (!workspace || workspace_bytes < hgf_diff_attention_backward_workspace_bytes(B, L, n_heads, head_dim)) return HGF_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 255u) return HGF_ERR_MISALIGNED;
+    if (!grads->dq && !grads->dk) return HGF_OK;
+    AttnBackParams p = {};
+    p.B = (int)B;
+    p.L = (int)L;
+    p.h = n_heads;
+    p.lambda = lambda;
+    p.out_scale = out_scale;
+    p.scale = (float)(1.0 / sqrt((double)head_dim));
+    p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)head_dim));
+    const cudaError_t e = head_dim == 64 ? launch_backward<64>(q, k, v, dout, streams, lse, *grads, p, workspace, (cudaStream_t)stream)
+                                         : launch_backward<128>(q, k, v, dout, streams, lse, *grads, p, workspace, (cudaStream_t)stream);
+    return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
+}

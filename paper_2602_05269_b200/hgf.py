@@ -38,7 +38,8 @@ EXPORTS = ["hgf_packed_bytes", "hgf_pack_ternary", "hgf_unpack_ternary", "hgf_wo
            "hgf_linear_forward_phases", "hgf_linear_forward_ln",
            "hgf_packed_bytes_b3", "hgf_pack_ternary_b3", "hgf_unpack_ternary_b3",
            "hgf_selftest_wait_timeout", "hgf_group_create_ln",
-           "hgf_diff_attention_forward", "hgf_diff_lambda0", "hgf_backward_workspace_bytes", "hgf_linear_backward",
+           "hgf_diff_attention_forward", "hgf_diff_lambda0", "hgf_diff_attention_forward_train",
+           "hgf_diff_attention_backward_workspace_bytes", "hgf_diff_attention_backward", "hgf_backward_workspace_bytes", "hgf_linear_backward",
            "hgf_cache_reserve", "hgf_cache_append", "hgf_cache_read", "hgf_cache_fork", "hgf_cache_free",
            "hgf_cached_workspace_bytes", "hgf_diff_attention_cached"]
 
@@ -64,6 +65,10 @@ class DebugOut(ctypes.Structure):
 class Grads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dW", ctypes.c_void_p), ("dAt", ctypes.c_void_p), ("dBt", ctypes.c_void_p),
                 ("dgate", ctypes.c_void_p)]
+
+
+class AttentionGrads(ctypes.Structure):
+    _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p), ("dlambda", ctypes.c_void_p)]
 
 
 class Cache(ctypes.Structure):
@@ -124,6 +129,12 @@ def lib() -> ctypes.CDLL:
         L.hgf_selftest_wait_timeout.argtypes = [u32, vp]
         L.hgf_diff_attention_forward.restype = c.c_int
         L.hgf_diff_attention_forward.argtypes = [vp, vp, vp, i64, i64, i32, i32, c.c_float, c.c_float, vp, u32, vp]
+        L.hgf_diff_attention_forward_train.restype = c.c_int
+        L.hgf_diff_attention_forward_train.argtypes = [vp, vp, vp, i64, i64, i32, i32, c.c_float, c.c_float, vp, vp, vp, u32, vp]
+        L.hgf_diff_attention_backward_workspace_bytes.restype = sz
+        L.hgf_diff_attention_backward_workspace_bytes.argtypes = [i64, i64, i32, i32]
+        L.hgf_diff_attention_backward.restype = c.c_int
+        L.hgf_diff_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i32, i32, c.c_float, c.c_float, c.POINTER(AttentionGrads), vp, sz, u32, vp]
         L.hgf_diff_lambda0.restype = c.c_double
         L.hgf_diff_lambda0.argtypes = [c.c_double]
         L.hgf_backward_workspace_bytes.restype = sz
@@ -452,6 +463,76 @@ def diff_attention_forward(q, k, v, B: int, L: int, n_heads: int, head_dim: int,
            lib().hgf_diff_attention_forward(_ptr(q), _ptr(k), _ptr(v), B, L, n_heads, head_dim, ctypes.c_float(lam),
                                             ctypes.c_float(out_scale), _ptr(out), flags, _stream(stream)))
     return out
+
+
+def _current_device(device):
+    """Training calls run on the current device, and so has their memory to be there."""
+    assert device.type == "cuda" and device.index == torch.cuda.current_device(), f"the tensors are on {device}, which is not the current device"
+
+
+def _dense(what, t, dtype, shape, device):
+    assert t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.device == device and t.is_contiguous(), \
+        f"{what} has to be dense {dtype} {list(shape)} on {device}"
+
+
+def _attention_inputs(q, k, v, B, L, n_heads, head_dim):
+    width = n_heads * head_dim
+    _current_device(q.device)
+    for what, t, w in (("q", q, 2 * width), ("k", k, 2 * width), ("v", v, width)):
+        _dense(what, t, torch.bfloat16, (B * L, w), q.device)
+    return width
+
+
+def diff_attention_forward_train(q, k, v, B: int, L: int, n_heads: int, head_dim: int, lam: float, out_scale: float = 1.0, *,
+                                 out=None, streams=None, lse=None, flags: int = 0, stream=None):
+    """hgf_diff_attention_forward_train: diff_attention_forward that keeps what diff_attention_backward needs.  Returns (out, streams, lse):
+    streams bf16 [B*L][2*n_heads*head_dim], lse fp32 [B][n_heads][2][L]; all three are reused when given."""
+    width = _attention_inputs(q, k, v, B, L, n_heads, head_dim)
+    dtype = torch.bfloat16 if flags & FLAG_OUT_BF16 else torch.float32
+    with _on(stream):
+        out = torch.empty((B * L, width), dtype=dtype, device=q.device) if out is None else out
+        streams = torch.empty((B * L, 2 * width), dtype=torch.bfloat16, device=q.device) if streams is None else streams
+        lse = torch.empty((B, n_heads, 2, L), dtype=torch.float32, device=q.device) if lse is None else lse
+    _dense("out", out, dtype, (B * L, width), q.device)
+    _dense("streams", streams, torch.bfloat16, (B * L, 2 * width), q.device)
+    _dense("lse", lse, torch.float32, (B, n_heads, 2, L), q.device)
+    _check("hgf_diff_attention_forward_train",
+           lib().hgf_diff_attention_forward_train(_ptr(q), _ptr(k), _ptr(v), B, L, n_heads, head_dim, lam, out_scale, _ptr(out), _ptr(streams), _ptr(lse),
+                                                  flags, _stream(stream)))
+    return out, streams, lse
+
+
+def diff_attention_backward_workspace_bytes(B: int, L: int, n_heads: int, head_dim: int) -> int:
+    return int(lib().hgf_diff_attention_backward_workspace_bytes(B, L, n_heads, head_dim))
+
+
+def diff_attention_backward(q, k, v, dout, streams, lse, B: int, L: int, n_heads: int, head_dim: int, lam: float, out_scale: float = 1.0, *,
+                            want=None, out=None, workspace=None, stream=None):
+    """hgf_diff_attention_backward: dout bf16 [B*L][n_heads*head_dim], streams and lse as diff_attention_forward_train left them.  Returns a dict of
+    device tensors dq, dk, dv (bf16, as q, k, v) and dlambda (fp32 [1]); `want` restricts which are computed (dk and dv together, dlambda with dq
+    only).  `out` (a dict returned by an earlier call of the same shape) and `workspace` are reused when given."""
+    width = _attention_inputs(q, k, v, B, L, n_heads, head_dim)
+    _dense("dout", dout, torch.bfloat16, (B * L, width), q.device)
+    _dense("streams", streams, torch.bfloat16, (B * L, 2 * width), q.device)
+    _dense("lse", lse, torch.float32, (B, n_heads, 2, L), q.device)
+    like = {"dq": q, "dk": k, "dv": v}
+    names = [n for n in ("dq", "dk", "dv", "dlambda") if want is None or n in want]
+    need = diff_attention_backward_workspace_bytes(B, L, n_heads, head_dim)
+    if out is not None and workspace is None:
+        workspace = out.get("_workspace")
+    with _on(stream):
+        if out is None:
+            out = {n: torch.empty_like(like[n]) if n in like else torch.empty(1, dtype=torch.float32, device=q.device) for n in names}
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    for n in names:
+        _dense(n, out[n], torch.bfloat16 if n in like else torch.float32, like[n].shape if n in like else (1,), q.device)
+    assert workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.device == q.device, "the workspace is dense bytes on the tensors' device"
+    g = AttentionGrads(*[out[n].data_ptr() if n in names else None for n in ("dq", "dk", "dv", "dlambda")])
+    _check("hgf_diff_attention_backward",
+           lib().hgf_diff_attention_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(streams), _ptr(lse), B, L, n_heads, head_dim, lam, out_scale,
+                                             ctypes.byref(g), _ptr(workspace), workspace.numel(), 0, _stream(stream)))
+    return {**{n: out[n] for n in names}, "_workspace": workspace}
 
 
 CACHE_BLOCK = 64
