@@ -52,6 +52,7 @@ typedef enum {
 
 #define HGF_FLAG_NO_PDL 0x8u     /* do not use programmatic dependent launch (see hgf_linear_forward) */
 #define HGF_FLAG_BASE3 0x10u     /* `packed` is in the base-3 layout of hgf_pack_ternary_b3 */
+#define HGF_FLAG_ROTATE_PAIRS 0x20u /* hgf_qk_norm_rotate: pair i is dims 2 i and 2 i + 1, not i and i + rotary_dim / 2 */
 
 /* Largest token count the register-resident decode path handles; above it the GEMM path runs. */
 #define HGF_DECODE_MAX_M 16
@@ -387,6 +388,73 @@ hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void 
                                        const void *streams, const float *lse, int64_t B, int64_t L, int32_t n_heads,
                                        int32_t head_dim, float lambda, float out_scale, const hgf_attention_grads *grads,
                                        void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+
+/*
+ * Norms of the heads of Q and K with the rotation by position, between the projections and the attention (or hgf_cache_append), in one pass.  (The
+ * paper's attention knows no positions; this is what gives its tokens some.)  For a head x of d dims of a token at position p
+ *     u = x / sqrt(mean(x^2) + eps),   y = R(p) (u (.) weight)
+ * where R(p) turns pair i = 0 .. rotary_dim / 2 - 1 of dims (a, b) by the angle p base^(-2 i / rotary_dim):
+ *     y_a = a cos - b sin,  y_b = a sin + b cos
+ * The pair is dims i and i + rotary_dim / 2, with HGF_FLAG_ROTATE_PAIRS dims 2 i and 2 i + 1; dims from rotary_dim on are not turned.  Angles are
+ * formed in 64 bits, so that a far position loses nothing.
+ *   q, k       [n_rows][q_heads * head_dim], [n_rows][k_heads * head_dim]  bfloat16 (q_heads and k_heads count the heads of both streams); either
+ *              may be null and is left out
+ *   positions  device int32 [n_rows], any values
+ *   q_weight, k_weight  device fp32 [head_dim], shared by the heads; null = ones
+ *   q_out, k_out        bfloat16, laid out as q and k; they may be q and k themselves
+ * n_rows >= 1, head_dim 64 or 128, rotary_dim a multiple of 16 from 0 to head_dim, eps >= 0, base > 0, 16-byte aligned pointers.  Enqueue only.
+ *
+ * The backward call takes the same inputs (q and k as they were before the norm) and the gradients of q_out and k_out; with g = R(p)^T dy
+ *     dweight = sum over rows and heads of g (.) u        dx = ( g (.) weight - u mean(g (.) weight (.) u) ) / sqrt(mean(x^2) + eps)
+ *   dq_out, dk_out  bfloat16, laid out as q and k
+ *   grads           dq, dk bfloat16 (they may be dq_out and dk_out themselves); dwq, dwk fp32 [head_dim].  Null: not computed
+ *   workspace       hgf_qk_norm_rotate_workspace_bytes(head_dim) bytes, 256-byte aligned; scratch, not shared by calls that may overlap on the device,
+ *                   not needed without dwq and dwk
+ * Every sum has one order on a given GPU: equal calls give equal bits.
+ */
+typedef struct {
+    void *dq;
+    void *dk;
+    float *dwq;
+    float *dwk;
+} hgf_rotate_grads;
+hgf_status hgf_qk_norm_rotate(const void *q, const void *k, int64_t n_rows, int32_t q_heads, int32_t k_heads,
+                              int32_t head_dim, const int32_t *positions, const float *q_weight, const float *k_weight,
+                              float eps, double base, int32_t rotary_dim, void *q_out, void *k_out, uint32_t flags,
+                              void *stream);
+size_t hgf_qk_norm_rotate_workspace_bytes(int32_t head_dim);
+hgf_status hgf_qk_norm_rotate_backward(const void *q, const void *k, int64_t n_rows, int32_t q_heads, int32_t k_heads,
+                                       int32_t head_dim, const int32_t *positions, const float *q_weight,
+                                       const float *k_weight, float eps, double base, int32_t rotary_dim,
+                                       const void *dq_out, const void *dk_out, const hgf_rotate_grads *grads,
+                                       void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+
+/*
+ * The norm over all gradients of a training step (hgf_linear_backward, hgf_diff_attention_backward, hgf_qk_norm_rotate_backward, ...), and the
+ * gradients scaled so that it stays below a limit:
+ *     norm = sqrt(sum over all tensors of x^2),   y = x min(1, max_norm / (norm + 1e-6))
+ * The squares are summed in 64 bits in one order on a given GPU.  An infinite norm gives the factor 0, one that is no number a factor that is none.
+ *
+ * hgf_grad_list_create records the tensors (pointers are kept, not the data: the tensors stay owned by the caller and must stay valid) and allocates
+ * the list's descriptors and workspace on the current device; it is a set-up call that synchronises.
+ *   x, y   device, n elements of type HGF_FP32 or HGF_BF16, aligned to their element (16-byte aligned ones are read and written in 16-byte words);
+ *          y may be x itself: the gradient is scaled in place (and not touched where the factor is 1).  n may be 0.
+ * An y that overlaps another y, or an x other than its own, is refused (HGF_ERR_INVALID_ARG).
+ * hgf_clip_grad_norm only enqueues; max_norm >= 0 (infinity: the norm alone), norm: device fp32, nullable.  The current device must be the list's.
+ * Calls on one list must not overlap on the device.  hgf_grad_list_destroy frees the list (the caller makes sure no call is still running).
+ */
+#define HGF_FP32 0
+#define HGF_BF16 1
+typedef struct {
+    const void *x;
+    void *y;
+    int64_t n;
+    int32_t type;
+} hgf_tensor;
+typedef struct hgf_grad_list hgf_grad_list;
+hgf_status hgf_grad_list_create(const hgf_tensor *tensors /* host array */, int32_t n, hgf_grad_list **out);
+hgf_status hgf_clip_grad_norm(hgf_grad_list *list, float max_norm, float *norm, void *stream);
+void hgf_grad_list_destroy(hgf_grad_list *list);
 
 /*
  * ---- K/V cache of the differential attention, in 8 bits ------------------------------------------------------

@@ -1,0 +1,212 @@
+// The norm over all gradients of a training step, and the gradients scaled so that it stays below a limit:
+//     norm = sqrt(sum of all g^2),   y = g min(1, max_norm / (norm + 1e-6))
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "hgf_common.cuh"
+#include "hgf_warp.cuh"
+
+namespace hgf {
+
+// A piece of a tensor, worked by one warp.  All but the ends of a tensor begin at a 16-byte boundary of x.
+struct alignas(32) ClipPiece {
+    const void *x;
+    void *y;
+    int n;               // elements
+    int bf16, vx, vy;    // x (and y) in 16-byte words
+};
+
+constexpr int kClipThreads = 256, kClipWarps = kClipThreads / 32, kClipBytes = 16384;
+
+__device__ __forceinline__ double square_sum(uint4 v, int bf16) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (bf16) {
+            const double a = bf16lo_to_float(w[i]), b = bf16hi_to_float(w[i]);
+            s = fma(a, a, fma(b, b, s));
+        } else {
+            const double a = __uint_as_float(w[i]);
+            s = fma(a, a, s);
+        }
+    }
+    return s;
+}
+__device__ __forceinline__ float clip_element(const ClipPiece &c, int i) {
+    return c.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(c.x)[i]) : static_cast<const float *>(c.x)[i];
+}
+
+// Sums of squares in 64 bits: no magnitude of a gradient overflows or vanishes, and the order moves nothing that fp32 shows.
+__global__ void __launch_bounds__(kClipThreads) clip_sums_kernel(const ClipPiece *pieces, int n, double *part) {
+    __shared__ double s_sum[kClipWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = gridDim.x * kClipWarps;
+    double sum = 0.0;
+    for (int i = blockIdx.x * kClipWarps + warp; i < n; i += warps) {
+        const ClipPiece c = pieces[i];
+        int at = 0;
+        if (c.vx) {
+            const int per = c.bf16 ? 8 : 4, words = c.n / per;
+            const uint4 *x = static_cast<const uint4 *>(c.x);
+            for (int j = lane; j < words; j += 128) {
+                uint4 v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = j + 32 * u < words ? x[j + 32 * u] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sum += square_sum(v[u], c.bf16);
+            }
+            at = words * per;
+        }
+        for (int j = at + lane; j < c.n; j += 32) {
+            const double a = clip_element(c, j);
+            sum = fma(a, a, sum);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int q = 1; q < kClipWarps; ++q) sum += s_sum[q];
+        part[blockIdx.x] = sum;
+    }
+}
+
+__device__ __forceinline__ uint32_t scaled_word(uint32_t w, float f, int bf16) {
+    if (!bf16) return __float_as_uint(__uint_as_float(w) * f);
+    const __nv_bfloat162 b = __floats2bfloat162_rn(bf16lo_to_float(w) * f, bf16hi_to_float(w) * f);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+
+__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipPiece *pieces, int n, const double *part, int n_part, float max_norm, float *norm_out) {
+    __shared__ double s_sum[kClipWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = gridDim.x * kClipWarps;
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < n_part; i += kClipThreads) sum += part[i];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int q = 0; q < kClipWarps; ++q) sum += s_sum[q];
+    const double norm = sqrt(sum), ratio = (double)max_norm / (norm + 1e-6);
+    const float f = ratio >= 1.0 ? 1.0f : (float)ratio;  // (a norm that is no number gives a factor that is none)
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    // backwards: the pieces that were read last may still be in the L2 cache
+    for (int i = n - 1 - (blockIdx.x * kClipWarps + warp); i >= 0; i -= warps) {
+        const ClipPiece c = pieces[i];
+        if (f == 1.0f && c.x == c.y) continue;
+        int at = 0;
+        if (c.vx && c.vy) {
+            const int per = c.bf16 ? 8 : 4, words = c.n / per;
+            const uint4 *x = static_cast<const uint4 *>(c.x);
+            uint4 *y = static_cast<uint4 *>(c.y);
+            for (int j = lane; j < words; j += 128) {
+                uint4 v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (j + 32 * u < words) v[u] = x[j + 32 * u];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (j + 32 * u < words)
+                        y[j + 32 * u] = make_uint4(scaled_word(v[u].x, f, c.bf16), scaled_word(v[u].y, f, c.bf16), scaled_word(v[u].z, f, c.bf16), scaled_word(v[u].w, f, c.bf16));
+            }
+            at = words * per;
+        }
+        for (int j = at + lane; j < c.n; j += 32) {
+            const float v = clip_element(c, j) * f;
+            if (c.bf16) static_cast<__nv_bfloat16 *>(c.y)[j] = __float2bfloat16_rn(v);
+            else static_cast<float *>(c.y)[j] = v;
+        }
+    }
+}
+
+}  // namespace hgf
+
+using namespace hgf;
+
+struct hgf_grad_list {
+    int device, n, grid;
+    void *mem;           // pieces, then the blocks' sums
+    double *part;
+};
+
+extern "C" hgf_status hgf_grad_list_create(const hgf_tensor *tensors, int32_t n, hgf_grad_list **out) try {
+    if (!tensors || !out || n <= 0) return HGF_ERR_INVALID_ARG;
+    *out = nullptr;
+    std::vector<ClipPiece> pieces;
+    for (int32_t i = 0; i < n; ++i) {
+        const hgf_tensor &t = tensors[i];
+        if (t.n < 0 || t.n > ((int64_t)1 << 48) || (t.n && (!t.x || !t.y)) || (t.type != HGF_FP32 && t.type != HGF_BF16)) return HGF_ERR_INVALID_ARG;
+        const int size = t.type == HGF_BF16 ? 2 : 4;
+        if ((((uintptr_t)t.x) | ((uintptr_t)t.y)) & (size - 1)) return HGF_ERR_MISALIGNED;
+    }
+    // nothing is written twice, or read by one warp while another writes it
+    struct Range { uintptr_t begin, end; int32_t tensor; };
+    std::vector<Range> ys;
+    for (int32_t i = 0; i < n; ++i)
+        if (tensors[i].n) ys.push_back(Range{(uintptr_t)tensors[i].y, (uintptr_t)tensors[i].y + tensors[i].n * (tensors[i].type == HGF_BF16 ? 2 : 4), i});
+    std::sort(ys.begin(), ys.end(), [](const Range &a, const Range &b) { return a.begin < b.begin; });
+    for (size_t i = 1; i < ys.size(); ++i)
+        if (ys[i].begin < ys[i - 1].end) return HGF_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < n; ++i) {
+        const hgf_tensor &t = tensors[i];
+        if (!t.n) continue;
+        const uintptr_t begin = (uintptr_t)t.x, end = begin + t.n * (t.type == HGF_BF16 ? 2 : 4);
+        auto y = std::upper_bound(ys.begin(), ys.end(), begin, [](uintptr_t a, const Range &b) { return a < b.end; });  // the first that ends behind x's beginning
+        for (; y != ys.end() && y->begin < end; ++y)
+            if (y->tensor != i || y->begin != begin) return HGF_ERR_INVALID_ARG;
+    }
+    for (int32_t i = 0; i < n; ++i) {
+        const hgf_tensor &t = tensors[i];
+        const int size = t.type == HGF_BF16 ? 2 : 4;
+        for (int64_t at = 0; at < t.n;) {
+            const uintptr_t x = (uintptr_t)t.x + at * size, y = (uintptr_t)t.y + at * size;
+            const int64_t most = x & 15 ? (int64_t)(16 - (x & 15)) / size : kClipBytes / size, len = most < t.n - at ? most : t.n - at;
+            if (pieces.size() >= 0x7fffffffu / sizeof(ClipPiece)) return HGF_ERR_TOO_LARGE;
+            pieces.push_back(ClipPiece{(const void *)x, (void *)y, (int)len, size == 2, (x & 15) == 0, (y & 15) == 0});
+            at += len;
+        }
+    }
+    const int sms = device_sm_count(), dev = current_device();
+    if (!sms || dev < 0) return HGF_ERR_CUDA;
+    const long long blocks = ((long long)pieces.size() + kClipWarps - 1) / kClipWarps;
+    const int grid = blocks < 1 ? 1 : blocks < 4 * sms ? (int)blocks : 4 * sms;
+    const size_t off = align_up(pieces.size() * sizeof(ClipPiece), 256);
+    void *mem = nullptr;
+    if (cudaMalloc(&mem, off + grid * sizeof(double)) != cudaSuccess) {
+        cudaGetLastError();
+        return HGF_ERR_CUDA;
+    }
+    hgf_grad_list *l = new (std::nothrow) hgf_grad_list{dev, (int)pieces.size(), grid, mem, (double *)((char *)mem + off)};
+    if (!l || cudaMemcpy(mem, pieces.data(), pieces.size() * sizeof(ClipPiece), cudaMemcpyHostToDevice) != cudaSuccess) {
+        cudaFree(mem);
+        delete l;
+        return HGF_ERR_CUDA;
+    }
+    *out = l;
+    return HGF_OK;
+} catch (...) {  // (out of host memory)
+    return HGF_ERR_TOO_LARGE;
+}
+
+extern "C" hgf_status hgf_clip_grad_norm(hgf_grad_list *list, float max_norm, float *norm, void *stream) {
+    if (!list || !(max_norm >= 0.0f)) return HGF_ERR_INVALID_ARG;
+    if ((uintptr_t)norm & 3u) return HGF_ERR_MISALIGNED;
+    if (current_device() != list->device) return HGF_ERR_INVALID_ARG;
+    const ClipPiece *pieces = (const ClipPiece *)list->mem;
+    clip_sums_kernel<<<list->grid, kClipThreads, 0, (cudaStream_t)stream>>>(pieces, list->n, list->part);
+    count_launch();
+    if (cudaGetLastError() != cudaSuccess) return HGF_ERR_CUDA;
+    clip_scale_kernel<<<list->grid, kClipThreads, 0, (cudaStream_t)stream>>>(pieces, list->n, list->part, list->grid, max_norm, norm);
+    count_launch();
+    return cudaGetLastError() == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
+}
+
+extern "C" void hgf_grad_list_destroy(hgf_grad_list *list) {
+    if (!list) return;
+    cudaFree(list->mem);
+    delete list;
+}

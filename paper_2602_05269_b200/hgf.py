@@ -26,6 +26,7 @@ FLAG_NO_SILU = 0x2
 FLAG_FORCE_GEMM = 0x4
 FLAG_NO_PDL = 0x8
 FLAG_BASE3 = 0x10
+FLAG_ROTATE_PAIRS = 0x20
 DECODE_MAX_M = 16
 PHASE_PROLOGUE = 0x1
 PHASE_GEMV = 0x2
@@ -39,7 +40,9 @@ EXPORTS = ["hgf_packed_bytes", "hgf_pack_ternary", "hgf_unpack_ternary", "hgf_wo
            "hgf_packed_bytes_b3", "hgf_pack_ternary_b3", "hgf_unpack_ternary_b3",
            "hgf_selftest_wait_timeout", "hgf_group_create_ln",
            "hgf_diff_attention_forward", "hgf_diff_lambda0", "hgf_diff_attention_forward_train",
-           "hgf_diff_attention_backward_workspace_bytes", "hgf_diff_attention_backward", "hgf_backward_workspace_bytes", "hgf_linear_backward",
+           "hgf_diff_attention_backward_workspace_bytes", "hgf_diff_attention_backward",
+           "hgf_qk_norm_rotate", "hgf_qk_norm_rotate_workspace_bytes", "hgf_qk_norm_rotate_backward",
+           "hgf_grad_list_create", "hgf_clip_grad_norm", "hgf_grad_list_destroy", "hgf_backward_workspace_bytes", "hgf_linear_backward",
            "hgf_cache_reserve", "hgf_cache_append", "hgf_cache_read", "hgf_cache_fork", "hgf_cache_free",
            "hgf_cached_workspace_bytes", "hgf_diff_attention_cached"]
 
@@ -69,6 +72,14 @@ class Grads(ctypes.Structure):
 
 class AttentionGrads(ctypes.Structure):
     _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p), ("dlambda", ctypes.c_void_p)]
+
+
+class RotateGrads(ctypes.Structure):
+    _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dwq", ctypes.c_void_p), ("dwk", ctypes.c_void_p)]
+
+
+class TensorEntry(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32)]
 
 
 class Cache(ctypes.Structure):
@@ -141,6 +152,19 @@ def lib() -> ctypes.CDLL:
         L.hgf_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
         L.hgf_linear_backward.restype = c.c_int
         L.hgf_linear_backward.argtypes = [vp, i64, vp, c.c_float, i64, i64, vp, vp, i32, vp, vp, c.POINTER(Grads), vp, sz, u32, vp]
+        L.hgf_qk_norm_rotate.restype = c.c_int
+        L.hgf_qk_norm_rotate.argtypes = [vp, vp, i64, i32, i32, i32, vp, vp, vp, c.c_float, c.c_double, i32, vp, vp, u32, vp]
+        L.hgf_qk_norm_rotate_workspace_bytes.restype = sz
+        L.hgf_qk_norm_rotate_workspace_bytes.argtypes = [i32]
+        L.hgf_qk_norm_rotate_backward.restype = c.c_int
+        L.hgf_qk_norm_rotate_backward.argtypes = [vp, vp, i64, i32, i32, i32, vp, vp, vp, c.c_float, c.c_double, i32, vp, vp, c.POINTER(RotateGrads), vp, sz, u32,
+                                                  vp]
+        L.hgf_grad_list_create.restype = c.c_int
+        L.hgf_grad_list_create.argtypes = [c.POINTER(TensorEntry), i32, c.POINTER(vp)]
+        L.hgf_clip_grad_norm.restype = c.c_int
+        L.hgf_clip_grad_norm.argtypes = [vp, c.c_float, vp, vp]
+        L.hgf_grad_list_destroy.restype = None
+        L.hgf_grad_list_destroy.argtypes = [vp]
         cache = c.POINTER(Cache)
         L.hgf_cache_reserve.restype = c.c_int
         L.hgf_cache_reserve.argtypes = [cache, vp, vp, i64, vp, vp]
@@ -533,6 +557,117 @@ def diff_attention_backward(q, k, v, dout, streams, lse, B: int, L: int, n_heads
            lib().hgf_diff_attention_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(streams), _ptr(lse), B, L, n_heads, head_dim, lam, out_scale,
                                              ctypes.byref(g), _ptr(workspace), workspace.numel(), 0, _stream(stream)))
     return {**{n: out[n] for n in names}, "_workspace": workspace}
+
+
+def _rotate_inputs(q, k, positions, head_dim, wq, wk):
+    """Checks what both directions read; returns (the device, rows, heads of q, heads of k)."""
+    some = q if q is not None else k
+    assert some is not None and head_dim > 0, "qk_norm_rotate takes q, k or both"
+    device, rows = some.device, some.shape[0]
+    _current_device(device)
+    for what, x in (("q", q), ("k", k)):
+        assert x is None or (x.dim() == 2 and x.shape[1] % head_dim == 0), f"{what} is a matrix of heads of {head_dim}"
+        if x is not None:
+            _dense(what, x, torch.bfloat16, (rows, x.shape[1]), device)
+    _dense("positions", positions, torch.int32, (rows,), device)
+    for what, w in (("wq", wq), ("wk", wk)):
+        if w is not None:
+            _dense(what, w, torch.float32, (head_dim,), device)
+    return device, rows, 0 if q is None else q.shape[1] // head_dim, 0 if k is None else k.shape[1] // head_dim
+
+
+def qk_norm_rotate(q, k, positions, head_dim: int, wq=None, wk=None, *, eps: float = 1e-6, base: float = 10000.0, rotary_dim: int | None = None,
+                   q_out=None, k_out=None, flags: int = 0, stream=None):
+    """hgf_qk_norm_rotate: the heads of q (bf16 [n_rows][heads * head_dim]) and k, each normalised, weighed by wq or wk (fp32 [head_dim], None: ones)
+    and rotated by the row's position (int32 [n_rows]) -> (q_out, k_out), which may be q and k themselves.  q or k may be None.  rotary_dim: dims that
+    are rotated (None: all).  FLAG_ROTATE_PAIRS: neighbouring dims are the pairs."""
+    device, rows, hq, hk = _rotate_inputs(q, k, positions, head_dim, wq, wk)
+    with _on(stream):
+        q_out = torch.empty_like(q) if q_out is None and q is not None else q_out
+        k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
+    for what, x, y in (("q_out", q, q_out), ("k_out", k, k_out)):
+        assert (x is None) == (y is None), f"{what} without its input"
+        if x is not None:
+            _dense(what, y, torch.bfloat16, x.shape, device)
+    _check("hgf_qk_norm_rotate",
+           lib().hgf_qk_norm_rotate(_ptr(q), _ptr(k), rows, hq, hk, head_dim, _ptr(positions), _ptr(wq), _ptr(wk), eps, base,
+                                    head_dim if rotary_dim is None else rotary_dim, _ptr(q_out), _ptr(k_out), flags, _stream(stream)))
+    return q_out, k_out
+
+
+def qk_norm_rotate_backward(q, k, positions, head_dim: int, dq_out, dk_out, wq=None, wk=None, *, eps: float = 1e-6, base: float = 10000.0,
+                            rotary_dim: int | None = None, want=None, out=None, workspace=None, flags: int = 0, stream=None):
+    """hgf_qk_norm_rotate_backward: q, k as they went into qk_norm_rotate, dq_out and dk_out (bf16) the gradients of what came out.  Returns a dict of
+    dq, dk (bf16) and dwq, dwk (fp32 [head_dim]) of the inputs that are given; `want` restricts which are computed.  `out` (a dict returned by an
+    earlier call of the same shape, or tensors of the caller's: dq may be dq_out itself) and `workspace` are reused when given."""
+    device, rows, hq, hk = _rotate_inputs(q, k, positions, head_dim, wq, wk)
+    like = {}
+    for what, x, g in (("q", q, dq_out), ("k", k, dk_out)):
+        assert (x is None) == (g is None), f"d{what}_out without {what}, or the other way round"
+        if x is not None:
+            _dense(f"d{what}_out", g, torch.bfloat16, x.shape, device)
+            like["d" + what], like["dw" + what] = (torch.bfloat16, x.shape), (torch.float32, (head_dim,))
+    names = [n for n in like if want is None or n in want]
+    if out is not None and workspace is None:
+        workspace = out.get("_workspace")
+    with _on(stream):
+        if out is None:
+            out = {n: torch.empty(like[n][1], dtype=like[n][0], device=device) for n in names}
+        if workspace is None:
+            workspace = torch.empty(int(lib().hgf_qk_norm_rotate_workspace_bytes(head_dim)), dtype=torch.uint8, device=device)
+    for n in names:
+        _dense(n, out[n], *like[n], device)
+    assert workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.device == device, "the workspace is dense bytes on the tensors' device"
+    g = RotateGrads(*[out[n].data_ptr() if n in names else None for n in ("dq", "dk", "dwq", "dwk")])
+    _check("hgf_qk_norm_rotate_backward",
+           lib().hgf_qk_norm_rotate_backward(_ptr(q), _ptr(k), rows, hq, hk, head_dim, _ptr(positions), _ptr(wq), _ptr(wk), eps, base,
+                                             head_dim if rotary_dim is None else rotary_dim, _ptr(dq_out), _ptr(dk_out), ctypes.byref(g), _ptr(workspace),
+                                             workspace.numel(), flags, _stream(stream)))
+    return {**{n: out[n] for n in names}, "_workspace": workspace}
+
+
+class GradList:
+    """The gradients of a training step (hgf_grad_list_create): dense fp32 or bf16 tensors on the current device, clipped together by clip().  They are
+    scaled in place, or into the tensors of `out`, of the same types and shapes.  The list goes by the tensors' addresses and keeps them alive: it has to
+    be made anew when a gradient becomes another tensor."""
+
+    def __init__(self, grads, out=None):
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        assert len(grads) == len(out) and grads, "a list has a tensor for each gradient"
+        self._handle = ctypes.c_void_p()
+        self.device = grads[0].device
+        _current_device(self.device)
+        arr = (TensorEntry * len(grads))()
+        for i, (x, y) in enumerate(zip(grads, out)):
+            assert x.dtype in (torch.float32, torch.bfloat16), "gradients are fp32 or bf16"
+            _dense(f"gradient {i}", x, x.dtype, x.shape, self.device)
+            _dense(f"output {i}", y, x.dtype, x.shape, self.device)
+            arr[i] = TensorEntry(x.data_ptr(), y.data_ptr(), x.numel(), int(x.dtype == torch.bfloat16))
+        self._keep = grads, out
+        _check("hgf_grad_list_create", lib().hgf_grad_list_create(arr, len(grads), ctypes.byref(self._handle)))
+
+    def clip(self, max_norm: float, *, norm=None, stream=None):
+        """hgf_clip_grad_norm: scales the gradients so that their common norm is at most max_norm.  Returns the norm before that (fp32 [1] on the
+        device, made here if not given)."""
+        _current_device(self.device)
+        if norm is None:
+            with _on(stream):
+                norm = torch.empty(1, dtype=torch.float32, device=self.device)
+        _dense("norm", norm, torch.float32, (1,), self.device)
+        _check("hgf_clip_grad_norm", lib().hgf_clip_grad_norm(self._handle, max_norm, _ptr(norm), _stream(stream)))
+        return norm
+
+    def close(self) -> None:
+        if self._handle:
+            lib().hgf_grad_list_destroy(self._handle)
+            self._handle = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 CACHE_BLOCK = 64
