@@ -11,8 +11,8 @@ namespace hgf {
 
 struct AttnBackParams {
     __nv_bfloat16 *d2, *d1;          // gradients of the two-stream tensor (dK or dQ) and, for keys, of V; d1 null for queries
-    const float *stats;              // [B*h][ceil(L / 64)][-lse_1, -lse_2, -D_1, -D_2][64]
-    double *dl_part;                 // (queries) [grid][8] partial sums of P_2 (.) A
+    const uint8_t *stats;            // [B*h][ceil(L / 64)] blocks of kTbStatBytes, see attention_stats_kernel
+    double *dl_part;                 // (queries) [grid][warps] partial sums of P_2 (.) A
     const double *dl_in;             // (keys) the same, of the launch before; null: none
     float *dlambda;
     int dl_n;
@@ -35,14 +35,29 @@ __device__ __forceinline__ uint32_t tb_pack_bf16(uint64_t v) {
     return tb_pack_bf16(lo, hi);
 }
 
+__device__ __forceinline__ void tb_load(uint32_t at, uint32_t (&v)[32]) { tmem_ld32(at, v); }
+__device__ __forceinline__ void tb_load(uint32_t at, uint32_t (&v)[16]) { tmem_ld16(at, v); }
+__device__ __forceinline__ void tb_store(uint32_t at, const uint32_t (&v)[16]) { tmem_st16(at, v); }
+__device__ __forceinline__ void tb_store(uint32_t at, const uint32_t (&v)[8]) { tmem_st8(at, v); }
+
 // ---- D and lse in the order in which the main kernels read them ------------------------------------------------------
-// A block takes 64 tokens of a (batch element, head): a row of G, O_1 and O_2 is read by head_dim / 8 lanes, 16 bytes each, the 256
-// results of the block are one contiguous KiB.  Rows behind the sequence get probability 0 (-lse = -infinity).
+// Where a lane is a key, D and lse belong to columns, and every thread would read all of them from shared memory: a wavefront a value and
+// warp (128-bit loads of one address take four), 1024 a step, half of what shared memory can do beside the products' operands.  So the
+// products subtract them: each score product takes 16 more terms, ones times a query's -lse / scale_log2 in three bf16 parts
+// (24 bits), A likewise -D.  Heads of 64, 4 x 4096 tokens:.
+// A block of 64 queries of a (batch element, head):
+//   [64][16] bf16, rows of 32 bytes with 32-byte swizzle: parts of -lse_1 / scale_log2 (0-2), -lse_2 / scale_log2 (3-5), -D_1 (6-8), -D_2 (9-11), 0
+//   [64] fp32 D_1 - D_2
+//   [4][64] fp32 -lse_1, -lse_2, -D_1, -D_2 for the lanes that are queries
+// Rows behind the sequence get probability 0 (an exponent of -infinity, or of -10^30 where 0 times it is formed).
+constexpr int kTbTileBytes = 2048, kTbDeltaBytes = 256, kTbStatBytes = kTbTileBytes + kTbDeltaBytes + 1024;
+
+// A thread block takes 64 tokens: a row of G, O_1 and O_2 is read by head_dim / 8 lanes, 16 bytes each.
 template <int DH>
 __global__ void __launch_bounds__(256)
-attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, const float *lse, float *stats, int B, int L, int h) {
+attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, const float *lse, uint8_t *stats, int B, int L, int h, float scale_log2) {
     constexpr int LPR = DH / 8, RPW = 32 / LPR;
-    __shared__ float s_d[2][64];
+    __shared__ float s_v[4][64];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = (L + 63) / 64;
     const long long tiles = (long long)B * h * blocks;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
@@ -72,16 +87,33 @@ attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, 
                 d2 += __shfl_xor_sync(0xffffffffu, d2, o);
             }
             if (lane % LPR == 0) {
-                s_d[0][r] = d1;
-                s_d[1][r] = d2;
+                s_v[2][r] = -d1;
+                s_v[3][r] = -d2;
             }
         }
+        const int kind = threadIdx.x >> 6, r = threadIdx.x & 63;
+        if (kind < 2) s_v[kind][r] = i0 + r < L ? -__ldg(lse + (bh * 2 + kind) * L + i0 + r) : -INFINITY;
         __syncthreads();
-        const int kind = threadIdx.x >> 6, r = threadIdx.x & 63, i = i0 + r;
-        float v;
-        if (kind < 2) v = i < L ? -__ldg(lse + (bh * 2 + kind) * L + i) : -INFINITY;
-        else v = i < L ? -s_d[kind - 2][r] : 0.0f;
-        stats[tile * 256 + threadIdx.x] = v;
+        uint8_t *at = stats + tile * kTbStatBytes;
+        reinterpret_cast<float *>(at + kTbTileBytes + kTbDeltaBytes)[threadIdx.x] = s_v[kind][r];
+        if (kind == 0) {
+            __nv_bfloat16 part[16] = {};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float v = s_v[q][r];
+                if (q < 2) v = i0 + r < L ? v / scale_log2 : -1e30f;
+#pragma unroll
+                for (int n = 0; n < 3; ++n) {
+                    part[3 * q + n] = __float2bfloat16_rn(v);
+                    v = v == -1e30f ? 0.0f : v - __bfloat162float(part[3 * q + n]);
+                }
+            }
+            const uint4 *w = reinterpret_cast<const uint4 *>(part);
+            reinterpret_cast<uint4 *>(at)[2 * r + ((r >> 2) & 1)] = w[0];
+            reinterpret_cast<uint4 *>(at)[2 * r + (((r >> 2) & 1) ^ 1)] = w[1];
+        } else if (kind == 1) {
+            reinterpret_cast<float *>(at + kTbTileBytes)[r] = s_v[3][r] - s_v[2][r];
+        }
         __syncthreads();
     }
 }
@@ -94,20 +126,22 @@ attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, 
 //   warp 1      front products: the scores of a step and A, [128 x 64] fp32 in tensor memory
 //   warp 2      back products: the accumulators += T_s (or P) times the step's rows; the first operand is bf16 in tensor
 //               memory, written over the scores that it came from; the second the streamed tile in its stored form
-//   warps 4-11  a thread owns a lane and half of the step's columns
+//   warps 4-19  a thread owns a lane and a quarter of the step's columns
 // NS streams are in flight at a time: two for head_dim 64; for head_dim 128 the accumulators take too many columns, so the
 // streams are items of their own, one after the other (with dV kept over both).
-constexpr int kTbThreads = 384, kTbTile = 128, kTbStep = 64;
+constexpr int kTbTile = 128, kTbStep = 64;
 
 template <int DH, bool KEYS>
 struct TbCfg {
     static constexpr int NS = DH == 64 ? 2 : 1;
+    static constexpr int PARTS = 4, COLS = kTbStep / PARTS, WARPS = 4 * PARTS, THREADS = 128 + 32 * WARPS;  // a thread's columns of a step, warps of them
     static constexpr int NBLK = DH / 64;
     static constexpr int NRES = DH == 64 ? 2 : 1;   // buffers of the resident operands
-    static constexpr int ST = DH == 64 ? 5 : 4;     // ring stages
+    static constexpr int ST = DH == 64 && !KEYS ? 5 : 4;  // ring stages
     static constexpr int RES_TILE = NBLK * kTbTile * 128, RES_BYTES = (NS + 1) * RES_TILE;
     static constexpr int ROW_BLOCK = kTbStep * 128, ROW_TILE = NBLK * ROW_BLOCK, ROW_BYTES = (NS + 1) * ROW_TILE;
-    static constexpr int OFF_RING = NRES * RES_BYTES, OFF_STATS = OFF_RING + ST * ROW_BYTES, OFF_BAR = OFF_STATS + (KEYS ? ST * 1024 : 0);
+    static constexpr int STAT_COPY = kTbTileBytes + (NS == 2 ? kTbDeltaBytes : 0), STAT_STAGE = kTbTileBytes + 512, ONES_TILE = kTbTile * 32;
+    static constexpr int OFF_RING = NRES * RES_BYTES, OFF_STATS = OFF_RING + ST * ROW_BYTES, OFF_ONES = OFF_STATS + (KEYS ? ST * STAT_STAGE : 0), OFF_BAR = OFF_ONES + (KEYS ? 4 * ONES_TILE : 0);
     static constexpr int BAR_RESFULL = 0, BAR_RESEMPTY = BAR_RESFULL + NRES, BAR_FULL = BAR_RESEMPTY + NRES, BAR_EMPTY = BAR_FULL + ST,
                          BAR_S = BAR_EMPTY + ST,       // [parity of the step] scores are there
                          BAR_A = BAR_S + 2,            // A is there
@@ -127,7 +161,7 @@ struct TbCfg {
 };
 
 template <int DH, bool KEYS>
-__global__ void __launch_bounds__(kTbThreads, 1)
+__global__ void __launch_bounds__(TbCfg<DH, KEYS>::THREADS, 1)
 attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __grid_constant__ CUtensorMap map_res1,
                           const __grid_constant__ CUtensorMap map_row2, const __grid_constant__ CUtensorMap map_row1, const AttnBackParams p,
                           unsigned int *status) {
@@ -172,14 +206,26 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(C::BAR_S + i), 1);
             mbar_init(bar(C::BAR_A + i), 1);
-            mbar_init(bar(C::BAR_AREAD + i), 8);
-            mbar_init(bar(C::BAR_P + i), 8);
+            mbar_init(bar(C::BAR_AREAD + i), C::WARPS);
+            mbar_init(bar(C::BAR_P + i), C::WARPS);
             mbar_init(bar(C::BAR_BACK + i), 1);
         }
         mbar_init(bar(C::BAR_ACC), 1);
-        mbar_init(bar(C::BAR_ACCREAD), 8);
+        mbar_init(bar(C::BAR_ACCREAD), C::WARPS);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        fence_proxy_async();
+    }
+    if constexpr (KEYS) {  // four first operands [128][16], ones where the parts of a value are and zeros elsewhere
+        for (int i = tid; i < 4 * kTbTile; i += C::THREADS) {
+            const int q = i / kTbTile, r = i % kTbTile;
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = (2 * e / 3 == q && 2 * e < 12 ? 0x3f80u : 0u) | ((2 * e + 1) / 3 == q && 2 * e + 1 < 12 ? 0x3f800000u : 0u);
+            uint4 *dst = reinterpret_cast<uint4 *>(smem + C::OFF_ONES + q * C::ONES_TILE) + 2 * r;
+            dst[(r >> 2) & 1] = make_uint4(w[0], w[1], w[2], w[3]);
+            dst[((r >> 2) & 1) ^ 1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
         fence_proxy_async();
     }
     if (warp == 1) {
@@ -221,13 +267,13 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                 if (lane == 0) {
                     const uint32_t full = bar(C::BAR_FULL + s), dst = sbase + C::OFF_RING + s * C::ROW_BYTES;
                     const int row = t.s0 + j * kTbStep;
-                    mbar_arrive_expect_tx(full, C::ROW_BYTES + (KEYS ? 1024 : 0));
+                    mbar_arrive_expect_tx(full, C::ROW_BYTES + (KEYS ? C::STAT_COPY : 0));
                     for (int blk = 0; blk < C::NBLK; ++blk) {
                         for (int a = 0; a < NS; ++a)
                             tma_load_3d(dst + a * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row2, ((t.st + a) * h + t.hd) * DH + 64 * blk, row, t.b, full);
                         tma_load_3d(dst + NS * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row1, t.hd * DH + 64 * blk, row, t.b, full);
                     }
-                    if constexpr (KEYS) bulk_load_1d(sbase + C::OFF_STATS + s * 1024, p.stats + (t.bh * n64 + row / kTbStep) * 256, 1024, full);
+                    if constexpr (KEYS) bulk_load_1d(sbase + C::OFF_STATS + s * C::STAT_STAGE, p.stats + (t.bh * n64 + row / kTbStep) * kTbStatBytes, C::STAT_COPY, full);
                 }
                 ++issued[s];
                 if (++s == C::ST) { s = 0; ph ^= 1u; }
@@ -251,6 +297,11 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                     warp_mma_f16(d, a + (uint64_t)(blk * (kTbTile * 128 >> 4) + 2 * kk), b + (uint64_t)(blk * (C::ROW_BLOCK >> 4) + 2 * kk), C::IDESC_F,
                                  (blk | kk) ? 1u : 0u);
         };
+        // (KEYS) minus a value of the step's queries from every row
+        const uint64_t ones_desc = make_sw32_desc(sbase + C::OFF_ONES), part_desc = make_sw32_desc(sbase + C::OFF_STATS);
+        auto subtract = [&](uint32_t d, int which, int stage) {
+            if constexpr (KEYS) warp_mma_f16(d, ones_desc + (uint64_t)(which * (C::ONES_TILE >> 4)), part_desc + (uint64_t)(stage * (C::STAT_STAGE >> 4)), C::IDESC_F, 1u);
+        };
         bool ok = true;
         int s = 0, rb = 0, g = 0;
         uint32_t ph = 0, rph = 0;
@@ -266,14 +317,17 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                 if (!(ok = wait(C::BAR_BACK + par, ((uint32_t)(g >> 1) & 1u) ^ 1u, 0xb14u))) break;
                 tc_fence_after();
 #pragma unroll
-                for (int a = 0; a < NS; ++a)
+                for (int a = 0; a < NS; ++a) {
                     product(tmem + C::COL_S + (par * NS + a) * kTbStep, res + (uint64_t)(a * (C::RES_TILE >> 4)), rows + (uint64_t)(a * (C::ROW_TILE >> 4)));
+                    subtract(tmem + C::COL_S + (par * NS + a) * kTbStep, t.st + a, s);
+                }
                 warp_commit(bar(C::BAR_S + par));
                 if constexpr (C::NA == 1) {
                     if (!(ok = wait(C::BAR_AREAD, ((uint32_t)g & 1u) ^ 1u, 0xb16u))) break;
                     tc_fence_after();
                 }
                 product(tmem + C::COL_A + ab * kTbStep, res + (uint64_t)(NS * (C::RES_TILE >> 4)), rows + (uint64_t)(NS * (C::ROW_TILE >> 4)));
+                subtract(tmem + C::COL_A + ab * kTbStep, 2 + t.st, s);
                 warp_commit(bar(C::BAR_A + ab));
                 if (++s == C::ST) { s = 0; ph ^= 1u; }
             }
@@ -284,10 +338,10 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
     } else if (warp == 2) {
         // ------------------------------------------------------------------ back products
         const uint64_t row_desc = make_sw128_mn_desc(sbase + C::OFF_RING, C::ROW_BLOCK);
-        auto product = [&](uint32_t d, uint32_t a, uint64_t b, bool first) {  // (a: sixteen columns of each half of the step)
+        auto product = [&](uint32_t d, uint32_t a, uint64_t b, bool first) {  // (a: a half of the columns of each part's scores)
 #pragma unroll
             for (int kk = 0; kk < kTbStep / 16; ++kk)
-                warp_mma_f16_ts(d, a + (kk >> 1) * 32 + (kk & 1) * 8, b + (uint64_t)(128 * kk), C::IDESC_B, (!first || kk) ? 1u : 0u);
+                warp_mma_f16_ts(d, a + kk * 16 / C::COLS * C::COLS + kk * 16 % C::COLS / 2, b + (uint64_t)(128 * kk), C::IDESC_B, (!first || kk) ? 1u : 0u);
         };
         bool ok = true;
         int s = 0, g = 0;
@@ -300,7 +354,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                 if (!(ok = wait(C::BAR_P + par, (uint32_t)(g >> 1) & 1u, 0xb22u))) break;
                 tc_fence_after();
                 const uint32_t col = tmem + C::COL_S + par * NS * kTbStep;
-                if constexpr (KEYS) product(tmem + C::COL_V, col + 16, rows + (uint64_t)(NS * (C::ROW_TILE >> 4)), j == 0 && (NS == 2 || t.st == 1));
+                if constexpr (KEYS) product(tmem + C::COL_V, col + C::COLS / 2, rows + (uint64_t)(NS * (C::ROW_TILE >> 4)), j == 0 && (NS == 2 || t.st == 1));
 #pragma unroll
                 for (int a = 0; a < NS; ++a)
                     product(tmem + C::COL_T + a * DH, col + a * kTbStep, rows + (uint64_t)(a * (C::ROW_TILE >> 4)), j == 0);
@@ -313,7 +367,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
         }
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ probabilities and their gradients
-        const int half = warp >= 8 ? 1 : 0, quarter = warp & 3, row = 32 * quarter + lane;
+        constexpr int COLS = C::COLS;
+        const int part = (warp - 4) >> 2, quarter = warp & 3, row = 32 * quarter + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
         const float c = p.scale_log2;
         const uint64_t c2 = pack_f32x2(c, c);
@@ -323,11 +378,12 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
         Item t;
         for (int k = 0; ok && item_of(k, t); ++k) {
             const int mine = t.r0 + row, w0 = t.r0 + 32 * quarter;  // the thread's key or query; the warp's first
-            uint64_t nl[2] = {}, nd[2] = {}, sum = 0;               // (queries) -lse and -D of the row, twice each
+            uint64_t nl[NS] = {}, nd[NS] = {}, sum = 0;             // (queries) -lse and -D of the row, twice each
             if constexpr (!KEYS) {
 #pragma unroll
                 for (int a = 0; a < NS; ++a) {
-                    const float *st = p.stats + (t.bh * n64 + mine / 64) * 256 + mine % 64 + 64 * (t.st + a);
+                    const float *st = reinterpret_cast<const float *>(p.stats + (t.bh * n64 + mine / 64) * kTbStatBytes + kTbTileBytes + kTbDeltaBytes) + mine % 64 +
+                                      64 * (t.st + a);
                     const float l = mine < L ? __ldg(st) : -INFINITY, d = mine < L ? __ldg(st + 128) : 0.0f;
                     nl[a] = pack_f32x2(l, l);
                     nd[a] = pack_f32x2(d, d);
@@ -337,39 +393,37 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
             const float wp = NS == 2 || t.st == 1 ? -p.lambda : 1.0f;
             const uint64_t wp2 = pack_f32x2(wp, wp);
             for (int j = 0; j < t.J; ++j, ++g) {
-                const int par = g & 1, ab = C::NA == 2 ? par : 0, c0 = t.s0 + j * kTbStep + 32 * half;  // the thread's first column
-                const uint32_t s_addr = lane_base + C::COL_S + par * NS * kTbStep + 32 * half;
-                const float *stats = reinterpret_cast<const float *>(smem + C::OFF_STATS + s * 1024) + 32 * half + 64 * t.st;
+                const int par = g & 1, ab = C::NA == 2 ? par : 0, c0 = t.s0 + j * kTbStep + COLS * part;  // the thread's first column
+                const uint32_t s_addr = lane_base + C::COL_S + par * NS * kTbStep + COLS * part;
+                const float *delta = reinterpret_cast<const float *>(smem + C::OFF_STATS + s * C::STAT_STAGE + kTbTileBytes) + COLS * part;
                 if (!(ok = wait(C::BAR_S + par, (uint32_t)(g >> 1) & 1u, 0xb30u))) break;
                 tc_fence_after();
-                uint32_t x[NS][32];
+                uint32_t x[NS][COLS];
 #pragma unroll
-                for (int a = 0; a < NS; ++a) tmem_ld32(s_addr + a * kTbStep, x[a]);
+                for (int a = 0; a < NS; ++a) tb_load(s_addr + a * kTbStep, x[a]);
                 tmem_ld_wait();
                 // some pair of the warp has its key behind its query
-                if (KEYS ? c0 < w0 + 31 : c0 + 31 > w0) {
+                if (KEYS ? c0 < w0 + 31 : c0 + COLS - 1 > w0) {
 #pragma unroll
                     for (int a = 0; a < NS; ++a)
 #pragma unroll
-                        for (int u = 0; u < 32; ++u)
+                        for (int u = 0; u < COLS; ++u)
                             if (KEYS ? c0 + u < mine : c0 + u > mine) x[a][u] = 0xff800000u;  // -inf: probability 0
                 }
 #pragma unroll
                 for (int a = 0; a < NS; ++a)
 #pragma unroll
-                    for (int u = 0; u < 32; u += 4) {
-                        ulonglong2 n = make_ulonglong2(nl[a], nl[a]);
-                        if constexpr (KEYS) n = *reinterpret_cast<const ulonglong2 *>(stats + 64 * a + u);
-                        float y[4];
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[a][u]), __uint_as_float(x[a][u + 1])), c2, n.x), y[0], y[1]);
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[a][u + 2]), __uint_as_float(x[a][u + 3])), c2, n.y), y[2], y[3]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[a][u + e] = __float_as_uint(tb_ex2(y[e]));
+                    for (int u = 0; u < COLS; u += 2) {
+                        const uint64_t v = pack_f32x2(__uint_as_float(x[a][u]), __uint_as_float(x[a][u + 1]));
+                        float y0, y1;
+                        unpack_f32x2(KEYS ? mul_f32x2(v, c2) : fma_f32x2(v, c2, nl[a]), y0, y1);
+                        x[a][u] = __float_as_uint(tb_ex2(y0));
+                        x[a][u + 1] = __float_as_uint(tb_ex2(y1));
                     }
                 if (!(ok = wait(C::BAR_A + ab, C::NA == 2 ? (uint32_t)(g >> 1) & 1u : (uint32_t)g & 1u, 0xb32u))) break;
                 tc_fence_after();
-                uint32_t dp[32];
-                tmem_ld32(lane_base + C::COL_A + ab * kTbStep + 32 * half, dp);
+                uint32_t dp[COLS];
+                tb_load(lane_base + C::COL_A + ab * kTbStep + COLS * part, dp);
                 tmem_ld_wait();
                 if constexpr (C::NA == 1) {
                     tc_fence_before();
@@ -379,25 +433,34 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                 auto two = [](const uint32_t *v) { return pack_f32x2(__uint_as_float(v[0]), __uint_as_float(v[1])); };
                 // P and T are rounded to bf16 for the products (2^-9 each, fp32 sums), as the forward pass rounds P
                 if constexpr (KEYS) {
-                    uint32_t o[16];
+                    uint32_t o[COLS / 2];
 #pragma unroll
-                    for (int u = 0; u < 32; u += 2)
+                    for (int u = 0; u < COLS; u += 2)
                         o[u >> 1] = tb_pack_bf16(NS == 2 ? fma_f32x2(two(&x[NS - 1][u]), wp2, two(&x[0][u])) : mul_f32x2(two(&x[0][u]), wp2));
-                    tmem_st16(s_addr + 16, o);
+                    tb_store(s_addr + COLS / 2, o);
                 }
 #pragma unroll
                 for (int a = 0; a < NS; ++a) {
-                    uint32_t o[16];
+                    uint32_t o[COLS / 2];
 #pragma unroll
-                    for (int u = 0; u < 32; u += 4) {
-                        ulonglong2 n = make_ulonglong2(nd[a], nd[a]);
-                        if constexpr (KEYS) n = *reinterpret_cast<const ulonglong2 *>(stats + 128 + 64 * a + u);
-                        const uint64_t t0 = mul_f32x2(two(&x[a][u]), add_f32x2(two(&dp[u]), n.x)), t1 = mul_f32x2(two(&x[a][u + 2]), add_f32x2(two(&dp[u + 2]), n.y));
+                    for (int u = 0; u < COLS; u += 4) {
+                        uint64_t d0 = two(&dp[u]), d1 = two(&dp[u + 2]);
+                        if constexpr (KEYS) {  // (D_1 is subtracted, or with one stream its own)
+                            if (a == 1) {
+                                const ulonglong2 n = *reinterpret_cast<const ulonglong2 *>(delta + u);
+                                d0 = add_f32x2(d0, n.x);
+                                d1 = add_f32x2(d1, n.y);
+                            }
+                        } else {
+                            d0 = add_f32x2(d0, nd[a]);
+                            d1 = add_f32x2(d1, nd[a]);
+                        }
+                        const uint64_t t0 = mul_f32x2(two(&x[a][u]), d0), t1 = mul_f32x2(two(&x[a][u + 2]), d1);
                         o[u >> 1] = tb_pack_bf16(t0);
                         o[(u >> 1) + 1] = tb_pack_bf16(t1);
                         if (!KEYS && a == NS - 1) sum = add_f32x2(add_f32x2(t0, t1), sum);  // (of the second stream, or of the one at hand)
                     }
-                    tmem_st16(s_addr + a * kTbStep, o);
+                    tb_store(s_addr + a * kTbStep, o);
                 }
                 tmem_st_wait();
                 tc_fence_before();
@@ -412,27 +475,25 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                     float a, b, d, unused;
                     unpack_f32x2(sum, a, b);
                     unpack_f32x2(nd[NS - 1], d, unused);
-                    dl += (double)a + (double)b - (half ? 0.0 : (double)d);
+                    dl += (double)a + (double)b - (part ? 0.0 : (double)d);
                 }
             }
-            // ---- outputs: this warp's rows, half of each accumulator's columns
+            // ---- outputs: this warp's rows, its part of each accumulator's columns
             if (!(ok = wait(C::BAR_ACC, (uint32_t)k & 1u, 0xb40u))) break;
             tc_fence_after();
             const size_t tok = (size_t)t.b * L + mine, width = (size_t)h * DH;
             auto put = [&](uint32_t col, float f, __nv_bfloat16 *dst) {
+                constexpr int N = DH / C::PARTS;
+                uint32_t v[N];
+                tb_load(lane_base + col + part * N, v);
+                tmem_ld_wait();
+                if (mine < L) {
 #pragma unroll
-                for (int cc = 0; cc < DH / 2; cc += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(lane_base + col + half * (DH / 2) + cc, v);
-                    tmem_ld_wait();
-                    if (mine < L) {
+                    for (int u = 0; u < N; u += 8) {
+                        uint32_t o[4];
 #pragma unroll
-                        for (int u = 0; u < 32; u += 8) {
-                            uint32_t o[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[e] = tb_pack_bf16(__uint_as_float(v[u + 2 * e]) * f, __uint_as_float(v[u + 2 * e + 1]) * f);
-                            *reinterpret_cast<uint4 *>(dst + half * (DH / 2) + cc + u) = make_uint4(o[0], o[1], o[2], o[3]);
-                        }
+                        for (int e = 0; e < 4; ++e) o[e] = tb_pack_bf16(__uint_as_float(v[u + 2 * e]) * f, __uint_as_float(v[u + 2 * e + 1]) * f);
+                        *reinterpret_cast<uint4 *>(dst + part * N + u) = make_uint4(o[0], o[1], o[2], o[3]);
                     }
                 }
             };
@@ -449,7 +510,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
         if constexpr (!KEYS) {
 #pragma unroll
             for (int o = 16; o; o >>= 1) dl += __shfl_xor_sync(0xffffffffu, dl, o);
-            if (lane == 0) p.dl_part[(size_t)blockIdx.x * 8 + warp - 4] = dl;
+            if (lane == 0) p.dl_part[(size_t)blockIdx.x * C::WARPS + warp - 4] = dl;
         }
     }
     tc_fence_before();
@@ -493,13 +554,13 @@ static cudaError_t launch_backward_pass(const AttnBackParams &p, const void *res
     if (!make_map_tokens(&m[0], res2, 2 * w, p.L, p.B, kTbTile) || !make_map_tokens(&m[1], res1, w, p.L, p.B, kTbTile) ||
         !make_map_tokens(&m[2], row2, 2 * w, p.L, p.B, kTbStep) || !make_map_tokens(&m[3], row1, w, p.L, p.B, kTbStep))
         return cudaErrorInvalidValue;
-    attention_backward_kernel<DH, KEYS><<<grid, kTbThreads, C::SMEM_BYTES, stream>>>(m[0], m[1], m[2], m[3], p, status);
+    attention_backward_kernel<DH, KEYS><<<grid, C::THREADS, C::SMEM_BYTES, stream>>>(m[0], m[1], m[2], m[3], p, status);
     count_launch();
     return cudaGetLastError();
 }
 
 constexpr int kTbMaxGrid = 1024;
-static size_t stats_bytes(int64_t B, int64_t L, int64_t h) { return (size_t)(B * h) * (size_t)((L + 63) / 64) * 1024; }
+static size_t stats_bytes(int64_t B, int64_t L, int64_t h) { return (size_t)(B * h) * (size_t)((L + 63) / 64) * kTbStatBytes; }
 
 template <int DH>
 static cudaError_t launch_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
@@ -508,11 +569,11 @@ static cudaError_t launch_backward(const void *q, const void *k, const void *v, 
     if (!sms) return cudaErrorInvalidDevice;
     const long long bhs = (long long)p.B * p.h, blocks = bhs * ((p.L + 63) / 64), tiles = bhs * ((p.L + kTbTile - 1) / kTbTile);
     const int most = sms < kTbMaxGrid ? sms : kTbMaxGrid, grid = tiles < most ? (int)tiles : most;
-    float *stats = (float *)workspace;
+    uint8_t *stats = (uint8_t *)workspace;
     p.stats = stats;
     p.dl_part = (double *)((char *)workspace + stats_bytes(p.B, p.L, p.h));
     attention_stats_kernel<DH><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream>>>(
-        (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)streams, lse, stats, p.B, p.L, p.h);
+        (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)streams, lse, stats, p.B, p.L, p.h, p.scale_log2);
     count_launch();
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess && (grads.dk || grads.dv)) {
@@ -526,7 +587,7 @@ static cudaError_t launch_backward(const void *q, const void *k, const void *v, 
         e = launch_backward_pass<DH, false>(p, q, dout, k, v, grid, stream);
     }
     if (e == cudaSuccess && grads.dlambda) {
-        attention_dlambda_kernel<<<1, 32, 0, stream>>>(p.dl_part, grid * 8, p.out_scale, grads.dlambda);
+        attention_dlambda_kernel<<<1, 32, 0, stream>>>(p.dl_part, grid * TbCfg<DH, false>::WARPS, p.out_scale, grads.dlambda);
         count_launch();
         e = cudaGetLastError();
     }
@@ -544,7 +605,7 @@ static bool backward_sizes_ok(int64_t B, int64_t L, int32_t n_heads, int32_t hea
 
 extern "C" size_t hgf_diff_attention_backward_workspace_bytes(int64_t B, int64_t L, int32_t n_heads, int32_t head_dim) {
     if (B <= 0 || L <= 0 || n_heads <= 0 || !backward_sizes_ok(B, L, n_heads, head_dim)) return 0;
-    return stats_bytes(B, L, n_heads) + (size_t)kTbMaxGrid * 8 * sizeof(double);
+    return stats_bytes(B, L, n_heads) + (size_t)kTbMaxGrid * 16 * sizeof(double);
 }
 
 extern "C" hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
