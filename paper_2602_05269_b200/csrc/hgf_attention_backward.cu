@@ -6,17 +6,17 @@
 #include <cmath>
 
 #include "hgf_tc.cuh"
+#include "hgf_warp.cuh"
 
 namespace hgf {
 
 struct AttnBackParams {
-    __nv_bfloat16 *d2, *d1;          // gradients of the two-stream tensor (dK or dQ) and, for keys, of V; d1 null for queries
     const uint8_t *stats;            // [B*h][ceil(L / 64)] blocks of kTbStatBytes, see attention_stats_kernel
-    double *dl_part;                 // (queries) [grid][warps] partial sums of P_2 (.) A
-    const double *dl_in;             // (keys) the same, of the launch before; null: none
-    float *dlambda;
-    int dl_n;
+    double *dl_part;                 // [grid][warps] partial sums of P_2 (.) A
+    unsigned int *arrivals;          // CTAs that have left theirs
+    float *dlambda;                  // null: not asked for
     int B, L, h;
+    int keys, queries, both;         // which passes run
     float lambda, out_scale, scale, scale_log2;  // scale = 1 / sqrt(dh), scale_log2 = log2(e) / sqrt(dh)
 };
 
@@ -55,11 +55,15 @@ constexpr int kTbTileBytes = 2048, kTbDeltaBytes = 256, kTbStatBytes = kTbTileBy
 // A thread block takes 64 tokens: a row of G, O_1 and O_2 is read by head_dim / 8 lanes, 16 bytes each.
 template <int DH>
 __global__ void __launch_bounds__(256)
-attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, const float *lse, uint8_t *stats, int B, int L, int h, float scale_log2) {
+attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, const float *lse, uint8_t *stats, unsigned int *arrivals, int B, int L, int h,
+                       float scale_log2) {
     constexpr int LPR = DH / 8, RPW = 32 / LPR;
     __shared__ float s_v[4][64];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = (L + 63) / 64;
     const long long tiles = (long long)B * h * blocks;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *arrivals = 0;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const long long bh = tile / blocks;
         const int i0 = (int)(tile % blocks) * 64, hd = (int)(bh % h);
@@ -119,79 +123,101 @@ attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, 
 }
 
 // ---- the gradients ----------------------------------------------------------------------------------------------------
-// One skeleton for both sides.  KEYS: a tile is 128 keys, lane = key, in steps of 64 queries from the tile's first on (dK, dV).
+// One skeleton for both passes.  KEYS: a tile is 128 keys, lane = key, in steps of 64 queries from the tile's first on (dK, dV).
 // Otherwise a tile is 128 queries, lane = query, in steps of 64 keys up to the tile's last (dQ).  Two passes form the scores twice,
 // 11 products instead of 8, but every sum has one owner and one order: no atomics, no fp32 copy of dQ.
-//   warp 0      TMA producer: the tile's resident operands (K_s and V, or Q_s and G), then a step's streamed ones
-//   warp 1      front products: the scores of a step and A, [128 x 64] fp32 in tensor memory
+//   warp 0      TMA producer: a step's streamed rows, and a tile's resident ones that stay in shared memory
+//   warp 1      front products: the scores of a step, then A, [128 x 64] fp32 in tensor memory
 //   warp 2      back products: the accumulators += T_s (or P) times the step's rows; the first operand is bf16 in tensor
-//               memory, written over the scores that it came from; the second the streamed tile in its stored form
-//   warps 4-19  a thread owns a lane and a quarter of the step's columns
+//               memory, the second the streamed tile in its stored form
+//   warps 4-19  a thread owns a lane and a quarter of the step's columns; they also bring resident rows into tensor memory
 // NS streams are in flight at a time: two for head_dim 64; for head_dim 128 the accumulators take too many columns, so the
 // streams are items of their own, one after the other (with dV kept over both).
-constexpr int kTbTile = 128, kTbStep = 64;
+// What bounds it: a product of 64 columns whose first operand lies in shared memory reads 6 KB for 32 clocks of arithmetic, at 128 bytes
+// a clock 48 of them, so as many resident operands as fit are kept in tensor memory (TRES); then the exponentials (1024 clocks a step of
+// both streams) and the power limit.
+constexpr int kTbTile = 128, kTbStep = 64, kTbBarBytes = 512;
 
 template <int DH, bool KEYS>
 struct TbCfg {
     static constexpr int NS = DH == 64 ? 2 : 1;
     static constexpr int PARTS = 4, COLS = kTbStep / PARTS, WARPS = 4 * PARTS, THREADS = 128 + 32 * WARPS;  // a thread's columns of a step, warps of them
     static constexpr int NBLK = DH / 64;
-    static constexpr int NRES = DH == 64 ? 2 : 1;   // buffers of the resident operands
-    static constexpr int ST = DH == 64 && !KEYS ? 5 : 4;  // ring stages
-    static constexpr int RES_TILE = NBLK * kTbTile * 128, RES_BYTES = (NS + 1) * RES_TILE;
+    // T (and P) are written over A, whose two buffers the back products then hold; the scores' buffers are free once they are read.
+    // With two streams and P there are three such operands, which do not fit: they lie over the scores, two buffers each, and A has one.
+    static constexpr bool OVER_A = DH == 128 || !KEYS;
+    static constexpr int TRES = KEYS ? (DH == 128 ? 1 : 0) : NS + 1, SRES = NS + 1 - TRES;  // resident operands in tensor and in shared memory
+    static constexpr int NSB = OVER_A && (DH == 64 || KEYS) ? 1 : 2, NA = OVER_A ? 2 : 1;   // buffers of the scores and of A
+    static constexpr int NRES = 2;                                                          // of the resident operands in shared memory
+    static constexpr int ST = KEYS ? 4 : (DH == 64 ? 8 : 6);                                // ring stages
+    static constexpr int RES_TILE = NBLK * kTbTile * 128, RES_BYTES = SRES * RES_TILE;
     static constexpr int ROW_BLOCK = kTbStep * 128, ROW_TILE = NBLK * ROW_BLOCK, ROW_BYTES = (NS + 1) * ROW_TILE;
     static constexpr int STAT_COPY = kTbTileBytes + (NS == 2 ? kTbDeltaBytes : 0), STAT_STAGE = kTbTileBytes + 512, ONES_TILE = kTbTile * 32;
-    static constexpr int OFF_RING = NRES * RES_BYTES, OFF_STATS = OFF_RING + ST * ROW_BYTES, OFF_ONES = OFF_STATS + (KEYS ? ST * STAT_STAGE : 0), OFF_BAR = OFF_ONES + (KEYS ? 4 * ONES_TILE : 0);
+    static constexpr int OFF_RES = 2 * kTbBarBytes, OFF_RING = OFF_RES + (SRES ? NRES * RES_BYTES : 0), OFF_STATS = OFF_RING + ST * ROW_BYTES,
+                         OFF_ONES = OFF_STATS + (KEYS ? ST * STAT_STAGE : 0), SMEM_BYTES = OFF_ONES + (KEYS ? 4 * ONES_TILE : 0) + 1024;
     static constexpr int BAR_RESFULL = 0, BAR_RESEMPTY = BAR_RESFULL + NRES, BAR_FULL = BAR_RESEMPTY + NRES, BAR_EMPTY = BAR_FULL + ST,
-                         BAR_S = BAR_EMPTY + ST,       // [parity of the step] scores are there
+                         BAR_RT = BAR_EMPTY + ST,      // resident rows are in tensor memory
+                         BAR_S = BAR_RT + 1,           // scores are there
                          BAR_A = BAR_S + 2,            // A is there
-                         BAR_AREAD = BAR_A + 2,        // A has been read
-                         BAR_P = BAR_AREAD + 2,        // first operands of the back products are there
+                         BAR_READ = BAR_A + 2,         // scores (OVER_A) or A (otherwise) have been read
+                         BAR_P = BAR_READ + 2,         // first operands of the back products are there
                          BAR_BACK = BAR_P + 2,         // back products are complete
                          BAR_ACC = BAR_BACK + 2,       // all products of an item
                          BAR_ACCREAD = BAR_ACC + 1, BAR_COUNT = BAR_ACCREAD + 1;
-    static constexpr int SMEM_BYTES = OFF_BAR + 512 + 1024;
-    // tensor-memory columns: accumulators (dV, then dK_s or dQ_s), score buffers [parity][stream], A buffers
-    static constexpr int NA = DH == 64 && KEYS ? 1 : 2;
-    static constexpr int COL_V = 0, COL_T = KEYS ? DH : 0, COL_S = COL_T + NS * DH, COL_A = COL_S + 2 * NS * kTbStep;
+    // tensor-memory columns: accumulators (dV, then dK_s or dQ_s), score buffers [buffer][stream], A buffers, resident rows
+    static constexpr int COL_V = 0, COL_T = KEYS ? DH : 0, COL_S = COL_T + NS * DH, COL_A = COL_S + NSB * NS * kTbStep, COL_R = COL_A + NA * kTbStep;
     static constexpr uint32_t IDESC_F = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTbStep >> 3) << 17) | ((uint32_t)(kTbTile >> 4) << 24);
     static constexpr uint32_t IDESC_B = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kTbTile >> 4) << 24);
-    static_assert(BAR_COUNT * 8 + 16 <= 512, "barrier block");
-    static_assert(COL_A + NA * kTbStep <= 512 && SMEM_BYTES <= 227 * 1024, "tensor and shared memory");
+    static_assert(BAR_COUNT * 8 <= kTbBarBytes - 16, "barrier block");
+    static_assert(COL_R + TRES * (DH / 2) <= 512 && SMEM_BYTES <= 227 * 1024, "tensor and shared memory");
+};
+
+// What a pass reads and writes: res2, res1 the resident tensors of both streams and of one, row2, row1 the streamed ones.
+struct TbPass {
+    const __nv_bfloat16 *res2, *res1;
+    __nv_bfloat16 *d2, *d1;          // gradients of the two-stream tensor (dK or dQ) and, for keys, of V
 };
 
 template <int DH, bool KEYS>
-__global__ void __launch_bounds__(TbCfg<DH, KEYS>::THREADS, 1)
-attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __grid_constant__ CUtensorMap map_res1,
-                          const __grid_constant__ CUtensorMap map_row2, const __grid_constant__ CUtensorMap map_row1, const AttnBackParams p,
-                          unsigned int *status) {
+__device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map_res2, const CUtensorMap &map_res1, const CUtensorMap &map_row2, const CUtensorMap &map_row1,
+                                                          const TbPass &pass, const AttnBackParams &p, uint8_t *smem, uint32_t tmem, volatile int *abort_flag,
+                                                          unsigned int *status) {
     using C = TbCfg<DH, KEYS>;
     constexpr int NS = C::NS;
-    extern __shared__ uint8_t tb_smem_raw[];
-    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)tb_smem_raw + 1023) & ~(uintptr_t)1023);
-    const uint32_t sbase = smem_u32(smem), bar0 = sbase + C::OFF_BAR;
+    const uint32_t sbase = smem_u32(smem), bar0 = sbase + (KEYS ? 0 : kTbBarBytes);
     auto bar = [&](int i) { return bar0 + 8u * i; };
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::OFF_BAR + C::BAR_COUNT * 8);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::OFF_BAR + C::BAR_COUNT * 8 + 4);
-
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    const int L = p.L, h = p.h, nt = (L + kTbTile - 1) / kTbTile, n64 = (L + kTbStep - 1) / kTbStep, G = (int)gridDim.x;
-    const long long bhs = (long long)p.B * h, tiles = nt * bhs;
-    // The CTA's k-th item; tiles in order of falling length are dealt in rounds, every other round backwards.
-    struct Item { int r0, s0, J, b, hd, st; long long bh; };
-    auto item_of = [&](int k, Item &t) {
-        const int kt = NS == 2 ? k : k >> 1;
-        const long long i = (long long)kt * G + ((kt & 1) ? G - 1 - (int)blockIdx.x : (int)blockIdx.x);
-        if (i >= tiles) return false;
-        const int rank = (int)(i / bhs), tile = KEYS ? rank : nt - 1 - rank;
-        t.bh = i % bhs;
-        t.r0 = tile * kTbTile;
-        t.s0 = KEYS ? t.r0 : 0;
-        t.J = KEYS ? n64 - t.r0 / kTbStep : min(n64, t.r0 / kTbStep + 2);
-        t.b = (int)(t.bh / h);
-        t.hd = (int)(t.bh % h);
-        t.st = NS == 2 ? 0 : 1 - (k & 1);  // (one stream at a time: the second first)
-        return true;
+    const int L = p.L, h = p.h, nt = (L + kTbTile - 1) / kTbTile, n64 = (L + kTbStep - 1) / kTbStep, G = (int)gridDim.x, bhs = p.B * h;
+    const long long per_rank = (p.both ? 2ll : 1ll) * bhs, tiles = nt * per_rank;
+    // The tiles of both passes in order of falling length are dealt to the CTAs in rounds, every other round backwards; a CTA works those of the
+    // keys first.  (Tiles of the keys, then those of the queries in rounds of their own: 5 to 40 % more steps in the longest CTA for batches of
+    // a few hundred tiles.)
+    struct Item { int r0, s0, J, b, hd, st, bh; };
+    struct Cursor { int round; bool second; };
+    auto next = [&](Cursor &c, Item &t) {
+        if (NS == 1 && c.second) {  // (one stream at a time: the second first)
+            c.second = false;
+            t.st = 0;
+            return true;
+        }
+        for (;; ++c.round) {
+            const long long i = (long long)c.round * G + ((c.round & 1) ? G - 1 - (int)blockIdx.x : (int)blockIdx.x);
+            if (i >= tiles) return false;
+            const int rank = (int)(i / per_rank);
+            const long long of = i % per_rank;
+            if (p.both && (of < bhs) != KEYS) continue;
+            const int tile = KEYS ? rank : nt - 1 - rank;
+            t.bh = (int)(of % bhs);
+            t.r0 = tile * kTbTile;
+            t.s0 = KEYS ? t.r0 : 0;
+            t.J = KEYS ? n64 - t.r0 / kTbStep : min(n64, t.r0 / kTbStep + 2);
+            t.b = t.bh / h;
+            t.hd = t.bh % h;
+            t.st = NS == 2 ? 0 : 1;
+            c.second = NS == 1;
+            ++c.round;
+            return true;
+        }
     };
 
     if (tid == 0) {
@@ -206,15 +232,14 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(C::BAR_S + i), 1);
             mbar_init(bar(C::BAR_A + i), 1);
-            mbar_init(bar(C::BAR_AREAD + i), C::WARPS);
+            mbar_init(bar(C::BAR_READ + i), C::WARPS);
             mbar_init(bar(C::BAR_P + i), C::WARPS);
             mbar_init(bar(C::BAR_BACK + i), 1);
         }
+        mbar_init(bar(C::BAR_RT), C::WARPS);
         mbar_init(bar(C::BAR_ACC), 1);
         mbar_init(bar(C::BAR_ACCREAD), C::WARPS);
-        *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
-        fence_proxy_async();
     }
     if constexpr (KEYS) {  // four first operands [128][16], ones where the parts of a value are and zeros elsewhere
         for (int i = tid; i < 4 * kTbTile; i += C::THREADS) {
@@ -226,41 +251,39 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
             dst[(r >> 2) & 1] = make_uint4(w[0], w[1], w[2], w[3]);
             dst[((r >> 2) & 1) ^ 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
-        fence_proxy_async();
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
-    }
-    tc_fence_before();
+    fence_proxy_async();
     __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     auto wait = [&](int i, uint32_t par, unsigned int code) {
         return __all_sync(0xffffffffu, mbar_wait_poll(bar(i), par, abort_flag, status, code)) != 0;
     };
+    auto phase = [](int g, int buffers) { return (uint32_t)(buffers == 2 ? g >> 1 : g) & 1u; };
+    double dl = 0.0;
 
+    Cursor c = {0, false};
+    Item t;
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
         uint32_t issued[C::ST] = {}, res_issued[C::NRES] = {};
         int s = 0, rb = 0;
         uint32_t ph = 1, rph = 1;
         bool ok = true;
-        Item t;
-        for (int k = 0; ok && item_of(k, t); ++k) {
-            ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_RESEMPTY + rb), rph, abort_flag, status, 0xb00u + rb)) != 0;
-            if (!ok) break;
-            if (lane == 0) {
-                const uint32_t full = bar(C::BAR_RESFULL + rb), dst = sbase + rb * C::RES_BYTES;
-                mbar_arrive_expect_tx(full, C::RES_BYTES);
-                for (int blk = 0; blk < C::NBLK; ++blk) {
-                    for (int a = 0; a < NS; ++a)
-                        tma_load_3d(dst + a * C::RES_TILE + blk * kTbTile * 128, &map_res2, ((t.st + a) * h + t.hd) * DH + 64 * blk, t.r0, t.b, full);
-                    tma_load_3d(dst + NS * C::RES_TILE + blk * kTbTile * 128, &map_res1, t.hd * DH + 64 * blk, t.r0, t.b, full);
+        while (ok && next(c, t)) {
+            if constexpr (C::SRES > 0) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_RESEMPTY + rb), rph, abort_flag, status, 0xb00u + rb)) != 0;
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t full = bar(C::BAR_RESFULL + rb), dst = sbase + C::OFF_RES + rb * C::RES_BYTES;
+                    mbar_arrive_expect_tx(full, C::RES_BYTES);
+                    for (int blk = 0; blk < C::NBLK; ++blk) {
+                        for (int a = 0; a + 1 < C::SRES; ++a)
+                            tma_load_3d(dst + a * C::RES_TILE + blk * kTbTile * 128, &map_res2, ((t.st + a) * h + t.hd) * DH + 64 * blk, t.r0, t.b, full);
+                        tma_load_3d(dst + (C::SRES - 1) * C::RES_TILE + blk * kTbTile * 128, &map_res1, t.hd * DH + 64 * blk, t.r0, t.b, full);
+                    }
                 }
+                ++res_issued[rb];
+                if (++rb == C::NRES) { rb = 0; rph ^= 1u; }
             }
-            ++res_issued[rb];
-            if (++rb == C::NRES) { rb = 0; rph ^= 1u; }
             for (int j = 0; j < t.J; ++j) {
                 ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_EMPTY + s), ph, abort_flag, status, 0xb08u + s)) != 0;
                 if (!ok) break;
@@ -273,7 +296,8 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                             tma_load_3d(dst + a * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row2, ((t.st + a) * h + t.hd) * DH + 64 * blk, row, t.b, full);
                         tma_load_3d(dst + NS * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row1, t.hd * DH + 64 * blk, row, t.b, full);
                     }
-                    if constexpr (KEYS) bulk_load_1d(sbase + C::OFF_STATS + s * C::STAT_STAGE, p.stats + (t.bh * n64 + row / kTbStep) * kTbStatBytes, C::STAT_COPY, full);
+                    if constexpr (KEYS)
+                        bulk_load_1d(sbase + C::OFF_STATS + s * C::STAT_STAGE, p.stats + ((size_t)t.bh * n64 + row / kTbStep) * kTbStatBytes, C::STAT_COPY, full);
                 }
                 ++issued[s];
                 if (++s == C::ST) { s = 0; ph ^= 1u; }
@@ -288,76 +312,87 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                 for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(bar(C::BAR_RESFULL + q), (res_issued[q] - 1u) & 1u); ++i) {}
     } else if (warp == 1) {
         // ------------------------------------------------------------------ front products
-        const uint64_t res_desc = make_sw128_desc(sbase), row_desc = make_sw128_desc(sbase + C::OFF_RING);
-        auto product = [&](uint32_t d, uint64_t a, uint64_t b) {
+        const uint64_t res_desc = make_sw128_desc(sbase + C::OFF_RES), row_desc = make_sw128_desc(sbase + C::OFF_RING);
+        // resident operand `which` (of the streams, then the single one) times its streamed tile
+        auto product = [&](uint32_t d, int which, int rb, int s) {
+            const uint64_t b = row_desc + (uint64_t)(s * (C::ROW_BYTES >> 4) + which * (C::ROW_TILE >> 4));
+            const uint64_t a = res_desc + (uint64_t)(rb * (C::RES_BYTES >> 4) + (which - C::TRES) * (C::RES_TILE >> 4));
 #pragma unroll
             for (int blk = 0; blk < C::NBLK; ++blk)
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    warp_mma_f16(d, a + (uint64_t)(blk * (kTbTile * 128 >> 4) + 2 * kk), b + (uint64_t)(blk * (C::ROW_BLOCK >> 4) + 2 * kk), C::IDESC_F,
-                                 (blk | kk) ? 1u : 0u);
+                for (int kk = 0; kk < 4; ++kk) {
+                    const uint64_t rows = b + (uint64_t)(blk * (C::ROW_BLOCK >> 4) + 2 * kk);
+                    if (which < C::TRES) warp_mma_f16_ts(d, tmem + C::COL_R + which * (DH / 2) + 32 * blk + 8 * kk, rows, C::IDESC_F, (blk | kk) ? 1u : 0u);
+                    else warp_mma_f16(d, a + (uint64_t)(blk * (kTbTile * 128 >> 4) + 2 * kk), rows, C::IDESC_F, (blk | kk) ? 1u : 0u);
+                }
         };
         // (KEYS) minus a value of the step's queries from every row
         const uint64_t ones_desc = make_sw32_desc(sbase + C::OFF_ONES), part_desc = make_sw32_desc(sbase + C::OFF_STATS);
-        auto subtract = [&](uint32_t d, int which, int stage) {
-            if constexpr (KEYS) warp_mma_f16(d, ones_desc + (uint64_t)(which * (C::ONES_TILE >> 4)), part_desc + (uint64_t)(stage * (C::STAT_STAGE >> 4)), C::IDESC_F, 1u);
+        auto subtract = [&](uint32_t d, int which, int s) {
+            if constexpr (KEYS) warp_mma_f16(d, ones_desc + (uint64_t)(which * (C::ONES_TILE >> 4)), part_desc + (uint64_t)(s * (C::STAT_STAGE >> 4)), C::IDESC_F, 1u);
         };
         bool ok = true;
         int s = 0, rb = 0, g = 0;
-        uint32_t ph = 0, rph = 0;
-        Item t;
-        for (int k = 0; ok && item_of(k, t); ++k) {
-            if (!(ok = wait(C::BAR_RESFULL + rb, rph, 0xb10u))) break;
-            const uint64_t res = res_desc + (uint64_t)(rb * (C::RES_BYTES >> 4));
+        uint32_t ph = 0, rph = 0, tph = 0;
+        while (ok && next(c, t)) {
+            if constexpr (C::SRES > 0)
+                if (!(ok = wait(C::BAR_RESFULL + rb, rph, 0xb10u))) break;
+            if constexpr (C::TRES > 0) {
+                if (!(ok = wait(C::BAR_RT, tph, 0xb11u))) break;
+                tph ^= 1u;
+            }
             for (int j = 0; j < t.J; ++j, ++g) {
-                const int par = g & 1, ab = C::NA == 2 ? par : 0;
-                const uint64_t rows = row_desc + (uint64_t)(s * (C::ROW_BYTES >> 4));
+                const int par = g & 1, sb = C::NSB == 2 ? par : 0, ab = C::NA == 2 ? par : 0;
                 if (!(ok = wait(C::BAR_FULL + s, ph, 0xb12u))) break;
-                // the buffers are free when the back products of two steps before are complete
-                if (!(ok = wait(C::BAR_BACK + par, ((uint32_t)(g >> 1) & 1u) ^ 1u, 0xb14u))) break;
+                if (C::OVER_A) ok = wait(C::BAR_READ + sb, phase(g, C::NSB) ^ 1u, 0xb13u);
+                else ok = wait(C::BAR_BACK + par, phase(g, 2) ^ 1u, 0xb14u);
+                if (!ok) break;
                 tc_fence_after();
 #pragma unroll
                 for (int a = 0; a < NS; ++a) {
-                    product(tmem + C::COL_S + (par * NS + a) * kTbStep, res + (uint64_t)(a * (C::RES_TILE >> 4)), rows + (uint64_t)(a * (C::ROW_TILE >> 4)));
-                    subtract(tmem + C::COL_S + (par * NS + a) * kTbStep, t.st + a, s);
+                    product(tmem + C::COL_S + (sb * NS + a) * kTbStep, a, rb, s);
+                    subtract(tmem + C::COL_S + (sb * NS + a) * kTbStep, t.st + a, s);
                 }
-                warp_commit(bar(C::BAR_S + par));
-                if constexpr (C::NA == 1) {
-                    if (!(ok = wait(C::BAR_AREAD, ((uint32_t)g & 1u) ^ 1u, 0xb16u))) break;
-                    tc_fence_after();
-                }
-                product(tmem + C::COL_A + ab * kTbStep, res + (uint64_t)(NS * (C::RES_TILE >> 4)), rows + (uint64_t)(NS * (C::ROW_TILE >> 4)));
+                warp_commit(bar(C::BAR_S + sb));
+                if (C::OVER_A) ok = wait(C::BAR_BACK + par, phase(g, 2) ^ 1u, 0xb15u);
+                else ok = wait(C::BAR_READ, phase(g, 1) ^ 1u, 0xb16u);
+                if (!ok) break;
+                tc_fence_after();
+                product(tmem + C::COL_A + ab * kTbStep, NS, rb, s);
                 subtract(tmem + C::COL_A + ab * kTbStep, 2 + t.st, s);
                 warp_commit(bar(C::BAR_A + ab));
                 if (++s == C::ST) { s = 0; ph ^= 1u; }
             }
             if (!ok) break;
-            warp_commit(bar(C::BAR_RESEMPTY + rb));
-            if (++rb == C::NRES) { rb = 0; rph ^= 1u; }
+            if constexpr (C::SRES > 0) {
+                warp_commit(bar(C::BAR_RESEMPTY + rb));
+                if (++rb == C::NRES) { rb = 0; rph ^= 1u; }
+            }
         }
     } else if (warp == 2) {
         // ------------------------------------------------------------------ back products
         const uint64_t row_desc = make_sw128_mn_desc(sbase + C::OFF_RING, C::ROW_BLOCK);
-        auto product = [&](uint32_t d, uint32_t a, uint64_t b, bool first) {  // (a: a half of the columns of each part's scores)
+        auto product = [&](uint32_t d, uint32_t a, uint64_t b, bool first) {  // (a: COLS / 2 columns in each part's COLS)
 #pragma unroll
             for (int kk = 0; kk < kTbStep / 16; ++kk)
                 warp_mma_f16_ts(d, a + kk * 16 / C::COLS * C::COLS + kk * 16 % C::COLS / 2, b + (uint64_t)(128 * kk), C::IDESC_B, (!first || kk) ? 1u : 0u);
         };
         bool ok = true;
         int s = 0, g = 0;
-        Item t;
-        for (int k = 0; ok && item_of(k, t); ++k) {
-            if (!(ok = wait(C::BAR_ACCREAD, ((uint32_t)k & 1u) ^ 1u, 0xb20u))) break;
+        uint32_t ph = 1;
+        while (ok && next(c, t)) {
+            if (!(ok = wait(C::BAR_ACCREAD, ph, 0xb20u))) break;
+            ph ^= 1u;
             for (int j = 0; j < t.J; ++j, ++g) {
                 const int par = g & 1;
                 const uint64_t rows = row_desc + (uint64_t)(s * (C::ROW_BYTES >> 4));
-                if (!(ok = wait(C::BAR_P + par, (uint32_t)(g >> 1) & 1u, 0xb22u))) break;
+                if (!(ok = wait(C::BAR_P + par, phase(g, 2), 0xb22u))) break;
                 tc_fence_after();
-                const uint32_t col = tmem + C::COL_S + par * NS * kTbStep;
+                const uint32_t col = tmem + (C::OVER_A ? C::COL_A + par * kTbStep : C::COL_S + par * NS * kTbStep);
                 if constexpr (KEYS) product(tmem + C::COL_V, col + C::COLS / 2, rows + (uint64_t)(NS * (C::ROW_TILE >> 4)), j == 0 && (NS == 2 || t.st == 1));
 #pragma unroll
                 for (int a = 0; a < NS; ++a)
-                    product(tmem + C::COL_T + a * DH, col + a * kTbStep, rows + (uint64_t)(a * (C::ROW_TILE >> 4)), j == 0);
+                    product(tmem + C::COL_T + a * DH, col + a * (C::OVER_A ? C::COLS / 2 : kTbStep), rows + (uint64_t)(a * (C::ROW_TILE >> 4)), j == 0);
                 warp_commit(bar(C::BAR_BACK + par));
                 warp_commit(bar(C::BAR_EMPTY + s));
                 if (++s == C::ST) s = 0;
@@ -370,19 +405,48 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
         constexpr int COLS = C::COLS;
         const int part = (warp - 4) >> 2, quarter = warp & 3, row = 32 * quarter + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
-        const float c = p.scale_log2;
-        const uint64_t c2 = pack_f32x2(c, c);
-        double dl = 0.0;
+        const size_t width = (size_t)h * DH;
+        const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
+        // The thread's quarter of the item's resident rows into tensor memory.  An item's last scores and A have been read when the next one's
+        // rows come, so no product reads them any more.
+        auto bring = [&](const Item &n) {
+            if constexpr (C::TRES > 0) {
+                uint32_t v[C::TRES][DH / 8] = {};
+                const size_t tok = (size_t)n.b * L + n.r0 + row;
+                if (n.r0 + row < L) {
+#pragma unroll
+                    for (int a = 0; a < C::TRES; ++a) {
+                        const __nv_bfloat16 *src = a < NS ? pass.res2 + tok * 2 * width + ((size_t)(n.st + a) * h + n.hd) * DH : pass.res1 + tok * width + (size_t)n.hd * DH;
+#pragma unroll
+                        for (int u = 0; u < DH / 32; ++u) {
+                            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(src + part * (DH / 4)) + u);
+                            v[a][4 * u] = w.x; v[a][4 * u + 1] = w.y; v[a][4 * u + 2] = w.z; v[a][4 * u + 3] = w.w;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int a = 0; a < C::TRES; ++a) tb_store(lane_base + C::COL_R + a * (DH / 2) + part * (DH / 8), v[a]);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::BAR_RT));
+            }
+        };
+        auto two = [](const uint32_t *v) { return pack_f32x2(__uint_as_float(v[0]), __uint_as_float(v[1])); };
         bool ok = true;
         int s = 0, g = 0;
-        Item t;
-        for (int k = 0; ok && item_of(k, t); ++k) {
+        uint32_t ph = 0;
+        Item n;
+        bool more = next(c, n);
+        if (more) bring(n);
+        while (ok && more) {
+            t = n;
             const int mine = t.r0 + row, w0 = t.r0 + 32 * quarter;  // the thread's key or query; the warp's first
             uint64_t nl[NS] = {}, nd[NS] = {}, sum = 0;             // (queries) -lse and -D of the row, twice each
             if constexpr (!KEYS) {
 #pragma unroll
                 for (int a = 0; a < NS; ++a) {
-                    const float *st = reinterpret_cast<const float *>(p.stats + (t.bh * n64 + mine / 64) * kTbStatBytes + kTbTileBytes + kTbDeltaBytes) + mine % 64 +
+                    const float *st = reinterpret_cast<const float *>(p.stats + ((size_t)t.bh * n64 + mine / 64) * kTbStatBytes + kTbTileBytes + kTbDeltaBytes) + mine % 64 +
                                       64 * (t.st + a);
                     const float l = mine < L ? __ldg(st) : -INFINITY, d = mine < L ? __ldg(st + 128) : 0.0f;
                     nl[a] = pack_f32x2(l, l);
@@ -393,15 +457,20 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
             const float wp = NS == 2 || t.st == 1 ? -p.lambda : 1.0f;
             const uint64_t wp2 = pack_f32x2(wp, wp);
             for (int j = 0; j < t.J; ++j, ++g) {
-                const int par = g & 1, ab = C::NA == 2 ? par : 0, c0 = t.s0 + j * kTbStep + COLS * part;  // the thread's first column
-                const uint32_t s_addr = lane_base + C::COL_S + par * NS * kTbStep + COLS * part;
+                const int par = g & 1, sb = C::NSB == 2 ? par : 0, ab = C::NA == 2 ? par : 0, c0 = t.s0 + j * kTbStep + COLS * part;  // the thread's first column
+                const uint32_t s_addr = lane_base + C::COL_S + sb * NS * kTbStep + COLS * part, a_addr = lane_base + C::COL_A + ab * kTbStep + COLS * part;
                 const float *delta = reinterpret_cast<const float *>(smem + C::OFF_STATS + s * C::STAT_STAGE + kTbTileBytes) + COLS * part;
-                if (!(ok = wait(C::BAR_S + par, (uint32_t)(g >> 1) & 1u, 0xb30u))) break;
+                if (!(ok = wait(C::BAR_S + sb, phase(g, C::NSB), 0xb30u))) break;
                 tc_fence_after();
                 uint32_t x[NS][COLS];
 #pragma unroll
                 for (int a = 0; a < NS; ++a) tb_load(s_addr + a * kTbStep, x[a]);
                 tmem_ld_wait();
+                if constexpr (C::OVER_A) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(C::BAR_READ + sb));
+                }
                 // some pair of the warp has its key behind its query
                 if (KEYS ? c0 < w0 + 31 : c0 + COLS - 1 > w0) {
 #pragma unroll
@@ -414,30 +483,29 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                 for (int a = 0; a < NS; ++a)
 #pragma unroll
                     for (int u = 0; u < COLS; u += 2) {
-                        const uint64_t v = pack_f32x2(__uint_as_float(x[a][u]), __uint_as_float(x[a][u + 1]));
                         float y0, y1;
-                        unpack_f32x2(KEYS ? mul_f32x2(v, c2) : fma_f32x2(v, c2, nl[a]), y0, y1);
+                        unpack_f32x2(KEYS ? mul_f32x2(two(&x[a][u]), c2) : fma_f32x2(two(&x[a][u]), c2, nl[a]), y0, y1);
                         x[a][u] = __float_as_uint(tb_ex2(y0));
                         x[a][u + 1] = __float_as_uint(tb_ex2(y1));
                     }
-                if (!(ok = wait(C::BAR_A + ab, C::NA == 2 ? (uint32_t)(g >> 1) & 1u : (uint32_t)g & 1u, 0xb32u))) break;
+                if (!(ok = wait(C::BAR_A + ab, phase(g, C::NA), 0xb32u))) break;
                 tc_fence_after();
                 uint32_t dp[COLS];
-                tb_load(lane_base + C::COL_A + ab * kTbStep + COLS * part, dp);
+                tb_load(a_addr, dp);
                 tmem_ld_wait();
-                if constexpr (C::NA == 1) {
+                if constexpr (!C::OVER_A) {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(C::BAR_AREAD));
+                    if (lane == 0) mbar_arrive(bar(C::BAR_READ));
                 }
-                auto two = [](const uint32_t *v) { return pack_f32x2(__uint_as_float(v[0]), __uint_as_float(v[1])); };
                 // P and T are rounded to bf16 for the products (2^-9 each, fp32 sums), as the forward pass rounds P
+                const uint32_t o_addr = C::OVER_A ? a_addr : s_addr;
                 if constexpr (KEYS) {
                     uint32_t o[COLS / 2];
 #pragma unroll
                     for (int u = 0; u < COLS; u += 2)
                         o[u >> 1] = tb_pack_bf16(NS == 2 ? fma_f32x2(two(&x[NS - 1][u]), wp2, two(&x[0][u])) : mul_f32x2(two(&x[0][u]), wp2));
-                    tb_store(s_addr + COLS / 2, o);
+                    tb_store(o_addr + COLS / 2, o);
                 }
 #pragma unroll
                 for (int a = 0; a < NS; ++a) {
@@ -447,9 +515,9 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                         uint64_t d0 = two(&dp[u]), d1 = two(&dp[u + 2]);
                         if constexpr (KEYS) {  // (D_1 is subtracted, or with one stream its own)
                             if (a == 1) {
-                                const ulonglong2 n = *reinterpret_cast<const ulonglong2 *>(delta + u);
-                                d0 = add_f32x2(d0, n.x);
-                                d1 = add_f32x2(d1, n.y);
+                                const ulonglong2 e = *reinterpret_cast<const ulonglong2 *>(delta + u);
+                                d0 = add_f32x2(d0, e.x);
+                                d1 = add_f32x2(d1, e.y);
                             }
                         } else {
                             d0 = add_f32x2(d0, nd[a]);
@@ -460,7 +528,7 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                         o[(u >> 1) + 1] = tb_pack_bf16(t1);
                         if (!KEYS && a == NS - 1) sum = add_f32x2(add_f32x2(t0, t1), sum);  // (of the second stream, or of the one at hand)
                     }
-                    tb_store(s_addr + a * kTbStep, o);
+                    tb_store(o_addr + a * (C::OVER_A ? COLS / 2 : kTbStep), o);
                 }
                 tmem_st_wait();
                 tc_fence_before();
@@ -478,10 +546,12 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                     dl += (double)a + (double)b - (part ? 0.0 : (double)d);
                 }
             }
+            if ((more = next(c, n))) bring(n);
             // ---- outputs: this warp's rows, its part of each accumulator's columns
-            if (!(ok = wait(C::BAR_ACC, (uint32_t)k & 1u, 0xb40u))) break;
+            if (!(ok = wait(C::BAR_ACC, ph, 0xb40u))) break;
+            ph ^= 1u;
             tc_fence_after();
-            const size_t tok = (size_t)t.b * L + mine, width = (size_t)h * DH;
+            const size_t tok = (size_t)t.b * L + mine;
             auto put = [&](uint32_t col, float f, __nv_bfloat16 *dst) {
                 constexpr int N = DH / C::PARTS;
                 uint32_t v[N];
@@ -498,36 +568,76 @@ attention_backward_kernel(const __grid_constant__ CUtensorMap map_res2, const __
                 }
             };
             if constexpr (KEYS)
-                if (NS == 2 || t.st == 0) put(C::COL_V, p.out_scale, p.d1 + tok * width + (size_t)t.hd * DH);
+                if (NS == 2 || t.st == 0) put(C::COL_V, p.out_scale, pass.d1 + tok * width + (size_t)t.hd * DH);
 #pragma unroll
             for (int a = 0; a < NS; ++a)
-                put(C::COL_T + a * DH, p.out_scale * p.scale * (t.st + a == 1 ? -p.lambda : 1.0f),
-                    p.d2 + tok * 2 * width + ((size_t)(t.st + a) * h + t.hd) * DH);
+                put(C::COL_T + a * DH, p.out_scale * p.scale * (t.st + a == 1 ? -p.lambda : 1.0f), pass.d2 + tok * 2 * width + ((size_t)(t.st + a) * h + t.hd) * DH);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::BAR_ACCREAD));
         }
-        if constexpr (!KEYS) {
-#pragma unroll
-            for (int o = 16; o; o >>= 1) dl += __shfl_xor_sync(0xffffffffu, dl, o);
-            if (lane == 0) p.dl_part[(size_t)blockIdx.x * C::WARPS + warp - 4] = dl;
-        }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) {
-        tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512) : "memory");
-    }
+    tc_fence_after();
+    return dl;
 }
 
-// dlambda = -out_scale times the sum of the partial sums, in one order.
-__global__ void __launch_bounds__(32) attention_dlambda_kernel(const double *part, int n, float out_scale, float *dlambda) {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += 32) s += part[i];
+struct TbMaps {
+    CUtensorMap res2, res1, row2, row1;
+};
+
+template <int DH>
+__global__ void __launch_bounds__(TbCfg<DH, true>::THREADS, 1)
+attention_backward_kernel(const __grid_constant__ TbMaps keys, const __grid_constant__ TbMaps queries, const TbPass of_keys, const TbPass of_queries,
+                          const AttnBackParams p, unsigned int *status) {
+    constexpr int WARPS = TbCfg<DH, true>::WARPS, THREADS = TbCfg<DH, true>::THREADS;
+    extern __shared__ uint8_t tb_smem_raw[];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort, s_last;
+    uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)tb_smem_raw + 1023) & ~(uintptr_t)1023);
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) s_abort = 0;
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    pdl_wait();
+    if (p.keys) attention_backward_pass<DH, true>(keys.res2, keys.res1, keys.row2, keys.row1, of_keys, p, smem, tmem, &s_abort, status);
+    if (p.queries) {
+        double dl = attention_backward_pass<DH, false>(queries.res2, queries.res1, queries.row2, queries.row1, of_queries, p, smem, tmem, &s_abort, status);
+        if (p.dlambda) {
+            // a sum for each warp; the CTA that comes last adds them all up, in one order
 #pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (threadIdx.x == 0) *dlambda = (float)(-(double)out_scale * s);
+            for (int o = 16; o; o >>= 1) dl += __shfl_xor_sync(0xffffffffu, dl, o);
+            if (warp >= 4 && lane == 0) {
+                p.dl_part[(size_t)blockIdx.x * WARPS + warp - 4] = dl;
+                __threadfence();
+            }
+            __syncthreads();
+            if (threadIdx.x == 0) s_last = atomicAdd(p.arrivals, 1u) == gridDim.x - 1;
+            __syncthreads();
+            if (s_last) {
+                double *s_sum = reinterpret_cast<double *>(smem + 2 * kTbBarBytes);
+                __threadfence();
+                double v = 0.0;
+                for (int i = threadIdx.x; i < (int)gridDim.x * WARPS; i += THREADS) v += __ldcg(p.dl_part + i);
+#pragma unroll
+                for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                if (lane == 0) s_sum[warp] = v;
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    for (int i = 1; i < THREADS / 32; ++i) v += s_sum[i];
+                    *p.dlambda = (float)(-(double)p.out_scale * v);
+                }
+            }
+        }
+    }
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512) : "memory");
 }
 
 static bool make_map_tokens(CUtensorMap *map, const void *base, uint64_t width, uint64_t L, uint64_t B, uint32_t rows) {
@@ -539,59 +649,63 @@ static bool make_map_tokens(CUtensorMap *map, const void *base, uint64_t width, 
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-template <int DH, bool KEYS>
-static cudaError_t launch_backward_pass(const AttnBackParams &p, const void *res2, const void *res1, const void *row2, const void *row1, int grid,
-                                        cudaStream_t stream) {
-    using C = TbCfg<DH, KEYS>;
-    static std::atomic<unsigned long long> attr_done{0};
-    cudaError_t e = ensure_dynamic_smem(attention_backward_kernel<DH, KEYS>, C::SMEM_BYTES, attr_done);
-    if (e != cudaSuccess) return e;
-    unsigned int *status = device_status_word();
-    if (!status) return cudaErrorMemoryAllocation;
-    const uint64_t w = (uint64_t)p.h * DH;
-    CUtensorMap m[4];
-    if (!make_map_tokens(&m[0], res2, 2 * w, p.L, p.B, kTbTile) || !make_map_tokens(&m[1], res1, w, p.L, p.B, kTbTile) ||
-        !make_map_tokens(&m[2], row2, 2 * w, p.L, p.B, kTbStep) || !make_map_tokens(&m[3], row1, w, p.L, p.B, kTbStep))
-        return cudaErrorInvalidValue;
-    attention_backward_kernel<DH, KEYS><<<grid, C::THREADS, C::SMEM_BYTES, stream>>>(m[0], m[1], m[2], m[3], p, status);
-    count_launch();
-    return cudaGetLastError();
+static bool make_maps(TbMaps *m, const void *res2, const void *res1, const void *row2, const void *row1, int dh, const AttnBackParams &p) {
+    const uint64_t w = (uint64_t)p.h * dh;
+    return make_map_tokens(&m->res2, res2, 2 * w, p.L, p.B, kTbTile) && make_map_tokens(&m->res1, res1, w, p.L, p.B, kTbTile) &&
+           make_map_tokens(&m->row2, row2, 2 * w, p.L, p.B, kTbStep) && make_map_tokens(&m->row1, row1, w, p.L, p.B, kTbStep);
 }
 
 constexpr int kTbMaxGrid = 1024;
+// workspace: blocks of statistics, the warps' sums for dlambda, the count of CTAs that have left theirs
 static size_t stats_bytes(int64_t B, int64_t L, int64_t h) { return (size_t)(B * h) * (size_t)((L + 63) / 64) * kTbStatBytes; }
+constexpr size_t kTbPartBytes = (size_t)kTbMaxGrid * TbCfg<64, true>::WARPS * sizeof(double);
+
+template <typename... F, typename... A>
+static cudaError_t launch_early(void (*kernel)(F...), unsigned grid, int threads, int smem, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, F(args)...);
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
 
 template <int DH>
 static cudaError_t launch_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
                                    const hgf_attention_grads &grads, AttnBackParams p, void *workspace, cudaStream_t stream) {
+    constexpr int SMEM = TbCfg<DH, true>::SMEM_BYTES > TbCfg<DH, false>::SMEM_BYTES ? TbCfg<DH, true>::SMEM_BYTES : TbCfg<DH, false>::SMEM_BYTES;
+    static std::atomic<unsigned long long> attr_done{0};
+    cudaError_t e = ensure_dynamic_smem(attention_backward_kernel<DH>, SMEM, attr_done);
+    if (e != cudaSuccess) return e;
+    unsigned int *status = device_status_word();
+    if (!status) return cudaErrorMemoryAllocation;
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;
-    const long long bhs = (long long)p.B * p.h, blocks = bhs * ((p.L + 63) / 64), tiles = bhs * ((p.L + kTbTile - 1) / kTbTile);
-    const int most = sms < kTbMaxGrid ? sms : kTbMaxGrid, grid = tiles < most ? (int)tiles : most;
     uint8_t *stats = (uint8_t *)workspace;
     p.stats = stats;
-    p.dl_part = (double *)((char *)workspace + stats_bytes(p.B, p.L, p.h));
-    attention_stats_kernel<DH><<<(unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream>>>(
-        (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)streams, lse, stats, p.B, p.L, p.h, p.scale_log2);
-    count_launch();
-    cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess && (grads.dk || grads.dv)) {
-        p.d2 = (__nv_bfloat16 *)grads.dk;
-        p.d1 = (__nv_bfloat16 *)grads.dv;
-        e = launch_backward_pass<DH, true>(p, k, v, q, dout, grid, stream);
-    }
-    if (e == cudaSuccess && (grads.dq || grads.dlambda)) {
-        p.d2 = (__nv_bfloat16 *)grads.dq;
-        p.d1 = nullptr;
-        e = launch_backward_pass<DH, false>(p, q, dout, k, v, grid, stream);
-    }
-    if (e == cudaSuccess && grads.dlambda) {
-        attention_dlambda_kernel<<<1, 32, 0, stream>>>(p.dl_part, grid * TbCfg<DH, false>::WARPS, p.out_scale, grads.dlambda);
-        count_launch();
-        e = cudaGetLastError();
-    }
-    return e;
+    p.dl_part = (double *)(stats + stats_bytes(p.B, p.L, p.h));
+    p.arrivals = (unsigned int *)(stats + stats_bytes(p.B, p.L, p.h) + kTbPartBytes);
+    p.keys = grads.dk != nullptr;
+    p.queries = grads.dq != nullptr;
+    p.both = p.keys && p.queries;
+    p.dlambda = grads.dlambda;
+    const long long bhs = (long long)p.B * p.h, blocks = bhs * ((p.L + 63) / 64), tiles = bhs * ((p.L + kTbTile - 1) / kTbTile) * (p.both ? 2 : 1);
+    const int most = sms < kTbMaxGrid ? sms : kTbMaxGrid, grid = tiles < most ? (int)tiles : most;
+    TbMaps keys, queries;
+    if (!make_maps(&keys, k, v, q, dout, DH, p) || !make_maps(&queries, q, dout, k, v, DH, p)) return cudaErrorInvalidValue;
+    const TbPass of_keys = {(const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v, (__nv_bfloat16 *)grads.dk, (__nv_bfloat16 *)grads.dv};
+    const TbPass of_queries = {(const __nv_bfloat16 *)q, (const __nv_bfloat16 *)dout, (__nv_bfloat16 *)grads.dq, nullptr};
+    e = launch_early(attention_stats_kernel<DH>, (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream, (const __nv_bfloat16 *)dout,
+                     (const __nv_bfloat16 *)streams, lse, stats, p.arrivals, p.B, p.L, p.h, p.scale_log2);
+    if (e != cudaSuccess) return e;
+    return launch_early(attention_backward_kernel<DH>, (unsigned)grid, TbCfg<DH, true>::THREADS, SMEM, stream, keys, queries, of_keys, of_queries, p, status);
 }
 
 }  // namespace hgf
@@ -605,7 +719,7 @@ static bool backward_sizes_ok(int64_t B, int64_t L, int32_t n_heads, int32_t hea
 
 extern "C" size_t hgf_diff_attention_backward_workspace_bytes(int64_t B, int64_t L, int32_t n_heads, int32_t head_dim) {
     if (B <= 0 || L <= 0 || n_heads <= 0 || !backward_sizes_ok(B, L, n_heads, head_dim)) return 0;
-    return stats_bytes(B, L, n_heads) + (size_t)kTbMaxGrid * 16 * sizeof(double);
+    return stats_bytes(B, L, n_heads) + kTbPartBytes + 256;
 }
 
 extern "C" hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
