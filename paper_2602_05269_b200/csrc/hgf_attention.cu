@@ -76,25 +76,6 @@ __device__ __forceinline__ float ex2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
     return y;
 }
-// Four lanes (lane / 4 alike) with four 16-byte blocks each: afterwards block q of lane 4 i + t is what block t of lane
-// 4 i + q was.
-__device__ __forceinline__ void exchange_blocks(uint32_t (&v)[16], int lane) {
-#pragma unroll
-    for (int step = 1; step <= 2; step *= 2) {
-        const bool upper = (lane & step) != 0;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            if (b & step) continue;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t &lo = v[4 * b + e], &hi = v[4 * (b + step) + e];
-                const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, step);
-                if (upper) lo = got; else hi = got;
-            }
-        }
-    }
-}
-
 // SAVE: for the backward pass each stream's own output O_s / l_s (bf16) and log2 of its sum of 2^(scale s) go to memory, too.
 template <int DH, bool SAVE>
 __global__ void __launch_bounds__(kTaThreads, 1)

@@ -407,25 +407,28 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
         const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
         const size_t width = (size_t)h * DH;
         const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
-        // The thread's quarter of the item's resident rows into tensor memory.  An item's last scores and A have been read when the next one's
-        // rows come, so no product reads them any more.
+        // The item's resident rows into tensor memory, in units of 32 dims.  An item's last scores and A have been read when the next one's rows
+        // come, so no product reads them any more.  Four neighbouring lanes read 64 consecutive bytes of one row at a time and exchange blocks
+        // of 16 bytes, so that each has its own row: a lane along its own row touches 32 lines with every instruction, 1.5 us a tile.
         auto bring = [&](const Item &n) {
             if constexpr (C::TRES > 0) {
-                uint32_t v[C::TRES][DH / 8] = {};
-                const size_t tok = (size_t)n.b * L + n.r0 + row;
-                if (n.r0 + row < L) {
 #pragma unroll
-                    for (int a = 0; a < C::TRES; ++a) {
-                        const __nv_bfloat16 *src = a < NS ? pass.res2 + tok * 2 * width + ((size_t)(n.st + a) * h + n.hd) * DH : pass.res1 + tok * width + (size_t)n.hd * DH;
+                for (int r = 0; r < (C::TRES * DH / 32 + C::PARTS - 1) / C::PARTS; ++r) {
+                    const int unit = r * C::PARTS + part, a = unit / (DH / 32), dims = unit % (DH / 32) * 32;
+                    if (unit >= C::TRES * DH / 32) continue;
+                    const int first = n.r0 + 32 * quarter + (lane & ~3);
+                    const __nv_bfloat16 *src = a < NS ? pass.res2 + ((size_t)(n.st + a) * h + n.hd) * DH : pass.res1 + (size_t)n.hd * DH;
+                    const size_t pitch = a < NS ? 2 * width : width;
+                    uint32_t v[16];
 #pragma unroll
-                        for (int u = 0; u < DH / 32; ++u) {
-                            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(src + part * (DH / 4)) + u);
-                            v[a][4 * u] = w.x; v[a][4 * u + 1] = w.y; v[a][4 * u + 2] = w.z; v[a][4 * u + 3] = w.w;
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        uint4 w = make_uint4(0, 0, 0, 0);
+                        if (first + e < L) w = __ldg(reinterpret_cast<const uint4 *>(src + ((size_t)n.b * L + first + e) * pitch + dims + 8 * (lane & 3)));
+                        v[4 * e] = w.x; v[4 * e + 1] = w.y; v[4 * e + 2] = w.z; v[4 * e + 3] = w.w;
                     }
+                    exchange_blocks(v, lane);
+                    tmem_st16(lane_base + C::COL_R + unit * 16, v);
                 }
-#pragma unroll
-                for (int a = 0; a < C::TRES; ++a) tb_store(lane_base + C::COL_R + a * (DH / 2) + part * (DH / 8), v[a]);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -547,31 +550,30 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                 }
             }
             if ((more = next(c, n))) bring(n);
-            // ---- outputs: this warp's rows, its part of each accumulator's columns
+            // ---- outputs: this warp's rows, in units of 32 columns of an accumulator (64 bytes of a row, stored by four lanes as above)
             if (!(ok = wait(C::BAR_ACC, ph, 0xb40u))) break;
             ph ^= 1u;
             tc_fence_after();
-            const size_t tok = (size_t)t.b * L + mine;
-            auto put = [&](uint32_t col, float f, __nv_bfloat16 *dst) {
-                constexpr int N = DH / C::PARTS;
-                uint32_t v[N];
-                tb_load(lane_base + col + part * N, v);
+            const bool with_v = KEYS && (NS == 2 || t.st == 0);
+            const int units = (NS + (with_v ? 1 : 0)) * DH / 32;
+            for (int unit = part; unit < units; unit += C::PARTS) {
+                const int a = unit / (DH / 32), dims = unit % (DH / 32) * 32;  // (stream a of the tile's, or V)
+                uint32_t v[32], o[16];
+                tmem_ld32(lane_base + (a < NS ? C::COL_T + a * DH : C::COL_V) + dims, v);
                 tmem_ld_wait();
-                if (mine < L) {
+                const float f = a < NS ? p.out_scale * p.scale * (t.st + a == 1 ? -p.lambda : 1.0f) : p.out_scale;
 #pragma unroll
-                    for (int u = 0; u < N; u += 8) {
-                        uint32_t o[4];
+                for (int e = 0; e < 16; ++e) o[e] = tb_pack_bf16(__uint_as_float(v[2 * e]) * f, __uint_as_float(v[2 * e + 1]) * f);
+                exchange_blocks(o, lane);
+                const int first = w0 + (lane & ~3);
+                __nv_bfloat16 *dst = a < NS ? pass.d2 + ((size_t)(t.st + a) * h + t.hd) * DH : pass.d1 + (size_t)t.hd * DH;
+                const size_t pitch = a < NS ? 2 * width : width;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = tb_pack_bf16(__uint_as_float(v[u + 2 * e]) * f, __uint_as_float(v[u + 2 * e + 1]) * f);
-                        *reinterpret_cast<uint4 *>(dst + part * N + u) = make_uint4(o[0], o[1], o[2], o[3]);
-                    }
-                }
-            };
-            if constexpr (KEYS)
-                if (NS == 2 || t.st == 0) put(C::COL_V, p.out_scale, pass.d1 + tok * width + (size_t)t.hd * DH);
-#pragma unroll
-            for (int a = 0; a < NS; ++a)
-                put(C::COL_T + a * DH, p.out_scale * p.scale * (t.st + a == 1 ? -p.lambda : 1.0f), pass.d2 + tok * 2 * width + ((size_t)(t.st + a) * h + t.hd) * DH);
+                for (int e = 0; e < 4; ++e)
+                    if (first + e < L)
+                        *reinterpret_cast<uint4 *>(dst + ((size_t)t.b * L + first + e) * pitch + dims + 8 * (lane & 3)) =
+                            make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::BAR_ACCREAD));

@@ -183,6 +183,26 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 
+// Four lanes (lane / 4 alike) with four 16-byte blocks each: afterwards block q of lane 4 i + t is what block t of lane
+// 4 i + q was.
+__device__ __forceinline__ void exchange_blocks(uint32_t (&v)[16], int lane) {
+#pragma unroll
+    for (int step = 1; step <= 2; step *= 2) {
+        const bool upper = (lane & step) != 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            if (b & step) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t &lo = v[4 * b + e], &hi = v[4 * (b + step) + e];
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, step);
+                if (upper) lo = got; else hi = got;
+            }
+        }
+    }
+}
+
+
 // Shared-memory operand descriptor: K-major rows of 128 bytes, 128-byte swizzle, groups of 8 rows
 // 1024 bytes apart.  Fields: start address >> 4 (bits 0-13), leading byte offset >> 4 (16-29,
 // unused for this layout, set to 1), stride byte offset >> 4 (32-45), version 1 (46-47),
