@@ -220,6 +220,11 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
         }
     };
 
+    {
+        Cursor any = {0, false};
+        Item t;
+        if (!next(any, t)) return 0.0;
+    }
     if (tid == 0) {
         for (int i = 0; i < C::NRES; ++i) {
             mbar_init(bar(C::BAR_RESFULL + i), 1);
@@ -600,6 +605,11 @@ attention_backward_kernel(const __grid_constant__ TbMaps keys, const __grid_cons
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)tb_smem_raw + 1023) & ~(uintptr_t)1023);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) s_abort = 0;
+    if (warp == 0 && lane < 8) {
+        const TbMaps &m = lane < 4 ? keys : queries;
+        const CUtensorMap *map = (lane & 3) == 0 ? &m.res2 : (lane & 3) == 1 ? &m.res1 : (lane & 3) == 2 ? &m.row2 : &m.row1;
+        asm volatile("prefetch.tensormap [%0];\n" ::"l"(map) : "memory");
+    }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");

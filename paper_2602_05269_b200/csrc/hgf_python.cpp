@@ -134,19 +134,16 @@ decltype(&hgf_cache_fork) g_fork = nullptr;
 decltype(&hgf_cache_free) g_free = nullptr;
 decltype(&hgf_diff_attention_cached) g_attend = nullptr;
 
-struct CacheCall {
-    const hgf_cache *cache;
-    int64_t device;
+// A call on tensors of the current device: its stream, and whether all that it has been given is what it takes.
+struct DeviceCall {
+    int64_t device = -1;
     void *stream = nullptr;
     bool ok = true;
 
-    CacheCall(PyObject *at, PyObject *dev, PyObject *stream_) {
-        unsigned long long v = 0, d = 0;
-        ok = integer(at, &v) && integer(dev, &d);  // (a cache in host memory has -1)
-        cache = reinterpret_cast<const hgf_cache *>(v);
-        device = (int64_t)d;
+    void begin(PyObject *stream_) {
         ok = ok && device >= 0 && device == (int64_t)at::cuda::current_device();
         if (!ok) return;
+        unsigned long long v = 0;
         if (stream_ == Py_None) {
             stream = at::cuda::getCurrentCUDAStream().stream();
         } else {
@@ -155,6 +152,12 @@ struct CacheCall {
             Py_XDECREF(s);
             stream = reinterpret_cast<void *>(v);
         }
+    }
+    // The device of the first tensor that is one.
+    DeviceCall &of(PyObject *o) {
+        const at::Tensor *t = plain_tensor(o);
+        if (device < 0 && t && t->is_cuda()) device = t->device().index();
+        return *this;
     }
     const at::Tensor *tensor(PyObject *o, at::ScalarType type) {
         const at::Tensor *t = plain_tensor(o);
@@ -180,6 +183,36 @@ struct CacheCall {
         const at::Tensor *t = plain_tensor(o);
         ok = ok && t && t->dim() == 2;
         return ok ? t->size(0) : 0;
+    }
+    int64_t cols(PyObject *o) { return height(o) || ok ? plain_tensor(o)->size(1) : 0; }
+    void *vector(PyObject *o, at::ScalarType type, int64_t n) {
+        const at::Tensor *t = tensor(o, type);
+        ok = ok && t->dim() == 1 && t->size(0) == n;
+        return ok ? t->data_ptr() : nullptr;
+    }
+    // (None: a null pointer)
+    void *matrix_or_none(PyObject *o, at::ScalarType type, int64_t rows, int64_t n) { return o == Py_None ? nullptr : matrix(o, type, rows, n); }
+    void *vector_or_none(PyObject *o, at::ScalarType type, int64_t n) { return o == Py_None ? nullptr : vector(o, type, n); }
+    double number(PyObject *o) {
+        const double v = PyFloat_AsDouble(o);
+        ok = ok && !(v == -1.0 && PyErr_Occurred());
+        return v;
+    }
+    int64_t whole(PyObject *o) {
+        int64_t v = 0;
+        ok = ok && integer(o, &v);
+        return v;
+    }
+};
+struct CacheCall : DeviceCall {
+    const hgf_cache *cache;
+
+    CacheCall(PyObject *at, PyObject *dev, PyObject *stream_) {
+        unsigned long long v = 0, d = 0;
+        ok = integer(at, &v) && integer(dev, &d);  // (a cache in host memory has -1)
+        cache = reinterpret_cast<const hgf_cache *>(v);
+        device = (int64_t)d;
+        begin(stream_);
     }
 };
 PyObject *given_back() { return PyErr_Occurred() ? nullptr : PyLong_FromLong(-1); }
@@ -292,6 +325,145 @@ PyObject *bind_cache(PyObject *, PyObject *args) {
     Py_RETURN_NONE;
 }
 
+// ---- training calls -----------------------------------------------------------------------------------------------------------
+// As the cache calls: the arguments of the function of the same name in hgf.py, every tensor made already; -1 where one is not what the call takes.
+decltype(&hgf_diff_attention_forward_train) g_attention = nullptr;
+decltype(&hgf_diff_attention_backward) g_attention_backward = nullptr;
+decltype(&hgf_qk_norm_rotate) g_rotate = nullptr;
+decltype(&hgf_qk_norm_rotate_backward) g_rotate_backward = nullptr;
+decltype(&hgf_clip_grad_norm) g_clip = nullptr;
+
+struct AttentionCall : DeviceCall {
+    int64_t B, L, h, dh, width = 0, rows = 0;
+    double lambda, scale;
+    const void *q, *k, *v, *streams;
+    const float *lse;
+    // q, k, v, then at n: B, L, n_heads, head_dim, lambda, out_scale
+    AttentionCall(PyObject *const *a, int n, PyObject *streams_, PyObject *lse_, PyObject *stream_) {
+        of(a[0]);
+        begin(stream_);
+        B = whole(a[n]), L = whole(a[n + 1]), h = whole(a[n + 2]), dh = whole(a[n + 3]);
+        lambda = number(a[n + 4]), scale = number(a[n + 5]);
+        ok = ok && B > 0 && L > 0 && h > 0 && dh > 0 && B < (1 << 24) && L < (1ll << 32) && h < (1 << 24) && dh < (1 << 12);
+        if (!ok) return;
+        rows = B * L, width = h * dh;
+        q = matrix(a[0], at::kBFloat16, rows, 2 * width), k = matrix(a[1], at::kBFloat16, rows, 2 * width), v = matrix(a[2], at::kBFloat16, rows, width);
+        streams = matrix(streams_, at::kBFloat16, rows, 2 * width);
+        const at::Tensor *t = tensor(lse_, at::kFloat);
+        ok = ok && t->dim() == 4 && t->size(0) == B && t->size(1) == h && t->size(2) == 2 && t->size(3) == L;
+        lse = ok ? static_cast<const float *>(t->data_ptr()) : nullptr;
+    }
+};
+// (q, k, v, B, L, n_heads, head_dim, lambda, out_scale, out, streams, lse, flags, stream)
+PyObject *diff_attention_forward_train(PyObject *, PyObject *const *a, Py_ssize_t n_) {
+    return guarded(n_, 14, [&]() -> PyObject * {
+        AttentionCall c(a, 3, a[10], a[11], a[13]);
+        const int64_t flags = c.whole(a[12]);
+        void *out = c.matrix(a[9], flags & HGF_FLAG_OUT_BF16 ? at::kBFloat16 : at::kFloat, c.rows, c.width);
+        if (!c.ok) return given_back();
+        return called([&] {
+            return g_attention(c.q, c.k, c.v, c.B, c.L, (int32_t)c.h, (int32_t)c.dh, (float)c.lambda, (float)c.scale, out, const_cast<void *>(c.streams),
+                               const_cast<float *>(c.lse), (uint32_t)flags, c.stream);
+        });
+    });
+}
+// (q, k, v, dout, streams, lse, B, L, n_heads, head_dim, lambda, out_scale, dq, dk, dv, dlambda, workspace, stream)
+PyObject *diff_attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n_) {
+    return guarded(n_, 18, [&]() -> PyObject * {
+        AttentionCall c(a, 6, a[4], a[5], a[17]);
+        const void *dout = c.matrix(a[3], at::kBFloat16, c.rows, c.width);
+        hgf_attention_grads g = {};
+        g.dq = c.matrix_or_none(a[12], at::kBFloat16, c.rows, 2 * c.width);
+        g.dk = c.matrix_or_none(a[13], at::kBFloat16, c.rows, 2 * c.width);
+        g.dv = c.matrix_or_none(a[14], at::kBFloat16, c.rows, c.width);
+        g.dlambda = static_cast<float *>(c.vector_or_none(a[15], at::kFloat, 1));
+        const at::Tensor *workspace = c.tensor(a[16], at::kByte);
+        if (!c.ok) return given_back();
+        return called([&] {
+            return g_attention_backward(c.q, c.k, c.v, dout, c.streams, c.lse, c.B, c.L, (int32_t)c.h, (int32_t)c.dh, (float)c.lambda, (float)c.scale, &g,
+                                        workspace->data_ptr(), (size_t)workspace->numel(), 0u, c.stream);
+        });
+    });
+}
+
+struct RotateCall : DeviceCall {
+    int64_t rows = 0, dh, rot, flags, wide_q = 0, wide_k = 0;
+    const void *q = nullptr, *k = nullptr;
+    const int32_t *pos = nullptr;
+    const float *wq = nullptr, *wk = nullptr;
+    double eps, base;
+    // q, k, positions, head_dim, wq, wk, eps, base, rotary_dim, flags
+    RotateCall(PyObject *const *a, PyObject *stream_) {
+        of(a[0]).of(a[1]);
+        begin(stream_);
+        dh = whole(a[3]), eps = number(a[6]), base = number(a[7]), rot = whole(a[8]), flags = whole(a[9]);
+        ok = ok && dh > 0 && dh < (1 << 12) && rot >= 0 && rot <= dh;
+        if (!ok) return;
+        PyObject *some = a[0] != Py_None ? a[0] : a[1];
+        rows = height(some);
+        if (a[0] != Py_None) wide_q = cols(a[0]);
+        if (a[1] != Py_None) wide_k = cols(a[1]);
+        ok = ok && wide_q % dh == 0 && wide_k % dh == 0 && (wide_q | wide_k) < (1ll << 31);
+        q = matrix_or_none(a[0], at::kBFloat16, rows, wide_q), k = matrix_or_none(a[1], at::kBFloat16, rows, wide_k);
+        pos = list(a[2], rows);
+        wq = static_cast<const float *>(vector_or_none(a[4], at::kFloat, dh)), wk = static_cast<const float *>(vector_or_none(a[5], at::kFloat, dh));
+    }
+};
+// (q, k, positions, head_dim, wq, wk, eps, base, rotary_dim, flags, q_out, k_out, stream)
+PyObject *qk_norm_rotate(PyObject *, PyObject *const *a, Py_ssize_t n_) {
+    return guarded(n_, 13, [&]() -> PyObject * {
+        RotateCall c(a, a[12]);
+        void *qo = c.matrix_or_none(a[10], at::kBFloat16, c.rows, c.wide_q), *ko = c.matrix_or_none(a[11], at::kBFloat16, c.rows, c.wide_k);
+        if (!c.ok || !qo != !c.q || !ko != !c.k) return given_back();
+        return called([&] {
+            return g_rotate(c.q, c.k, c.rows, (int32_t)(c.wide_q / c.dh), (int32_t)(c.wide_k / c.dh), (int32_t)c.dh, c.pos, c.wq, c.wk, (float)c.eps, c.base,
+                            (int32_t)c.rot, qo, ko, (uint32_t)c.flags, c.stream);
+        });
+    });
+}
+// (q, k, positions, head_dim, wq, wk, eps, base, rotary_dim, flags, dq_out, dk_out, dq, dk, dwq, dwk, workspace, stream)
+PyObject *qk_norm_rotate_backward(PyObject *, PyObject *const *a, Py_ssize_t n_) {
+    return guarded(n_, 18, [&]() -> PyObject * {
+        RotateCall c(a, a[17]);
+        const void *gq = c.matrix_or_none(a[10], at::kBFloat16, c.rows, c.wide_q), *gk = c.matrix_or_none(a[11], at::kBFloat16, c.rows, c.wide_k);
+        hgf_rotate_grads g = {};
+        g.dq = c.matrix_or_none(a[12], at::kBFloat16, c.rows, c.wide_q);
+        g.dk = c.matrix_or_none(a[13], at::kBFloat16, c.rows, c.wide_k);
+        g.dwq = static_cast<float *>(c.vector_or_none(a[14], at::kFloat, c.dh));
+        g.dwk = static_cast<float *>(c.vector_or_none(a[15], at::kFloat, c.dh));
+        const at::Tensor *workspace = c.tensor(a[16], at::kByte);
+        if (!c.ok || !gq != !c.q || !gk != !c.k) return given_back();
+        return called([&] {
+            return g_rotate_backward(c.q, c.k, c.rows, (int32_t)(c.wide_q / c.dh), (int32_t)(c.wide_k / c.dh), (int32_t)c.dh, c.pos, c.wq, c.wk, (float)c.eps, c.base,
+                                     (int32_t)c.rot, gq, gk, &g, workspace->data_ptr(), (size_t)workspace->numel(), (uint32_t)c.flags, c.stream);
+        });
+    });
+}
+// (handle, device, max_norm, norm, stream)
+PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_) {
+    return guarded(n_, 5, [&]() -> PyObject * {
+        DeviceCall c;
+        unsigned long long handle = 0;
+        if (!integer(a[0], &handle) || !integer(a[1], &c.device)) return nullptr;
+        c.begin(a[4]);
+        const double max_norm = c.number(a[2]);
+        void *norm = c.vector(a[3], at::kFloat, 1);
+        if (!c.ok) return given_back();
+        return called([&] { return g_clip(reinterpret_cast<hgf_grad_list *>(handle), (float)max_norm, static_cast<float *>(norm), c.stream); });
+    });
+}
+// bind_train(addresses of the five calls, in the order above)
+PyObject *bind_train(PyObject *, PyObject *args) {
+    unsigned long long f[5];
+    if (!PyArg_ParseTuple(args, "KKKKK", f, f + 1, f + 2, f + 3, f + 4)) return nullptr;
+    g_attention = reinterpret_cast<decltype(g_attention)>(f[0]);
+    g_attention_backward = reinterpret_cast<decltype(g_attention_backward)>(f[1]);
+    g_rotate = reinterpret_cast<decltype(g_rotate)>(f[2]);
+    g_rotate_backward = reinterpret_cast<decltype(g_rotate_backward)>(f[3]);
+    g_clip = reinterpret_cast<decltype(g_clip)>(f[4]);
+    Py_RETURN_NONE;
+}
+
 // bind(address of hgf_linear_forward, address of hgf_linear_forward_ln): in the library that hgf.lib() has loaded
 PyObject *bind(PyObject *, PyObject *args) {
     unsigned long long forward, forward_ln;
@@ -307,6 +479,9 @@ PyMethodDef methods[] = {{"linear_forward", reinterpret_cast<PyCFunction>(reinte
                          HGF_CACHE_METHOD(cache_reserve), HGF_CACHE_METHOD(cache_append), HGF_CACHE_METHOD(cache_read), HGF_CACHE_METHOD(cache_fork),
                          HGF_CACHE_METHOD(cache_free), HGF_CACHE_METHOD(diff_attention_cached),
                          {"bind_cache", bind_cache, METH_VARARGS, nullptr},
+                         HGF_CACHE_METHOD(diff_attention_forward_train), HGF_CACHE_METHOD(diff_attention_backward), HGF_CACHE_METHOD(qk_norm_rotate),
+                         HGF_CACHE_METHOD(qk_norm_rotate_backward), HGF_CACHE_METHOD(clip_grad_norm),
+                         {"bind_train", bind_train, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hgf_python", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

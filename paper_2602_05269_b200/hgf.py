@@ -97,11 +97,12 @@ class FrontEnd(ctypes.Structure):
 _lib = None
 _native_forward = None  # linear_forward's marshalling (set with _lib; None: ctypes)
 _native_cache = None    # the native module, for the cache calls' (likewise)
+_native_train = None    # the same, for the training calls'
 
 
 def lib() -> ctypes.CDLL:
     """Load the CUDA library (built in-tree by paper_2602_05269_b200.build)."""
-    global _lib, _native_forward, _native_cache
+    global _lib, _native_forward, _native_cache, _native_train
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_2602_05269_b200.build` "
@@ -206,7 +207,9 @@ def lib() -> ctypes.CDLL:
             _native_forward = native.linear_forward
             native.bind_cache(*(c.cast(f, vp).value for f in (L.hgf_cache_reserve, L.hgf_cache_append, L.hgf_cache_read, L.hgf_cache_fork, L.hgf_cache_free,
                                                               L.hgf_diff_attention_cached)))
-            _native_cache = native
+            native.bind_train(*(c.cast(f, vp).value for f in (L.hgf_diff_attention_forward_train, L.hgf_diff_attention_backward, L.hgf_qk_norm_rotate,
+                                                              L.hgf_qk_norm_rotate_backward, L.hgf_clip_grad_norm)))
+            _native_cache = _native_train = native
         _lib = L
     return _lib
 
@@ -511,6 +514,10 @@ def diff_attention_forward_train(q, k, v, B: int, L: int, n_heads: int, head_dim
                                  out=None, streams=None, lse=None, flags: int = 0, stream=None):
     """hgf_diff_attention_forward_train: diff_attention_forward that keeps what diff_attention_backward needs.  Returns (out, streams, lse):
     streams bf16 [B*L][2*n_heads*head_dim], lse fp32 [B][n_heads][2][L]; all three are reused when given."""
+    if out is not None and streams is not None and lse is not None and _native_train and _done(
+            "hgf_diff_attention_forward_train",
+            _native_train.diff_attention_forward_train(q, k, v, B, L, n_heads, head_dim, lam, out_scale, out, streams, lse, flags, stream)):
+        return out, streams, lse
     width = _attention_inputs(q, k, v, B, L, n_heads, head_dim)
     dtype = torch.bfloat16 if flags & FLAG_OUT_BF16 else torch.float32
     with _on(stream):
@@ -535,6 +542,12 @@ def diff_attention_backward(q, k, v, dout, streams, lse, B: int, L: int, n_heads
     """hgf_diff_attention_backward: dout bf16 [B*L][n_heads*head_dim], streams and lse as diff_attention_forward_train left them.  Returns a dict of
     device tensors dq, dk, dv (bf16, as q, k, v) and dlambda (fp32 [1]); `want` restricts which are computed (dk and dv together, dlambda with dq
     only).  `out` (a dict returned by an earlier call of the same shape) and `workspace` are reused when given."""
+    if out is not None and want is None and _native_train:
+        ws = out.get("_workspace") if workspace is None else workspace
+        if ws is not None and _done("hgf_diff_attention_backward",
+                                    _native_train.diff_attention_backward(q, k, v, dout, streams, lse, B, L, n_heads, head_dim, lam, out_scale, out["dq"], out["dk"],
+                                                                          out["dv"], out["dlambda"], ws, stream)):
+            return {"dq": out["dq"], "dk": out["dk"], "dv": out["dv"], "dlambda": out["dlambda"], "_workspace": ws}
     width = _attention_inputs(q, k, v, B, L, n_heads, head_dim)
     _dense("dout", dout, torch.bfloat16, (B * L, width), q.device)
     _dense("streams", streams, torch.bfloat16, (B * L, 2 * width), q.device)
@@ -581,6 +594,10 @@ def qk_norm_rotate(q, k, positions, head_dim: int, wq=None, wk=None, *, eps: flo
     """hgf_qk_norm_rotate: the heads of q (bf16 [n_rows][heads * head_dim]) and k, each normalised, weighed by wq or wk (fp32 [head_dim], None: ones)
     and rotated by the row's position (int32 [n_rows]) -> (q_out, k_out), which may be q and k themselves.  q or k may be None.  rotary_dim: dims that
     are rotated (None: all).  FLAG_ROTATE_PAIRS: neighbouring dims are the pairs."""
+    rotary_dim = head_dim if rotary_dim is None else rotary_dim
+    if (q_out is not None or k_out is not None) and _native_train and _done(
+            "hgf_qk_norm_rotate", _native_train.qk_norm_rotate(q, k, positions, head_dim, wq, wk, eps, base, rotary_dim, flags, q_out, k_out, stream)):
+        return q_out, k_out
     device, rows, hq, hk = _rotate_inputs(q, k, positions, head_dim, wq, wk)
     with _on(stream):
         q_out = torch.empty_like(q) if q_out is None and q is not None else q_out
@@ -591,7 +608,7 @@ def qk_norm_rotate(q, k, positions, head_dim: int, wq=None, wk=None, *, eps: flo
             _dense(what, y, torch.bfloat16, x.shape, device)
     _check("hgf_qk_norm_rotate",
            lib().hgf_qk_norm_rotate(_ptr(q), _ptr(k), rows, hq, hk, head_dim, _ptr(positions), _ptr(wq), _ptr(wk), eps, base,
-                                    head_dim if rotary_dim is None else rotary_dim, _ptr(q_out), _ptr(k_out), flags, _stream(stream)))
+                                    rotary_dim, _ptr(q_out), _ptr(k_out), flags, _stream(stream)))
     return q_out, k_out
 
 
@@ -600,6 +617,16 @@ def qk_norm_rotate_backward(q, k, positions, head_dim: int, dq_out, dk_out, wq=N
     """hgf_qk_norm_rotate_backward: q, k as they went into qk_norm_rotate, dq_out and dk_out (bf16) the gradients of what came out.  Returns a dict of
     dq, dk (bf16) and dwq, dwk (fp32 [head_dim]) of the inputs that are given; `want` restricts which are computed.  `out` (a dict returned by an
     earlier call of the same shape, or tensors of the caller's: dq may be dq_out itself) and `workspace` are reused when given."""
+    rotary_dim = head_dim if rotary_dim is None else rotary_dim
+    if out is not None and want is None and _native_train:
+        ws = out.get("_workspace") if workspace is None else workspace
+        if ws is not None:
+            g = {n: out[n] for x, names in ((q, ("dq", "dwq")), (k, ("dk", "dwk"))) if x is not None for n in names}
+            if _done("hgf_qk_norm_rotate_backward",
+                     _native_train.qk_norm_rotate_backward(q, k, positions, head_dim, wq, wk, eps, base, rotary_dim, flags, dq_out, dk_out, g.get("dq"), g.get("dk"),
+                                                           g.get("dwq"), g.get("dwk"), ws, stream)):
+                g["_workspace"] = ws
+                return g
     device, rows, hq, hk = _rotate_inputs(q, k, positions, head_dim, wq, wk)
     like = {}
     for what, x, g in (("q", q, dq_out), ("k", k, dk_out)):
@@ -621,7 +648,7 @@ def qk_norm_rotate_backward(q, k, positions, head_dim: int, dq_out, dk_out, wq=N
     g = RotateGrads(*[out[n].data_ptr() if n in names else None for n in ("dq", "dk", "dwq", "dwk")])
     _check("hgf_qk_norm_rotate_backward",
            lib().hgf_qk_norm_rotate_backward(_ptr(q), _ptr(k), rows, hq, hk, head_dim, _ptr(positions), _ptr(wq), _ptr(wk), eps, base,
-                                             head_dim if rotary_dim is None else rotary_dim, _ptr(dq_out), _ptr(dk_out), ctypes.byref(g), _ptr(workspace),
+                                             rotary_dim, _ptr(dq_out), _ptr(dk_out), ctypes.byref(g), _ptr(workspace),
                                              workspace.numel(), flags, _stream(stream)))
     return {**{n: out[n] for n in names}, "_workspace": workspace}
 
@@ -650,6 +677,9 @@ class GradList:
     def clip(self, max_norm: float, *, norm=None, stream=None):
         """hgf_clip_grad_norm: scales the gradients so that their common norm is at most max_norm.  Returns the norm before that (fp32 [1] on the
         device, made here if not given)."""
+        if norm is not None and self._handle and _native_train and _done(
+                "hgf_clip_grad_norm", _native_train.clip_grad_norm(self._handle.value, self.device.index, max_norm, norm, stream)):
+            return norm
         _current_device(self.device)
         if norm is None:
             with _on(stream):

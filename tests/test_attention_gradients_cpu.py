@@ -79,6 +79,7 @@ def test_the_binding_refuses_what_does_not_fit(hgf, monkeypatch):
 
     library = Library()
     library.called = False
+    monkeypatch.setattr(hgf, "_native_train", None)
     monkeypatch.setattr(hgf, "lib", lambda: library)
     monkeypatch.setattr(hgf, "_stream", lambda s: None)
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731

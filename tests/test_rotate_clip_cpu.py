@@ -99,7 +99,7 @@ def test_the_binding_refuses_what_does_not_fit(hgf, monkeypatch):
             pass
 
     library, z = Library(), lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)
-    monkeypatch.setattr(hgf, "_native_cache", None)
+    monkeypatch.setattr(hgf, "_native_train", None)
     monkeypatch.setattr(hgf, "lib", lambda: library)
     monkeypatch.setattr(hgf, "_stream", lambda s: None)
     q, k, pos, w = z(5, 256), z(5, 128), z(5, dt=torch.int32), z(64, dt=torch.float32)
