@@ -672,23 +672,6 @@ constexpr int kTbMaxGrid = 1024;
 static size_t stats_bytes(int64_t B, int64_t L, int64_t h) { return (size_t)(B * h) * (size_t)((L + 63) / 64) * kTbStatBytes; }
 constexpr size_t kTbPartBytes = (size_t)kTbMaxGrid * TbCfg<64, true>::WARPS * sizeof(double);
 
-template <typename... F, typename... A>
-static cudaError_t launch_early(void (*kernel)(F...), unsigned grid, int threads, int smem, cudaStream_t stream, A... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, F(args)...);
-    if (e == cudaSuccess) count_launch();
-    return e;
-}
-
 template <int DH>
 static cudaError_t launch_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
                                    const hgf_attention_grads &grads, AttnBackParams p, void *workspace, cudaStream_t stream) {
@@ -714,10 +697,10 @@ static cudaError_t launch_backward(const void *q, const void *k, const void *v, 
     if (!make_maps(&keys, k, v, q, dout, DH, p) || !make_maps(&queries, q, dout, k, v, DH, p)) return cudaErrorInvalidValue;
     const TbPass of_keys = {(const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v, (__nv_bfloat16 *)grads.dk, (__nv_bfloat16 *)grads.dv};
     const TbPass of_queries = {(const __nv_bfloat16 *)q, (const __nv_bfloat16 *)dout, (__nv_bfloat16 *)grads.dq, nullptr};
-    e = launch_early(attention_stats_kernel<DH>, (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream, (const __nv_bfloat16 *)dout,
+    e = launch_overlapped(attention_stats_kernel<DH>, (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream, (const __nv_bfloat16 *)dout,
                      (const __nv_bfloat16 *)streams, lse, stats, p.arrivals, p.B, p.L, p.h, p.scale_log2);
     if (e != cudaSuccess) return e;
-    return launch_early(attention_backward_kernel<DH>, (unsigned)grid, TbCfg<DH, true>::THREADS, SMEM, stream, keys, queries, of_keys, of_queries, p, status);
+    return launch_overlapped(attention_backward_kernel<DH>, (unsigned)grid, TbCfg<DH, true>::THREADS, SMEM, stream, keys, queries, of_keys, of_queries, p, status);
 }
 
 }  // namespace hgf

@@ -41,6 +41,24 @@ static inline cudaError_t ensure_dynamic_smem(Kernel kernel, int bytes, std::ato
     return cudaSuccess;
 }
 
+// A launch whose blocks may start before the work in front of it on the stream has ended (the kernel waits for that itself: pdl_wait).
+template <typename... F, typename... A>
+static inline cudaError_t launch_overlapped(void (*kernel)(F...), unsigned grid, int threads, int smem, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, F(args)...);
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
+
 // ---- packed weight layout ---------------------------------------------------------------------
 // Tiles of 16 output rows x 256 input columns, 1 KiB each, row-major inside the tile (64 bytes per
 // row), tiles ordered with the column-tile index fastest.  d_in is padded to a multiple of 256 and

@@ -19,228 +19,296 @@ struct RotateSide {
 struct RotateParams {
     RotateSide side[2];
     const int32_t *pos;
-    float *part;              // (backward) [grid][2][dh] sums of the blocks, null: not asked for
-    int rows, rot, pairs, per_warp;  // per_warp: groups of heads that a warp takes, one after the other
+    float *part;              // (backward) [grid][dh] sums of the blocks, null: not asked for
+    int rows, rot, pairs, per_warp, q_blocks;  // per_warp: groups of heads that a warp takes, one after the other
     float eps;
     double turns[64];         // base^(-2 i / rot) / (2 pi)
 };
 
-// DH / 16 lanes share a head, each with two eights of its dims, so that both dims of a pair are one lane's: pairs (i, i + rot / 2) lie in
-// eights e and e + rot / 16, neighbours (2 i, 2 i + 1) in one.  In either case lane l has pairs 8 l .. 8 l + 7, if 8 l < rot / 2.
-template <int DH>
+// DH / 8 lanes share a head, eight neighbouring dims each, so that a warp's loads and stores are 512 consecutive bytes and a lane has few registers
+// and many loads in flight (a lane with both dims of its pairs, sixteen in all, needed twice the registers for the same bytes: 61 us instead of
+// 44 at 16384 tokens of 2 x 32 heads of 64; copying them takes 43).  The other dims of its pairs are in lane `source`, or with neighbouring
+// pairs its own, exchanged.  Values are kept two to a 64-bit register.
+struct Eight {
+    uint64_t v[4];
+};
+template <int DH, bool NEIGHBOURS>
 struct RotateLane {
-    static constexpr int LPH = DH / 16, HPW = 32 / LPH;  // lanes of a head, heads of a warp
-    int l, head, e0, e1;
-    bool turned, pairs;
-    float cosine[8], sine[8];
+    static constexpr int LPH = DH / 8, HPW = 32 / LPH;  // lanes of a head, heads of a warp
+    int l, head, source, index;                         // index: the first of the lane's pairs, -1: it turns by nothing
+    bool second;                                        // it has the second dims
 
-    __device__ __forceinline__ RotateLane(const RotateParams &p, int lane) {
+    __device__ __forceinline__ RotateLane(int rot, int lane) {
         l = lane % LPH;
         head = lane / LPH;
-        turned = l < p.rot / 16;
-        pairs = p.pairs != 0;
-        e0 = turned && !pairs ? l : 2 * l;
-        e1 = turned && !pairs ? l + p.rot / 16 : 2 * l + 1;
+        const int n = rot / 16;                         // lanes of the first dims
+        second = !NEIGHBOURS && l >= n;
+        source = NEIGHBOURS || l >= 2 * n ? lane : lane + (second ? -n : n);
+        index = l >= 2 * n ? -1 : NEIGHBOURS ? 4 * l : 8 * (second ? l - n : l);
     }
-    // The token's cosines and sines.  The angle is taken in turns and in 64 bits, its whole turns dropped: a far position loses no digits.
-    // A lane forms those of its own number (and 32 on), the lanes exchange them.
-    __device__ __forceinline__ void turn(const RotateParams &p, int pos, int lane) {
-        float c[LPH / 4], s[LPH / 4];
+    // Cosines and signed sines of the lane's dims: a dim turns forward into itself times `c` plus its partner times `s`.  The angle is taken in
+    // turns and in 64 bits, its whole turns dropped: a far position loses no digits.  A lane forms those of its own number (and 32 on).
+    __device__ __forceinline__ void turn(const RotateParams &p, int pos, int lane, float (&c)[8], float (&s)[8]) const {
+        float mc[DH / 64], ms[DH / 64];
 #pragma unroll
-        for (int n = 0; n < LPH / 4; ++n) {
+        for (int n = 0; n < DH / 64; ++n) {
             const int i = 32 * n + lane;
-            c[n] = 1.0f;
-            s[n] = 0.0f;
+            mc[n] = 1.0f;
+            ms[n] = 0.0f;
             if (2 * i < p.rot) {
                 const double t = (double)pos * p.turns[i];
-                sincospif(2.0f * (float)(t - rint(t)), &s[n], &c[n]);
+                sincospif(2.0f * (float)(t - rint(t)), &ms[n], &mc[n]);
             }
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int from = (8 * l + e) & 31;
-            cosine[e] = __shfl_sync(0xffffffffu, c[0], from);
-            sine[e] = __shfl_sync(0xffffffffu, s[0], from);
-            if constexpr (LPH == 8) {
-                const float c1 = __shfl_sync(0xffffffffu, c[1], from), s1 = __shfl_sync(0xffffffffu, s[1], from);
-                if (l >= 4) { cosine[e] = c1; sine[e] = s1; }
+        for (int e = 0; e < 8; e += NEIGHBOURS ? 2 : 1) {
+            const int i = (index < 0 ? 0 : index) + (NEIGHBOURS ? e / 2 : e);
+            c[e] = __shfl_sync(0xffffffffu, mc[0], i & 31);
+            s[e] = __shfl_sync(0xffffffffu, ms[0], i & 31);
+            if constexpr (DH == 128) {
+                const float c1 = __shfl_sync(0xffffffffu, mc[1], i & 31), s1 = __shfl_sync(0xffffffffu, ms[1], i & 31);
+                if (i >= 32) { c[e] = c1; s[e] = s1; }
             }
+            if (index < 0) { c[e] = 1.0f; s[e] = 0.0f; }
+            if (NEIGHBOURS) {
+                c[e + 1] = c[e];
+                s[e + 1] = s[e];
+                s[e] = -s[e];
+            } else if (!second) s[e] = -s[e];
         }
     }
-    // v[0..7] the dims of e0, v[8..15] those of e1; BACK: by the angles' negatives
-    template <bool BACK>
-    __device__ __forceinline__ void rotate(float (&v)[16]) const {
-        if (!turned) return;
-        auto two = [&](float &a, float &b, int i) {
-            const float s = BACK ? -sine[i] : sine[i], a0 = a;
-            a = a0 * cosine[i] - b * s;
-            b = a0 * s + b * cosine[i];
-        };
-        if (pairs) {
+    __device__ __forceinline__ Eight own(uint4 x) const {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        Eight r;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) two(v[2 * i], v[2 * i + 1], i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) two(v[i], v[8 + i], i);
-        }
+        for (int k = 0; k < 4; ++k) r.v[k] = pack_f32x2(bf16lo_to_float(w[k]), bf16hi_to_float(w[k]));
+        return r;
     }
-    __device__ __forceinline__ float head_sum(float v) const {
+    __device__ __forceinline__ Eight partner(uint4 x) const {
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        Eight r;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (!NEIGHBOURS) w[k] = __shfl_sync(0xffffffffu, w[k], source);
+            r.v[k] = NEIGHBOURS ? pack_f32x2(bf16hi_to_float(w[k]), bf16lo_to_float(w[k])) : pack_f32x2(bf16lo_to_float(w[k]), bf16hi_to_float(w[k]));
+        }
+        return r;
+    }
+    // Sum over a head of products of its values.
+    __device__ __forceinline__ float dot(const Eight &x, const Eight &y) const {
+        uint64_t a = mul_f32x2(x.v[0], y.v[0]), b = mul_f32x2(x.v[1], y.v[1]);
+        a = fma_f32x2(x.v[2], y.v[2], a);
+        b = fma_f32x2(x.v[3], y.v[3], b);
+        float lo, hi;
+        unpack_f32x2(add_f32x2(a, b), lo, hi);
+        float v = lo + hi;
 #pragma unroll
         for (int o = LPH / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         return v;
     }
-    __device__ __forceinline__ void load(const __nv_bfloat16 *head_at, float (&v)[16]) const {
-        const uint4 a = reinterpret_cast<const uint4 *>(head_at)[e0], b = reinterpret_cast<const uint4 *>(head_at)[e1];  // (the output may be the input)
-        const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    __device__ __forceinline__ void weights(const float *w, float (&own_w)[8]) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[2 * i] = bf16lo_to_float(x[i]);
-            v[2 * i + 1] = bf16hi_to_float(x[i]);
+        for (int e = 0; e < 8; e += 4) {
+            const float4 q = w ? __ldg(reinterpret_cast<const float4 *>(w + 8 * l + e)) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+            own_w[e] = q.x; own_w[e + 1] = q.y; own_w[e + 2] = q.z; own_w[e + 3] = q.w;
         }
-    }
-    __device__ __forceinline__ void store(__nv_bfloat16 *head_at, const float (&v)[16]) const {
-        uint32_t x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            x[i] = *reinterpret_cast<const uint32_t *>(&b);
-        }
-        reinterpret_cast<uint4 *>(head_at)[e0] = make_uint4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<uint4 *>(head_at)[e1] = make_uint4(x[4], x[5], x[6], x[7]);
-    }
-    __device__ __forceinline__ void weights(const float *w, float (&v)[16]) const {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = w ? __ldg(w + 8 * (i < 8 ? e0 : e1) + (i & 7)) : 1.0f;
     }
 };
+__device__ __forceinline__ uint4 rotate_words(const Eight &r) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float lo, hi;
+        unpack_f32x2(r.v[k], lo, hi);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+        w[k] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 
-constexpr int kRotateThreads = 256;
+constexpr int kRotateThreads = 256, kRotateAhead = 4, kRotateBlocks = 4, kRotateMost = 8, kRotateBack = 4, kRotateBackBlocks = 2;
 
-// A warp takes `per_warp` neighbouring groups of HPW heads of one token; Q's groups come before K's.
-template <int DH>
-__global__ void __launch_bounds__(kRotateThreads)
+// A warp takes `per_warp` neighbouring groups of HPW heads of one token in Q or K, kRotateAhead of them asked for at once.
+template <int DH, bool NEIGHBOURS>
+__global__ void __launch_bounds__(kRotateThreads, kRotateBlocks)
 qk_norm_rotate_kernel(const __grid_constant__ RotateParams p) {
-    using R = RotateLane<DH>;
+    using R = RotateLane<DH, NEIGHBOURS>;
     const int lane = threadIdx.x & 31;
-    R r(p, lane);
-    const int gq = (p.side[0].heads + R::HPW - 1) / R::HPW, groups = gq + (p.side[1].heads + R::HPW - 1) / R::HPW;
-    const int parts = (groups + p.per_warp - 1) / p.per_warp;
+    const int gq = (p.side[0].heads + R::HPW - 1) / R::HPW, gk = (p.side[1].heads + R::HPW - 1) / R::HPW;
+    const int pq = (gq + p.per_warp - 1) / p.per_warp, parts = pq + (gk + p.per_warp - 1) / p.per_warp;
     const long long unit = (long long)blockIdx.x * (kRotateThreads / 32) + (threadIdx.x >> 5);
-    const long long row = unit / parts;
+    const int row = (int)(unit / parts), part = (int)(unit - (long long)row * parts);
     if (row >= p.rows) return;
-    const int first = (int)(unit % parts) * p.per_warp, last = min(first + p.per_warp, groups);
-    r.turn(p, __ldg(p.pos + row), lane);
-    float w[16];
-    int side = -1;
-    for (int grp = first; grp < last; ++grp) {
-        const int s = grp >= gq;
-        const RotateSide &a = p.side[s];
-        if (s != side) {
-            r.weights(a.w, w);
-            side = s;
+    const RotateSide &a = p.side[part >= pq];
+    int grp = (part >= pq ? part - pq : part) * p.per_warp;
+    const int end = min(grp + p.per_warp, part >= pq ? gk : gq), words = a.heads * (DH / 8);
+    const R r(p.rot, lane);
+    const uint4 *x = reinterpret_cast<const uint4 *>(a.x + (size_t)row * a.heads * DH);
+    uint4 *y = reinterpret_cast<uint4 *>(a.out + (size_t)row * a.heads * DH);
+    uint4 raw[kRotateAhead];
+    // (a lane whose head is behind the last reads the last word instead, and stores nothing; plain loads: the output may be the input)
+    auto ask = [&](int from) {
+#pragma unroll
+        for (int u = 0; u < kRotateAhead; ++u)
+            if (from + u < end) raw[u] = x[min(32 * (from + u) + lane, words - 1)];
+    };
+    ask(grp);
+    Eight P, Q;  // a dim becomes n (itself times P plus its partner times Q), with the weights in the factors
+    {
+        float c[8], sn[8], w[8];
+        r.turn(p, __ldg(p.pos + row), lane, c, sn);
+        r.weights(a.w, w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float w0, w1;
+            if (NEIGHBOURS) { w0 = w[2 * k + 1]; w1 = w[2 * k]; }
+            else {
+                w0 = __shfl_sync(0xffffffffu, w[2 * k], r.source);
+                w1 = __shfl_sync(0xffffffffu, w[2 * k + 1], r.source);
+            }
+            P.v[k] = pack_f32x2(w[2 * k] * c[2 * k], w[2 * k + 1] * c[2 * k + 1]);
+            Q.v[k] = pack_f32x2(w0 * sn[2 * k], w1 * sn[2 * k + 1]);
         }
-        const int head = (grp - (s ? gq : 0)) * R::HPW + r.head;
-        const bool there = head < a.heads;
-        const size_t at = ((size_t)row * a.heads + (there ? head : 0)) * DH;
-        float v[16], sum = 0.0f;
-        r.load(a.x + at, v);
+    }
+    for (;;) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
-        const float n = rsqrtf(r.head_sum(sum) * (1.0f / DH) + p.eps);
+        for (int u = 0; u < kRotateAhead; ++u) {
+            if (grp + u >= end) break;
+            Eight v = r.own(raw[u]);
+            const Eight o = r.partner(raw[u]);
+            const float n = rsqrtf(r.dot(v, v) * (1.0f / DH) + p.eps);
+            const uint64_t n2 = pack_f32x2(n, n);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = v[i] * n * w[i];
-        r.template rotate<false>(v);
-        if (there) r.store(a.out + at, v);
+            for (int k = 0; k < 4; ++k) v.v[k] = mul_f32x2(fma_f32x2(v.v[k], P.v[k], mul_f32x2(o.v[k], Q.v[k])), n2);
+            if (32 * (grp + u) + lane < words) y[32 * (grp + u) + lane] = rotate_words(v);
+        }
+        if ((grp += kRotateAhead) >= end) break;
+        ask(grp);
     }
 }
 
-template <int DH>
-__global__ void __launch_bounds__(kRotateThreads)
+// The same the other way round; the first p.q_blocks blocks take Q, the others K, a warp every `warps`-th unit, kRotateBack groups
+// at a time.  What a lane turns by waits in shared memory: with it in registers two groups at a time is all that fits without spills, 91 us instead of
+// 77 at 16384 tokens of 2 x 32 heads of 64 (403 MB, 62 at the rate of a copy); three blocks an SM spill: 100.
+template <int DH, bool NEIGHBOURS>
+__global__ void __launch_bounds__(kRotateThreads, kRotateBackBlocks)
 qk_norm_rotate_backward_kernel(const __grid_constant__ RotateParams p) {
-    using R = RotateLane<DH>;
+    using R = RotateLane<DH, NEIGHBOURS>;
     __shared__ float s_dw[kRotateThreads / 32][DH];
+    __shared__ ulonglong2 s_turn[kRotateThreads / 32][4][32];  // cosines, sines
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    R r(p, lane);
-    const long long warps = (long long)gridDim.x * (kRotateThreads / 32), me = (long long)blockIdx.x * (kRotateThreads / 32) + warp;
-#pragma unroll 1
-    for (int s = 0; s < 2; ++s) {
-        const RotateSide &a = p.side[s];
-        const int groups = (a.heads + R::HPW - 1) / R::HPW, parts = (groups + p.per_warp - 1) / p.per_warp;
-        float dw[16] = {}, w[16];
-        r.weights(a.w, w);
-        for (long long unit = me; unit < (long long)p.rows * parts; unit += warps) {
-            const long long row = unit / parts;
-            const int first = (int)(unit % parts) * p.per_warp, last = min(first + p.per_warp, groups);
-            r.turn(p, __ldg(p.pos + row), lane);
-            for (int grp = first; grp < last; ++grp) {
-                const int head = grp * R::HPW + r.head;
-                const bool there = head < a.heads;
-                const size_t at = ((size_t)row * a.heads + (there ? head : 0)) * DH;
-                float x[16], g[16], sum = 0.0f, mean = 0.0f;
-                r.load(a.x + at, x);
-                r.load(a.dy + at, g);
+    const bool of_k = (int)blockIdx.x >= p.q_blocks;
+    const int blocks = of_k ? (int)gridDim.x - p.q_blocks : p.q_blocks, block = (int)blockIdx.x - (of_k ? p.q_blocks : 0);
+    const int warps = blocks * (kRotateThreads / 32), me = block * (kRotateThreads / 32) + warp;
+    const R r(p.rot, lane);
+    pdl_launch_dependents();
+    const RotateSide &a = p.side[of_k];
+    const int groups = (a.heads + R::HPW - 1) / R::HPW, parts = (groups + p.per_warp - 1) / p.per_warp, words = a.heads * (DH / 8);
+    const long long units = (long long)p.rows * parts;
+    Eight dw = {}, w;
+    {
+        float f[8];
+        r.weights(a.w, f);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum = fmaf(x[i], x[i], sum);
-                const float n = rsqrtf(r.head_sum(sum) * (1.0f / DH) + p.eps);
-                r.template rotate<true>(g);
+        for (int k = 0; k < 4; ++k) w.v[k] = pack_f32x2(f[2 * k], f[2 * k + 1]);
+    }
+    int turned = -1;
+    for (long long unit = me; unit < units; unit += warps) {
+        const int row = (int)(unit / parts);
+        int grp = (int)(unit - (long long)row * parts) * p.per_warp;
+        const int last = min(grp + p.per_warp, groups);
+        const size_t at = (size_t)row * a.heads * DH;
+        const uint4 *x = reinterpret_cast<const uint4 *>(a.x + at), *dy = reinterpret_cast<const uint4 *>(a.dy + at);
+        uint4 *dx = reinterpret_cast<uint4 *>(a.out + at);
+        for (; grp < last; grp += kRotateBack) {
+            uint4 rx[kRotateBack], rg[kRotateBack];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    x[i] *= n;
-                    if (there) dw[i] = fmaf(g[i], x[i], dw[i]);
-                    g[i] *= w[i];
-                    mean = fmaf(g[i], x[i], mean);
+            for (int u = 0; u < kRotateBack; ++u)
+                {
+                    const int word = min(32 * min(grp + u, last - 1) + lane, words - 1);
+                    rx[u] = x[word];
+                    rg[u] = dy[word];
                 }
-                mean = r.head_sum(mean) * (1.0f / DH);
+            if (row != turned) {
+                float c[8], sn[8];
+                r.turn(p, __ldg(p.pos + row), lane, c, sn);
+                turned = row;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) g[i] = n * fmaf(-x[i], mean, g[i]);
-                if (there && a.out) r.store(a.out + at, g);
+                for (int k = 0; k < 2; ++k) {  // (a lane reads what it wrote)
+                    s_turn[warp][k][lane] = make_ulonglong2(pack_f32x2(c[4 * k], c[4 * k + 1]), pack_f32x2(c[4 * k + 2], c[4 * k + 3]));
+                    s_turn[warp][2 + k][lane] = make_ulonglong2(pack_f32x2(-sn[4 * k], -sn[4 * k + 1]), pack_f32x2(-sn[4 * k + 2], -sn[4 * k + 3]));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kRotateBack; ++u) {
+                const int word = grp + u < last ? 32 * (grp + u) + lane : words;  // (no branch: groups' chains of latencies run side by side)
+                Eight v = r.own(rx[u]), g = r.own(rg[u]);
+                const Eight o = r.partner(rg[u]);
+                const float n = rsqrtf(r.dot(v, v) * (1.0f / DH) + p.eps);
+                const uint64_t n2 = pack_f32x2(n, n);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const ulonglong2 cc = s_turn[warp][k >> 1][lane], ss = s_turn[warp][2 + (k >> 1)][lane];
+                    v.v[k] = mul_f32x2(v.v[k], n2);
+                    g.v[k] = fma_f32x2(g.v[k], k & 1 ? cc.y : cc.x, mul_f32x2(o.v[k], k & 1 ? ss.y : ss.x));
+                    if (word < words) dw.v[k] = fma_f32x2(g.v[k], v.v[k], dw.v[k]);
+                    g.v[k] = mul_f32x2(g.v[k], w.v[k]);
+                }
+                const float mean = r.dot(g, v) * (-1.0f / DH);
+                const uint64_t m2 = pack_f32x2(mean, mean);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) g.v[k] = mul_f32x2(fma_f32x2(v.v[k], m2, g.v[k]), n2);
+                if (word < words && a.out) dx[word] = rotate_words(g);
             }
         }
-        if (!p.part) continue;
-        // the block's sum for each dim, in one order: over the heads of a warp, then over the warps
+    }
+    if (!p.part) return;
+    // the block's sum for each dim, in one order: over the heads of a warp, then over the warps
+    float f[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+    for (int k = 0; k < 4; ++k) unpack_f32x2(dw.v[k], f[2 * k], f[2 * k + 1]);
 #pragma unroll
-            for (int o = 16; o >= R::LPH; o >>= 1) dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
-        if (lane < R::LPH)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s_dw[warp][8 * (i < 8 ? r.e0 : r.e1) + (i & 7)] = dw[i];
-        __syncthreads();
-        if (threadIdx.x < DH) {
-            float v = 0.0f;
+        for (int o = 16; o >= R::LPH; o >>= 1) f[i] += __shfl_xor_sync(0xffffffffu, f[i], o);
+    if (lane < R::LPH)
 #pragma unroll
-            for (int q = 0; q < kRotateThreads / 32; ++q) v += s_dw[q][threadIdx.x];
-            p.part[((size_t)blockIdx.x * 2 + s) * DH + threadIdx.x] = v;
-        }
-        __syncthreads();
+        for (int i = 0; i < 8; ++i) s_dw[warp][8 * lane + i] = f[i];
+    __syncthreads();
+    if (threadIdx.x < DH) {
+        float v = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kRotateThreads / 32; ++q) v += s_dw[q][threadIdx.x];
+        p.part[(size_t)blockIdx.x * DH + threadIdx.x] = v;
     }
 }
 
-// The blocks' sums added up, in 64 bits: a block takes 32 dims of a side, its warps every eighth block's sums.
-__global__ void __launch_bounds__(256) rotate_weight_sums_kernel(const float *part, int n, int dh, float *dwq, float *dwk) {
-    __shared__ double s_sum[8][32];
+// The blocks' sums added up, in 64 bits: a block takes 32 dims of a side, a warp every 32nd block's sums, in one order.
+__global__ void __launch_bounds__(1024) rotate_weight_sums_kernel(const float *part, int q_blocks, int blocks, int dh, float *dwq, float *dwk) {
+    __shared__ double s_sum[32][33];
     const int per_side = dh / 32, s = blockIdx.x / per_side, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, dim = (blockIdx.x % per_side) * 32 + lane;
     float *out = s ? dwk : dwq;
+    pdl_wait();
     if (!out) return;
     double v = 0.0;
-    for (int i = warp; i < n; i += 8) v += part[((size_t)i * 2 + s) * dh + dim];
-    s_sum[warp][lane] = v;
+#pragma unroll 8
+    for (int i = (s ? q_blocks : 0) + warp; i < (s ? blocks : q_blocks); i += 32) v += part[(size_t)i * dh + dim];
+    s_sum[lane][warp] = v;
     __syncthreads();
-    if (warp == 0) {
-        for (int q = 1; q < 8; ++q) v += s_sum[q][lane];
-        out[dim] = (float)v;
-    }
+    v = s_sum[warp][lane];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane == 0) out[(blockIdx.x % per_side) * 32 + warp] = (float)v;
 }
 
 constexpr int kRotateMaxGrid = 1024;
 
-static void rotate_plan(RotateParams &p, int dh, double base, int sms) {
+static void rotate_plan(RotateParams &p, int groups, double base, int sms) {
     for (int i = 0; i < p.rot / 2; ++i) p.turns[i] = pow(base, -2.0 * i / p.rot) / 6.283185307179586476925286766559;
-    // few tokens: a warp a group of heads; many: up to eight, so that a token's angles are formed rarely
-    const int hpw = 32 / (dh / 16), groups = (p.side[0].heads + hpw - 1) / hpw + (p.side[1].heads + hpw - 1) / hpw;
-    const long long all = (long long)p.rows * groups, want = (long long)sms * 32;
+    // few tokens: a warp a group of heads; many: as many as a warp takes, so that a token's angles are formed rarely
+    const long long all = (long long)p.rows * groups, want = (long long)sms * 16;
     p.per_warp = 1;
-    while (p.per_warp < 8 && p.per_warp < groups && all / (2 * p.per_warp) >= want) p.per_warp *= 2;
+    while (p.per_warp < kRotateMost && p.per_warp < groups && all / (2 * p.per_warp) >= want) p.per_warp *= 2;
 }
 
 static hgf_status rotate_arguments(RotateParams &p, const void *q, const void *k, int64_t n_rows, int32_t q_heads, int32_t k_heads, int32_t head_dim,
@@ -282,18 +350,19 @@ extern "C" hgf_status hgf_qk_norm_rotate(const void *q, const void *k, int64_t n
     p.side[1].out = (__nv_bfloat16 *)k_out;
     const int sms = device_sm_count();
     if (!sms) return HGF_ERR_CUDA;
-    rotate_plan(p, head_dim, base, sms);
-    const int hpw = 32 / (head_dim / 16), groups = (p.side[0].heads + hpw - 1) / hpw + (p.side[1].heads + hpw - 1) / hpw;
-    const long long units = (long long)p.rows * ((groups + p.per_warp - 1) / p.per_warp), blocks = (units + kRotateThreads / 32 - 1) / (kRotateThreads / 32);
+    const int hpw = 32 / (head_dim / 8), gq = (p.side[0].heads + hpw - 1) / hpw, gk = (p.side[1].heads + hpw - 1) / hpw;
+    rotate_plan(p, gq + gk, base, sms);
+    const long long units = (long long)p.rows * ((gq + p.per_warp - 1) / p.per_warp + (gk + p.per_warp - 1) / p.per_warp), blocks = (units + kRotateThreads / 32 - 1) / (kRotateThreads / 32);
     if (blocks > 0x7fffffffll) return HGF_ERR_UNSUPPORTED_SHAPE;
-    if (head_dim == 64) qk_norm_rotate_kernel<64><<<(unsigned)blocks, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
-    else qk_norm_rotate_kernel<128><<<(unsigned)blocks, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
+    auto *kernel = head_dim == 64 ? (p.pairs ? qk_norm_rotate_kernel<64, true> : qk_norm_rotate_kernel<64, false>)
+                                  : (p.pairs ? qk_norm_rotate_kernel<128, true> : qk_norm_rotate_kernel<128, false>);
+    kernel<<<(unsigned)blocks, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
     count_launch();
     return cudaGetLastError() == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
 }
 
 extern "C" size_t hgf_qk_norm_rotate_workspace_bytes(int32_t head_dim) {
-    return head_dim == 64 || head_dim == 128 ? (size_t)kRotateMaxGrid * 2 * head_dim * sizeof(float) : 0;
+    return head_dim == 64 || head_dim == 128 ? (size_t)kRotateMaxGrid * head_dim * sizeof(float) : 0;
 }
 
 extern "C" hgf_status hgf_qk_norm_rotate_backward(const void *q, const void *k, int64_t n_rows, int32_t q_heads, int32_t k_heads, int32_t head_dim,
@@ -312,27 +381,33 @@ extern "C" hgf_status hgf_qk_norm_rotate_backward(const void *q, const void *k, 
         if ((uintptr_t)workspace & 255u) return HGF_ERR_MISALIGNED;
         p.part = (float *)workspace;
     }
-    if (!grads->dq && !grads->dwq) p.side[0].heads = 0;
-    if (!grads->dk && !grads->dwk) p.side[1].heads = 0;
-    if (!p.side[0].heads && !p.side[1].heads) return HGF_OK;
+    const bool of_q = grads->dq || grads->dwq, of_k = grads->dk || grads->dwk;
+    if (!of_q && !of_k) return HGF_OK;
     p.side[0].dy = (const __nv_bfloat16 *)dq_out;
     p.side[1].dy = (const __nv_bfloat16 *)dk_out;
     p.side[0].out = (__nv_bfloat16 *)grads->dq;
     p.side[1].out = (__nv_bfloat16 *)grads->dk;
     const int sms = device_sm_count();
     if (!sms) return HGF_ERR_CUDA;
-    rotate_plan(p, head_dim, base, sms);
-    const int hpw = 32 / (head_dim / 16), most = p.side[0].heads > p.side[1].heads ? p.side[0].heads : p.side[1].heads, groups = (most + hpw - 1) / hpw;
-    const long long units = (long long)p.rows * ((groups + p.per_warp - 1) / p.per_warp), blocks = (units + kRotateThreads / 32 - 1) / (kRotateThreads / 32);
-    const int cap = 2 * sms < kRotateMaxGrid ? 2 * sms : kRotateMaxGrid, grid = blocks < cap ? (int)blocks : cap;
-    if (head_dim == 64) qk_norm_rotate_backward_kernel<64><<<grid, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
-    else qk_norm_rotate_backward_kernel<128><<<grid, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
+    // as many blocks as run at once, shared out to Q and K by their heads, fewer where there is less to do; a side that is not asked for has none, and
+    // the other's stay as they are, so that its sums do
+    const int hpw = 32 / (head_dim / 8), gq = (p.side[0].heads + hpw - 1) / hpw, gk = (p.side[1].heads + hpw - 1) / hpw;
+    rotate_plan(p, gq + gk, base, sms);
+    auto blocks_of = [&](int groups) { return ((long long)p.rows * ((groups + p.per_warp - 1) / p.per_warp) + kRotateThreads / 32 - 1) / (kRotateThreads / 32); };
+    const int cap = kRotateBackBlocks * sms < kRotateMaxGrid ? kRotateBackBlocks * sms : kRotateMaxGrid;
+    int q_most = (int)((long long)cap * gq / (gq + gk));
+    q_most = !gq ? 0 : !gk ? cap : q_most < 1 ? 1 : q_most >= cap ? cap - 1 : q_most;
+    const long long bq = blocks_of(gq), bk = blocks_of(gk);
+    p.q_blocks = !of_q ? 0 : bq < q_most ? (int)bq : q_most;
+    const int grid = p.q_blocks + (!of_k ? 0 : bk < cap - q_most ? (int)bk : cap - q_most);
+    auto *kernel = head_dim == 64 ? (p.pairs ? qk_norm_rotate_backward_kernel<64, true> : qk_norm_rotate_backward_kernel<64, false>)
+                                  : (p.pairs ? qk_norm_rotate_backward_kernel<128, true> : qk_norm_rotate_backward_kernel<128, false>);
+    kernel<<<grid, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
     count_launch();
     if (cudaGetLastError() != cudaSuccess) return HGF_ERR_CUDA;
     if (p.part) {
-        rotate_weight_sums_kernel<<<2 * head_dim / 32, 256, 0, (cudaStream_t)stream>>>(p.part, grid, head_dim, grads->dwq, grads->dwk);
-        count_launch();
-        if (cudaGetLastError() != cudaSuccess) return HGF_ERR_CUDA;
+        if (launch_overlapped(rotate_weight_sums_kernel, 2u * head_dim / 32, 1024, 0, (cudaStream_t)stream, (const float *)p.part, p.q_blocks, grid, (int)head_dim, grads->dwq, grads->dwk) != cudaSuccess)
+            return HGF_ERR_CUDA;
     }
     return HGF_OK;
 }

@@ -119,7 +119,7 @@ def test_in_place_and_equal_bits(hgf, dh):
     s = inputs(300, 6, 10, dh, seed=7)
     one = hgf.qk_norm_rotate(s["q"], s["k"], s["pos"], dh, s["wq"], s["wk"])
     g = hgf.qk_norm_rotate_backward(s["q"], s["k"], s["pos"], dh, s["gq"], s["gk"], s["wq"], s["wk"])
-    ws = torch.full((1 << 21,), 255, dtype=torch.uint8, device="cuda")
+    ws = torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda")
     for want in (None, ("dq",), ("dwk",), ("dk", "dwq"), ()):
         part = hgf.qk_norm_rotate_backward(s["q"], s["k"], s["pos"], dh, s["gq"], s["gk"], s["wq"], s["wk"], want=want, workspace=ws)
         assert set(part) - {"_workspace"} == set(("dq", "dk", "dwq", "dwk") if want is None else want)
