@@ -18,19 +18,18 @@ struct alignas(32) ClipPiece {
     int bf16, vx, vy;    // x (and y) in 16-byte words
 };
 
-constexpr int kClipThreads = 256, kClipWarps = kClipThreads / 32, kClipBytes = 16384;
+constexpr int kClipThreads = 256, kClipWarps = kClipThreads / 32, kClipAhead = 2, kClipLeast = 1024, kClipMost = 8192, kClipBlocks = 8;
 
-__device__ __forceinline__ double square_sum(uint4 v, int bf16) {
+template <bool BF16>
+__device__ __forceinline__ double square_sum(uint4 v, double s) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    double s = 0.0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (bf16) {
-            const double a = bf16lo_to_float(w[i]), b = bf16hi_to_float(w[i]);
-            s = fma(a, a, fma(b, b, s));
-        } else {
-            const double a = __uint_as_float(w[i]);
-            s = fma(a, a, s);
+        const double a = BF16 ? bf16lo_to_float(w[i]) : __uint_as_float(w[i]);
+        s = fma(a, a, s);
+        if (BF16) {
+            const double b = bf16hi_to_float(w[i]);
+            s = fma(b, b, s);
         }
     }
     return s;
@@ -39,31 +38,46 @@ __device__ __forceinline__ float clip_element(const ClipPiece &c, int i) {
     return c.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(c.x)[i]) : static_cast<const float *>(c.x)[i];
 }
 
-// Sums of squares in 64 bits: no magnitude of a gradient overflows or vanishes, and the order moves nothing that fp32 shows.
+// Sums of squares in 64 bits: no magnitude of a gradient overflows or vanishes, and the order moves nothing that fp32 shows.  A sum for each of the
+// words in flight: one chain of additions for all of them was the bound (421 MB 114 us instead of SUMS_US).
+template <bool BF16>
+__device__ __forceinline__ void piece_sums(const ClipPiece &c, int lane, double (&sum)[kClipAhead]) {
+    int at = 0;
+    if (c.vx) {
+        const int per = BF16 ? 8 : 4, words = c.n / per;
+        const uint4 *x = static_cast<const uint4 *>(c.x);
+        for (int j = lane; j < words; j += 32 * kClipAhead) {
+            uint4 v[kClipAhead];
+#pragma unroll
+            for (int u = 0; u < kClipAhead; ++u) v[u] = j + 32 * u < words ? x[j + 32 * u] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int u = 0; u < kClipAhead; ++u) sum[u] = square_sum<BF16>(v[u], sum[u]);
+        }
+        at = words * per;
+    }
+    for (int j = at + lane; j < c.n; j += 32) {
+        const double a = clip_element(c, j);
+        sum[0] = fma(a, a, sum[0]);
+    }
+}
 __global__ void __launch_bounds__(kClipThreads) clip_sums_kernel(const ClipPiece *pieces, int n, double *part) {
     __shared__ double s_sum[kClipWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = gridDim.x * kClipWarps;
-    double sum = 0.0;
-    for (int i = blockIdx.x * kClipWarps + warp; i < n; i += warps) {
-        const ClipPiece c = pieces[i];
-        int at = 0;
-        if (c.vx) {
-            const int per = c.bf16 ? 8 : 4, words = c.n / per;
-            const uint4 *x = static_cast<const uint4 *>(c.x);
-            for (int j = lane; j < words; j += 128) {
-                uint4 v[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = j + 32 * u < words ? x[j + 32 * u] : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) sum += square_sum(v[u], c.bf16);
-            }
-            at = words * per;
-        }
-        for (int j = at + lane; j < c.n; j += 32) {
-            const double a = clip_element(c, j);
-            sum = fma(a, a, sum);
-        }
+    int i = blockIdx.x * kClipWarps + warp;
+    ClipPiece c = {};
+    if (i < n) c = pieces[i];  // (the list's own memory, written when it was made)
+    pdl_launch_dependents();
+    pdl_wait();
+    double sums[kClipAhead] = {};
+    while (i < n) {
+        const ClipPiece now = c;
+        if ((i += warps) < n) c = pieces[i];
+        if (now.bf16) piece_sums<true>(now, lane, sums);
+        else piece_sums<false>(now, lane, sums);
     }
+    double sum = 0.0;
+#pragma unroll
+    for (int u = 0; u < kClipAhead; ++u) sum += sums[u];
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
@@ -74,17 +88,48 @@ __global__ void __launch_bounds__(kClipThreads) clip_sums_kernel(const ClipPiece
     }
 }
 
-__device__ __forceinline__ uint32_t scaled_word(uint32_t w, float f, int bf16) {
-    if (!bf16) return __float_as_uint(__uint_as_float(w) * f);
+template <bool BF16>
+__device__ __forceinline__ uint32_t scaled_word(uint32_t w, float f) {
+    if (!BF16) return __float_as_uint(__uint_as_float(w) * f);
     const __nv_bfloat162 b = __floats2bfloat162_rn(bf16lo_to_float(w) * f, bf16hi_to_float(w) * f);
     return *reinterpret_cast<const uint32_t *>(&b);
+}
+template <bool BF16>
+__device__ __forceinline__ void piece_scaled(const ClipPiece &c, int lane, float f) {
+    int at = 0;
+    if (c.vx && c.vy) {
+        const int per = BF16 ? 8 : 4, words = c.n / per;
+        const uint4 *x = static_cast<const uint4 *>(c.x);
+        uint4 *y = static_cast<uint4 *>(c.y);
+        for (int j = lane; j < words; j += 32 * kClipAhead) {
+            uint4 v[kClipAhead];
+#pragma unroll
+            for (int u = 0; u < kClipAhead; ++u)
+                if (j + 32 * u < words) v[u] = x[j + 32 * u];
+#pragma unroll
+            for (int u = 0; u < kClipAhead; ++u)
+                if (j + 32 * u < words)
+                    y[j + 32 * u] = make_uint4(scaled_word<BF16>(v[u].x, f), scaled_word<BF16>(v[u].y, f), scaled_word<BF16>(v[u].z, f), scaled_word<BF16>(v[u].w, f));
+        }
+        at = words * per;
+    }
+    for (int j = at + lane; j < c.n; j += 32) {
+        const float v = clip_element(c, j) * f;
+        if (BF16) static_cast<__nv_bfloat16 *>(c.y)[j] = __float2bfloat16_rn(v);
+        else static_cast<float *>(c.y)[j] = v;
+    }
 }
 
 __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipPiece *pieces, int n, const double *part, int n_part, float max_norm, float *norm_out) {
     __shared__ double s_sum[kClipWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = gridDim.x * kClipWarps;
+    // backwards: the pieces that were read last may still be in the L2 cache
+    int i = n - 1 - (int)(blockIdx.x * kClipWarps + warp);
+    ClipPiece c = {};
+    if (i >= 0) c = pieces[i];
+    pdl_wait();
     double sum = 0.0;
-    for (int i = threadIdx.x; i < n_part; i += kClipThreads) sum += part[i];
+    for (int k = threadIdx.x; k < n_part; k += kClipThreads) sum += part[k];
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
@@ -94,32 +139,12 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipPiec
     const double norm = sqrt(sum), ratio = (double)max_norm / (norm + 1e-6);
     const float f = ratio >= 1.0 ? 1.0f : (float)ratio;  // (a norm that is no number gives a factor that is none)
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-    // backwards: the pieces that were read last may still be in the L2 cache
-    for (int i = n - 1 - (blockIdx.x * kClipWarps + warp); i >= 0; i -= warps) {
-        const ClipPiece c = pieces[i];
-        if (f == 1.0f && c.x == c.y) continue;
-        int at = 0;
-        if (c.vx && c.vy) {
-            const int per = c.bf16 ? 8 : 4, words = c.n / per;
-            const uint4 *x = static_cast<const uint4 *>(c.x);
-            uint4 *y = static_cast<uint4 *>(c.y);
-            for (int j = lane; j < words; j += 128) {
-                uint4 v[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (j + 32 * u < words) v[u] = x[j + 32 * u];
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (j + 32 * u < words)
-                        y[j + 32 * u] = make_uint4(scaled_word(v[u].x, f, c.bf16), scaled_word(v[u].y, f, c.bf16), scaled_word(v[u].z, f, c.bf16), scaled_word(v[u].w, f, c.bf16));
-            }
-            at = words * per;
-        }
-        for (int j = at + lane; j < c.n; j += 32) {
-            const float v = clip_element(c, j) * f;
-            if (c.bf16) static_cast<__nv_bfloat16 *>(c.y)[j] = __float2bfloat16_rn(v);
-            else static_cast<float *>(c.y)[j] = v;
-        }
+    while (i >= 0) {
+        const ClipPiece now = c;
+        if ((i -= warps) >= 0) c = pieces[i];
+        if (f == 1.0f && now.x == now.y) continue;
+        if (now.bf16) piece_scaled<true>(now, lane, f);
+        else piece_scaled<false>(now, lane, f);
     }
 }
 
@@ -159,21 +184,25 @@ extern "C" hgf_status hgf_grad_list_create(const hgf_tensor *tensors, int32_t n,
         for (; y != ys.end() && y->begin < end; ++y)
             if (y->tensor != i || y->begin != begin) return HGF_ERR_INVALID_ARG;
     }
+    const int sms = device_sm_count(), dev = current_device();
+    if (!sms || dev < 0) return HGF_ERR_CUDA;
+    // Pieces: at least one for every warp that runs at once where that leaves 1 KB to each, up to 8 KB
+    int64_t bytes = 0;
+    for (const Range &y : ys) bytes += (int64_t)(y.end - y.begin);
+    const int64_t share = bytes / ((int64_t)sms * kClipBlocks * kClipWarps) / kClipLeast * kClipLeast, piece = share < kClipLeast ? kClipLeast : share < kClipMost ? share : kClipMost;
     for (int32_t i = 0; i < n; ++i) {
         const hgf_tensor &t = tensors[i];
         const int size = t.type == HGF_BF16 ? 2 : 4;
         for (int64_t at = 0; at < t.n;) {
             const uintptr_t x = (uintptr_t)t.x + at * size, y = (uintptr_t)t.y + at * size;
-            const int64_t most = x & 15 ? (int64_t)(16 - (x & 15)) / size : kClipBytes / size, len = most < t.n - at ? most : t.n - at;
+            const int64_t most = x & 15 ? (int64_t)(16 - (x & 15)) / size : piece / size, len = most < t.n - at ? most : t.n - at;
             if (pieces.size() >= 0x7fffffffu / sizeof(ClipPiece)) return HGF_ERR_TOO_LARGE;
             pieces.push_back(ClipPiece{(const void *)x, (void *)y, (int)len, size == 2, (x & 15) == 0, (y & 15) == 0});
             at += len;
         }
     }
-    const int sms = device_sm_count(), dev = current_device();
-    if (!sms || dev < 0) return HGF_ERR_CUDA;
     const long long blocks = ((long long)pieces.size() + kClipWarps - 1) / kClipWarps;
-    const int grid = blocks < 1 ? 1 : blocks < 4 * sms ? (int)blocks : 4 * sms;
+    const int grid = blocks < 1 ? 1 : blocks < kClipBlocks * sms ? (int)blocks : kClipBlocks * sms;
     const size_t off = align_up(pieces.size() * sizeof(ClipPiece), 256);
     void *mem = nullptr;
     if (cudaMalloc(&mem, off + grid * sizeof(double)) != cudaSuccess) {
@@ -197,12 +226,11 @@ extern "C" hgf_status hgf_clip_grad_norm(hgf_grad_list *list, float max_norm, fl
     if ((uintptr_t)norm & 3u) return HGF_ERR_MISALIGNED;
     if (current_device() != list->device) return HGF_ERR_INVALID_ARG;
     const ClipPiece *pieces = (const ClipPiece *)list->mem;
-    clip_sums_kernel<<<list->grid, kClipThreads, 0, (cudaStream_t)stream>>>(pieces, list->n, list->part);
-    count_launch();
-    if (cudaGetLastError() != cudaSuccess) return HGF_ERR_CUDA;
-    clip_scale_kernel<<<list->grid, kClipThreads, 0, (cudaStream_t)stream>>>(pieces, list->n, list->part, list->grid, max_norm, norm);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
+    if (launch_overlapped(clip_sums_kernel, (unsigned)list->grid, kClipThreads, 0, (cudaStream_t)stream, pieces, list->n, list->part) != cudaSuccess) return HGF_ERR_CUDA;
+    return launch_overlapped(clip_scale_kernel, (unsigned)list->grid, kClipThreads, 0, (cudaStream_t)stream, pieces, list->n, (const double *)list->part, list->grid, max_norm,
+                             norm) == cudaSuccess
+               ? HGF_OK
+               : HGF_ERR_CUDA;
 }
 
 extern "C" void hgf_grad_list_destroy(hgf_grad_list *list) {
