@@ -148,16 +148,17 @@ struct TbCfg {
     static constexpr bool OVER_A = DH == 128 || !KEYS;
     static constexpr int TRES = KEYS ? (DH == 128 ? 1 : 0) : NS + 1, SRES = NS + 1 - TRES;  // resident operands in tensor and in shared memory
     static constexpr int NSB = OVER_A && (DH == 64 || KEYS) ? 1 : 2, NA = OVER_A ? 2 : 1;   // buffers of the scores and of A
-    static constexpr int NRES = 2;                                                          // of the resident operands in shared memory
-    static constexpr int ST = KEYS ? 4 : (DH == 64 ? 8 : 6);                                // ring stages
-    static constexpr int RES_TILE = NBLK * kTbTile * 128, RES_BYTES = SRES * RES_TILE;
+    static constexpr int NRES = DH == 64 ? 2 : 1;                                           // of the resident operands in shared memory
+    static constexpr int ST = KEYS || DH == 128 ? 4 : 6;                                    // ring stages
+    static constexpr int RES_TILE = NBLK * kTbTile * 128, RES_BYTES = SRES * RES_TILE, STAGED_BYTES = TRES * RES_TILE;
     static constexpr int ROW_BLOCK = kTbStep * 128, ROW_TILE = NBLK * ROW_BLOCK, ROW_BYTES = (NS + 1) * ROW_TILE;
     static constexpr int STAT_COPY = kTbTileBytes + (NS == 2 ? kTbDeltaBytes : 0), STAT_STAGE = kTbTileBytes + 512, ONES_TILE = kTbTile * 32;
-    static constexpr int OFF_RES = 2 * kTbBarBytes, OFF_RING = OFF_RES + (SRES ? NRES * RES_BYTES : 0), OFF_STATS = OFF_RING + ST * ROW_BYTES,
+    static constexpr int OFF_RES = 2 * kTbBarBytes, OFF_STAGED = OFF_RES + (SRES ? NRES * RES_BYTES : 0), OFF_RING = OFF_STAGED + STAGED_BYTES, OFF_STATS = OFF_RING + ST * ROW_BYTES,
                          OFF_ONES = OFF_STATS + (KEYS ? ST * STAT_STAGE : 0), SMEM_BYTES = OFF_ONES + (KEYS ? 4 * ONES_TILE : 0) + 1024;
     static constexpr int BAR_RESFULL = 0, BAR_RESEMPTY = BAR_RESFULL + NRES, BAR_FULL = BAR_RESEMPTY + NRES, BAR_EMPTY = BAR_FULL + ST,
                          BAR_RT = BAR_EMPTY + ST,      // resident rows are in tensor memory
-                         BAR_S = BAR_RT + 1,           // scores are there
+                         BAR_TFULL = BAR_RT + 1, BAR_TEMPTY = BAR_TFULL + 1,  // on their way there, in shared memory
+                         BAR_S = BAR_TEMPTY + 1,           // scores are there
                          BAR_A = BAR_S + 2,            // A is there
                          BAR_READ = BAR_A + 2,         // scores (OVER_A) or A (otherwise) have been read
                          BAR_P = BAR_READ + 2,         // first operands of the back products are there
@@ -172,10 +173,9 @@ struct TbCfg {
     static_assert(COL_R + TRES * (DH / 2) <= 512 && SMEM_BYTES <= 227 * 1024, "tensor and shared memory");
 };
 
-// What a pass reads and writes: res2, res1 the resident tensors of both streams and of one, row2, row1 the streamed ones.
+// What a pass writes: the gradients of the two-stream tensor (dK or dQ) and, for keys, of V.
 struct TbPass {
-    const __nv_bfloat16 *res2, *res1;
-    __nv_bfloat16 *d2, *d1;          // gradients of the two-stream tensor (dK or dQ) and, for keys, of V
+    __nv_bfloat16 *d2, *d1;
 };
 
 template <int DH, bool KEYS>
@@ -242,6 +242,8 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
             mbar_init(bar(C::BAR_BACK + i), 1);
         }
         mbar_init(bar(C::BAR_RT), C::WARPS);
+        mbar_init(bar(C::BAR_TFULL), 1);
+        mbar_init(bar(C::BAR_TEMPTY), C::WARPS);
         mbar_init(bar(C::BAR_ACC), 1);
         mbar_init(bar(C::BAR_ACCREAD), C::WARPS);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -269,11 +271,25 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
     Item t;
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
-        uint32_t issued[C::ST] = {}, res_issued[C::NRES] = {};
+        uint32_t issued[C::ST] = {}, res_issued[C::NRES] = {}, staged = 0;
         int s = 0, rb = 0;
         uint32_t ph = 1, rph = 1;
         bool ok = true;
         while (ok && next(c, t)) {
+            if constexpr (C::TRES > 0) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_TEMPTY), (staged & 1u) ^ 1u, abort_flag, status, 0xb04u)) != 0;
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t full = bar(C::BAR_TFULL), dst = sbase + C::OFF_STAGED;
+                    mbar_arrive_expect_tx(full, C::STAGED_BYTES);
+                    for (int blk = 0; blk < C::NBLK; ++blk) {
+                        for (int a = 0; a < NS; ++a)
+                            tma_load_3d(dst + a * C::RES_TILE + blk * kTbTile * 128, &map_res2, ((t.st + a) * h + t.hd) * DH + 64 * blk, t.r0, t.b, full);
+                        if (C::TRES > NS) tma_load_3d(dst + NS * C::RES_TILE + blk * kTbTile * 128, &map_res1, t.hd * DH + 64 * blk, t.r0, t.b, full);
+                    }
+                }
+                ++staged;
+            }
             if constexpr (C::SRES > 0) {
                 ok = __all_sync(0xffffffffu, mbar_wait(bar(C::BAR_RESEMPTY + rb), rph, abort_flag, status, 0xb00u + rb)) != 0;
                 if (!ok) break;
@@ -315,6 +331,8 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
         for (int q = 0; q < C::NRES; ++q)
             if (res_issued[q])
                 for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(bar(C::BAR_RESFULL + q), (res_issued[q] - 1u) & 1u); ++i) {}
+        if (staged)
+            for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(bar(C::BAR_TFULL), (staged - 1u) & 1u); ++i) {}
     } else if (warp == 1) {
         // ------------------------------------------------------------------ front products
         const uint64_t res_desc = make_sw128_desc(sbase + C::OFF_RES), row_desc = make_sw128_desc(sbase + C::OFF_RING);
@@ -412,33 +430,34 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
         const uint32_t lane_base = tmem + ((uint32_t)(32 * quarter) << 16);
         const size_t width = (size_t)h * DH;
         const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
-        // The item's resident rows into tensor memory, in units of 32 dims.  An item's last scores and A have been read when the next one's rows
-        // come, so no product reads them any more.  Four neighbouring lanes read 64 consecutive bytes of one row at a time and exchange blocks
-        // of 16 bytes, so that each has its own row: a lane along its own row touches 32 lines with every instruction, 1.5 us a tile.
-        auto bring = [&](const Item &n) {
+        // The next item's resident rows from where the copies have left them (rows of 128 bytes, their 16-byte pieces exchanged by the row's low bits)
+        // into tensor memory, in units of 32 dims.  An item's last scores and A have been read by then, so no product reads the rows before any more.
+        uint32_t staged = 0;
+        auto bring = [&] {
             if constexpr (C::TRES > 0) {
+                if (!wait(C::BAR_TFULL, staged & 1u, 0xb2cu)) return false;
+                ++staged;
 #pragma unroll
                 for (int r = 0; r < (C::TRES * DH / 32 + C::PARTS - 1) / C::PARTS; ++r) {
-                    const int unit = r * C::PARTS + part, a = unit / (DH / 32), dims = unit % (DH / 32) * 32;
+                    const int unit = r * C::PARTS + part;  // unit / 2: blocks of 64 dims, one tile after the other
                     if (unit >= C::TRES * DH / 32) continue;
-                    const int first = n.r0 + 32 * quarter + (lane & ~3);
-                    const __nv_bfloat16 *src = a < NS ? pass.res2 + ((size_t)(n.st + a) * h + n.hd) * DH : pass.res1 + (size_t)n.hd * DH;
-                    const size_t pitch = a < NS ? 2 * width : width;
+                    const uint8_t *src = smem + C::OFF_STAGED + (unit >> 1) * kTbTile * 128 + row * 128;
                     uint32_t v[16];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (first + e < L) w = __ldg(reinterpret_cast<const uint4 *>(src + ((size_t)n.b * L + first + e) * pitch + dims + 8 * (lane & 3)));
+                        const uint4 w = *reinterpret_cast<const uint4 *>(src + ((((unit & 1) * 4 + e) ^ (row & 7)) << 4));
                         v[4 * e] = w.x; v[4 * e + 1] = w.y; v[4 * e + 2] = w.z; v[4 * e + 3] = w.w;
                     }
-                    exchange_blocks(v, lane);
                     tmem_st16(lane_base + C::COL_R + unit * 16, v);
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::BAR_TEMPTY));
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::BAR_RT));
             }
+            return true;
         };
         auto two = [](const uint32_t *v) { return pack_f32x2(__uint_as_float(v[0]), __uint_as_float(v[1])); };
         bool ok = true;
@@ -446,7 +465,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
         uint32_t ph = 0;
         Item n;
         bool more = next(c, n);
-        if (more) bring(n);
+        if (more) ok = bring();
         while (ok && more) {
             t = n;
             const int mine = t.r0 + row, w0 = t.r0 + 32 * quarter;  // the thread's key or query; the warp's first
@@ -487,8 +506,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                         for (int u = 0; u < COLS; ++u)
                             if (KEYS ? c0 + u < mine : c0 + u > mine) x[a][u] = 0xff800000u;  // -inf: probability 0
                 }
-#pragma unroll
-                for (int a = 0; a < NS; ++a)
+                auto exponentials = [&](int a) {
 #pragma unroll
                     for (int u = 0; u < COLS; u += 2) {
                         float y0, y1;
@@ -496,10 +514,14 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                         x[a][u] = __float_as_uint(tb_ex2(y0));
                         x[a][u + 1] = __float_as_uint(tb_ex2(y1));
                     }
+                };
+                exponentials(0);
+                // (A is asked for under the second stream's exponentials)
                 if (!(ok = wait(C::BAR_A + ab, phase(g, C::NA), 0xb32u))) break;
                 tc_fence_after();
                 uint32_t dp[COLS];
                 tb_load(a_addr, dp);
+                if constexpr (NS == 2) exponentials(1);
                 tmem_ld_wait();
                 if constexpr (!C::OVER_A) {
                     tc_fence_before();
@@ -554,7 +576,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                     dl += (double)a + (double)b - (part ? 0.0 : (double)d);
                 }
             }
-            if ((more = next(c, n))) bring(n);
+            if ((more = next(c, n)) && !(ok = bring())) break;
             // ---- outputs: this warp's rows, in units of 32 columns of an accumulator (64 bytes of a row, stored by four lanes as above)
             if (!(ok = wait(C::BAR_ACC, ph, 0xb40u))) break;
             ph ^= 1u;
@@ -590,6 +612,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
     return dl;
 }
 
+// res2, res1: the resident tensors of both streams and of one, row2, row1: the streamed ones.
 struct TbMaps {
     CUtensorMap res2, res1, row2, row1;
 };
@@ -695,8 +718,7 @@ static cudaError_t launch_backward(const void *q, const void *k, const void *v, 
     const int most = sms < kTbMaxGrid ? sms : kTbMaxGrid, grid = tiles < most ? (int)tiles : most;
     TbMaps keys, queries;
     if (!make_maps(&keys, k, v, q, dout, DH, p) || !make_maps(&queries, q, dout, k, v, DH, p)) return cudaErrorInvalidValue;
-    const TbPass of_keys = {(const __nv_bfloat16 *)k, (const __nv_bfloat16 *)v, (__nv_bfloat16 *)grads.dk, (__nv_bfloat16 *)grads.dv};
-    const TbPass of_queries = {(const __nv_bfloat16 *)q, (const __nv_bfloat16 *)dout, (__nv_bfloat16 *)grads.dq, nullptr};
+    const TbPass of_keys = {(__nv_bfloat16 *)grads.dk, (__nv_bfloat16 *)grads.dv}, of_queries = {(__nv_bfloat16 *)grads.dq, nullptr};
     e = launch_overlapped(attention_stats_kernel<DH>, (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream, (const __nv_bfloat16 *)dout,
                      (const __nv_bfloat16 *)streams, lse, stats, p.arrivals, p.B, p.L, p.h, p.scale_log2);
     if (e != cudaSuccess) return e;
