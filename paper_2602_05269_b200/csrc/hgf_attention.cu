@@ -95,13 +95,14 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     const int L = p.L, h = p.h, nqt = (L + kTaBM - 1) / kTaBM, bhs = p.B * h, items = nqt * bhs, G = (int)gridDim.x;
     // The CTA's k-th tile: the tiles in order of falling length (late queries first) are dealt in rounds, every other
     // round backwards, so that the CTAs' sums stay close.
-    struct Tile { int q0, tok0, hd, J, bh; };
+    struct Tile { int q0, b, tok0, hd, J, bh; };
     auto tile_of = [&](int k, Tile &t) {
         const int i = k * G + ((k & 1) ? G - 1 - (int)blockIdx.x : (int)blockIdx.x);
         if (i >= items) return false;
         const int qt = nqt - 1 - i / bhs, bh = i % bhs, keys = (qt + 1) * kTaBM < L ? (qt + 1) * kTaBM : L;  // keys visible to the tile
         t.q0 = qt * kTaBM;
-        t.tok0 = (bh / h) * L;
+        t.b = bh / h;
+        t.tok0 = t.b * L;
         t.hd = bh % h;
         t.bh = bh;
         t.J = (keys + KV - 1) / KV;
@@ -156,7 +157,7 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                 mbar_arrive_expect_tx(full, 2 * C::Q_BYTES);
                 for (int st = 0; st < 2; ++st)
                     for (int blk = 0; blk < C::NBLK; ++blk)
-                        tma_load_2d(sbase + (2 * qb + st) * C::Q_BYTES + blk * kTaBM * 128, &tmap_q, (st * h + t.hd) * DH + 64 * blk, t.tok0 + t.q0, full);
+                        tma_load_3d(sbase + (2 * qb + st) * C::Q_BYTES + blk * kTaBM * 128, &tmap_q, (st * h + t.hd) * DH + 64 * blk, t.q0, t.b, full);
             }
             ++q_issued[qb];
             if (++qb == C::NQ) { qb = 0; qph ^= 1u; }
@@ -167,8 +168,8 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     const uint32_t dst = sbase + C::OFF_K + ks * 2 * C::K_BYTES, full = bar(C::BAR_KFULL + ks);
                     mbar_arrive_expect_tx(full, 2 * C::K_BYTES);
                     for (int blk = 0; blk < C::NBLK; ++blk) {
-                        tma_load_2d(dst + blk * KV * 128, &tmap_k, t.hd * DH + 64 * blk, t.tok0 + j * KV, full);
-                        tma_load_2d(dst + C::K_BYTES + blk * KV * 128, &tmap_k, (h + t.hd) * DH + 64 * blk, t.tok0 + j * KV, full);
+                        tma_load_3d(dst + blk * KV * 128, &tmap_k, t.hd * DH + 64 * blk, j * KV, t.b, full);
+                        tma_load_3d(dst + C::K_BYTES + blk * KV * 128, &tmap_k, (h + t.hd) * DH + 64 * blk, j * KV, t.b, full);
                     }
                 }
                 ++k_issued[ks];
@@ -179,7 +180,7 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     const uint32_t full = bar(C::BAR_VFULL + vs);
                     mbar_arrive_expect_tx(full, C::V_BYTES);
                     for (int blk = 0; blk < C::NBLK; ++blk)
-                        tma_load_2d(sbase + C::OFF_V + vs * C::V_BYTES + blk * C::V_BLOCK, &tmap_v, t.hd * DH + 64 * blk, t.tok0 + j * KV, full);
+                        tma_load_3d(sbase + C::OFF_V + vs * C::V_BYTES + blk * C::V_BLOCK, &tmap_v, t.hd * DH + 64 * blk, j * KV, t.b, full);
                 }
                 ++v_issued[vs];
                 if (++vs == C::VST) { vs = 0; vph ^= 1u; }
@@ -515,11 +516,9 @@ static cudaError_t launch_attention_tc(const AttnParams &p, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     unsigned int *status = device_status_word();
     if (!status) return cudaErrorMemoryAllocation;
-    const uint64_t rows = (uint64_t)p.B * p.L, dq = (uint64_t)2 * p.h * DH, dv = (uint64_t)p.h * DH;
+    const uint64_t w = (uint64_t)p.h * DH;
     CUtensorMap mq, mk, mv;
-    if (!make_map_2d(&mq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.q, dq, rows, dq * 2, 64, kTaBM, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map_2d(&mk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.k, dq, rows, dq * 2, 64, kTaKV, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map_2d(&mv, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.v, dv, rows, dv * 2, 64, kTaKV, CU_TENSOR_MAP_SWIZZLE_128B))
+    if (!make_map_tokens(&mq, p.q, 2 * w, p.L, p.B, kTaBM) || !make_map_tokens(&mk, p.k, 2 * w, p.L, p.B, kTaKV) || !make_map_tokens(&mv, p.v, w, p.L, p.B, kTaKV))
         return cudaErrorInvalidValue;
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;

@@ -675,15 +675,6 @@ attention_backward_kernel(const __grid_constant__ TbMaps keys, const __grid_cons
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512) : "memory");
 }
 
-static bool make_map_tokens(CUtensorMap *map, const void *base, uint64_t width, uint64_t L, uint64_t B, uint32_t rows) {
-    EncodeTiledFn fn = get_encode_fn();
-    if (!fn) return false;
-    // (a dimension of its own for the batch: what lies behind a sequence reads as zeros, not as the next one)
-    cuuint64_t dims[3] = {width, L, B}, strides[2] = {width * 2, width * 2 * L};
-    cuuint32_t box[3] = {64, rows, 1}, one[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 static bool make_maps(TbMaps *m, const void *res2, const void *res1, const void *row2, const void *row1, int dh, const AttnBackParams &p) {
     const uint64_t w = (uint64_t)p.h * dh;
     return make_map_tokens(&m->res2, res2, 2 * w, p.L, p.B, kTbTile) && make_map_tokens(&m->res1, res1, w, p.L, p.B, kTbTile) &&

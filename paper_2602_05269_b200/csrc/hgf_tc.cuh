@@ -299,6 +299,17 @@ static inline bool make_map_blocks(CUtensorMap *map, CUtensorMapDataType dt, con
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Token rows [B][L][width] of bf16 in boxes of 64 columns and `rows` tokens.  The batch has a dimension of its own: what lies behind a sequence reads as
+// zeros, not as the next one, whose values may not be finite (0 times those would not be 0).
+static inline bool make_map_tokens(CUtensorMap *map, const void *base, uint64_t width, uint64_t L, uint64_t B, uint32_t rows) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {width, L, B}, strides[2] = {width * 2, width * 2 * L};
+    cuuint32_t box[3] = {64, rows, 1}, one[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static inline bool make_map_4d(CUtensorMap *map, CUtensorMapDataType dt, const void *base, const uint64_t (&dims)[4], const uint64_t (&stride_bytes)[3],
                                const uint32_t (&box)[4], CUtensorMapSwizzle sw) {
     EncodeTiledFn fn = get_encode_fn();

@@ -84,13 +84,14 @@ def test_sequences_do_not_touch_each_other(hgf, dh):
     """A sequence of a batch whose values are not finite leaves the gradients of the others as they are, at lengths inside a tile."""
     B, L, h, lam = 3, 77, 2, 0.8
     q, k, v, g = ref.inputs(B, L, h, dh, 10, "cuda")
-    _, streams, lse = hgf.diff_attention_forward_train(q, k, v, B, L, h, dh, lam)
-    clean = hgf.diff_attention_backward(q, k, v, g, streams, lse, B, L, h, dh, lam)
-    for x in (q, k, v, g, streams):
+    out, streams, lse = hgf.diff_attention_forward_train(q, k, v, B, L, h, dh, lam)
+    clean = {"out": out, "streams": streams, **hgf.diff_attention_backward(q, k, v, g, streams, lse, B, L, h, dh, lam)}
+    for x in (q, k, v, g):
         x[L:2 * L] = float("nan")
-    lse[1] = float("inf")
-    dirty = hgf.diff_attention_backward(q, k, v, g, streams, lse, B, L, h, dh, lam)
-    for n in ("dq", "dk", "dv"):
+    out, streams, dirty_lse = hgf.diff_attention_forward_train(q, k, v, B, L, h, dh, lam)
+    assert torch.equal(lse[0], dirty_lse[0]) and torch.equal(lse[2], dirty_lse[2]) and not dirty_lse[1].isfinite().any()
+    dirty = {"out": out, "streams": streams, **hgf.diff_attention_backward(q, k, v, g, streams, dirty_lse, B, L, h, dh, lam)}
+    for n in ("out", "streams", "dq", "dk", "dv"):
         assert torch.equal(clean[n][:L], dirty[n][:L]) and torch.equal(clean[n][2 * L:], dirty[n][2 * L:])
         assert not dirty[n][L:2 * L].isfinite().all()
 
