@@ -358,7 +358,7 @@ double hgf_diff_lambda0(double head_dim);
 
 /*
  * The same for training: hgf_diff_attention_forward, which also keeps what the backward pass needs,
- *   streams  [B*L][2 * n_heads * head_dim]  bfloat16, laid out as q: each stream's own Softmax(Q_s K_s^T / sqrt(d_h)) V, not scaled
+ *   streams  [B*L][2 * n_heads * head_dim]  fp32, laid out as q: each stream's own Softmax(Q_s K_s^T / sqrt(d_h)) V, not scaled
  *   lse      [B][n_heads][2][L]             fp32: log2 of each query's sum of 2^(log2(e) q.k / sqrt(d_h)) in stream 1 and 2
  * (both are written whole), and the gradients with respect to its inputs: with P_s the probabilities and dO = dout
  *     dV = ( P_1 - lambda P_2 )^T dO * out_scale        T_s = P_s (.) ( dO V^T - rowsum(dO (.) streams_s) )
@@ -369,8 +369,9 @@ double hgf_diff_lambda0(double head_dim);
  *   grads    dq, dk laid out as q, k, and dv as v, bfloat16; dlambda one fp32 value.  Null: not computed (dk and dv together; dlambda with dq only)
  *   workspace  hgf_diff_attention_backward_workspace_bytes(...) bytes, 256-byte aligned; scratch, not shared by calls that may overlap on the device
  *   flags    0
- * q, k, v, lambda, out_scale, sizes and refusals as in the forward pass.  P and T enter their products rounded to bfloat16 (fp32 accumulation),
- * dlambda is summed from unrounded ones; every sum has one order, so that equal calls give equal bits.  The sequences of a batch do not touch one
+ * q, k, v, lambda, out_scale, sizes and refusals as in the forward pass.  Here the forward pass takes the probabilities to 2^-16 (two bfloat16
+ * parts), so that its output is nearer than hgf_diff_attention_forward's; backward P and T enter their products rounded to bfloat16 (fp32
+ * accumulation), dlambda is summed from unrounded ones; every sum has one order, so that equal calls give equal bits.  The sequences of a batch do not touch one
  * another's gradients; within a sequence a value that is not finite can reach every gradient of its head, hidden positions too (0 times it is no
  * zero), so padding behind a text has to be finite, with dout zero.
  */
@@ -382,10 +383,10 @@ typedef struct {
 } hgf_attention_grads;
 hgf_status hgf_diff_attention_forward_train(const void *q, const void *k, const void *v, int64_t B, int64_t L,
                                             int32_t n_heads, int32_t head_dim, float lambda, float out_scale,
-                                            void *out, void *streams, float *lse, uint32_t flags, void *stream);
+                                            void *out, float *streams, float *lse, uint32_t flags, void *stream);
 size_t hgf_diff_attention_backward_workspace_bytes(int64_t B, int64_t L, int32_t n_heads, int32_t head_dim);
 hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void *v, const void *dout,
-                                       const void *streams, const float *lse, int64_t B, int64_t L, int32_t n_heads,
+                                       const float *streams, const float *lse, int64_t B, int64_t L, int32_t n_heads,
                                        int32_t head_dim, float lambda, float out_scale, const hgf_attention_grads *grads,
                                        void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
 

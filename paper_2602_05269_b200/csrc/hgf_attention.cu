@@ -12,7 +12,7 @@ namespace hgf {
 struct AttnParams {
     const __nv_bfloat16 *q, *k, *v;  // q, k [B*L][2*h*dh]; v [B*L][h*dh]
     void *out;                       // [B*L][h*dh] fp32 or bf16
-    __nv_bfloat16 *streams;          // [B*L][2*h*dh] (for the backward pass, else null)
+    float *streams;                  // [B*L][2*h*dh] (for the backward pass, else null)
     float *lse;                      // [B][h][2][L]
     int B, L, h;
     float lambda, out_scale, scale_log2;  // scale_log2 = log2(e) / sqrt(dh)
@@ -76,7 +76,10 @@ __device__ __forceinline__ float ex2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
     return y;
 }
-// SAVE: for the backward pass each stream's own output O_s / l_s (bf16) and log2 of its sum of 2^(scale s) go to memory, too.
+// SAVE: for the backward pass each stream's own output O_s / l_s and log2 of its sum of 2^(scale s) go to memory, too.  The backward pass takes
+// D = dO . O_s from them, and what D is off by weighs every key of a row at once: with P rounded to bf16, and O_s too, the gradients of Q and K were
+// 1.7 (rows of few keys 2.4) times as far from 64 bits as their own rounding puts them.  So P enters the second product in two bf16 parts, both in
+// the columns of the scores that they come from, and O_s stays in fp32.
 template <int DH, bool SAVE>
 __global__ void __launch_bounds__(kTaThreads, 1)
 ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
@@ -223,6 +226,10 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
 #pragma unroll
             for (int kk = 0; kk < KV / 16; ++kk)
                 warp_mma_f16_ts(o_col, s_col + buf * KV + 8 * kk, vd + (uint64_t)(128 * kk), C::IDESC_PV, (!first || kk) ? 1u : 0u);
+            if constexpr (SAVE)
+#pragma unroll
+                for (int kk = 0; kk < KV / 16; ++kk)
+                    warp_mma_f16_ts(o_col, s_col + buf * KV + KV / 2 + 8 * kk, vd + (uint64_t)(128 * kk), C::IDESC_PV, 1u);
         };
         // The steps of all tiles are one sequence, g: the scores of step g + 2 follow P V of step g also across
         // the end of a tile, while its outputs are still being written.  (sj, sk, stile: the score side, two steps ahead.)
@@ -315,10 +322,13 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                 ok = mbar_wait_poll(bar(C::BAR_SFULL + 2 * st + buf), (uint32_t)(g >> 1) & 1u, abort_flag, status, 0xa40u + st);
                 if (!(ok = __all_sync(0xffffffffu, ok))) break;
                 tc_fence_after();
-                uint32_t pk[32];
+                uint32_t pk[32], rest[SAVE ? 32 : 1];  // probabilities as bf16 pairs; what they are rounded by, likewise
                 if (k0 > w0 + 31) {  // every key of the step lies after every query of the warp
 #pragma unroll
                     for (int u = 0; u < 32; ++u) pk[u] = 0u;
+                    if constexpr (SAVE)
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) rest[u] = 0u;
                 } else {
                     uint32_t v0[32], v1[32];
                     tmem_ld32(s_addr, v0);
@@ -367,20 +377,27 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     m = m_new;
                     // probabilities as bf16 pairs
                     const uint64_t c2 = pack_f32x2(c, c), nmc2 = pack_f32x2(-m_new * c, -m_new * c);
-                    auto pair = [&](uint32_t a, uint32_t b, uint64_t &sum) {
+                    auto pair = [&](uint32_t a, uint32_t b, uint64_t &sum, uint32_t &less) {
                         float x0, x1;
                         unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(a), __uint_as_float(b)), c2, nmc2), x0, x1);
                         const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                         sum = add_f32x2(sum, pack_f32x2(p0, p1));
-                        return pack_bf16(p0, p1);
+                        const uint32_t near = pack_bf16(p0, p1);
+                        if constexpr (SAVE) {
+                            float r0, r1;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(bf16lo_to_float(near), bf16hi_to_float(near)), pack_f32x2(-1.0f, -1.0f), pack_f32x2(p0, p1)), r0, r1);
+                            less = pack_bf16(r0, r1);
+                        }
+                        return near;
                     };
 #pragma unroll
                     for (int u = 0; u < 32; u += 2) {
-                        pk[u >> 1] = pair(v0[u], v0[u + 1], l2a);
-                        pk[16 + (u >> 1)] = pair(v1[u], v1[u + 1], l2b);
+                        pk[u >> 1] = pair(v0[u], v0[u + 1], l2a, rest[SAVE ? u >> 1 : 0]);
+                        pk[16 + (u >> 1)] = pair(v1[u], v1[u + 1], l2b, rest[SAVE ? 16 + (u >> 1) : 0]);
                     }
                 }
                 tmem_st32(s_addr, pk);
+                if constexpr (SAVE) tmem_st32(s_addr + KV / 2, rest);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -422,20 +439,21 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     if (lane == 0) mbar_arrive(bar(C::BAR_OEMPTY + ob));
                 }
                 if constexpr (SAVE) {
+                    // (four lanes store 64 bytes of a row, as below)
                     const float r1 = 1.0f / sl[row], r2 = 1.0f / sl[kTaBM + row];
-                    __nv_bfloat16 *dst = p.streams + (size_t)(t.tok0 + qi) * (2 * (size_t)h * DH) + (size_t)t.hd * DH + cc;
-                    if (qi < L) {
+                    const int quad = t.q0 + 32 * quarter + (lane & ~3);
+                    float *dst = p.streams + (size_t)(t.tok0 + quad) * (2 * (size_t)h * DH) + (size_t)t.hd * DH + cc + 4 * (lane & 3);
 #pragma unroll
-                        for (int u = 0; u < 32; u += 8) {
-                            uint32_t o1[4], o2[4];
+                    for (int n = 0; n < 4; ++n) {
+                        uint32_t o[16];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                o1[e] = pack_bf16(__uint_as_float(v1[u + 2 * e]) * r1, __uint_as_float(v1[u + 2 * e + 1]) * r1);
-                                o2[e] = pack_bf16(__uint_as_float(v2[u + 2 * e]) * r2, __uint_as_float(v2[u + 2 * e + 1]) * r2);
-                            }
-                            *reinterpret_cast<uint4 *>(dst + u) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
-                            *reinterpret_cast<uint4 *>(dst + (size_t)h * DH + u) = make_uint4(o2[0], o2[1], o2[2], o2[3]);
-                        }
+                        for (int e = 0; e < 16; ++e)
+                            o[e] = n < 2 ? __float_as_uint(__uint_as_float(v1[16 * (n & 1) + e]) * r1) : __float_as_uint(__uint_as_float(v2[16 * (n & 1) + e]) * r2);
+                        exchange_blocks(o, lane);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (quad + e < L)
+                                *reinterpret_cast<uint4 *>(dst + ((size_t)e * 2 + (n >> 1)) * h * DH + 16 * (n & 1)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                     }
                 }
                 if constexpr (DH == 128) {
@@ -533,7 +551,7 @@ static cudaError_t launch_attention_tc(const AttnParams &p, cudaStream_t stream)
 using namespace hgf;
 
 static hgf_status attention_forward(const void *q, const void *k, const void *v, int64_t B, int64_t L, int32_t n_heads, int32_t head_dim,
-                                    float lambda, float out_scale, void *out, bool save, void *streams, float *lse, uint32_t flags,
+                                    float lambda, float out_scale, void *out, bool save, float *streams, float *lse, uint32_t flags,
                                     void *stream) {
     if (!q || !k || !v || !out || B <= 0 || L <= 0 || n_heads <= 0) return HGF_ERR_INVALID_ARG;
     if (save && (!streams || !lse)) return HGF_ERR_INVALID_ARG;
@@ -547,7 +565,7 @@ static hgf_status attention_forward(const void *q, const void *k, const void *v,
     p.k = (const __nv_bfloat16 *)k;
     p.v = (const __nv_bfloat16 *)v;
     p.out = out;
-    p.streams = (__nv_bfloat16 *)streams;
+    p.streams = streams;
     p.lse = lse;
     p.B = (int)B;
     p.L = (int)L;
@@ -569,7 +587,7 @@ extern "C" hgf_status hgf_diff_attention_forward(const void *q, const void *k, c
 }
 
 extern "C" hgf_status hgf_diff_attention_forward_train(const void *q, const void *k, const void *v, int64_t B, int64_t L, int32_t n_heads,
-                                                       int32_t head_dim, float lambda, float out_scale, void *out, void *streams, float *lse,
+                                                       int32_t head_dim, float lambda, float out_scale, void *out, float *streams, float *lse,
                                                        uint32_t flags, void *stream) {
     return attention_forward(q, k, v, B, L, n_heads, head_dim, lambda, out_scale, out, true, streams, lse, flags, stream);
 }

@@ -52,10 +52,10 @@ __device__ __forceinline__ void tb_store(uint32_t at, const uint32_t (&v)[8]) { 
 // Rows behind the sequence get probability 0 (an exponent of -infinity, or of -10^30 where 0 times it is formed).
 constexpr int kTbTileBytes = 2048, kTbDeltaBytes = 256, kTbStatBytes = kTbTileBytes + kTbDeltaBytes + 1024;
 
-// A thread block takes 64 tokens: a row of G, O_1 and O_2 is read by head_dim / 8 lanes, 16 bytes each.
+// A thread block takes 64 tokens: a row of G, O_1 and O_2 is read by head_dim / 8 lanes, eight dims each.
 template <int DH>
 __global__ void __launch_bounds__(256)
-attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, const float *lse, uint8_t *stats, unsigned int *arrivals, int B, int L, int h,
+attention_stats_kernel(const __nv_bfloat16 *dout, const float *streams, const float *lse, uint8_t *stats, unsigned int *arrivals, int B, int L, int h,
                        float scale_log2) {
     constexpr int LPR = DH / 8, RPW = 32 / LPR;
     __shared__ float s_v[4][64];
@@ -75,14 +75,14 @@ attention_stats_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *streams, 
             if (i < L) {
                 const size_t col = (size_t)hd * DH + (lane % LPR) * 8;
                 const uint4 g = __ldg(reinterpret_cast<const uint4 *>(dout + (tok0 + i) * width + col));
-                const uint4 a = __ldg(reinterpret_cast<const uint4 *>(streams + (tok0 + i) * 2 * width + col));
-                const uint4 b = __ldg(reinterpret_cast<const uint4 *>(streams + (tok0 + i) * 2 * width + width + col));
-                const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+                const float4 *a = reinterpret_cast<const float4 *>(streams + (tok0 + i) * 2 * width + col), *b = a + width / 4;
+                const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float g0 = bf16lo_to_float(gw[e]), g1 = bf16hi_to_float(gw[e]);
-                    d1 = fmaf(g0, bf16lo_to_float(aw[e]), fmaf(g1, bf16hi_to_float(aw[e]), d1));
-                    d2 = fmaf(g0, bf16lo_to_float(bw[e]), fmaf(g1, bf16hi_to_float(bw[e]), d2));
+                for (int e = 0; e < 2; ++e) {
+                    const float4 x = __ldg(a + e), y = __ldg(b + e);
+                    const float g0 = bf16lo_to_float(gw[2 * e]), g1 = bf16hi_to_float(gw[2 * e]), g2 = bf16lo_to_float(gw[2 * e + 1]), g3 = bf16hi_to_float(gw[2 * e + 1]);
+                    d1 = fmaf(g0, x.x, fmaf(g1, x.y, fmaf(g2, x.z, fmaf(g3, x.w, d1))));
+                    d2 = fmaf(g0, y.x, fmaf(g1, y.y, fmaf(g2, y.z, fmaf(g3, y.w, d2))));
                 }
             }
 #pragma unroll
@@ -687,7 +687,7 @@ static size_t stats_bytes(int64_t B, int64_t L, int64_t h) { return (size_t)(B *
 constexpr size_t kTbPartBytes = (size_t)kTbMaxGrid * TbCfg<64, true>::WARPS * sizeof(double);
 
 template <int DH>
-static cudaError_t launch_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
+static cudaError_t launch_backward(const void *q, const void *k, const void *v, const void *dout, const float *streams, const float *lse,
                                    const hgf_attention_grads &grads, AttnBackParams p, void *workspace, cudaStream_t stream) {
     constexpr int SMEM = TbCfg<DH, true>::SMEM_BYTES > TbCfg<DH, false>::SMEM_BYTES ? TbCfg<DH, true>::SMEM_BYTES : TbCfg<DH, false>::SMEM_BYTES;
     static std::atomic<unsigned long long> attr_done{0};
@@ -711,7 +711,7 @@ static cudaError_t launch_backward(const void *q, const void *k, const void *v, 
     if (!make_maps(&keys, k, v, q, dout, DH, p) || !make_maps(&queries, q, dout, k, v, DH, p)) return cudaErrorInvalidValue;
     const TbPass of_keys = {(__nv_bfloat16 *)grads.dk, (__nv_bfloat16 *)grads.dv}, of_queries = {(__nv_bfloat16 *)grads.dq, nullptr};
     e = launch_overlapped(attention_stats_kernel<DH>, (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, stream, (const __nv_bfloat16 *)dout,
-                     (const __nv_bfloat16 *)streams, lse, stats, p.arrivals, p.B, p.L, p.h, p.scale_log2);
+                     streams, lse, stats, p.arrivals, p.B, p.L, p.h, p.scale_log2);
     if (e != cudaSuccess) return e;
     return launch_overlapped(attention_backward_kernel<DH>, (unsigned)grid, TbCfg<DH, true>::THREADS, SMEM, stream, keys, queries, of_keys, of_queries, p, status);
 }
@@ -730,7 +730,7 @@ extern "C" size_t hgf_diff_attention_backward_workspace_bytes(int64_t B, int64_t
     return stats_bytes(B, L, n_heads) + kTbPartBytes + 256;
 }
 
-extern "C" hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void *v, const void *dout, const void *streams, const float *lse,
+extern "C" hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void *v, const void *dout, const float *streams, const float *lse,
                                                   int64_t B, int64_t L, int32_t n_heads, int32_t head_dim, float lambda, float out_scale,
                                                   const hgf_attention_grads *grads, void *workspace, size_t workspace_bytes, uint32_t flags,
                                                   void *stream) {

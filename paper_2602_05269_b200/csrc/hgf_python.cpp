@@ -336,8 +336,8 @@ decltype(&hgf_clip_grad_norm) g_clip = nullptr;
 struct AttentionCall : DeviceCall {
     int64_t B, L, h, dh, width = 0, rows = 0;
     double lambda, scale;
-    const void *q, *k, *v, *streams;
-    const float *lse;
+    const void *q, *k, *v;
+    const float *streams, *lse;
     // q, k, v, then at n: B, L, n_heads, head_dim, lambda, out_scale
     AttentionCall(PyObject *const *a, int n, PyObject *streams_, PyObject *lse_, PyObject *stream_) {
         of(a[0]);
@@ -348,7 +348,7 @@ struct AttentionCall : DeviceCall {
         if (!ok) return;
         rows = B * L, width = h * dh;
         q = matrix(a[0], at::kBFloat16, rows, 2 * width), k = matrix(a[1], at::kBFloat16, rows, 2 * width), v = matrix(a[2], at::kBFloat16, rows, width);
-        streams = matrix(streams_, at::kBFloat16, rows, 2 * width);
+        streams = static_cast<const float *>(matrix(streams_, at::kFloat, rows, 2 * width));
         const at::Tensor *t = tensor(lse_, at::kFloat);
         ok = ok && t->dim() == 4 && t->size(0) == B && t->size(1) == h && t->size(2) == 2 && t->size(3) == L;
         lse = ok ? static_cast<const float *>(t->data_ptr()) : nullptr;
@@ -362,7 +362,7 @@ PyObject *diff_attention_forward_train(PyObject *, PyObject *const *a, Py_ssize_
         void *out = c.matrix(a[9], flags & HGF_FLAG_OUT_BF16 ? at::kBFloat16 : at::kFloat, c.rows, c.width);
         if (!c.ok) return given_back();
         return called([&] {
-            return g_attention(c.q, c.k, c.v, c.B, c.L, (int32_t)c.h, (int32_t)c.dh, (float)c.lambda, (float)c.scale, out, const_cast<void *>(c.streams),
+            return g_attention(c.q, c.k, c.v, c.B, c.L, (int32_t)c.h, (int32_t)c.dh, (float)c.lambda, (float)c.scale, out, const_cast<float *>(c.streams),
                                const_cast<float *>(c.lse), (uint32_t)flags, c.stream);
         });
     });

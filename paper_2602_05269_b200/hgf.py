@@ -513,7 +513,7 @@ def _attention_inputs(q, k, v, B, L, n_heads, head_dim):
 def diff_attention_forward_train(q, k, v, B: int, L: int, n_heads: int, head_dim: int, lam: float, out_scale: float = 1.0, *,
                                  out=None, streams=None, lse=None, flags: int = 0, stream=None):
     """hgf_diff_attention_forward_train: diff_attention_forward that keeps what diff_attention_backward needs.  Returns (out, streams, lse):
-    streams bf16 [B*L][2*n_heads*head_dim], lse fp32 [B][n_heads][2][L]; all three are reused when given."""
+    streams fp32 [B*L][2*n_heads*head_dim], lse fp32 [B][n_heads][2][L]; all three are reused when given."""
     if out is not None and streams is not None and lse is not None and _native_train and _done(
             "hgf_diff_attention_forward_train",
             _native_train.diff_attention_forward_train(q, k, v, B, L, n_heads, head_dim, lam, out_scale, out, streams, lse, flags, stream)):
@@ -522,10 +522,10 @@ def diff_attention_forward_train(q, k, v, B: int, L: int, n_heads: int, head_dim
     dtype = torch.bfloat16 if flags & FLAG_OUT_BF16 else torch.float32
     with _on(stream):
         out = torch.empty((B * L, width), dtype=dtype, device=q.device) if out is None else out
-        streams = torch.empty((B * L, 2 * width), dtype=torch.bfloat16, device=q.device) if streams is None else streams
+        streams = torch.empty((B * L, 2 * width), dtype=torch.float32, device=q.device) if streams is None else streams
         lse = torch.empty((B, n_heads, 2, L), dtype=torch.float32, device=q.device) if lse is None else lse
     _dense("out", out, dtype, (B * L, width), q.device)
-    _dense("streams", streams, torch.bfloat16, (B * L, 2 * width), q.device)
+    _dense("streams", streams, torch.float32, (B * L, 2 * width), q.device)
     _dense("lse", lse, torch.float32, (B, n_heads, 2, L), q.device)
     _check("hgf_diff_attention_forward_train",
            lib().hgf_diff_attention_forward_train(_ptr(q), _ptr(k), _ptr(v), B, L, n_heads, head_dim, lam, out_scale, _ptr(out), _ptr(streams), _ptr(lse),
@@ -550,7 +550,7 @@ def diff_attention_backward(q, k, v, dout, streams, lse, B: int, L: int, n_heads
             return {"dq": out["dq"], "dk": out["dk"], "dv": out["dv"], "dlambda": out["dlambda"], "_workspace": ws}
     width = _attention_inputs(q, k, v, B, L, n_heads, head_dim)
     _dense("dout", dout, torch.bfloat16, (B * L, width), q.device)
-    _dense("streams", streams, torch.bfloat16, (B * L, 2 * width), q.device)
+    _dense("streams", streams, torch.float32, (B * L, 2 * width), q.device)
     _dense("lse", lse, torch.float32, (B, n_heads, 2, L), q.device)
     like = {"dq": q, "dk": k, "dv": v}
     names = [n for n in ("dq", "dk", "dv", "dlambda") if want is None or n in want]

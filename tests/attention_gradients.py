@@ -29,8 +29,8 @@ def reference(q, k, v, g, B, L, h, dh, lam, scale):
     out, dv = scale * mix @ V, scale * T_(mix) @ G
     dq = torch.stack([c * w[s] * T[s] @ K[s] for s in (0, 1)])
     dk = torch.stack([c * w[s] * T_(T[s]) @ Q[s] for s in (0, 1)])
-    # D comes from O in bf16, which itself comes from P in bf16: twice half a step of each term of G . O
-    off = 2 * HALF * (G.abs() * (P @ V.abs())).sum(-1, keepdim=True)
+    # D comes from O in fp32, which comes from P in two bf16 parts: half a step of the half step that the first is off by
+    off = (HALF * HALF + SLACK) * (G.abs() * (P @ V.abs())).sum(-1, keepdim=True)
     # every T is rounded to bf16; the probability has SLACK, D has `off`; what A - D is made of counts where they cancel
     each = HALF * T.abs() + P * (off + SLACK * (A.abs() + D.abs()))
     e_dq = torch.stack([c * abs(w[s]) * each[s] @ K[s].abs() for s in (0, 1)])
@@ -39,14 +39,14 @@ def reference(q, k, v, g, B, L, h, dh, lam, scale):
     # heads of 64: P_1 - lambda P_2 is rounded once; of 128, where a stream follows the other: P_1 and lambda P_2 each, half a step of |P_1| and
     # one of |lambda P_2|, and those do not cancel as the values do
     e_dv = abs(scale) * T_(HALF * (mix.abs() if dh < 128 else size) + SLACK * size) @ G.abs()
-    e_out = abs(scale) * (HALF + SLACK) * size @ V.abs()
+    e_out = abs(scale) * (HALF * HALF + SLACK) * size @ V.abs()
     back2 = lambda x: x.permute(1, 3, 0, 2, 4).reshape(B * L, -1)  # noqa: E731
     back1 = lambda x: x.permute(0, 2, 1, 3).reshape(B * L, -1)  # noqa: E731
     final = lambda x, e: (x, e + HALF * (x.abs() + e))  # noqa: E731  (the output is bf16)
     terms = P[1] * A
     return {"out": final(back1(out), back1(e_out)), "dq": final(back2(dq), back2(e_dq)), "dk": final(back2(dk), back2(e_dk)), "dv": final(back1(dv), back1(e_dv)),
             "dlambda": (-scale * terms.sum().view(1), abs(scale) * SLACK * (terms.abs().sum() + (P[1] * D[1].abs()).sum()).view(1)),
-            "streams": final(back2(O), back2((HALF + SLACK) * P @ V.abs())),
+            "streams": (back2(O), back2((HALF * HALF + SLACK) * P @ V.abs())),
             "lse": (torch.logsumexp((c * Q @ K.transpose(-1, -2)).masked_fill(hidden, -math.inf), -1).permute(1, 2, 0, 3) / math.log(2.0), None)}
 
 

@@ -83,7 +83,7 @@ def test_the_binding_refuses_what_does_not_fit(hgf, monkeypatch):
     monkeypatch.setattr(hgf, "lib", lambda: library)
     monkeypatch.setattr(hgf, "_stream", lambda s: None)
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731
-    good = {"q": z(10, 256), "k": z(10, 256), "v": z(10, 128), "dout": z(10, 128), "streams": z(10, 256), "lse": z(2, 2, 2, 5, dt=torch.float32)}
+    good = {"q": z(10, 256), "k": z(10, 256), "v": z(10, 128), "dout": z(10, 128), "streams": z(10, 256, dt=torch.float32), "lse": z(2, 2, 2, 5, dt=torch.float32)}
 
     def back(want=None, **change):
         a = {**good, **{n: change.pop(n) for n in list(change) if n in good}}
