@@ -4,6 +4,7 @@
 //     dQ_s,i = c w_s sum_j T_s,ij K_s,j      dK_s,j = c w_s sum_i T_s,ij Q_s,i      dlambda = -out_scale sum_ij P_2,ij A_ij
 // The probabilities are not kept: they are formed again, P = 2^(scale_log2 q.k - lse), from the forward pass's lse (base 2).
 #include <cmath>
+#include <type_traits>
 
 #include "hgf_tc.cuh"
 #include "hgf_warp.cuh"
@@ -35,6 +36,10 @@ __device__ __forceinline__ uint32_t tb_pack_bf16(uint64_t v) {
     return tb_pack_bf16(lo, hi);
 }
 
+// What two values were rounded by.
+__device__ __forceinline__ uint32_t tb_rounded_by(uint64_t v, uint32_t near) {
+    return tb_pack_bf16(fma_f32x2(pack_f32x2(bf16lo_to_float(near), bf16hi_to_float(near)), pack_f32x2(-1.0f, -1.0f), v));
+}
 __device__ __forceinline__ void tb_load(uint32_t at, uint32_t (&v)[32]) { tmem_ld32(at, v); }
 __device__ __forceinline__ void tb_load(uint32_t at, uint32_t (&v)[16]) { tmem_ld16(at, v); }
 __device__ __forceinline__ void tb_store(uint32_t at, const uint32_t (&v)[16]) { tmem_st16(at, v); }
@@ -192,8 +197,15 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
     // The tiles of both passes in order of falling length are dealt to the CTAs in rounds, every other round backwards; a CTA works those of the
     // keys first.  (Tiles of the keys, then those of the queries in rounds of their own: 5 to 40 % more steps in the longest CTA for batches of
     // a few hundred tiles.)
-    struct Item { int r0, s0, J, b, hd, st, bh; };
+    // A sequence's first tile begins with a step of its own, `extra`: its first 64 queries or keys, with what P and T are going to be rounded by in
+    // their places.  A text's first tokens share their attention among few others, both streams alike, so that P_1 - lambda P_2 and the sums over T are
+    // small against their terms and the roundings of those show: dV of 64 tokens with heads of 128 was 1.5 times as far from 64 bits as the gradients'
+    // own rounding to bf16 puts it, of 3 tokens 1.7 (now 1.0; of 1500 tokens 1.44, now 1.37).
+    struct Item { int r0, s0, J, extra, b, hd, st, bh; };
     struct Cursor { int round; bool second; };
+    // (What the warps go by has to be in uniform registers: where an item looked as if lanes could differ in it, an MMA took 75 clocks to issue instead
+    // of 25 and the kernel a fifth longer.)
+    auto same = [](int v) { return (int)__reduce_or_sync(0xffffffffu, (unsigned)v); };
     auto next = [&](Cursor &c, Item &t) {
         if (NS == 1 && c.second) {  // (one stream at a time: the second first)
             c.second = false;
@@ -205,12 +217,13 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
             if (i >= tiles) return false;
             const int rank = (int)(i / per_rank);
             const long long of = i % per_rank;
-            if (p.both && (of < bhs) != KEYS) continue;
+            if (p.both && same(of < bhs) != (KEYS ? 1 : 0)) continue;
             const int tile = KEYS ? rank : nt - 1 - rank;
-            t.bh = (int)(of % bhs);
-            t.r0 = tile * kTbTile;
+            t.bh = same((int)(of % bhs));
+            t.r0 = same(tile) * kTbTile;
             t.s0 = KEYS ? t.r0 : 0;
-            t.J = KEYS ? n64 - t.r0 / kTbStep : min(n64, t.r0 / kTbStep + 2);
+            t.extra = t.r0 == 0;
+            t.J = same((KEYS ? n64 - t.r0 / kTbStep : min(n64, t.r0 / kTbStep + 2)) + t.extra);
             t.b = t.bh / h;
             t.hd = t.bh % h;
             t.st = NS == 2 ? 0 : 1;
@@ -310,7 +323,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                 if (!ok) break;
                 if (lane == 0) {
                     const uint32_t full = bar(C::BAR_FULL + s), dst = sbase + C::OFF_RING + s * C::ROW_BYTES;
-                    const int row = t.s0 + j * kTbStep;
+                    const int row = t.s0 + max(j - t.extra, 0) * kTbStep;
                     mbar_arrive_expect_tx(full, C::ROW_BYTES + (KEYS ? C::STAT_COPY : 0));
                     for (int blk = 0; blk < C::NBLK; ++blk) {
                         for (int a = 0; a < NS; ++a)
@@ -480,14 +493,13 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                     nd[a] = pack_f32x2(d, d);
                 }
             }
-            // what P is weighed by on its way into dV: 1 and -lambda
-            const float wp = NS == 2 || t.st == 1 ? -p.lambda : 1.0f;
-            const uint64_t wp2 = pack_f32x2(wp, wp);
-            for (int j = 0; j < t.J; ++j, ++g) {
-                const int par = g & 1, sb = C::NSB == 2 ? par : 0, ab = C::NA == 2 ? par : 0, c0 = t.s0 + j * kTbStep + COLS * part;  // the thread's first column
+            const uint64_t less = pack_f32x2(-p.lambda, -p.lambda);
+            // (a step of its own for the roundings: with a branch in it the ordinary one was a fifth slower)
+            auto step = [&](auto rest, int j) {
+                const int par = g & 1, sb = C::NSB == 2 ? par : 0, ab = C::NA == 2 ? par : 0, c0 = t.s0 + max(j - t.extra, 0) * kTbStep + COLS * part;  // the thread's first column
                 const uint32_t s_addr = lane_base + C::COL_S + sb * NS * kTbStep + COLS * part, a_addr = lane_base + C::COL_A + ab * kTbStep + COLS * part;
                 const float *delta = reinterpret_cast<const float *>(smem + C::OFF_STATS + s * C::STAT_STAGE + kTbTileBytes) + COLS * part;
-                if (!(ok = wait(C::BAR_S + sb, phase(g, C::NSB), 0xb30u))) break;
+                if (!wait(C::BAR_S + sb, phase(g, C::NSB), 0xb30u)) return false;
                 tc_fence_after();
                 uint32_t x[NS][COLS];
 #pragma unroll
@@ -517,7 +529,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                 };
                 exponentials(0);
                 // (A is asked for under the second stream's exponentials)
-                if (!(ok = wait(C::BAR_A + ab, phase(g, C::NA), 0xb32u))) break;
+                if (!wait(C::BAR_A + ab, phase(g, C::NA), 0xb32u)) return false;
                 tc_fence_after();
                 uint32_t dp[COLS];
                 tb_load(a_addr, dp);
@@ -532,32 +544,33 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                 const uint32_t o_addr = C::OVER_A ? a_addr : s_addr;
                 if constexpr (KEYS) {
                     uint32_t o[COLS / 2];
+                    auto mix = [&](int u) { return NS == 2 ? fma_f32x2(two(&x[NS - 1][u]), less, two(&x[0][u])) : two(&x[0][u]); };
 #pragma unroll
-                    for (int u = 0; u < COLS; u += 2)
-                        o[u >> 1] = tb_pack_bf16(NS == 2 ? fma_f32x2(two(&x[NS - 1][u]), wp2, two(&x[0][u])) : mul_f32x2(two(&x[0][u]), wp2));
+                    for (int u = 0; u < COLS; u += 2) o[u >> 1] = tb_pack_bf16(mix(u));
+                    if constexpr (rest.value)
+#pragma unroll
+                        for (int u = 0; u < COLS; u += 2) o[u >> 1] = tb_rounded_by(mix(u), o[u >> 1]);
                     tb_store(o_addr + COLS / 2, o);
                 }
 #pragma unroll
                 for (int a = 0; a < NS; ++a) {
                     uint32_t o[COLS / 2];
+                    auto gradient = [&](int u) {
+                        uint64_t d = two(&dp[u]);
+                        if constexpr (!KEYS) d = add_f32x2(d, nd[a]);
+                        else if (a == 1) d = add_f32x2(d, *reinterpret_cast<const uint64_t *>(delta + u));  // (D_1 is subtracted, or with one stream its own)
+                        return mul_f32x2(two(&x[a][u]), d);
+                    };
 #pragma unroll
                     for (int u = 0; u < COLS; u += 4) {
-                        uint64_t d0 = two(&dp[u]), d1 = two(&dp[u + 2]);
-                        if constexpr (KEYS) {  // (D_1 is subtracted, or with one stream its own)
-                            if (a == 1) {
-                                const ulonglong2 e = *reinterpret_cast<const ulonglong2 *>(delta + u);
-                                d0 = add_f32x2(d0, e.x);
-                                d1 = add_f32x2(d1, e.y);
-                            }
-                        } else {
-                            d0 = add_f32x2(d0, nd[a]);
-                            d1 = add_f32x2(d1, nd[a]);
-                        }
-                        const uint64_t t0 = mul_f32x2(two(&x[a][u]), d0), t1 = mul_f32x2(two(&x[a][u + 2]), d1);
+                        const uint64_t t0 = gradient(u), t1 = gradient(u + 2);
                         o[u >> 1] = tb_pack_bf16(t0);
                         o[(u >> 1) + 1] = tb_pack_bf16(t1);
-                        if (!KEYS && a == NS - 1) sum = add_f32x2(add_f32x2(t0, t1), sum);  // (of the second stream, or of the one at hand)
+                        if (!KEYS && !rest.value && a == NS - 1) sum = add_f32x2(add_f32x2(t0, t1), sum);  // (of the second stream, or of the one at hand)
                     }
+                    if constexpr (rest.value)
+#pragma unroll
+                        for (int u = 0; u < COLS; u += 2) o[u >> 1] = tb_rounded_by(gradient(u), o[u >> 1]);
                     tb_store(o_addr + a * (C::OVER_A ? COLS / 2 : kTbStep), o);
                 }
                 tmem_st_wait();
@@ -565,7 +578,11 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::BAR_P + par));
                 if (++s == C::ST) s = 0;
-            }
+                ++g;
+                return true;
+            };
+            if (t.extra) ok = step(std::true_type{}, 0);
+            for (int j = t.extra; ok && j < t.J; ++j) ok = step(std::false_type{}, j);
             if (!ok) break;
             if constexpr (!KEYS) {
                 // sum_j P_2 A = D_2 + sum_j T_2: what P_2's sum is off from 1 then weighs the small T only
@@ -581,8 +598,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
             if (!(ok = wait(C::BAR_ACC, ph, 0xb40u))) break;
             ph ^= 1u;
             tc_fence_after();
-            const bool with_v = KEYS && (NS == 2 || t.st == 0);
-            const int units = (NS + (with_v ? 1 : 0)) * DH / 32;
+            const int units = (NS + (KEYS && (NS == 2 || t.st == 0) ? 1 : 0)) * DH / 32;
             for (int unit = part; unit < units; unit += C::PARTS) {
                 const int a = unit / (DH / 32), dims = unit % (DH / 32) * 32;  // (stream a of the tile's, or V)
                 uint32_t v[32], o[16];
@@ -601,6 +617,20 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                         *reinterpret_cast<uint4 *>(dst + ((size_t)t.b * L + first + e) * pitch + dims + 8 * (lane & 3)) =
                             make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
             }
+            if constexpr (KEYS && NS == 1)
+                if (t.st == 1) {
+                    // dV is P_2^T G so far; times -lambda here and not in P, where its own rounding to bf16 would weigh every row alike (a text's first
+                    // tokens, whose probabilities are exact, were 4 times as far off as the others)
+                    for (int unit = part; unit < DH / 32; unit += C::PARTS) {
+                        uint32_t v[32];
+                        tmem_ld32(lane_base + C::COL_V + 32 * unit, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * -p.lambda);
+                        tmem_st32(lane_base + C::COL_V + 32 * unit, v);
+                    }
+                    tmem_st_wait();
+                }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(C::BAR_ACCREAD));

@@ -31,14 +31,16 @@ def reference(q, k, v, g, B, L, h, dh, lam, scale):
     dk = torch.stack([c * w[s] * T_(T[s]) @ Q[s] for s in (0, 1)])
     # D comes from O in fp32, which comes from P in two bf16 parts: half a step of the half step that the first is off by
     off = (HALF * HALF + SLACK) * (G.abs() * (P @ V.abs())).sum(-1, keepdim=True)
-    # every T is rounded to bf16; the probability has SLACK, D has `off`; what A - D is made of counts where they cancel
-    each = HALF * T.abs() + P * (off + SLACK * (A.abs() + D.abs()))
+    # every T is rounded to bf16 (up to 64 tokens: taken in two bf16 parts, half a step of half a step); the probability has SLACK, D has `off`; what
+    # A - D is made of counts where they cancel
+    near = HALF if L > 64 else HALF * HALF
+    each = near * T.abs() + P * (off + SLACK * (A.abs() + D.abs()))
     e_dq = torch.stack([c * abs(w[s]) * each[s] @ K[s].abs() for s in (0, 1)])
     e_dk = torch.stack([c * abs(w[s]) * T_(each[s]) @ Q[s].abs() for s in (0, 1)])
     size = P[0] + abs(lam) * P[1]
     # heads of 64: P_1 - lambda P_2 is rounded once; of 128, where a stream follows the other: P_1 and lambda P_2 each, half a step of |P_1| and
     # one of |lambda P_2|, and those do not cancel as the values do
-    e_dv = abs(scale) * T_(HALF * (mix.abs() if dh < 128 else size) + SLACK * size) @ G.abs()
+    e_dv = abs(scale) * T_(near * (mix.abs() if dh < 128 else size) + SLACK * size) @ G.abs()
     e_out = abs(scale) * (HALF * HALF + SLACK) * size @ V.abs()
     back2 = lambda x: x.permute(1, 3, 0, 2, 4).reshape(B * L, -1)  # noqa: E731
     back1 = lambda x: x.permute(0, 2, 1, 3).reshape(B * L, -1)  # noqa: E731
