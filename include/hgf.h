@@ -366,7 +366,8 @@ double hgf_diff_lambda0(double head_dim);
  *     dlambda = -out_scale * sum( P_2 (.) dO V^T )
  * The probabilities are formed again from q, k and lse; nothing of size L x L is kept.
  *   dout     [B*L][n_heads * head_dim]      bfloat16
- *   grads    dq, dk laid out as q, k, and dv as v, bfloat16; dlambda one fp32 value.  Null: not computed (dk and dv together; dlambda with dq only)
+ *   grads    dq, dk laid out as q, k, and dv as v, bfloat16; dlambda one fp32 value.  Null: not computed (dk and dv together; dlambda with dq only).
+ *            None may lie over an input or another one
  *   workspace  hgf_diff_attention_backward_workspace_bytes(...) bytes, 256-byte aligned; scratch, not shared by calls that may overlap on the device
  *   flags    0
  * q, k, v, lambda, out_scale, sizes and refusals as in the forward pass.  Here the forward pass takes the probabilities to 2^-16 (two bfloat16
@@ -402,8 +403,9 @@ hgf_status hgf_diff_attention_backward(const void *q, const void *k, const void 
  *              may be null and is left out
  *   positions  device int32 [n_rows], any values
  *   q_weight, k_weight  device fp32 [head_dim], shared by the heads; null = ones
- *   q_out, k_out        bfloat16, laid out as q and k; they may be q and k themselves
- * n_rows >= 1, head_dim 64 or 128, rotary_dim a multiple of 16 from 0 to head_dim, eps >= 0, base > 0, 16-byte aligned pointers.  Enqueue only.
+ *   q_out, k_out        bfloat16, laid out as q and k; they may be q and k themselves, and lie over no other input, nor each other
+ * Squares and sums over a head are fp32: a head whose sum of squares is above its range (values of 2^60 and more) gives zeros.
+ * n_rows >= 1, head_dim 64 or 128, rotary_dim a multiple of 16 from 0 to head_dim, eps >= 0, base > 0, 16-byte aligned pointers (positions: 4).  Enqueue only.
  *
  * The backward call takes the same inputs (q and k as they were before the norm) and the gradients of q_out and k_out; with g = R(p)^T dy
  *     dweight = sum over rows and heads of g (.) u        dx = ( g (.) weight - u mean(g (.) weight (.) u) ) / sqrt(mean(x^2) + eps)
@@ -434,7 +436,8 @@ hgf_status hgf_qk_norm_rotate_backward(const void *q, const void *k, int64_t n_r
  * The norm over all gradients of a training step (hgf_linear_backward, hgf_diff_attention_backward, hgf_qk_norm_rotate_backward, ...), and the
  * gradients scaled so that it stays below a limit:
  *     norm = sqrt(sum over all tensors of x^2),   y = x min(1, max_norm / (norm + 1e-6))
- * The squares are summed in 64 bits in one order on a given GPU.  An infinite norm gives the factor 0, one that is no number a factor that is none.
+ * The squares are summed in 64 bits in one order on a given GPU.  An infinite norm gives the factor 0, one that is no number a factor that is none;
+ * where max_norm is infinite the factor is 1, whatever the gradients hold.
  *
  * hgf_grad_list_create records the tensors (pointers are kept, not the data: the tensors stay owned by the caller and must stay valid) and allocates
  * the list's descriptors and workspace on the current device; it is a set-up call that synchronises.

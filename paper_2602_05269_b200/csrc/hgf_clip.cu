@@ -39,7 +39,7 @@ __device__ __forceinline__ float clip_element(const ClipPiece &c, int i) {
 }
 
 // Sums of squares in 64 bits: no magnitude of a gradient overflows or vanishes, and the order moves nothing that fp32 shows.  A sum for each of the
-// words in flight: one chain of additions for all of them was the bound (421 MB 114 us instead of SUMS_US).
+// words in flight: one chain of additions for all of them was the bound (421 MB 114 us instead of 77).
 template <bool BF16>
 __device__ __forceinline__ void piece_sums(const ClipPiece &c, int lane, double (&sum)[kClipAhead]) {
     int at = 0;
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipPiec
     sum = 0.0;
     for (int q = 0; q < kClipWarps; ++q) sum += s_sum[q];
     const double norm = sqrt(sum), ratio = (double)max_norm / (norm + 1e-6);
-    const float f = ratio >= 1.0 ? 1.0f : (float)ratio;  // (a norm that is no number gives a factor that is none)
+    const float f = ratio >= 1.0 || max_norm == INFINITY ? 1.0f : (float)ratio;  // (a norm that is no number gives a factor that is none)
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     while (i >= 0) {
         const ClipPiece now = c;

@@ -319,7 +319,7 @@ static hgf_status rotate_arguments(RotateParams &p, const void *q, const void *k
         return HGF_ERR_INVALID_ARG;
     if ((head_dim != 64 && head_dim != 128) || n_rows > 0x7fffffff || rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 16 || q_heads > (1 << 20) || k_heads > (1 << 20))
         return HGF_ERR_UNSUPPORTED_SHAPE;
-    if ((((uintptr_t)q) | ((uintptr_t)k) | ((uintptr_t)q_weight) | ((uintptr_t)k_weight) | ((uintptr_t)positions)) & 15u) return HGF_ERR_MISALIGNED;
+    if ((((uintptr_t)q) | ((uintptr_t)k) | ((uintptr_t)q_weight) | ((uintptr_t)k_weight)) & 15u || ((uintptr_t)positions & 3u)) return HGF_ERR_MISALIGNED;
     p.side[0].x = (const __nv_bfloat16 *)q;
     p.side[0].w = q_weight;
     p.side[0].heads = q ? q_heads : 0;

@@ -48,8 +48,9 @@ def test_what_the_rotation_refuses(hgf):
             assert call(**bad) == 1, bad
         for bad in ({"dh": 96}, {"rot": 8}, {"rot": 80}, {"rot": -16}, {"n": 1 << 31}):
             assert call(**bad) == 2, bad
-        for name in ("q", "k", "pos", "wq", "wk", "qo", "ko"):
+        for name in ("q", "k", "wq", "wk", "qo", "ko"):
             assert call(**{name: odd}) == 3, name
+        assert call(pos=p(4098)) == 3
     assert bwd(grads=False) == bwd(q=None, qo=None, hq=0) == bwd(k=None, ko=None) == 1
     assert bwd(dq=4100) == bwd(dk=4100) == bwd(dwq=4100) == bwd(dwk=4100) == bwd(ws=p(4096 + 64)) == 3
     need = L.hgf_qk_norm_rotate_workspace_bytes(64)
