@@ -13,7 +13,7 @@ namespace hgf {
 
 struct AttnBackParams {
     const uint8_t *stats;            // [B*h][ceil(L / 64)] blocks of kTbStatBytes, see attention_stats_kernel
-    double *dl_part;                 // [grid][warps] partial sums of P_2 (.) A
+    double *dl_part;                 // [grid] partial sums of P_2 (.) A
     unsigned int *arrivals;          // CTAs that have left theirs
     float *dlambda;                  // null: not asked for
     int B, L, h;
@@ -66,8 +66,8 @@ attention_stats_kernel(const __nv_bfloat16 *dout, const float *streams, const fl
     __shared__ float s_v[4][64];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = (L + 63) / 64;
     const long long tiles = (long long)B * h * blocks;
-    pdl_launch_dependents();
     pdl_wait();
+    pdl_launch_dependents();  // (only now: what the main kernel reads before its own wait is the call's inputs, complete when this one's wait has ended)
     if (blockIdx.x == 0 && threadIdx.x == 0) *arrivals = 0;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const long long bh = tile / blocks;
@@ -169,7 +169,9 @@ struct TbCfg {
                          BAR_P = BAR_READ + 2,         // first operands of the back products are there
                          BAR_BACK = BAR_P + 2,         // back products are complete
                          BAR_ACC = BAR_BACK + 2,       // all products of an item
-                         BAR_ACCREAD = BAR_ACC + 1, BAR_COUNT = BAR_ACCREAD + 1;
+                         BAR_ACCREAD = BAR_ACC + 1,
+                         BAR_DL = BAR_ACCREAD + 1,     // the warps' sums for dlambda
+                         BAR_COUNT = BAR_DL + 1;
     // tensor-memory columns: accumulators (dV, then dK_s or dQ_s), score buffers [buffer][stream], A buffers, resident rows
     static constexpr int COL_V = 0, COL_T = KEYS ? DH : 0, COL_S = COL_T + NS * DH, COL_A = COL_S + NSB * NS * kTbStep, COL_R = COL_A + NA * kTbStep;
     static constexpr uint32_t IDESC_F = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTbStep >> 3) << 17) | ((uint32_t)(kTbTile >> 4) << 24);
@@ -183,10 +185,29 @@ struct TbPass {
     __nv_bfloat16 *d2, *d1;
 };
 
+// One warp leaves the CTA's sum of P_2 (.) A (that of `v` over its lanes); the CTA that comes last adds them all up, in one order.
+__device__ __noinline__ void tb_leave_dlambda(double *dl_part, unsigned int *arrivals, float *dlambda, float out_scale, double v, int lane) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    unsigned int before = 0;
+    if (lane == 0) {
+        dl_part[blockIdx.x] = v;
+        __threadfence();
+        before = atomicAdd(arrivals, 1u);
+    }
+    if (__shfl_sync(0xffffffffu, before, 0) != gridDim.x - 1) return;
+    __threadfence();
+    v = 0.0;
+    for (int i = lane; i < (int)gridDim.x; i += 32) v += __ldcg(dl_part + i);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane == 0) *dlambda = (float)(-(double)out_scale * v);
+}
+
 template <int DH, bool KEYS>
-__device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map_res2, const CUtensorMap &map_res1, const CUtensorMap &map_row2, const CUtensorMap &map_row1,
-                                                          const TbPass &pass, const AttnBackParams &p, uint8_t *smem, uint32_t tmem, volatile int *abort_flag,
-                                                          unsigned int *status) {
+__device__ __forceinline__ void attention_backward_pass(const CUtensorMap &map_res2, const CUtensorMap &map_res1, const CUtensorMap &map_row2, const CUtensorMap &map_row1,
+                                                          const TbPass &pass, const AttnBackParams &p, uint8_t *smem, double *s_dl, uint32_t tmem, volatile int *abort_flag,
+                                                        unsigned int *status) {
     using C = TbCfg<DH, KEYS>;
     constexpr int NS = C::NS;
     const uint32_t sbase = smem_u32(smem), bar0 = sbase + (KEYS ? 0 : kTbBarBytes);
@@ -236,7 +257,11 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
     {
         Cursor any = {0, false};
         Item t;
-        if (!next(any, t)) return 0.0;
+        if (!next(any, t)) {
+            pdl_wait();
+            if (!KEYS && p.dlambda && warp == 1) tb_leave_dlambda(p.dl_part, p.arrivals, p.dlambda, p.out_scale, 0.0, lane);
+            return;
+        }
     }
     if (tid == 0) {
         for (int i = 0; i < C::NRES; ++i) {
@@ -259,6 +284,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
         mbar_init(bar(C::BAR_TEMPTY), C::WARPS);
         mbar_init(bar(C::BAR_ACC), 1);
         mbar_init(bar(C::BAR_ACCREAD), C::WARPS);
+        mbar_init(bar(C::BAR_DL), C::WARPS);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if constexpr (KEYS) {  // four first operands [128][16], ones where the parts of a value are and zeros elsewhere
@@ -330,8 +356,10 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                             tma_load_3d(dst + a * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row2, ((t.st + a) * h + t.hd) * DH + 64 * blk, row, t.b, full);
                         tma_load_3d(dst + NS * C::ROW_TILE + blk * C::ROW_BLOCK, &map_row1, t.hd * DH + 64 * blk, row, t.b, full);
                     }
-                    if constexpr (KEYS)
+                    if constexpr (KEYS) {
+                        if (j == 0) pdl_wait();
                         bulk_load_1d(sbase + C::OFF_STATS + s * C::STAT_STAGE, p.stats + ((size_t)t.bh * n64 + row / kTbStep) * kTbStatBytes, C::STAT_COPY, full);
+                    }
                 }
                 ++issued[s];
                 if (++s == C::ST) { s = 0; ph ^= 1u; }
@@ -405,6 +433,9 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                 if (++rb == C::NRES) { rb = 0; rph ^= 1u; }
             }
         }
+        // (this warp has nothing to do any more when the last sums are there: 2.6 us of an address' and a counter's round trips lie under the outputs)
+        if constexpr (!KEYS)
+            if (ok && p.dlambda && wait(C::BAR_DL, 0, 0xb17u)) tb_leave_dlambda(p.dl_part, p.arrivals, p.dlambda, p.out_scale, lane < C::WARPS ? s_dl[lane] : 0.0, lane);
     } else if (warp == 2) {
         // ------------------------------------------------------------------ back products
         const uint64_t row_desc = make_sw128_mn_desc(sbase + C::OFF_RING, C::ROW_BLOCK);
@@ -479,6 +510,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
         Item n;
         bool more = next(c, n);
         if (more) ok = bring();
+        if constexpr (!KEYS) pdl_wait();  // (lse and D come from the launch before)
         while (ok && more) {
             t = n;
             const int mine = t.r0 + row, w0 = t.r0 + 32 * quarter;  // the thread's key or query; the warp's first
@@ -498,7 +530,7 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
             auto step = [&](auto rest, int j) {
                 const int par = g & 1, sb = C::NSB == 2 ? par : 0, ab = C::NA == 2 ? par : 0, c0 = t.s0 + max(j - t.extra, 0) * kTbStep + COLS * part;  // the thread's first column
                 const uint32_t s_addr = lane_base + C::COL_S + sb * NS * kTbStep + COLS * part, a_addr = lane_base + C::COL_A + ab * kTbStep + COLS * part;
-                const float *delta = reinterpret_cast<const float *>(smem + C::OFF_STATS + s * C::STAT_STAGE + kTbTileBytes) + COLS * part;
+                [[maybe_unused]] const float *delta = reinterpret_cast<const float *>(smem + C::OFF_STATS + s * C::STAT_STAGE + kTbTileBytes) + COLS * part;
                 if (!wait(C::BAR_S + sb, phase(g, C::NSB), 0xb30u)) return false;
                 tc_fence_after();
                 uint32_t x[NS][COLS];
@@ -593,7 +625,18 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
                     dl += (double)a + (double)b - (part ? 0.0 : (double)d);
                 }
             }
-            if ((more = next(c, n)) && !(ok = bring())) break;
+            more = next(c, n);
+            if constexpr (!KEYS)
+                if (!more && p.dlambda) {
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) dl += __shfl_xor_sync(0xffffffffu, dl, o);
+                    if (lane == 0) {
+                        s_dl[warp - 4] = dl;
+                        mbar_arrive(bar(C::BAR_DL));
+                    }
+                }
+            if (more) ok = bring();
+            if (!ok) break;
             // ---- outputs: this warp's rows, in units of 32 columns of an accumulator (64 bytes of a row, stored by four lanes as above)
             if (!(ok = wait(C::BAR_ACC, ph, 0xb40u))) break;
             ph ^= 1u;
@@ -639,7 +682,6 @@ __device__ __forceinline__ double attention_backward_pass(const CUtensorMap &map
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    return dl;
 }
 
 // res2, res1: the resident tensors of both streams and of one, row2, row1: the streamed ones.
@@ -651,10 +693,10 @@ template <int DH>
 __global__ void __launch_bounds__(TbCfg<DH, true>::THREADS, 1)
 attention_backward_kernel(const __grid_constant__ TbMaps keys, const __grid_constant__ TbMaps queries, const TbPass of_keys, const TbPass of_queries,
                           const AttnBackParams p, unsigned int *status) {
-    constexpr int WARPS = TbCfg<DH, true>::WARPS, THREADS = TbCfg<DH, true>::THREADS;
     extern __shared__ uint8_t tb_smem_raw[];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort, s_last;
+    __shared__ int s_abort;
+    __shared__ double s_dl[TbCfg<DH, true>::WARPS];
     uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)tb_smem_raw + 1023) & ~(uintptr_t)1023);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) s_abort = 0;
@@ -671,37 +713,8 @@ attention_backward_kernel(const __grid_constant__ TbMaps keys, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    pdl_wait();
-    if (p.keys) attention_backward_pass<DH, true>(keys.res2, keys.res1, keys.row2, keys.row1, of_keys, p, smem, tmem, &s_abort, status);
-    if (p.queries) {
-        double dl = attention_backward_pass<DH, false>(queries.res2, queries.res1, queries.row2, queries.row1, of_queries, p, smem, tmem, &s_abort, status);
-        if (p.dlambda) {
-            // a sum for each warp; the CTA that comes last adds them all up, in one order
-#pragma unroll
-            for (int o = 16; o; o >>= 1) dl += __shfl_xor_sync(0xffffffffu, dl, o);
-            if (warp >= 4 && lane == 0) {
-                p.dl_part[(size_t)blockIdx.x * WARPS + warp - 4] = dl;
-                __threadfence();
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) s_last = atomicAdd(p.arrivals, 1u) == gridDim.x - 1;
-            __syncthreads();
-            if (s_last) {
-                double *s_sum = reinterpret_cast<double *>(smem + 2 * kTbBarBytes);
-                __threadfence();
-                double v = 0.0;
-                for (int i = threadIdx.x; i < (int)gridDim.x * WARPS; i += THREADS) v += __ldcg(p.dl_part + i);
-#pragma unroll
-                for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (lane == 0) s_sum[warp] = v;
-                __syncthreads();
-                if (threadIdx.x == 0) {
-                    for (int i = 1; i < THREADS / 32; ++i) v += s_sum[i];
-                    *p.dlambda = (float)(-(double)p.out_scale * v);
-                }
-            }
-        }
-    }
+    if (p.keys) attention_backward_pass<DH, true>(keys.res2, keys.res1, keys.row2, keys.row1, of_keys, p, smem, s_dl, tmem, &s_abort, status);
+    if (p.queries) attention_backward_pass<DH, false>(queries.res2, queries.res1, queries.row2, queries.row1, of_queries, p, smem, s_dl, tmem, &s_abort, status);
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512) : "memory");
 }
 
@@ -712,9 +725,9 @@ static bool make_maps(TbMaps *m, const void *res2, const void *res1, const void 
 }
 
 constexpr int kTbMaxGrid = 1024;
-// workspace: blocks of statistics, the warps' sums for dlambda, the count of CTAs that have left theirs
+// workspace: blocks of statistics, the CTAs' sums for dlambda, the count of CTAs that have left theirs
 static size_t stats_bytes(int64_t B, int64_t L, int64_t h) { return (size_t)(B * h) * (size_t)((L + 63) / 64) * kTbStatBytes; }
-constexpr size_t kTbPartBytes = (size_t)kTbMaxGrid * TbCfg<64, true>::WARPS * sizeof(double);
+constexpr size_t kTbPartBytes = (size_t)kTbMaxGrid * sizeof(double);
 
 template <int DH>
 static cudaError_t launch_backward(const void *q, const void *k, const void *v, const void *dout, const float *streams, const float *lse,
