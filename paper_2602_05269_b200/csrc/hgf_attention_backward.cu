@@ -49,7 +49,7 @@ __device__ __forceinline__ void tb_store(uint32_t at, const uint32_t (&v)[8]) { 
 // Where a lane is a key, D and lse belong to columns, and every thread would read all of them from shared memory: a wavefront a value and
 // warp (128-bit loads of one address take four), 1024 a step, half of what shared memory can do beside the products' operands.  So the
 // products subtract them: each score product takes 16 more terms, ones times a query's -lse / scale_log2 in three bf16 parts
-// (24 bits), A likewise -D: 64 of them cost less than 64 additions a lane and the loads (heads of 64, 4 x 4096 tokens: the key pass 558 -> 508 us).
+// (24 bits), A likewise -D (heads of 64, 4 x 4096 tokens: the key pass, then a launch of its own, 558 -> 508 us).
 // A block of 64 queries of a (batch element, head):
 //   [64][16] bf16, rows of 32 bytes with 32-byte swizzle: parts of -lse_1 / scale_log2 (0-2), -lse_2 / scale_log2 (3-5), -D_1 (6-8), -D_2 (9-11), 0
 //   [64] fp32 D_1 - D_2
@@ -186,6 +186,7 @@ struct TbPass {
 };
 
 // One warp leaves the CTA's sum of P_2 (.) A (that of `v` over its lanes); the CTA that comes last adds them all up, in one order.
+// (Not inlined: at both of its places it took registers from the steps, 3 x 517 tokens 40.9 us for 40.2.)
 __device__ __noinline__ void tb_leave_dlambda(double *dl_part, unsigned int *arrivals, float *dlambda, float out_scale, double v, int lane) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

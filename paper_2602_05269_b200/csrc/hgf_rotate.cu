@@ -187,13 +187,22 @@ qk_norm_rotate_kernel(const __grid_constant__ RotateParams p) {
     }
 }
 
-// The same the other way round; the first p.q_blocks blocks take Q, the others K, a warp every `warps`-th unit, kRotateBack groups
-// at a time.  What a lane turns by waits in shared memory: with it in registers two groups at a time is all that fits without spills, 91 us instead of
-// 77 at 16384 tokens of 2 x 32 heads of 64 (403 MB, 62 at the rate of a copy); three blocks an SM spill: 100.
+__device__ __forceinline__ void copy16_async(uint4 *to, const uint4 *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(LEFT) : "memory"); }
+
+// The same the other way round; the first p.q_blocks blocks take Q, the others K.  What a lane turns by waits in shared memory (in registers it leaves
+// room for two groups at a time: 91 us instead of 77 at 16384 tokens of 2 x 32 heads of 64, 403 MB), and so do the groups that are asked for: with
+// them in registers nothing was asked for while a batch was worked on, 74 us instead of 69 (62 at the rate of a copy), 300 tokens 8.6 instead of 5.5.
+// Four batches of two groups, or three, instead of two of four: 70 to 72; three blocks an SM spill: 83.
 template <int DH, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kRotateThreads, kRotateBackBlocks)
 qk_norm_rotate_backward_kernel(const __grid_constant__ RotateParams p) {
     using R = RotateLane<DH, NEIGHBOURS>;
+    extern __shared__ uint4 s_ring[];                          // [warps][2][kRotateBack][x, dy][32]
     __shared__ float s_dw[kRotateThreads / 32][DH];
     __shared__ ulonglong2 s_turn[kRotateThreads / 32][4][32];  // cosines, sines
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -203,8 +212,28 @@ qk_norm_rotate_backward_kernel(const __grid_constant__ RotateParams p) {
     const R r(p.rot, lane);
     pdl_launch_dependents();
     const RotateSide &a = p.side[of_k];
-    const int groups = (a.heads + R::HPW - 1) / R::HPW, parts = (groups + p.per_warp - 1) / p.per_warp, words = a.heads * (DH / 8);
-    const long long units = (long long)p.rows * parts;
+    const int groups = (a.heads + R::HPW - 1) / R::HPW, per_row = (groups + kRotateBack - 1) / kRotateBack, words = a.heads * (DH / 8);
+    // A warp takes its share of all batches of kRotateBack groups of a token, one after the other: one is copied to shared memory while the one
+    // before is worked on.
+    const long long batches = (long long)p.rows * per_row;
+    long long left = batches * (me + 1) / warps - batches * me / warps;
+    struct Batch { int row, grp; };
+    uint4 *ring = s_ring + warp * (2 * 2 * kRotateBack * 32) + lane;  // (a lane reads what it copied)
+    auto ask = [&](const Batch &t, int stage) {
+        const size_t at = (size_t)t.row * a.heads * DH;
+        const uint4 *x = reinterpret_cast<const uint4 *>(a.x + at), *dy = reinterpret_cast<const uint4 *>(a.dy + at);
+        uint4 *to = ring + stage * (2 * kRotateBack * 32);
+#pragma unroll
+        for (int u = 0; u < kRotateBack; ++u) {
+            const int word = min(32 * min(t.grp + u, groups - 1) + lane, words - 1);
+            copy16_async(to + 64 * u, x + word);
+            copy16_async(to + 64 * u + 32, dy + word);
+        }
+    };
+    int turned = -1, stage = 0;
+    Batch now, then = {(int)(batches * me / warps / per_row), (int)(batches * me / warps % per_row) * kRotateBack};
+    if (left > 0) ask(then, 0);
+    copies_commit();
     Eight dw = {}, w;
     {
         float f[8];
@@ -212,55 +241,50 @@ qk_norm_rotate_backward_kernel(const __grid_constant__ RotateParams p) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) w.v[k] = pack_f32x2(f[2 * k], f[2 * k + 1]);
     }
-    int turned = -1;
-    for (long long unit = me; unit < units; unit += warps) {
-        const int row = (int)(unit / parts);
-        int grp = (int)(unit - (long long)row * parts) * p.per_warp;
-        const int last = min(grp + p.per_warp, groups);
-        const size_t at = (size_t)row * a.heads * DH;
-        const uint4 *x = reinterpret_cast<const uint4 *>(a.x + at), *dy = reinterpret_cast<const uint4 *>(a.dy + at);
-        uint4 *dx = reinterpret_cast<uint4 *>(a.out + at);
-        for (; grp < last; grp += kRotateBack) {
-            uint4 rx[kRotateBack], rg[kRotateBack];
+    for (; left > 0; --left) {
+        now = then;
+        if ((then.grp += kRotateBack) >= groups) {
+            then.grp = 0;
+            ++then.row;
+        }
+        if (left > 1) ask(then, stage ^ 1);
+        copies_commit();
+        if (now.row != turned) {
+            float c[8], sn[8];
+            r.turn(p, __ldg(p.pos + now.row), lane, c, sn);
+            turned = now.row;
 #pragma unroll
-            for (int u = 0; u < kRotateBack; ++u)
-                {
-                    const int word = min(32 * min(grp + u, last - 1) + lane, words - 1);
-                    rx[u] = x[word];
-                    rg[u] = dy[word];
-                }
-            if (row != turned) {
-                float c[8], sn[8];
-                r.turn(p, __ldg(p.pos + row), lane, c, sn);
-                turned = row;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {  // (a lane reads what it wrote)
-                    s_turn[warp][k][lane] = make_ulonglong2(pack_f32x2(c[4 * k], c[4 * k + 1]), pack_f32x2(c[4 * k + 2], c[4 * k + 3]));
-                    s_turn[warp][2 + k][lane] = make_ulonglong2(pack_f32x2(-sn[4 * k], -sn[4 * k + 1]), pack_f32x2(-sn[4 * k + 2], -sn[4 * k + 3]));
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kRotateBack; ++u) {
-                const int word = grp + u < last ? 32 * (grp + u) + lane : words;  // (no branch: groups' chains of latencies run side by side)
-                Eight v = r.own(rx[u]), g = r.own(rg[u]);
-                const Eight o = r.partner(rg[u]);
-                const float n = rsqrtf(r.dot(v, v) * (1.0f / DH) + p.eps);
-                const uint64_t n2 = pack_f32x2(n, n);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const ulonglong2 cc = s_turn[warp][k >> 1][lane], ss = s_turn[warp][2 + (k >> 1)][lane];
-                    v.v[k] = mul_f32x2(v.v[k], n2);
-                    g.v[k] = fma_f32x2(g.v[k], k & 1 ? cc.y : cc.x, mul_f32x2(o.v[k], k & 1 ? ss.y : ss.x));
-                    if (word < words) dw.v[k] = fma_f32x2(g.v[k], v.v[k], dw.v[k]);
-                    g.v[k] = mul_f32x2(g.v[k], w.v[k]);
-                }
-                const float mean = r.dot(g, v) * (-1.0f / DH);
-                const uint64_t m2 = pack_f32x2(mean, mean);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) g.v[k] = mul_f32x2(fma_f32x2(v.v[k], m2, g.v[k]), n2);
-                if (word < words && a.out) dx[word] = rotate_words(g);
+            for (int k = 0; k < 2; ++k) {  // (a lane reads what it wrote)
+                s_turn[warp][k][lane] = make_ulonglong2(pack_f32x2(c[4 * k], c[4 * k + 1]), pack_f32x2(c[4 * k + 2], c[4 * k + 3]));
+                s_turn[warp][2 + k][lane] = make_ulonglong2(pack_f32x2(-sn[4 * k], -sn[4 * k + 1]), pack_f32x2(-sn[4 * k + 2], -sn[4 * k + 3]));
             }
         }
+        copies_wait<1>();
+        uint4 *dx = reinterpret_cast<uint4 *>(a.out + (size_t)now.row * a.heads * DH);
+        const uint4 *from = ring + stage * (2 * kRotateBack * 32);
+#pragma unroll
+        for (int u = 0; u < kRotateBack; ++u) {
+            const int word = now.grp + u < groups ? 32 * (now.grp + u) + lane : words;  // (no branch: groups' chains of latencies run side by side)
+            const uint4 rg = from[64 * u + 32];
+            Eight v = r.own(from[64 * u]), g = r.own(rg);
+            const Eight o = r.partner(rg);
+            const float n = rsqrtf(r.dot(v, v) * (1.0f / DH) + p.eps);
+            const uint64_t n2 = pack_f32x2(n, n);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const ulonglong2 cc = s_turn[warp][k >> 1][lane], ss = s_turn[warp][2 + (k >> 1)][lane];
+                v.v[k] = mul_f32x2(v.v[k], n2);
+                g.v[k] = fma_f32x2(g.v[k], k & 1 ? cc.y : cc.x, mul_f32x2(o.v[k], k & 1 ? ss.y : ss.x));
+                if (word < words) dw.v[k] = fma_f32x2(g.v[k], v.v[k], dw.v[k]);
+                g.v[k] = mul_f32x2(g.v[k], w.v[k]);
+            }
+            const float mean = r.dot(g, v) * (-1.0f / DH);
+            const uint64_t m2 = pack_f32x2(mean, mean);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) g.v[k] = mul_f32x2(fma_f32x2(v.v[k], m2, g.v[k]), n2);
+            if (word < words && a.out) dx[word] = rotate_words(g);
+        }
+        stage ^= 1;
     }
     if (!p.part) return;
     // the block's sum for each dim, in one order: over the heads of a warp, then over the warps
@@ -301,7 +325,7 @@ __global__ void __launch_bounds__(1024) rotate_weight_sums_kernel(const float *p
     if (lane == 0) out[(blockIdx.x % per_side) * 32 + warp] = (float)v;
 }
 
-constexpr int kRotateMaxGrid = 1024;
+constexpr int kRotateMaxGrid = 1024, kRotateRing = kRotateThreads / 32 * 2 * 2 * kRotateBack * 512;
 
 static void rotate_plan(RotateParams &p, int groups, double base, int sms) {
     for (int i = 0; i < p.rot / 2; ++i) p.turns[i] = pow(base, -2.0 * i / p.rot) / 6.283185307179586476925286766559;
@@ -393,7 +417,7 @@ extern "C" hgf_status hgf_qk_norm_rotate_backward(const void *q, const void *k, 
     // the other's stay as they are, so that its sums do
     const int hpw = 32 / (head_dim / 8), gq = (p.side[0].heads + hpw - 1) / hpw, gk = (p.side[1].heads + hpw - 1) / hpw;
     rotate_plan(p, gq + gk, base, sms);
-    auto blocks_of = [&](int groups) { return ((long long)p.rows * ((groups + p.per_warp - 1) / p.per_warp) + kRotateThreads / 32 - 1) / (kRotateThreads / 32); };
+    auto blocks_of = [&](int groups) { return ((long long)p.rows * ((groups + kRotateBack - 1) / kRotateBack) + kRotateThreads / 32 - 1) / (kRotateThreads / 32); };
     const int cap = kRotateBackBlocks * sms < kRotateMaxGrid ? kRotateBackBlocks * sms : kRotateMaxGrid;
     int q_most = (int)((long long)cap * gq / (gq + gk));
     q_most = !gq ? 0 : !gk ? cap : q_most < 1 ? 1 : q_most >= cap ? cap - 1 : q_most;
@@ -402,7 +426,10 @@ extern "C" hgf_status hgf_qk_norm_rotate_backward(const void *q, const void *k, 
     const int grid = p.q_blocks + (!of_k ? 0 : bk < cap - q_most ? (int)bk : cap - q_most);
     auto *kernel = head_dim == 64 ? (p.pairs ? qk_norm_rotate_backward_kernel<64, true> : qk_norm_rotate_backward_kernel<64, false>)
                                   : (p.pairs ? qk_norm_rotate_backward_kernel<128, true> : qk_norm_rotate_backward_kernel<128, false>);
-    kernel<<<grid, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
+    static std::atomic<unsigned long long> room[4];
+    const int which = (head_dim == 128 ? 2 : 0) + (p.pairs ? 1 : 0);
+    if (ensure_dynamic_smem(kernel, kRotateRing, room[which]) != cudaSuccess) return HGF_ERR_CUDA;
+    kernel<<<grid, kRotateThreads, kRotateRing, (cudaStream_t)stream>>>(p);
     count_launch();
     if (cudaGetLastError() != cudaSuccess) return HGF_ERR_CUDA;
     if (p.part) {
