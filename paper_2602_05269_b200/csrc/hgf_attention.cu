@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "hgf_tc.cuh"
+#include "hgf_warp.cuh"
 
 namespace hgf {
 
@@ -136,6 +137,7 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_proxy_async();
     }
+    if constexpr (SAVE) pdl_wait();  // (launched early; before tensor memory is taken, which the work in front may still ask for)
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
@@ -551,6 +553,8 @@ static cudaError_t launch_attention_tc(const AttnParams &p, cudaStream_t stream)
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;
     const unsigned items = (unsigned)(((p.L + kTaBM - 1) / kTaBM) * p.B * p.h), grid = items < (unsigned)sms ? items : (unsigned)sms;
+    // (in a stream, not captured: 61 tokens forward and backward 20.5 -> 18.9 us)
+    if (SAVE) return launch_overlapped(ta_diff_attention_kernel<DH, SAVE>, (unsigned)grid, kTaThreads, C::SMEM_BYTES, stream, mq, mk, mv, p, status);
     ta_diff_attention_kernel<DH, SAVE><<<grid, kTaThreads, C::SMEM_BYTES, stream>>>(mq, mk, mv, p, status);
     count_launch();
     return cudaGetLastError();

@@ -133,6 +133,8 @@ template <int DH, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kRotateThreads, kRotateBlocks)
 qk_norm_rotate_kernel(const __grid_constant__ RotateParams p) {
     using R = RotateLane<DH, NEIGHBOURS>;
+    pdl_wait();
+    pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
     const int gq = (p.side[0].heads + R::HPW - 1) / R::HPW, gk = (p.side[1].heads + R::HPW - 1) / R::HPW;
     const int pq = (gq + p.per_warp - 1) / p.per_warp, parts = pq + (gk + p.per_warp - 1) / p.per_warp;
@@ -210,6 +212,9 @@ qk_norm_rotate_backward_kernel(const __grid_constant__ RotateParams p) {
     const int blocks = of_k ? (int)gridDim.x - p.q_blocks : p.q_blocks, block = (int)blockIdx.x - (of_k ? p.q_blocks : 0);
     const int warps = blocks * (kRotateThreads / 32), me = block * (kRotateThreads / 32) + warp;
     const R r(p.rot, lane);
+    // what follows is the launch that adds up the sums, or anything: that starts when the work in front of this has ended
+    if (p.part) pdl_launch_dependents();
+    pdl_wait();
     pdl_launch_dependents();
     const RotateSide &a = p.side[of_k];
     const int groups = (a.heads + R::HPW - 1) / R::HPW, per_row = (groups + kRotateBack - 1) / kRotateBack, words = a.heads * (DH / 8);
@@ -380,9 +385,7 @@ extern "C" hgf_status hgf_qk_norm_rotate(const void *q, const void *k, int64_t n
     if (blocks > 0x7fffffffll) return HGF_ERR_UNSUPPORTED_SHAPE;
     auto *kernel = head_dim == 64 ? (p.pairs ? qk_norm_rotate_kernel<64, true> : qk_norm_rotate_kernel<64, false>)
                                   : (p.pairs ? qk_norm_rotate_kernel<128, true> : qk_norm_rotate_kernel<128, false>);
-    kernel<<<(unsigned)blocks, kRotateThreads, 0, (cudaStream_t)stream>>>(p);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
+    return launch_overlapped(kernel, (unsigned)blocks, kRotateThreads, 0, (cudaStream_t)stream, p) == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
 }
 
 extern "C" size_t hgf_qk_norm_rotate_workspace_bytes(int32_t head_dim) {
@@ -429,9 +432,7 @@ extern "C" hgf_status hgf_qk_norm_rotate_backward(const void *q, const void *k, 
     static std::atomic<unsigned long long> room[4];
     const int which = (head_dim == 128 ? 2 : 0) + (p.pairs ? 1 : 0);
     if (ensure_dynamic_smem(kernel, kRotateRing, room[which]) != cudaSuccess) return HGF_ERR_CUDA;
-    kernel<<<grid, kRotateThreads, kRotateRing, (cudaStream_t)stream>>>(p);
-    count_launch();
-    if (cudaGetLastError() != cudaSuccess) return HGF_ERR_CUDA;
+    if (launch_overlapped(kernel, (unsigned)grid, kRotateThreads, kRotateRing, (cudaStream_t)stream, p) != cudaSuccess) return HGF_ERR_CUDA;
     if (p.part) {
         if (launch_overlapped(rotate_weight_sums_kernel, 2u * head_dim / 32, 1024, 0, (cudaStream_t)stream, (const float *)p.part, p.q_blocks, grid, (int)head_dim, grads->dwq, grads->dwk) != cudaSuccess)
             return HGF_ERR_CUDA;
