@@ -221,3 +221,43 @@ def test_refusals_leave_the_outputs(hgf):
     torch.cuda.synchronize()
     assert all(torch.equal(kept[n], was[n]) for n in kept)
     hgf.check_status()
+
+
+@pytest.mark.parametrize("B,L,h,dh", [(1, 61, 4, 64), (2, 300, 9, 64), (1, 200, 3, 128)])
+def test_calls_close_behind_one_another(hgf, B, L, h, dh):
+    """Launches start before the work in front of them has ended: passes whose inputs, outputs and workspaces the next one writes over, none waited for
+    (once in a stream, once captured with the copies between them), give what they give one at a time."""
+    inputs = [(*attention.inputs(B, L, h, dh, 70 + n, "cuda"), *rotation(B * L, 2 * h, dh, n)) for n in range(3)]
+    a = [torch.empty_like(x) for x in inputs[0]]
+    q, k, v, g, x, y, pos, gx, gy, wx, wy = a
+    out, streams, lse = hgf.diff_attention_forward_train(q.zero_(), k.zero_(), v.zero_(), B, L, h, dh, 0.8)
+    back = hgf.diff_attention_backward(q, k, v, g.zero_(), streams, lse, B, L, h, dh, 0.8)
+    xo, yo = torch.empty_like(x), torch.empty_like(y)
+    rot = hgf.qk_norm_rotate_backward(x, y, pos.zero_(), dh, gx, gy, wx, wy)
+    clip, norm = hgf.GradList([back["dq"], back["dk"], back["dv"], back["dlambda"], rot["dwq"]]), torch.empty(1, device="cuda")
+
+    def step(n):
+        for to, new in zip(a, inputs[n]):
+            to.copy_(new)
+        hgf.qk_norm_rotate(x, y, pos, dh, wx, wy, q_out=xo, k_out=yo)
+        hgf.diff_attention_forward_train(xo, yo, v, B, L, h, dh, 0.8, out=out, streams=streams, lse=lse)
+        hgf.diff_attention_backward(xo, yo, v, g, streams, lse, B, L, h, dh, 0.8, out=back)
+        hgf.qk_norm_rotate_backward(x, y, pos, dh, back["dq"], back["dk"], wx, wy, out=rot)
+        clip.clip(1e-3, norm=norm)
+        hgf.diff_attention_forward_train(q, k, v, B, L, h, dh, 0.8, out=out, streams=streams, lse=lse)
+        return [t.clone() for t in (xo, yo, out, streams, lse, back["dq"], back["dk"], back["dv"], back["dlambda"], rot["dq"], rot["dk"], rot["dwq"], rot["dwk"], norm)]
+    alone = []
+    for n in range(3):
+        alone.append(step(n))
+        torch.cuda.synchronize()
+    got = [step(n % 3) for n in range(30)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(s, t) for n, r in enumerate(got) for s, t in zip(r, alone[n % 3]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [step(n % 3) for n in range(6)]
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(s, t) for n, r in enumerate(got) for s, t in zip(r, alone[n % 3]))
+    hgf.check_status()
