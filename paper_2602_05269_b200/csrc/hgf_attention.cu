@@ -81,7 +81,10 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // D = dO . O_s from them, and what D is off by weighs every key of a row at once: with P rounded to bf16, and O_s too, the gradients of Q and K were
 // 1.7 (rows of few keys 2.4) times as far from 64 bits as their own rounding puts them.  So P enters the second product in two bf16 parts, both in
 // the columns of the scores that they come from, and O_s stays in fp32.
-template <int DH, bool SAVE>
+// APART: V's last step of a sequence would bring the next one's rows, and 0 times a value that is not finite is no zero, so V comes by a map of three
+// dimensions, which fills rows behind a sequence with zeros.  (Not where no step reaches behind it: Q, K and V by such maps 406 us instead of 398 at
+// 4 x 4096 tokens, 16 heads of 64.  Scores of rows behind are hidden or belong to rows that are not stored.)
+template <int DH, bool SAVE, bool APART>
 __global__ void __launch_bounds__(kTaThreads, 1)
 ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                          const __grid_constant__ CUtensorMap tmap_v, const AttnParams p, unsigned int *status) {
@@ -162,7 +165,7 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                 mbar_arrive_expect_tx(full, 2 * C::Q_BYTES);
                 for (int st = 0; st < 2; ++st)
                     for (int blk = 0; blk < C::NBLK; ++blk)
-                        tma_load_3d(sbase + (2 * qb + st) * C::Q_BYTES + blk * kTaBM * 128, &tmap_q, (st * h + t.hd) * DH + 64 * blk, t.q0, t.b, full);
+                        tma_load_2d(sbase + (2 * qb + st) * C::Q_BYTES + blk * kTaBM * 128, &tmap_q, (st * h + t.hd) * DH + 64 * blk, t.tok0 + t.q0, full);
             }
             ++q_issued[qb];
             if (++qb == C::NQ) { qb = 0; qph ^= 1u; }
@@ -173,8 +176,8 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     const uint32_t dst = sbase + C::OFF_K + ks * 2 * C::K_BYTES, full = bar(C::BAR_KFULL + ks);
                     mbar_arrive_expect_tx(full, 2 * C::K_BYTES);
                     for (int blk = 0; blk < C::NBLK; ++blk) {
-                        tma_load_3d(dst + blk * KV * 128, &tmap_k, t.hd * DH + 64 * blk, j * KV, t.b, full);
-                        tma_load_3d(dst + C::K_BYTES + blk * KV * 128, &tmap_k, (h + t.hd) * DH + 64 * blk, j * KV, t.b, full);
+                        tma_load_2d(dst + blk * KV * 128, &tmap_k, t.hd * DH + 64 * blk, t.tok0 + j * KV, full);
+                        tma_load_2d(dst + C::K_BYTES + blk * KV * 128, &tmap_k, (h + t.hd) * DH + 64 * blk, t.tok0 + j * KV, full);
                     }
                 }
                 ++k_issued[ks];
@@ -184,8 +187,11 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                 if (lane == 0) {
                     const uint32_t full = bar(C::BAR_VFULL + vs);
                     mbar_arrive_expect_tx(full, C::V_BYTES);
-                    for (int blk = 0; blk < C::NBLK; ++blk)
-                        tma_load_3d(sbase + C::OFF_V + vs * C::V_BYTES + blk * C::V_BLOCK, &tmap_v, t.hd * DH + 64 * blk, j * KV, t.b, full);
+                    for (int blk = 0; blk < C::NBLK; ++blk) {
+                        const uint32_t dst = sbase + C::OFF_V + vs * C::V_BYTES + blk * C::V_BLOCK;
+                        if constexpr (APART) tma_load_3d(dst, &tmap_v, t.hd * DH + 64 * blk, j * KV, t.b, full);
+                        else tma_load_2d(dst, &tmap_v, t.hd * DH + 64 * blk, t.tok0 + j * KV, full);
+                    }
                 }
                 ++v_issued[vs];
                 if (++vs == C::VST) { vs = 0; vph ^= 1u; }
@@ -328,8 +334,10 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                 if (k0 > w0 + 31) {  // every key of the step lies after every query of the warp
 #pragma unroll
                     for (int u = 0; u < 32; ++u) pk[u] = 0u;
-                    tmem_st32(s_addr, pk);
-                    if constexpr (SAVE) tmem_st32(s_addr + KV / 2, pk);
+                    if constexpr (SAVE) {
+                        tmem_st32(s_addr, pk);
+                        tmem_st32(s_addr + KV / 2, pk);
+                    }
                 } else {
                     uint32_t v0[32], v1[32];
                     tmem_ld32(s_addr, v0);
@@ -407,9 +415,9 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                             pk[u >> 1] = pair(v0[u], v0[u + 1], l2a, nullptr);
                             pk[16 + (u >> 1)] = pair(v1[u], v1[u + 1], l2b, nullptr);
                         }
-                        tmem_st32(s_addr, pk);
                     }
                 }
+                if constexpr (!SAVE) tmem_st32(s_addr, pk);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -538,24 +546,28 @@ ta_diff_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     }
 }
 
-template <int DH, bool SAVE>
+template <int DH, bool SAVE, bool APART>
 static cudaError_t launch_attention_tc(const AttnParams &p, cudaStream_t stream) {
     using C = TaCfg<DH>;
     static std::atomic<unsigned long long> attr_done{0};
-    cudaError_t e = ensure_dynamic_smem(ta_diff_attention_kernel<DH, SAVE>, C::SMEM_BYTES, attr_done);
+    cudaError_t e = ensure_dynamic_smem(ta_diff_attention_kernel<DH, SAVE, APART>, C::SMEM_BYTES, attr_done);
     if (e != cudaSuccess) return e;
     unsigned int *status = device_status_word();
     if (!status) return cudaErrorMemoryAllocation;
     const uint64_t w = (uint64_t)p.h * DH;
     CUtensorMap mq, mk, mv;
-    if (!make_map_tokens(&mq, p.q, 2 * w, p.L, p.B, kTaBM) || !make_map_tokens(&mk, p.k, 2 * w, p.L, p.B, kTaKV) || !make_map_tokens(&mv, p.v, w, p.L, p.B, kTaKV))
+    const uint64_t rows = (uint64_t)p.B * p.L;
+    if (!make_map_2d(&mq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.q, 2 * w, rows, 4 * w, 64, kTaBM, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_2d(&mk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.k, 2 * w, rows, 4 * w, 64, kTaKV, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !(APART ? make_map_tokens(&mv, p.v, w, p.L, p.B, kTaKV)
+                  : make_map_2d(&mv, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.v, w, rows, 2 * w, 64, kTaKV, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorInvalidValue;
     const int sms = device_sm_count();
     if (!sms) return cudaErrorInvalidDevice;
     const unsigned items = (unsigned)(((p.L + kTaBM - 1) / kTaBM) * p.B * p.h), grid = items < (unsigned)sms ? items : (unsigned)sms;
     // (in a stream, not captured: 61 tokens forward and backward 20.5 -> 18.9 us)
-    if (SAVE) return launch_overlapped(ta_diff_attention_kernel<DH, SAVE>, (unsigned)grid, kTaThreads, C::SMEM_BYTES, stream, mq, mk, mv, p, status);
-    ta_diff_attention_kernel<DH, SAVE><<<grid, kTaThreads, C::SMEM_BYTES, stream>>>(mq, mk, mv, p, status);
+    if (SAVE) return launch_overlapped(ta_diff_attention_kernel<DH, SAVE, APART>, (unsigned)grid, kTaThreads, C::SMEM_BYTES, stream, mq, mk, mv, p, status);
+    ta_diff_attention_kernel<DH, SAVE, APART><<<grid, kTaThreads, C::SMEM_BYTES, stream>>>(mq, mk, mv, p, status);
     count_launch();
     return cudaGetLastError();
 }
@@ -589,8 +601,12 @@ static hgf_status attention_forward(const void *q, const void *k, const void *v,
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)head_dim));
     p.flags = flags;
     cudaStream_t s = (cudaStream_t)stream;
-    const cudaError_t e = head_dim == 64 ? (save ? launch_attention_tc<64, true>(p, s) : launch_attention_tc<64, false>(p, s))
-                                         : (save ? launch_attention_tc<128, true>(p, s) : launch_attention_tc<128, false>(p, s));
+    const bool apart = B > 1 && L % kTaKV != 0;
+    auto launch = head_dim == 64 ? (save ? (apart ? launch_attention_tc<64, true, true> : launch_attention_tc<64, true, false>)
+                                         : (apart ? launch_attention_tc<64, false, true> : launch_attention_tc<64, false, false>))
+                                 : (save ? (apart ? launch_attention_tc<128, true, true> : launch_attention_tc<128, true, false>)
+                                         : (apart ? launch_attention_tc<128, false, true> : launch_attention_tc<128, false, false>));
+    const cudaError_t e = launch(p, s);
     return e == cudaSuccess ? HGF_OK : HGF_ERR_CUDA;
 }
 

@@ -261,3 +261,24 @@ def test_calls_close_behind_one_another(hgf, B, L, h, dh):
     torch.cuda.synchronize()
     assert all(torch.equal(s, t) for n, r in enumerate(got) for s, t in zip(r, alone[n % 3]))
     hgf.check_status()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("L", [1, 64, 65, 192, 320])
+def test_sequences_at_the_ends_of_steps(hgf, L, dh):
+    """Sequences that end with a step, inside one and inside a tile only: one whose values are not finite leaves the others as they are."""
+    B, h = 3, 2
+    q, k, v, g = attention.inputs(B, L, h, dh, 80, "cuda")
+
+    def everything():
+        plain = hgf.diff_attention_forward(q, k, v, B, L, h, dh, 0.8)
+        out, streams, lse = hgf.diff_attention_forward_train(q, k, v, B, L, h, dh, 0.8)
+        b = hgf.diff_attention_backward(q, k, v, g, streams, lse, B, L, h, dh, 0.8)
+        return plain, out, streams, lse.permute(0, 3, 1, 2).reshape(B * L, -1), b["dq"], b["dk"], b["dv"]
+    clean = everything()
+    for bad in (math.nan, math.inf):
+        for x in (q, k, v, g):
+            x[L:2 * L] = bad
+        for a, b in zip(clean, everything()):
+            assert torch.equal(a[:L], b[:L]) and torch.equal(a[2 * L:], b[2 * L:]) and not b[L:2 * L].isfinite().all()
+    hgf.check_status()
